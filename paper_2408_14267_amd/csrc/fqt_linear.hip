@@ -1,0 +1,531 @@
+// Matrix product with bias, activation and residual in its epilogue, and its backward pass.
+//
+// The forward is one launch of matrix tiles (fqt_tile.hpp) whose epilogue scales, adds the bias,
+// applies the activation and adds the residual to the float32 sums: no intermediate touches memory
+// but the pre-activation, if asked for.  Contractions that are long for the number of output tiles
+// are split over workgroups; their float32 partial sums meet, in a fixed order, in a second launch
+// with the same epilogue.
+//
+// The backward is one pass over dy (and z) that writes dz = dy act'(z) in bf16 and sums dbias, then
+// the two products, which read dz and the operands as they are stored: dx = dz w reads w along n
+// (COLS), dw = dz^T x reads both operands along m.
+#include "fqt_tile.hpp"
+
+namespace fqt {
+namespace dense {
+namespace {
+
+#pragma clang fp contract(fast)
+
+using tile::Operand;
+using tile::ROWS;
+using tile::COLS;
+
+// ----------------------------------------------------------------------------- activations
+
+template <int ACT>
+__device__ __forceinline__ float activate(float z) {
+  if constexpr (ACT == FQT_ACT_RELU) return z > 0.0f ? z : (z != z ? z : 0.0f);
+  else if constexpr (ACT == FQT_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
+  else if constexpr (ACT == FQT_ACT_SILU) return z / (1.0f + expf(-z));
+  else if constexpr (ACT == FQT_ACT_HARDTANH) return z != z ? z : fminf(fmaxf(z, -1.0f), 1.0f);
+  else return z;
+}
+template <int ACT>
+__device__ __forceinline__ float slope(float z) {
+  if constexpr (ACT == FQT_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
+  else if constexpr (ACT == FQT_ACT_GELU)
+    return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
+  else if constexpr (ACT == FQT_ACT_SILU) {
+    const float t = 1.0f / (1.0f + expf(-z));
+    return t * (1.0f + z * (1.0f - t));
+  } else if constexpr (ACT == FQT_ACT_HARDTANH) return z > -1.0f && z < 1.0f ? 1.0f : 0.0f;
+  else return 1.0f;
+}
+// Calls f.template operator()<ACT>() for the runtime code (uniform over the launch).
+template <typename F>
+__device__ __forceinline__ void with_act(int act, F &&f) {
+  switch (act) {
+    case FQT_ACT_RELU: f.template operator()<FQT_ACT_RELU>(); break;
+    case FQT_ACT_GELU: f.template operator()<FQT_ACT_GELU>(); break;
+    case FQT_ACT_SILU: f.template operator()<FQT_ACT_SILU>(); break;
+    case FQT_ACT_HARDTANH: f.template operator()<FQT_ACT_HARDTANH>(); break;
+    default: f.template operator()<FQT_ACT_NONE>();
+  }
+}
+
+// ----------------------------------------------------------------------------- epilogue
+
+struct Epilogue {
+  const float *sx, *sw, *bias;
+  const void *res;
+  void *z, *y;
+  int64_t M, N, ldr, ldz, ldy;
+  int32_t y_dtype, act;
+  int32_t vec;           // rows of res, z and y start on 16 bytes
+};
+
+// Loads or stores of 8 elements whose type is known at run time (uniform).
+__device__ __forceinline__ void load8(const void *p, int64_t at, int dt, bool full, int n, float (&o)[8]) {
+  if (dt == FQT_BF16) load8f(static_cast<const bf16 *>(p) + at, full, n, o);
+  else load8f(static_cast<const float *>(p) + at, full, n, o);
+}
+__device__ __forceinline__ void store8(void *p, int64_t at, int dt, bool full, int n, const float (&v)[8]) {
+  if (dt == FQT_BF16) store8f(static_cast<bf16 *>(p) + at, full, n, v);
+  else store8f(static_cast<float *>(p) + at, full, n, v);
+}
+
+// y of 8 consecutive n (v: the sums over k).
+template <int ACT>
+__device__ __forceinline__ void finish8(const Epilogue &e, int64_t m, int64_t n, float (&v)[8]) {
+  if (m >= e.M || n >= e.N) return;
+  const int cnt = int(min(e.N - n, int64_t(8)));
+  const bool eight = cnt == 8, full = eight && e.vec;
+  float t[8];
+  if (e.sx) {
+    const float s = e.sx[m];
+    load8f(e.sw + n, eight && aligned_g(e.sw), cnt, t);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= s * t[i];
+  }
+  if (e.bias) {
+    load8f(e.bias + n, eight && aligned_g(e.bias), cnt, t);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += t[i];
+  }
+  if (e.z) store8(e.z, m * e.ldz + n, e.y_dtype, full, cnt, v);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] = activate<ACT>(v[i]);
+  if (e.res) {
+    load8(e.res, m * e.ldr + n, e.y_dtype, full, cnt, t);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] += t[i];
+  }
+  store8(e.y, m * e.ldy + n, e.y_dtype, full, cnt, v);
+}
+
+// ----------------------------------------------------------------------------- products
+
+struct Product {
+  Operand x, w;
+  int64_t M, N, K;
+  uint32_t nm, nn;       // tiles
+  uint32_t splits;
+  int64_t steps;         // contraction steps of one split
+  float *part;           // [splits][M][ldp] partial sums (splits > 1)
+  int64_t ldp;
+};
+
+template <int KIND, int LX, int LW, typename S>
+__global__ void __launch_bounds__(S::THREADS) k_product(Product p, Epilogue e) {
+  __shared__ __attribute__((aligned(16))) char lds[S::LDS];
+  const uint32_t tiles = p.nm * p.nn, split = blockIdx.x / tiles;
+  const tile::TileAt at = tile::tile_at(blockIdx.x % tiles, p.nm, p.nn);
+  const int64_t m0 = int64_t(at.m) * S::BM, n0 = int64_t(at.n) * S::BN;
+  constexpr int64_t STEP = tile::KB / tile::elem_bytes<KIND>;
+  const int64_t total = (p.K + STEP - 1) / STEP;
+  const int64_t t0 = split * p.steps, t1 = min(total, t0 + p.steps);
+  const Operand x[1] = {p.x}, w[1] = {p.w};
+  typename tile::Acc<KIND>::type acc[S::FM][S::FN];
+  tile::run_tile<KIND, LX, LW, S>(x, w, p.K, m0, n0, t0, t1, lds, acc);
+  if (p.splits > 1) {
+    float *part = p.part + split * p.M * p.ldp;
+    tile::for_rows8<KIND, S>(acc, lds, m0, n0, [&](int64_t m, int64_t n, float (&v)[8]) {
+      if (m < p.M && n < p.ldp) store8f(part + m * p.ldp + n, true, 8, v);
+    });
+  } else {
+    with_act(e.act, [&]<int ACT>() {
+      tile::for_rows8<KIND, S>(acc, lds, m0, n0, [&](int64_t m, int64_t n, float (&v)[8]) {
+        finish8<ACT>(e, m, n, v);
+      });
+    });
+  }
+}
+
+// The partial sums of a split contraction, added in order, through the epilogue.  part: rows of ldp
+// (a multiple of 8) floats.
+__global__ void __launch_bounds__(256) k_product_finish(Product p, Epilogue e) {
+  const int64_t groups = p.ldp / 8, all = p.M * groups;
+  with_act(e.act, [&]<int ACT>() {
+    for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
+      const int64_t m = i / groups, n = i % groups * 8;
+      float v[8] = {}, t[8];
+      for (uint32_t s = 0; s < p.splits; ++s) {
+        load8f(p.part + (s * p.M + m) * p.ldp + n, true, 8, t);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] += t[j];
+      }
+      finish8<ACT>(e, m, n, v);
+    }
+  });
+}
+
+// ----------------------------------------------------------------------------- operand copies
+
+// Rows of src (cols elements, stride ld) to rows of `pitch` elements, zero past cols, 8-bit codes
+// widened to bf16 (exact) where ST is one and DT is bf16.
+template <typename ST, typename DT>
+__device__ __forceinline__ DT widen(ST v);
+template <> __device__ __forceinline__ bf16 widen<bf16, bf16>(bf16 v) { return v; }
+template <> __device__ __forceinline__ int8_t widen<int8_t, int8_t>(int8_t v) { return v; }
+template <> __device__ __forceinline__ bf16 widen<int8_t, bf16>(int8_t v) { return from_f32<bf16>(float(v)); }
+template <> __device__ __forceinline__ bf16 widen<e4m3, bf16>(e4m3 v) {
+  return from_f32<bf16>(__builtin_amdgcn_cvt_f32_fp8(int(v.v), 0));
+}
+template <typename ST, typename DT>
+__global__ void __launch_bounds__(256) k_repack(const ST *src, int64_t rows, int64_t cols, int64_t ld,
+                                                DT *dst, int64_t pitch) {
+  constexpr int V = 16 / sizeof(DT);
+  const int64_t groups = pitch / V, all = rows * groups;
+  for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
+    const int64_t r = i / groups, c = i % groups * V;
+    DT o[V];
+#pragma unroll
+    for (int j = 0; j < V; ++j) o[j] = c + j < cols ? widen<ST, DT>(src[r * ld + c + j]) : DT{};
+    uint4 u;
+    __builtin_memcpy(&u, o, 16);
+    *reinterpret_cast<uint4 *>(dst + r * pitch + c) = u;
+  }
+}
+
+// ----------------------------------------------------------------------------- dz
+
+struct DzArgs {
+  const void *z, *dy;
+  const float *sx, *sw;
+  bf16 *dzx, *dzw;       // dz sw (for dx) and dz sx (for dw), rows of `pitch`; may be one array
+  float *part;           // [gridDim.y][N] partial column sums of dz, or null
+  int64_t M, N, ldz, ldy, pitch;
+  int32_t y_dtype, act, vec;
+};
+// A thread takes 8 columns over the rows blockIdx.y, + gridDim.y, ...
+__global__ void __launch_bounds__(64) k_dz(DzArgs a) {
+  const int64_t n = (int64_t(blockIdx.x) * 64 + threadIdx.x) * 8;
+  if (n >= a.pitch) return;
+  const int cnt = int(min(a.N - n, int64_t(8)));
+  const bool full = cnt == 8 && a.vec;
+  float sw[8], sum[8] = {};
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sw[i] = a.sw && i < cnt ? a.sw[n + i] : 1.0f;
+  with_act(a.act, [&]<int ACT>() {
+    for (int64_t m = blockIdx.y; m < a.M; m += gridDim.y) {
+      float d[8], z[8];
+      load8(a.dy, m * a.ldy + n, a.y_dtype, full, cnt, d);
+      if constexpr (ACT != FQT_ACT_NONE) {
+        load8(a.z, m * a.ldz + n, a.y_dtype, full, cnt, z);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] *= slope<ACT>(z[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum[i] += d[i];
+      if (a.dzx) {
+        float o[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = d[i] * sw[i];
+        store8f(a.dzx + m * a.pitch + n, true, 8, o);
+      }
+      if (a.dzw && a.dzw != a.dzx) {
+        const float s = a.sx ? a.sx[m] : 1.0f;
+        float o[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) o[i] = d[i] * s;
+        store8f(a.dzw + m * a.pitch + n, true, 8, o);
+      }
+    }
+  });
+  if (a.part && cnt > 0) store8f(a.part + int64_t(blockIdx.y) * a.N + n, false, cnt, sum);
+}
+
+// dbias[n] = sum of the partial rows: 32 columns per workgroup, 8 threads per column, fixed order.
+__global__ void __launch_bounds__(256) k_dbias(const float *part, int32_t parts, int64_t N, float *dbias) {
+  __shared__ float s[8][32];
+  const int64_t c = int64_t(blockIdx.x) * 32 + threadIdx.x % 32;
+  const int k = threadIdx.x / 32;
+  float v = 0.0f;
+  if (c < N)
+#pragma unroll 8
+    for (int p = k; p < parts; p += 8) v += part[int64_t(p) * N + c];
+  s[k][threadIdx.x % 32] = v;
+  __syncthreads();
+  if (k == 0 && c < N) {
+#pragma unroll
+    for (int j = 1; j < 8; ++j) v += s[j][threadIdx.x];
+    dbias[c] = v;
+  }
+}
+__global__ void __launch_bounds__(256) k_zero(char *p, int64_t rows, int64_t bytes, int64_t ld) {
+  for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < rows * bytes; i += int64_t(gridDim.x) * 256)
+    p[i / bytes * ld + i % bytes] = 0;
+}
+
+// ----------------------------------------------------------------------------- host side
+
+struct Sizes {
+  int64_t M, N, K;
+  int64_t ldx, ldw, ldr, ldy, ldz, lddx, lddw;
+  size_t xe;             // bytes of an operand element
+};
+int check_linear(const fqt_linear_desc *d, Sizes *s) {
+  if (!d) return FQT_E_NULL;
+  if (!(d->x_dtype == FQT_BF16 || code_type(d->x_dtype)) || !float_type(d->y_dtype) ||
+      !float_type(d->dx_dtype) || !float_type(d->dw_dtype))
+    return FQT_E_DTYPE;
+  if (d->act < FQT_ACT_NONE || d->act > FQT_ACT_HARDTANH) return FQT_E_INVAL;
+  if (d->M < 0 || d->N < 0 || d->K < 0 || d->M >= FQT_MAX_ROWS || d->N > FQT_MAX_LD || d->K > FQT_MAX_LD)
+    return FQT_E_SHAPE;
+  if (d->x_dtype == FQT_I8 && d->K > 133144) return FQT_E_SHAPE;   // 127^2 K < 2^31
+  *s = {d->M, d->N, d->K, row_stride(d->ldx, d->K), row_stride(d->ldw, d->K), row_stride(d->ldr, d->N),
+        row_stride(d->ldy, d->N), row_stride(d->ldz, d->N), row_stride(d->lddx, d->K),
+        row_stride(d->lddw, d->K), elem_size(d->x_dtype)};
+  if (!s->ldx || !s->ldw || !s->ldr || !s->ldy || !s->ldz || !s->lddx || !s->lddw) return FQT_E_SHAPE;
+  return FQT_OK;
+}
+
+int64_t round_up(int64_t v, int64_t q) { return (v + q - 1) / q * q; }
+// Whether rows of n elements, ld apart, are whole 16-byte pieces.
+bool whole_pieces(int64_t n, int64_t ld, size_t e) { return n * e % 16 == 0 && ld * e % 16 == 0; }
+
+// Tiles and splits of an M x N product over K.  v1: the largest tile that gives the chip work.
+struct Plan {
+  int shape;             // 0: 256 x 256, 1: 128 x 128, 2: 64 x 64
+  uint32_t nm, nn, splits;
+  int64_t steps;         // of one split
+};
+using Shape0 = tile::Shape<256, 256, 2, 4>;
+using Shape1 = tile::Shape<128, 128, 2, 2>;
+using Shape2 = tile::Shape<64, 64, 2, 2>;
+Plan make_plan(int64_t M, int64_t N, int64_t K, size_t e) {
+  auto tiles = [&](int64_t b) { return ((M + b - 1) / b) * ((N + b - 1) / b); };
+  Plan p{};
+  const int64_t b = tiles(256) >= 200 ? 256 : tiles(128) >= 200 ? 128 : 64;
+  p.shape = b == 256 ? 0 : b == 128 ? 1 : 2;
+  p.nm = uint32_t((M + b - 1) / b);
+  p.nn = uint32_t((N + b - 1) / b);
+  const int64_t total = (K * int64_t(e) + tile::KB - 1) / tile::KB;
+  int64_t splits = 1;
+  if (p.shape == 2) splits = std::max<int64_t>(1, std::min<int64_t>(1024 / std::max<int64_t>(1, tiles(64)), total / 8));
+  p.steps = std::max<int64_t>(1, (total + splits - 1) / splits);
+  p.splits = uint32_t(std::max<int64_t>(1, (total + p.steps - 1) / p.steps));
+  return p;
+}
+size_t part_bytes(const Plan &p, int64_t M, int64_t N) {
+  return p.splits > 1 ? align256(size_t(p.splits) * M * round_up(N, 8) * 4) : 0;
+}
+
+template <int KIND, int LX, int LW>
+int launch_product(const Plan &pl, Operand x, Operand w, int64_t M, int64_t N, int64_t K, Epilogue e,
+                   float *part, hipStream_t st) {
+  if (M == 0 || N == 0) return FQT_OK;
+  Product p{x, w, M, N, K, pl.nm, pl.nn, pl.splits, pl.steps, part, round_up(N, 8)};
+  const size_t ye = elem_size(e.y_dtype);
+  auto on16 = [&](const void *q, int64_t ld) { return !q || (aligned(q, 16) && ld * ye % 16 == 0); };
+  e.M = M;
+  e.N = N;
+  e.vec = on16(e.res, e.ldr) && on16(e.z, e.ldz) && on16(e.y, e.ldy);
+  const dim3 grid(pl.nm * pl.nn * pl.splits);
+  auto go = [&]<typename S>(S) {
+    k_product<KIND, LX, LW, S><<<grid, dim3(S::THREADS), 0, st>>>(p, e);
+  };
+  if (pl.shape == 0) go(Shape0{});
+  else if (pl.shape == 1) go(Shape1{});
+  else go(Shape2{});
+  FQT_TRY_(last_launch_status());
+  if (pl.splits > 1) {
+    const int64_t all = M * (p.ldp / 8);
+    k_product_finish<<<dim3(std::min<int64_t>((all + 255) / 256, 4096)), dim3(256), 0, st>>>(p, e);
+    return last_launch_status();
+  }
+  return FQT_OK;
+}
+
+template <typename ST, typename DT>
+int repack(const void *src, int64_t rows, int64_t cols, int64_t ld, void *dst, int64_t pitch, hipStream_t st) {
+  const int64_t all = rows * (pitch / int64_t(16 / sizeof(DT)));
+  if (all == 0) return FQT_OK;
+  k_repack<ST, DT><<<dim3(std::min<int64_t>((all + 255) / 256, 8192)), dim3(256), 0, st>>>(
+      static_cast<const ST *>(src), rows, cols, ld, static_cast<DT *>(dst), pitch);
+  return last_launch_status();
+}
+
+// Workspace of the forward: padded copies of operands whose rows are not whole 16-byte pieces, and
+// the partial sums of a split contraction.
+struct FwdWs { size_t x, w, part, total; int64_t pitch; Plan plan; bool copy_x, copy_w; };
+FwdWs fwd_ws(const Sizes &s) {
+  FwdWs f{};
+  f.pitch = round_up(s.K, 16 / s.xe);
+  f.copy_x = !whole_pieces(s.K, s.ldx, s.xe);
+  f.copy_w = !whole_pieces(s.K, s.ldw, s.xe);
+  f.plan = make_plan(s.M, s.N, s.K, s.xe);
+  f.x = 0;
+  f.w = f.x + (f.copy_x ? align256(s.M * f.pitch * s.xe) : 0);
+  f.part = f.w + (f.copy_w ? align256(s.N * f.pitch * s.xe) : 0);
+  f.total = f.part + part_bytes(f.plan, s.M, s.N);
+  return f;
+}
+
+// Workspace of the backward: dz in bf16 (twice for scaled operands), bf16 copies of operands that
+// are codes or whose rows are not whole pieces, the partial sums of dbias, and those of the products
+// (which run one after the other).
+struct BwdWs { size_t dzx, dzw, x, w, bias, part, total; int64_t dz_pitch, pitch, rows; Plan dx, dw; bool copy_x, copy_w; };
+BwdWs bwd_ws(const Sizes &s) {
+  BwdWs f{};
+  const bool codes = s.xe == 1;
+  f.dz_pitch = round_up(s.N, 8);
+  f.pitch = round_up(s.K, 8);
+  f.copy_x = codes || !whole_pieces(s.K, s.ldx, 2);
+  f.copy_w = codes || !whole_pieces(s.K, s.ldw, 2);
+  f.rows = std::max<int64_t>(1, std::min<int64_t>(s.M, 256));
+  f.dx = make_plan(s.M, s.K, s.N, 2);
+  f.dw = make_plan(s.N, s.K, s.M, 2);
+  const size_t dz = align256(size_t(s.M) * f.dz_pitch * 2);
+  f.dzx = 0;
+  f.dzw = codes ? dz : 0;
+  f.x = f.dzw + dz;
+  f.w = f.x + (f.copy_x ? align256(size_t(s.M) * f.pitch * 2) : 0);
+  f.bias = f.w + (f.copy_w ? align256(size_t(s.N) * f.pitch * 2) : 0);
+  f.part = f.bias + align256(size_t(f.rows) * s.N * 4);
+  f.total = f.part + std::max(part_bytes(f.dx, s.M, s.K), part_bytes(f.dw, s.N, s.K));
+  return f;
+}
+
+int zero_matrix(void *p, int64_t rows, int64_t cols, int64_t ld, size_t e, hipStream_t st) {
+  if (rows == 0 || cols == 0) return FQT_OK;
+  k_zero<<<dim3(std::min<int64_t>((rows * cols * int64_t(e) + 255) / 256, 4096)), dim3(256), 0, st>>>(
+      static_cast<char *>(p), rows, cols * e, ld * e);
+  return last_launch_status();
+}
+
+}  // namespace
+}  // namespace dense
+}  // namespace fqt
+
+using namespace fqt;
+using namespace fqt::dense;
+
+extern "C" int fqt_linear_workspace_size(const fqt_linear_desc *d, int32_t backward, size_t *bytes) {
+  Sizes s;
+  FQT_TRY_(check_linear(d, &s));
+  if (!bytes) return FQT_E_NULL;
+  *bytes = std::max<size_t>(256, backward ? bwd_ws(s).total : fwd_ws(s).total);
+  return FQT_OK;
+}
+
+extern "C" int fqt_linear_forward(const fqt_linear_desc *d, const void *x, const void *w,
+                                  const float *x_scale, const float *w_scale, const float *bias,
+                                  const void *residual, void *z, void *y, void *ws, size_t ws_bytes,
+                                  void *hip_stream) {
+  Sizes s;
+  FQT_TRY_(check_linear(d, &s));
+  const bool codes = code_type(d->x_dtype);
+  if (!codes && (x_scale || w_scale)) return FQT_E_DTYPE;
+  if (s.M == 0 || s.N == 0) return FQT_OK;
+  if (!y || !ws || (s.K && (!x || !w)) || (codes && (!x_scale || !w_scale))) return FQT_E_NULL;
+  if (!aligned(x, 16) || !aligned(w, 16) || !aligned(x_scale, 4) || !aligned(w_scale, 4) ||
+      !aligned(bias, 4) || !elem_aligned(residual, d->y_dtype) || !elem_aligned(z, d->y_dtype) ||
+      !elem_aligned(y, d->y_dtype) || !aligned(ws, 256))
+    return FQT_E_ALIGN;
+  const FwdWs f = fwd_ws(s);
+  if (ws_bytes < f.total) return FQT_E_WORKSPACE;
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  char *base = static_cast<char *>(ws);
+  auto operand = [&](const void *p, bool copy, size_t at, int64_t rows, int64_t ld, Operand *o) -> int {
+    const int64_t e = int64_t(s.xe);
+    if (!copy) {
+      *o = {static_cast<const char *>(p), ld * e, rows};
+      return FQT_OK;
+    }
+    *o = {base + at, f.pitch * e, rows};
+    return codes ? repack<int8_t, int8_t>(p, rows, s.K, ld, base + at, f.pitch, st)
+                 : repack<bf16, bf16>(p, rows, s.K, ld, base + at, f.pitch, st);
+  };
+  Operand xo, wo;
+  FQT_TRY_(operand(x, f.copy_x, f.x, s.M, s.ldx, &xo));
+  FQT_TRY_(operand(w, f.copy_w, f.w, s.N, s.ldw, &wo));
+  const int64_t K = f.copy_x || f.copy_w ? f.pitch : s.K;
+  Epilogue e{x_scale, w_scale, bias, residual, z, y, 0, 0, s.ldr, s.ldz, s.ldy, d->y_dtype, d->act, 0};
+  float *part = reinterpret_cast<float *>(base + f.part);
+  if (d->x_dtype == FQT_BF16)
+    return launch_product<tile::BF16K, ROWS, ROWS>(f.plan, xo, wo, s.M, s.N, K, e, part, st);
+  if (d->x_dtype == FQT_I8)
+    return launch_product<tile::I8K, ROWS, ROWS>(f.plan, xo, wo, s.M, s.N, K, e, part, st);
+  return launch_product<tile::E4M3K, ROWS, ROWS>(f.plan, xo, wo, s.M, s.N, K, e, part, st);
+}
+
+extern "C" int fqt_linear_backward(const fqt_linear_desc *d, const void *x, const void *w,
+                                   const float *x_scale, const float *w_scale, const void *z,
+                                   const void *dy, void *dx, void *dw, float *dbias, void *ws,
+                                   size_t ws_bytes, void *hip_stream) {
+  Sizes s;
+  FQT_TRY_(check_linear(d, &s));
+  const bool codes = code_type(d->x_dtype);
+  if (!codes && (x_scale || w_scale)) return FQT_E_DTYPE;
+  if (!dx && !dw && !dbias) return FQT_OK;
+  const bool any = s.M && s.N;
+  if (!ws || (any && !dy) || (any && d->act != FQT_ACT_NONE && !z) || (dx && any && s.K && !w) ||
+      (dw && any && s.K && !x) || (codes && any && ((dw && !x_scale) || (dx && !w_scale))))
+    return FQT_E_NULL;
+  if (!aligned(x, 16) || !aligned(w, 16) || !aligned(x_scale, 4) || !aligned(w_scale, 4) ||
+      !elem_aligned(z, d->y_dtype) || !elem_aligned(dy, d->y_dtype) || !elem_aligned(dx, d->dx_dtype) ||
+      !elem_aligned(dw, d->dw_dtype) || !aligned(dbias, 4) || !aligned(ws, 256))
+    return FQT_E_ALIGN;
+  const BwdWs f = bwd_ws(s);
+  if (ws_bytes < f.total) return FQT_E_WORKSPACE;
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (!any) {            // sums over nothing
+    if (dx) FQT_TRY_(zero_matrix(dx, s.M, s.K, s.lddx, elem_size(d->dx_dtype), st));
+    if (dw) FQT_TRY_(zero_matrix(dw, s.N, s.K, s.lddw, elem_size(d->dw_dtype), st));
+    if (dbias) FQT_TRY_(zero_matrix(dbias, 1, s.N, s.N, 4, st));
+    return FQT_OK;
+  }
+  char *base = static_cast<char *>(ws);
+  // dy is dz itself where nothing changes it.
+  const bool same = d->act == FQT_ACT_NONE && d->y_dtype == FQT_BF16 && !codes &&
+                    whole_pieces(s.N, s.ldy, 2) && aligned(dy, 16);
+  Operand dzx{base + f.dzx, f.dz_pitch * 2, s.M}, dzw{base + f.dzw, f.dz_pitch * 2, s.M};
+  if (same) dzx = dzw = {static_cast<const char *>(dy), s.ldy * 2, s.M};
+  if (!same || dbias) {
+    DzArgs a{};
+    a.z = z; a.dy = dy;
+    a.sx = x_scale; a.sw = w_scale;
+    if (!same && dx) a.dzx = reinterpret_cast<bf16 *>(base + f.dzx);
+    if (!same && dw) a.dzw = reinterpret_cast<bf16 *>(base + f.dzw);
+    a.part = dbias ? reinterpret_cast<float *>(base + f.bias) : nullptr;
+    a.M = s.M; a.N = s.N; a.ldz = s.ldz; a.ldy = s.ldy; a.pitch = f.dz_pitch;
+    a.y_dtype = d->y_dtype; a.act = d->act;
+    const size_t ye = elem_size(d->y_dtype);
+    a.vec = aligned(dy, 16) && s.ldy * ye % 16 == 0 && (!z || (aligned(z, 16) && s.ldz * ye % 16 == 0));
+    k_dz<<<dim3((f.dz_pitch + 511) / 512, f.rows), dim3(64), 0, st>>>(a);
+    FQT_TRY_(last_launch_status());
+    if (dbias) {
+      k_dbias<<<dim3((s.N + 31) / 32), dim3(256), 0, st>>>(a.part, int32_t(f.rows), s.N, dbias);
+      FQT_TRY_(last_launch_status());
+    }
+  }
+  if (s.K == 0) return FQT_OK;
+  auto operand = [&](const void *p, bool copy, size_t at, int64_t rows, int64_t ld, Operand *o) -> int {
+    if (!copy) {
+      *o = {static_cast<const char *>(p), ld * 2, s.K};
+      return FQT_OK;
+    }
+    *o = {base + at, f.pitch * 2, f.pitch};
+    if (d->x_dtype == FQT_I8) return repack<int8_t, bf16>(p, rows, s.K, ld, base + at, f.pitch, st);
+    if (d->x_dtype == FQT_E4M3) return repack<e4m3, bf16>(p, rows, s.K, ld, base + at, f.pitch, st);
+    return repack<bf16, bf16>(p, rows, s.K, ld, base + at, f.pitch, st);
+  };
+  float *part = reinterpret_cast<float *>(base + f.part);
+  if (dx) {
+    Operand wo;
+    FQT_TRY_(operand(w, f.copy_w, f.w, s.N, s.ldw, &wo));
+    Epilogue e{nullptr, nullptr, nullptr, nullptr, nullptr, dx, 0, 0, 0, 0, s.lddx, d->dx_dtype, FQT_ACT_NONE, 0};
+    // dz rows are pitch long in the workspace (zeros past N): the contraction may end on a whole piece
+    FQT_TRY_((launch_product<tile::BF16K, ROWS, COLS>(f.dx, dzx, wo, s.M, s.K, s.N, e, part, st)));
+  }
+  if (dw) {
+    Operand xo;
+    FQT_TRY_(operand(x, f.copy_x, f.x, s.M, s.ldx, &xo));
+    Epilogue e{nullptr, nullptr, nullptr, nullptr, nullptr, dw, 0, 0, 0, 0, s.lddw, d->dw_dtype, FQT_ACT_NONE, 0};
+    dzw.rows = same ? s.N : f.dz_pitch;
+    FQT_TRY_((launch_product<tile::BF16K, COLS, COLS>(f.dw, dzw, xo, s.N, s.K, s.M, e, part, st)));
+  }
+  return FQT_OK;
+}

@@ -1,0 +1,572 @@
+// RMS norm of a residual sum with 8-bit output, its backward pass, and the row quantiser.
+//
+// The forward reads each row once: the row stays in registers while the sum of its squares and the
+// maximum of |h g| are reduced together (|y| = rstd |h g|, so the scale needs no second sweep).
+// The backward keeps h and dy of a row in registers for its one reduction, and each thread adds
+// dy t of its own columns over all rows of its workgroup, so that dg costs one partial row per
+// workgroup.  Both are bound by memory traffic.
+#include "fqt_dense.hpp"
+
+namespace fqt {
+namespace dense {
+namespace {
+
+#pragma clang fp contract(fast)
+
+struct NormArgs {
+  const void *x, *r;
+  const float *g;
+  void *h, *y;
+  uint8_t *q;
+  float *scale, *rstd;
+  int64_t rows;
+  int32_t cols;
+  int64_t ldx, ldr, ldh, ldy, ldq;
+  int32_t q_dtype;
+  float eps;
+  int32_t norm;        // 0: the row quantiser (y = x)
+  int32_t vec;         // every row of every tensor starts on 16 bytes (codes on 8)
+};
+
+__device__ __forceinline__ float wave_sum(float v) {
+  v += lane_xor_f<1>(v);
+  v += lane_xor_f<2>(v);
+  v += lane_xor_f<4>(v);
+  v += lane_xor_f<8>(v);
+  v += lane_xor_f<16>(v);
+  return v + lane_xor_f<32>(v);
+}
+__device__ __forceinline__ uint32_t wave_umax(uint32_t v) {
+  v = max(v, lane_xor<1>(v));
+  v = max(v, lane_xor<2>(v));
+  v = max(v, lane_xor<4>(v));
+  v = max(v, lane_xor<8>(v));
+  v = max(v, lane_xor<16>(v));
+  return max(v, lane_xor<32>(v));
+}
+// The bits of |v|: their unsigned order is the order of the values, with NaN on top.
+__device__ __forceinline__ uint32_t abs_bits(float v) { return __float_as_uint(v) & 0x7FFFFFFFu; }
+
+// Sum and maximum over the TPR threads of a row.  One barrier: the slots alternate between two
+// halves, and a wave can be at most one row ahead of the others.
+template <int TPR>
+__device__ __forceinline__ void reduce_row(float &ss, uint32_t &mx, float2 (*slots)[16], int &half) {
+  ss = wave_sum(ss);
+  mx = wave_umax(mx);
+  if constexpr (TPR > 64) {
+    constexpr int WAVES = TPR / 64;
+    if ((threadIdx.x & 63) == 0) slots[half][threadIdx.x >> 6] = make_float2(ss, __uint_as_float(mx));
+    __syncthreads();
+    ss = 0.0f;
+    mx = 0u;
+#pragma unroll
+    for (int w = 0; w < WAVES; ++w) {
+      const float2 o = slots[half][w];
+      ss += o.x;
+      mx = max(mx, __float_as_uint(o.y));
+    }
+    half ^= 1;
+  }
+}
+
+// What a row's codes are multiplied by: T / max, in two factors so that a maximum near the smallest
+// float32 values does not overflow it.
+struct CodeScale { float pre, inv; };
+__device__ __forceinline__ CodeScale code_scale(uint32_t mx, float top) {
+  const float m = __uint_as_float(mx);
+  CodeScale c;
+  c.pre = m < 1e-30f ? 0x1p100f : 1.0f;
+  c.inv = mx ? top / (m * c.pre) : 0.0f;
+  return c;
+}
+
+__device__ __forceinline__ void store_codes(uint8_t *q, int q_dtype, bool full, int n, const float (&v)[8]) {
+  uint32_t a, b;
+  if (q_dtype == FQT_I8) {
+    a = codes4<FQT_I8>(v[0], v[1], v[2], v[3]);
+    b = codes4<FQT_I8>(v[4], v[5], v[6], v[7]);
+  } else {
+    a = codes4<FQT_E4M3>(v[0], v[1], v[2], v[3]);
+    b = codes4<FQT_E4M3>(v[4], v[5], v[6], v[7]);
+  }
+  if (full) {
+    *reinterpret_cast<uint2 *>(q) = make_uint2(a, b);
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < n) q[i] = uint8_t((i < 4 ? a : b) >> (8 * (i & 3)));
+  }
+}
+
+// One row per TPR threads, VPT groups of 8 columns per thread.  Workgroups walk the rows with g in
+// registers.
+template <typename XT, typename YT, int TPR, int VPT>
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_norm_fwd(NormArgs a) {
+  constexpr int ROWS = TPR < 256 ? 256 / TPR : 1;
+  __shared__ float2 slots[2][16];
+  const int t = threadIdx.x % TPR;
+  int half = 0;
+  float g[VPT][8];
+#pragma unroll
+  for (int v = 0; v < VPT; ++v) {
+    const int c = (v * TPR + t) * 8, n = a.cols - c;
+    if (a.g) {
+      load8f(a.g + c, n >= 8 && aligned_g(a.g), n, g[v]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) g[v][i] = 1.0f;
+    }
+  }
+  for (int64_t row = int64_t(blockIdx.x) * ROWS + threadIdx.x / TPR; row < a.rows;
+       row += int64_t(gridDim.x) * ROWS) {
+    const XT *x = static_cast<const XT *>(a.x) + row * a.ldx;
+    const XT *r = static_cast<const XT *>(a.r) + row * a.ldr;
+    float h[VPT][8];
+#pragma unroll
+    for (int v = 0; v < VPT; ++v) {
+      const int c = (v * TPR + t) * 8, n = a.cols - c;
+      load8f(x + c, a.vec && n >= 8, n, h[v]);
+    }
+    if (a.r) {
+#pragma unroll
+      for (int v = 0; v < VPT; ++v) {
+        const int c = (v * TPR + t) * 8, n = a.cols - c;
+        float u[8];
+        load8f(r + c, a.vec && n >= 8, n, u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[v][i] += u[i];
+      }
+    }
+    float ss = 0.0f;
+    uint32_t mx = 0;
+#pragma unroll
+    for (int v = 0; v < VPT; ++v)
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        ss = fmaf(h[v][i], h[v][i], ss);
+        mx = max(mx, abs_bits(h[v][i] * g[v][i]));
+      }
+    reduce_row<TPR>(ss, mx, slots, half);
+    const float rstd = a.norm ? 1.0f / sqrtf(ss / float(a.cols) + a.eps) : 1.0f;
+    if (t == 0) {
+      if (a.rstd) a.rstd[row] = rstd;
+      if (a.scale) a.scale[row] = rstd * __uint_as_float(mx) / code_top(a.q_dtype);
+    }
+    const CodeScale cs = code_scale(mx, code_top(a.q_dtype));
+#pragma unroll
+    for (int v = 0; v < VPT; ++v) {
+      const int c = (v * TPR + t) * 8, n = a.cols - c;
+      if (n <= 0) continue;
+      const bool full = a.vec && n >= 8;
+      if (a.h) store8f(static_cast<XT *>(a.h) + row * a.ldh + c, full, n, h[v]);
+      if (a.q) {
+        float u[8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = h[v][i] * g[v][i] * cs.pre * cs.inv;
+        store_codes(a.q + row * a.ldq + c, a.q_dtype, full, n, u);
+      }
+      if (a.y) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[v][i] = h[v][i] * rstd * g[v][i];
+        store8f(static_cast<YT *>(a.y) + row * a.ldy + c, full, n, h[v]);
+      }
+    }
+  }
+}
+
+// Rows too long for registers: a workgroup per row reads it twice (statistics, then outputs; the
+// second sweep comes from L2 up to some megabytes).  An element is read again before its own place
+// in h is written, so h may be x or the residual here too.
+constexpr int LONG_TPR = 1024;
+template <typename XT, typename YT>
+__global__ void __launch_bounds__(LONG_TPR) k_norm_fwd_long(NormArgs a) {
+  __shared__ float2 slots[2][16];
+  int half = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const XT *x = static_cast<const XT *>(a.x) + row * a.ldx;
+    const XT *r = static_cast<const XT *>(a.r) + row * a.ldr;
+    auto load_h = [&](int c, int n, bool full, float (&h)[8], float (&g)[8]) {
+      load8f(x + c, full, n, h);
+      if (a.r) {
+        float u[8];
+        load8f(r + c, full, n, u);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) h[i] += u[i];
+      }
+      if (a.g) {
+        load8f(a.g + c, n >= 8 && aligned_g(a.g), n, g);
+      } else {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) g[i] = 1.0f;
+      }
+    };
+    float ss = 0.0f;
+    uint32_t mx = 0;
+    for (int c = threadIdx.x * 8; c < a.cols; c += LONG_TPR * 8) {
+      float h[8], g[8];
+      load_h(c, a.cols - c, a.vec && a.cols - c >= 8, h, g);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        ss = fmaf(h[i], h[i], ss);
+        mx = max(mx, abs_bits(h[i] * g[i]));
+      }
+    }
+    reduce_row<LONG_TPR>(ss, mx, slots, half);
+    const float rstd = a.norm ? 1.0f / sqrtf(ss / float(a.cols) + a.eps) : 1.0f;
+    if (threadIdx.x == 0) {
+      if (a.rstd) a.rstd[row] = rstd;
+      if (a.scale) a.scale[row] = rstd * __uint_as_float(mx) / code_top(a.q_dtype);
+    }
+    const CodeScale cs = code_scale(mx, code_top(a.q_dtype));
+    for (int c = threadIdx.x * 8; c < a.cols; c += LONG_TPR * 8) {
+      const int n = a.cols - c;
+      const bool full = a.vec && n >= 8;
+      float h[8], g[8], u[8];
+      load_h(c, n, full, h, g);
+      if (a.h) store8f(static_cast<XT *>(a.h) + row * a.ldh + c, full, n, h);
+      if (a.q) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = h[i] * g[i] * cs.pre * cs.inv;
+        store_codes(a.q + row * a.ldq + c, a.q_dtype, full, n, u);
+      }
+      if (a.y) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) u[i] = h[i] * rstd * g[i];
+        store8f(static_cast<YT *>(a.y) + row * a.ldy + c, full, n, u);
+      }
+    }
+  }
+}
+
+// ----------------------------------------------------------------------------- backward
+
+struct NormBwdArgs {
+  const void *h, *dy, *dres;
+  const float *g, *rstd;
+  void *dx;
+  float *part;         // [workgroups][cols] partial sums of dg
+  int64_t rows;
+  int32_t cols;
+  int64_t ldh, ldy, ldr, ldx;
+  int32_t vec;
+};
+
+template <typename XT, typename YT, int TPR, int VPT>
+__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_norm_bwd(NormBwdArgs a) {
+  constexpr int ROWS = TPR < 256 ? 256 / TPR : 1;
+  __shared__ float2 slots[2][16];
+  __shared__ float merge[ROWS > 1 ? ROWS - 1 : 1][ROWS > 1 ? TPR * VPT * 8 : 1];
+  const int t = threadIdx.x % TPR;
+  int half = 0;
+  float dg[VPT][8] = {};
+  for (int64_t row = int64_t(blockIdx.x) * ROWS + threadIdx.x / TPR; row < a.rows;
+       row += int64_t(gridDim.x) * ROWS) {
+    const XT *hp = static_cast<const XT *>(a.h) + row * a.ldh;
+    const YT *dyp = static_cast<const YT *>(a.dy) + row * a.ldy;
+    const XT *rp = static_cast<const XT *>(a.dres) + row * a.ldr;
+    const float rstd = a.rstd[row];
+    float h[VPT][8], u[VPT][8];
+    float dot = 0.0f;
+#pragma unroll
+    for (int v = 0; v < VPT; ++v) {
+      const int c = (v * TPR + t) * 8, n = a.cols - c;
+      load8f(hp + c, a.vec && n >= 8, n, h[v]);
+      load8f(dyp + c, a.vec && n >= 8, n, u[v]);
+    }
+#pragma unroll
+    for (int v = 0; v < VPT; ++v) {
+      const int c = (v * TPR + t) * 8, n = a.cols - c;
+      float g[8];
+      load8f(a.g + c, n >= 8 && aligned_g(a.g), n, g);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        h[v][i] *= rstd;                                    // t
+        dg[v][i] = fmaf(u[v][i], h[v][i], dg[v][i]);
+        u[v][i] *= g[i];
+        dot = fmaf(u[v][i], h[v][i], dot);
+      }
+    }
+    uint32_t none = 0;
+    reduce_row<TPR>(dot, none, slots, half);
+    const float m = dot / float(a.cols);
+#pragma unroll
+    for (int v = 0; v < VPT; ++v) {
+      const int c = (v * TPR + t) * 8, n = a.cols - c;
+      if (n <= 0) continue;
+      const bool full = a.vec && n >= 8;
+      float d[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i) d[i] = rstd * (u[v][i] - h[v][i] * m);
+      if (a.dres) {
+        float e[8];
+        load8f(rp + c, full, n, e);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] += e[i];
+      }
+      store8f(static_cast<XT *>(a.dx) + row * a.ldx + c, full, n, d);
+    }
+  }
+  if constexpr (ROWS > 1) {            // the rows' waves meet in LDS
+    const int w = threadIdx.x / TPR;
+    if (w > 0)
+#pragma unroll
+      for (int v = 0; v < VPT; ++v)
+#pragma unroll
+        for (int i = 0; i < 8; ++i) merge[w - 1][(v * 8 + i) * TPR + t] = dg[v][i];
+    __syncthreads();
+    if (w > 0) return;
+#pragma unroll
+    for (int v = 0; v < VPT; ++v)
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+#pragma unroll
+        for (int k = 0; k < ROWS - 1; ++k) dg[v][i] += merge[k][(v * 8 + i) * TPR + t];
+  }
+  float *out = a.part + int64_t(blockIdx.x) * a.cols;
+#pragma unroll
+  for (int v = 0; v < VPT; ++v) {
+    const int c = (v * TPR + t) * 8, n = a.cols - c;
+    if (n > 0) store8f(out + c, n >= 8 && (a.cols & 3) == 0, n, dg[v]);
+  }
+}
+
+// dx of rows too long for registers: h and dy are read twice.
+template <typename XT, typename YT>
+__global__ void __launch_bounds__(LONG_TPR) k_norm_bwd_long(NormBwdArgs a) {
+  __shared__ float2 slots[2][16];
+  int half = 0;
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const XT *hp = static_cast<const XT *>(a.h) + row * a.ldh;
+    const YT *dyp = static_cast<const YT *>(a.dy) + row * a.ldy;
+    const XT *rp = static_cast<const XT *>(a.dres) + row * a.ldr;
+    const float rstd = a.rstd[row];
+    float dot = 0.0f;
+    auto load = [&](int c, int n, bool full, float (&t)[8], float (&u)[8]) {
+      float g[8];
+      load8f(hp + c, full, n, t);
+      load8f(dyp + c, full, n, u);
+      load8f(a.g + c, n >= 8 && aligned_g(a.g), n, g);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) t[i] *= rstd, u[i] *= g[i];
+    };
+    for (int c = threadIdx.x * 8; c < a.cols; c += LONG_TPR * 8) {
+      float t[8], u[8];
+      load(c, a.cols - c, a.vec && a.cols - c >= 8, t, u);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) dot = fmaf(u[i], t[i], dot);
+    }
+    uint32_t none = 0;
+    reduce_row<LONG_TPR>(dot, none, slots, half);
+    const float m = dot / float(a.cols);
+    for (int c = threadIdx.x * 8; c < a.cols; c += LONG_TPR * 8) {
+      const int n = a.cols - c;
+      const bool full = a.vec && n >= 8;
+      float t[8], u[8], d[8];
+      load(c, n, full, t, u);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) d[i] = rstd * (u[i] - t[i] * m);
+      if (a.dres) {
+        load8f(rp + c, full, n, t);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] += t[i];
+      }
+      store8f(static_cast<XT *>(a.dx) + row * a.ldx + c, full, n, d);
+    }
+  }
+}
+// Partial sums of dg of those rows: a thread per 8 columns, gridDim.y row groups.
+template <typename XT, typename YT>
+__global__ void __launch_bounds__(64) k_norm_dg_long(NormBwdArgs a) {
+  const int c = (blockIdx.x * 64 + threadIdx.x) * 8, n = a.cols - c;
+  if (n <= 0) return;
+  const bool full = a.vec && n >= 8;
+  float dg[8] = {};
+  for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
+    float h[8], u[8];
+    load8f(static_cast<const XT *>(a.h) + row * a.ldh + c, full, n, h);
+    load8f(static_cast<const YT *>(a.dy) + row * a.ldy + c, full, n, u);
+    const float rstd = a.rstd[row];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) dg[i] = fmaf(u[i], h[i] * rstd, dg[i]);
+  }
+  store8f(a.part + int64_t(blockIdx.y) * a.cols + c, n >= 8 && (a.cols & 3) == 0, n, dg);
+}
+
+// dg[c] = sum of the partial rows: 32 columns per workgroup, 8 threads per column, in a fixed order.
+__global__ void __launch_bounds__(256) k_norm_dg(const float *part, int32_t parts, int32_t cols, float *dg) {
+  __shared__ float s[8][32];
+  const int c = blockIdx.x * 32 + threadIdx.x % 32, k = threadIdx.x / 32;
+  float v = 0.0f;
+  if (c < cols)
+#pragma unroll 8
+    for (int p = k; p < parts; p += 8) v += part[int64_t(p) * cols + c];
+  s[k][threadIdx.x % 32] = v;
+  __syncthreads();
+  if (k == 0 && c < cols) {
+#pragma unroll
+    for (int j = 1; j < 8; ++j) v += s[j][threadIdx.x];
+    dg[c] = v;
+  }
+}
+
+// ----------------------------------------------------------------------------- host side
+
+// Calls f.template operator()<TPR, VPT>() with the smallest row shape that holds `cols`; false when
+// the row does not fit registers.  A wave per row up to 2048 columns (no barrier), then a workgroup.
+template <int MAX_COLS, typename F>
+bool dispatch_row(int64_t cols, F &&f) {
+  const int64_t v = (cols + 7) / 8;
+  if (cols > MAX_COLS) return false;
+  if (v <= 64) f.template operator()<64, 1>();
+  else if (v <= 128) f.template operator()<64, 2>();
+  else if (v <= 256) f.template operator()<64, 4>();
+  else if (v <= 512) f.template operator()<256, 2>();
+  else if (v <= 1024) f.template operator()<256, 4>();
+  else f.template operator()<512, 4>();
+  return true;
+}
+constexpr int FWD_MAX_COLS = 16384, BWD_MAX_COLS = 16384;
+
+template <typename F>
+void dispatch_xy(int xt, int yt, F &&f) {
+  if (xt == FQT_BF16) {
+    if (yt == FQT_BF16) f.template operator()<bf16, bf16>();
+    else f.template operator()<bf16, float>();
+  } else {
+    if (yt == FQT_BF16) f.template operator()<float, bf16>();
+    else f.template operator()<float, float>();
+  }
+}
+
+struct Strides { int64_t x, r, h, y, q; };
+int check_norm(const fqt_norm_desc *d, Strides *s) {
+  if (!d) return FQT_E_NULL;
+  if (!float_type(d->x_dtype) || !float_type(d->y_dtype) ||
+      !(code_type(d->q_dtype) || d->q_dtype == FQT_NO_CODES))
+    return FQT_E_DTYPE;
+  if (d->rows < 0 || d->cols < 0 || d->rows >= FQT_MAX_ROWS || d->cols > FQT_MAX_LD) return FQT_E_SHAPE;
+  if (!(d->eps > 0.0f) || !std::isfinite(d->eps)) return FQT_E_INVAL;
+  *s = {row_stride(d->ldx, d->cols), row_stride(d->ldr, d->cols), row_stride(d->ldh, d->cols),
+        row_stride(d->ldy, d->cols), row_stride(d->ldq, d->cols)};
+  if (!s->x || !s->r || !s->h || !s->y || !s->q) return FQT_E_SHAPE;
+  return FQT_OK;
+}
+bool on16(const void *p, int64_t ld, size_t e) { return !p || (aligned(p, 16) && ld * e % 16 == 0); }
+
+int run_norm(const fqt_norm_desc *d, NormArgs a, hipStream_t st) {
+  if (d->rows == 0 || d->cols == 0) return FQT_OK;
+  const size_t xe = elem_size(d->x_dtype), ye = elem_size(d->y_dtype);
+  a.rows = d->rows;
+  a.cols = int32_t(d->cols);
+  a.q_dtype = d->q_dtype;
+  a.eps = d->eps;
+  a.vec = on16(a.x, a.ldx, xe) && on16(a.r, a.ldr, xe) && on16(a.h, a.ldh, xe) &&
+          on16(a.y, a.ldy, ye) && (!a.q || (aligned(a.q, 8) && a.ldq % 8 == 0));
+  dispatch_xy(d->x_dtype, d->y_dtype, [&]<typename XT, typename YT>() {
+    if (!dispatch_row<FWD_MAX_COLS>(d->cols, [&]<int TPR, int VPT>() {
+          constexpr int ROWS = TPR < 256 ? 256 / TPR : 1;
+          const int64_t blocks = std::min<int64_t>((d->rows + ROWS - 1) / ROWS, 2048);
+          k_norm_fwd<XT, YT, TPR, VPT><<<dim3(blocks), dim3(TPR < 256 ? 256 : TPR), 0, st>>>(a);
+        }))
+      k_norm_fwd_long<XT, YT><<<dim3(std::min<int64_t>(d->rows, 512)), dim3(LONG_TPR), 0, st>>>(a);
+  });
+  return last_launch_status();
+}
+
+// Workgroups of the backward = rows of partial sums.
+int64_t bwd_parts(int64_t rows, int64_t cols) {
+  if (cols > BWD_MAX_COLS) return std::min<int64_t>(std::max<int64_t>(rows, 1), 64);
+  const int64_t per = cols <= 2048 ? 4 : 1;
+  return std::min<int64_t>(std::max<int64_t>((rows + per - 1) / per, 1), 512);
+}
+
+}  // namespace
+}  // namespace dense
+}  // namespace fqt
+
+using namespace fqt;
+using namespace fqt::dense;
+
+extern "C" int fqt_rmsnorm_forward(const fqt_norm_desc *d, const void *x, const void *residual,
+                                   const float *g, void *h, void *y, void *q, float *scale,
+                                   float *rstd, void *hip_stream) {
+  Strides s;
+  FQT_TRY_(check_norm(d, &s));
+  if (q && d->q_dtype == FQT_NO_CODES) return FQT_E_DTYPE;
+  if (d->rows == 0 || d->cols == 0) return FQT_OK;
+  if (!x || !g || (q && !scale) || (scale && !q)) return FQT_E_NULL;
+  if (!elem_aligned(x, d->x_dtype) || !elem_aligned(residual, d->x_dtype) || !aligned(g, 4) ||
+      !elem_aligned(h, d->x_dtype) || !elem_aligned(y, d->y_dtype) || !aligned(scale, 4) ||
+      !aligned(rstd, 4))
+    return FQT_E_ALIGN;
+  NormArgs a{};
+  a.x = x; a.r = residual; a.g = g; a.h = h; a.y = y;
+  a.q = static_cast<uint8_t *>(q);
+  a.scale = scale; a.rstd = rstd;
+  a.ldx = s.x; a.ldr = s.r; a.ldh = s.h; a.ldy = s.y; a.ldq = s.q;
+  a.norm = 1;
+  return run_norm(d, a, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" int fqt_quantize_rows(const fqt_norm_desc *d, const void *x, void *q, float *scale,
+                                 void *hip_stream) {
+  Strides s;
+  FQT_TRY_(check_norm(d, &s));
+  if (!code_type(d->q_dtype)) return FQT_E_DTYPE;
+  if (d->rows == 0 || d->cols == 0) return FQT_OK;
+  if (!x || !q || !scale) return FQT_E_NULL;
+  if (!elem_aligned(x, d->x_dtype) || !aligned(scale, 4)) return FQT_E_ALIGN;
+  NormArgs a{};
+  a.x = x;
+  a.q = static_cast<uint8_t *>(q);
+  a.scale = scale;
+  a.ldx = s.x; a.ldq = s.q;
+  return run_norm(d, a, static_cast<hipStream_t>(hip_stream));
+}
+
+extern "C" int fqt_norm_workspace_size(const fqt_norm_desc *d, size_t *bytes) {
+  Strides s;
+  FQT_TRY_(check_norm(d, &s));
+  if (!bytes) return FQT_E_NULL;
+  *bytes = align256(size_t(bwd_parts(d->rows, d->cols)) * size_t(d->cols) * sizeof(float));
+  return FQT_OK;
+}
+
+extern "C" int fqt_rmsnorm_backward(const fqt_norm_desc *d, const void *h, const float *g,
+                                    const float *rstd, const void *dy, const void *dres, void *dx,
+                                    float *dg, void *ws, size_t ws_bytes, void *hip_stream) {
+  Strides s;
+  FQT_TRY_(check_norm(d, &s));
+  size_t need = 0;
+  FQT_TRY_(fqt_norm_workspace_size(d, &need));
+  if (d->cols == 0) return FQT_OK;
+  if (!g || !dg || !ws || (d->rows && (!h || !rstd || !dy || !dx))) return FQT_E_NULL;
+  if (!elem_aligned(h, d->x_dtype) || !aligned(g, 4) || !aligned(rstd, 4) ||
+      !elem_aligned(dy, d->y_dtype) || !elem_aligned(dres, d->x_dtype) ||
+      !elem_aligned(dx, d->x_dtype) || !aligned(dg, 4) || !aligned(ws, 256))
+    return FQT_E_ALIGN;
+  if (ws_bytes < need) return FQT_E_WORKSPACE;
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  const size_t xe = elem_size(d->x_dtype), ye = elem_size(d->y_dtype);
+  NormBwdArgs a{};
+  a.h = h; a.dy = dy; a.dres = dres; a.g = g; a.rstd = rstd; a.dx = dx;
+  a.part = static_cast<float *>(ws);
+  a.rows = d->rows;
+  a.cols = int32_t(d->cols);
+  a.ldh = s.h; a.ldy = s.y; a.ldr = s.r; a.ldx = s.x;
+  a.vec = on16(h, s.h, xe) && on16(dy, s.y, ye) && on16(dres, s.r, xe) && on16(dx, s.x, xe);
+  const int64_t parts = bwd_parts(d->rows, d->cols);
+  dispatch_xy(d->x_dtype, d->y_dtype, [&]<typename XT, typename YT>() {
+    if (dispatch_row<BWD_MAX_COLS>(d->cols, [&]<int TPR, int VPT>() {
+          k_norm_bwd<XT, YT, TPR, VPT><<<dim3(parts), dim3(TPR < 256 ? 256 : TPR), 0, st>>>(a);
+        }))
+      return;
+    if (d->rows)
+      k_norm_bwd_long<XT, YT><<<dim3(std::min<int64_t>(d->rows, 512)), dim3(LONG_TPR), 0, st>>>(a);
+    k_norm_dg_long<XT, YT><<<dim3((d->cols + 511) / 512, parts), dim3(64), 0, st>>>(a);
+  });
+  FQT_TRY_(last_launch_status());
+  k_norm_dg<<<dim3((d->cols + 31) / 32), dim3(256), 0, st>>>(a.part, int32_t(parts),
+                                                             int32_t(d->cols), dg);
+  return last_launch_status();
+}
