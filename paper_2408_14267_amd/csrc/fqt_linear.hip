@@ -23,22 +23,44 @@ using tile::COLS;
 
 // ----------------------------------------------------------------------------- activations
 
+__device__ __forceinline__ float exp_neg(float v) {        // exp(-v)
+  return __builtin_amdgcn_exp2f(v * -1.44269504088896341f);
+}
+// Phi(-|z|) and exp(-z^2 / 2), Phi the normal distribution function: Phi(-|z|) = exp(-z^2 / 2) times a
+// quintic in t = 1 / (1 + p |z| / sqrt 2) (Abramowitz and Stegun 7.1.26 halved; absolute error below
+// 8e-8).  About 20 issue slots; the library's erf costs four times that, and a 256 x 256 tile pays
+// 0.4 us for each slot.
+__device__ __forceinline__ float normal_tail(float z, float *e) {
+  const float a = fabsf(z);
+  const float t = __builtin_amdgcn_rcpf(fmaf(a, 0.3275911f * 0.70710678118654752f, 1.0f));
+  float q = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
+  q = fmaf(t, q, 0.5f * 1.421413741f);
+  q = fmaf(t, q, 0.5f * -0.284496736f);
+  q = fmaf(t, q, 0.5f * 0.254829592f);
+  *e = exp_neg(0.5f * z * z);
+  return q * t * *e;
+}
 template <int ACT>
 __device__ __forceinline__ float activate(float z) {
   if constexpr (ACT == FQT_ACT_RELU) return z > 0.0f ? z : (z != z ? z : 0.0f);
-  else if constexpr (ACT == FQT_ACT_GELU) return 0.5f * z * (1.0f + erff(z * 0.70710678118654752f));
-  else if constexpr (ACT == FQT_ACT_SILU) return z / (1.0f + expf(-z));
+  else if constexpr (ACT == FQT_ACT_GELU) {
+    float e;
+    const float q = normal_tail(z, &e);
+    return z * (z > 0.0f ? 1.0f - q : q);
+  } else if constexpr (ACT == FQT_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + exp_neg(z));
   else if constexpr (ACT == FQT_ACT_HARDTANH) return z != z ? z : fminf(fmaxf(z, -1.0f), 1.0f);
   else return z;
 }
 template <int ACT>
 __device__ __forceinline__ float slope(float z) {
   if constexpr (ACT == FQT_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
-  else if constexpr (ACT == FQT_ACT_GELU)
-    return 0.5f * (1.0f + erff(z * 0.70710678118654752f)) + z * expf(-0.5f * z * z) * 0.39894228040143268f;
-  else if constexpr (ACT == FQT_ACT_SILU) {
-    const float t = 1.0f / (1.0f + expf(-z));
-    return t * (1.0f + z * (1.0f - t));
+  else if constexpr (ACT == FQT_ACT_GELU) {
+    float e;
+    const float q = normal_tail(z, &e);
+    return fmaf(z * 0.39894228040143268f, e, z > 0.0f ? 1.0f - q : q);
+  } else if constexpr (ACT == FQT_ACT_SILU) {
+    const float t = __builtin_amdgcn_rcpf(1.0f + exp_neg(z));
+    return t * fmaf(z, 1.0f - t, 1.0f);
   } else if constexpr (ACT == FQT_ACT_HARDTANH) return z > -1.0f && z < 1.0f ? 1.0f : 0.0f;
   else return 1.0f;
 }
@@ -109,33 +131,27 @@ __device__ __forceinline__ void finish8(const Epilogue &e, int64_t m, int64_t n,
 struct Product {
   Operand x, w;
   int64_t M, N, K;
-  uint32_t nm, nn;       // tiles
-  uint32_t splits;
-  int64_t steps;         // contraction steps of one split
+  tile::Tiles tiles;
   float *part;           // [splits][M][ldp] partial sums (splits > 1)
   int64_t ldp;
 };
 
-template <int KIND, int LX, int LW, typename S>
-__global__ void __launch_bounds__(S::THREADS) k_product(Product p, Epilogue e) {
+template <int KIND, int LX, int LW, int SHAPE>
+__global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_product(Product p, Epilogue e) {
+  typedef typename tile::ShapeOf<SHAPE>::type S;
   __shared__ __attribute__((aligned(16))) char lds[S::LDS];
-  const uint32_t tiles = p.nm * p.nn, split = blockIdx.x / tiles;
-  const tile::TileAt at = tile::tile_at(blockIdx.x % tiles, p.nm, p.nn);
-  const int64_t m0 = int64_t(at.m) * S::BM, n0 = int64_t(at.n) * S::BN;
-  constexpr int64_t STEP = tile::KB / tile::elem_bytes<KIND>;
-  const int64_t total = (p.K + STEP - 1) / STEP;
-  const int64_t t0 = split * p.steps, t1 = min(total, t0 + p.steps);
-  const Operand x[1] = {p.x}, w[1] = {p.w};
+  const tile::Place at = tile::place<SHAPE>(p.tiles, blockIdx.x);
+  if (at.m0 >= p.M || at.n0 >= p.N) return;              // (parts of an edge tile)
   typename tile::Acc<KIND>::type acc[S::FM][S::FN];
-  tile::run_tile<KIND, LX, LW, S>(x, w, p.K, m0, n0, t0, t1, lds, acc);
-  if (p.splits > 1) {
-    float *part = p.part + split * p.M * p.ldp;
-    tile::for_rows8<KIND, S>(acc, lds, m0, n0, [&](int64_t m, int64_t n, float (&v)[8]) {
+  tile::contract<KIND, LX, LW, SHAPE, S>(p.x, p.w, p.K, at, p.tiles, lds, acc);
+  if (p.tiles.splits > 1) {
+    float *part = p.part + at.split * p.M * p.ldp;
+    tile::for_rows8<KIND, S>(acc, lds, at.m0, at.n0, [&](int64_t m, int64_t n, float (&v)[8]) {
       if (m < p.M && n < p.ldp) store8f(part + m * p.ldp + n, true, 8, v);
     });
   } else {
     with_act(e.act, [&]<int ACT>() {
-      tile::for_rows8<KIND, S>(acc, lds, m0, n0, [&](int64_t m, int64_t n, float (&v)[8]) {
+      tile::for_rows8<KIND, S>(acc, lds, at.m0, at.n0, [&](int64_t m, int64_t n, float (&v)[8]) {
         finish8<ACT>(e, m, n, v);
       });
     });
@@ -150,7 +166,7 @@ __global__ void __launch_bounds__(256) k_product_finish(Product p, Epilogue e) {
     for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
       const int64_t m = i / groups, n = i % groups * 8;
       float v[8] = {}, t[8];
-      for (uint32_t s = 0; s < p.splits; ++s) {
+      for (uint32_t s = 0; s < p.tiles.splits; ++s) {
         load8f(p.part + (s * p.M + m) * p.ldp + n, true, 8, t);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] += t[j];
@@ -285,52 +301,29 @@ int64_t round_up(int64_t v, int64_t q) { return (v + q - 1) / q * q; }
 // Whether rows of n elements, ld apart, are whole 16-byte pieces.
 bool whole_pieces(int64_t n, int64_t ld, size_t e) { return n * e % 16 == 0 && ld * e % 16 == 0; }
 
-// Tiles and splits of an M x N product over K.  v1: the largest tile that gives the chip work.
-struct Plan {
-  int shape;             // 0: 256 x 256, 1: 128 x 128, 2: 64 x 64
-  uint32_t nm, nn, splits;
-  int64_t steps;         // of one split
-};
-using Shape0 = tile::Shape<256, 256, 2, 4>;
-using Shape1 = tile::Shape<128, 128, 2, 2>;
-using Shape2 = tile::Shape<64, 64, 2, 2>;
-Plan make_plan(int64_t M, int64_t N, int64_t K, size_t e) {
-  auto tiles = [&](int64_t b) { return ((M + b - 1) / b) * ((N + b - 1) / b); };
-  Plan p{};
-  const int64_t b = tiles(256) >= 200 ? 256 : tiles(128) >= 200 ? 128 : 64;
-  p.shape = b == 256 ? 0 : b == 128 ? 1 : 2;
-  p.nm = uint32_t((M + b - 1) / b);
-  p.nn = uint32_t((N + b - 1) / b);
-  const int64_t total = (K * int64_t(e) + tile::KB - 1) / tile::KB;
-  int64_t splits = 1;
-  if (p.shape == 2) splits = std::max<int64_t>(1, std::min<int64_t>(1024 / std::max<int64_t>(1, tiles(64)), total / 8));
-  p.steps = std::max<int64_t>(1, (total + splits - 1) / splits);
-  p.splits = uint32_t(std::max<int64_t>(1, (total + p.steps - 1) / p.steps));
-  return p;
+tile::Plan plan_of(int64_t M, int64_t N, int64_t K, size_t e) {
+  return tile::make_plan(M, N, (K * int64_t(e) + tile::KB - 1) / tile::KB, false);
 }
-size_t part_bytes(const Plan &p, int64_t M, int64_t N) {
+size_t part_bytes(const tile::Plan &p, int64_t M, int64_t N) {
   return p.splits > 1 ? align256(size_t(p.splits) * M * round_up(N, 8) * 4) : 0;
 }
 
 template <int KIND, int LX, int LW>
-int launch_product(const Plan &pl, Operand x, Operand w, int64_t M, int64_t N, int64_t K, Epilogue e,
+int launch_product(const tile::Plan &plan, Operand x, Operand w, int64_t M, int64_t N, int64_t K, Epilogue e,
                    float *part, hipStream_t st) {
   if (M == 0 || N == 0) return FQT_OK;
-  Product p{x, w, M, N, K, pl.nm, pl.nn, pl.splits, pl.steps, part, round_up(N, 8)};
+  Product p{x, w, M, N, K, plan.t[0], part, round_up(N, 8)};
   const size_t ye = elem_size(e.y_dtype);
   auto on16 = [&](const void *q, int64_t ld) { return !q || (aligned(q, 16) && ld * ye % 16 == 0); };
   e.M = M;
   e.N = N;
   e.vec = on16(e.res, e.ldr) && on16(e.z, e.ldz) && on16(e.y, e.ldy);
-  const dim3 grid(pl.nm * pl.nn * pl.splits);
-  auto go = [&]<typename S>(S) {
-    k_product<KIND, LX, LW, S><<<grid, dim3(S::THREADS), 0, st>>>(p, e);
-  };
-  if (pl.shape == 0) go(Shape0{});
-  else if (pl.shape == 1) go(Shape1{});
-  else go(Shape2{});
+  tile::for_launches(plan, [&]<int SHAPE>(const tile::Tiles &t) {
+    p.tiles = t;
+    k_product<KIND, LX, LW, SHAPE><<<dim3(tile::blocks_of(SHAPE, t)), dim3(tile::ShapeOf<SHAPE>::type::THREADS), 0, st>>>(p, e);
+  });
   FQT_TRY_(last_launch_status());
-  if (pl.splits > 1) {
+  if (plan.splits > 1) {
     const int64_t all = M * (p.ldp / 8);
     k_product_finish<<<dim3(std::min<int64_t>((all + 255) / 256, 4096)), dim3(256), 0, st>>>(p, e);
     return last_launch_status();
@@ -349,16 +342,21 @@ int repack(const void *src, int64_t rows, int64_t cols, int64_t ld, void *dst, i
 
 // Workspace of the forward: padded copies of operands whose rows are not whole 16-byte pieces, and
 // the partial sums of a split contraction.
-struct FwdWs { size_t x, w, part, total; int64_t pitch; Plan plan; bool copy_x, copy_w; };
-FwdWs fwd_ws(const Sizes &s) {
+struct FwdWs { size_t x, w, part, total; int64_t pitch, e; tile::Plan plan; bool widen, copy_x, copy_w; };
+FwdWs fwd_ws(const fqt_linear_desc &d, const Sizes &s) {
   FwdWs f{};
-  f.pitch = round_up(s.K, 16 / s.xe);
-  f.copy_x = !whole_pieces(s.K, s.ldx, s.xe);
-  f.copy_w = !whole_pieces(s.K, s.ldw, s.xe);
-  f.plan = make_plan(s.M, s.N, s.K, s.xe);
+  // The e4m3 matrix instruction adds the products of a step in fewer bits than float32 has (sums off by
+  // 1e-5 to 6e-5 of their norm): below the rounding of a bf16 output, not of a float32 one, for which the
+  // codes go through bf16 copies (exact) and that type's instruction.
+  f.widen = d.x_dtype == FQT_E4M3 && d.y_dtype == FQT_F32;
+  f.e = f.widen ? 2 : int64_t(s.xe);
+  f.pitch = round_up(s.K, 16 / f.e);
+  f.copy_x = f.widen || !whole_pieces(s.K, s.ldx, s.xe);
+  f.copy_w = f.widen || !whole_pieces(s.K, s.ldw, s.xe);
+  f.plan = plan_of(s.M, s.N, s.K, f.e);
   f.x = 0;
-  f.w = f.x + (f.copy_x ? align256(s.M * f.pitch * s.xe) : 0);
-  f.part = f.w + (f.copy_w ? align256(s.N * f.pitch * s.xe) : 0);
+  f.w = f.x + (f.copy_x ? align256(s.M * f.pitch * f.e) : 0);
+  f.part = f.w + (f.copy_w ? align256(s.N * f.pitch * f.e) : 0);
   f.total = f.part + part_bytes(f.plan, s.M, s.N);
   return f;
 }
@@ -366,7 +364,7 @@ FwdWs fwd_ws(const Sizes &s) {
 // Workspace of the backward: dz in bf16 (twice for scaled operands), bf16 copies of operands that
 // are codes or whose rows are not whole pieces, the partial sums of dbias, and those of the products
 // (which run one after the other).
-struct BwdWs { size_t dzx, dzw, x, w, bias, part, total; int64_t dz_pitch, pitch, rows; Plan dx, dw; bool copy_x, copy_w; };
+struct BwdWs { size_t dzx, dzw, x, w, bias, part, total; int64_t dz_pitch, pitch, rows; tile::Plan dx, dw; bool copy_x, copy_w; };
 BwdWs bwd_ws(const Sizes &s) {
   BwdWs f{};
   const bool codes = s.xe == 1;
@@ -375,8 +373,8 @@ BwdWs bwd_ws(const Sizes &s) {
   f.copy_x = codes || !whole_pieces(s.K, s.ldx, 2);
   f.copy_w = codes || !whole_pieces(s.K, s.ldw, 2);
   f.rows = std::max<int64_t>(1, std::min<int64_t>(s.M, 256));
-  f.dx = make_plan(s.M, s.K, s.N, 2);
-  f.dw = make_plan(s.N, s.K, s.M, 2);
+  f.dx = plan_of(s.M, s.K, s.N, 2);
+  f.dw = plan_of(s.N, s.K, s.M, 2);
   const size_t dz = align256(size_t(s.M) * f.dz_pitch * 2);
   f.dzx = 0;
   f.dzw = codes ? dz : 0;
@@ -406,7 +404,7 @@ extern "C" int fqt_linear_workspace_size(const fqt_linear_desc *d, int32_t backw
   Sizes s;
   FQT_TRY_(check_linear(d, &s));
   if (!bytes) return FQT_E_NULL;
-  *bytes = std::max<size_t>(256, backward ? bwd_ws(s).total : fwd_ws(s).total);
+  *bytes = std::max<size_t>(256, backward ? bwd_ws(s).total : fwd_ws(*d, s).total);
   return FQT_OK;
 }
 
@@ -424,17 +422,17 @@ extern "C" int fqt_linear_forward(const fqt_linear_desc *d, const void *x, const
       !aligned(bias, 4) || !elem_aligned(residual, d->y_dtype) || !elem_aligned(z, d->y_dtype) ||
       !elem_aligned(y, d->y_dtype) || !aligned(ws, 256))
     return FQT_E_ALIGN;
-  const FwdWs f = fwd_ws(s);
+  const FwdWs f = fwd_ws(*d, s);
   if (ws_bytes < f.total) return FQT_E_WORKSPACE;
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   char *base = static_cast<char *>(ws);
   auto operand = [&](const void *p, bool copy, size_t at, int64_t rows, int64_t ld, Operand *o) -> int {
-    const int64_t e = int64_t(s.xe);
     if (!copy) {
-      *o = {static_cast<const char *>(p), ld * e, rows};
+      *o = {static_cast<const char *>(p), ld * f.e, rows};
       return FQT_OK;
     }
-    *o = {base + at, f.pitch * e, rows};
+    *o = {base + at, f.pitch * f.e, rows};
+    if (f.widen) return repack<e4m3, bf16>(p, rows, s.K, ld, base + at, f.pitch, st);
     return codes ? repack<int8_t, int8_t>(p, rows, s.K, ld, base + at, f.pitch, st)
                  : repack<bf16, bf16>(p, rows, s.K, ld, base + at, f.pitch, st);
   };
@@ -444,7 +442,7 @@ extern "C" int fqt_linear_forward(const fqt_linear_desc *d, const void *x, const
   const int64_t K = f.copy_x || f.copy_w ? f.pitch : s.K;
   Epilogue e{x_scale, w_scale, bias, residual, z, y, 0, 0, s.ldr, s.ldz, s.ldy, d->y_dtype, d->act, 0};
   float *part = reinterpret_cast<float *>(base + f.part);
-  if (d->x_dtype == FQT_BF16)
+  if (d->x_dtype == FQT_BF16 || f.widen)
     return launch_product<tile::BF16K, ROWS, ROWS>(f.plan, xo, wo, s.M, s.N, K, e, part, st);
   if (d->x_dtype == FQT_I8)
     return launch_product<tile::I8K, ROWS, ROWS>(f.plan, xo, wo, s.M, s.N, K, e, part, st);

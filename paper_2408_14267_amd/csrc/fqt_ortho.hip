@@ -1,17 +1,17 @@
 // Newton-Schulz orthogonalisation and the optimizer step on it.
 //
-// X is kept on the short side of the matrix (m x n, m <= n), padded with zeros to whole tiles, as
-// two float16 planes hi + lo of X 2^15 (hi the nearest float16, lo the nearest to the rest): 22 bits
-// and their rounding, as good as float32 where entries are not 2^-24 of the largest.  A product is
-// the sum of hi hi, hi lo and lo hi on the 16-bit matrix cores with float32 sums; lo lo is below the
-// rounding.  That is three passes of matrix instructions at many times the rate of float32 ones.
+// X is kept on the short side of the matrix (m x n, m <= n), padded with zeros to multiples of 64, as
+// float16 pairs hi + lo of X 2^15 (hi the nearest float16, lo the nearest to the rest): 22 bits and
+// their rounding, as good as float32 where entries are not 2^-24 of the largest.  A product is the sum
+// of hi hi, hi lo and lo hi on the 16-bit matrix cores with float32 sums; lo lo is below the rounding.
+// That is three matrix instructions at 16 times the rate of the float32 ones.
 //
 // The powers of two keep every entry inside float16: the singular values of X stay below 1.21 (the
 // quintic maps [0, 1.21] into itself), so |X| < 2^15 1.21, |P| = |X X^T| < 1.47 (2^14) and
 // |b P + c P^2| < 2.81 (2^13) are below 65504 with the factors in brackets.
 //
 // A step is three products: P = X X^T and Q = b P + c P P, both symmetric, of which only the tiles on
-// and above the diagonal are computed and stored twice; X' = a X + Q X, which reads X along m (COLS).
+// and above the diagonal are computed and stored twice; X' = a X + Q X, which reads X along m (PANEL_COLS).
 // The last step's product stores the result, or updates the weights, instead of X'.
 #include "fqt_tile.hpp"
 
@@ -22,8 +22,8 @@ namespace {
 #pragma clang fp contract(fast)
 
 using tile::Operand;
-using tile::ROWS;
-using tile::COLS;
+using tile::PANEL_ROWS;
+using tile::PANEL_COLS;
 
 constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
 constexpr float X_UNIT = 32768.0f;      // 2^15
@@ -37,8 +37,17 @@ __device__ __forceinline__ Split split(float v) {
 __device__ __forceinline__ float join(uint16_t hi, uint16_t lo) {
   return static_cast<float>(__builtin_bit_cast(_Float16, hi)) + static_cast<float>(__builtin_bit_cast(_Float16, lo));
 }
-struct Planes { uint16_t *hi, *lo; };
-__device__ __forceinline__ void store_split8(const Planes &p, int64_t at, const float (&v)[8]) {
+// A matrix of pairs in panels of 32 columns (tile::SPLITK): row r of panel c is the 64 values
+// at (c * rows + r) * 64.
+struct Pairs {
+  uint16_t *p;
+  int64_t rows;
+  __device__ __forceinline__ uint16_t *at(int64_t r, int64_t c) const {
+    return p + (c / 32 * rows + r) * 64 + c % 32;
+  }
+};
+// 8 columns from c (a multiple of 8) of row r.
+__device__ __forceinline__ void store_split8(const Pairs &p, int64_t r, int64_t c, const float (&v)[8]) {
   uint32_t h[4], l[4];
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -46,11 +55,13 @@ __device__ __forceinline__ void store_split8(const Planes &p, int64_t at, const 
     h[i] = a.hi | uint32_t(b.hi) << 16;
     l[i] = a.lo | uint32_t(b.lo) << 16;
   }
-  *reinterpret_cast<uint4 *>(p.hi + at) = make_uint4(h[0], h[1], h[2], h[3]);
-  *reinterpret_cast<uint4 *>(p.lo + at) = make_uint4(l[0], l[1], l[2], l[3]);
+  uint16_t *q = p.at(r, c);
+  *reinterpret_cast<uint4 *>(q) = make_uint4(h[0], h[1], h[2], h[3]);
+  *reinterpret_cast<uint4 *>(q + 32) = make_uint4(l[0], l[1], l[2], l[3]);
 }
-__device__ __forceinline__ void load_split8(const Planes &p, int64_t at, float (&v)[8]) {
-  const uint4 h = *reinterpret_cast<const uint4 *>(p.hi + at), l = *reinterpret_cast<const uint4 *>(p.lo + at);
+__device__ __forceinline__ void load_split8(const Pairs &p, int64_t r, int64_t c, float (&v)[8]) {
+  const uint16_t *q = p.at(r, c);
+  const uint4 h = *reinterpret_cast<const uint4 *>(q), l = *reinterpret_cast<const uint4 *>(q + 32);
   const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
 #pragma unroll
   for (int i = 0; i < 4; ++i) {
@@ -97,11 +108,11 @@ __global__ void __launch_bounds__(256) k_ns_norm(Source s, double *part) {
   if (threadIdx.x == 0) part[blockIdx.x] = sums[0] + sums[1] + sums[2] + sums[3];
 }
 
-// X_0 = u / (|u| + eps) as planes [mp][np], zeros in the padding.  A workgroup takes a 64 x 64 tile of
+// X_0 = u / (|u| + eps) as pairs, zeros in the padding.  A workgroup takes a 64 x 64 tile of
 // X; tall matrices are transposed on the way.
 template <bool TALL>
 __global__ void __launch_bounds__(256) k_ns_start(Source s, const double *part, int32_t parts, float eps,
-                                                  Planes x, int64_t np) {
+                                                  Pairs x) {
   __shared__ double sums[4];
   __shared__ float t[64][65];
   double sum = 0.0;
@@ -134,7 +145,7 @@ __global__ void __launch_bounds__(256) k_ns_start(Source s, const double *part, 
     float v[8];
 #pragma unroll
     for (int j = 0; j < 8; ++j) v[j] = t[a][b + j];
-    store_split8(x, (x0 + a) * np + y0 + b, v);
+    store_split8(x, x0 + a, y0 + b, v);
   }
 }
 
@@ -142,11 +153,10 @@ __global__ void __launch_bounds__(256) k_ns_start(Source s, const double *part, 
 
 enum Mode { GRAM, POLY, APPLY };
 struct NsArgs {
-  Planes x, p, q, next;  // X [mp][np]; P, Q [mp][mp]; the next X
+  Pairs x, p, q, next;   // X [mp][np]; P, Q [mp][mp]; the next X
   int64_t mp, np;
   int64_t m, n;          // without padding
-  uint32_t nm, nn, tiles, splits;
-  int64_t steps;
+  tile::Tiles tiles;
   float *part;
   // the last step's result
   void *out;             // o, or null
@@ -161,11 +171,11 @@ __device__ __forceinline__ void ns_finish8(const NsArgs &a, int64_t m, int64_t n
   if constexpr (MODE == APPLY) {
     if (m >= a.mp || n >= a.np) return;
     float x[8];
-    load_split8(a.x, m * a.np + n, x);
+    load_split8(a.x, m, n, x);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = fmaf(NS_A, x[i], v[i] * 0x1p-13f);      // X' 2^15
     if (!a.last) {
-      store_split8(a.next, m * a.np + n, v);
+      store_split8(a.next, m, n, v);
       return;
     }
     if (m >= a.m) return;
@@ -180,119 +190,82 @@ __device__ __forceinline__ void ns_finish8(const NsArgs &a, int64_t m, int64_t n
     }
   } else {
     if (m >= a.mp || n >= a.mp) return;
-    const Planes &to = MODE == GRAM ? a.p : a.q;
+    const Pairs &to = MODE == GRAM ? a.p : a.q;
     if constexpr (MODE == GRAM) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] *= 0x1p-16f;                            // P 2^14 of sums 2^30
     } else {
       float p[8];
-      load_split8(a.p, m * a.mp + n, p);
+      load_split8(a.p, m, n, p);
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] = fmaf(NS_B * 0.5f, p[i], v[i] * (NS_C * 0x1p-15f));   // Q 2^13
     }
-    store_split8(to, m * a.mp + n, v);
+    store_split8(to, m, n, v);
     if (mirror) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const Split s = split(v[i]);
-        to.hi[(n + i) * a.mp + m] = s.hi;
-        to.lo[(n + i) * a.mp + m] = s.lo;
+        uint16_t *q = to.at(n + i, m);
+        q[0] = s.hi;
+        q[32] = s.lo;
       }
     }
   }
 }
 
-// Tile t of the tiles on and above the diagonal of k x k, by columns.
-__device__ __forceinline__ tile::TileAt upper_tile(uint32_t t) {
-  uint32_t c = uint32_t((sqrtf(8.0f * float(t) + 1.0f) - 1.0f) * 0.5f);
-  while (c * (c + 1) / 2 > t) --c;
-  while ((c + 1) * (c + 2) / 2 <= t) ++c;
-  return {t - c * (c + 1) / 2, c};
-}
-
-template <int MODE, typename S>
-__global__ void __launch_bounds__(S::THREADS) k_ns(NsArgs a) {
+template <int MODE, int SHAPE>
+__global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_ns(NsArgs a) {
+  typedef typename tile::ShapeOf<SHAPE>::type S;
   __shared__ __attribute__((aligned(16))) char lds[S::LDS];
-  const uint32_t sp = blockIdx.x / a.tiles, b = blockIdx.x % a.tiles;
-  const tile::TileAt at = MODE == APPLY ? tile::tile_at(b, a.nm, a.nn) : upper_tile(b);
-  const int64_t m0 = int64_t(at.m) * S::BM, n0 = int64_t(at.n) * S::BN;
+  const tile::Place at = tile::place<SHAPE>(a.tiles, blockIdx.x);
   const int64_t K = MODE == GRAM ? a.np : a.mp;
-  const int64_t t0 = sp * a.steps, t1 = min(3 * (K / 64), t0 + a.steps);
-  auto op = [&](const uint16_t *p, int64_t ld, int64_t rows) {
-    return Operand{reinterpret_cast<const char *>(p), ld * 2, rows};
+  if (at.m0 >= a.mp || at.n0 >= (MODE == APPLY ? a.np : a.mp)) return;       // (parts of an edge tile)
+  // rows: of the result along the operand; a panel holds `rows of the matrix` x 128 bytes
+  auto op = [&](const Pairs &p, int64_t rows) {
+    return Operand{reinterpret_cast<const char *>(p.p), p.rows * tile::KB, rows};
   };
-  typename tile::Acc<tile::F16K>::type acc[S::FM][S::FN];
-  if constexpr (MODE == GRAM) {
-    const Operand h = op(a.x.hi, a.np, a.mp), l = op(a.x.lo, a.np, a.mp);
-    const Operand x[3] = {h, h, l}, w[3] = {h, l, h};
-    tile::run_tile<tile::F16K, ROWS, ROWS, S>(x, w, K, m0, n0, t0, t1, lds, acc);
-  } else if constexpr (MODE == POLY) {
-    const Operand h = op(a.p.hi, a.mp, a.mp), l = op(a.p.lo, a.mp, a.mp);
-    const Operand x[3] = {h, h, l}, w[3] = {h, l, h};
-    tile::run_tile<tile::F16K, ROWS, ROWS, S>(x, w, K, m0, n0, t0, t1, lds, acc);
-  } else {
-    const Operand qh = op(a.q.hi, a.mp, a.mp), ql = op(a.q.lo, a.mp, a.mp);
-    const Operand xh = op(a.x.hi, a.np, a.np), xl = op(a.x.lo, a.np, a.np);
-    const Operand x[3] = {qh, qh, ql}, w[3] = {xh, xl, xh};
-    tile::run_tile<tile::F16K, ROWS, COLS, S>(x, w, K, m0, n0, t0, t1, lds, acc);
-  }
-  if (a.splits > 1) {
+  typename tile::Acc<tile::SPLITK>::type acc[S::FM][S::FN];
+  if constexpr (MODE == GRAM)
+    tile::contract<tile::SPLITK, PANEL_ROWS, PANEL_ROWS, SHAPE, S>(op(a.x, a.mp), op(a.x, a.mp), K, at, a.tiles, lds, acc);
+  else if constexpr (MODE == POLY)
+    tile::contract<tile::SPLITK, PANEL_ROWS, PANEL_ROWS, SHAPE, S>(op(a.p, a.mp), op(a.p, a.mp), K, at, a.tiles, lds, acc);
+  else
+    tile::contract<tile::SPLITK, PANEL_ROWS, PANEL_COLS, SHAPE, S>(op(a.q, a.mp), op(a.x, a.np), K, at, a.tiles, lds, acc);
+  if (a.tiles.splits > 1) {
     const int64_t N = MODE == APPLY ? a.np : a.mp;
-    float *part = a.part + sp * a.mp * N;
-    tile::for_rows8<tile::F16K, S>(acc, lds, m0, n0, [&](int64_t m, int64_t n, float (&v)[8]) {
+    float *part = a.part + at.split * a.mp * N;
+    tile::for_rows8<tile::SPLITK, S>(acc, lds, at.m0, at.n0, [&](int64_t m, int64_t n, float (&v)[8]) {
       if (m < a.mp && n < N) store8f(part + m * N + n, true, 8, v);
     });
   } else {
-    tile::for_rows8<tile::F16K, S>(acc, lds, m0, n0, [&](int64_t m, int64_t n, float (&v)[8]) {
-      ns_finish8<MODE>(a, m, n, at.m != at.n, v);
+    tile::for_rows8<tile::SPLITK, S>(acc, lds, at.m0, at.n0, [&](int64_t m, int64_t n, float (&v)[8]) {
+      ns_finish8<MODE>(a, m, n, !at.diagonal, v);
     });
   }
 }
 
-template <int MODE, typename S>
+// The partial sums of a split contraction, added in order.  B: edge of the tiles, of which a symmetric
+// product has those on and above the diagonal.
+template <int MODE, int B>
 __global__ void __launch_bounds__(256) k_ns_join(NsArgs a) {
   const int64_t N = MODE == APPLY ? a.np : a.mp, groups = N / 8, all = a.mp * groups;
   for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
     const int64_t m = i / groups, n = i % groups * 8;
-    if (MODE != APPLY && m / S::BM > n / S::BN) continue;                      // stored with its mirror image
+    if (MODE != APPLY && m / B > n / B) continue;
     float v[8] = {}, t[8];
-    for (uint32_t s = 0; s < a.splits; ++s) {
+    for (uint32_t s = 0; s < a.tiles.splits; ++s) {
       load8f(a.part + (s * a.mp + m) * N + n, true, 8, t);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] += t[j];
     }
-    ns_finish8<MODE>(a, m, n, m / S::BM != n / S::BN, v);
+    ns_finish8<MODE>(a, m, n, m / B != n / B, v);
   }
 }
 
 // ----------------------------------------------------------------------------- host side
 
-using Large = tile::Shape<256, 256, 2, 4>;
-using Middle = tile::Shape<128, 128, 2, 2>;
-using Small = tile::Shape<64, 64, 2, 2>;
-
-struct NsPlan { int shape; uint32_t nm, nn, tiles, splits; int64_t steps; };
-NsPlan ns_plan(int64_t M, int64_t N, int64_t K, bool symmetric) {
-  auto tiles = [&](int64_t b) {
-    const int64_t r = (M + b - 1) / b, c = (N + b - 1) / b;
-    return symmetric ? r * (r + 1) / 2 : r * c;
-  };
-  NsPlan p{};
-  const int64_t b = tiles(256) >= 200 ? 256 : tiles(128) >= 200 ? 128 : 64;
-  p.shape = b == 256 ? 0 : b == 128 ? 1 : 2;
-  p.nm = uint32_t((M + b - 1) / b);
-  p.nn = uint32_t((N + b - 1) / b);
-  p.tiles = uint32_t(tiles(b));
-  const int64_t total = 3 * (K / 64);
-  int64_t splits = 1;
-  if (b == 64) splits = std::max<int64_t>(1, std::min<int64_t>(1024 / p.tiles, total / 8));
-  p.steps = (total + splits - 1) / splits;
-  p.splits = uint32_t((total + p.steps - 1) / p.steps);
-  return p;
-}
-
 struct NsSizes { int64_t m, n, mp, np, ldg, ldo, ldm; bool tall; };
-struct NsWs { size_t norm, x[2], p, q, part, total; NsPlan gram, poly, apply; };
+struct NsWs { size_t norm, x[2], p, q, part, total; tile::Plan gram, poly, apply; };
 
 int check_ortho(const fqt_ortho_desc *d, NsSizes *s) {
   if (!d) return FQT_E_NULL;
@@ -307,14 +280,14 @@ int check_ortho(const fqt_ortho_desc *d, NsSizes *s) {
   s->ldg = row_stride(d->ldg, d->cols);
   s->ldo = row_stride(d->ldo, d->cols);
   s->ldm = row_stride(d->ldm, d->cols);
-  if (!s->ldg || !s->ldo || !s->ldm) return FQT_E_SHAPE;
+  if (!s->ldg || !s->ldo || !s->ldm || s->m > 65536) return FQT_E_SHAPE;
   return FQT_OK;
 }
 NsWs ns_ws(const NsSizes &s) {
   NsWs w{};
-  w.gram = ns_plan(s.mp, s.mp, s.np, true);
-  w.poly = ns_plan(s.mp, s.mp, s.mp, true);
-  w.apply = ns_plan(s.mp, s.np, s.mp, false);
+  w.gram = tile::make_plan(s.mp, s.mp, s.np / 32, true);
+  w.poly = tile::make_plan(s.mp, s.mp, s.mp / 32, true);
+  w.apply = tile::make_plan(s.mp, s.np, s.mp / 32, false);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += align256(bytes); return o; };
   w.norm = take(NORM_BLOCKS * sizeof(double));
@@ -323,25 +296,23 @@ NsWs ns_ws(const NsSizes &s) {
   w.x[1] = take(x);
   w.p = take(p);
   w.q = take(p);
-  auto part = [&](const NsPlan &pl, size_t entries) { return pl.splits > 1 ? size_t(pl.splits) * entries * 4 : 0; };
+  auto part = [&](const tile::Plan &pl, size_t entries) { return pl.splits > 1 ? size_t(pl.splits) * entries * 4 : 0; };
   w.part = take(std::max({part(w.gram, s.mp * s.mp), part(w.poly, s.mp * s.mp), part(w.apply, s.mp * s.np)}));
   w.total = at;
   return w;
 }
 
 template <int MODE>
-int launch_ns(const NsPlan &pl, NsArgs a, hipStream_t st) {
-  a.nm = pl.nm; a.nn = pl.nn; a.tiles = pl.tiles; a.splits = pl.splits; a.steps = pl.steps;
-  auto go = [&]<typename S>(S) {
-    k_ns<MODE, S><<<dim3(pl.tiles * pl.splits), dim3(S::THREADS), 0, st>>>(a);
-    if (pl.splits > 1) {
+int launch_ns(const tile::Plan &plan, NsArgs a, hipStream_t st) {
+  tile::for_launches(plan, [&]<int SHAPE>(const tile::Tiles &t) {
+    a.tiles = t;
+    k_ns<MODE, SHAPE><<<dim3(tile::blocks_of(SHAPE, t)), dim3(tile::ShapeOf<SHAPE>::type::THREADS), 0, st>>>(a);
+    if (t.splits > 1) {
       const int64_t all = a.mp * (MODE == APPLY ? a.np : a.mp) / 8;
-      k_ns_join<MODE, S><<<dim3(std::min<int64_t>((all + 255) / 256, 4096)), dim3(256), 0, st>>>(a);
+      k_ns_join<MODE, tile::ShapeOf<SHAPE>::type::BM>
+          <<<dim3(std::min<int64_t>((all + 255) / 256, 4096)), dim3(256), 0, st>>>(a);
     }
-  };
-  if (pl.shape == 0) go(Large{});
-  else if (pl.shape == 1) go(Middle{});
-  else go(Small{});
+  });
   return last_launch_status();
 }
 
@@ -350,24 +321,20 @@ int run_ortho(const fqt_ortho_desc *d, const NsSizes &s, Source src, NsArgs a, v
   const NsWs w = ns_ws(s);
   if (ws_bytes < w.total) return FQT_E_WORKSPACE;
   char *base = static_cast<char *>(ws);
-  auto planes = [&](size_t at, size_t entries) {
-    uint16_t *p = reinterpret_cast<uint16_t *>(base + at);
-    return Planes{p, p + entries};
-  };
+  auto pairs = [&](size_t at) { return Pairs{reinterpret_cast<uint16_t *>(base + at), s.mp}; };
   double *norm = reinterpret_cast<double *>(base + w.norm);
-  const size_t xe = size_t(s.mp) * s.np, pe = size_t(s.mp) * s.mp;
-  Planes x = planes(w.x[0], xe), next = planes(w.x[1], xe);
+  Pairs x = pairs(w.x[0]), next = pairs(w.x[1]);
   const int64_t all = d->rows * d->cols;
   const int parts = int(std::min<int64_t>((all + 1023) / 1024, NORM_BLOCKS));
   k_ns_norm<<<dim3(parts), dim3(256), 0, st>>>(src, norm);
   FQT_TRY_(last_launch_status());
   const dim3 grid(s.np / 64, s.mp / 64);
-  if (s.tall) k_ns_start<true><<<grid, dim3(256), 0, st>>>(src, norm, parts, d->eps, x, s.np);
-  else k_ns_start<false><<<grid, dim3(256), 0, st>>>(src, norm, parts, d->eps, x, s.np);
+  if (s.tall) k_ns_start<true><<<grid, dim3(256), 0, st>>>(src, norm, parts, d->eps, x);
+  else k_ns_start<false><<<grid, dim3(256), 0, st>>>(src, norm, parts, d->eps, x);
   FQT_TRY_(last_launch_status());
   a.mp = s.mp; a.np = s.np; a.m = s.m; a.n = s.n;
-  a.p = planes(w.p, pe);
-  a.q = planes(w.q, pe);
+  a.p = pairs(w.p);
+  a.q = pairs(w.q);
   a.part = reinterpret_cast<float *>(base + w.part);
   a.ldo = s.ldo;
   a.o_dtype = d->o_dtype;

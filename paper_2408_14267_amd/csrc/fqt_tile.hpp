@@ -10,6 +10,13 @@
 // The order of the k's inside a fragment does not matter as long as both operands use the same, so
 // 8-bit fragments are simply the 16-byte pieces l / 16 and 4 + l / 16 of a 128-byte row.
 //
+// SPLIT operands hold float16 pairs hi + lo in panels: panel c has the columns 32 c ... 32 c + 31 of
+// all rows, 128 bytes a row, the 32 hi before the 32 lo.  A step is 32 columns; the two pieces of a
+// fragment are its hi and its lo, and three matrix instructions (hi hi, hi lo, lo hi) feed on them: half
+// the reads and loads of three products one after the other.  Panels make every load of a step
+// contiguous, along k (PANEL_ROWS) as well as across it (PANEL_COLS: LDS rows 0-31 are the hi, 32-63 the
+// lo of 32 k's).
+//
 // LDS swizzle (in 16-byte pieces, on the source side of the load, since a load to LDS writes the
 // 64 lanes' pieces in a row).  ROWS: piece c of row r at c ^ (r & 7), so that the 16 rows of a
 // fragment, 128 bytes apart, meet all banks.  COLS: piece c of row k at c ^ 2 f(k), f = k's low two
@@ -21,21 +28,23 @@
 namespace fqt {
 namespace tile {
 
-enum Kind { BF16K, F16K, I8K, E4M3K };
-enum Layout { ROWS, COLS };
+enum Kind { BF16K, SPLITK, I8K, E4M3K };
+enum Layout { ROWS, COLS, PANEL_ROWS, PANEL_COLS };
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
 typedef short i16x4 __attribute__((ext_vector_type(4)));
+typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
 constexpr int KB = 128;             // bytes of a row per contraction step
+constexpr bool by_rows(int layout) { return layout == ROWS || layout == PANEL_ROWS; }
 
 template <int KIND> struct Acc { typedef f32x4 type; };
 template <> struct Acc<I8K> { typedef i32x4 type; };
-template <int KIND> constexpr int elem_bytes = KIND == I8K || KIND == E4M3K ? 1 : 2;
+template <int KIND> constexpr int elem_bytes = KIND == I8K || KIND == E4M3K ? 1 : KIND == SPLITK ? 4 : 2;
 
 // acc += w-fragment (rows of the result tile) x x-fragment (columns) over one 128-byte step, from
 // the two 16-byte pieces of each.  Lane l of the result holds n = 4 (l / 16) + i, m = l % 16.
@@ -46,11 +55,11 @@ __device__ __forceinline__ void mma(typename Acc<KIND>::type &acc, const i32x4 (
     for (int s = 0; s < 2; ++s)
       acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[s]),
                                                     __builtin_bit_cast(bf16x8, x[s]), acc, 0, 0, 0);
-  } else if constexpr (KIND == F16K) {
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-      acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, w[s]),
-                                                   __builtin_bit_cast(f16x8, x[s]), acc, 0, 0, 0);
+  } else if constexpr (KIND == SPLITK) {
+    auto h = [](const i32x4 &v) { return __builtin_bit_cast(f16x8, v); };
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(h(w[0]), h(x[1]), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(h(w[1]), h(x[0]), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(h(w[0]), h(x[0]), acc, 0, 0, 0);
   } else if constexpr (KIND == I8K) {
 #pragma unroll
     for (int s = 0; s < 2; ++s) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[s], x[s], acc, 0, 0, 0);
@@ -62,7 +71,8 @@ __device__ __forceinline__ void mma(typename Acc<KIND>::type &acc, const i32x4 (
   }
 }
 
-// One operand as a kernel argument: `rows` x K elements, row stride ld bytes (of a k row in COLS).
+// One operand as a kernel argument: `rows` x K elements, row stride ld bytes (of a k row in COLS, of a
+// panel in PANEL_*).
 struct Operand {
   const char *p;
   int64_t ld;
@@ -74,66 +84,116 @@ __device__ __forceinline__ lds_char *lds_ptr(const char *p) {
   return (lds_char *)(uint32_t)(uintptr_t)p;
 }
 
+// 16 bytes per lane from r at `off` to lds + 16 lane (lds wave-uniform).
+__device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, char *lds, uint32_t off) {
+  __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds_ptr(lds), 16, off, 0, 0, 0);
+}
+
 // The loads of one operand's step: LINES rows of the tile, THREADS threads.
 template <int LAYOUT, int LINES, int THREADS>
 struct Loader {
   static constexpr int PIECES = LINES * KB / 16;          // 16-byte pieces of a step
   static constexpr int PER = PIECES / THREADS;
-  static constexpr int ROW_PIECES = LAYOUT == ROWS ? KB / 16 : LINES / 8;
+  static constexpr int ROW_PIECES = by_rows(LAYOUT) ? KB / 16 : LINES / 8;
   static_assert(PIECES % THREADS == 0, "whole pieces per thread");
   const char *base;      // first byte of the next step
   int64_t step;          // bytes from one step to the next
   uint32_t off[PER];     // byte offset of each piece from base, BUF_NONE past the operand
-  uint32_t kpos[PER];    // its position along k: bytes (ROWS) or rows (COLS)
+  uint32_t kpos[PER];    // its position along k: bytes (ROWS), rows (COLS); panels are whole steps
 
   // line0: the tile's first row.
   __device__ __forceinline__ void init(const Operand &o, int64_t line0) {
     if constexpr (LAYOUT == ROWS) {
       base = o.p + line0 * o.ld;
       step = KB;
-    } else {
+    } else if constexpr (LAYOUT == COLS) {
       base = o.p + line0 * 2;
       step = (KB / 2) * o.ld;
+    } else if constexpr (LAYOUT == PANEL_ROWS) {
+      base = o.p + line0 * KB;
+      step = o.ld;
+    } else {
+      base = o.p + line0 / 32 * o.ld;
+      step = 32 * KB;
     }
 #pragma unroll
     for (int j = 0; j < PER; ++j) {
       const uint32_t p = j * THREADS + threadIdx.x;
       const uint32_t row = p / ROW_PIECES, slot = p % ROW_PIECES;
-      if constexpr (LAYOUT == ROWS) {
+      if constexpr (by_rows(LAYOUT)) {
         const uint32_t piece = slot ^ (row & 7);
         // rows past the operand read its last one: their results are not stored
         const int64_t r = min(int64_t(row), o.rows - 1 - line0);
-        off[j] = uint32_t(r * o.ld) + piece * 16;
-        kpos[j] = piece * 16;
+        off[j] = uint32_t(r * (LAYOUT == ROWS ? o.ld : KB)) + piece * 16;
+        kpos[j] = LAYOUT == ROWS ? piece * 16 : 0;
       } else {
         const uint32_t f = (row & 3) | ((row >> 1) & 12);
         const uint32_t piece = slot ^ ((2 * f) & (ROW_PIECES - 1));
-        off[j] = line0 + int64_t(piece) * 8 < o.rows ? uint32_t(row * o.ld) + piece * 16 : BUF_NONE;
-        kpos[j] = row;
+        const bool in = line0 + int64_t(piece) * 8 < o.rows;
+        if constexpr (LAYOUT == COLS) {
+          off[j] = in ? uint32_t(row * o.ld) + piece * 16 : BUF_NONE;
+          kpos[j] = row;
+        } else {
+          off[j] = in ? piece / 4 * uint32_t(o.ld) + row % 32 * KB + row / 32 * (KB / 2) + piece % 4 * 16 : BUF_NONE;
+          kpos[j] = 0;
+        }
       }
     }
   }
   // left: bytes (ROWS) or rows (COLS) of the contraction that are left from here.  Pieces past it
   // are written as zeros.
+  template <int FROM, int TO>
   __device__ __forceinline__ void load(char *lds, int64_t left) {
-    const uint32_t lim = uint32_t(min(left, int64_t(KB)));
+    const uint32_t lim = uint32_t(max(int64_t(0), min(left, int64_t(KB))));
     const __amdgpu_buffer_rsrc_t r = buffer_of(base, 0x7FFFFFFFu);
     char *at = lds + wave_id() * 1024;
 #pragma unroll
-    for (int j = 0; j < PER; ++j)
-      __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds_ptr(at + j * THREADS * 16), 16,
-                                               kpos[j] < lim ? off[j] : BUF_NONE, 0, 0, 0);
-    base += step;
+    for (int j = FROM; j < TO; ++j)
+      load_to_lds(r, at + j * THREADS * 16, kpos[j] < lim ? off[j] : BUF_NONE);
+    if (TO == PER) base += step;
   }
 };
+
+__device__ __forceinline__ i16x4 read_tr(const char *p) {
+  typedef __attribute__((address_space(3))) i16x4 lds_v4;
+  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4 *)(uint32_t)(uintptr_t)p);
+}
+// Two fragments of a COLS operand by transposing reads, from the lane's addresses a and b, as one block
+// of assembly with its own wait.  For the builtin the compiler waits until every load to LDS in flight
+// has arrived, though those fill other buffers; where one tile's step has to hide the next one's loads
+// (run_tile) that costs more than the closer wait: 128 x 128 tiles of 8192 x 8192 x 4096 in 501 instead
+// of 566 us.
+template <int LINES>
+__device__ __forceinline__ void read_cols(const char *a, const char *b, i32x4 (&x)[2], i32x4 (&y)[2]) {
+  typedef int i32x2 __attribute__((ext_vector_type(2)));
+  i32x2 r[8];
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %8\n"
+      "ds_read_b64_tr_b16 %1, %8 offset:%10\n"
+      "ds_read_b64_tr_b16 %2, %8 offset:%11\n"
+      "ds_read_b64_tr_b16 %3, %8 offset:%12\n"
+      "ds_read_b64_tr_b16 %4, %9\n"
+      "ds_read_b64_tr_b16 %5, %9 offset:%10\n"
+      "ds_read_b64_tr_b16 %6, %9 offset:%11\n"
+      "ds_read_b64_tr_b16 %7, %9 offset:%12\n"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7])
+      : "v"((uint32_t)(uintptr_t)a), "v"((uint32_t)(uintptr_t)b), "i"(4 * LINES * 2), "i"(32 * LINES * 2),
+        "i"(36 * LINES * 2)
+      : "memory");
+  x[0] = __builtin_shufflevector(r[0], r[1], 0, 1, 2, 3);
+  x[1] = __builtin_shufflevector(r[2], r[3], 0, 1, 2, 3);
+  y[0] = __builtin_shufflevector(r[4], r[5], 0, 1, 2, 3);
+  y[1] = __builtin_shufflevector(r[6], r[7], 0, 1, 2, 3);
+}
 
 // Fragment reads of one operand's step by a wave: FRAGS tiles of 16 lines from line0.
 template <int LAYOUT, int LINES, int FRAGS>
 struct Reader {
-  uint32_t at[LAYOUT == ROWS ? 2 : FRAGS];
+  uint32_t at[by_rows(LAYOUT) ? 2 : FRAGS];
   __device__ __forceinline__ void init(uint32_t line0) {
     const uint32_t l = __lane_id();
-    if constexpr (LAYOUT == ROWS) {
+    if constexpr (by_rows(LAYOUT)) {
 #pragma unroll
       for (int s = 0; s < 2; ++s)
         at[s] = (line0 + l % 16) * KB + ((s * 4 + l / 16) ^ (l & 7)) * 16;
@@ -147,106 +207,216 @@ struct Reader {
       }
     }
   }
-  __device__ __forceinline__ void read(const char *lds, int i, i32x4 (&o)[2]) const {
-    if constexpr (LAYOUT == ROWS) {
+  // Fragments i ... i + N - 1.  WHOLE: COLS fragments come with their own wait (read_cols).
+  template <bool WHOLE, int N>
+  __device__ __forceinline__ void read(const char *lds, int i, i32x4 (&o)[N][2]) const {
+    if constexpr (by_rows(LAYOUT)) {
 #pragma unroll
-      for (int s = 0; s < 2; ++s) o[s] = *reinterpret_cast<const i32x4 *>(lds + at[s] + i * 16 * KB);
+      for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int s = 0; s < 2; ++s)
+          o[j][s] = *reinterpret_cast<const i32x4 *>(lds + at[s] + (i + j) * 16 * KB);
+    } else if constexpr (!WHOLE) {
+#pragma unroll
+      for (int j = 0; j < N; ++j)
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const char *p = lds + at[i + j] + s * 32 * LINES * 2;
+          const i16x8 c = __builtin_shufflevector(read_tr(p), read_tr(p + 4 * LINES * 2), 0, 1, 2, 3, 4, 5, 6, 7);
+          o[j][s] = __builtin_bit_cast(i32x4, c);
+        }
     } else {
+      static_assert(N % 2 == 0, "fragments in pairs");
 #pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        typedef __attribute__((address_space(3))) i16x4 lds_v4;
-        const char *p = lds + at[i] + s * 32 * LINES * 2;
-        const i16x4 a = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4 *)(uint32_t)(uintptr_t)p);
-        const i16x4 b = __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4 *)(uint32_t)(uintptr_t)(p + 4 * LINES * 2));
-        typedef short i16x8 __attribute__((ext_vector_type(8)));
-        const i16x8 c = __builtin_shufflevector(a, b, 0, 1, 2, 3, 4, 5, 6, 7);
-        o[s] = __builtin_bit_cast(i32x4, c);
-      }
+      for (int j = 0; j < N; j += 2) read_cols<LINES>(lds + at[i + j], lds + at[i + j + 1], o[j], o[j + 1]);
     }
   }
 };
 
-template <int BM_, int BN_, int WM_, int WN_>
+// The steps [t0, t1) of one operand.  Steps past the last are loaded as zeros without touching memory,
+// so that the count of loads in flight is the same in every step.
+template <int KIND, int LAYOUT, int LINES, int THREADS>
+struct Feed {
+  typedef Loader<LAYOUT, LINES, THREADS> L;
+  static constexpr int64_t STEP = KB / elem_bytes<KIND>;   // elements of a step
+  static constexpr int UNIT = LAYOUT == ROWS ? elem_bytes<KIND> : 1;
+  L g;
+  int64_t left, todo;      // elements from here on, steps to load
+  __device__ __forceinline__ void init(const Operand &o, int64_t K, int64_t line0, int64_t t0, int64_t t1) {
+    g.init(o, line0);
+    g.base += t0 * g.step;
+    left = K - t0 * STEP;
+    todo = t1 - t0;
+  }
+  template <int FROM = 0, int TO = L::PER>
+  __device__ __forceinline__ void load(char *lds) {
+    g.template load<FROM, TO>(lds, todo > 0 ? left * UNIT : 0);
+    if constexpr (TO == L::PER) {
+      --todo;
+      left -= STEP;
+    }
+  }
+};
+
+// BM x BN outputs by WM x WN waves, through BUFS step buffers.
+template <int BM_, int BN_, int WM_, int WN_, int BUFS_ = 2>
 struct Shape {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, BUFS = BUFS_;
   static constexpr int THREADS = 64 * WM * WN;
   static constexpr int TM = BM / WM, TN = BN / WN;        // outputs of a wave
   static constexpr int FM = TM / 16, FN = TN / 16;
   static constexpr int BUF = (BM + BN) * KB;              // bytes of one step
-  static constexpr int LDS = 2 * BUF;
+  static constexpr int LDS = BUFS * BUF;
 };
 
-// The accumulators of the tile at (m0, n0) over the steps [t0, t1) of the contraction (K: elements
-// of a row in all).  SEGS products are summed, product s from operands x[s] and w[s]: its steps
-// follow those of product s - 1.
-template <int KIND, int LX, int LW, typename S, int SEGS>
-__device__ __forceinline__ void run_tile(const Operand (&x)[SEGS], const Operand (&w)[SEGS], int64_t K,
-                                         int64_t m0, int64_t n0, int64_t t0, int64_t t1, char *lds,
-                                         typename Acc<KIND>::type (&acc)[S::FM][S::FN]) {
-  constexpr int64_t STEP = KB / elem_bytes<KIND>;          // elements of a step
-  const int64_t steps = (K + STEP - 1) / STEP;             // of one product
-  const uint32_t wave = wave_id();
-  const uint32_t wm = (wave / S::WN) * S::TM, wn = (wave % S::WN) * S::TN;
-  Reader<LX, S::BM, S::FM> rx;
-  Reader<LW, S::BN, S::FN> rw;
-  rx.init(wm);
-  rw.init(wn);
+// A barrier of the workgroup that waits for nothing else: what has to be complete is waited for by
+// name.
+__device__ __forceinline__ void barrier_only() {
+  __builtin_amdgcn_sched_barrier(0);
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_sched_barrier(0);
+}
+template <int N>
+__device__ __forceinline__ void wait_loads() {             // all but the last N loads are complete
+  __builtin_amdgcn_s_waitcnt((N & 15) | (N >> 4) << 14 | 0x0F70);
+}
+__device__ __forceinline__ void wait_lds() { __builtin_amdgcn_s_waitcnt(0xC07F); }
+
+template <int KIND, typename S>
+__device__ __forceinline__ void clear_acc(typename Acc<KIND>::type (&acc)[S::FM][S::FN]) {
 #pragma unroll
   for (int i = 0; i < S::FM; ++i)
 #pragma unroll
     for (int j = 0; j < S::FN; ++j) acc[i][j] = typename Acc<KIND>::type{};
-  if (t0 >= t1) return;
+}
 
-  Loader<LX, S::BM, S::THREADS> gx;
-  Loader<LW, S::BN, S::THREADS> gw;
-  int seg = 0;
-  int64_t t = t0;
-  if constexpr (SEGS > 1) {
-    seg = int(t / steps);
-    t -= seg * steps;
+// The accumulators of the tile at (m0, n0) over the steps [t0, t1) of the contraction.  BUFS - 1
+// steps are in flight; one barrier per step, after which the step is in LDS for everyone and the
+// buffer of the step before it is free.
+template <int KIND, int LX, int LW, typename S>
+__device__ __forceinline__ void run_tile(const Operand &x, const Operand &w, int64_t K,
+                                         int64_t m0, int64_t n0, int64_t t0, int64_t t1, char *lds,
+                                         typename Acc<KIND>::type (&acc)[S::FM][S::FN]) {
+  const uint32_t wave = wave_id();
+  Reader<LX, S::BM, S::FM> rx;
+  Reader<LW, S::BN, S::FN> rw;
+  rx.init((wave / S::WN) * S::TM);
+  rw.init((wave % S::WN) * S::TN);
+  clear_acc<KIND, S>(acc);
+  if (t0 >= t1) return;
+  Feed<KIND, LX, S::BM, S::THREADS> gx;
+  Feed<KIND, LW, S::BN, S::THREADS> gw;
+  gx.init(x, K, m0, t0, t1);
+  gw.init(w, K, n0, t0, t1);
+  constexpr int AHEAD = S::BUFS - 1, LOADS = gx.g.PER + gw.g.PER;
+#pragma unroll
+  for (int b = 0; b < AHEAD; ++b) {
+    gx.load(lds + b * S::BUF);
+    gw.load(lds + b * S::BUF + S::BM * KB);
   }
-  auto start = [&](int s, int64_t at) {
-    gx.init(x[s], m0);
-    gw.init(w[s], n0);
-    gx.base += at * gx.step;
-    gw.base += at * gw.step;
-  };
-  auto stage = [&](int buf) {
-    const int64_t left = K - t * STEP;                     // elements
-    char *p = lds + buf * S::BUF;
-    gx.load(p, LX == ROWS ? left * elem_bytes<KIND> : left);
-    gw.load(p + S::BM * KB, LW == ROWS ? left * elem_bytes<KIND> : left);
-    ++t;
-    if constexpr (SEGS > 1) {
-      if (t == steps && seg + 1 < SEGS) {
-        t = 0;
-        ++seg;
-        // (the operands of one product differ from the last one's in their addresses only)
-        gx.base = x[seg].p + (LX == ROWS ? m0 * x[0].ld : m0 * 2);
-        gw.base = w[seg].p + (LW == ROWS ? n0 * w[0].ld : n0 * 2);
-      }
-    }
-  };
-  start(seg, t);
-  stage(0);
-  int buf = 0;
+  char *at = lds, *to = lds + AHEAD * S::BUF;
+  auto next = [&](char *p) { return p == lds + (S::BUFS - 1) * S::BUF ? lds : p + S::BUF; };
   for (int64_t i = t0; i < t1; ++i) {
-    __builtin_amdgcn_s_waitcnt(0x0F70);                    // vmcnt(0): this step is in LDS
-    __syncthreads();                                       // ... everyone's, and the other buffer is free
-    if (i + 1 < t1) stage(buf ^ 1);
-    const char *p = lds + buf * S::BUF;
+    wait_loads<(AHEAD - 1) * LOADS>();
+    // (not barrier_only: matrix instructions of the last step may be issued behind the barrier)
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_barrier();
+    asm volatile("" ::: "memory");
+    gx.load(to);
+    gw.load(to + S::BM * KB);
     i32x4 fw[S::FN][2];
+    rw.template read<true>(at + S::BM * KB, 0, fw);
+    constexpr int XS = by_rows(LX) ? 1 : 2;                // x fragments read at a time
 #pragma unroll
-    for (int j = 0; j < S::FN; ++j) rw.read(p + S::BM * KB, j, fw[j]);
+    for (int k = 0; k < S::FM; k += XS) {
+      i32x4 fx[XS][2];
+      rx.template read<true>(at, k, fx);
 #pragma unroll
-    for (int k = 0; k < S::FM; ++k) {
-      i32x4 fx[2];
-      rx.read(p, k, fx);
+      for (int i = 0; i < XS; ++i)
 #pragma unroll
-      for (int j = 0; j < S::FN; ++j) mma<KIND>(acc[k][j], fw[j], fx);
+        for (int j = 0; j < S::FN; ++j) mma<KIND>(acc[k + i][j], fw[j], fx[i]);
     }
+    at = next(at);
+    to = next(to);
+  }
+  wait_loads<0>();
+  __syncthreads();                                         // LDS is free for the epilogue
+}
+
+// The same for workgroups of eight waves, two per SIMD, with 256 or so outputs a side: while one wave
+// of a SIMD issues matrix instructions, the other one reads fragments and starts loads.  Waves 4-7
+// run one barrier behind waves 0-3 for that.  A step is four quarters of a wave's tile, each a
+// reading phase and a matrix phase with a barrier after it:
+//   quarter   fragments read            step loaded (half of its pieces per quarter)
+//   0         x, first half             x of step t + 1, into the other buffer
+//   1         w, second half            x of step t + 1
+//   2         x, second half            w of step t + 2, into this buffer (w is read by now)
+//   3         w, first half, step t+1   w of step t + 2
+// so that w has four, x two to four quarters to arrive.  A wave waits for its own loads at the end of
+// the reading phase before the one that needs them, and the barrier between makes them everyone's.
+template <int KIND, int LX, int LW, typename S>
+__device__ __forceinline__ void run_tile8(const Operand &x, const Operand &w, int64_t K,
+                                          int64_t m0, int64_t n0, int64_t t0, int64_t t1, char *lds,
+                                          typename Acc<KIND>::type (&acc)[S::FM][S::FN]) {
+  static_assert(S::THREADS == 512 && S::FM % 2 == 0 && S::FN % 2 == 0 && S::BUFS == 2, "tiles in quarters");
+  constexpr int HM = S::FM / 2, HN = S::FN / 2;
+  const uint32_t wave = wave_id();
+  Reader<LX, S::BM, S::FM> rx;
+  Reader<LW, S::BN, S::FN> rw;
+  rx.init((wave / S::WN) * S::TM);
+  rw.init((wave % S::WN) * S::TN);
+  clear_acc<KIND, S>(acc);
+  if (t0 >= t1) return;
+  Feed<KIND, LX, S::BM, S::THREADS> gx;
+  Feed<KIND, LW, S::BN, S::THREADS> gw;
+  gx.init(x, K, m0, t0, t1);
+  gw.init(w, K, n0, t0, t1);
+  constexpr int NX = gx.g.PER, NW = gw.g.PER, NX0 = (NX + 1) / 2, NW0 = (NW + 1) / 2;
+  auto xbuf = [&](int b) { return lds + b * S::BUF; };
+  auto wbuf = [&](int b) { return lds + b * S::BUF + S::BM * KB; };
+  gw.load(wbuf(0));
+  gx.load(xbuf(0));
+  gw.load(wbuf(1));
+  wait_loads<NW>();
+  barrier_only();
+  i32x4 fx[HM][2], fa[HN][2], fb[HN][2], fn[HN][2];
+  rw.template read<false>(wbuf(0), 0, fn);
+  if (wave >= 4) barrier_only();
+  auto quarter = [&](int m, int n, i32x4 (&f)[HN][2]) {
+    wait_lds();
+    barrier_only();
+    __builtin_amdgcn_s_setprio(1);
+#pragma unroll
+    for (int i = 0; i < HM; ++i)
+#pragma unroll
+      for (int j = 0; j < HN; ++j) mma<KIND>(acc[m + i][n + j], f[j], fx[i]);
+    __builtin_amdgcn_s_setprio(0);
+    barrier_only();
+  };
+  int buf = 0;
+  for (int64_t t = t0; t < t1; ++t) {
+#pragma unroll
+    for (int j = 0; j < HN; ++j) fa[j][0] = fn[j][0], fa[j][1] = fn[j][1];
+    rx.template read<false>(xbuf(buf), 0, fx);
+    gx.template load<0, NX0>(xbuf(buf ^ 1));
+    quarter(0, 0, fa);
+    rw.template read<false>(wbuf(buf), HN, fb);
+    gx.template load<NX0, NX>(xbuf(buf ^ 1));
+    quarter(0, HN, fb);
+    rx.template read<false>(xbuf(buf), HM, fx);
+    gw.template load<0, NW0>(wbuf(buf));
+    wait_loads<NX + NW0>();                                // w of step t + 1
+    quarter(HM, HN, fb);
+    rw.template read<false>(wbuf(buf ^ 1), 0, fn);
+    gw.template load<NW0, NW>(wbuf(buf));
+    wait_loads<NW>();                                      // x of step t + 1
+    quarter(HM, 0, fa);
     buf ^= 1;
   }
+  if (wave < 4) barrier_only();
+  wait_loads<0>();
   __syncthreads();                                         // LDS is free for the epilogue
 }
 
@@ -286,17 +456,158 @@ __device__ __forceinline__ void for_rows8(const typename Acc<KIND>::type (&acc)[
   }
 }
 
-// Tile of workgroup b of nm x nn tiles.  Each XCD (b % 8) walks a contiguous run of the order below,
-// which goes down GROUP tiles of m before the next n, so that the tiles an XCD has in flight share
-// operand rows in its L2.
-struct TileAt { uint32_t m, n; };
-__device__ __forceinline__ TileAt tile_at(uint32_t b, uint32_t nm, uint32_t nn) {
-  constexpr uint32_t GROUP = 8;
-  const uint32_t total = nm * nn, q = total / XCDS, r = total % XCDS, x = b % XCDS;
-  const uint32_t s = x * q + min(x, r) + b / XCDS;
-  const uint32_t per = GROUP * nn, g = s / per, in = s % per;
-  const uint32_t rows = min(GROUP, nm - g * GROUP);
-  return {g * GROUP + in % rows, in / rows};
+// ----------------------------------------------------------------------------- plans
+// The shapes of a workgroup's tile.  us of a 128-byte step of the contraction, measured on bf16 with
+// one (two) workgroups per CU: Large 1.58; Middle 0.60 (0.90); Small 0.27 (0.40); Part 0.37.
+using Large = Shape<256, 256, 2, 4>;
+using Middle = Shape<128, 128, 2, 2>;
+using Small = Shape<64, 64, 2, 2, 4>;
+// An eighth of a Large tile, for the tiles that a last round of workgroups would leave most CUs idle
+// with: 32 Large tiles over 64 steps take 104 us, their 256 parts 29 us.
+using Part = Shape<128, 64, 4, 2, 5>;
+enum ShapeId { LARGE, MIDDLE, SMALL, PART };
+
+// One launch of a product: `count` tiles from tile `first` on, of an order over nm x nn tiles (those of
+// shape Large for Part) or, symmetric, over the tiles on and above the diagonal.
+struct Tiles {
+  uint32_t nm, nn, first, count;
+  uint32_t splits;         // parts of the contraction, each `steps` long
+  uint32_t steps;
+  int32_t symmetric;
+};
+struct Plan {
+  int shape[2];
+  Tiles t[2];
+  int launches;
+  uint32_t splits;
+};
+
+inline Plan make_plan(int64_t M, int64_t N, int64_t steps, bool symmetric) {
+  auto grid = [&](int64_t b) {
+    Tiles t{};
+    t.nm = uint32_t((M + b - 1) / b);
+    t.nn = uint32_t((N + b - 1) / b);
+    t.count = symmetric ? t.nm * (t.nm + 1) / 2 : t.nm * t.nn;
+    t.splits = 1;
+    t.steps = uint32_t(steps);
+    t.symmetric = symmetric;
+    return t;
+  };
+  Plan best{};
+  double cost = 1e30;
+  auto take = [&](double c, const Plan &p) {
+    if (c < cost) cost = c, best = p;
+  };
+  const double s = double(steps);
+  const double entries = double(M) * double(N) * (symmetric ? 0.5 : 1.0);
+  {
+    const Tiles t = grid(256);
+    const uint32_t tail = t.count % 256, rounds = t.count / 256;
+    Plan p{{LARGE, PART}, {t, t}, 1, 1};
+    take((rounds + (tail > 0)) * (1.58 * s + 6) + 3, p);
+    if (tail) {
+      const double parts = ((8 * tail + 255) / 256) * (0.37 * s + 4) + 3;
+      p.t[0].count = t.count - tail;
+      p.t[1].first = t.count - tail;
+      p.t[1].count = tail;
+      if (rounds == 0) {
+        p.shape[0] = PART;
+        p.t[0] = p.t[1];
+      } else {
+        p.launches = 2;
+      }
+      take(rounds * (1.58 * s + 6) + 3 + parts, p);
+    }
+  }
+  // `full` workgroups at a time; us of a step with one and with two of them on a CU
+  auto split = [&](int shape, int64_t b, uint32_t full, double one, double two) {
+    const Tiles g = grid(b);
+    for (int64_t n = 1; n <= 64 && (n == 1 || steps / n >= 4); n += n < 16 ? 1 : 8) {
+      Tiles t = g;
+      t.steps = uint32_t(std::max<int64_t>(1, (steps + n - 1) / n));
+      t.splits = uint32_t(std::max<int64_t>(1, (steps + t.steps - 1) / t.steps));
+      const uint32_t blocks = t.count * t.splits, rest = blocks % full;
+      double c = (blocks / full) * (two * t.steps + 5) + 3;
+      if (rest) c += (rest > 256 ? two : one) * t.steps + 5;
+      // the partial sums, written and read at 4 TB/s, and their launch
+      if (t.splits > 1) c += 4 + t.splits * entries * 8 / 4e6;
+      take(c, Plan{{shape, shape}, {t, t}, 1, t.splits});
+    }
+  };
+  split(LARGE, 256, 256, 1.58, 1.58);
+  split(MIDDLE, 128, 512, 0.60, 0.90);
+  split(SMALL, 64, 512, 0.27, 0.40);
+  return best;
+}
+
+// Where workgroup b of a launch works.
+struct Place {
+  int64_t m0, n0;
+  uint32_t split;
+  bool diagonal;           // of a symmetric product: the tile is its own mirror image
+};
+template <int SHAPE> struct ShapeOf;
+template <> struct ShapeOf<LARGE> { typedef Large type; };
+template <> struct ShapeOf<MIDDLE> { typedef Middle type; };
+template <> struct ShapeOf<SMALL> { typedef Small type; };
+template <> struct ShapeOf<PART> { typedef Part type; };
+
+// Each XCD (b % 8) walks a contiguous run of the order below, which goes down GROUP tiles of m before
+// the next n, so that the tiles an XCD has in flight share operand rows in its L2.
+template <int SHAPE>
+__device__ __forceinline__ Place place(const Tiles &t, uint32_t b) {
+  constexpr uint32_t PARTS = SHAPE == PART ? 8 : 1;
+  const uint32_t total = t.count * PARTS;
+  const uint32_t split = b / total;
+  b %= total;
+  const uint32_t q = total / XCDS, r = total % XCDS, x = b % XCDS;
+  uint32_t s = x * q + min(x, r) + b / XCDS;
+  const uint32_t part = s % PARTS;
+  s = s / PARTS + t.first;
+  uint32_t m, n;
+  if (t.symmetric) {       // by columns of the upper triangle
+    n = uint32_t((sqrtf(8.0f * float(s) + 1.0f) - 1.0f) * 0.5f);
+    while (n * (n + 1) / 2 > s) --n;
+    while ((n + 1) * (n + 2) / 2 <= s) ++n;
+    m = s - n * (n + 1) / 2;
+  } else {
+    constexpr uint32_t GROUP = 8;
+    const uint32_t per = GROUP * t.nn, g = s / per, in = s % per;
+    const uint32_t rows = min(GROUP, t.nm - g * GROUP);
+    m = g * GROUP + in % rows;
+    n = in / rows;
+  }
+  if constexpr (SHAPE == PART)
+    return {int64_t(m) * 256 + part / 4 * 128, int64_t(n) * 256 + part % 4 * 64, split, m == n};
+  typedef typename ShapeOf<SHAPE>::type S;
+  return {int64_t(m) * S::BM, int64_t(n) * S::BN, split, m == n};
+}
+// Workgroups of a launch.
+inline uint32_t blocks_of(int shape, const Tiles &t) { return t.count * t.splits * (shape == PART ? 8 : 1); }
+
+// The accumulators of a placed tile, by the loop that suits the shape.
+template <int KIND, int LX, int LW, int SHAPE, typename S>
+__device__ __forceinline__ void contract(const Operand &x, const Operand &w, int64_t K,
+                                         const Place &at, const Tiles &t, char *lds,
+                                         typename Acc<KIND>::type (&acc)[S::FM][S::FN]) {
+  constexpr int64_t STEP = KB / elem_bytes<KIND>;
+  const int64_t total = (K + STEP - 1) / STEP;
+  const int64_t t0 = int64_t(at.split) * t.steps, t1 = min(total, t0 + t.steps);
+  if constexpr (SHAPE == LARGE) run_tile8<KIND, LX, LW, S>(x, w, K, at.m0, at.n0, t0, t1, lds, acc);
+  else run_tile<KIND, LX, LW, S>(x, w, K, at.m0, at.n0, t0, t1, lds, acc);
+}
+// Calls f.template operator()<SHAPE>(tiles) for each launch of a plan.
+template <typename F>
+inline void for_launches(const Plan &p, F &&f) {
+  for (int i = 0; i < p.launches; ++i) {
+    if (p.t[i].count == 0) continue;
+    switch (p.shape[i]) {
+      case LARGE: f.template operator()<LARGE>(p.t[i]); break;
+      case MIDDLE: f.template operator()<MIDDLE>(p.t[i]); break;
+      case SMALL: f.template operator()<SMALL>(p.t[i]); break;
+      default: f.template operator()<PART>(p.t[i]);
+    }
+  }
 }
 
 }  // namespace tile
