@@ -97,34 +97,76 @@ __device__ __forceinline__ void store8(void *p, int64_t at, int dt, bool full, i
   else store8f(static_cast<float *>(p) + at, full, n, v);
 }
 
-// y of 8 consecutive n (v: the sums over k).
+// The epilogue of 8 consecutive n (tile::run_epilogue).
 template <int ACT>
-__device__ __forceinline__ void finish8(const Epilogue &e, int64_t m, int64_t n, float (&v)[8]) {
-  if (m >= e.M || n >= e.N) return;
-  const int cnt = int(min(e.N - n, int64_t(8)));
-  const bool eight = cnt == 8, full = eight && e.vec;
-  float t[8];
-  if (e.sx) {
-    const float s = e.sx[m];
-    load8f(e.sw + n, eight && aligned_g(e.sw), cnt, t);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] *= s * t[i];
+struct Finish {
+  static constexpr int DEPTH = 4;
+  struct Fetch {
+    uint32_t res[8];       // the residual: 8 float32, or 8 bf16 in the first four
+    float sx;
+  };
+  const Epilogue &e;
+  float sw[8], bias[8];
+  int cnt;                 // columns of the group that exist
+  bool full;
+  __device__ __forceinline__ Finish(const Epilogue &e_) : e(e_) {}
+  __device__ __forceinline__ void columns(int64_t n) {
+    cnt = int(max(int64_t(0), min(e.N - n, int64_t(8))));
+    full = cnt == 8 && e.vec;
+    if (e.sw) load8f(e.sw + n, cnt == 8 && aligned_g(e.sw), cnt, sw);
+    if (e.bias) load8f(e.bias + n, cnt == 8 && aligned_g(e.bias), cnt, bias);
   }
-  if (e.bias) {
-    load8f(e.bias + n, eight && aligned_g(e.bias), cnt, t);
+  __device__ __forceinline__ Fetch fetch(int64_t m, int64_t n) {
+    Fetch f;
+    if (m >= e.M || cnt == 0) return f;
+    if (e.sx) f.sx = e.sx[m];
+    if (e.res) {
+      const int64_t at = m * e.ldr + n;
+      if (e.y_dtype == FQT_BF16) {
+        const bf16 *p = static_cast<const bf16 *>(e.res) + at;
+        if (full) {
+          __builtin_memcpy(f.res, __builtin_assume_aligned(p, 16), 16);
+        } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += t[i];
+          for (int i = 0; i < 8; ++i) {
+            const uint32_t v = i < cnt ? p[i].v : 0;
+            f.res[i / 2] = i & 1 ? f.res[i / 2] | v << 16 : v;
+          }
+        }
+      } else {
+        const float *p = static_cast<const float *>(e.res) + at;
+        float t[8];
+        load8f(p, full, cnt, t);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) f.res[i] = __float_as_uint(t[i]);
+      }
+    }
+    return f;
   }
-  if (e.z) store8(e.z, m * e.ldz + n, e.y_dtype, full, cnt, v);
+  __device__ __forceinline__ void finish(int64_t m, int64_t n, float (&v)[8], const Fetch &f) {
+    if (m >= e.M || cnt == 0) return;
+    if (e.sx) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = activate<ACT>(v[i]);
-  if (e.res) {
-    load8(e.res, m * e.ldr + n, e.y_dtype, full, cnt, t);
+      for (int i = 0; i < 8; ++i) v[i] *= f.sx * sw[i];
+    }
+    if (e.bias) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] += t[i];
+      for (int i = 0; i < 8; ++i) v[i] += bias[i];
+    }
+    if (e.z) store8(e.z, m * e.ldz + n, e.y_dtype, full, cnt, v);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = activate<ACT>(v[i]);
+    if (e.res) {
+      const bool half = e.y_dtype == FQT_BF16;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const uint32_t two = f.res[i / 2];
+        v[i] += __uint_as_float(half ? (i & 1 ? two & 0xFFFF0000u : two << 16) : f.res[i]);
+      }
+    }
+    store8(e.y, m * e.ldy + n, e.y_dtype, full, cnt, v);
   }
-  store8(e.y, m * e.ldy + n, e.y_dtype, full, cnt, v);
-}
+};
 
 // ----------------------------------------------------------------------------- products
 
@@ -144,18 +186,10 @@ __global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_prod
   if (at.m0 >= p.M || at.n0 >= p.N) return;              // (parts of an edge tile)
   typename tile::Acc<KIND>::type acc[S::FM][S::FN];
   tile::contract<KIND, LX, LW, SHAPE, S>(p.x, p.w, p.K, at, p.tiles, lds, acc);
-  if (p.tiles.splits > 1) {
-    float *part = p.part + at.split * p.M * p.ldp;
-    tile::for_rows8<KIND, S>(acc, lds, at.m0, at.n0, [&](int64_t m, int64_t n, float (&v)[8]) {
-      if (m < p.M && n < p.ldp) store8f(part + m * p.ldp + n, true, 8, v);
-    });
-  } else {
-    with_act(e.act, [&]<int ACT>() {
-      tile::for_rows8<KIND, S>(acc, lds, at.m0, at.n0, [&](int64_t m, int64_t n, float (&v)[8]) {
-        finish8<ACT>(e, m, n, v);
-      });
-    });
-  }
+  if (p.tiles.splits > 1)
+    tile::run_epilogue<KIND, S>(acc, lds, at.m0, at.n0, tile::StorePart{p.part + at.split * p.M * p.ldp, p.M, p.ldp});
+  else
+    with_act(e.act, [&]<int ACT>() { tile::run_epilogue<KIND, S>(acc, lds, at.m0, at.n0, Finish<ACT>(e)); });
 }
 
 // The partial sums of a split contraction, added in order, through the epilogue.  part: rows of ldp
@@ -165,13 +199,18 @@ __global__ void __launch_bounds__(256) k_product_finish(Product p, Epilogue e) {
   with_act(e.act, [&]<int ACT>() {
     for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
       const int64_t m = i / groups, n = i % groups * 8;
-      float v[8] = {}, t[8];
+      Finish<ACT> f(e);
+      f.columns(n);
+      const auto q = f.fetch(m, n);
+      float v[8] = {};
+#pragma unroll 4
       for (uint32_t s = 0; s < p.tiles.splits; ++s) {
+        float t[8];
         load8f(p.part + (s * p.M + m) * p.ldp + n, true, 8, t);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] += t[j];
       }
-      finish8<ACT>(e, m, n, v);
+      f.finish(m, n, v, q);
     }
   });
 }

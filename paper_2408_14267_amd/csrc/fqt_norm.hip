@@ -69,6 +69,9 @@ __device__ __forceinline__ void reduce_row(float &ss, uint32_t &mx, float2 (*slo
   }
 }
 
+// Threads of a workgroup: four rows of a wave each, or one row of TPR threads.
+template <int TPR> constexpr int block_of = TPR == 64 ? 256 : TPR;
+
 // What a row's codes are multiplied by: T / max, in two factors so that a maximum near the smallest
 // float32 values does not overflow it.
 struct CodeScale { float pre, inv; };
@@ -80,95 +83,137 @@ __device__ __forceinline__ CodeScale code_scale(uint32_t mx, float top) {
   return c;
 }
 
-__device__ __forceinline__ void store_codes(uint8_t *q, int q_dtype, bool full, int n, const float (&v)[8]) {
-  uint32_t a, b;
-  if (q_dtype == FQT_I8) {
-    a = codes4<FQT_I8>(v[0], v[1], v[2], v[3]);
-    b = codes4<FQT_I8>(v[4], v[5], v[6], v[7]);
-  } else {
-    a = codes4<FQT_E4M3>(v[0], v[1], v[2], v[3]);
-    b = codes4<FQT_E4M3>(v[4], v[5], v[6], v[7]);
+// The columns of a thread.  VEC (rows start on 16 bytes and are multiples of 8 columns): group v of VPT
+// is 8 consecutive columns, all or none of which exist.  Otherwise it is 8 columns TPR apart, so that
+// the lanes of an access are neighbours there too.  Columns past the row's end are 0.
+template <int TPR, bool VEC>
+struct Columns {
+  int t, cols;
+  __device__ __forceinline__ int col(int v, int i) const { return VEC ? (v * TPR + t) * 8 + i : (v * 8 + i) * TPR + t; }
+  __device__ __forceinline__ bool some(int v) const { return col(v, 0) < cols; }
+};
+// 8 elements as they are stored: loaded early, widened where they are used.
+template <typename T>
+struct Raw8 {
+  uint32_t w[sizeof(T) * 2];
+  template <int TPR, bool VEC>
+  __device__ __forceinline__ void load(const T *row, const Columns<TPR, VEC> &c, int v) {
+    if constexpr (VEC) {
+      if (!c.some(v)) {
+#pragma unroll
+        for (uint32_t &x : w) x = 0;
+        return;
+      }
+      const uint4 *p = reinterpret_cast<const uint4 *>(row + c.col(v, 0));
+#pragma unroll
+      for (int j = 0; j < int(sizeof(T)) / 2; ++j) {
+        const uint4 u = p[j];
+        w[4 * j] = u.x; w[4 * j + 1] = u.y; w[4 * j + 2] = u.z; w[4 * j + 3] = u.w;
+      }
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const int k = c.col(v, i);
+        T e{};
+        if (k < c.cols) e = row[k];
+        if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(e);
+        else w[i / 2] = i & 1 ? w[i / 2] | uint32_t(e.v) << 16 : e.v;
+      }
+    }
   }
-  if (full) {
-    *reinterpret_cast<uint2 *>(q) = make_uint2(a, b);
+  __device__ __forceinline__ float get(int i) const {
+    if constexpr (sizeof(T) == 4) return __uint_as_float(w[i]);
+    else return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
+  }
+};
+template <typename T, int TPR, bool VEC>
+__device__ __forceinline__ void store_cols(T *row, const Columns<TPR, VEC> &c, int v, const float (&x)[8]) {
+  if constexpr (VEC) {
+    if (c.some(v)) store8f(row + c.col(v, 0), true, 8, x);
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (i < n) q[i] = uint8_t((i < 4 ? a : b) >> (8 * (i & 3)));
+      if (c.col(v, i) < c.cols) row[c.col(v, i)] = from_f32<T>(x[i]);
+  }
+}
+__device__ __forceinline__ uint2 codes8(int q_dtype, const float (&v)[8]) {
+  if (q_dtype == FQT_I8)
+    return make_uint2(codes4<FQT_I8>(v[0], v[1], v[2], v[3]), codes4<FQT_I8>(v[4], v[5], v[6], v[7]));
+  return make_uint2(codes4<FQT_E4M3>(v[0], v[1], v[2], v[3]), codes4<FQT_E4M3>(v[4], v[5], v[6], v[7]));
+}
+template <int TPR, bool VEC>
+__device__ __forceinline__ void store_codes(uint8_t *row, int q_dtype, const Columns<TPR, VEC> &c, int v, const float (&x)[8]) {
+  const uint2 q = codes8(q_dtype, x);
+  if constexpr (VEC) {
+    if (c.some(v)) *reinterpret_cast<uint2 *>(row + c.col(v, 0)) = q;
+  } else {
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (c.col(v, i) < c.cols) row[c.col(v, i)] = uint8_t((i < 4 ? q.x : q.y) >> (8 * (i & 3)));
   }
 }
 
 // One row per TPR threads, VPT groups of 8 columns per thread.  Workgroups walk the rows with g in
-// registers.
-template <typename XT, typename YT, int TPR, int VPT>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_norm_fwd(NormArgs a) {
-  constexpr int ROWS = TPR < 256 ? 256 / TPR : 1;
+// registers and the next row's loads under way.  4608 x 4096 bf16 with residual, sum, norm and codes
+// (170 MB): 28 us, at what a copy of these bytes reaches.
+template <typename XT, typename YT, int TPR, int VPT, bool VEC>
+__global__ void __launch_bounds__(block_of<TPR>) k_norm_fwd(NormArgs a) {
+  constexpr int ROWS = block_of<TPR> / TPR;
   __shared__ float2 slots[2][16];
-  const int t = threadIdx.x % TPR;
+  const Columns<TPR, VEC> c{int(threadIdx.x % TPR), a.cols};
   int half = 0;
   float g[VPT][8];
 #pragma unroll
-  for (int v = 0; v < VPT; ++v) {
-    const int c = (v * TPR + t) * 8, n = a.cols - c;
-    if (a.g) {
-      load8f(a.g + c, n >= 8 && aligned_g(a.g), n, g[v]);
-    } else {
+  for (int v = 0; v < VPT; ++v)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) g[v][i] = 1.0f;
-    }
-  }
-  for (int64_t row = int64_t(blockIdx.x) * ROWS + threadIdx.x / TPR; row < a.rows;
-       row += int64_t(gridDim.x) * ROWS) {
-    const XT *x = static_cast<const XT *>(a.x) + row * a.ldx;
-    const XT *r = static_cast<const XT *>(a.r) + row * a.ldr;
+    for (int i = 0; i < 8; ++i) g[v][i] = a.g && c.col(v, i) < a.cols ? a.g[c.col(v, i)] : 1.0f;
+  const int64_t stride = int64_t(gridDim.x) * ROWS;
+  int64_t row = int64_t(blockIdx.x) * ROWS + threadIdx.x / TPR;
+  Raw8<XT> nx[VPT], nr[VPT];
+  auto fetch = [&](int64_t at) {
+    if (at >= a.rows) return;
+#pragma unroll
+    for (int v = 0; v < VPT; ++v) nx[v].load(static_cast<const XT *>(a.x) + at * a.ldx, c, v);
+    if (a.r)
+#pragma unroll
+      for (int v = 0; v < VPT; ++v) nr[v].load(static_cast<const XT *>(a.r) + at * a.ldr, c, v);
+  };
+  fetch(row);
+  for (; row < a.rows; row += stride) {
     float h[VPT][8];
-#pragma unroll
-    for (int v = 0; v < VPT; ++v) {
-      const int c = (v * TPR + t) * 8, n = a.cols - c;
-      load8f(x + c, a.vec && n >= 8, n, h[v]);
-    }
-    if (a.r) {
-#pragma unroll
-      for (int v = 0; v < VPT; ++v) {
-        const int c = (v * TPR + t) * 8, n = a.cols - c;
-        float u[8];
-        load8f(r + c, a.vec && n >= 8, n, u);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) h[v][i] += u[i];
-      }
-    }
     float ss = 0.0f;
     uint32_t mx = 0;
 #pragma unroll
     for (int v = 0; v < VPT; ++v)
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
+        h[v][i] = nx[v].get(i);
+        if (a.r) h[v][i] += nr[v].get(i);
         ss = fmaf(h[v][i], h[v][i], ss);
         mx = max(mx, abs_bits(h[v][i] * g[v][i]));
       }
+    fetch(row + stride);
     reduce_row<TPR>(ss, mx, slots, half);
     const float rstd = a.norm ? 1.0f / sqrtf(ss / float(a.cols) + a.eps) : 1.0f;
-    if (t == 0) {
+    if (c.t == 0) {
       if (a.rstd) a.rstd[row] = rstd;
       if (a.scale) a.scale[row] = rstd * __uint_as_float(mx) / code_top(a.q_dtype);
     }
     const CodeScale cs = code_scale(mx, code_top(a.q_dtype));
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
-      const int c = (v * TPR + t) * 8, n = a.cols - c;
-      if (n <= 0) continue;
-      const bool full = a.vec && n >= 8;
-      if (a.h) store8f(static_cast<XT *>(a.h) + row * a.ldh + c, full, n, h[v]);
+      if (!c.some(v)) continue;
+      if (a.h) store_cols(static_cast<XT *>(a.h) + row * a.ldh, c, v, h[v]);
       if (a.q) {
         float u[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) u[i] = h[v][i] * g[v][i] * cs.pre * cs.inv;
-        store_codes(a.q + row * a.ldq + c, a.q_dtype, full, n, u);
+        store_codes(a.q + row * a.ldq, a.q_dtype, c, v, u);
       }
       if (a.y) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) h[v][i] = h[v][i] * rstd * g[v][i];
-        store8f(static_cast<YT *>(a.y) + row * a.ldy + c, full, n, h[v]);
+        store_cols(static_cast<YT *>(a.y) + row * a.ldy, c, v, h[v]);
       }
     }
   }
@@ -227,7 +272,15 @@ __global__ void __launch_bounds__(LONG_TPR) k_norm_fwd_long(NormArgs a) {
       if (a.q) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) u[i] = h[i] * g[i] * cs.pre * cs.inv;
-        store_codes(a.q + row * a.ldq + c, a.q_dtype, full, n, u);
+        const uint2 o = codes8(a.q_dtype, u);
+        uint8_t *q = a.q + row * a.ldq + c;
+        if (full) {
+          *reinterpret_cast<uint2 *>(q) = o;
+        } else {
+#pragma unroll
+          for (int i = 0; i < 8; ++i)
+            if (i < n) q[i] = uint8_t((i < 4 ? o.x : o.y) >> (8 * (i & 3)));
+        }
       }
       if (a.y) {
 #pragma unroll
@@ -251,59 +304,69 @@ struct NormBwdArgs {
   int32_t vec;
 };
 
-template <typename XT, typename YT, int TPR, int VPT>
-__global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_norm_bwd(NormBwdArgs a) {
-  constexpr int ROWS = TPR < 256 ? 256 / TPR : 1;
+// 8192 x 4096 bf16 with dres (269 MB): see the row shapes below for its time.
+template <typename XT, typename YT, int TPR, int VPT, bool VEC>
+__global__ void __launch_bounds__(block_of<TPR>) k_norm_bwd(NormBwdArgs a) {
+  constexpr int ROWS = block_of<TPR> / TPR;
   __shared__ float2 slots[2][16];
   __shared__ float merge[ROWS > 1 ? ROWS - 1 : 1][ROWS > 1 ? TPR * VPT * 8 : 1];
-  const int t = threadIdx.x % TPR;
+  const Columns<TPR, VEC> c{int(threadIdx.x % TPR), a.cols};
+  const int t = c.t;
   int half = 0;
-  float dg[VPT][8] = {};
-  for (int64_t row = int64_t(blockIdx.x) * ROWS + threadIdx.x / TPR; row < a.rows;
-       row += int64_t(gridDim.x) * ROWS) {
-    const XT *hp = static_cast<const XT *>(a.h) + row * a.ldh;
-    const YT *dyp = static_cast<const YT *>(a.dy) + row * a.ldy;
-    const XT *rp = static_cast<const XT *>(a.dres) + row * a.ldr;
-    const float rstd = a.rstd[row];
+  float dg[VPT][8] = {}, g[VPT][8];
+#pragma unroll
+  for (int v = 0; v < VPT; ++v)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) g[v][i] = c.col(v, i) < a.cols ? a.g[c.col(v, i)] : 0.0f;
+  const int64_t stride = int64_t(gridDim.x) * ROWS;
+  int64_t row = int64_t(blockIdx.x) * ROWS + threadIdx.x / TPR;
+  Raw8<XT> nh[VPT], nr[VPT];
+  Raw8<YT> ny[VPT];
+  float nrstd = 0.0f;
+  auto fetch = [&](int64_t at) {
+    if (at >= a.rows) return;
+    nrstd = a.rstd[at];
+#pragma unroll
+    for (int v = 0; v < VPT; ++v) {
+      nh[v].load(static_cast<const XT *>(a.h) + at * a.ldh, c, v);
+      ny[v].load(static_cast<const YT *>(a.dy) + at * a.ldy, c, v);
+    }
+    if (a.dres)
+#pragma unroll
+      for (int v = 0; v < VPT; ++v) nr[v].load(static_cast<const XT *>(a.dres) + at * a.ldr, c, v);
+  };
+  fetch(row);
+  for (; row < a.rows; row += stride) {
+    const float rstd = nrstd;
     float h[VPT][8], u[VPT][8];
+    Raw8<XT> r[VPT];
     float dot = 0.0f;
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
-      const int c = (v * TPR + t) * 8, n = a.cols - c;
-      load8f(hp + c, a.vec && n >= 8, n, h[v]);
-      load8f(dyp + c, a.vec && n >= 8, n, u[v]);
-    }
-#pragma unroll
-    for (int v = 0; v < VPT; ++v) {
-      const int c = (v * TPR + t) * 8, n = a.cols - c;
-      float g[8];
-      load8f(a.g + c, n >= 8 && aligned_g(a.g), n, g);
+      r[v] = nr[v];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        h[v][i] *= rstd;                                    // t
-        dg[v][i] = fmaf(u[v][i], h[v][i], dg[v][i]);
-        u[v][i] *= g[i];
+        h[v][i] = nh[v].get(i) * rstd;                      // t
+        const float d = ny[v].get(i);
+        dg[v][i] = fmaf(d, h[v][i], dg[v][i]);
+        u[v][i] = d * g[v][i];
         dot = fmaf(u[v][i], h[v][i], dot);
       }
     }
+    fetch(row + stride);
     uint32_t none = 0;
     reduce_row<TPR>(dot, none, slots, half);
     const float m = dot / float(a.cols);
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
-      const int c = (v * TPR + t) * 8, n = a.cols - c;
-      if (n <= 0) continue;
-      const bool full = a.vec && n >= 8;
+      if (!c.some(v)) continue;
       float d[8];
 #pragma unroll
-      for (int i = 0; i < 8; ++i) d[i] = rstd * (u[v][i] - h[v][i] * m);
-      if (a.dres) {
-        float e[8];
-        load8f(rp + c, full, n, e);
-#pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] += e[i];
+      for (int i = 0; i < 8; ++i) {
+        d[i] = rstd * (u[v][i] - h[v][i] * m);
+        if (a.dres) d[i] += r[v].get(i);
       }
-      store8f(static_cast<XT *>(a.dx) + row * a.ldx + c, full, n, d);
+      store_cols(static_cast<XT *>(a.dx) + row * a.ldx, c, v, d);
     }
   }
   if constexpr (ROWS > 1) {            // the rows' waves meet in LDS
@@ -325,8 +388,7 @@ __global__ void __launch_bounds__(TPR < 256 ? 256 : TPR) k_norm_bwd(NormBwdArgs 
   float *out = a.part + int64_t(blockIdx.x) * a.cols;
 #pragma unroll
   for (int v = 0; v < VPT; ++v) {
-    const int c = (v * TPR + t) * 8, n = a.cols - c;
-    if (n > 0) store8f(out + c, n >= 8 && (a.cols & 3) == 0, n, dg[v]);
+    store_cols(out, c, v, dg[v]);
   }
 }
 
@@ -412,20 +474,20 @@ __global__ void __launch_bounds__(256) k_norm_dg(const float *part, int32_t part
 // ----------------------------------------------------------------------------- host side
 
 // Calls f.template operator()<TPR, VPT>() with the smallest row shape that holds `cols`; false when
-// the row does not fit registers.  A wave per row up to 2048 columns (no barrier), then a workgroup.
+// the row does not fit registers.  A wave per row up to 1024 columns (no barrier), then a workgroup; 16
+// columns a thread leave registers for the next row's loads (32 a thread spill them).
+constexpr int FWD_MAX_COLS = 16384, BWD_MAX_COLS = 8192;
 template <int MAX_COLS, typename F>
 bool dispatch_row(int64_t cols, F &&f) {
-  const int64_t v = (cols + 7) / 8;
   if (cols > MAX_COLS) return false;
-  if (v <= 64) f.template operator()<64, 1>();
-  else if (v <= 128) f.template operator()<64, 2>();
-  else if (v <= 256) f.template operator()<64, 4>();
-  else if (v <= 512) f.template operator()<256, 2>();
-  else if (v <= 1024) f.template operator()<256, 4>();
-  else f.template operator()<512, 4>();
+  if (cols <= 512) f.template operator()<64, 1>();
+  else if (cols <= 1024) f.template operator()<64, 2>();
+  else if (cols <= 2048) f.template operator()<128, 2>();
+  else if (cols <= 4096) f.template operator()<256, 2>();
+  else if (cols <= 8192) f.template operator()<512, 2>();
+  else if constexpr (MAX_COLS > 8192) f.template operator()<1024, 2>();
   return true;
 }
-constexpr int FWD_MAX_COLS = 16384, BWD_MAX_COLS = 16384;
 
 template <typename F>
 void dispatch_xy(int xt, int yt, F &&f) {
@@ -464,9 +526,11 @@ int run_norm(const fqt_norm_desc *d, NormArgs a, hipStream_t st) {
           on16(a.y, a.ldy, ye) && (!a.q || (aligned(a.q, 8) && a.ldq % 8 == 0));
   dispatch_xy(d->x_dtype, d->y_dtype, [&]<typename XT, typename YT>() {
     if (!dispatch_row<FWD_MAX_COLS>(d->cols, [&]<int TPR, int VPT>() {
-          constexpr int ROWS = TPR < 256 ? 256 / TPR : 1;
-          const int64_t blocks = std::min<int64_t>((d->rows + ROWS - 1) / ROWS, 2048);
-          k_norm_fwd<XT, YT, TPR, VPT><<<dim3(blocks), dim3(TPR < 256 ? 256 : TPR), 0, st>>>(a);
+          constexpr int ROWS = block_of<TPR> / TPR;
+          const int64_t blocks = std::min<int64_t>((d->rows + ROWS - 1) / ROWS, 1024 * 512 / std::max(TPR, 256));
+          const dim3 block(block_of<TPR>);
+          if (a.vec && d->cols % 8 == 0) k_norm_fwd<XT, YT, TPR, VPT, true><<<dim3(blocks), block, 0, st>>>(a);
+          else k_norm_fwd<XT, YT, TPR, VPT, false><<<dim3(blocks), block, 0, st>>>(a);
         }))
       k_norm_fwd_long<XT, YT><<<dim3(std::min<int64_t>(d->rows, 512)), dim3(LONG_TPR), 0, st>>>(a);
   });
@@ -476,7 +540,7 @@ int run_norm(const fqt_norm_desc *d, NormArgs a, hipStream_t st) {
 // Workgroups of the backward = rows of partial sums.
 int64_t bwd_parts(int64_t rows, int64_t cols) {
   if (cols > BWD_MAX_COLS) return std::min<int64_t>(std::max<int64_t>(rows, 1), 64);
-  const int64_t per = cols <= 2048 ? 4 : 1;
+  const int64_t per = cols <= 1024 ? 4 : 1;     // rows of a workgroup at a time
   return std::min<int64_t>(std::max<int64_t>((rows + per - 1) / per, 1), 512);
 }
 
@@ -554,11 +618,13 @@ extern "C" int fqt_rmsnorm_backward(const fqt_norm_desc *d, const void *h, const
   a.rows = d->rows;
   a.cols = int32_t(d->cols);
   a.ldh = s.h; a.ldy = s.y; a.ldr = s.r; a.ldx = s.x;
-  a.vec = on16(h, s.h, xe) && on16(dy, s.y, ye) && on16(dres, s.r, xe) && on16(dx, s.x, xe);
+  a.vec = on16(h, s.h, xe) && on16(dy, s.y, ye) && on16(dres, s.r, xe) && on16(dx, s.x, xe) && aligned(ws, 16);
   const int64_t parts = bwd_parts(d->rows, d->cols);
   dispatch_xy(d->x_dtype, d->y_dtype, [&]<typename XT, typename YT>() {
     if (dispatch_row<BWD_MAX_COLS>(d->cols, [&]<int TPR, int VPT>() {
-          k_norm_bwd<XT, YT, TPR, VPT><<<dim3(parts), dim3(TPR < 256 ? 256 : TPR), 0, st>>>(a);
+          const dim3 block(block_of<TPR>);
+          if (a.vec && d->cols % 8 == 0) k_norm_bwd<XT, YT, TPR, VPT, true><<<dim3(parts), block, 0, st>>>(a);
+          else k_norm_bwd<XT, YT, TPR, VPT, false><<<dim3(parts), block, 0, st>>>(a);
         }))
       return;
     if (d->rows)

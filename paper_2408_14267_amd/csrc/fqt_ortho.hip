@@ -166,52 +166,62 @@ struct NsArgs {
   float keep, rate;      // w = keep w - rate X
 };
 
+// The epilogue of 8 consecutive n (tile::run_epilogue).  mirror: the group is stored transposed too.
 template <int MODE>
-__device__ __forceinline__ void ns_finish8(const NsArgs &a, int64_t m, int64_t n, bool mirror, float (&v)[8]) {
-  if constexpr (MODE == APPLY) {
-    if (m >= a.mp || n >= a.np) return;
-    float x[8];
-    load_split8(a.x, m, n, x);
+struct Finish {
+  static constexpr int DEPTH = MODE == GRAM ? 1 : 4;
+  struct Fetch { float x[MODE == GRAM ? 1 : 8]; };         // X, or P
+  const NsArgs &a;
+  bool mirror;
+  __device__ __forceinline__ bool in(int64_t m, int64_t n) const {
+    return m < a.mp && n < (MODE == APPLY ? a.np : a.mp);
+  }
+  __device__ __forceinline__ void columns(int64_t) {}
+  __device__ __forceinline__ Fetch fetch(int64_t m, int64_t n) {
+    Fetch f;
+    if constexpr (MODE != GRAM)
+      if (in(m, n)) load_split8(MODE == APPLY ? a.x : a.p, m, n, f.x);
+    return f;
+  }
+  __device__ __forceinline__ void finish(int64_t m, int64_t n, float (&v)[8], const Fetch &f) {
+    if (!in(m, n)) return;
+    if constexpr (MODE == APPLY) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = fmaf(NS_A, x[i], v[i] * 0x1p-13f);      // X' 2^15
-    if (!a.last) {
-      store_split8(a.next, m, n, v);
-      return;
-    }
-    if (m >= a.m) return;
-#pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      if (n + i >= a.n) break;
-      const int64_t at = a.tall ? (n + i) * a.ldo + m : m * a.ldo + n + i;
-      const float o = v[i] * (1.0f / X_UNIT);
-      if (a.w) a.w[at] = fmaf(a.keep, a.w[at], -a.rate * o);
-      else if (a.o_dtype == FQT_BF16) static_cast<bf16 *>(a.out)[at] = from_f32<bf16>(o);
-      else static_cast<float *>(a.out)[at] = o;
-    }
-  } else {
-    if (m >= a.mp || n >= a.mp) return;
-    const Pairs &to = MODE == GRAM ? a.p : a.q;
-    if constexpr (MODE == GRAM) {
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] *= 0x1p-16f;                            // P 2^14 of sums 2^30
-    } else {
-      float p[8];
-      load_split8(a.p, m, n, p);
-#pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = fmaf(NS_B * 0.5f, p[i], v[i] * (NS_C * 0x1p-15f));   // Q 2^13
-    }
-    store_split8(to, m, n, v);
-    if (mirror) {
+      for (int i = 0; i < 8; ++i) v[i] = fmaf(NS_A, f.x[i], v[i] * 0x1p-13f);  // X' 2^15
+      if (!a.last) {
+        store_split8(a.next, m, n, v);
+        return;
+      }
+      if (m >= a.m) return;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const Split s = split(v[i]);
-        uint16_t *q = to.at(n + i, m);
-        q[0] = s.hi;
-        q[32] = s.lo;
+        if (n + i >= a.n) break;
+        const int64_t at = a.tall ? (n + i) * a.ldo + m : m * a.ldo + n + i;
+        const float o = v[i] * (1.0f / X_UNIT);
+        if (a.w) a.w[at] = fmaf(a.keep, a.w[at], -a.rate * o);
+        else if (a.o_dtype == FQT_BF16) static_cast<bf16 *>(a.out)[at] = from_f32<bf16>(o);
+        else static_cast<float *>(a.out)[at] = o;
+      }
+    } else {
+      const Pairs &to = MODE == GRAM ? a.p : a.q;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        if constexpr (MODE == GRAM) v[i] *= 0x1p-16f;                          // P 2^14 of sums 2^30
+        else v[i] = fmaf(NS_B * 0.5f, f.x[i], v[i] * (NS_C * 0x1p-15f));       // Q 2^13
+      }
+      store_split8(to, m, n, v);
+      if (mirror) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          const Split s = split(v[i]);
+          uint16_t *q = to.at(n + i, m);
+          q[0] = s.hi;
+          q[32] = s.lo;
+        }
       }
     }
   }
-}
+};
 
 template <int MODE, int SHAPE>
 __global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_ns(NsArgs a) {
@@ -233,14 +243,9 @@ __global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_ns(N
     tile::contract<tile::SPLITK, PANEL_ROWS, PANEL_COLS, SHAPE, S>(op(a.q, a.mp), op(a.x, a.np), K, at, a.tiles, lds, acc);
   if (a.tiles.splits > 1) {
     const int64_t N = MODE == APPLY ? a.np : a.mp;
-    float *part = a.part + at.split * a.mp * N;
-    tile::for_rows8<tile::SPLITK, S>(acc, lds, at.m0, at.n0, [&](int64_t m, int64_t n, float (&v)[8]) {
-      if (m < a.mp && n < N) store8f(part + m * N + n, true, 8, v);
-    });
+    tile::run_epilogue<tile::SPLITK, S>(acc, lds, at.m0, at.n0, tile::StorePart{a.part + at.split * a.mp * N, a.mp, N});
   } else {
-    tile::for_rows8<tile::SPLITK, S>(acc, lds, at.m0, at.n0, [&](int64_t m, int64_t n, float (&v)[8]) {
-      ns_finish8<MODE>(a, m, n, !at.diagonal, v);
-    });
+    tile::run_epilogue<tile::SPLITK, S>(acc, lds, at.m0, at.n0, Finish<MODE>{a, !at.diagonal});
   }
 }
 
@@ -252,13 +257,17 @@ __global__ void __launch_bounds__(256) k_ns_join(NsArgs a) {
   for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
     const int64_t m = i / groups, n = i % groups * 8;
     if (MODE != APPLY && m / B > n / B) continue;
-    float v[8] = {}, t[8];
+    Finish<MODE> f{a, m / B != n / B};
+    const auto q = f.fetch(m, n);
+    float v[8] = {};
+#pragma unroll 4
     for (uint32_t s = 0; s < a.tiles.splits; ++s) {
+      float t[8];
       load8f(a.part + (s * a.mp + m) * N + n, true, 8, t);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] += t[j];
     }
-    ns_finish8<MODE>(a, m, n, m / B != n / B, v);
+    f.finish(m, n, v, q);
   }
 }
 

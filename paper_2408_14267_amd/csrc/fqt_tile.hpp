@@ -420,17 +420,37 @@ __device__ __forceinline__ void run_tile8(const Operand &x, const Operand &w, in
   __syncthreads();                                         // LDS is free for the epilogue
 }
 
-// Hands the wave's results to f(m, n, v): 8 consecutive n of one row m each, through the wave's own
-// 16 x TN patch of LDS, so that a row's stores cover whole lines.
-template <int KIND, typename S, typename F>
-__device__ __forceinline__ void for_rows8(const typename Acc<KIND>::type (&acc)[S::FM][S::FN], char *lds,
-                                          int64_t m0, int64_t n0, F &&f) {
+// Orders the LDS accesses of a wave's lanes for the compiler (the hardware keeps a wave's in order).
+__device__ __forceinline__ void wave_fence() {
+  __builtin_amdgcn_fence(__ATOMIC_RELEASE, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  __builtin_amdgcn_fence(__ATOMIC_ACQUIRE, "wavefront");
+}
+
+// Takes a wave's results through the epilogue e, 8 consecutive n of one row m at a time, by way of the
+// wave's own 16 x TN patch of LDS, so that a row's stores cover whole lines.  A lane keeps its columns:
+//   e.columns(n)              called first: what depends on the columns alone
+//   e.fetch(m, n)             what the epilogue reads for a group; DEPTH groups are under way, since
+//                             the latency of one after the other would cost as much as a third of a
+//                             product over 64 steps
+//   e.finish(m, n, v, f)      the group's sums v and its fetch f
+template <int KIND, typename S, typename E>
+__device__ __forceinline__ void run_epilogue(const typename Acc<KIND>::type (&acc)[S::FM][S::FN], char *lds,
+                                             int64_t m0, int64_t n0, E &&e) {
   constexpr int PITCH = S::TN + 4;                         // floats; rows shifted against the banks
   static_assert(S::WM * S::WN * 16 * PITCH * 4 <= S::LDS, "patches fit");
+  constexpr int PER_ROW = S::TN / 8, ROWS_AT_ONCE = 64 / PER_ROW, G = 16 / ROWS_AT_ONCE;
+  static_assert(PER_ROW * ROWS_AT_ONCE == 64 && G >= 1, "a lane keeps its columns");
+  typedef typename std::remove_reference_t<E>::Fetch Fetch;
+  constexpr int ALL = S::FM * G, DEPTH = ALL < std::remove_reference_t<E>::DEPTH ? ALL : std::remove_reference_t<E>::DEPTH;
   const uint32_t wave = wave_id(), l = __lane_id();
   float *patch = reinterpret_cast<float *>(lds) + wave * 16 * PITCH;
-  const int64_t mw = m0 + (wave / S::WN) * S::TM, nw = n0 + (wave % S::WN) * S::TN;
-  constexpr int GROUPS = 16 * S::TN / 8;                   // 8-element groups of the patch
+  const uint32_t r = l / PER_ROW, c = l % PER_ROW * 8;
+  const int64_t m = m0 + (wave / S::WN) * S::TM + r, n = n0 + (wave % S::WN) * S::TN + c;
+  e.columns(n);
+  Fetch q[DEPTH];
+#pragma unroll
+  for (int i = 0; i < DEPTH; ++i) q[i] = e.fetch(m + i * ROWS_AT_ONCE, n);
 #pragma unroll
   for (int k = 0; k < S::FM; ++k) {
 #pragma unroll
@@ -439,22 +459,34 @@ __device__ __forceinline__ void for_rows8(const typename Acc<KIND>::type (&acc)[
       *reinterpret_cast<float4 *>(patch + (l % 16) * PITCH + j * 16 + 4 * (l / 16)) =
           make_float4(float(a[0]), float(a[1]), float(a[2]), float(a[3]));
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_fence();
 #pragma unroll
-    for (int g = 0; g < (GROUPS + 63) / 64; ++g) {
-      const uint32_t q = g * 64 + l;
-      if (GROUPS % 64 && q >= GROUPS) break;
-      const uint32_t r = q / (S::TN / 8), c = q % (S::TN / 8) * 8;
+    for (int g = 0; g < G; ++g) {
+      const int i = k * G + g;
       float v[8];
-      const float4 a = *reinterpret_cast<const float4 *>(patch + r * PITCH + c);
-      const float4 b = *reinterpret_cast<const float4 *>(patch + r * PITCH + c + 4);
+      const float4 a = *reinterpret_cast<const float4 *>(patch + (g * ROWS_AT_ONCE + r) * PITCH + c);
+      const float4 b = *reinterpret_cast<const float4 *>(patch + (g * ROWS_AT_ONCE + r) * PITCH + c + 4);
       v[0] = a.x; v[1] = a.y; v[2] = a.z; v[3] = a.w;
       v[4] = b.x; v[5] = b.y; v[6] = b.z; v[7] = b.w;
-      f(mw + k * 16 + r, nw + c, v);
+      const Fetch f = q[i % DEPTH];
+      if (i + DEPTH < ALL) q[i % DEPTH] = e.fetch(m + (i + DEPTH) * ROWS_AT_ONCE, n);
+      e.finish(m + i * ROWS_AT_ONCE, n, v, f);
     }
-    __builtin_amdgcn_wave_barrier();
+    wave_fence();
   }
 }
+// Partial sums of a split contraction: rows of ld (a multiple of 8) floats.
+struct StorePart {
+  static constexpr int DEPTH = 1;
+  struct Fetch {};
+  float *part;
+  int64_t M, ld;
+  __device__ __forceinline__ void columns(int64_t) {}
+  __device__ __forceinline__ Fetch fetch(int64_t, int64_t) { return {}; }
+  __device__ __forceinline__ void finish(int64_t m, int64_t n, float (&v)[8], const Fetch &) {
+    if (m < M && n < ld) dense::store8f(part + m * ld + n, true, 8, v);
+  }
+};
 
 // ----------------------------------------------------------------------------- plans
 // The shapes of a workgroup's tile.  us of a 128-byte step of the contraction, measured on bf16 with

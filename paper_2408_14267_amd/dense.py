@@ -114,13 +114,19 @@ def ortho_desc(rows, cols, g_dtype=FQT_F32, o_dtype=FQT_F32, steps=5, eps=1e-7, 
 
 # ----------------------------------------------------------------------------- checks
 
+_device_of = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
 def _matrix(where, name, t, dtype, rows, cols, ld):
     """Raise unless t is the matrix that the descriptor describes (a kernel would read or write
     outside it)."""
     dt = _TORCH_OF.get(dtype)
+    if (t.dtype is dt and t.is_cuda and t.shape == (rows, cols) and
+            t.stride() == (ld or cols, 1) and t.get_device() == _device_of()):
+        return
     if t.dtype is not dt:
         raise ValueError(f"{where}: {name}: dtype {t.dtype} does not match the descriptor's {dt}")
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols:
+    if t.shape != (rows, cols):
         raise ValueError(f"{where}: {name}: shape {tuple(t.shape)}, the descriptor has "
                          f"({rows}, {cols})")
     if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) != (ld or cols)):
@@ -130,9 +136,12 @@ def _matrix(where, name, t, dtype, rows, cols, ld):
 
 
 def _vector(where, name, t, n):
+    if (t.dtype is torch.float32 and t.is_cuda and t.shape == (n,) and t.is_contiguous() and
+            t.get_device() == _device_of()):
+        return
     if t.dtype is not torch.float32:
         raise ValueError(f"{where}: {name}: dtype {t.dtype}, float32 is needed")
-    if t.dim() != 1 or t.shape[0] != n or (n > 1 and t.stride(0) != 1):
+    if t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{where}: {name}: shape {tuple(t.shape)}, strides {t.stride()}: "
                          f"{n} contiguous elements are needed")
     _device(where, name, t)
@@ -141,9 +150,8 @@ def _vector(where, name, t, n):
 def _device(where, name, t):
     if not t.is_cuda:
         raise ValueError(f"{where}: {name}: expected a device tensor, got one on {t.device}")
-    if t.get_device() != torch.cuda.current_device():
-        raise ValueError(f"{where}: {name}: on {t.device}, the current device is "
-                         f"{torch.cuda.current_device()}")
+    if t.get_device() != _device_of():
+        raise ValueError(f"{where}: {name}: on {t.device}, the current device is {_device_of()}")
 
 
 def _required(where, **tensors):
