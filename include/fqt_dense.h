@@ -122,7 +122,8 @@ int fqt_linear_backward(const fqt_linear_desc *desc, const void *x, const void *
  *   X_{i+1} = a X_i + (b P + c P^2) X_i,  P = X_i X_i^T,  (a, b, c) = (3.4445, -4.7750, 2.0315)
  * taken on the short side of u; steps of them bring the singular values of u near 1.  The products
  * run on the 16-bit matrix cores from operands split in two (22 bits and their rounding), with
- * float32 sums: results as from float32 products.  The shorter side is at most 65536. */
+ * float32 sums: results as from float32 products.  The shorter side is at most 65536, rows times cols
+ * below 2^34 (FQT_E_SHAPE otherwise). */
 typedef struct {
   int64_t rows, cols;
   int64_t ldg, ldo, ldm;              /* g; o and w; m                                           */

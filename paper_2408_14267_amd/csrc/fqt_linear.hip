@@ -101,6 +101,7 @@ __device__ __forceinline__ void store8(void *p, int64_t at, int dt, bool full, i
 template <int ACT>
 struct Finish {
   static constexpr int DEPTH = 4;
+  static constexpr bool MIRROR = false;
   struct Fetch {
     uint32_t res[8];       // the residual: 8 float32, or 8 bf16 in the first four
     float sx;

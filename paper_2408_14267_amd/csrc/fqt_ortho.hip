@@ -78,75 +78,101 @@ struct Source {
   int64_t rows, cols, ldg, ldm;
   int32_t g_dtype, nesterov;
   float momentum;
+  int32_t vec;           // rows of g and m start on 16 bytes
 };
-__device__ __forceinline__ float load_g(const Source &s, int64_t r, int64_t c) {
-  const int64_t at = r * s.ldg + c;
-  return s.g_dtype == FQT_BF16 ? to_f32(static_cast<const bf16 *>(s.g)[at]) : static_cast<const float *>(s.g)[at];
-}
-constexpr int NORM_BLOCKS = 512;
-
-// Updates the momentum and adds up u^2 in float64, a partial sum per workgroup.
-__global__ void __launch_bounds__(256) k_ns_norm(Source s, double *part) {
-  __shared__ double sums[4];
-  double sum = 0.0;
-  const int64_t all = s.rows * s.cols;
-  for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
-    const int64_t r = i / s.cols, c = i % s.cols;
-    float u = load_g(s, r, c);
-    if (s.m) {
-      float *m = s.m + r * s.ldm + c;
-      const float v = fmaf(s.momentum, *m, u);
-      *m = v;
-      u = s.nesterov ? fmaf(s.momentum, v, u) : v;
-    }
-    sum += double(u) * double(u);
-  }
+// u of 8 columns from c of row r, 0 past the matrix.  UPDATE: the momentum takes its step first.
+template <bool UPDATE>
+__device__ __forceinline__ void load_u(const Source &s, int64_t r, int64_t c, float (&u)[8]) {
+  const int n = int(min(s.cols - c, int64_t(8)));
+  if (r >= s.rows || n <= 0) {
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-  if ((threadIdx.x & 63) == 0) sums[threadIdx.x / 64] = sum;
+    for (int i = 0; i < 8; ++i) u[i] = 0.0f;
+    return;
+  }
+  const bool full = s.vec && n == 8;
+  if (!s.m || UPDATE || s.nesterov) {
+    const int64_t at = r * s.ldg + c;
+    if (s.g_dtype == FQT_BF16) load8f(static_cast<const bf16 *>(s.g) + at, full, n, u);
+    else load8f(static_cast<const float *>(s.g) + at, full, n, u);
+  }
+  if (s.m) {
+    float *p = s.m + r * s.ldm + c;
+    float m[8];
+    load8f(p, full, n, m);
+    if constexpr (UPDATE) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) m[i] = fmaf(s.momentum, m[i], u[i]);
+      store8f(p, full, n, m);
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) u[i] = s.nesterov ? fmaf(s.momentum, m[i], u[i]) : m[i];
+  }
+}
+constexpr int NORM_BLOCKS = 1024;
+
+__device__ __forceinline__ double block_sum(double v, double *slots) {        // of 256 threads
+#pragma unroll
+  for (int o = 1; o < 64; o <<= 1) v += __shfl_xor(v, o);
+  if ((threadIdx.x & 63) == 0) slots[threadIdx.x / 64] = v;
   __syncthreads();
-  if (threadIdx.x == 0) part[blockIdx.x] = sums[0] + sums[1] + sums[2] + sums[3];
+  return slots[0] + slots[1] + slots[2] + slots[3];
 }
 
-// X_0 = u / (|u| + eps) as pairs, zeros in the padding.  A workgroup takes a 64 x 64 tile of
-// X; tall matrices are transposed on the way.
-template <bool TALL>
-__global__ void __launch_bounds__(256) k_ns_start(Source s, const double *part, int32_t parts, float eps,
-                                                  Pairs x) {
-  __shared__ double sums[4];
-  __shared__ float t[64][65];
+// Updates the momentum and adds up u^2 in float64 (no overflow, no underflow), a partial sum per
+// workgroup; groups: 8-column groups of a row.
+__global__ void __launch_bounds__(256) k_ns_norm(Source s, FastDiv groups, uint32_t all, double *part) {
+  __shared__ double slots[4];
+  double sum = 0.0;
+  for (uint32_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += gridDim.x * 256) {
+    const uint32_t r = fdiv(i, groups);
+    float u[8];
+    load_u<true>(s, r, int64_t(i - r * groups.d) * 8, u);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) sum += double(u[j]) * double(u[j]);
+  }
+  sum = block_sum(sum, slots);
+  if (threadIdx.x == 0) part[blockIdx.x] = sum;
+}
+// 2^15 / (|u| + eps) from the partial sums.
+__device__ __forceinline__ float unit_scale(const double *part, int32_t parts, float eps, double *slots) {
   double sum = 0.0;
   for (int i = threadIdx.x; i < parts; i += 256) sum += part[i];
+  return float(double(X_UNIT) / (sqrt(block_sum(sum, slots)) + double(eps)));
+}
+// The 64 x 64 tile of X_0 2^15 at (x0, y0): put(row, column, 8 values) in the tile.  Tall matrices are
+// transposed on the way, through t.
+template <bool TALL, typename F>
+__device__ __forceinline__ void start_tile(const Source &s, float inv, int64_t x0, int64_t y0, float (*t)[65], F &&put) {
+  if constexpr (TALL) {
+    for (int i = threadIdx.x; i < 512; i += 256) {
+      float u[8];
+      load_u<false>(s, y0 + i / 8, x0 + i % 8 * 8, u);
 #pragma unroll
-  for (int o = 1; o < 64; o <<= 1) sum += __shfl_xor(sum, o);
-  if ((threadIdx.x & 63) == 0) sums[threadIdx.x / 64] = sum;
-  __syncthreads();
-  const double norm = sqrt(sums[0] + sums[1] + sums[2] + sums[3]);
-  const float inv = float(double(X_UNIT) / (norm + double(eps)));
-  const int64_t x0 = int64_t(blockIdx.y) * 64, y0 = int64_t(blockIdx.x) * 64;   // row and column of X
-  for (int i = threadIdx.x; i < 64 * 64; i += 256) {
-    const int a = i / 64, b = i % 64;                                          // b runs along u's columns
-    const int64_t r = (TALL ? y0 : x0) + a, c = (TALL ? x0 : y0) + b;
-    float u = 0.0f;
-    if (r < s.rows && c < s.cols) {
-      if (!s.m) {
-        u = load_g(s, r, c);
-      } else {
-        const float v = s.m[r * s.ldm + c];
-        u = s.nesterov ? fmaf(s.momentum, v, load_g(s, r, c)) : v;
-      }
+      for (int j = 0; j < 8; ++j) t[i % 8 * 8 + j][i / 8] = u[j] * inv;
     }
-    if constexpr (TALL) t[b][a] = u * inv;
-    else t[a][b] = u * inv;
+    __syncthreads();
   }
-  __syncthreads();
-  for (int i = threadIdx.x; i < 64 * 8; i += 256) {
-    const int a = i / 8, b = i % 8 * 8;
+  for (int i = threadIdx.x; i < 512; i += 256) {
     float v[8];
+    if constexpr (TALL) {
 #pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = t[a][b + j];
-    store_split8(x, x0 + a, y0 + b, v);
+      for (int j = 0; j < 8; ++j) v[j] = t[i / 8][i % 8 * 8 + j];
+    } else {
+      load_u<false>(s, x0 + i / 8, y0 + i % 8 * 8, v);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] *= inv;
+    }
+    put(i / 8, i % 8 * 8, v);
   }
+}
+// X_0 = u / (|u| + eps) as pairs, zeros in the padding.
+template <bool TALL>
+__global__ void __launch_bounds__(256) k_ns_start(Source s, const double *part, int32_t parts, float eps, Pairs x) {
+  __shared__ double slots[4];
+  __shared__ float t[TALL ? 64 : 1][65];
+  const float inv = unit_scale(part, parts, eps, slots);
+  const int64_t x0 = int64_t(blockIdx.y) * 64, y0 = int64_t(blockIdx.x) * 64;
+  start_tile<TALL>(s, inv, x0, y0, t, [&](int r, int c, const float (&v)[8]) { store_split8(x, x0 + r, y0 + c, v); });
 }
 
 // ----------------------------------------------------------------------------- products
@@ -166,13 +192,32 @@ struct NsArgs {
   float keep, rate;      // w = keep w - rate X
 };
 
-// The epilogue of 8 consecutive n (tile::run_epilogue).  mirror: the group is stored transposed too.
+// X' or its last form, 8 columns from n of row m: v is X' 2^15.
+__device__ __forceinline__ void store_result8(const NsArgs &a, int64_t m, int64_t n, const float (&v)[8]) {
+  if (m >= a.m) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if (n + i >= a.n) break;
+    const int64_t at = a.tall ? (n + i) * a.ldo + m : m * a.ldo + n + i;
+    const float o = v[i] * (1.0f / X_UNIT);
+    if (a.w) a.w[at] = fmaf(a.keep, a.w[at], -a.rate * o);
+    else if (a.o_dtype == FQT_BF16) static_cast<bf16 *>(a.out)[at] = from_f32<bf16>(o);
+    else static_cast<float *>(a.out)[at] = o;
+  }
+}
+// P 2^14 from sums 2^30; Q 2^13 from sums 2^28 and P 2^14; X' 2^15 from sums 2^28 and X 2^15.
+__device__ __forceinline__ float gram_of(float sum) { return sum * 0x1p-16f; }
+__device__ __forceinline__ float poly_of(float sum, float p) { return fmaf(NS_B * 0.5f, p, sum * (NS_C * 0x1p-15f)); }
+__device__ __forceinline__ float apply_of(float sum, float x) { return fmaf(NS_A, x, sum * 0x1p-13f); }
+
+// The epilogue of 8 consecutive n (tile::run_epilogue).  diagonal: the tile holds its own mirror image.
 template <int MODE>
 struct Finish {
   static constexpr int DEPTH = MODE == GRAM ? 1 : 4;
+  static constexpr bool MIRROR = MODE != APPLY;
   struct Fetch { float x[MODE == GRAM ? 1 : 8]; };         // X, or P
   const NsArgs &a;
-  bool mirror;
+  bool diagonal;
   __device__ __forceinline__ bool in(int64_t m, int64_t n) const {
     return m < a.mp && n < (MODE == APPLY ? a.np : a.mp);
   }
@@ -185,41 +230,17 @@ struct Finish {
   }
   __device__ __forceinline__ void finish(int64_t m, int64_t n, float (&v)[8], const Fetch &f) {
     if (!in(m, n)) return;
-    if constexpr (MODE == APPLY) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] = fmaf(NS_A, f.x[i], v[i] * 0x1p-13f);  // X' 2^15
-      if (!a.last) {
-        store_split8(a.next, m, n, v);
-        return;
-      }
-      if (m >= a.m) return;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if (n + i >= a.n) break;
-        const int64_t at = a.tall ? (n + i) * a.ldo + m : m * a.ldo + n + i;
-        const float o = v[i] * (1.0f / X_UNIT);
-        if (a.w) a.w[at] = fmaf(a.keep, a.w[at], -a.rate * o);
-        else if (a.o_dtype == FQT_BF16) static_cast<bf16 *>(a.out)[at] = from_f32<bf16>(o);
-        else static_cast<float *>(a.out)[at] = o;
-      }
-    } else {
-      const Pairs &to = MODE == GRAM ? a.p : a.q;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        if constexpr (MODE == GRAM) v[i] *= 0x1p-16f;                          // P 2^14 of sums 2^30
-        else v[i] = fmaf(NS_B * 0.5f, f.x[i], v[i] * (NS_C * 0x1p-15f));       // Q 2^13
-      }
-      store_split8(to, m, n, v);
-      if (mirror) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i) {
-          const Split s = split(v[i]);
-          uint16_t *q = to.at(n + i, m);
-          q[0] = s.hi;
-          q[32] = s.lo;
-        }
-      }
+    for (int i = 0; i < 8; ++i) {
+      if constexpr (MODE == GRAM) v[i] = gram_of(v[i]);
+      else if constexpr (MODE == POLY) v[i] = poly_of(v[i], f.x[i]);
+      else v[i] = apply_of(v[i], f.x[i]);
     }
+    if (MODE == APPLY && a.last) store_result8(a, m, n, v);
+    else store_split8(MODE == GRAM ? a.p : MODE == POLY ? a.q : a.next, m, n, v);
+  }
+  __device__ __forceinline__ void mirror(int64_t n, int64_t m, const float (&v)[8]) {
+    if (!diagonal && in(m, n)) store_split8(MODE == GRAM ? a.p : a.q, n, m, v);
   }
 };
 
@@ -245,30 +266,239 @@ __global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_ns(N
     const int64_t N = MODE == APPLY ? a.np : a.mp;
     tile::run_epilogue<tile::SPLITK, S>(acc, lds, at.m0, at.n0, tile::StorePart{a.part + at.split * a.mp * N, a.mp, N});
   } else {
-    tile::run_epilogue<tile::SPLITK, S>(acc, lds, at.m0, at.n0, Finish<MODE>{a, !at.diagonal});
+    tile::run_epilogue<tile::SPLITK, S>(acc, lds, at.m0, at.n0, Finish<MODE>{a, at.diagonal});
   }
 }
 
-// The partial sums of a split contraction, added in order.  B: edge of the tiles, of which a symmetric
-// product has those on and above the diagonal.
-template <int MODE, int B>
+// The partial sums of a split contraction, added in order.  APPLY: a thread per 8 columns.
 __global__ void __launch_bounds__(256) k_ns_join(NsArgs a) {
-  const int64_t N = MODE == APPLY ? a.np : a.mp, groups = N / 8, all = a.mp * groups;
+  const int64_t groups = a.np / 8, all = a.mp * groups;
   for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
     const int64_t m = i / groups, n = i % groups * 8;
-    if (MODE != APPLY && m / B > n / B) continue;
-    Finish<MODE> f{a, m / B != n / B};
+    Finish<APPLY> f{a, false};
     const auto q = f.fetch(m, n);
     float v[8] = {};
 #pragma unroll 4
     for (uint32_t s = 0; s < a.tiles.splits; ++s) {
       float t[8];
-      load8f(a.part + (s * a.mp + m) * N + n, true, 8, t);
+      load8f(a.part + (s * a.mp + m) * a.np + n, true, 8, t);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] += t[j];
     }
     f.finish(m, n, v, q);
   }
+}
+// The symmetric products: a workgroup per 64 x 64 tile on or above the diagonal of tiles of edge B, whose
+// mirror image goes out through LDS (4096 x 4096, 8 splits: see the step's times in the launches).
+template <int MODE, int B>
+__global__ void __launch_bounds__(256) k_ns_join_symmetric(NsArgs a) {
+  __shared__ float t[64][65];
+  const int64_t m0 = int64_t(blockIdx.y) * 64, n0 = int64_t(blockIdx.x) * 64;
+  if (m0 / B > n0 / B) return;
+  Finish<MODE> f{a, m0 / B == n0 / B};
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int r = (h * 256 + threadIdx.x) / 8, c = threadIdx.x % 8 * 8;
+    const auto q = f.fetch(m0 + r, n0 + c);
+    float v[8] = {};
+#pragma unroll 4
+    for (uint32_t s = 0; s < a.tiles.splits; ++s) {
+      float u[8];
+      load8f(a.part + (s * a.mp + m0 + r) * a.mp + n0 + c, true, 8, u);
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] += u[j];
+    }
+    f.finish(m0 + r, n0 + c, v, q);
+#pragma unroll
+    for (int j = 0; j < 8; ++j) t[r][c + j] = v[j];
+  }
+  if (f.diagonal) return;
+  __syncthreads();
+#pragma unroll
+  for (int h = 0; h < 2; ++h) {
+    const int n = (h * 256 + threadIdx.x) / 8, m = threadIdx.x % 8 * 8;
+    float v[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) v[j] = t[m + j][n];
+    f.mirror(n0 + n, m0 + m, v);
+  }
+}
+
+// ----------------------------------------------------------------------------- few rows
+// Up to 64 rows: a launch per step instead of three or four.  Workgroup b keeps columns
+// [b slice, (b + 1) slice) of X.  It adds up everyone's partial sums of P (in order), takes Q from it in
+// LDS, and goes over its columns 64 at a time: X' = a X + Q X, and its part of the next P = X' X'^T.
+// All operands are 64 rows of 128 bytes per 32 columns, swizzled as fqt_tile.hpp says.
+struct SmallArgs {
+  NsArgs n;
+  const float *from;     // [workgroups][64][64] partial sums of P 2^30
+  float *to;
+  int64_t slice;         // columns of a workgroup, a multiple of 64
+};
+constexpr int PANEL = 64 * tile::KB;                       // bytes of 32 columns
+constexpr int SMALL_BLOCKS = 32;                           // at most; each reads all partial sums
+
+// Byte offset of columns n ... (8-byte steps) of row m of a matrix of row panels, plane hi or lo.
+__device__ __forceinline__ uint32_t panel_at(uint32_t m, uint32_t n, int lo) {
+  return n / 32 * PANEL + m * tile::KB + (((n % 32 / 8 + 4 * lo) ^ (m & 7)) * 16) + (n & 7) * 2;
+}
+__device__ __forceinline__ void put4(char *lds, uint32_t m, uint32_t n, const float (&v)[4]) {
+  Split s[4];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s[i] = split(v[i]);
+  *reinterpret_cast<uint2 *>(lds + panel_at(m, n, 0)) = make_uint2(s[0].hi | uint32_t(s[1].hi) << 16, s[2].hi | uint32_t(s[3].hi) << 16);
+  *reinterpret_cast<uint2 *>(lds + panel_at(m, n, 1)) = make_uint2(s[0].lo | uint32_t(s[1].lo) << 16, s[2].lo | uint32_t(s[3].lo) << 16);
+}
+__device__ __forceinline__ void join4(const char *hi, const char *lo, float (&v)[4]) {
+  const uint2 h = *reinterpret_cast<const uint2 *>(hi), l = *reinterpret_cast<const uint2 *>(lo);
+  v[0] = join(uint16_t(h.x), uint16_t(l.x));
+  v[1] = join(uint16_t(h.x >> 16), uint16_t(l.x >> 16));
+  v[2] = join(uint16_t(h.y), uint16_t(l.y));
+  v[3] = join(uint16_t(h.y >> 16), uint16_t(l.y >> 16));
+}
+typedef tile::f32x4 SmallAcc[2][2];
+// acc += x w^T over 64 k's; LW: PANEL_ROWS (rows of w along k) or PANEL_COLS (two steps of 32 k's).
+template <int LW>
+__device__ __forceinline__ void small_product(const char *x, const char *w, uint32_t wm, uint32_t wn, SmallAcc &acc) {
+  tile::Reader<PANEL_ROWS, 64, 2> rx;
+  tile::Reader<LW, 64, 2> rw;
+  rx.init(wm);
+  rw.init(wn);
+#pragma unroll
+  for (int s = 0; s < 2; ++s) {
+    tile::i32x4 fx[2][2], fw[2][2];
+    rx.template read<true>(x + s * PANEL, 0, fx);
+    rw.template read<true>(w + s * PANEL, 0, fw);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) tile::mma<tile::SPLITK>(acc[i][j], fw[j], fx[i]);
+  }
+}
+__device__ __forceinline__ void store_small_part(const SmallAcc &acc, uint32_t wm, uint32_t wn, float *to) {
+  const uint32_t l = __lane_id();
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int j = 0; j < 2; ++j)
+      *reinterpret_cast<tile::f32x4 *>(to + (wm + i * 16 + l % 16) * 64 + wn + j * 16 + 4 * (l / 16)) = acc[i][j];
+}
+// 64 columns of row panels between LDS and X (at column n).
+__device__ __forceinline__ void panels_out(const char *lds, const Pairs &x, int64_t n) {
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const uint32_t p = k * 256 + threadIdx.x, panel = p / 512, m = p / 8 % 64, piece = p % 8;
+    const uint4 v = *reinterpret_cast<const uint4 *>(lds + panel * PANEL + m * tile::KB + ((piece ^ (m & 7)) * 16));
+    *reinterpret_cast<uint4 *>(x.p + ((n / 32 + panel) * 64 + m) * 64 + piece * 8) = v;
+  }
+}
+
+// X_0 and its partial sums of P.
+template <bool TALL>
+__global__ void __launch_bounds__(256) k_ns_small_start(Source s, const double *norm, int32_t parts, float eps, SmallArgs a) {
+  __shared__ double slots[4];
+  __shared__ float t[TALL ? 64 : 1][65];
+  __shared__ __attribute__((aligned(16))) char x[2 * PANEL];
+  const float inv = unit_scale(norm, parts, eps, slots);
+  const uint32_t wave = wave_id(), wm = wave / 2 * 32, wn = wave % 2 * 32;
+  SmallAcc acc{};
+  const int64_t end = min(a.n.np, (blockIdx.x + 1) * a.slice);
+  for (int64_t n0 = blockIdx.x * a.slice; n0 < end; n0 += 64) {
+    start_tile<TALL>(s, inv, 0, n0, t, [&](int r, int c, const float (&v)[8]) {
+      const float lo[4] = {v[0], v[1], v[2], v[3]}, hi[4] = {v[4], v[5], v[6], v[7]};
+      put4(x, r, c, lo);
+      put4(x, r, c + 4, hi);
+    });
+    __syncthreads();
+    panels_out(x, a.n.x, n0);
+    small_product<PANEL_ROWS>(x, x, wm, wn, acc);
+    __syncthreads();
+  }
+  store_small_part(acc, wm, wn, a.to + int64_t(blockIdx.x) * 4096);
+}
+
+__global__ void __launch_bounds__(256) k_ns_small(SmallArgs a, int32_t blocks) {
+  __shared__ __attribute__((aligned(16))) char p[2 * PANEL], q[2 * PANEL], x[2 * PANEL], y[2 * PANEL];
+  const uint32_t wave = wave_id(), l = __lane_id(), wm = wave / 2 * 32, wn = wave % 2 * 32;
+  const int64_t n_first = blockIdx.x * a.slice, end = min(a.n.np, n_first + a.slice);
+  // X is read along its rows' order (m is the contraction)
+  const Operand xo{reinterpret_cast<const char *>(a.n.x.p), 64 * tile::KB, a.n.np};
+  auto load_x = [&](int64_t n0) {
+    tile::Loader<PANEL_COLS, 64, 256> g;
+    g.init(xo, n0);
+    g.template load<0, 2>(x, 1);
+    g.template load<0, 2>(x + PANEL, 1);
+  };
+  load_x(n_first);
+  {
+    float v[4][4] = {};
+#pragma unroll 4
+    for (int b = 0; b < blocks; ++b)
+#pragma unroll
+      for (int k = 0; k < 4; ++k) {
+        const tile::f32x4 u = *reinterpret_cast<const tile::f32x4 *>(a.from + b * 4096 + (k * 256 + threadIdx.x) * 4);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[k][i] += u[i];
+      }
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      const uint32_t at = (k * 256 + threadIdx.x) * 4;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) v[k][i] = gram_of(v[k][i]);
+      put4(p, at / 64, at % 64, v[k]);
+    }
+  }
+  __syncthreads();
+  {
+    SmallAcc acc{};
+    small_product<PANEL_ROWS>(p, p, wm, wn, acc);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t m = wm + i * 16 + l % 16, n = wn + j * 16 + 4 * (l / 16);
+        float o[4], v[4];
+        join4(p + panel_at(m, n, 0), p + panel_at(m, n, 1), o);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = poly_of(acc[i][j][k], o[k]);
+        put4(q, m, n, v);
+      }
+  }
+  SmallAcc gram{};
+  for (int64_t n0 = n_first; n0 < end; n0 += 64) {
+    __builtin_amdgcn_s_waitcnt(0x0F70);                    // vmcnt(0): x has arrived
+    __syncthreads();
+    SmallAcc acc{};
+    small_product<PANEL_COLS>(q, x, wm, wn, acc);
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int j = 0; j < 2; ++j) {
+        const uint32_t m = wm + i * 16 + l % 16, n = wn + j * 16 + 4 * (l / 16);
+        // X in the layout of its transposing reads: row m % 32 (hi), 32 + m % 32 (lo) of step m / 32
+        const uint32_t f = (m & 3) | ((m >> 1) & 12);       // (the same for both: bit 5 is not in it)
+        const char *at = x + m / 32 * PANEL + m % 32 * tile::KB + ((n / 8 ^ (2 * f & 7)) * 16) + (n & 7) * 2;
+        float o[4], v[4];
+        join4(at, at + 32 * tile::KB, o);
+#pragma unroll
+        for (int k = 0; k < 4; ++k) v[k] = apply_of(acc[i][j][k], o[k]);
+        if (a.n.last) {
+          float r[8] = {v[0], v[1], v[2], v[3]};
+          NsArgs cut = a.n;
+          cut.n = min(a.n.n, n0 + n + 4);
+          store_result8(cut, m, n0 + n, r);
+        } else {
+          put4(y, m, n, v);
+        }
+      }
+    __syncthreads();
+    if (n0 + 64 < end) load_x(n0 + 64);
+    if (!a.n.last) {
+      panels_out(y, a.n.next, n0);
+      small_product<PANEL_ROWS>(y, y, wm, wn, gram);
+    }
+  }
+  if (!a.n.last) store_small_part(gram, wm, wn, a.to + int64_t(blockIdx.x) * 4096);
 }
 
 // ----------------------------------------------------------------------------- host side
@@ -289,7 +519,9 @@ int check_ortho(const fqt_ortho_desc *d, NsSizes *s) {
   s->ldg = row_stride(d->ldg, d->cols);
   s->ldo = row_stride(d->ldo, d->cols);
   s->ldm = row_stride(d->ldm, d->cols);
-  if (!s->ldg || !s->ldo || !s->ldm || s->m > 65536) return FQT_E_SHAPE;
+  // (the norm counts groups of 8 columns in 31 bits)
+  if (!s->ldg || !s->ldo || !s->ldm || s->m > 65536 || d->rows * ((d->cols + 7) / 8) >= int64_t(1) << 31)
+    return FQT_E_SHAPE;
   return FQT_OK;
 }
 NsWs ns_ws(const NsSizes &s) {
@@ -305,6 +537,11 @@ NsWs ns_ws(const NsSizes &s) {
   w.x[1] = take(x);
   w.p = take(p);
   w.q = take(p);
+  if (s.mp == 64) {        // two sets of partial sums of P
+    w.part = take(2 * SMALL_BLOCKS * 4096 * sizeof(float));
+    w.total = at;
+    return w;
+  }
   auto part = [&](const tile::Plan &pl, size_t entries) { return pl.splits > 1 ? size_t(pl.splits) * entries * 4 : 0; };
   w.part = take(std::max({part(w.gram, s.mp * s.mp), part(w.poly, s.mp * s.mp), part(w.apply, s.mp * s.np)}));
   w.total = at;
@@ -317,9 +554,10 @@ int launch_ns(const tile::Plan &plan, NsArgs a, hipStream_t st) {
     a.tiles = t;
     k_ns<MODE, SHAPE><<<dim3(tile::blocks_of(SHAPE, t)), dim3(tile::ShapeOf<SHAPE>::type::THREADS), 0, st>>>(a);
     if (t.splits > 1) {
-      const int64_t all = a.mp * (MODE == APPLY ? a.np : a.mp) / 8;
-      k_ns_join<MODE, tile::ShapeOf<SHAPE>::type::BM>
-          <<<dim3(std::min<int64_t>((all + 255) / 256, 4096)), dim3(256), 0, st>>>(a);
+      if constexpr (MODE == APPLY)
+        k_ns_join<<<dim3(std::min<int64_t>((a.mp * a.np / 8 + 255) / 256, 4096)), dim3(256), 0, st>>>(a);
+      else
+        k_ns_join_symmetric<MODE, tile::ShapeOf<SHAPE>::type::BM><<<dim3(a.mp / 64, a.mp / 64), dim3(256), 0, st>>>(a);
     }
   });
   return last_launch_status();
@@ -333,13 +571,9 @@ int run_ortho(const fqt_ortho_desc *d, const NsSizes &s, Source src, NsArgs a, v
   auto pairs = [&](size_t at) { return Pairs{reinterpret_cast<uint16_t *>(base + at), s.mp}; };
   double *norm = reinterpret_cast<double *>(base + w.norm);
   Pairs x = pairs(w.x[0]), next = pairs(w.x[1]);
-  const int64_t all = d->rows * d->cols;
-  const int parts = int(std::min<int64_t>((all + 1023) / 1024, NORM_BLOCKS));
-  k_ns_norm<<<dim3(parts), dim3(256), 0, st>>>(src, norm);
-  FQT_TRY_(last_launch_status());
-  const dim3 grid(s.np / 64, s.mp / 64);
-  if (s.tall) k_ns_start<true><<<grid, dim3(256), 0, st>>>(src, norm, parts, d->eps, x);
-  else k_ns_start<false><<<grid, dim3(256), 0, st>>>(src, norm, parts, d->eps, x);
+  const uint32_t groups = uint32_t((d->cols + 7) / 8), all = uint32_t(d->rows * groups);
+  const int parts = int(std::min<uint32_t>((all + 255) / 256, NORM_BLOCKS));
+  k_ns_norm<<<dim3(parts), dim3(256), 0, st>>>(src, make_fastdiv(groups), all, norm);
   FQT_TRY_(last_launch_status());
   a.mp = s.mp; a.np = s.np; a.m = s.m; a.n = s.n;
   a.p = pairs(w.p);
@@ -348,6 +582,31 @@ int run_ortho(const fqt_ortho_desc *d, const NsSizes &s, Source src, NsArgs a, v
   a.ldo = s.ldo;
   a.o_dtype = d->o_dtype;
   a.tall = s.tall;
+  if (s.mp == 64) {
+    const int64_t tiles = s.np / 64, per = (tiles + SMALL_BLOCKS - 1) / SMALL_BLOCKS;
+    const int blocks = int((tiles + per - 1) / per);
+    float *sums[2] = {a.part, a.part + SMALL_BLOCKS * 4096};
+    SmallArgs q{a, nullptr, sums[0], per * 64};
+    q.n.x = x;
+    if (s.tall) k_ns_small_start<true><<<dim3(blocks), dim3(256), 0, st>>>(src, norm, parts, d->eps, q);
+    else k_ns_small_start<false><<<dim3(blocks), dim3(256), 0, st>>>(src, norm, parts, d->eps, q);
+    FQT_TRY_(last_launch_status());
+    for (int i = 0; i < d->steps; ++i) {
+      q.n.x = x;
+      q.n.next = next;
+      q.n.last = i + 1 == d->steps;
+      q.from = sums[i & 1];
+      q.to = sums[~i & 1];
+      k_ns_small<<<dim3(blocks), dim3(256), 0, st>>>(q, blocks);
+      FQT_TRY_(last_launch_status());
+      std::swap(x, next);
+    }
+    return FQT_OK;
+  }
+  const dim3 grid(s.np / 64, s.mp / 64);
+  if (s.tall) k_ns_start<true><<<grid, dim3(256), 0, st>>>(src, norm, parts, d->eps, x);
+  else k_ns_start<false><<<grid, dim3(256), 0, st>>>(src, norm, parts, d->eps, x);
+  FQT_TRY_(last_launch_status());
   for (int i = 0; i < d->steps; ++i) {
     a.x = x;
     a.next = next;
@@ -382,7 +641,8 @@ extern "C" int fqt_orthogonalize(const fqt_ortho_desc *d, const void *g, void *o
   if (s.m == 0) return FQT_OK;
   if (!g || !o || !ws) return FQT_E_NULL;
   if (!elem_aligned(g, d->g_dtype) || !elem_aligned(o, d->o_dtype) || !aligned(ws, 256)) return FQT_E_ALIGN;
-  Source src{g, nullptr, d->rows, d->cols, s.ldg, 0, d->g_dtype, 0, 0.0f};
+  Source src{g, nullptr, d->rows, d->cols, s.ldg, 0, d->g_dtype, 0, 0.0f, 0};
+  src.vec = aligned(g, 16) && s.ldg * elem_size(d->g_dtype) % 16 == 0;
   NsArgs a{};
   a.out = o;
   return run_ortho(d, s, src, a, ws, ws_bytes, static_cast<hipStream_t>(hip_stream));
@@ -400,7 +660,8 @@ extern "C" int fqt_muon_step(const fqt_ortho_desc *d, const fqt_muon_cfg *cfg, c
   if (s.m == 0) return FQT_OK;
   if (!g || !m || !w || !ws) return FQT_E_NULL;
   if (!elem_aligned(g, d->g_dtype) || !aligned(m, 4) || !aligned(w, 4) || !aligned(ws, 256)) return FQT_E_ALIGN;
-  Source src{g, m, d->rows, d->cols, s.ldg, s.ldm, d->g_dtype, cfg->nesterov ? 1 : 0, cfg->momentum};
+  Source src{g, m, d->rows, d->cols, s.ldg, s.ldm, d->g_dtype, cfg->nesterov ? 1 : 0, cfg->momentum, 0};
+  src.vec = aligned(g, 16) && s.ldg * elem_size(d->g_dtype) % 16 == 0 && aligned(m, 16) && s.ldm % 4 == 0;
   NsArgs a{};
   a.w = w;
   a.keep = 1.0f - cfg->lr * cfg->weight_decay;

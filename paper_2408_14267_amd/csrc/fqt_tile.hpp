@@ -434,6 +434,7 @@ __device__ __forceinline__ void wave_fence() {
 //                             the latency of one after the other would cost as much as a third of a
 //                             product over 64 steps
 //   e.finish(m, n, v, f)      the group's sums v and its fetch f
+//   e.mirror(n, m, v)         E::MIRROR only: 8 finished values of column n from row m on
 template <int KIND, typename S, typename E>
 __device__ __forceinline__ void run_epilogue(const typename Acc<KIND>::type (&acc)[S::FM][S::FN], char *lds,
                                              int64_t m0, int64_t n0, E &&e) {
@@ -471,13 +472,30 @@ __device__ __forceinline__ void run_epilogue(const typename Acc<KIND>::type (&ac
       const Fetch f = q[i % DEPTH];
       if (i + DEPTH < ALL) q[i % DEPTH] = e.fetch(m + (i + DEPTH) * ROWS_AT_ONCE, n);
       e.finish(m + i * ROWS_AT_ONCE, n, v, f);
+      if constexpr (std::remove_reference_t<E>::MIRROR) {
+        float *p = patch + (g * ROWS_AT_ONCE + r) * PITCH + c;
+        *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
+        *reinterpret_cast<float4 *>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+      }
     }
     wave_fence();
+    if constexpr (std::remove_reference_t<E>::MIRROR) {
+#pragma unroll
+      for (int h = 0; h < S::TN / 32; ++h) {
+        const uint32_t i = h * 64 + l, col = i % S::TN, half = i / S::TN * 8;
+        float v[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) v[j] = patch[(half + j) * PITCH + col];
+        e.mirror(n - c + col, m - r + k * 16 + half, v);
+      }
+      wave_fence();
+    }
   }
 }
 // Partial sums of a split contraction: rows of ld (a multiple of 8) floats.
 struct StorePart {
   static constexpr int DEPTH = 1;
+  static constexpr bool MIRROR = false;
   struct Fetch {};
   float *part;
   int64_t M, ld;

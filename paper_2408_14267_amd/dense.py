@@ -114,15 +114,12 @@ def ortho_desc(rows, cols, g_dtype=FQT_F32, o_dtype=FQT_F32, steps=5, eps=1e-7, 
 
 # ----------------------------------------------------------------------------- checks
 
-_device_of = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
-
-
-def _matrix(where, name, t, dtype, rows, cols, ld):
-    """Raise unless t is the matrix that the descriptor describes (a kernel would read or write
-    outside it)."""
+def _matrix(where, name, t, dtype, rows, cols, ld, dev):
+    """Raise unless t is the matrix that the descriptor describes, on device `dev` (a kernel would
+    read or write outside it)."""
     dt = _TORCH_OF.get(dtype)
-    if (t.dtype is dt and t.is_cuda and t.shape == (rows, cols) and
-            t.stride() == (ld or cols, 1) and t.get_device() == _device_of()):
+    if (t.dtype is dt and t.shape == (rows, cols) and t.get_device() == dev and
+            (t.stride() == (ld, 1) if ld else t.is_contiguous())):
         return
     if t.dtype is not dt:
         raise ValueError(f"{where}: {name}: dtype {t.dtype} does not match the descriptor's {dt}")
@@ -132,26 +129,30 @@ def _matrix(where, name, t, dtype, rows, cols, ld):
     if (cols > 1 and t.stride(1) != 1) or (rows > 1 and t.stride(0) != (ld or cols)):
         raise ValueError(f"{where}: {name}: strides {t.stride()}, the descriptor has "
                          f"({ld or cols}, 1)")
-    _device(where, name, t)
+    if t.get_device() != dev:
+        raise ValueError(f"{where}: {name}: expected a device tensor on device {dev}, got one on "
+                         f"{t.device}")
 
 
-def _vector(where, name, t, n):
-    if (t.dtype is torch.float32 and t.is_cuda and t.shape == (n,) and t.is_contiguous() and
-            t.get_device() == _device_of()):
+def _vector(where, name, t, n, dev):
+    if t.dtype is torch.float32 and t.shape == (n,) and t.is_contiguous() and t.get_device() == dev:
         return
     if t.dtype is not torch.float32:
         raise ValueError(f"{where}: {name}: dtype {t.dtype}, float32 is needed")
     if t.shape != (n,) or not t.is_contiguous():
         raise ValueError(f"{where}: {name}: shape {tuple(t.shape)}, strides {t.stride()}: "
                          f"{n} contiguous elements are needed")
-    _device(where, name, t)
+    raise ValueError(f"{where}: {name}: expected a device tensor on device {dev}, got one on "
+                     f"{t.device}")
 
 
-def _device(where, name, t):
-    if not t.is_cuda:
-        raise ValueError(f"{where}: {name}: expected a device tensor, got one on {t.device}")
-    if t.get_device() != _device_of():
-        raise ValueError(f"{where}: {name}: on {t.device}, the current device is {_device_of()}")
+def _current(where, dev):
+    """Raise unless `dev`, where all tensors of a call are, is the current HIP device."""
+    if dev < 0:
+        raise ValueError(f"{where}: expected device tensors")
+    if dev != torch.cuda.current_device():
+        raise ValueError(f"{where}: tensors on device {dev}, the current device is "
+                         f"{torch.cuda.current_device()}")
 
 
 def _required(where, **tensors):
@@ -160,12 +161,12 @@ def _required(where, **tensors):
             raise ValueError(f"{where}: {name}: a tensor is required")
 
 
-def _workspace(where, ws):
+def _workspace(where, ws, dev):
     if ws is None:
         raise ValueError(f"{where}: ws: a workspace is required")
-    _device(where, "ws", ws)
-    if not ws.is_contiguous():
-        raise ValueError(f"{where}: ws: the workspace must be contiguous")
+    if ws.get_device() != dev or not ws.is_contiguous():
+        raise ValueError(f"{where}: ws: a contiguous workspace on device {dev} is needed, got one on "
+                         f"{ws.device}")
     return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
@@ -183,21 +184,23 @@ def fqt_rmsnorm_forward(desc, x, g, residual=None, h=None, y=None, q=None, scale
                         stream=None):
     where, R, C = "fqt_rmsnorm_forward", desc.rows, desc.cols
     _required(where, x=x, g=g)
+    dev = x.get_device()
     if (q is None) != (scale is None):
         raise ValueError(f"{where}: q and scale come together")
-    _matrix(where, "x", x, desc.x_dtype, R, C, desc.ldx)
-    _vector(where, "g", g, C)
+    _matrix(where, "x", x, desc.x_dtype, R, C, desc.ldx, dev)
+    _vector(where, "g", g, C, dev)
     if residual is not None:
-        _matrix(where, "residual", residual, desc.x_dtype, R, C, desc.ldr)
+        _matrix(where, "residual", residual, desc.x_dtype, R, C, desc.ldr, dev)
     if h is not None:
-        _matrix(where, "h", h, desc.x_dtype, R, C, desc.ldh)
+        _matrix(where, "h", h, desc.x_dtype, R, C, desc.ldh, dev)
     if y is not None:
-        _matrix(where, "y", y, desc.y_dtype, R, C, desc.ldy)
+        _matrix(where, "y", y, desc.y_dtype, R, C, desc.ldy, dev)
     if q is not None:
-        _matrix(where, "q", q, desc.q_dtype, R, C, desc.ldq)
-        _vector(where, "scale", scale, R)
+        _matrix(where, "q", q, desc.q_dtype, R, C, desc.ldq, dev)
+        _vector(where, "scale", scale, R, dev)
     if rstd is not None:
-        _vector(where, "rstd", rstd, R)
+        _vector(where, "rstd", rstd, R, dev)
+    _current(where, dev)
     _check(_lib.fqt_rmsnorm_forward(desc, x.data_ptr(), _ptr(residual), g.data_ptr(), _ptr(h),
                                     _ptr(y), _ptr(q), _ptr(scale), _ptr(rstd), _stream(stream)),
            where)
@@ -212,25 +215,29 @@ def fqt_norm_workspace_size(desc):
 def fqt_rmsnorm_backward(desc, h, g, rstd, dy, dx, dg, ws, dres=None, stream=None):
     where, R, C = "fqt_rmsnorm_backward", desc.rows, desc.cols
     _required(where, h=h, g=g, rstd=rstd, dy=dy, dx=dx, dg=dg)
-    _matrix(where, "h", h, desc.x_dtype, R, C, desc.ldh)
-    _vector(where, "g", g, C)
-    _vector(where, "rstd", rstd, R)
-    _matrix(where, "dy", dy, desc.y_dtype, R, C, desc.ldy)
-    _matrix(where, "dx", dx, desc.x_dtype, R, C, desc.ldx)
-    _vector(where, "dg", dg, C)
+    dev = h.get_device()
+    _matrix(where, "h", h, desc.x_dtype, R, C, desc.ldh, dev)
+    _vector(where, "g", g, C, dev)
+    _vector(where, "rstd", rstd, R, dev)
+    _matrix(where, "dy", dy, desc.y_dtype, R, C, desc.ldy, dev)
+    _matrix(where, "dx", dx, desc.x_dtype, R, C, desc.ldx, dev)
+    _vector(where, "dg", dg, C, dev)
     if dres is not None:
-        _matrix(where, "dres", dres, desc.x_dtype, R, C, desc.ldr)
+        _matrix(where, "dres", dres, desc.x_dtype, R, C, desc.ldr, dev)
+    _current(where, dev)
     _check(_lib.fqt_rmsnorm_backward(desc, h.data_ptr(), g.data_ptr(), rstd.data_ptr(),
                                      dy.data_ptr(), _ptr(dres), dx.data_ptr(), dg.data_ptr(),
-                                     *_workspace(where, ws), _stream(stream)), where)
+                                     *_workspace(where, ws, dev), _stream(stream)), where)
 
 
 def fqt_quantize_rows(desc, x, q, scale, stream=None):
     where, R, C = "fqt_quantize_rows", desc.rows, desc.cols
     _required(where, x=x, q=q, scale=scale)
-    _matrix(where, "x", x, desc.x_dtype, R, C, desc.ldx)
-    _matrix(where, "q", q, desc.q_dtype, R, C, desc.ldq)
-    _vector(where, "scale", scale, R)
+    dev = x.get_device()
+    _matrix(where, "x", x, desc.x_dtype, R, C, desc.ldx, dev)
+    _matrix(where, "q", q, desc.q_dtype, R, C, desc.ldq, dev)
+    _vector(where, "scale", scale, R, dev)
+    _current(where, dev)
     _check(_lib.fqt_quantize_rows(desc, x.data_ptr(), q.data_ptr(), scale.data_ptr(),
                                   _stream(stream)), where)
 
@@ -244,51 +251,55 @@ def fqt_linear_workspace_size(desc, backward=False):
     return n.value
 
 
-def _operands(where, desc, x, w, x_scale, w_scale):
+def _operands(where, desc, x, w, x_scale, w_scale, dev):
     if x is not None:
-        _matrix(where, "x", x, desc.x_dtype, desc.M, desc.K, desc.ldx)
+        _matrix(where, "x", x, desc.x_dtype, desc.M, desc.K, desc.ldx, dev)
     if w is not None:
-        _matrix(where, "w", w, desc.x_dtype, desc.N, desc.K, desc.ldw)
+        _matrix(where, "w", w, desc.x_dtype, desc.N, desc.K, desc.ldw, dev)
     if x_scale is not None:
-        _vector(where, "x_scale", x_scale, desc.M)
+        _vector(where, "x_scale", x_scale, desc.M, dev)
     if w_scale is not None:
-        _vector(where, "w_scale", w_scale, desc.N)
+        _vector(where, "w_scale", w_scale, desc.N, dev)
 
 
 def fqt_linear_forward(desc, x, w, y, ws, bias=None, residual=None, x_scale=None, w_scale=None,
                        z=None, stream=None):
     where, M, N = "fqt_linear_forward", desc.M, desc.N
     _required(where, x=x, w=w, y=y)
-    _operands(where, desc, x, w, x_scale, w_scale)
-    _matrix(where, "y", y, desc.y_dtype, M, N, desc.ldy)
+    dev = y.get_device()
+    _operands(where, desc, x, w, x_scale, w_scale, dev)
+    _matrix(where, "y", y, desc.y_dtype, M, N, desc.ldy, dev)
     if bias is not None:
-        _vector(where, "bias", bias, N)
+        _vector(where, "bias", bias, N, dev)
     if residual is not None:
-        _matrix(where, "residual", residual, desc.y_dtype, M, N, desc.ldr)
+        _matrix(where, "residual", residual, desc.y_dtype, M, N, desc.ldr, dev)
     if z is not None:
-        _matrix(where, "z", z, desc.y_dtype, M, N, desc.ldz)
+        _matrix(where, "z", z, desc.y_dtype, M, N, desc.ldz, dev)
+    _current(where, dev)
     _check(_lib.fqt_linear_forward(desc, x.data_ptr(), w.data_ptr(), _ptr(x_scale), _ptr(w_scale),
                                    _ptr(bias), _ptr(residual), _ptr(z), y.data_ptr(),
-                                   *_workspace(where, ws), _stream(stream)), where)
+                                   *_workspace(where, ws, dev), _stream(stream)), where)
 
 
 def fqt_linear_backward(desc, x, w, dy, ws, z=None, x_scale=None, w_scale=None, dx=None, dw=None,
                         dbias=None, stream=None):
     where, M, N, K = "fqt_linear_backward", desc.M, desc.N, desc.K
     _required(where, dy=dy)
-    _operands(where, desc, x, w, x_scale, w_scale)
-    _matrix(where, "dy", dy, desc.y_dtype, M, N, desc.ldy)
+    dev = dy.get_device()
+    _operands(where, desc, x, w, x_scale, w_scale, dev)
+    _matrix(where, "dy", dy, desc.y_dtype, M, N, desc.ldy, dev)
     if z is not None:
-        _matrix(where, "z", z, desc.y_dtype, M, N, desc.ldz)
+        _matrix(where, "z", z, desc.y_dtype, M, N, desc.ldz, dev)
     if dx is not None:
-        _matrix(where, "dx", dx, desc.dx_dtype, M, K, desc.lddx)
+        _matrix(where, "dx", dx, desc.dx_dtype, M, K, desc.lddx, dev)
     if dw is not None:
-        _matrix(where, "dw", dw, desc.dw_dtype, N, K, desc.lddw)
+        _matrix(where, "dw", dw, desc.dw_dtype, N, K, desc.lddw, dev)
     if dbias is not None:
-        _vector(where, "dbias", dbias, N)
+        _vector(where, "dbias", dbias, N, dev)
+    _current(where, dev)
     _check(_lib.fqt_linear_backward(desc, _ptr(x), _ptr(w), _ptr(x_scale), _ptr(w_scale), _ptr(z),
                                     dy.data_ptr(), _ptr(dx), _ptr(dw), _ptr(dbias),
-                                    *_workspace(where, ws), _stream(stream)), where)
+                                    *_workspace(where, ws, dev), _stream(stream)), where)
 
 
 # ----------------------------------------------------------------------------- orthogonalisation
@@ -302,9 +313,11 @@ def fqt_ortho_workspace_size(desc):
 def fqt_orthogonalize(desc, g, o, ws, stream=None):
     where, R, C = "fqt_orthogonalize", desc.rows, desc.cols
     _required(where, g=g, o=o)
-    _matrix(where, "g", g, desc.g_dtype, R, C, desc.ldg)
-    _matrix(where, "o", o, desc.o_dtype, R, C, desc.ldo)
-    _check(_lib.fqt_orthogonalize(desc, g.data_ptr(), o.data_ptr(), *_workspace(where, ws),
+    dev = g.get_device()
+    _matrix(where, "g", g, desc.g_dtype, R, C, desc.ldg, dev)
+    _matrix(where, "o", o, desc.o_dtype, R, C, desc.ldo, dev)
+    _current(where, dev)
+    _check(_lib.fqt_orthogonalize(desc, g.data_ptr(), o.data_ptr(), *_workspace(where, ws, dev),
                                   _stream(stream)), where)
 
 
@@ -312,12 +325,14 @@ def fqt_muon_step(desc, w, g, m, ws, lr, momentum=0.95, weight_decay=0.0, scale=
                   stream=None):
     where, R, C = "fqt_muon_step", desc.rows, desc.cols
     _required(where, w=w, g=g, m=m)
-    _matrix(where, "g", g, desc.g_dtype, R, C, desc.ldg)
-    _matrix(where, "m", m, FQT_F32, R, C, desc.ldm)
-    _matrix(where, "w", w, desc.o_dtype, R, C, desc.ldo)
+    dev = w.get_device()
+    _matrix(where, "g", g, desc.g_dtype, R, C, desc.ldg, dev)
+    _matrix(where, "m", m, FQT_F32, R, C, desc.ldm, dev)
+    _matrix(where, "w", w, desc.o_dtype, R, C, desc.ldo, dev)
     cfg = fqt_muon_cfg(lr, momentum, weight_decay, scale, int(nesterov))
+    _current(where, dev)
     _check(_lib.fqt_muon_step(desc, cfg, g.data_ptr(), m.data_ptr(), w.data_ptr(),
-                              *_workspace(where, ws), _stream(stream)), where)
+                              *_workspace(where, ws, dev), _stream(stream)), where)
 
 
 # ----------------------------------------------------------------------------- workspaces
