@@ -26,7 +26,13 @@ using tile::PANEL_ROWS;
 using tile::PANEL_COLS;
 
 constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
-constexpr float X_UNIT = 32768.0f;      // 2^15
+// Where |u| is small beside eps every X_i is: |X_i| <= a^i |X_0|.  All of X, P and Q are then stored
+// with k more bits of scale (2^15+k, 2^14+2k, 2^13+2k; k = 0 for |X_0| a^steps >= 1/4), so that float16
+// holds the smallest gradients as well as any.  The factors depend on |u|, so they stay on the device:
+struct Units {
+  float down;            // 2^-2k, in the terms of Q and X' that have P once more
+  float out;             // 2^-(15+k), from the stored X to X
+};
 
 struct Split { uint16_t hi, lo; };
 __device__ __forceinline__ Split split(float v) {
@@ -133,22 +139,34 @@ __global__ void __launch_bounds__(256) k_ns_norm(Source s, FastDiv groups, uint3
   sum = block_sum(sum, slots);
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
-// 2^15 / (|u| + eps) from the partial sums.
-__device__ __forceinline__ float unit_scale(const double *part, int32_t parts, float eps, double *slots) {
+// 2^(15+k) / (|u| + eps) from the partial sums; one workgroup writes the units of the stored matrices.
+struct Start {
+  const double *part;
+  int32_t parts, steps;
+  float eps;
+  Units *units;
+};
+__device__ __forceinline__ double unit_scale(const Start &s, double *slots, bool write) {
   double sum = 0.0;
-  for (int i = threadIdx.x; i < parts; i += 256) sum += part[i];
-  return float(double(X_UNIT) / (sqrt(block_sum(sum, slots)) + double(eps)));
+  for (int i = threadIdx.x; i < s.parts; i += 256) sum += s.part[i];
+  const double norm = sqrt(block_sum(sum, slots));
+  double most = norm / (norm + double(s.eps));             // bound of |X_i| over the steps
+  for (int i = 0; i < s.steps; ++i) most = fmin(1.0, most * double(NS_A));
+  // |X_i| < 2^-k: X below 2^15, P below 2^14, Q (|b| P at most) below 4.8 2^13.  (NaN: 0)
+  const int k = most > 0.0 ? max(0, -ilogb(most) - 1) : 0;
+  if (write && threadIdx.x == 0) *s.units = {float(ldexp(1.0, -2 * k)), float(ldexp(1.0, -15 - k))};
+  return ldexp(1.0, 15 + k) / (norm + double(s.eps));
 }
 // The 64 x 64 tile of X_0 2^15 at (x0, y0): put(row, column, 8 values) in the tile.  Tall matrices are
 // transposed on the way, through t.
 template <bool TALL, typename F>
-__device__ __forceinline__ void start_tile(const Source &s, float inv, int64_t x0, int64_t y0, float (*t)[65], F &&put) {
+__device__ __forceinline__ void start_tile(const Source &s, double inv, int64_t x0, int64_t y0, float (*t)[65], F &&put) {
   if constexpr (TALL) {
     for (int i = threadIdx.x; i < 512; i += 256) {
       float u[8];
       load_u<false>(s, y0 + i / 8, x0 + i % 8 * 8, u);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) t[i % 8 * 8 + j][i / 8] = u[j] * inv;
+      for (int j = 0; j < 8; ++j) t[i % 8 * 8 + j][i / 8] = float(u[j] * inv);
     }
     __syncthreads();
   }
@@ -160,17 +178,17 @@ __device__ __forceinline__ void start_tile(const Source &s, float inv, int64_t x
     } else {
       load_u<false>(s, x0 + i / 8, y0 + i % 8 * 8, v);
 #pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] *= inv;
+      for (int j = 0; j < 8; ++j) v[j] = float(v[j] * inv);
     }
     put(i / 8, i % 8 * 8, v);
   }
 }
 // X_0 = u / (|u| + eps) as pairs, zeros in the padding.
 template <bool TALL>
-__global__ void __launch_bounds__(256) k_ns_start(Source s, const double *part, int32_t parts, float eps, Pairs x) {
+__global__ void __launch_bounds__(256) k_ns_start(Source s, Start b, Pairs x) {
   __shared__ double slots[4];
   __shared__ float t[TALL ? 64 : 1][65];
-  const float inv = unit_scale(part, parts, eps, slots);
+  const double inv = unit_scale(b, slots, blockIdx.x + blockIdx.y == 0);
   const int64_t x0 = int64_t(blockIdx.y) * 64, y0 = int64_t(blockIdx.x) * 64;
   start_tile<TALL>(s, inv, x0, y0, t, [&](int r, int c, const float (&v)[8]) { store_split8(x, x0 + r, y0 + c, v); });
 }
@@ -184,6 +202,7 @@ struct NsArgs {
   int64_t m, n;          // without padding
   tile::Tiles tiles;
   float *part;
+  const Units *units;
   // the last step's result
   void *out;             // o, or null
   float *w;              // weights, or null
@@ -199,16 +218,19 @@ __device__ __forceinline__ void store_result8(const NsArgs &a, int64_t m, int64_
   for (int i = 0; i < 8; ++i) {
     if (n + i >= a.n) break;
     const int64_t at = a.tall ? (n + i) * a.ldo + m : m * a.ldo + n + i;
-    const float o = v[i] * (1.0f / X_UNIT);
+    const float o = v[i] * a.units->out;
     if (a.w) a.w[at] = fmaf(a.keep, a.w[at], -a.rate * o);
     else if (a.o_dtype == FQT_BF16) static_cast<bf16 *>(a.out)[at] = from_f32<bf16>(o);
     else static_cast<float *>(a.out)[at] = o;
   }
 }
-// P 2^14 from sums 2^30; Q 2^13 from sums 2^28 and P 2^14; X' 2^15 from sums 2^28 and X 2^15.
+// P 2^14 from sums 2^30; Q 2^13 from sums 2^28 and P 2^14; X' 2^15 from sums 2^28 and X 2^15 (and the k
+// bits of each; down = 2^-2k).
 __device__ __forceinline__ float gram_of(float sum) { return sum * 0x1p-16f; }
-__device__ __forceinline__ float poly_of(float sum, float p) { return fmaf(NS_B * 0.5f, p, sum * (NS_C * 0x1p-15f)); }
-__device__ __forceinline__ float apply_of(float sum, float x) { return fmaf(NS_A, x, sum * 0x1p-13f); }
+__device__ __forceinline__ float poly_of(float sum, float p, float down) {
+  return fmaf(NS_B * 0.5f, p, sum * (NS_C * 0x1p-15f) * down);
+}
+__device__ __forceinline__ float apply_of(float sum, float x, float down) { return fmaf(NS_A, x, sum * 0x1p-13f * down); }
 
 // The epilogue of 8 consecutive n (tile::run_epilogue).  diagonal: the tile holds its own mirror image.
 template <int MODE>
@@ -221,7 +243,10 @@ struct Finish {
   __device__ __forceinline__ bool in(int64_t m, int64_t n) const {
     return m < a.mp && n < (MODE == APPLY ? a.np : a.mp);
   }
-  __device__ __forceinline__ void columns(int64_t) {}
+  float down;
+  __device__ __forceinline__ void columns(int64_t) {
+    if constexpr (MODE != GRAM) down = a.units->down;
+  }
   __device__ __forceinline__ Fetch fetch(int64_t m, int64_t n) {
     Fetch f;
     if constexpr (MODE != GRAM)
@@ -233,8 +258,8 @@ struct Finish {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if constexpr (MODE == GRAM) v[i] = gram_of(v[i]);
-      else if constexpr (MODE == POLY) v[i] = poly_of(v[i], f.x[i]);
-      else v[i] = apply_of(v[i], f.x[i]);
+      else if constexpr (MODE == POLY) v[i] = poly_of(v[i], f.x[i], down);
+      else v[i] = apply_of(v[i], f.x[i], down);
     }
     if (MODE == APPLY && a.last) store_result8(a, m, n, v);
     else store_split8(MODE == GRAM ? a.p : MODE == POLY ? a.q : a.next, m, n, v);
@@ -276,6 +301,7 @@ __global__ void __launch_bounds__(256) k_ns_join(NsArgs a) {
   for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
     const int64_t m = i / groups, n = i % groups * 8;
     Finish<APPLY> f{a, false};
+    f.columns(n);
     const auto q = f.fetch(m, n);
     float v[8] = {};
 #pragma unroll 4
@@ -296,6 +322,7 @@ __global__ void __launch_bounds__(256) k_ns_join_symmetric(NsArgs a) {
   const int64_t m0 = int64_t(blockIdx.y) * 64, n0 = int64_t(blockIdx.x) * 64;
   if (m0 / B > n0 / B) return;
   Finish<MODE> f{a, m0 / B == n0 / B};
+  f.columns(n0);
 #pragma unroll
   for (int h = 0; h < 2; ++h) {
     const int r = (h * 256 + threadIdx.x) / 8, c = threadIdx.x % 8 * 8;
@@ -395,11 +422,11 @@ __device__ __forceinline__ void panels_out(const char *lds, const Pairs &x, int6
 
 // X_0 and its partial sums of P.
 template <bool TALL>
-__global__ void __launch_bounds__(256) k_ns_small_start(Source s, const double *norm, int32_t parts, float eps, SmallArgs a) {
+__global__ void __launch_bounds__(256) k_ns_small_start(Source s, Start b, SmallArgs a) {
   __shared__ double slots[4];
   __shared__ float t[TALL ? 64 : 1][65];
   __shared__ __attribute__((aligned(16))) char x[2 * PANEL];
-  const float inv = unit_scale(norm, parts, eps, slots);
+  const double inv = unit_scale(b, slots, blockIdx.x == 0);
   const uint32_t wave = wave_id(), wm = wave / 2 * 32, wn = wave % 2 * 32;
   SmallAcc acc{};
   const int64_t end = min(a.n.np, (blockIdx.x + 1) * a.slice);
@@ -421,6 +448,7 @@ __global__ void __launch_bounds__(256) k_ns_small(SmallArgs a, int32_t blocks) {
   __shared__ __attribute__((aligned(16))) char p[2 * PANEL], q[2 * PANEL], x[2 * PANEL], y[2 * PANEL];
   const uint32_t wave = wave_id(), l = __lane_id(), wm = wave / 2 * 32, wn = wave % 2 * 32;
   const int64_t n_first = blockIdx.x * a.slice, end = min(a.n.np, n_first + a.slice);
+  const float down = a.n.units->down;
   // X is read along its rows' order (m is the contraction)
   const Operand xo{reinterpret_cast<const char *>(a.n.x.p), 64 * tile::KB, a.n.np};
   auto load_x = [&](int64_t n0) {
@@ -460,7 +488,7 @@ __global__ void __launch_bounds__(256) k_ns_small(SmallArgs a, int32_t blocks) {
         float o[4], v[4];
         join4(p + panel_at(m, n, 0), p + panel_at(m, n, 1), o);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = poly_of(acc[i][j][k], o[k]);
+        for (int k = 0; k < 4; ++k) v[k] = poly_of(acc[i][j][k], o[k], down);
         put4(q, m, n, v);
       }
   }
@@ -481,7 +509,7 @@ __global__ void __launch_bounds__(256) k_ns_small(SmallArgs a, int32_t blocks) {
         float o[4], v[4];
         join4(at, at + 32 * tile::KB, o);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = apply_of(acc[i][j][k], o[k]);
+        for (int k = 0; k < 4; ++k) v[k] = apply_of(acc[i][j][k], o[k], down);
         if (a.n.last) {
           float r[8] = {v[0], v[1], v[2], v[3]};
           NsArgs cut = a.n;
@@ -531,7 +559,7 @@ NsWs ns_ws(const NsSizes &s) {
   w.apply = tile::make_plan(s.mp, s.np, s.mp / 32, false);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += align256(bytes); return o; };
-  w.norm = take(NORM_BLOCKS * sizeof(double));
+  w.norm = take(NORM_BLOCKS * sizeof(double) + sizeof(Units));
   const size_t x = size_t(s.mp) * s.np * 4, p = size_t(s.mp) * s.mp * 4;       // two planes of 2 bytes
   w.x[0] = take(x);
   w.x[1] = take(x);
@@ -579,6 +607,8 @@ int run_ortho(const fqt_ortho_desc *d, const NsSizes &s, Source src, NsArgs a, v
   a.p = pairs(w.p);
   a.q = pairs(w.q);
   a.part = reinterpret_cast<float *>(base + w.part);
+  const Start start{norm, parts, d->steps, d->eps, reinterpret_cast<Units *>(norm + NORM_BLOCKS)};
+  a.units = start.units;
   a.ldo = s.ldo;
   a.o_dtype = d->o_dtype;
   a.tall = s.tall;
@@ -588,8 +618,8 @@ int run_ortho(const fqt_ortho_desc *d, const NsSizes &s, Source src, NsArgs a, v
     float *sums[2] = {a.part, a.part + SMALL_BLOCKS * 4096};
     SmallArgs q{a, nullptr, sums[0], per * 64};
     q.n.x = x;
-    if (s.tall) k_ns_small_start<true><<<dim3(blocks), dim3(256), 0, st>>>(src, norm, parts, d->eps, q);
-    else k_ns_small_start<false><<<dim3(blocks), dim3(256), 0, st>>>(src, norm, parts, d->eps, q);
+    if (s.tall) k_ns_small_start<true><<<dim3(blocks), dim3(256), 0, st>>>(src, start, q);
+    else k_ns_small_start<false><<<dim3(blocks), dim3(256), 0, st>>>(src, start, q);
     FQT_TRY_(last_launch_status());
     for (int i = 0; i < d->steps; ++i) {
       q.n.x = x;
@@ -604,8 +634,8 @@ int run_ortho(const fqt_ortho_desc *d, const NsSizes &s, Source src, NsArgs a, v
     return FQT_OK;
   }
   const dim3 grid(s.np / 64, s.mp / 64);
-  if (s.tall) k_ns_start<true><<<grid, dim3(256), 0, st>>>(src, norm, parts, d->eps, x);
-  else k_ns_start<false><<<grid, dim3(256), 0, st>>>(src, norm, parts, d->eps, x);
+  if (s.tall) k_ns_start<true><<<grid, dim3(256), 0, st>>>(src, start, x);
+  else k_ns_start<false><<<grid, dim3(256), 0, st>>>(src, start, x);
   FQT_TRY_(last_launch_status());
   for (int i = 0; i < d->steps; ++i) {
     a.x = x;
