@@ -1,0 +1,322 @@
+"""Residual blocks and an optimizer around binary layers: torch modules over the dense operators.
+
+RMSNorm, Linear and NormLinear call fqt_rmsnorm_*, fqt_quantize_rows and fqt_linear_* (forward and
+backward); NormLinear keeps the activations between the norm and the product as 8-bit codes.  Muon
+updates latent weight matrices (and convolution weights, unfolded) by fqt_muon_step.  ResidualMLP puts
+them together with BinaryLinear: a float32 residual stream, blocks of a normed 8-bit expansion with
+GELU and a binary projection, the first and last layers at full width as in the networks of `train`.
+
+Modules take [..., features] inputs of float32 or bfloat16, keep float32 parameters, and cast or
+quantize the weight in every forward pass.  Their backward cannot be differentiated again.
+"""
+import math
+
+import torch
+import torch.nn as nn
+from torch.autograd.function import once_differentiable
+
+from . import dense, fqt, train
+
+_BF16, _F32 = torch.bfloat16, torch.float32
+
+
+class _Slots:
+    """Workspaces per call shape, device and stream (one serves one call at a time).  A capture takes one
+    that is there: a new one would belong to the graph's pool."""
+
+    def __init__(self):
+        self.slots = {}
+
+    def get(self, key, size, device):
+        slots = self.slots.setdefault(key, {})
+        at = device.index, fqt.current_stream()
+        ws = slots.get(at)
+        if ws is None:
+            if torch.cuda.is_current_stream_capturing():
+                for (index, _), ws in slots.items():
+                    if index == device.index:
+                        return ws
+            ws = slots[at] = torch.empty(max(size, 1), dtype=torch.uint8, device=device)
+        return ws
+
+
+def _rows(t, cols, name):
+    """t as a matrix [rows][cols]: dense rows on 16 bytes."""
+    if t.dtype not in (_F32, _BF16) or t.shape[-1] != cols:
+        raise ValueError(f"{name}: float32 or bfloat16 with {cols} features is needed, got "
+                         f"{t.dtype} {tuple(t.shape)}")
+    t = t.reshape(-1, cols).contiguous()
+    return t if t.data_ptr() % 16 == 0 else t.clone()
+
+
+class _NormFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, g, mod):
+        rows, cols = x.shape
+        desc = dense.norm_desc(rows, cols, x_dtype=x.dtype, y_dtype=mod.out_dtype or x.dtype, eps=mod.eps)
+        h = torch.empty_like(x) if residual is not None else x
+        y = torch.empty(rows, cols, dtype=mod.out_dtype or x.dtype, device=x.device)
+        rstd = torch.empty(rows, device=x.device)
+        dense.fqt_rmsnorm_forward(desc, x, g, residual=residual, h=h if residual is not None else None,
+                                  y=y, rstd=rstd)
+        ctx.save_for_backward(h, g, rstd)
+        ctx.desc, ctx.mod, ctx.residual = desc, mod, residual is not None
+        return (y, h) if ctx.residual else y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dh=None):
+        h, g, rstd = ctx.saved_tensors
+        desc = ctx.desc
+        dx, dg = torch.empty_like(h), torch.empty_like(g)
+        ws = ctx.mod.slots.get(("norm", desc.rows), dense.fqt_norm_workspace_size(desc), h.device)
+        dense.fqt_rmsnorm_backward(desc, h, g, rstd, dy.contiguous(), dx, dg, ws,
+                                   dres=dh.contiguous() if ctx.residual else None)
+        return dx, dx if ctx.residual else None, dg, None
+
+
+class RMSNorm(nn.Module):
+    """y = h / sqrt(mean h^2 + eps) * weight for h = x + residual; forward(x) returns y, forward(x,
+    residual) returns (y, h)."""
+
+    def __init__(self, features, eps=1e-6, out_dtype=None):
+        super().__init__()
+        self.weight = nn.Parameter(torch.ones(features))
+        self.features, self.eps, self.out_dtype = features, eps, out_dtype
+        self.slots = _Slots()
+
+    def forward(self, x, residual=None):
+        m = _rows(x, self.features, "x")
+        r = None if residual is None else _rows(residual, self.features, "residual").to(m.dtype)
+        if r is None:
+            return _NormFn.apply(m, None, self.weight, self).view(x.shape)
+        y, h = _NormFn.apply(m, r, self.weight, self)
+        return y.view(x.shape), h.view(x.shape)
+
+
+def _quantized(w, kind):
+    """Codes and scales of a weight's rows, or its bf16 copy."""
+    if kind == "bf16":
+        return w.to(_BF16), None
+    q = torch.empty(w.shape, dtype=dense._TORCH_OF[dense.dtype_code(kind)], device=w.device)
+    scale = torch.empty(w.shape[0], device=w.device)
+    dense.fqt_quantize_rows(dense.norm_desc(*w.shape, x_dtype=w.dtype, q_dtype=kind), w, q, scale)
+    return q, scale
+
+
+def _linear_forward(mod, x, x_scale, w, bias, residual, out_dtype):
+    """y, the pre-activation (None without an activation), the operand form of w, and the descriptor."""
+    (M, K), N = x.shape, w.shape[0]
+    wq, w_scale = _quantized(w, mod.operands)
+    desc = dense.linear_desc(M, N, K, x_dtype=mod.operands, y_dtype=out_dtype, act=mod.act, dx_dtype=_BF16,
+                             dw_dtype=_F32)
+    y = torch.empty(M, N, dtype=out_dtype, device=x.device)
+    z = torch.empty_like(y) if mod.act != "none" else None
+    ws = mod.slots.get(("fwd", M, out_dtype), dense.fqt_linear_workspace_size(desc), x.device)
+    dense.fqt_linear_forward(desc, x, wq, y, ws, bias=bias, residual=residual, x_scale=x_scale,
+                             w_scale=w_scale, z=z)
+    return y, z, wq, w_scale, desc
+
+
+def _linear_backward(ctx, mod, desc, x, x_scale, wq, w_scale, z, dy, need_x, need_bias):
+    dy = dy.contiguous()
+    dx = torch.empty(desc.M, desc.K, dtype=_BF16, device=dy.device) if need_x else None
+    dw = torch.empty(desc.N, desc.K, device=dy.device)
+    db = torch.empty(desc.N, device=dy.device) if need_bias else None
+    ws = mod.slots.get(("bwd", desc.M, dy.dtype), dense.fqt_linear_workspace_size(desc, True), dy.device)
+    dense.fqt_linear_backward(desc, x, wq, dy, ws, z=z, x_scale=x_scale, w_scale=w_scale, dx=dx, dw=dw,
+                              dbias=db)
+    return dx, dw, db
+
+
+class _LinearFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, w, bias, mod):
+        xq, x_scale = _quantized(x, mod.operands)
+        y, z, wq, w_scale, desc = _linear_forward(mod, xq, x_scale, w, bias, residual,
+                                                  residual.dtype if residual is not None else x.dtype)
+        ctx.save_for_backward(xq, x_scale, wq, w_scale, z)
+        ctx.desc, ctx.mod, ctx.x_dtype = desc, mod, x.dtype
+        ctx.residual, ctx.bias = residual is not None, bias is not None
+        return y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy):
+        xq, x_scale, wq, w_scale, z = ctx.saved_tensors
+        dx, dw, db = _linear_backward(ctx, ctx.mod, ctx.desc, xq, x_scale, wq, w_scale, z, dy,
+                                      ctx.needs_input_grad[0], ctx.bias)
+        return (None if dx is None else dx.to(ctx.x_dtype)), (dy if ctx.residual else None), dw, db, None
+
+
+class Linear(nn.Module):
+    """act(x W^T + bias) + residual with bf16, int8 or e4m3 operands (quantized per row, gradients passed
+    through the rounding)."""
+
+    def __init__(self, fin, fout, bias=True, act="none", operands="bf16"):
+        super().__init__()
+        dense.linear_desc(1, fout, fin, x_dtype=operands, act=act)       # refuses what does not exist
+        self.weight = nn.Parameter(torch.empty(fout, fin))
+        nn.init.kaiming_uniform_(self.weight, a=5 ** 0.5)
+        self.bias = nn.Parameter(torch.zeros(fout)) if bias else None
+        self.fin, self.fout, self.act, self.operands = fin, fout, act, operands
+        self.slots = _Slots()
+
+    def forward(self, x, residual=None):
+        r = None if residual is None else _rows(residual, self.fout, "residual")
+        y = _LinearFn.apply(_rows(x, self.fin, "x"), r, self.weight, self.bias, self)
+        return y.view(*x.shape[:-1], self.fout)
+
+
+class _NormLinearFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, residual, g, w, bias, mod):
+        rows, cols = x.shape
+        kind = mod.operands
+        desc = dense.norm_desc(rows, cols, x_dtype=x.dtype, y_dtype=_BF16,
+                               q_dtype=None if kind == "bf16" else kind, eps=mod.eps)
+        h = torch.empty_like(x) if residual is not None else x
+        rstd = torch.empty(rows, device=x.device)
+        out = dict(residual=residual, h=h if residual is not None else None, rstd=rstd)
+        scale = None
+        if kind == "bf16":
+            n = torch.empty(rows, cols, dtype=_BF16, device=x.device)
+            dense.fqt_rmsnorm_forward(desc, x, g, y=n, **out)
+        else:
+            n = torch.empty(rows, cols, dtype=dense._TORCH_OF[dense.dtype_code(kind)], device=x.device)
+            scale = torch.empty(rows, device=x.device)
+            dense.fqt_rmsnorm_forward(desc, x, g, q=n, scale=scale, **out)
+        y, z, wq, w_scale, ldesc = _linear_forward(mod, n, scale, w, bias, None, mod.out_dtype)
+        ctx.save_for_backward(h, g, rstd, n, scale, wq, w_scale, z)
+        ctx.descs, ctx.mod = (desc, ldesc), mod
+        ctx.residual, ctx.bias = residual is not None, bias is not None
+        return (y, h) if ctx.residual else y
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, dy, dh=None):
+        h, g, rstd, n, scale, wq, w_scale, z = ctx.saved_tensors
+        desc, ldesc = ctx.descs
+        dn, dw, db = _linear_backward(ctx, ctx.mod, ldesc, n, scale, wq, w_scale, z, dy, True, ctx.bias)
+        dx, dg = torch.empty_like(h), torch.empty_like(g)
+        ws = ctx.mod.slots.get(("norm", desc.rows), dense.fqt_norm_workspace_size(desc), h.device)
+        dense.fqt_rmsnorm_backward(desc, h, g, rstd, dn, dx, dg, ws,
+                                   dres=dh.contiguous() if ctx.residual else None)
+        return dx, dx if ctx.residual else None, dg, dw, db, None
+
+
+class NormLinear(nn.Module):
+    """act(norm(x + residual) W^T + bias), the normed rows as 8-bit codes (operands "int8" or "e4m3") or
+    bf16.  forward(x) returns y, forward(x, residual) returns (y, h) with h = x + residual."""
+
+    def __init__(self, fin, fout, bias=True, act="none", operands="int8", eps=1e-6, out_dtype=_F32):
+        super().__init__()
+        dense.linear_desc(1, fout, fin, x_dtype=operands, act=act)
+        self.norm_weight = nn.Parameter(torch.ones(fin))
+        self.weight = nn.Parameter(torch.empty(fout, fin))
+        nn.init.kaiming_uniform_(self.weight, a=5 ** 0.5)
+        self.bias = nn.Parameter(torch.zeros(fout)) if bias else None
+        self.fin, self.fout, self.act, self.operands = fin, fout, act, operands
+        self.eps, self.out_dtype = eps, out_dtype
+        self.slots = _Slots()
+
+    def forward(self, x, residual=None):
+        m = _rows(x, self.fin, "x")
+        r = None if residual is None else _rows(residual, self.fin, "residual").to(m.dtype)
+        shape = (*x.shape[:-1], self.fout)
+        if r is None:
+            return _NormLinearFn.apply(m, None, self.norm_weight, self.weight, self.bias, self).view(shape)
+        y, h = _NormLinearFn.apply(m, r, self.norm_weight, self.weight, self.bias, self)
+        return y.view(shape), h.view(x.shape)
+
+
+class Muon(torch.optim.Optimizer):
+    """Orthogonalised momentum for float32 weights of two or more dimensions (a convolution's is unfolded to
+    [out][in kh kw]): m = momentum m + g, u = g + momentum m (nesterov) or m, w = (1 - lr weight_decay) w
+    - lr sqrt(max(1, rows / cols)) NS(u), one fqt_muon_step per weight."""
+
+    def __init__(self, params, lr=0.02, momentum=0.95, weight_decay=0.0, nesterov=True, steps=5, eps=1e-7):
+        if lr < 0 or not 0 <= momentum < 1 or weight_decay < 0:
+            raise ValueError(f"lr {lr}, momentum {momentum}, weight_decay {weight_decay}: out of range")
+        super().__init__(params, dict(lr=lr, momentum=momentum, weight_decay=weight_decay,
+                                      nesterov=nesterov, steps=steps, eps=eps))
+        for group in self.param_groups:
+            for p in group["params"]:
+                if p.dim() < 2 or p.dtype != _F32:
+                    raise ValueError(f"Muon updates float32 matrices, got {p.dtype} {tuple(p.shape)}")
+        self._slots = _Slots()
+
+    @torch.no_grad()
+    def step(self, closure=None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        for group in self.param_groups:
+            for p in group["params"]:
+                if p.grad is None:
+                    continue
+                if not p.is_contiguous():
+                    raise ValueError("Muon updates contiguous weights in place")
+                w = p.view(p.shape[0], -1)
+                g = p.grad.reshape(p.shape[0], -1).contiguous()
+                state = self.state[p]
+                if "momentum" not in state:
+                    state["momentum"] = torch.zeros_like(p)
+                desc = dense.ortho_desc(*w.shape, g_dtype=g.dtype, steps=group["steps"], eps=group["eps"])
+                ws = self._slots.get(tuple(w.shape), dense.fqt_ortho_workspace_size(desc), p.device)
+                dense.fqt_muon_step(desc, w, g, state["momentum"].view_as(w), ws, lr=group["lr"],
+                                    momentum=group["momentum"], weight_decay=group["weight_decay"],
+                                    scale=math.sqrt(max(1.0, w.shape[0] / w.shape[1])),
+                                    nesterov=group["nesterov"])
+        return loss
+
+
+class Optimizers:
+    """Several optimizers behind the interface that train.train_step uses."""
+
+    def __init__(self, *optimizers):
+        self.optimizers = optimizers
+
+    def zero_grad(self, set_to_none=True):
+        for o in self.optimizers:
+            o.zero_grad(set_to_none=set_to_none)
+
+    def step(self):
+        for o in self.optimizers:
+            o.step()
+
+
+def muon_and_adam(model, lr=0.02, adam_lr=1e-3, first_last=()):
+    """Muon for the weight matrices of a model, Adam for its vectors and for the modules in first_last
+    (input and output layers, whose singular values carry meaning)."""
+    apart = {id(p) for m in first_last for p in m.parameters()}
+    matrices = [p for p in model.parameters() if p.dim() >= 2 and id(p) not in apart]
+    chosen = {id(p) for p in matrices}
+    rest = [p for p in model.parameters() if id(p) not in chosen]
+    return Optimizers(Muon(matrices, lr=lr), torch.optim.Adam(rest, lr=adam_lr))
+
+
+class ResidualMLP(nn.Module):
+    """features -> width, `depth` residual blocks, norm, classes.  A block norms the stream, expands it by
+    an 8-bit product with GELU, and projects back by a binary layer (1-bit FQT backward) whose input is
+    brought into its straight-through range by Hardtanh."""
+
+    def __init__(self, features, classes, width=256, hidden=512, depth=3, bits=4, operands="int8"):
+        super().__init__()
+        self.stem = Linear(features, width)
+        self.up = nn.ModuleList(NormLinear(width, hidden, act="gelu", operands=operands) for _ in range(depth))
+        self.down = nn.ModuleList(train.BinaryLinear(hidden, width, bits=bits, layer_id=i) for i in range(depth))
+        self.norm = RMSNorm(width)
+        self.head = Linear(width, classes)
+
+    def forward(self, x):
+        h, add = self.stem(x), None
+        for up, down in zip(self.up, self.down):
+            if add is None:
+                z = up(h)
+            else:
+                z, h = up(add, h)
+            add = down(nn.functional.hardtanh(z))
+        y, _ = self.norm(add, h)
+        return self.head(y)
