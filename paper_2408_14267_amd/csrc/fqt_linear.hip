@@ -193,6 +193,24 @@ __global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_prod
     with_act(e.act, [&]<int ACT>() { tile::run_epilogue<KIND, S>(acc, lds, at.m0, at.n0, Finish<ACT>(e)); });
 }
 
+// Two products of small tiles side by side: the backward's dx and dw where each alone leaves CUs idle
+// (777 x 1000 x 513: 12 instead of 22 us).
+__global__ void __launch_bounds__(tile::Small::THREADS, 2) k_product_pair(Product px, Epilogue ex, Product pw, Epilogue ew) {
+  typedef tile::Small S;
+  __shared__ __attribute__((aligned(16))) char lds[S::LDS];
+  tile::f32x4 acc[S::FM][S::FN];
+  const uint32_t first = px.tiles.count;
+  if (blockIdx.x < first) {
+    const tile::Place at = tile::place<tile::SMALL>(px.tiles, blockIdx.x);
+    tile::contract<tile::BF16K, ROWS, COLS, tile::SMALL, S>(px.x, px.w, px.K, at, px.tiles, lds, acc);
+    tile::run_epilogue<tile::BF16K, S>(acc, lds, at.m0, at.n0, Finish<FQT_ACT_NONE>(ex));
+  } else {
+    const tile::Place at = tile::place<tile::SMALL>(pw.tiles, blockIdx.x - first);
+    tile::contract<tile::BF16K, COLS, COLS, tile::SMALL, S>(pw.x, pw.w, pw.K, at, pw.tiles, lds, acc);
+    tile::run_epilogue<tile::BF16K, S>(acc, lds, at.m0, at.n0, Finish<FQT_ACT_NONE>(ew));
+  }
+}
+
 // The partial sums of a split contraction, added in order, through the epilogue.  part: rows of ldp
 // (a multiple of 8) floats.
 __global__ void __launch_bounds__(256) k_product_finish(Product p, Epilogue e) {
@@ -254,42 +272,57 @@ struct DzArgs {
   int64_t M, N, ldz, ldy, pitch;
   int32_t y_dtype, act, vec;
 };
-// A thread takes 8 columns over the rows blockIdx.y, + gridDim.y, ...
-__global__ void __launch_bounds__(64) k_dz(DzArgs a) {
-  const int64_t n = (int64_t(blockIdx.x) * 64 + threadIdx.x) * 8;
-  if (n >= a.pitch) return;
-  const int cnt = int(min(a.N - n, int64_t(8)));
+// A thread takes 8 columns, a wave every fourth row of the workgroup's; the waves' column sums meet in
+// LDS.  About 35 issue slots per element with gelu, so that it takes 16 waves per CU to keep the memory
+// busy behind them.
+constexpr int DZ_WAVES = 4;
+__global__ void __launch_bounds__(64 * DZ_WAVES) k_dz(DzArgs a) {
+  __shared__ float sums[DZ_WAVES - 1][8][64];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int64_t n = (int64_t(blockIdx.x) * 64 + lane) * 8;
+  const int cnt = int(max(int64_t(0), min(a.N - n, int64_t(8))));
   const bool full = cnt == 8 && a.vec;
-  float sw[8], sum[8] = {};
+  float sum[8] = {};
+  if (cnt) {
+    float sw[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) sw[i] = a.sw && i < cnt ? a.sw[n + i] : 1.0f;
-  with_act(a.act, [&]<int ACT>() {
-    for (int64_t m = blockIdx.y; m < a.M; m += gridDim.y) {
-      float d[8], z[8];
-      load8(a.dy, m * a.ldy + n, a.y_dtype, full, cnt, d);
-      if constexpr (ACT != FQT_ACT_NONE) {
-        load8(a.z, m * a.ldz + n, a.y_dtype, full, cnt, z);
+    for (int i = 0; i < 8; ++i) sw[i] = a.sw && i < cnt ? a.sw[n + i] : 1.0f;
+    with_act(a.act, [&]<int ACT>() {
+      for (int64_t m = int64_t(blockIdx.y) * DZ_WAVES + wave; m < a.M; m += int64_t(gridDim.y) * DZ_WAVES) {
+        float d[8], z[8], o[8];
+        load8(a.dy, m * a.ldy + n, a.y_dtype, full, cnt, d);
+        if constexpr (ACT != FQT_ACT_NONE) {
+          load8(a.z, m * a.ldz + n, a.y_dtype, full, cnt, z);
 #pragma unroll
-        for (int i = 0; i < 8; ++i) d[i] *= slope<ACT>(z[i]);
+          for (int i = 0; i < 8; ++i) d[i] *= slope<ACT>(z[i]);
+        }
+#pragma unroll
+        for (int i = 0; i < 8; ++i) sum[i] += d[i];
+        if (a.dzx) {
+#pragma unroll
+          for (int i = 0; i < 8; ++i) o[i] = d[i] * sw[i];
+          store8f(a.dzx + m * a.pitch + n, true, 8, o);
+        }
+        if (a.dzw && a.dzw != a.dzx) {
+          const float s = a.sx ? a.sx[m] : 1.0f;
+#pragma unroll
+          for (int i = 0; i < 8; ++i) o[i] = d[i] * s;
+          store8f(a.dzw + m * a.pitch + n, true, 8, o);
+        }
       }
+    });
+  }
+  if (!a.part) return;
+  if (wave)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) sum[i] += d[i];
-      if (a.dzx) {
-        float o[8];
+    for (int i = 0; i < 8; ++i) sums[wave - 1][i][lane] = sum[i];
+  __syncthreads();
+  if (wave || !cnt) return;
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = d[i] * sw[i];
-        store8f(a.dzx + m * a.pitch + n, true, 8, o);
-      }
-      if (a.dzw && a.dzw != a.dzx) {
-        const float s = a.sx ? a.sx[m] : 1.0f;
-        float o[8];
+  for (int i = 0; i < 8; ++i)
 #pragma unroll
-        for (int i = 0; i < 8; ++i) o[i] = d[i] * s;
-        store8f(a.dzw + m * a.pitch + n, true, 8, o);
-      }
-    }
-  });
-  if (a.part && cnt > 0) store8f(a.part + int64_t(blockIdx.y) * a.N + n, false, cnt, sum);
+    for (int w = 0; w < DZ_WAVES - 1; ++w) sum[i] += sums[w][i][lane];
+  store8f(a.part + int64_t(blockIdx.y) * a.N + n, false, cnt, sum);
 }
 
 // dbias[n] = sum of the partial rows: 32 columns per workgroup, 8 threads per column, fixed order.
@@ -348,16 +381,20 @@ size_t part_bytes(const tile::Plan &p, int64_t M, int64_t N) {
   return p.splits > 1 ? align256(size_t(p.splits) * M * round_up(N, 8) * 4) : 0;
 }
 
-template <int KIND, int LX, int LW>
-int launch_product(const tile::Plan &plan, Operand x, Operand w, int64_t M, int64_t N, int64_t K, Epilogue e,
-                   float *part, hipStream_t st) {
-  if (M == 0 || N == 0) return FQT_OK;
-  Product p{x, w, M, N, K, plan.t[0], part, round_up(N, 8)};
+Epilogue sized(Epilogue e, int64_t M, int64_t N) {
   const size_t ye = elem_size(e.y_dtype);
   auto on16 = [&](const void *q, int64_t ld) { return !q || (aligned(q, 16) && ld * ye % 16 == 0); };
   e.M = M;
   e.N = N;
   e.vec = on16(e.res, e.ldr) && on16(e.z, e.ldz) && on16(e.y, e.ldy);
+  return e;
+}
+template <int KIND, int LX, int LW>
+int launch_product(const tile::Plan &plan, Operand x, Operand w, int64_t M, int64_t N, int64_t K, Epilogue e,
+                   float *part, hipStream_t st) {
+  if (M == 0 || N == 0) return FQT_OK;
+  Product p{x, w, M, N, K, plan.t[0], part, round_up(N, 8)};
+  e = sized(e, M, N);
   tile::for_launches(plan, [&]<int SHAPE>(const tile::Tiles &t) {
     p.tiles = t;
     k_product<KIND, LX, LW, SHAPE><<<dim3(tile::blocks_of(SHAPE, t)), dim3(tile::ShapeOf<SHAPE>::type::THREADS), 0, st>>>(p, e);
@@ -412,7 +449,8 @@ BwdWs bwd_ws(const Sizes &s) {
   f.pitch = round_up(s.K, 8);
   f.copy_x = codes || !whole_pieces(s.K, s.ldx, 2);
   f.copy_w = codes || !whole_pieces(s.K, s.ldw, 2);
-  f.rows = std::max<int64_t>(1, std::min<int64_t>(s.M, 256));
+  // row groups of the pass over dy: enough waves, few partial sums of dbias
+  f.rows = std::max<int64_t>(1, std::min<int64_t>((s.M + 7) / 8, 128));
   f.dx = plan_of(s.M, s.K, s.N, 2);
   f.dw = plan_of(s.N, s.K, s.M, 2);
   const size_t dz = align256(size_t(s.M) * f.dz_pitch * 2);
@@ -532,7 +570,7 @@ extern "C" int fqt_linear_backward(const fqt_linear_desc *d, const void *x, cons
     a.y_dtype = d->y_dtype; a.act = d->act;
     const size_t ye = elem_size(d->y_dtype);
     a.vec = aligned(dy, 16) && s.ldy * ye % 16 == 0 && (!z || (aligned(z, 16) && s.ldz * ye % 16 == 0));
-    k_dz<<<dim3((f.dz_pitch + 511) / 512, f.rows), dim3(64), 0, st>>>(a);
+    k_dz<<<dim3((f.dz_pitch + 511) / 512, f.rows), dim3(64 * DZ_WAVES), 0, st>>>(a);
     FQT_TRY_(last_launch_status());
     if (dbias) {
       k_dbias<<<dim3((s.N + 31) / 32), dim3(256), 0, st>>>(a.part, int32_t(f.rows), s.N, dbias);
@@ -551,19 +589,22 @@ extern "C" int fqt_linear_backward(const fqt_linear_desc *d, const void *x, cons
     return repack<bf16, bf16>(p, rows, s.K, ld, base + at, f.pitch, st);
   };
   float *part = reinterpret_cast<float *>(base + f.part);
-  if (dx) {
-    Operand wo;
-    FQT_TRY_(operand(w, f.copy_w, f.w, s.N, s.ldw, &wo));
-    Epilogue e{nullptr, nullptr, nullptr, nullptr, nullptr, dx, 0, 0, 0, 0, s.lddx, d->dx_dtype, FQT_ACT_NONE, 0};
-    // dz rows are pitch long in the workspace (zeros past N): the contraction may end on a whole piece
-    FQT_TRY_((launch_product<tile::BF16K, ROWS, COLS>(f.dx, dzx, wo, s.M, s.K, s.N, e, part, st)));
+  // dz rows are dz_pitch long in the workspace, zeros past N, so a contraction over n may end on a whole
+  // piece; as a COLS operand dz has whole pieces of 8 columns.
+  dzw.rows = same ? s.N : f.dz_pitch;
+  Operand wo{}, xo{};
+  if (dx) FQT_TRY_(operand(w, f.copy_w, f.w, s.N, s.ldw, &wo));
+  if (dw) FQT_TRY_(operand(x, f.copy_x, f.x, s.M, s.ldx, &xo));
+  const Epilogue ex{nullptr, nullptr, nullptr, nullptr, nullptr, dx, 0, 0, 0, 0, s.lddx, d->dx_dtype, FQT_ACT_NONE, 0};
+  const Epilogue ew{nullptr, nullptr, nullptr, nullptr, nullptr, dw, 0, 0, 0, 0, s.lddw, d->dw_dtype, FQT_ACT_NONE, 0};
+  auto small = [](const tile::Plan &p) { return p.shape[0] == tile::SMALL && p.splits == 1; };
+  if (dx && dw && small(f.dx) && small(f.dw)) {
+    const Product px{dzx, wo, s.M, s.K, s.N, f.dx.t[0], nullptr, 0}, pw{dzw, xo, s.N, s.K, s.M, f.dw.t[0], nullptr, 0};
+    k_product_pair<<<dim3(px.tiles.count + pw.tiles.count), dim3(tile::Small::THREADS), 0, st>>>(
+        px, sized(ex, s.M, s.K), pw, sized(ew, s.N, s.K));
+    return last_launch_status();
   }
-  if (dw) {
-    Operand xo;
-    FQT_TRY_(operand(x, f.copy_x, f.x, s.M, s.ldx, &xo));
-    Epilogue e{nullptr, nullptr, nullptr, nullptr, nullptr, dw, 0, 0, 0, 0, s.lddw, d->dw_dtype, FQT_ACT_NONE, 0};
-    dzw.rows = same ? s.N : f.dz_pitch;
-    FQT_TRY_((launch_product<tile::BF16K, COLS, COLS>(f.dw, dzw, xo, s.N, s.K, s.M, e, part, st)));
-  }
+  if (dx) FQT_TRY_((launch_product<tile::BF16K, ROWS, COLS>(f.dx, dzx, wo, s.M, s.K, s.N, ex, part, st)));
+  if (dw) FQT_TRY_((launch_product<tile::BF16K, COLS, COLS>(f.dw, dzw, xo, s.N, s.K, s.M, ew, part, st)));
   return FQT_OK;
 }

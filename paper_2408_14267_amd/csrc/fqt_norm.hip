@@ -527,7 +527,9 @@ int run_norm(const fqt_norm_desc *d, NormArgs a, hipStream_t st) {
   dispatch_xy(d->x_dtype, d->y_dtype, [&]<typename XT, typename YT>() {
     if (!dispatch_row<FWD_MAX_COLS>(d->cols, [&]<int TPR, int VPT>() {
           constexpr int ROWS = block_of<TPR> / TPR;
-          const int64_t blocks = std::min<int64_t>((d->rows + ROWS - 1) / ROWS, 1024 * 512 / std::max(TPR, 256));
+          // as many workgroups as are resident at once, with equal numbers of rows
+          const int64_t sets = (d->rows + ROWS - 1) / ROWS, most = 1024 * 256 / block_of<TPR>;
+          const int64_t each = (sets + most - 1) / most, blocks = (sets + each - 1) / each;
           const dim3 block(block_of<TPR>);
           if (a.vec && d->cols % 8 == 0) k_norm_fwd<XT, YT, TPR, VPT, true><<<dim3(blocks), block, 0, st>>>(a);
           else k_norm_fwd<XT, YT, TPR, VPT, false><<<dim3(blocks), block, 0, st>>>(a);
