@@ -193,24 +193,6 @@ __global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_prod
     with_act(e.act, [&]<int ACT>() { tile::run_epilogue<KIND, S>(acc, lds, at.m0, at.n0, Finish<ACT>(e)); });
 }
 
-// Two products of small tiles side by side: the backward's dx and dw where each alone leaves CUs idle
-// (777 x 1000 x 513: 12 instead of 22 us).
-__global__ void __launch_bounds__(tile::Small::THREADS, 2) k_product_pair(Product px, Epilogue ex, Product pw, Epilogue ew) {
-  typedef tile::Small S;
-  __shared__ __attribute__((aligned(16))) char lds[S::LDS];
-  tile::f32x4 acc[S::FM][S::FN];
-  const uint32_t first = px.tiles.count;
-  if (blockIdx.x < first) {
-    const tile::Place at = tile::place<tile::SMALL>(px.tiles, blockIdx.x);
-    tile::contract<tile::BF16K, ROWS, COLS, tile::SMALL, S>(px.x, px.w, px.K, at, px.tiles, lds, acc);
-    tile::run_epilogue<tile::BF16K, S>(acc, lds, at.m0, at.n0, Finish<FQT_ACT_NONE>(ex));
-  } else {
-    const tile::Place at = tile::place<tile::SMALL>(pw.tiles, blockIdx.x - first);
-    tile::contract<tile::BF16K, COLS, COLS, tile::SMALL, S>(pw.x, pw.w, pw.K, at, pw.tiles, lds, acc);
-    tile::run_epilogue<tile::BF16K, S>(acc, lds, at.m0, at.n0, Finish<FQT_ACT_NONE>(ew));
-  }
-}
-
 // The partial sums of a split contraction, added in order, through the epilogue.  part: rows of ldp
 // (a multiple of 8) floats.
 __global__ void __launch_bounds__(256) k_product_finish(Product p, Epilogue e) {
@@ -246,20 +228,32 @@ template <> __device__ __forceinline__ bf16 widen<int8_t, bf16>(int8_t v) { retu
 template <> __device__ __forceinline__ bf16 widen<e4m3, bf16>(e4m3 v) {
   return from_f32<bf16>(__builtin_amdgcn_cvt_f32_fp8(int(v.v), 0));
 }
+struct Copy {
+  const void *src;
+  void *dst;
+  int64_t rows, cols, ld, pitch;
+  uint32_t blocks;         // workgroups of 256 threads (0: no copy)
+};
 template <typename ST, typename DT>
-__global__ void __launch_bounds__(256) k_repack(const ST *src, int64_t rows, int64_t cols, int64_t ld,
-                                                DT *dst, int64_t pitch) {
+__device__ __forceinline__ void repack_rows(const Copy &a, uint32_t block) {
   constexpr int V = 16 / sizeof(DT);
-  const int64_t groups = pitch / V, all = rows * groups;
-  for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
+  const int64_t groups = a.pitch / V, all = a.rows * groups;
+  for (int64_t i = int64_t(block) * 256 + threadIdx.x; i < all; i += int64_t(a.blocks) * 256) {
     const int64_t r = i / groups, c = i % groups * V;
+    const ST *src = static_cast<const ST *>(a.src) + r * a.ld + c;
     DT o[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) o[j] = c + j < cols ? widen<ST, DT>(src[r * ld + c + j]) : DT{};
+    for (int j = 0; j < V; ++j) o[j] = c + j < a.cols ? widen<ST, DT>(src[j]) : DT{};
     uint4 u;
     __builtin_memcpy(&u, o, 16);
-    *reinterpret_cast<uint4 *>(dst + r * pitch + c) = u;
+    *reinterpret_cast<uint4 *>(static_cast<DT *>(a.dst) + r * a.pitch + c) = u;
   }
+}
+// Both operands' copies in one launch.
+template <typename ST, typename DT>
+__global__ void __launch_bounds__(256) k_repack(Copy x, Copy w) {
+  if (blockIdx.x < x.blocks) repack_rows<ST, DT>(x, blockIdx.x);
+  else repack_rows<ST, DT>(w, blockIdx.x - x.blocks);
 }
 
 // ----------------------------------------------------------------------------- dz
@@ -268,18 +262,20 @@ struct DzArgs {
   const void *z, *dy;
   const float *sx, *sw;
   bf16 *dzx, *dzw;       // dz sw (for dx) and dz sx (for dw), rows of `pitch`; may be one array
-  float *part;           // [gridDim.y][N] partial column sums of dz, or null
+  float *part;           // [rows][N] partial column sums of dz, or null
   int64_t M, N, ldz, ldy, pitch;
   int32_t y_dtype, act, vec;
+  uint32_t rows, blocks; // row groups; workgroups (row groups times 512-column groups)
 };
 // A thread takes 8 columns, a wave every fourth row of the workgroup's; the waves' column sums meet in
 // LDS.  About 35 issue slots per element with gelu, so that it takes 16 waves per CU to keep the memory
 // busy behind them.
 constexpr int DZ_WAVES = 4;
-__global__ void __launch_bounds__(64 * DZ_WAVES) k_dz(DzArgs a) {
+__device__ __forceinline__ void dz_pass(const DzArgs &a, uint32_t block) {
   __shared__ float sums[DZ_WAVES - 1][8][64];
   const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
-  const int64_t n = (int64_t(blockIdx.x) * 64 + lane) * 8;
+  const uint32_t row0 = block % a.rows;
+  const int64_t n = (int64_t(block / a.rows) * 64 + lane) * 8;
   const int cnt = int(max(int64_t(0), min(a.N - n, int64_t(8))));
   const bool full = cnt == 8 && a.vec;
   float sum[8] = {};
@@ -288,7 +284,7 @@ __global__ void __launch_bounds__(64 * DZ_WAVES) k_dz(DzArgs a) {
 #pragma unroll
     for (int i = 0; i < 8; ++i) sw[i] = a.sw && i < cnt ? a.sw[n + i] : 1.0f;
     with_act(a.act, [&]<int ACT>() {
-      for (int64_t m = int64_t(blockIdx.y) * DZ_WAVES + wave; m < a.M; m += int64_t(gridDim.y) * DZ_WAVES) {
+      for (int64_t m = int64_t(row0) * DZ_WAVES + wave; m < a.M; m += int64_t(a.rows) * DZ_WAVES) {
         float d[8], z[8], o[8];
         load8(a.dy, m * a.ldy + n, a.y_dtype, full, cnt, d);
         if constexpr (ACT != FQT_ACT_NONE) {
@@ -322,24 +318,64 @@ __global__ void __launch_bounds__(64 * DZ_WAVES) k_dz(DzArgs a) {
   for (int i = 0; i < 8; ++i)
 #pragma unroll
     for (int w = 0; w < DZ_WAVES - 1; ++w) sum[i] += sums[w][i][lane];
-  store8f(a.part + int64_t(blockIdx.y) * a.N + n, false, cnt, sum);
+  store8f(a.part + int64_t(row0) * a.N + n, false, cnt, sum);
+}
+
+// What the products wait for, in one launch: the pass over dy and the copies of both operands.
+template <typename ST>
+__global__ void __launch_bounds__(256) k_prepare(DzArgs a, Copy x, Copy w) {
+  static_assert(DZ_WAVES == 4, "256 threads");
+  const uint32_t b = blockIdx.x;
+  if (b < a.blocks) dz_pass(a, b);
+  else if (b < a.blocks + x.blocks) repack_rows<ST, bf16>(x, b - a.blocks);
+  else repack_rows<ST, bf16>(w, b - a.blocks - x.blocks);
 }
 
 // dbias[n] = sum of the partial rows: 32 columns per workgroup, 8 threads per column, fixed order.
-__global__ void __launch_bounds__(256) k_dbias(const float *part, int32_t parts, int64_t N, float *dbias) {
-  __shared__ float s[8][32];
-  const int64_t c = int64_t(blockIdx.x) * 32 + threadIdx.x % 32;
+struct DbiasArgs {
+  const float *part;
+  float *dbias;            // or null
+  int64_t N;
+  int32_t parts;
+};
+__device__ __forceinline__ void sum_dbias(const DbiasArgs &a, uint32_t block, float (*s)[32]) {
+  const int64_t c = int64_t(block) * 32 + threadIdx.x % 32;
   const int k = threadIdx.x / 32;
   float v = 0.0f;
-  if (c < N)
+  if (c < a.N)
 #pragma unroll 8
-    for (int p = k; p < parts; p += 8) v += part[int64_t(p) * N + c];
+    for (int p = k; p < a.parts; p += 8) v += a.part[int64_t(p) * a.N + c];
   s[k][threadIdx.x % 32] = v;
   __syncthreads();
-  if (k == 0 && c < N) {
+  if (k == 0 && c < a.N) {
 #pragma unroll
     for (int j = 1; j < 8; ++j) v += s[j][threadIdx.x];
-    dbias[c] = v;
+    a.dbias[c] = v;
+  }
+}
+__global__ void __launch_bounds__(256) k_dbias(DbiasArgs a) {
+  __shared__ float s[8][32];
+  sum_dbias(a, blockIdx.x, s);
+}
+
+// Two products of small tiles side by side, and dbias: the backward's dx and dw where each alone leaves
+// CUs idle (777 x 1000 x 513: 13 instead of 22 + 4 us).
+__global__ void __launch_bounds__(tile::Small::THREADS, 2) k_product_pair(Product px, Epilogue ex, Product pw, Epilogue ew, DbiasArgs b) {
+  typedef tile::Small S;
+  static_assert(S::THREADS == 256, "dbias takes 256 threads");
+  __shared__ __attribute__((aligned(16))) char lds[S::LDS];
+  tile::f32x4 acc[S::FM][S::FN];
+  const uint32_t first = px.tiles.count, second = first + pw.tiles.count;
+  if (blockIdx.x < first) {
+    const tile::Place at = tile::place<tile::SMALL>(px.tiles, blockIdx.x);
+    tile::contract<tile::BF16K, ROWS, COLS, tile::SMALL, S>(px.x, px.w, px.K, at, px.tiles, lds, acc);
+    tile::run_epilogue<tile::BF16K, S>(acc, lds, at.m0, at.n0, Finish<FQT_ACT_NONE>(ex));
+  } else if (blockIdx.x < second) {
+    const tile::Place at = tile::place<tile::SMALL>(pw.tiles, blockIdx.x - first);
+    tile::contract<tile::BF16K, COLS, COLS, tile::SMALL, S>(pw.x, pw.w, pw.K, at, pw.tiles, lds, acc);
+    tile::run_epilogue<tile::BF16K, S>(acc, lds, at.m0, at.n0, Finish<FQT_ACT_NONE>(ew));
+  } else {
+    sum_dbias(b, blockIdx.x - second, reinterpret_cast<float (*)[32]>(lds));
   }
 }
 __global__ void __launch_bounds__(256) k_zero(char *p, int64_t rows, int64_t bytes, int64_t ld) {
@@ -408,13 +444,10 @@ int launch_product(const tile::Plan &plan, Operand x, Operand w, int64_t M, int6
   return FQT_OK;
 }
 
-template <typename ST, typename DT>
-int repack(const void *src, int64_t rows, int64_t cols, int64_t ld, void *dst, int64_t pitch, hipStream_t st) {
-  const int64_t all = rows * (pitch / int64_t(16 / sizeof(DT)));
-  if (all == 0) return FQT_OK;
-  k_repack<ST, DT><<<dim3(std::min<int64_t>((all + 255) / 256, 8192)), dim3(256), 0, st>>>(
-      static_cast<const ST *>(src), rows, cols, ld, static_cast<DT *>(dst), pitch);
-  return last_launch_status();
+// The copy of an operand into rows of `pitch` elements of e bytes.
+Copy copy_of(const void *src, int64_t rows, int64_t cols, int64_t ld, void *dst, int64_t pitch, int64_t e) {
+  const int64_t all = rows * (pitch * e / 16);
+  return {src, dst, rows, cols, ld, pitch, uint32_t(std::min<int64_t>((all + 255) / 256, 4096))};
 }
 
 // Workspace of the forward: padded copies of operands whose rows are not whole 16-byte pieces, and
@@ -504,19 +537,19 @@ extern "C" int fqt_linear_forward(const fqt_linear_desc *d, const void *x, const
   if (ws_bytes < f.total) return FQT_E_WORKSPACE;
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   char *base = static_cast<char *>(ws);
-  auto operand = [&](const void *p, bool copy, size_t at, int64_t rows, int64_t ld, Operand *o) -> int {
-    if (!copy) {
-      *o = {static_cast<const char *>(p), ld * f.e, rows};
-      return FQT_OK;
-    }
-    *o = {base + at, f.pitch * f.e, rows};
-    if (f.widen) return repack<e4m3, bf16>(p, rows, s.K, ld, base + at, f.pitch, st);
-    return codes ? repack<int8_t, int8_t>(p, rows, s.K, ld, base + at, f.pitch, st)
-                 : repack<bf16, bf16>(p, rows, s.K, ld, base + at, f.pitch, st);
+  auto operand = [&](const void *p, bool copy, size_t at, int64_t rows, int64_t ld, Copy *c) -> Operand {
+    if (!copy) return {static_cast<const char *>(p), ld * f.e, rows};
+    *c = copy_of(p, rows, s.K, ld, base + at, f.pitch, f.e);
+    return {base + at, f.pitch * f.e, rows};
   };
-  Operand xo, wo;
-  FQT_TRY_(operand(x, f.copy_x, f.x, s.M, s.ldx, &xo));
-  FQT_TRY_(operand(w, f.copy_w, f.w, s.N, s.ldw, &wo));
+  Copy cx{}, cw{};
+  const Operand xo = operand(x, f.copy_x, f.x, s.M, s.ldx, &cx), wo = operand(w, f.copy_w, f.w, s.N, s.ldw, &cw);
+  if (const dim3 grid(cx.blocks + cw.blocks); grid.x) {
+    if (f.widen) k_repack<e4m3, bf16><<<grid, dim3(256), 0, st>>>(cx, cw);
+    else if (codes) k_repack<int8_t, int8_t><<<grid, dim3(256), 0, st>>>(cx, cw);
+    else k_repack<bf16, bf16><<<grid, dim3(256), 0, st>>>(cx, cw);
+    FQT_TRY_(last_launch_status());
+  }
   const int64_t K = f.copy_x || f.copy_w ? f.pitch : s.K;
   Epilogue e{x_scale, w_scale, bias, residual, z, y, 0, 0, s.ldr, s.ldz, s.ldy, d->y_dtype, d->act, 0};
   float *part = reinterpret_cast<float *>(base + f.part);
@@ -559,8 +592,17 @@ extern "C" int fqt_linear_backward(const fqt_linear_desc *d, const void *x, cons
                     whole_pieces(s.N, s.ldy, 2) && aligned(dy, 16);
   Operand dzx{base + f.dzx, f.dz_pitch * 2, s.M}, dzw{base + f.dzw, f.dz_pitch * 2, s.M};
   if (same) dzx = dzw = {static_cast<const char *>(dy), s.ldy * 2, s.M};
+  auto operand = [&](const void *p, bool copy, size_t at, int64_t rows, int64_t ld, Copy *c) -> Operand {
+    if (!copy) return {static_cast<const char *>(p), ld * 2, s.K};
+    *c = copy_of(p, rows, s.K, ld, base + at, f.pitch, 2);
+    return {base + at, f.pitch * 2, f.pitch};
+  };
+  Copy cx{}, cw{};
+  Operand wo{}, xo{};
+  if (dx) wo = operand(w, f.copy_w, f.w, s.N, s.ldw, &cw);
+  if (dw) xo = operand(x, f.copy_x, f.x, s.M, s.ldx, &cx);
+  DzArgs a{};
   if (!same || dbias) {
-    DzArgs a{};
     a.z = z; a.dy = dy;
     a.sx = x_scale; a.sw = w_scale;
     if (!same && dx) a.dzx = reinterpret_cast<bf16 *>(base + f.dzx);
@@ -570,40 +612,35 @@ extern "C" int fqt_linear_backward(const fqt_linear_desc *d, const void *x, cons
     a.y_dtype = d->y_dtype; a.act = d->act;
     const size_t ye = elem_size(d->y_dtype);
     a.vec = aligned(dy, 16) && s.ldy * ye % 16 == 0 && (!z || (aligned(z, 16) && s.ldz * ye % 16 == 0));
-    k_dz<<<dim3((f.dz_pitch + 511) / 512, f.rows), dim3(64 * DZ_WAVES), 0, st>>>(a);
-    FQT_TRY_(last_launch_status());
-    if (dbias) {
-      k_dbias<<<dim3((s.N + 31) / 32), dim3(256), 0, st>>>(a.part, int32_t(f.rows), s.N, dbias);
-      FQT_TRY_(last_launch_status());
-    }
+    a.rows = uint32_t(f.rows);
+    a.blocks = uint32_t((f.dz_pitch + 511) / 512 * f.rows);
   }
-  if (s.K == 0) return FQT_OK;
-  auto operand = [&](const void *p, bool copy, size_t at, int64_t rows, int64_t ld, Operand *o) -> int {
-    if (!copy) {
-      *o = {static_cast<const char *>(p), ld * 2, s.K};
-      return FQT_OK;
-    }
-    *o = {base + at, f.pitch * 2, f.pitch};
-    if (d->x_dtype == FQT_I8) return repack<int8_t, bf16>(p, rows, s.K, ld, base + at, f.pitch, st);
-    if (d->x_dtype == FQT_E4M3) return repack<e4m3, bf16>(p, rows, s.K, ld, base + at, f.pitch, st);
-    return repack<bf16, bf16>(p, rows, s.K, ld, base + at, f.pitch, st);
-  };
+  if (const dim3 grid(a.blocks + cx.blocks + cw.blocks); grid.x) {
+    if (d->x_dtype == FQT_I8) k_prepare<int8_t><<<grid, dim3(256), 0, st>>>(a, cx, cw);
+    else if (d->x_dtype == FQT_E4M3) k_prepare<e4m3><<<grid, dim3(256), 0, st>>>(a, cx, cw);
+    else k_prepare<bf16><<<grid, dim3(256), 0, st>>>(a, cx, cw);
+    FQT_TRY_(last_launch_status());
+  }
+  const DbiasArgs bias{a.part, dbias, s.N, int32_t(f.rows)};
+  const uint32_t bias_blocks = dbias ? uint32_t((s.N + 31) / 32) : 0;
   float *part = reinterpret_cast<float *>(base + f.part);
   // dz rows are dz_pitch long in the workspace, zeros past N, so a contraction over n may end on a whole
   // piece; as a COLS operand dz has whole pieces of 8 columns.
   dzw.rows = same ? s.N : f.dz_pitch;
-  Operand wo{}, xo{};
-  if (dx) FQT_TRY_(operand(w, f.copy_w, f.w, s.N, s.ldw, &wo));
-  if (dw) FQT_TRY_(operand(x, f.copy_x, f.x, s.M, s.ldx, &xo));
   const Epilogue ex{nullptr, nullptr, nullptr, nullptr, nullptr, dx, 0, 0, 0, 0, s.lddx, d->dx_dtype, FQT_ACT_NONE, 0};
   const Epilogue ew{nullptr, nullptr, nullptr, nullptr, nullptr, dw, 0, 0, 0, 0, s.lddw, d->dw_dtype, FQT_ACT_NONE, 0};
   auto small = [](const tile::Plan &p) { return p.shape[0] == tile::SMALL && p.splits == 1; };
-  if (dx && dw && small(f.dx) && small(f.dw)) {
+  if (dx && dw && s.K && small(f.dx) && small(f.dw)) {
     const Product px{dzx, wo, s.M, s.K, s.N, f.dx.t[0], nullptr, 0}, pw{dzw, xo, s.N, s.K, s.M, f.dw.t[0], nullptr, 0};
-    k_product_pair<<<dim3(px.tiles.count + pw.tiles.count), dim3(tile::Small::THREADS), 0, st>>>(
-        px, sized(ex, s.M, s.K), pw, sized(ew, s.N, s.K));
+    k_product_pair<<<dim3(px.tiles.count + pw.tiles.count + bias_blocks), dim3(tile::Small::THREADS), 0, st>>>(
+        px, sized(ex, s.M, s.K), pw, sized(ew, s.N, s.K), bias);
     return last_launch_status();
   }
+  if (dbias) {
+    k_dbias<<<dim3(bias_blocks), dim3(256), 0, st>>>(bias);
+    FQT_TRY_(last_launch_status());
+  }
+  if (s.K == 0) return FQT_OK;
   if (dx) FQT_TRY_((launch_product<tile::BF16K, ROWS, COLS>(f.dx, dzx, wo, s.M, s.K, s.N, ex, part, st)));
   if (dw) FQT_TRY_((launch_product<tile::BF16K, COLS, COLS>(f.dw, dzw, xo, s.N, s.K, s.M, ew, part, st)));
   return FQT_OK;
