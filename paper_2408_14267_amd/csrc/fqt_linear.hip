@@ -433,7 +433,7 @@ int launch_product(const tile::Plan &plan, Operand x, Operand w, int64_t M, int6
   e = sized(e, M, N);
   tile::for_launches(plan, [&]<int SHAPE>(const tile::Tiles &t) {
     p.tiles = t;
-    k_product<KIND, LX, LW, SHAPE><<<dim3(tile::blocks_of(SHAPE, t)), dim3(tile::ShapeOf<SHAPE>::type::THREADS), 0, st>>>(p, e);
+    k_product<KIND, LX, LW, SHAPE><<<dim3(tile::blocks_of(t)), dim3(tile::ShapeOf<SHAPE>::type::THREADS), 0, st>>>(p, e);
   });
   FQT_TRY_(last_launch_status());
   if (plan.splits > 1) {
@@ -629,7 +629,7 @@ extern "C" int fqt_linear_backward(const fqt_linear_desc *d, const void *x, cons
   dzw.rows = same ? s.N : f.dz_pitch;
   const Epilogue ex{nullptr, nullptr, nullptr, nullptr, nullptr, dx, 0, 0, 0, 0, s.lddx, d->dx_dtype, FQT_ACT_NONE, 0};
   const Epilogue ew{nullptr, nullptr, nullptr, nullptr, nullptr, dw, 0, 0, 0, 0, s.lddw, d->dw_dtype, FQT_ACT_NONE, 0};
-  auto small = [](const tile::Plan &p) { return p.shape[0] == tile::SMALL && p.splits == 1; };
+  auto small = [](const tile::Plan &p) { return p.shape[0] == tile::SMALL && p.launches == 1 && p.splits == 1; };
   if (dx && dw && s.K && small(f.dx) && small(f.dw)) {
     const Product px{dzx, wo, s.M, s.K, s.N, f.dx.t[0], nullptr, 0}, pw{dzw, xo, s.N, s.K, s.M, f.dw.t[0], nullptr, 0};
     k_product_pair<<<dim3(px.tiles.count + pw.tiles.count + bias_blocks), dim3(tile::Small::THREADS), 0, st>>>(

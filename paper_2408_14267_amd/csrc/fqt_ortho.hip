@@ -580,7 +580,7 @@ template <int MODE>
 int launch_ns(const tile::Plan &plan, NsArgs a, hipStream_t st) {
   tile::for_launches(plan, [&]<int SHAPE>(const tile::Tiles &t) {
     a.tiles = t;
-    k_ns<MODE, SHAPE><<<dim3(tile::blocks_of(SHAPE, t)), dim3(tile::ShapeOf<SHAPE>::type::THREADS), 0, st>>>(a);
+    k_ns<MODE, SHAPE><<<dim3(tile::blocks_of(t)), dim3(tile::ShapeOf<SHAPE>::type::THREADS), 0, st>>>(a);
     if (t.splits > 1) {
       if constexpr (MODE == APPLY)
         k_ns_join<<<dim3(std::min<int64_t>((a.mp * a.np / 8 + 255) / 256, 4096)), dim3(256), 0, st>>>(a);

@@ -507,23 +507,25 @@ struct StorePart {
 };
 
 // ----------------------------------------------------------------------------- plans
-// The shapes of a workgroup's tile.  us of a 128-byte step of the contraction, measured on bf16 with
-// one (two) workgroups per CU: Large 1.58; Middle 0.60 (0.90); Small 0.27 (0.40); Part 0.37.
+// The shapes of a workgroup's tile.
 using Large = Shape<256, 256, 2, 4>;
 using Middle = Shape<128, 128, 2, 2>;
-using Small = Shape<64, 64, 2, 2, 4>;
-// An eighth of a Large tile, for the tiles that a last round of workgroups would leave most CUs idle
-// with: 32 Large tiles over 64 steps take 104 us, their 256 parts 29 us.
-using Part = Shape<128, 64, 4, 2, 5>;
-enum ShapeId { LARGE, MIDDLE, SMALL, PART };
+using Small = Shape<64, 64, 2, 2, 3>;
+enum ShapeId { LARGE, MIDDLE, SMALL };
+template <int SHAPE> struct ShapeOf;
+template <> struct ShapeOf<LARGE> { typedef Large type; };
+template <> struct ShapeOf<MIDDLE> { typedef Middle type; };
+template <> struct ShapeOf<SMALL> { typedef Small type; };
 
-// One launch of a product: `count` tiles from tile `first` on, of an order over nm x nn tiles (those of
-// shape Large for Part) or, symmetric, over the tiles on and above the diagonal.
+// One launch of a product: `count` tiles from tile `first` on, of an order over nm x nn tiles or,
+// symmetric, over the tiles on and above the diagonal.  parts: workgroups take sixteenths (Small) of
+// the tiles of a Large grid, for the tiles that a last round of workgroups would leave most CUs idle
+// with: 32 Large tiles over 64 steps take 104 us, their 512 parts 26 us.
 struct Tiles {
   uint32_t nm, nn, first, count;
-  uint32_t splits;         // parts of the contraction, each `steps` long
+  uint32_t splits;         // pieces of the contraction, each `steps` long
   uint32_t steps;
-  int32_t symmetric;
+  int32_t symmetric, parts;
 };
 struct Plan {
   int shape[2];
@@ -550,43 +552,43 @@ inline Plan make_plan(int64_t M, int64_t N, int64_t steps, bool symmetric) {
   };
   const double s = double(steps);
   const double entries = double(M) * double(N) * (symmetric ? 0.5 : 1.0);
+  // us of `blocks` workgroups of `n` steps, `cu` of which fit a CU, at step[k] us a step with k + 1 of them
+  // there (measured on bf16) and `start` us before the first and after the last
+  auto run = [](uint32_t blocks, double n, int cu, const double *step, double start) {
+    const uint32_t full = 256 * cu, rest = blocks % full;
+    double c = blocks / full * (step[cu - 1] * n + start);
+    if (rest) c += step[(rest - 1) / 256] * n + start;
+    return c;
+  };
+  static const double large[] = {1.58}, middle[] = {0.60, 0.90}, small[] = {0.25, 0.40, 0.58};
+  const double launch = 3;
   {
     const Tiles t = grid(256);
-    const uint32_t tail = t.count % 256, rounds = t.count / 256;
-    Plan p{{LARGE, PART}, {t, t}, 1, 1};
-    take((rounds + (tail > 0)) * (1.58 * s + 6) + 3, p);
-    if (tail) {
-      const double parts = ((8 * tail + 255) / 256) * (0.37 * s + 4) + 3;
+    const uint32_t tail = t.count % 256;
+    if (tail && t.count > 256) {
+      Plan p{{LARGE, SMALL}, {t, t}, 2, 1};
       p.t[0].count = t.count - tail;
       p.t[1].first = t.count - tail;
       p.t[1].count = tail;
-      if (rounds == 0) {
-        p.shape[0] = PART;
-        p.t[0] = p.t[1];
-      } else {
-        p.launches = 2;
-      }
-      take(rounds * (1.58 * s + 6) + 3 + parts, p);
+      p.t[1].parts = 1;
+      take(run(p.t[0].count, s, 1, large, 6) + run(16 * tail, s, 3, small, 4) + 2 * launch, p);
     }
   }
-  // `full` workgroups at a time; us of a step with one and with two of them on a CU
-  auto split = [&](int shape, int64_t b, uint32_t full, double one, double two) {
+  auto split = [&](int shape, int64_t b, int cu, const double *step, double start) {
     const Tiles g = grid(b);
     for (int64_t n = 1; n <= 64 && (n == 1 || steps / n >= 4); n += n < 16 ? 1 : 8) {
       Tiles t = g;
       t.steps = uint32_t(std::max<int64_t>(1, (steps + n - 1) / n));
       t.splits = uint32_t(std::max<int64_t>(1, (steps + t.steps - 1) / t.steps));
-      const uint32_t blocks = t.count * t.splits, rest = blocks % full;
-      double c = (blocks / full) * (two * t.steps + 5) + 3;
-      if (rest) c += (rest > 256 ? two : one) * t.steps + 5;
+      double c = run(t.count * t.splits, t.steps, cu, step, start) + launch;
       // the partial sums, written and read at 4 TB/s, and their launch
       if (t.splits > 1) c += 4 + t.splits * entries * 8 / 4e6;
       take(c, Plan{{shape, shape}, {t, t}, 1, t.splits});
     }
   };
-  split(LARGE, 256, 256, 1.58, 1.58);
-  split(MIDDLE, 128, 512, 0.60, 0.90);
-  split(SMALL, 64, 512, 0.27, 0.40);
+  split(LARGE, 256, 1, large, 6);
+  split(MIDDLE, 128, 2, middle, 5);
+  split(SMALL, 64, 3, small, 4);
   return best;
 }
 
@@ -596,24 +598,19 @@ struct Place {
   uint32_t split;
   bool diagonal;           // of a symmetric product: the tile is its own mirror image
 };
-template <int SHAPE> struct ShapeOf;
-template <> struct ShapeOf<LARGE> { typedef Large type; };
-template <> struct ShapeOf<MIDDLE> { typedef Middle type; };
-template <> struct ShapeOf<SMALL> { typedef Small type; };
-template <> struct ShapeOf<PART> { typedef Part type; };
-
 // Each XCD (b % 8) walks a contiguous run of the order below, which goes down GROUP tiles of m before
 // the next n, so that the tiles an XCD has in flight share operand rows in its L2.
 template <int SHAPE>
 __device__ __forceinline__ Place place(const Tiles &t, uint32_t b) {
-  constexpr uint32_t PARTS = SHAPE == PART ? 8 : 1;
-  const uint32_t total = t.count * PARTS;
+  typedef typename ShapeOf<SHAPE>::type S;
+  const uint32_t parts = SHAPE == SMALL && t.parts ? 16 : 1;
+  const uint32_t total = t.count * parts;
   const uint32_t split = b / total;
   b %= total;
   const uint32_t q = total / XCDS, r = total % XCDS, x = b % XCDS;
   uint32_t s = x * q + min(x, r) + b / XCDS;
-  const uint32_t part = s % PARTS;
-  s = s / PARTS + t.first;
+  const uint32_t part = s % parts;
+  s = s / parts + t.first;
   uint32_t m, n;
   if (t.symmetric) {       // by columns of the upper triangle
     n = uint32_t((sqrtf(8.0f * float(s) + 1.0f) - 1.0f) * 0.5f);
@@ -627,13 +624,11 @@ __device__ __forceinline__ Place place(const Tiles &t, uint32_t b) {
     m = g * GROUP + in % rows;
     n = in / rows;
   }
-  if constexpr (SHAPE == PART)
-    return {int64_t(m) * 256 + part / 4 * 128, int64_t(n) * 256 + part % 4 * 64, split, m == n};
-  typedef typename ShapeOf<SHAPE>::type S;
+  if (parts > 1) return {int64_t(m) * 256 + part / 4 * 64, int64_t(n) * 256 + part % 4 * 64, split, m == n};
   return {int64_t(m) * S::BM, int64_t(n) * S::BN, split, m == n};
 }
 // Workgroups of a launch.
-inline uint32_t blocks_of(int shape, const Tiles &t) { return t.count * t.splits * (shape == PART ? 8 : 1); }
+inline uint32_t blocks_of(const Tiles &t) { return t.count * t.splits * (t.parts ? 16 : 1); }
 
 // The accumulators of a placed tile, by the loop that suits the shape.
 template <int KIND, int LX, int LW, int SHAPE, typename S>
@@ -654,8 +649,7 @@ inline void for_launches(const Plan &p, F &&f) {
     switch (p.shape[i]) {
       case LARGE: f.template operator()<LARGE>(p.t[i]); break;
       case MIDDLE: f.template operator()<MIDDLE>(p.t[i]); break;
-      case SMALL: f.template operator()<SMALL>(p.t[i]); break;
-      default: f.template operator()<PART>(p.t[i]);
+      default: f.template operator()<SMALL>(p.t[i]);
     }
   }
 }
