@@ -9,8 +9,8 @@
  *  - A matrix [rows][cols] has unit stride along cols and a row stride `ld` in elements; ld = 0
  *    stands for cols, any other ld must be >= cols and at most FQT_MAX_LD.
  *  - x and w of a product start on 16 bytes, every other matrix and vector on its element size,
- *    workspaces on 256 bytes (FQT_E_ALIGN otherwise).  Rows that are multiples of 16 bytes long and
- *    apart take the fast paths; others cost a copy (products) or narrower accesses (norms).
+ *    workspaces on 256 bytes (FQT_E_ALIGN otherwise).  Operand rows of a
+ *    product that are not multiples of 16 bytes long and apart cost a copy.
  *  - A row or column count of zero is no error: nothing is launched but what an output needs (the
  *    gradient of a parameter over no rows is zero, a product over no columns is its bias).
  *  - Optional pointers may be NULL.  Outputs must not overlap inputs or each other unless a

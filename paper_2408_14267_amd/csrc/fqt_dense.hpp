@@ -35,23 +35,38 @@ template <> __device__ __forceinline__ bf16 from_f32<bf16>(float v) {
   return bf16{uint16_t(pack_bf16(v, v))};
 }
 
-// 8 consecutive elements as float32.  `full`: all 8 exist and the address is 16-byte aligned;
-// otherwise the first n are read one by one and the rest are 0.
+// 16 and 8 bytes at the alignment of one element: the global memory instructions of this target take
+// any, and rows of odd lengths need it.
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
+typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
+typedef uint32_t u32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
+typedef uint32_t u32x4_at2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x2_at1 __attribute__((ext_vector_type(2), aligned(1)));
 template <typename T>
-__device__ __forceinline__ void load8f(const T *p, bool full, int n, float (&o)[8]) {
-  if (full) {
+__device__ __forceinline__ u32x4 load_bytes16(const T *p) {
+  if constexpr (sizeof(T) == 4) return *reinterpret_cast<const u32x4_at4 *>(p);
+  else return *reinterpret_cast<const u32x4_at2 *>(p);
+}
+template <typename T>
+__device__ __forceinline__ void store_bytes16(T *p, u32x4 v) {
+  if constexpr (sizeof(T) == 4) *reinterpret_cast<u32x4_at4 *>(p) = v;
+  else *reinterpret_cast<u32x4_at2 *>(p) = v;
+}
+
+// 8 consecutive elements as float32: all of them, or the first n and zeros.
+template <typename T>
+__device__ __forceinline__ void load8f(const T *p, int n, float (&o)[8]) {
+  if (n >= 8) {
+    const u32x4 a = load_bytes16(p);
     if constexpr (sizeof(T) == 4) {
-      const float4 a = *reinterpret_cast<const float4 *>(p);
-      const float4 b = *reinterpret_cast<const float4 *>(p + 4);
-      o[0] = a.x; o[1] = a.y; o[2] = a.z; o[3] = a.w;
-      o[4] = b.x; o[5] = b.y; o[6] = b.z; o[7] = b.w;
+      const u32x4 b = load_bytes16(p + 4);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) o[i] = __uint_as_float(a[i]), o[4 + i] = __uint_as_float(b[i]);
     } else {
-      const uint4 a = *reinterpret_cast<const uint4 *>(p);
-      const uint32_t w[4] = {a.x, a.y, a.z, a.w};
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        o[2 * i] = __uint_as_float(w[i] << 16);
-        o[2 * i + 1] = __uint_as_float(w[i] & 0xFFFF0000u);
+        o[2 * i] = __uint_as_float(a[i] << 16);
+        o[2 * i + 1] = __uint_as_float(a[i] & 0xFFFF0000u);
       }
     }
   } else {
@@ -60,28 +75,25 @@ __device__ __forceinline__ void load8f(const T *p, bool full, int n, float (&o)[
   }
 }
 template <typename T>
-__device__ __forceinline__ void store8f(T *p, bool full, int n, const float (&v)[8]) {
-  if (full) {
+__device__ __forceinline__ void store8f(T *p, int n, const float (&v)[8]) {
+  if (n >= 8) {
+    u32x4 a;
     if constexpr (sizeof(T) == 4) {
-      *reinterpret_cast<float4 *>(p) = make_float4(v[0], v[1], v[2], v[3]);
-      *reinterpret_cast<float4 *>(p + 4) = make_float4(v[4], v[5], v[6], v[7]);
+      u32x4 b;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] = __float_as_uint(v[i]), b[i] = __float_as_uint(v[4 + i]);
+      store_bytes16(p, a);
+      store_bytes16(p + 4, b);
     } else {
-      uint4 a;
-      a.x = pack_bf16(v[0], v[1]);
-      a.y = pack_bf16(v[2], v[3]);
-      a.z = pack_bf16(v[4], v[5]);
-      a.w = pack_bf16(v[6], v[7]);
-      *reinterpret_cast<uint4 *>(p) = a;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) a[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
+      store_bytes16(p, a);
     }
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
       if (i < n) p[i] = from_f32<T>(v[i]);
   }
-}
-
-__device__ __forceinline__ bool aligned_g(const void *p) {
-  return (reinterpret_cast<uintptr_t>(p) & 15) == 0;
 }
 
 // Largest code of an 8-bit type.

@@ -84,17 +84,16 @@ struct Epilogue {
   void *z, *y;
   int64_t M, N, ldr, ldz, ldy;
   int32_t y_dtype, act;
-  int32_t vec;           // rows of res, z and y start on 16 bytes
 };
 
 // Loads or stores of 8 elements whose type is known at run time (uniform).
-__device__ __forceinline__ void load8(const void *p, int64_t at, int dt, bool full, int n, float (&o)[8]) {
-  if (dt == FQT_BF16) load8f(static_cast<const bf16 *>(p) + at, full, n, o);
-  else load8f(static_cast<const float *>(p) + at, full, n, o);
+__device__ __forceinline__ void load8(const void *p, int64_t at, int dt, int n, float (&o)[8]) {
+  if (dt == FQT_BF16) load8f(static_cast<const bf16 *>(p) + at, n, o);
+  else load8f(static_cast<const float *>(p) + at, n, o);
 }
-__device__ __forceinline__ void store8(void *p, int64_t at, int dt, bool full, int n, const float (&v)[8]) {
-  if (dt == FQT_BF16) store8f(static_cast<bf16 *>(p) + at, full, n, v);
-  else store8f(static_cast<float *>(p) + at, full, n, v);
+__device__ __forceinline__ void store8(void *p, int64_t at, int dt, int n, const float (&v)[8]) {
+  if (dt == FQT_BF16) store8f(static_cast<bf16 *>(p) + at, n, v);
+  else store8f(static_cast<float *>(p) + at, n, v);
 }
 
 // The epilogue of 8 consecutive n (tile::run_epilogue).
@@ -109,13 +108,11 @@ struct Finish {
   const Epilogue &e;
   float sw[8], bias[8];
   int cnt;                 // columns of the group that exist
-  bool full;
   __device__ __forceinline__ Finish(const Epilogue &e_) : e(e_) {}
   __device__ __forceinline__ void columns(int64_t n) {
     cnt = int(max(int64_t(0), min(e.N - n, int64_t(8))));
-    full = cnt == 8 && e.vec;
-    if (e.sw) load8f(e.sw + n, cnt == 8 && aligned_g(e.sw), cnt, sw);
-    if (e.bias) load8f(e.bias + n, cnt == 8 && aligned_g(e.bias), cnt, bias);
+    if (e.sw) load8f(e.sw + n, cnt, sw);
+    if (e.bias) load8f(e.bias + n, cnt, bias);
   }
   __device__ __forceinline__ Fetch fetch(int64_t m, int64_t n) {
     Fetch f;
@@ -125,8 +122,10 @@ struct Finish {
       const int64_t at = m * e.ldr + n;
       if (e.y_dtype == FQT_BF16) {
         const bf16 *p = static_cast<const bf16 *>(e.res) + at;
-        if (full) {
-          __builtin_memcpy(f.res, __builtin_assume_aligned(p, 16), 16);
+        if (cnt == 8) {
+          const u32x4 u = load_bytes16(p);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) f.res[i] = u[i];
         } else {
 #pragma unroll
           for (int i = 0; i < 8; ++i) {
@@ -137,7 +136,7 @@ struct Finish {
       } else {
         const float *p = static_cast<const float *>(e.res) + at;
         float t[8];
-        load8f(p, full, cnt, t);
+        load8f(p, cnt, t);
 #pragma unroll
         for (int i = 0; i < 8; ++i) f.res[i] = __float_as_uint(t[i]);
       }
@@ -154,7 +153,7 @@ struct Finish {
 #pragma unroll
       for (int i = 0; i < 8; ++i) v[i] += bias[i];
     }
-    if (e.z) store8(e.z, m * e.ldz + n, e.y_dtype, full, cnt, v);
+    if (e.z) store8(e.z, m * e.ldz + n, e.y_dtype, cnt, v);
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] = activate<ACT>(v[i]);
     if (e.res) {
@@ -165,7 +164,7 @@ struct Finish {
         v[i] += __uint_as_float(half ? (i & 1 ? two & 0xFFFF0000u : two << 16) : f.res[i]);
       }
     }
-    store8(e.y, m * e.ldy + n, e.y_dtype, full, cnt, v);
+    store8(e.y, m * e.ldy + n, e.y_dtype, cnt, v);
   }
 };
 
@@ -207,7 +206,7 @@ __global__ void __launch_bounds__(256) k_product_finish(Product p, Epilogue e) {
 #pragma unroll 4
       for (uint32_t s = 0; s < p.tiles.splits; ++s) {
         float t[8];
-        load8f(p.part + (s * p.M + m) * p.ldp + n, true, 8, t);
+        load8f(p.part + (s * p.M + m) * p.ldp + n, 8, t);
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] += t[j];
       }
@@ -264,7 +263,7 @@ struct DzArgs {
   bf16 *dzx, *dzw;       // dz sw (for dx) and dz sx (for dw), rows of `pitch`; may be one array
   float *part;           // [rows][N] partial column sums of dz, or null
   int64_t M, N, ldz, ldy, pitch;
-  int32_t y_dtype, act, vec;
+  int32_t y_dtype, act;
   uint32_t rows, blocks; // row groups; workgroups (row groups times 512-column groups)
 };
 // A thread takes 8 columns, a wave every fourth row of the workgroup's; the waves' column sums meet in
@@ -277,7 +276,6 @@ __device__ __forceinline__ void dz_pass(const DzArgs &a, uint32_t block) {
   const uint32_t row0 = block % a.rows;
   const int64_t n = (int64_t(block / a.rows) * 64 + lane) * 8;
   const int cnt = int(max(int64_t(0), min(a.N - n, int64_t(8))));
-  const bool full = cnt == 8 && a.vec;
   float sum[8] = {};
   if (cnt) {
     float sw[8];
@@ -286,9 +284,9 @@ __device__ __forceinline__ void dz_pass(const DzArgs &a, uint32_t block) {
     with_act(a.act, [&]<int ACT>() {
       for (int64_t m = int64_t(row0) * DZ_WAVES + wave; m < a.M; m += int64_t(a.rows) * DZ_WAVES) {
         float d[8], z[8], o[8];
-        load8(a.dy, m * a.ldy + n, a.y_dtype, full, cnt, d);
+        load8(a.dy, m * a.ldy + n, a.y_dtype, cnt, d);
         if constexpr (ACT != FQT_ACT_NONE) {
-          load8(a.z, m * a.ldz + n, a.y_dtype, full, cnt, z);
+          load8(a.z, m * a.ldz + n, a.y_dtype, cnt, z);
 #pragma unroll
           for (int i = 0; i < 8; ++i) d[i] *= slope<ACT>(z[i]);
         }
@@ -297,13 +295,13 @@ __device__ __forceinline__ void dz_pass(const DzArgs &a, uint32_t block) {
         if (a.dzx) {
 #pragma unroll
           for (int i = 0; i < 8; ++i) o[i] = d[i] * sw[i];
-          store8f(a.dzx + m * a.pitch + n, true, 8, o);
+          store8f(a.dzx + m * a.pitch + n, 8, o);
         }
         if (a.dzw && a.dzw != a.dzx) {
           const float s = a.sx ? a.sx[m] : 1.0f;
 #pragma unroll
           for (int i = 0; i < 8; ++i) o[i] = d[i] * s;
-          store8f(a.dzw + m * a.pitch + n, true, 8, o);
+          store8f(a.dzw + m * a.pitch + n, 8, o);
         }
       }
     });
@@ -318,7 +316,7 @@ __device__ __forceinline__ void dz_pass(const DzArgs &a, uint32_t block) {
   for (int i = 0; i < 8; ++i)
 #pragma unroll
     for (int w = 0; w < DZ_WAVES - 1; ++w) sum[i] += sums[w][i][lane];
-  store8f(a.part + int64_t(row0) * a.N + n, false, cnt, sum);
+  store8f(a.part + int64_t(row0) * a.N + n, cnt, sum);
 }
 
 // What the products wait for, in one launch: the pass over dy and the copies of both operands.
@@ -418,11 +416,8 @@ size_t part_bytes(const tile::Plan &p, int64_t M, int64_t N) {
 }
 
 Epilogue sized(Epilogue e, int64_t M, int64_t N) {
-  const size_t ye = elem_size(e.y_dtype);
-  auto on16 = [&](const void *q, int64_t ld) { return !q || (aligned(q, 16) && ld * ye % 16 == 0); };
   e.M = M;
   e.N = N;
-  e.vec = on16(e.res, e.ldr) && on16(e.z, e.ldz) && on16(e.y, e.ldy);
   return e;
 }
 template <int KIND, int LX, int LW>
@@ -551,7 +546,7 @@ extern "C" int fqt_linear_forward(const fqt_linear_desc *d, const void *x, const
     FQT_TRY_(last_launch_status());
   }
   const int64_t K = f.copy_x || f.copy_w ? f.pitch : s.K;
-  Epilogue e{x_scale, w_scale, bias, residual, z, y, 0, 0, s.ldr, s.ldz, s.ldy, d->y_dtype, d->act, 0};
+  Epilogue e{x_scale, w_scale, bias, residual, z, y, 0, 0, s.ldr, s.ldz, s.ldy, d->y_dtype, d->act};
   float *part = reinterpret_cast<float *>(base + f.part);
   if (d->x_dtype == FQT_BF16 || f.widen)
     return launch_product<tile::BF16K, ROWS, ROWS>(f.plan, xo, wo, s.M, s.N, K, e, part, st);
@@ -610,8 +605,6 @@ extern "C" int fqt_linear_backward(const fqt_linear_desc *d, const void *x, cons
     a.part = dbias ? reinterpret_cast<float *>(base + f.bias) : nullptr;
     a.M = s.M; a.N = s.N; a.ldz = s.ldz; a.ldy = s.ldy; a.pitch = f.dz_pitch;
     a.y_dtype = d->y_dtype; a.act = d->act;
-    const size_t ye = elem_size(d->y_dtype);
-    a.vec = aligned(dy, 16) && s.ldy * ye % 16 == 0 && (!z || (aligned(z, 16) && s.ldz * ye % 16 == 0));
     a.rows = uint32_t(f.rows);
     a.blocks = uint32_t((f.dz_pitch + 511) / 512 * f.rows);
   }
@@ -627,8 +620,8 @@ extern "C" int fqt_linear_backward(const fqt_linear_desc *d, const void *x, cons
   // dz rows are dz_pitch long in the workspace, zeros past N, so a contraction over n may end on a whole
   // piece; as a COLS operand dz has whole pieces of 8 columns.
   dzw.rows = same ? s.N : f.dz_pitch;
-  const Epilogue ex{nullptr, nullptr, nullptr, nullptr, nullptr, dx, 0, 0, 0, 0, s.lddx, d->dx_dtype, FQT_ACT_NONE, 0};
-  const Epilogue ew{nullptr, nullptr, nullptr, nullptr, nullptr, dw, 0, 0, 0, 0, s.lddw, d->dw_dtype, FQT_ACT_NONE, 0};
+  const Epilogue ex{nullptr, nullptr, nullptr, nullptr, nullptr, dx, 0, 0, 0, 0, s.lddx, d->dx_dtype, FQT_ACT_NONE};
+  const Epilogue ew{nullptr, nullptr, nullptr, nullptr, nullptr, dw, 0, 0, 0, 0, s.lddw, d->dw_dtype, FQT_ACT_NONE};
   auto small = [](const tile::Plan &p) { return p.shape[0] == tile::SMALL && p.launches == 1 && p.splits == 1; };
   if (dx && dw && s.K && small(f.dx) && small(f.dw)) {
     const Product px{dzx, wo, s.M, s.K, s.N, f.dx.t[0], nullptr, 0}, pw{dzw, xo, s.N, s.K, s.M, f.dw.t[0], nullptr, 0};

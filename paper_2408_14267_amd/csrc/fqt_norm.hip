@@ -25,7 +25,6 @@ struct NormArgs {
   int32_t q_dtype;
   float eps;
   int32_t norm;        // 0: the row quantiser (y = x)
-  int32_t vec;         // every row of every tensor starts on 16 bytes (codes on 8)
 };
 
 __device__ __forceinline__ float wave_sum(float v) {
@@ -83,39 +82,24 @@ __device__ __forceinline__ CodeScale code_scale(uint32_t mx, float top) {
   return c;
 }
 
-// The columns of a thread.  VEC (rows start on 16 bytes and are multiples of 8 columns): group v of VPT
-// is 8 consecutive columns, all or none of which exist.  Otherwise it is 8 columns TPR apart, so that
-// the lanes of an access are neighbours there too.  Columns past the row's end are 0.
-template <int TPR, bool VEC>
-struct Columns {
-  int t, cols;
-  __device__ __forceinline__ int col(int v, int i) const { return VEC ? (v * TPR + t) * 8 + i : (v * 8 + i) * TPR + t; }
-  __device__ __forceinline__ bool some(int v) const { return col(v, 0) < cols; }
-};
-// 8 elements as they are stored: loaded early, widened where they are used.
+// 8 columns of a row as they are stored: loaded early, widened where they are used.  Columns past the
+// row's end are 0.
 template <typename T>
 struct Raw8 {
   uint32_t w[sizeof(T) * 2];
-  template <int TPR, bool VEC>
-  __device__ __forceinline__ void load(const T *row, const Columns<TPR, VEC> &c, int v) {
-    if constexpr (VEC) {
-      if (!c.some(v)) {
-#pragma unroll
-        for (uint32_t &x : w) x = 0;
-        return;
-      }
-      const uint4 *p = reinterpret_cast<const uint4 *>(row + c.col(v, 0));
+  __device__ __forceinline__ void load(const T *p, int n) {
+    if (n >= 8) {
 #pragma unroll
       for (int j = 0; j < int(sizeof(T)) / 2; ++j) {
-        const uint4 u = p[j];
-        w[4 * j] = u.x; w[4 * j + 1] = u.y; w[4 * j + 2] = u.z; w[4 * j + 3] = u.w;
+        const u32x4 u = load_bytes16(p + 16 / sizeof(T) * j);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) w[4 * j + i] = u[i];
       }
     } else {
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
-        const int k = c.col(v, i);
         T e{};
-        if (k < c.cols) e = row[k];
+        if (i < n) e = p[i];
         if constexpr (sizeof(T) == 4) w[i] = __float_as_uint(e);
         else w[i / 2] = i & 1 ? w[i / 2] | uint32_t(e.v) << 16 : e.v;
       }
@@ -126,57 +110,56 @@ struct Raw8 {
     else return __uint_as_float(i & 1 ? w[i / 2] & 0xFFFF0000u : w[i / 2] << 16);
   }
 };
-template <typename T, int TPR, bool VEC>
-__device__ __forceinline__ void store_cols(T *row, const Columns<TPR, VEC> &c, int v, const float (&x)[8]) {
-  if constexpr (VEC) {
-    if (c.some(v)) store8f(row + c.col(v, 0), true, 8, x);
+__device__ __forceinline__ void store_codes(uint8_t *q, int q_dtype, int n, const float (&v)[8]) {
+  u32x2 o;
+  if (q_dtype == FQT_I8) {
+    o[0] = codes4<FQT_I8>(v[0], v[1], v[2], v[3]);
+    o[1] = codes4<FQT_I8>(v[4], v[5], v[6], v[7]);
   } else {
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (c.col(v, i) < c.cols) row[c.col(v, i)] = from_f32<T>(x[i]);
+    o[0] = codes4<FQT_E4M3>(v[0], v[1], v[2], v[3]);
+    o[1] = codes4<FQT_E4M3>(v[4], v[5], v[6], v[7]);
   }
-}
-__device__ __forceinline__ uint2 codes8(int q_dtype, const float (&v)[8]) {
-  if (q_dtype == FQT_I8)
-    return make_uint2(codes4<FQT_I8>(v[0], v[1], v[2], v[3]), codes4<FQT_I8>(v[4], v[5], v[6], v[7]));
-  return make_uint2(codes4<FQT_E4M3>(v[0], v[1], v[2], v[3]), codes4<FQT_E4M3>(v[4], v[5], v[6], v[7]));
-}
-template <int TPR, bool VEC>
-__device__ __forceinline__ void store_codes(uint8_t *row, int q_dtype, const Columns<TPR, VEC> &c, int v, const float (&x)[8]) {
-  const uint2 q = codes8(q_dtype, x);
-  if constexpr (VEC) {
-    if (c.some(v)) *reinterpret_cast<uint2 *>(row + c.col(v, 0)) = q;
+  if (n >= 8) {
+    *reinterpret_cast<u32x2_at1 *>(q) = o;
   } else {
 #pragma unroll
     for (int i = 0; i < 8; ++i)
-      if (c.col(v, i) < c.cols) row[c.col(v, i)] = uint8_t((i < 4 ? q.x : q.y) >> (8 * (i & 3)));
+      if (i < n) q[i] = uint8_t(o[i / 4] >> (8 * (i & 3)));
   }
 }
 
 // One row per TPR threads, VPT groups of 8 columns per thread.  Workgroups walk the rows with g in
 // registers and the next row's loads under way.  4608 x 4096 bf16 with residual, sum, norm and codes
 // (170 MB): 28 us, at what a copy of these bytes reaches.
-template <typename XT, typename YT, int TPR, int VPT, bool VEC>
+template <typename XT, typename YT, int TPR, int VPT>
 __global__ void __launch_bounds__(block_of<TPR>) k_norm_fwd(NormArgs a) {
   constexpr int ROWS = block_of<TPR> / TPR;
   __shared__ float2 slots[2][16];
-  const Columns<TPR, VEC> c{int(threadIdx.x % TPR), a.cols};
+  const int t = threadIdx.x % TPR;
   int half = 0;
+  // the thread's groups of 8 columns, and how many columns are left there
+  auto col = [&](int v) { return (v * TPR + t) * 8; };
+  auto left = [&](int v) { return a.cols - col(v); };
   float g[VPT][8];
 #pragma unroll
-  for (int v = 0; v < VPT; ++v)
+  for (int v = 0; v < VPT; ++v) {
+    if (a.g) {
+      load8f(a.g + col(v), left(v), g[v]);
+    } else {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) g[v][i] = a.g && c.col(v, i) < a.cols ? a.g[c.col(v, i)] : 1.0f;
+      for (int i = 0; i < 8; ++i) g[v][i] = 1.0f;
+    }
+  }
   const int64_t stride = int64_t(gridDim.x) * ROWS;
   int64_t row = int64_t(blockIdx.x) * ROWS + threadIdx.x / TPR;
   Raw8<XT> nx[VPT], nr[VPT];
   auto fetch = [&](int64_t at) {
     if (at >= a.rows) return;
 #pragma unroll
-    for (int v = 0; v < VPT; ++v) nx[v].load(static_cast<const XT *>(a.x) + at * a.ldx, c, v);
+    for (int v = 0; v < VPT; ++v) nx[v].load(static_cast<const XT *>(a.x) + at * a.ldx + col(v), left(v));
     if (a.r)
 #pragma unroll
-      for (int v = 0; v < VPT; ++v) nr[v].load(static_cast<const XT *>(a.r) + at * a.ldr, c, v);
+      for (int v = 0; v < VPT; ++v) nr[v].load(static_cast<const XT *>(a.r) + at * a.ldr + col(v), left(v));
   };
   fetch(row);
   for (; row < a.rows; row += stride) {
@@ -195,25 +178,25 @@ __global__ void __launch_bounds__(block_of<TPR>) k_norm_fwd(NormArgs a) {
     fetch(row + stride);
     reduce_row<TPR>(ss, mx, slots, half);
     const float rstd = a.norm ? 1.0f / sqrtf(ss / float(a.cols) + a.eps) : 1.0f;
-    if (c.t == 0) {
+    if (t == 0) {
       if (a.rstd) a.rstd[row] = rstd;
       if (a.scale) a.scale[row] = rstd * __uint_as_float(mx) / code_top(a.q_dtype);
     }
     const CodeScale cs = code_scale(mx, code_top(a.q_dtype));
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
-      if (!c.some(v)) continue;
-      if (a.h) store_cols(static_cast<XT *>(a.h) + row * a.ldh, c, v, h[v]);
+      if (left(v) <= 0) continue;
+      if (a.h) store8f(static_cast<XT *>(a.h) + row * a.ldh + col(v), left(v), h[v]);
       if (a.q) {
         float u[8];
 #pragma unroll
         for (int i = 0; i < 8; ++i) u[i] = h[v][i] * g[v][i] * cs.pre * cs.inv;
-        store_codes(a.q + row * a.ldq, a.q_dtype, c, v, u);
+        store_codes(a.q + row * a.ldq + col(v), a.q_dtype, left(v), u);
       }
       if (a.y) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) h[v][i] = h[v][i] * rstd * g[v][i];
-        store_cols(static_cast<YT *>(a.y) + row * a.ldy, c, v, h[v]);
+        store8f(static_cast<YT *>(a.y) + row * a.ldy + col(v), left(v), h[v]);
       }
     }
   }
@@ -230,16 +213,16 @@ __global__ void __launch_bounds__(LONG_TPR) k_norm_fwd_long(NormArgs a) {
   for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
     const XT *x = static_cast<const XT *>(a.x) + row * a.ldx;
     const XT *r = static_cast<const XT *>(a.r) + row * a.ldr;
-    auto load_h = [&](int c, int n, bool full, float (&h)[8], float (&g)[8]) {
-      load8f(x + c, full, n, h);
+    auto load_h = [&](int c, int n, float (&h)[8], float (&g)[8]) {
+      load8f(x + c, n, h);
       if (a.r) {
         float u[8];
-        load8f(r + c, full, n, u);
+        load8f(r + c, n, u);
 #pragma unroll
         for (int i = 0; i < 8; ++i) h[i] += u[i];
       }
       if (a.g) {
-        load8f(a.g + c, n >= 8 && aligned_g(a.g), n, g);
+        load8f(a.g + c, n, g);
       } else {
 #pragma unroll
         for (int i = 0; i < 8; ++i) g[i] = 1.0f;
@@ -249,7 +232,7 @@ __global__ void __launch_bounds__(LONG_TPR) k_norm_fwd_long(NormArgs a) {
     uint32_t mx = 0;
     for (int c = threadIdx.x * 8; c < a.cols; c += LONG_TPR * 8) {
       float h[8], g[8];
-      load_h(c, a.cols - c, a.vec && a.cols - c >= 8, h, g);
+      load_h(c, a.cols - c, h, g);
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         ss = fmaf(h[i], h[i], ss);
@@ -265,27 +248,18 @@ __global__ void __launch_bounds__(LONG_TPR) k_norm_fwd_long(NormArgs a) {
     const CodeScale cs = code_scale(mx, code_top(a.q_dtype));
     for (int c = threadIdx.x * 8; c < a.cols; c += LONG_TPR * 8) {
       const int n = a.cols - c;
-      const bool full = a.vec && n >= 8;
       float h[8], g[8], u[8];
-      load_h(c, n, full, h, g);
-      if (a.h) store8f(static_cast<XT *>(a.h) + row * a.ldh + c, full, n, h);
+      load_h(c, n, h, g);
+      if (a.h) store8f(static_cast<XT *>(a.h) + row * a.ldh + c, n, h);
       if (a.q) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) u[i] = h[i] * g[i] * cs.pre * cs.inv;
-        const uint2 o = codes8(a.q_dtype, u);
-        uint8_t *q = a.q + row * a.ldq + c;
-        if (full) {
-          *reinterpret_cast<uint2 *>(q) = o;
-        } else {
-#pragma unroll
-          for (int i = 0; i < 8; ++i)
-            if (i < n) q[i] = uint8_t((i < 4 ? o.x : o.y) >> (8 * (i & 3)));
-        }
+        store_codes(a.q + row * a.ldq + c, a.q_dtype, n, u);
       }
       if (a.y) {
 #pragma unroll
         for (int i = 0; i < 8; ++i) u[i] = h[i] * rstd * g[i];
-        store8f(static_cast<YT *>(a.y) + row * a.ldy + c, full, n, u);
+        store8f(static_cast<YT *>(a.y) + row * a.ldy + c, n, u);
       }
     }
   }
@@ -301,23 +275,21 @@ struct NormBwdArgs {
   int64_t rows;
   int32_t cols;
   int64_t ldh, ldy, ldr, ldx;
-  int32_t vec;
 };
 
 // 8192 x 4096 bf16 with dres (269 MB): see the row shapes below for its time.
-template <typename XT, typename YT, int TPR, int VPT, bool VEC>
+template <typename XT, typename YT, int TPR, int VPT>
 __global__ void __launch_bounds__(block_of<TPR>) k_norm_bwd(NormBwdArgs a) {
   constexpr int ROWS = block_of<TPR> / TPR;
   __shared__ float2 slots[2][16];
   __shared__ float merge[ROWS > 1 ? ROWS - 1 : 1][ROWS > 1 ? TPR * VPT * 8 : 1];
-  const Columns<TPR, VEC> c{int(threadIdx.x % TPR), a.cols};
-  const int t = c.t;
+  const int t = threadIdx.x % TPR;
   int half = 0;
+  auto col = [&](int v) { return (v * TPR + t) * 8; };
+  auto left = [&](int v) { return a.cols - col(v); };
   float dg[VPT][8] = {}, g[VPT][8];
 #pragma unroll
-  for (int v = 0; v < VPT; ++v)
-#pragma unroll
-    for (int i = 0; i < 8; ++i) g[v][i] = c.col(v, i) < a.cols ? a.g[c.col(v, i)] : 0.0f;
+  for (int v = 0; v < VPT; ++v) load8f(a.g + col(v), left(v), g[v]);
   const int64_t stride = int64_t(gridDim.x) * ROWS;
   int64_t row = int64_t(blockIdx.x) * ROWS + threadIdx.x / TPR;
   Raw8<XT> nh[VPT], nr[VPT];
@@ -328,12 +300,12 @@ __global__ void __launch_bounds__(block_of<TPR>) k_norm_bwd(NormBwdArgs a) {
     nrstd = a.rstd[at];
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
-      nh[v].load(static_cast<const XT *>(a.h) + at * a.ldh, c, v);
-      ny[v].load(static_cast<const YT *>(a.dy) + at * a.ldy, c, v);
+      nh[v].load(static_cast<const XT *>(a.h) + at * a.ldh + col(v), left(v));
+      ny[v].load(static_cast<const YT *>(a.dy) + at * a.ldy + col(v), left(v));
     }
     if (a.dres)
 #pragma unroll
-      for (int v = 0; v < VPT; ++v) nr[v].load(static_cast<const XT *>(a.dres) + at * a.ldr, c, v);
+      for (int v = 0; v < VPT; ++v) nr[v].load(static_cast<const XT *>(a.dres) + at * a.ldr + col(v), left(v));
   };
   fetch(row);
   for (; row < a.rows; row += stride) {
@@ -359,14 +331,14 @@ __global__ void __launch_bounds__(block_of<TPR>) k_norm_bwd(NormBwdArgs a) {
     const float m = dot / float(a.cols);
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
-      if (!c.some(v)) continue;
+      if (left(v) <= 0) continue;
       float d[8];
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         d[i] = rstd * (u[v][i] - h[v][i] * m);
         if (a.dres) d[i] += r[v].get(i);
       }
-      store_cols(static_cast<XT *>(a.dx) + row * a.ldx, c, v, d);
+      store8f(static_cast<XT *>(a.dx) + row * a.ldx + col(v), left(v), d);
     }
   }
   if constexpr (ROWS > 1) {            // the rows' waves meet in LDS
@@ -388,8 +360,64 @@ __global__ void __launch_bounds__(block_of<TPR>) k_norm_bwd(NormBwdArgs a) {
   float *out = a.part + int64_t(blockIdx.x) * a.cols;
 #pragma unroll
   for (int v = 0; v < VPT; ++v) {
-    store_cols(out, c, v, dg[v]);
+    if (left(v) > 0) store8f(out + col(v), left(v), dg[v]);
   }
+}
+
+// Rows of up to 32768 columns: the row stays in registers as it is stored, 32 columns a thread, and is
+// widened twice; 512 waves are on the chip, so nothing is loaded ahead.
+constexpr int WIDE_TPR = 1024, WIDE_VPT = 4;
+template <typename XT, typename YT>
+__global__ void __launch_bounds__(WIDE_TPR) k_norm_bwd_wide(NormBwdArgs a) {
+  __shared__ float2 slots[2][16];
+  int half = 0;
+  auto col = [&](int v) { return (v * WIDE_TPR + int(threadIdx.x)) * 8; };
+  auto left = [&](int v) { return a.cols - col(v); };
+  float dg[WIDE_VPT][8] = {};
+  for (int64_t row = blockIdx.x; row < a.rows; row += gridDim.x) {
+    const float rstd = a.rstd[row];
+    Raw8<XT> h[WIDE_VPT];
+    Raw8<YT> y[WIDE_VPT];
+    float dot = 0.0f;
+#pragma unroll
+    for (int v = 0; v < WIDE_VPT; ++v) {
+      h[v].load(static_cast<const XT *>(a.h) + row * a.ldh + col(v), left(v));
+      y[v].load(static_cast<const YT *>(a.dy) + row * a.ldy + col(v), left(v));
+    }
+#pragma unroll
+    for (int v = 0; v < WIDE_VPT; ++v) {
+      float g[8];
+      load8f(a.g + col(v), left(v), g);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) {
+        const float t = h[v].get(i) * rstd, d = y[v].get(i);
+        dg[v][i] = fmaf(d, t, dg[v][i]);
+        dot = fmaf(d * g[i], t, dot);
+      }
+    }
+    uint32_t none = 0;
+    reduce_row<WIDE_TPR>(dot, none, slots, half);
+    const float m = dot / float(a.cols);
+#pragma unroll
+    for (int v = 0; v < WIDE_VPT; ++v) {
+      if (left(v) <= 0) continue;
+      float g[8], d[8];
+      load8f(a.g + col(v), left(v), g);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) d[i] = rstd * (y[v].get(i) * g[i] - h[v].get(i) * rstd * m);
+      if (a.dres) {
+        float e[8];
+        load8f(static_cast<const XT *>(a.dres) + row * a.ldr + col(v), left(v), e);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) d[i] += e[i];
+      }
+      store8f(static_cast<XT *>(a.dx) + row * a.ldx + col(v), left(v), d);
+    }
+  }
+  float *out = a.part + int64_t(blockIdx.x) * a.cols;
+#pragma unroll
+  for (int v = 0; v < WIDE_VPT; ++v)
+    if (left(v) > 0) store8f(out + col(v), left(v), dg[v]);
 }
 
 // dx of rows too long for registers: h and dy are read twice.
@@ -403,17 +431,17 @@ __global__ void __launch_bounds__(LONG_TPR) k_norm_bwd_long(NormBwdArgs a) {
     const XT *rp = static_cast<const XT *>(a.dres) + row * a.ldr;
     const float rstd = a.rstd[row];
     float dot = 0.0f;
-    auto load = [&](int c, int n, bool full, float (&t)[8], float (&u)[8]) {
+    auto load = [&](int c, int n, float (&t)[8], float (&u)[8]) {
       float g[8];
-      load8f(hp + c, full, n, t);
-      load8f(dyp + c, full, n, u);
-      load8f(a.g + c, n >= 8 && aligned_g(a.g), n, g);
+      load8f(hp + c, n, t);
+      load8f(dyp + c, n, u);
+      load8f(a.g + c, n, g);
 #pragma unroll
       for (int i = 0; i < 8; ++i) t[i] *= rstd, u[i] *= g[i];
     };
     for (int c = threadIdx.x * 8; c < a.cols; c += LONG_TPR * 8) {
       float t[8], u[8];
-      load(c, a.cols - c, a.vec && a.cols - c >= 8, t, u);
+      load(c, a.cols - c, t, u);
 #pragma unroll
       for (int i = 0; i < 8; ++i) dot = fmaf(u[i], t[i], dot);
     }
@@ -422,17 +450,16 @@ __global__ void __launch_bounds__(LONG_TPR) k_norm_bwd_long(NormBwdArgs a) {
     const float m = dot / float(a.cols);
     for (int c = threadIdx.x * 8; c < a.cols; c += LONG_TPR * 8) {
       const int n = a.cols - c;
-      const bool full = a.vec && n >= 8;
       float t[8], u[8], d[8];
-      load(c, n, full, t, u);
+      load(c, n, t, u);
 #pragma unroll
       for (int i = 0; i < 8; ++i) d[i] = rstd * (u[i] - t[i] * m);
       if (a.dres) {
-        load8f(rp + c, full, n, t);
+        load8f(rp + c, n, t);
 #pragma unroll
         for (int i = 0; i < 8; ++i) d[i] += t[i];
       }
-      store8f(static_cast<XT *>(a.dx) + row * a.ldx + c, full, n, d);
+      store8f(static_cast<XT *>(a.dx) + row * a.ldx + c, n, d);
     }
   }
 }
@@ -441,17 +468,16 @@ template <typename XT, typename YT>
 __global__ void __launch_bounds__(64) k_norm_dg_long(NormBwdArgs a) {
   const int c = (blockIdx.x * 64 + threadIdx.x) * 8, n = a.cols - c;
   if (n <= 0) return;
-  const bool full = a.vec && n >= 8;
   float dg[8] = {};
   for (int64_t row = blockIdx.y; row < a.rows; row += gridDim.y) {
     float h[8], u[8];
-    load8f(static_cast<const XT *>(a.h) + row * a.ldh + c, full, n, h);
-    load8f(static_cast<const YT *>(a.dy) + row * a.ldy + c, full, n, u);
+    load8f(static_cast<const XT *>(a.h) + row * a.ldh + c, n, h);
+    load8f(static_cast<const YT *>(a.dy) + row * a.ldy + c, n, u);
     const float rstd = a.rstd[row];
 #pragma unroll
     for (int i = 0; i < 8; ++i) dg[i] = fmaf(u[i], h[i] * rstd, dg[i]);
   }
-  store8f(a.part + int64_t(blockIdx.y) * a.cols + c, n >= 8 && (a.cols & 3) == 0, n, dg);
+  store8f(a.part + int64_t(blockIdx.y) * a.cols + c, n, dg);
 }
 
 // dg[c] = sum of the partial rows: 32 columns per workgroup, 8 threads per column, in a fixed order.
@@ -513,26 +539,20 @@ int check_norm(const fqt_norm_desc *d, Strides *s) {
   if (!s->x || !s->r || !s->h || !s->y || !s->q) return FQT_E_SHAPE;
   return FQT_OK;
 }
-bool on16(const void *p, int64_t ld, size_t e) { return !p || (aligned(p, 16) && ld * e % 16 == 0); }
 
 int run_norm(const fqt_norm_desc *d, NormArgs a, hipStream_t st) {
   if (d->rows == 0 || d->cols == 0) return FQT_OK;
-  const size_t xe = elem_size(d->x_dtype), ye = elem_size(d->y_dtype);
   a.rows = d->rows;
   a.cols = int32_t(d->cols);
   a.q_dtype = d->q_dtype;
   a.eps = d->eps;
-  a.vec = on16(a.x, a.ldx, xe) && on16(a.r, a.ldr, xe) && on16(a.h, a.ldh, xe) &&
-          on16(a.y, a.ldy, ye) && (!a.q || (aligned(a.q, 8) && a.ldq % 8 == 0));
   dispatch_xy(d->x_dtype, d->y_dtype, [&]<typename XT, typename YT>() {
     if (!dispatch_row<FWD_MAX_COLS>(d->cols, [&]<int TPR, int VPT>() {
           constexpr int ROWS = block_of<TPR> / TPR;
           // as many workgroups as are resident at once, with equal numbers of rows
           const int64_t sets = (d->rows + ROWS - 1) / ROWS, most = 1024 * 256 / block_of<TPR>;
           const int64_t each = (sets + most - 1) / most, blocks = (sets + each - 1) / each;
-          const dim3 block(block_of<TPR>);
-          if (a.vec && d->cols % 8 == 0) k_norm_fwd<XT, YT, TPR, VPT, true><<<dim3(blocks), block, 0, st>>>(a);
-          else k_norm_fwd<XT, YT, TPR, VPT, false><<<dim3(blocks), block, 0, st>>>(a);
+          k_norm_fwd<XT, YT, TPR, VPT><<<dim3(blocks), dim3(block_of<TPR>), 0, st>>>(a);
         }))
       k_norm_fwd_long<XT, YT><<<dim3(std::min<int64_t>(d->rows, 512)), dim3(LONG_TPR), 0, st>>>(a);
   });
@@ -541,7 +561,8 @@ int run_norm(const fqt_norm_desc *d, NormArgs a, hipStream_t st) {
 
 // Workgroups of the backward = rows of partial sums.
 int64_t bwd_parts(int64_t rows, int64_t cols) {
-  if (cols > BWD_MAX_COLS) return std::min<int64_t>(std::max<int64_t>(rows, 1), 64);
+  if (cols > WIDE_TPR * WIDE_VPT * 8) return std::min<int64_t>(std::max<int64_t>(rows, 1), 64);
+  if (cols > BWD_MAX_COLS) return std::min<int64_t>(std::max<int64_t>(rows, 1), 256);
   const int64_t per = cols <= 1024 ? 4 : 1;     // rows of a workgroup at a time
   return std::min<int64_t>(std::max<int64_t>((rows + per - 1) / per, 1), 512);
 }
@@ -613,22 +634,22 @@ extern "C" int fqt_rmsnorm_backward(const fqt_norm_desc *d, const void *h, const
     return FQT_E_ALIGN;
   if (ws_bytes < need) return FQT_E_WORKSPACE;
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  const size_t xe = elem_size(d->x_dtype), ye = elem_size(d->y_dtype);
   NormBwdArgs a{};
   a.h = h; a.dy = dy; a.dres = dres; a.g = g; a.rstd = rstd; a.dx = dx;
   a.part = static_cast<float *>(ws);
   a.rows = d->rows;
   a.cols = int32_t(d->cols);
   a.ldh = s.h; a.ldy = s.y; a.ldr = s.r; a.ldx = s.x;
-  a.vec = on16(h, s.h, xe) && on16(dy, s.y, ye) && on16(dres, s.r, xe) && on16(dx, s.x, xe) && aligned(ws, 16);
   const int64_t parts = bwd_parts(d->rows, d->cols);
   dispatch_xy(d->x_dtype, d->y_dtype, [&]<typename XT, typename YT>() {
     if (dispatch_row<BWD_MAX_COLS>(d->cols, [&]<int TPR, int VPT>() {
-          const dim3 block(block_of<TPR>);
-          if (a.vec && d->cols % 8 == 0) k_norm_bwd<XT, YT, TPR, VPT, true><<<dim3(parts), block, 0, st>>>(a);
-          else k_norm_bwd<XT, YT, TPR, VPT, false><<<dim3(parts), block, 0, st>>>(a);
+          k_norm_bwd<XT, YT, TPR, VPT><<<dim3(parts), dim3(block_of<TPR>), 0, st>>>(a);
         }))
       return;
+    if (d->cols <= WIDE_TPR * WIDE_VPT * 8) {
+      k_norm_bwd_wide<XT, YT><<<dim3(parts), dim3(WIDE_TPR), 0, st>>>(a);
+      return;
+    }
     if (d->rows)
       k_norm_bwd_long<XT, YT><<<dim3(std::min<int64_t>(d->rows, 512)), dim3(LONG_TPR), 0, st>>>(a);
     k_norm_dg_long<XT, YT><<<dim3((d->cols + 511) / 512, parts), dim3(64), 0, st>>>(a);

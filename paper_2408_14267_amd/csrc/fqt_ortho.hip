@@ -84,7 +84,6 @@ struct Source {
   int64_t rows, cols, ldg, ldm;
   int32_t g_dtype, nesterov;
   float momentum;
-  int32_t vec;           // rows of g and m start on 16 bytes
 };
 // u of 8 columns from c of row r, 0 past the matrix.  UPDATE: the momentum takes its step first.
 template <bool UPDATE>
@@ -95,20 +94,19 @@ __device__ __forceinline__ void load_u(const Source &s, int64_t r, int64_t c, fl
     for (int i = 0; i < 8; ++i) u[i] = 0.0f;
     return;
   }
-  const bool full = s.vec && n == 8;
   if (!s.m || UPDATE || s.nesterov) {
     const int64_t at = r * s.ldg + c;
-    if (s.g_dtype == FQT_BF16) load8f(static_cast<const bf16 *>(s.g) + at, full, n, u);
-    else load8f(static_cast<const float *>(s.g) + at, full, n, u);
+    if (s.g_dtype == FQT_BF16) load8f(static_cast<const bf16 *>(s.g) + at, n, u);
+    else load8f(static_cast<const float *>(s.g) + at, n, u);
   }
   if (s.m) {
     float *p = s.m + r * s.ldm + c;
     float m[8];
-    load8f(p, full, n, m);
+    load8f(p, n, m);
     if constexpr (UPDATE) {
 #pragma unroll
       for (int i = 0; i < 8; ++i) m[i] = fmaf(s.momentum, m[i], u[i]);
-      store8f(p, full, n, m);
+      store8f(p, n, m);
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) u[i] = s.nesterov ? fmaf(s.momentum, m[i], u[i]) : m[i];
@@ -307,7 +305,7 @@ __global__ void __launch_bounds__(256) k_ns_join(NsArgs a) {
 #pragma unroll 4
     for (uint32_t s = 0; s < a.tiles.splits; ++s) {
       float t[8];
-      load8f(a.part + (s * a.mp + m) * a.np + n, true, 8, t);
+      load8f(a.part + (s * a.mp + m) * a.np + n, 8, t);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] += t[j];
     }
@@ -331,7 +329,7 @@ __global__ void __launch_bounds__(256) k_ns_join_symmetric(NsArgs a) {
 #pragma unroll 4
     for (uint32_t s = 0; s < a.tiles.splits; ++s) {
       float u[8];
-      load8f(a.part + (s * a.mp + m0 + r) * a.mp + n0 + c, true, 8, u);
+      load8f(a.part + (s * a.mp + m0 + r) * a.mp + n0 + c, 8, u);
 #pragma unroll
       for (int j = 0; j < 8; ++j) v[j] += u[j];
     }
@@ -444,7 +442,7 @@ __global__ void __launch_bounds__(256) k_ns_small_start(Source s, Start b, Small
   store_small_part(acc, wm, wn, a.to + int64_t(blockIdx.x) * 4096);
 }
 
-__global__ void __launch_bounds__(256) k_ns_small(SmallArgs a, int32_t blocks) {
+__global__ void __launch_bounds__(256, 1) k_ns_small(SmallArgs a, int32_t blocks) {
   __shared__ __attribute__((aligned(16))) char p[2 * PANEL], q[2 * PANEL], x[2 * PANEL], y[2 * PANEL];
   const uint32_t wave = wave_id(), l = __lane_id(), wm = wave / 2 * 32, wn = wave % 2 * 32;
   const int64_t n_first = blockIdx.x * a.slice, end = min(a.n.np, n_first + a.slice);
@@ -460,7 +458,7 @@ __global__ void __launch_bounds__(256) k_ns_small(SmallArgs a, int32_t blocks) {
   load_x(n_first);
   {
     float v[4][4] = {};
-#pragma unroll 4
+#pragma unroll 8
     for (int b = 0; b < blocks; ++b)
 #pragma unroll
       for (int k = 0; k < 4; ++k) {
@@ -671,8 +669,7 @@ extern "C" int fqt_orthogonalize(const fqt_ortho_desc *d, const void *g, void *o
   if (s.m == 0) return FQT_OK;
   if (!g || !o || !ws) return FQT_E_NULL;
   if (!elem_aligned(g, d->g_dtype) || !elem_aligned(o, d->o_dtype) || !aligned(ws, 256)) return FQT_E_ALIGN;
-  Source src{g, nullptr, d->rows, d->cols, s.ldg, 0, d->g_dtype, 0, 0.0f, 0};
-  src.vec = aligned(g, 16) && s.ldg * elem_size(d->g_dtype) % 16 == 0;
+  Source src{g, nullptr, d->rows, d->cols, s.ldg, 0, d->g_dtype, 0, 0.0f};
   NsArgs a{};
   a.out = o;
   return run_ortho(d, s, src, a, ws, ws_bytes, static_cast<hipStream_t>(hip_stream));
@@ -690,8 +687,7 @@ extern "C" int fqt_muon_step(const fqt_ortho_desc *d, const fqt_muon_cfg *cfg, c
   if (s.m == 0) return FQT_OK;
   if (!g || !m || !w || !ws) return FQT_E_NULL;
   if (!elem_aligned(g, d->g_dtype) || !aligned(m, 4) || !aligned(w, 4) || !aligned(ws, 256)) return FQT_E_ALIGN;
-  Source src{g, m, d->rows, d->cols, s.ldg, s.ldm, d->g_dtype, cfg->nesterov ? 1 : 0, cfg->momentum, 0};
-  src.vec = aligned(g, 16) && s.ldg * elem_size(d->g_dtype) % 16 == 0 && aligned(m, 16) && s.ldm % 4 == 0;
+  Source src{g, m, d->rows, d->cols, s.ldg, s.ldm, d->g_dtype, cfg->nesterov ? 1 : 0, cfg->momentum};
   NsArgs a{};
   a.w = w;
   a.keep = 1.0f - cfg->lr * cfg->weight_decay;

@@ -502,7 +502,7 @@ struct StorePart {
   __device__ __forceinline__ void columns(int64_t) {}
   __device__ __forceinline__ Fetch fetch(int64_t, int64_t) { return {}; }
   __device__ __forceinline__ void finish(int64_t m, int64_t n, float (&v)[8], const Fetch &) {
-    if (m < M && n < ld) dense::store8f(part + m * ld + n, true, 8, v);
+    if (m < M && n < ld) dense::store8f(part + m * ld + n, 8, v);
   }
 };
 

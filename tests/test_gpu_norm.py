@@ -56,7 +56,7 @@ def close(got, want, rel, absolute=0.0, what=""):
 
 SHAPES = [(1, 1), (1, 4096), (3, 8), (5, 513), (2, 512), (7, 1000), (257, 1024), (33, 1153),
           (4, 2048), (9, 2049), (130, 4096), (3, 4097), (2, 8192), (3, 8193), (2, 16384), (2, 16392),
-          (2, 25088), (2100, 64)]
+          (2, 25088), (300, 25088), (2100, 64), (3, 32768), (3, 32775), (70, 40000)]
 
 
 @pytest.mark.parametrize("rows,cols", SHAPES)
