@@ -82,7 +82,9 @@ int fqt_quantize_rows(const fqt_norm_desc *desc, const void *x, void *q, float *
  * x [M][K] and w [N][K] of x_dtype; the scales (float32 [M], [N]) belong to the 8-bit types and are
  * NULL for FQT_BF16.  bias float32 [N], residual, z, y [M][N] of y_dtype; bias, residual and z are
  * optional.  z is stored rounded; y comes from the unrounded z.  y may be residual (same ld).
- * FQT_I8 sums are exact in int32, so K <= 133144 there (FQT_E_SHAPE). */
+ * FQT_I8 sums are exact in int32, so K <= 133144 there; M N, M K and N K are at most 2^40
+ * (FQT_E_SHAPE).  FQT_E4M3 sums have the precision of their matrix instruction, 1e-5 to 6e-5 of their
+ * norm, where y is FQT_BF16, and float32's (through bf16 copies of the codes) where it is FQT_F32. */
 #define FQT_ACT_NONE 0
 #define FQT_ACT_RELU 1
 #define FQT_ACT_GELU 2                    /* z * Phi(z), Phi by the error function */

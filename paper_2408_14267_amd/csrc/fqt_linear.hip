@@ -396,6 +396,9 @@ int check_linear(const fqt_linear_desc *d, Sizes *s) {
   if (d->act < FQT_ACT_NONE || d->act > FQT_ACT_HARDTANH) return FQT_E_INVAL;
   if (d->M < 0 || d->N < 0 || d->K < 0 || d->M >= FQT_MAX_ROWS || d->N > FQT_MAX_LD || d->K > FQT_MAX_LD)
     return FQT_E_SHAPE;
+  // (tiles and workgroups are counted in 32 bits)
+  constexpr double MOST = 1ull << 40;
+  if (double(d->M) * d->N > MOST || double(d->M) * d->K > MOST || double(d->N) * d->K > MOST) return FQT_E_SHAPE;
   if (d->x_dtype == FQT_I8 && d->K > 133144) return FQT_E_SHAPE;   // 127^2 K < 2^31
   *s = {d->M, d->N, d->K, row_stride(d->ldx, d->K), row_stride(d->ldw, d->K), row_stride(d->ldr, d->N),
         row_stride(d->ldy, d->N), row_stride(d->ldz, d->N), row_stride(d->lddx, d->K),

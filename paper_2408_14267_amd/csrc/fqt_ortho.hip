@@ -313,47 +313,41 @@ __global__ void __launch_bounds__(256) k_ns_join(NsArgs a) {
   }
 }
 // The symmetric products: a workgroup per 64 x 64 tile on or above the diagonal of tiles of edge B, whose
-// mirror image goes out through LDS (4096 x 4096, 8 splits: see the step's times in the launches).
+// mirror image goes out through LDS.
 template <int MODE, int B>
-__global__ void __launch_bounds__(256) k_ns_join_symmetric(NsArgs a) {
+__global__ void __launch_bounds__(512) k_ns_join_symmetric(NsArgs a) {
   __shared__ float t[64][65];
   const int64_t m0 = int64_t(blockIdx.y) * 64, n0 = int64_t(blockIdx.x) * 64;
   if (m0 / B > n0 / B) return;
   Finish<MODE> f{a, m0 / B == n0 / B};
   f.columns(n0);
+  const int r = threadIdx.x / 8, c = threadIdx.x % 8 * 8;
+  const auto q = f.fetch(m0 + r, n0 + c);
+  float v[8] = {};
+#pragma unroll 8
+  for (uint32_t s = 0; s < a.tiles.splits; ++s) {
+    float u[8];
+    load8f(a.part + (s * a.mp + m0 + r) * a.mp + n0 + c, 8, u);
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int r = (h * 256 + threadIdx.x) / 8, c = threadIdx.x % 8 * 8;
-    const auto q = f.fetch(m0 + r, n0 + c);
-    float v[8] = {};
-#pragma unroll 4
-    for (uint32_t s = 0; s < a.tiles.splits; ++s) {
-      float u[8];
-      load8f(a.part + (s * a.mp + m0 + r) * a.mp + n0 + c, 8, u);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] += u[j];
-    }
-    f.finish(m0 + r, n0 + c, v, q);
-#pragma unroll
-    for (int j = 0; j < 8; ++j) t[r][c + j] = v[j];
+    for (int j = 0; j < 8; ++j) v[j] += u[j];
   }
+  f.finish(m0 + r, n0 + c, v, q);
   if (f.diagonal) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) t[r][c + j] = v[j];
   __syncthreads();
 #pragma unroll
-  for (int h = 0; h < 2; ++h) {
-    const int n = (h * 256 + threadIdx.x) / 8, m = threadIdx.x % 8 * 8;
-    float v[8];
-#pragma unroll
-    for (int j = 0; j < 8; ++j) v[j] = t[m + j][n];
-    f.mirror(n0 + n, m0 + m, v);
-  }
+  for (int j = 0; j < 8; ++j) v[j] = t[c + j][r];
+  f.mirror(n0 + r, m0 + c, v);
 }
 
 // ----------------------------------------------------------------------------- few rows
-// Up to 64 rows: a launch per step instead of three or four.  Workgroup b keeps columns
+// Up to 64 rows: a launch or two per step instead of three or four.  Workgroup b keeps columns
 // [b slice, (b + 1) slice) of X.  It adds up everyone's partial sums of P (in order), takes Q from it in
 // LDS, and goes over its columns 64 at a time: X' = a X + Q X, and its part of the next P = X' X'^T.
-// All operands are 64 rows of 128 bytes per 32 columns, swizzled as fqt_tile.hpp says.
+// Past DIRECT workgroups the sums are joined by a launch of their own (64 x 25088: 13 instead of 32 us a
+// step on 32 workgroups).  All operands are 64 rows of 128 bytes per 32 columns, swizzled as
+// fqt_tile.hpp says.
 struct SmallArgs {
   NsArgs n;
   const float *from;     // [workgroups][64][64] partial sums of P 2^30
@@ -361,7 +355,7 @@ struct SmallArgs {
   int64_t slice;         // columns of a workgroup, a multiple of 64
 };
 constexpr int PANEL = 64 * tile::KB;                       // bytes of 32 columns
-constexpr int SMALL_BLOCKS = 32;                           // at most; each reads all partial sums
+constexpr int SMALL_BLOCKS = 256, DIRECT = 32;             // workgroups at most; reading all partial sums
 
 // Byte offset of columns n ... (8-byte steps) of row m of a matrix of row panels, plane hi or lo.
 __device__ __forceinline__ uint32_t panel_at(uint32_t m, uint32_t n, int lo) {
@@ -416,6 +410,21 @@ __device__ __forceinline__ void panels_out(const char *lds, const Pairs &x, int6
     const uint4 v = *reinterpret_cast<const uint4 *>(lds + panel * PANEL + m * tile::KB + ((piece ^ (m & 7)) * 16));
     *reinterpret_cast<uint4 *>(x.p + ((n / 32 + panel) * 64 + m) * 64 + piece * 8) = v;
   }
+}
+
+// out = the partial sums added up: 16 four-entry groups per workgroup, 16 threads each.
+__global__ void __launch_bounds__(256) k_ns_small_join(const float *from, int32_t blocks, float *out) {
+  __shared__ tile::f32x4 t[16][16];
+  const uint32_t at = (blockIdx.x * 16 + threadIdx.x % 16) * 4, k = threadIdx.x / 16;
+  tile::f32x4 v{};
+#pragma unroll 16
+  for (int b = k; b < blocks; b += 16) v += *reinterpret_cast<const tile::f32x4 *>(from + int64_t(b) * 4096 + at);
+  t[k][threadIdx.x % 16] = v;
+  __syncthreads();
+  if (k) return;
+#pragma unroll
+  for (int j = 1; j < 16; ++j) v += t[j][threadIdx.x];
+  *reinterpret_cast<tile::f32x4 *>(out + at) = v;
 }
 
 // X_0 and its partial sums of P.
@@ -563,8 +572,8 @@ NsWs ns_ws(const NsSizes &s) {
   w.x[1] = take(x);
   w.p = take(p);
   w.q = take(p);
-  if (s.mp == 64) {        // two sets of partial sums of P
-    w.part = take(2 * SMALL_BLOCKS * 4096 * sizeof(float));
+  if (s.mp == 64) {        // two sets of partial sums of P, and their sum
+    w.part = take((2 * SMALL_BLOCKS + 1) * 4096 * sizeof(float));
     w.total = at;
     return w;
   }
@@ -583,7 +592,7 @@ int launch_ns(const tile::Plan &plan, NsArgs a, hipStream_t st) {
       if constexpr (MODE == APPLY)
         k_ns_join<<<dim3(std::min<int64_t>((a.mp * a.np / 8 + 255) / 256, 4096)), dim3(256), 0, st>>>(a);
       else
-        k_ns_join_symmetric<MODE, tile::ShapeOf<SHAPE>::type::BM><<<dim3(a.mp / 64, a.mp / 64), dim3(256), 0, st>>>(a);
+        k_ns_join_symmetric<MODE, tile::ShapeOf<SHAPE>::type::BM><<<dim3(a.mp / 64, a.mp / 64), dim3(512), 0, st>>>(a);
     }
   });
   return last_launch_status();
@@ -613,7 +622,7 @@ int run_ortho(const fqt_ortho_desc *d, const NsSizes &s, Source src, NsArgs a, v
   if (s.mp == 64) {
     const int64_t tiles = s.np / 64, per = (tiles + SMALL_BLOCKS - 1) / SMALL_BLOCKS;
     const int blocks = int((tiles + per - 1) / per);
-    float *sums[2] = {a.part, a.part + SMALL_BLOCKS * 4096};
+    float *sums[2] = {a.part, a.part + SMALL_BLOCKS * 4096}, *joined = a.part + 2 * SMALL_BLOCKS * 4096;
     SmallArgs q{a, nullptr, sums[0], per * 64};
     q.n.x = x;
     if (s.tall) k_ns_small_start<true><<<dim3(blocks), dim3(256), 0, st>>>(src, start, q);
@@ -625,7 +634,12 @@ int run_ortho(const fqt_ortho_desc *d, const NsSizes &s, Source src, NsArgs a, v
       q.n.last = i + 1 == d->steps;
       q.from = sums[i & 1];
       q.to = sums[~i & 1];
-      k_ns_small<<<dim3(blocks), dim3(256), 0, st>>>(q, blocks);
+      if (blocks > DIRECT) {
+        k_ns_small_join<<<dim3(64), dim3(256), 0, st>>>(q.from, blocks, joined);
+        FQT_TRY_(last_launch_status());
+        q.from = joined;
+      }
+      k_ns_small<<<dim3(blocks), dim3(256), 0, st>>>(q, blocks > DIRECT ? 1 : blocks);
       FQT_TRY_(last_launch_status());
       std::swap(x, next);
     }

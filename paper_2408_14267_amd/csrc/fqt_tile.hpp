@@ -319,6 +319,7 @@ __device__ __forceinline__ void run_tile(const Operand &x, const Operand &w, int
   char *at = lds, *to = lds + AHEAD * S::BUF;
   auto next = [&](char *p) { return p == lds + (S::BUFS - 1) * S::BUF ? lds : p + S::BUF; };
   for (int64_t i = t0; i < t1; ++i) {
+    wait_lds();                                            // the step before is read
     wait_loads<(AHEAD - 1) * LOADS>();
     // (not barrier_only: matrix instructions of the last step may be issued behind the barrier)
     asm volatile("" ::: "memory");
@@ -581,8 +582,8 @@ inline Plan make_plan(int64_t M, int64_t N, int64_t steps, bool symmetric) {
       t.steps = uint32_t(std::max<int64_t>(1, (steps + n - 1) / n));
       t.splits = uint32_t(std::max<int64_t>(1, (steps + t.steps - 1) / t.steps));
       double c = run(t.count * t.splits, t.steps, cu, step, start) + launch;
-      // the partial sums, written and read at 4 TB/s, and their launch
-      if (t.splits > 1) c += 4 + t.splits * entries * 8 / 4e6;
+      // the partial sums, written and read at 4 TB/s one split after the other, and their launch
+      if (t.splits > 1) c += 4 + 0.2 * t.splits + t.splits * entries * 8 / 4e6;
       take(c, Plan{{shape, shape}, {t, t}, 1, t.splits});
     }
   };

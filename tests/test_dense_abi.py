@@ -124,6 +124,13 @@ def test_int8_sums_stay_in_32_bits(K, ok):
     assert dense.fqt_linear_workspace_size(dense.linear_desc(1, 1, K)) > 0      # bf16: no such bound
 
 
+def test_linear_size_limits():
+    for M, N, K in ((1 << 30, 1 << 22, 1), (1 << 30, 1, 1 << 22), (1, 1 << 22, 1 << 22)):
+        with pytest.raises(fqt.FqtError) as e:
+            dense.fqt_linear_workspace_size(dense.linear_desc(M, N, K))
+        assert e.value.status == fqt.FQT_E_SHAPE
+
+
 def test_linear_pointer_refusals():
     f, b = dense._lib.fqt_linear_forward, dense._lib.fqt_linear_backward
     d, q = _linear(), _linear(x_dtype=dense.FQT_I8)
