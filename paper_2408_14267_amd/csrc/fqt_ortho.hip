@@ -511,8 +511,7 @@ __global__ void __launch_bounds__(256, 1) k_ns_small(SmallArgs a, int32_t blocks
       for (int j = 0; j < 2; ++j) {
         const uint32_t m = wm + i * 16 + l % 16, n = wn + j * 16 + 4 * (l / 16);
         // X in the layout of its transposing reads: row m % 32 (hi), 32 + m % 32 (lo) of step m / 32
-        const uint32_t f = (m & 3) | ((m >> 1) & 12);       // (the same for both: bit 5 is not in it)
-        const char *at = x + m / 32 * PANEL + m % 32 * tile::KB + ((n / 8 ^ (2 * f & 7)) * 16) + (n & 7) * 2;
+        const char *at = x + m / 32 * PANEL + m % 32 * tile::KB + ((n / 8 ^ tile::cols_swizzle<64>(m)) * 16) + (n & 7) * 2;
         float o[4], v[4];
         join4(at, at + 32 * tile::KB, o);
 #pragma unroll

@@ -19,8 +19,8 @@
 //
 // LDS swizzle (in 16-byte pieces, on the source side of the load, since a load to LDS writes the
 // 64 lanes' pieces in a row).  ROWS: piece c of row r at c ^ (r & 7), so that the 16 rows of a
-// fragment, 128 bytes apart, meet all banks.  COLS: piece c of row k at c ^ 2 f(k), f = k's low two
-// bits and bits 3-4, so that the 16 rows that one transposing read touches lie in different banks.
+// fragment, 128 bytes apart, meet all banks.  COLS: piece c of row k at c ^ swizzle(k), so that the
+// eight 32-byte rows that half a transposing read touches lie in different banks.
 #pragma once
 
 #include "fqt_dense.hpp"
@@ -84,6 +84,15 @@ __device__ __forceinline__ lds_char *lds_ptr(const char *p) {
   return (lds_char *)(uint32_t)(uintptr_t)p;
 }
 
+// Swizzle of row k of a COLS step, in pieces.  Half a wave's transposing read touches 32 bytes of each of
+// rows 0-3 and 8-11 (plus 16, plus 4) of 2 LINES bytes; the banks repeat after 256 bytes.  The row's
+// bits 2 and 5 must not count: a lane reads rows 4 and 32 further from one address.
+template <int LINES>
+__device__ __forceinline__ uint32_t cols_swizzle(uint32_t k) {
+  if constexpr (LINES == 64) return 2 * (((k >> 1) & 1) | ((k >> 2) & 2));     // (odd rows start mid-way)
+  else return 2 * ((k & 3) | ((k >> 1) & 4));
+}
+
 // 16 bytes per lane from r at `off` to lds + 16 lane (lds wave-uniform).
 __device__ __forceinline__ void load_to_lds(__amdgpu_buffer_rsrc_t r, char *lds, uint32_t off) {
   __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds_ptr(lds), 16, off, 0, 0, 0);
@@ -127,8 +136,7 @@ struct Loader {
         off[j] = uint32_t(r * (LAYOUT == ROWS ? o.ld : KB)) + piece * 16;
         kpos[j] = LAYOUT == ROWS ? piece * 16 : 0;
       } else {
-        const uint32_t f = (row & 3) | ((row >> 1) & 12);
-        const uint32_t piece = slot ^ ((2 * f) & (ROW_PIECES - 1));
+        const uint32_t piece = slot ^ cols_swizzle<LINES>(row);
         const bool in = line0 + int64_t(piece) * 8 < o.rows;
         if constexpr (LAYOUT == COLS) {
           off[j] = in ? uint32_t(row * o.ld) + piece * 16 : BUF_NONE;
@@ -199,10 +207,10 @@ struct Reader {
         at[s] = (line0 + l % 16) * KB + ((s * 4 + l / 16) ^ (l & 7)) * 16;
     } else {
       // lane l points at row k = 8 (l / 16) + (l % 16) / 4, four columns from 4 (l % 4)
-      const uint32_t k = 8 * (l / 16) + (l % 16) / 4, f = (k & 3) | ((k >> 1) & 12);
+      const uint32_t k = 8 * (l / 16) + (l % 16) / 4;
 #pragma unroll
       for (int i = 0; i < FRAGS; ++i) {
-        const uint32_t piece = (line0 / 8 + 2 * i + (l % 4) / 2) ^ ((2 * f) & (LINES / 8 - 1));
+        const uint32_t piece = (line0 / 8 + 2 * i + (l % 4) / 2) ^ cols_swizzle<LINES>(k);
         at[i] = k * (LINES * 2) + piece * 16 + (l & 1) * 8;
       }
     }
