@@ -26,27 +26,30 @@ using tile::COLS;
 __device__ __forceinline__ float exp_neg(float v) {        // exp(-v)
   return __builtin_amdgcn_exp2f(v * -1.44269504088896341f);
 }
-// Phi(-|z|) and exp(-z^2 / 2), Phi the normal distribution function: Phi(-|z|) = exp(-z^2 / 2) times a
-// quintic in t = 1 / (1 + p |z| / sqrt 2) (Abramowitz and Stegun 7.1.26 halved; absolute error below
-// 8e-8).  About 20 issue slots; the library's erf costs four times that, and a 256 x 256 tile pays
+// Phi(-a) and exp(-a^2 / 2) for a >= 0, Phi the normal distribution function: Phi(-a) = exp(-a^2 / 2)
+// times a quintic in t = 1 / (1 + p a / sqrt 2) (Abramowitz and Stegun 7.1.26 halved; absolute error
+// below 8e-8).  About 20 issue slots; the library's erf costs four times that, and a 256 x 256 tile pays
 // 0.4 us for each slot.
-__device__ __forceinline__ float normal_tail(float z, float *e) {
-  const float a = fabsf(z);
+__device__ __forceinline__ float normal_tail(float a, float *e) {
   const float t = __builtin_amdgcn_rcpf(fmaf(a, 0.3275911f * 0.70710678118654752f, 1.0f));
   float q = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
   q = fmaf(t, q, 0.5f * 1.421413741f);
   q = fmaf(t, q, 0.5f * -0.284496736f);
   q = fmaf(t, q, 0.5f * 0.254829592f);
-  *e = exp_neg(0.5f * z * z);
+  *e = __builtin_amdgcn_exp2f(a * (a * -0.72134752044448170f));
   return q * t * *e;
 }
+// (Phi(-30) is 0 in float32: a need not be larger, and an infinite one would meet it.)
+__device__ __forceinline__ float tail_arg(float z) { return fminf(fabsf(z), 30.0f); }
 template <int ACT>
 __device__ __forceinline__ float activate(float z) {
   if constexpr (ACT == FQT_ACT_RELU) return z > 0.0f ? z : (z != z ? z : 0.0f);
   else if constexpr (ACT == FQT_ACT_GELU) {
+    // z Phi(z) = max(z, 0) - |z| Phi(-|z|)
+    const float a = tail_arg(z);
     float e;
-    const float q = normal_tail(z, &e);
-    return z * (z > 0.0f ? 1.0f - q : q);
+    const float q = normal_tail(a, &e);
+    return z != z ? z : fmaf(-a, q, fmaxf(z, 0.0f));
   } else if constexpr (ACT == FQT_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + exp_neg(z));
   else if constexpr (ACT == FQT_ACT_HARDTANH) return z != z ? z : fminf(fmaxf(z, -1.0f), 1.0f);
   else return z;
@@ -55,9 +58,10 @@ template <int ACT>
 __device__ __forceinline__ float slope(float z) {
   if constexpr (ACT == FQT_ACT_RELU) return z > 0.0f ? 1.0f : 0.0f;
   else if constexpr (ACT == FQT_ACT_GELU) {
+    const float a = tail_arg(z);
     float e;
-    const float q = normal_tail(z, &e);
-    return fmaf(z * 0.39894228040143268f, e, z > 0.0f ? 1.0f - q : q);
+    const float q = normal_tail(a, &e), d = z > 0.0f ? 1.0f - q : q;
+    return z != z ? z : fmaf(copysignf(a, z) * 0.39894228040143268f, e, d);
   } else if constexpr (ACT == FQT_ACT_SILU) {
     const float t = __builtin_amdgcn_rcpf(1.0f + exp_neg(z));
     return t * fmaf(z, 1.0f - t, 1.0f);

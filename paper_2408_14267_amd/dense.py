@@ -170,7 +170,15 @@ def _workspace(where, ws, dev):
     return ws.data_ptr(), ws.numel() * ws.element_size()
 
 
-_ptr, _stream = fqt._ptr, fqt._stream
+# torch's current device, without the initialisation check that a device tensor makes needless.
+_device = getattr(torch._C, "_cuda_getDevice", None) or torch.cuda.current_device
+
+
+def _stream(stream, dev):
+    """The stream's handle; dev is the current device."""
+    if stream is None and fqt._raw_stream is not None:
+        return fqt._raw_stream(dev)
+    return fqt._stream(stream)
 
 
 def _check(status, where):
@@ -183,7 +191,8 @@ def _check(status, where):
 def fqt_rmsnorm_forward(desc, x, g, residual=None, h=None, y=None, q=None, scale=None, rstd=None,
                         stream=None):
     where, R, C = "fqt_rmsnorm_forward", desc.rows, desc.cols
-    _required(where, x=x, g=g)
+    if x is None or g is None:
+        _required(where, x=x, g=g)
     dev = x.get_device()
     if (q is None) != (scale is None):
         raise ValueError(f"{where}: q and scale come together")
@@ -200,10 +209,13 @@ def fqt_rmsnorm_forward(desc, x, g, residual=None, h=None, y=None, q=None, scale
         _vector(where, "scale", scale, R, dev)
     if rstd is not None:
         _vector(where, "rstd", rstd, R, dev)
-    _current(where, dev)
-    _check(_lib.fqt_rmsnorm_forward(desc, x.data_ptr(), _ptr(residual), g.data_ptr(), _ptr(h),
-                                    _ptr(y), _ptr(q), _ptr(scale), _ptr(rstd), _stream(stream)),
-           where)
+    if dev < 0 or dev != _device():
+        _current(where, dev)
+    _check(_lib.fqt_rmsnorm_forward(
+        desc, x.data_ptr(), None if residual is None else residual.data_ptr(), g.data_ptr(),
+        None if h is None else h.data_ptr(), None if y is None else y.data_ptr(),
+        None if q is None else q.data_ptr(), None if scale is None else scale.data_ptr(),
+        None if rstd is None else rstd.data_ptr(), _stream(stream, dev)), where)
 
 
 def fqt_norm_workspace_size(desc):
@@ -214,7 +226,8 @@ def fqt_norm_workspace_size(desc):
 
 def fqt_rmsnorm_backward(desc, h, g, rstd, dy, dx, dg, ws, dres=None, stream=None):
     where, R, C = "fqt_rmsnorm_backward", desc.rows, desc.cols
-    _required(where, h=h, g=g, rstd=rstd, dy=dy, dx=dx, dg=dg)
+    if h is None or g is None or rstd is None or dy is None or dx is None or dg is None:
+        _required(where, h=h, g=g, rstd=rstd, dy=dy, dx=dx, dg=dg)
     dev = h.get_device()
     _matrix(where, "h", h, desc.x_dtype, R, C, desc.ldh, dev)
     _vector(where, "g", g, C, dev)
@@ -224,22 +237,26 @@ def fqt_rmsnorm_backward(desc, h, g, rstd, dy, dx, dg, ws, dres=None, stream=Non
     _vector(where, "dg", dg, C, dev)
     if dres is not None:
         _matrix(where, "dres", dres, desc.x_dtype, R, C, desc.ldr, dev)
-    _current(where, dev)
-    _check(_lib.fqt_rmsnorm_backward(desc, h.data_ptr(), g.data_ptr(), rstd.data_ptr(),
-                                     dy.data_ptr(), _ptr(dres), dx.data_ptr(), dg.data_ptr(),
-                                     *_workspace(where, ws, dev), _stream(stream)), where)
+    if dev < 0 or dev != _device():
+        _current(where, dev)
+    _check(_lib.fqt_rmsnorm_backward(
+        desc, h.data_ptr(), g.data_ptr(), rstd.data_ptr(), dy.data_ptr(),
+        None if dres is None else dres.data_ptr(), dx.data_ptr(), dg.data_ptr(),
+        *_workspace(where, ws, dev), _stream(stream, dev)), where)
 
 
 def fqt_quantize_rows(desc, x, q, scale, stream=None):
     where, R, C = "fqt_quantize_rows", desc.rows, desc.cols
-    _required(where, x=x, q=q, scale=scale)
+    if x is None or q is None or scale is None:
+        _required(where, x=x, q=q, scale=scale)
     dev = x.get_device()
     _matrix(where, "x", x, desc.x_dtype, R, C, desc.ldx, dev)
     _matrix(where, "q", q, desc.q_dtype, R, C, desc.ldq, dev)
     _vector(where, "scale", scale, R, dev)
-    _current(where, dev)
-    _check(_lib.fqt_quantize_rows(desc, x.data_ptr(), q.data_ptr(), scale.data_ptr(),
-                                  _stream(stream)), where)
+    if dev < 0 or dev != _device():
+        _current(where, dev)
+    _check(_lib.fqt_quantize_rows(
+        desc, x.data_ptr(), q.data_ptr(), scale.data_ptr(), _stream(stream, dev)), where)
 
 
 # ----------------------------------------------------------------------------- linear
@@ -265,7 +282,8 @@ def _operands(where, desc, x, w, x_scale, w_scale, dev):
 def fqt_linear_forward(desc, x, w, y, ws, bias=None, residual=None, x_scale=None, w_scale=None,
                        z=None, stream=None):
     where, M, N = "fqt_linear_forward", desc.M, desc.N
-    _required(where, x=x, w=w, y=y)
+    if x is None or w is None or y is None:
+        _required(where, x=x, w=w, y=y)
     dev = y.get_device()
     _operands(where, desc, x, w, x_scale, w_scale, dev)
     _matrix(where, "y", y, desc.y_dtype, M, N, desc.ldy, dev)
@@ -275,16 +293,20 @@ def fqt_linear_forward(desc, x, w, y, ws, bias=None, residual=None, x_scale=None
         _matrix(where, "residual", residual, desc.y_dtype, M, N, desc.ldr, dev)
     if z is not None:
         _matrix(where, "z", z, desc.y_dtype, M, N, desc.ldz, dev)
-    _current(where, dev)
-    _check(_lib.fqt_linear_forward(desc, x.data_ptr(), w.data_ptr(), _ptr(x_scale), _ptr(w_scale),
-                                   _ptr(bias), _ptr(residual), _ptr(z), y.data_ptr(),
-                                   *_workspace(where, ws, dev), _stream(stream)), where)
+    if dev < 0 or dev != _device():
+        _current(where, dev)
+    _check(_lib.fqt_linear_forward(
+        desc, x.data_ptr(), w.data_ptr(), None if x_scale is None else x_scale.data_ptr(),
+        None if w_scale is None else w_scale.data_ptr(), None if bias is None else bias.data_ptr(),
+        None if residual is None else residual.data_ptr(), None if z is None else z.data_ptr(),
+        y.data_ptr(), *_workspace(where, ws, dev), _stream(stream, dev)), where)
 
 
 def fqt_linear_backward(desc, x, w, dy, ws, z=None, x_scale=None, w_scale=None, dx=None, dw=None,
                         dbias=None, stream=None):
     where, M, N, K = "fqt_linear_backward", desc.M, desc.N, desc.K
-    _required(where, dy=dy)
+    if dy is None:
+        _required(where, dy=dy)
     dev = dy.get_device()
     _operands(where, desc, x, w, x_scale, w_scale, dev)
     _matrix(where, "dy", dy, desc.y_dtype, M, N, desc.ldy, dev)
@@ -296,10 +318,15 @@ def fqt_linear_backward(desc, x, w, dy, ws, z=None, x_scale=None, w_scale=None, 
         _matrix(where, "dw", dw, desc.dw_dtype, N, K, desc.lddw, dev)
     if dbias is not None:
         _vector(where, "dbias", dbias, N, dev)
-    _current(where, dev)
-    _check(_lib.fqt_linear_backward(desc, _ptr(x), _ptr(w), _ptr(x_scale), _ptr(w_scale), _ptr(z),
-                                    dy.data_ptr(), _ptr(dx), _ptr(dw), _ptr(dbias),
-                                    *_workspace(where, ws, dev), _stream(stream)), where)
+    if dev < 0 or dev != _device():
+        _current(where, dev)
+    _check(_lib.fqt_linear_backward(
+        desc, None if x is None else x.data_ptr(), None if w is None else w.data_ptr(),
+        None if x_scale is None else x_scale.data_ptr(),
+        None if w_scale is None else w_scale.data_ptr(), None if z is None else z.data_ptr(),
+        dy.data_ptr(), None if dx is None else dx.data_ptr(), None if dw is None else dw.data_ptr(),
+        None if dbias is None else dbias.data_ptr(), *_workspace(where, ws, dev),
+        _stream(stream, dev)), where)
 
 
 # ----------------------------------------------------------------------------- orthogonalisation
@@ -312,27 +339,32 @@ def fqt_ortho_workspace_size(desc):
 
 def fqt_orthogonalize(desc, g, o, ws, stream=None):
     where, R, C = "fqt_orthogonalize", desc.rows, desc.cols
-    _required(where, g=g, o=o)
+    if g is None or o is None:
+        _required(where, g=g, o=o)
     dev = g.get_device()
     _matrix(where, "g", g, desc.g_dtype, R, C, desc.ldg, dev)
     _matrix(where, "o", o, desc.o_dtype, R, C, desc.ldo, dev)
-    _current(where, dev)
-    _check(_lib.fqt_orthogonalize(desc, g.data_ptr(), o.data_ptr(), *_workspace(where, ws, dev),
-                                  _stream(stream)), where)
+    if dev < 0 or dev != _device():
+        _current(where, dev)
+    _check(_lib.fqt_orthogonalize(
+        desc, g.data_ptr(), o.data_ptr(), *_workspace(where, ws, dev), _stream(stream, dev)), where)
 
 
 def fqt_muon_step(desc, w, g, m, ws, lr, momentum=0.95, weight_decay=0.0, scale=1.0, nesterov=True,
                   stream=None):
     where, R, C = "fqt_muon_step", desc.rows, desc.cols
-    _required(where, w=w, g=g, m=m)
+    if w is None or g is None or m is None:
+        _required(where, w=w, g=g, m=m)
     dev = w.get_device()
     _matrix(where, "g", g, desc.g_dtype, R, C, desc.ldg, dev)
     _matrix(where, "m", m, FQT_F32, R, C, desc.ldm, dev)
     _matrix(where, "w", w, desc.o_dtype, R, C, desc.ldo, dev)
     cfg = fqt_muon_cfg(lr, momentum, weight_decay, scale, int(nesterov))
-    _current(where, dev)
-    _check(_lib.fqt_muon_step(desc, cfg, g.data_ptr(), m.data_ptr(), w.data_ptr(),
-                              *_workspace(where, ws, dev), _stream(stream)), where)
+    if dev < 0 or dev != _device():
+        _current(where, dev)
+    _check(_lib.fqt_muon_step(
+        desc, cfg, g.data_ptr(), m.data_ptr(), w.data_ptr(), *_workspace(where, ws, dev),
+        _stream(stream, dev)), where)
 
 
 # ----------------------------------------------------------------------------- workspaces
