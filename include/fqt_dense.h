@@ -10,7 +10,8 @@
  *    stands for cols, any other ld must be >= cols and at most FQT_MAX_LD.
  *  - x and w of a product start on 16 bytes, every other matrix and vector on its element size,
  *    workspaces on 256 bytes (FQT_E_ALIGN otherwise).  Operand rows of a
- *    product that are not multiples of 16 bytes long and apart cost a copy.
+ *    product that are not multiples of 16 bytes long and apart cost a copy, except in a forward of up
+ *    to four rows.
  *  - A row or column count of zero is no error: nothing is launched but what an output needs (the
  *    gradient of a parameter over no rows is zero, a product over no columns is its bias).
  *  - Optional pointers may be NULL.  Outputs must not overlap inputs or each other unless a
@@ -84,7 +85,8 @@ int fqt_quantize_rows(const fqt_norm_desc *desc, const void *x, void *q, float *
  * optional.  z is stored rounded; y comes from the unrounded z.  y may be residual (same ld).
  * FQT_I8 sums are exact in int32, so K <= 133144 there; M N, M K and N K are at most 2^40
  * (FQT_E_SHAPE).  FQT_E4M3 sums have the precision of their matrix instruction, 1e-5 to 6e-5 of their
- * norm, where y is FQT_BF16, and float32's (through bf16 copies of the codes) where it is FQT_F32. */
+ * norm, where y is FQT_BF16, and float32's (through bf16 copies of the codes) where it is FQT_F32.  Up to four
+ * rows, the form for single tokens, are summed on the vector units, in float32 for every type. */
 #define FQT_ACT_NONE 0
 #define FQT_ACT_RELU 1
 #define FQT_ACT_GELU 2                    /* z * Phi(z), Phi by the error function */

@@ -41,11 +41,13 @@ typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u32x2 __attribute__((ext_vector_type(2)));
 typedef uint32_t u32x4_at4 __attribute__((ext_vector_type(4), aligned(4)));
 typedef uint32_t u32x4_at2 __attribute__((ext_vector_type(4), aligned(2)));
+typedef uint32_t u32x4_at1 __attribute__((ext_vector_type(4), aligned(1)));
 typedef uint32_t u32x2_at1 __attribute__((ext_vector_type(2), aligned(1)));
 template <typename T>
 __device__ __forceinline__ u32x4 load_bytes16(const T *p) {
   if constexpr (sizeof(T) == 4) return *reinterpret_cast<const u32x4_at4 *>(p);
-  else return *reinterpret_cast<const u32x4_at2 *>(p);
+  else if constexpr (sizeof(T) == 2) return *reinterpret_cast<const u32x4_at2 *>(p);
+  else return *reinterpret_cast<const u32x4_at1 *>(p);
 }
 template <typename T>
 __device__ __forceinline__ void store_bytes16(T *p, u32x4 v) {

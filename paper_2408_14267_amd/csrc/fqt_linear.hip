@@ -118,6 +118,11 @@ struct Finish {
     if (e.sw) load8f(e.sw + n, cnt, sw);
     if (e.bias) load8f(e.bias + n, cnt, bias);
   }
+  __device__ __forceinline__ void column(int64_t n) {      // a single one
+    cnt = 1;
+    if (e.sw) sw[0] = e.sw[n];
+    if (e.bias) bias[0] = e.bias[n];
+  }
   __device__ __forceinline__ Fetch fetch(int64_t m, int64_t n) {
     Fetch f;
     if (m >= e.M || cnt == 0) return f;
@@ -216,6 +221,150 @@ __global__ void __launch_bounds__(256) k_product_finish(Product p, Epilogue e) {
       }
       f.finish(m, n, v, q);
     }
+  });
+}
+
+// ----------------------------------------------------------------------------- few rows
+// Up to FEW_MOST rows of x the bound is one pass over w, and a matrix tile would compute 60 empty rows,
+// want its contraction split to fill the chip, a second launch to join the parts and, for rows that
+// are not whole 16-byte pieces, a copy of w.  Here a workgroup takes R rows of w, its threads a 16-byte piece
+// each, on the vector units; the sums meet by shuffles and in LDS.  Four rows are where the vector units
+// are as busy as the memory.  1 x 25088 -> 4096 e4m3 with the tiles and here 23.6 and 19.8 us (5.2 TB/s), bf16
+// 41.0 and 37.2, four rows 23.8 and 22.9, 40.5 and 41.3; 1 x 4099 -> 2048 bf16 24.0 and 6.0 (the call).
+
+// The elements of a 16-byte piece, and the sum of their products: bf16 as float32, int8 by fours, e4m3 by
+// twos as float16, which holds them and their smallest exactly.
+typedef _Float16 f16x2 __attribute__((ext_vector_type(2)));
+template <typename T> struct Piece;
+template <>
+struct Piece<bf16> {
+  typedef float Sum;
+  static constexpr int N = 8;
+  float v[N];
+  __device__ __forceinline__ explicit Piece(u32x4 u) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __uint_as_float(u[i] << 16);
+      v[2 * i + 1] = __uint_as_float(u[i] & 0xFFFF0000u);
+    }
+  }
+  __device__ __forceinline__ void add(const Piece &o, float &sum) const {
+#pragma unroll
+    for (int i = 0; i < N; ++i) sum = fmaf(v[i], o.v[i], sum);
+  }
+};
+template <>
+struct Piece<e4m3> {
+  typedef float Sum;
+  static constexpr int N = 16;
+  f16x2 v[N / 2];
+  __device__ __forceinline__ explicit Piece(u32x4 u) {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[2 * i] = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(u[i], 1.0f, false));
+      v[2 * i + 1] = __builtin_bit_cast(f16x2, __builtin_amdgcn_cvt_scalef32_pk_f16_fp8(u[i], 1.0f, true));
+    }
+  }
+  __device__ __forceinline__ void add(const Piece &o, float &sum) const {
+#pragma unroll
+    for (int i = 0; i < N / 2; ++i) sum = __builtin_amdgcn_fdot2(v[i], o.v[i], sum, false);
+  }
+};
+template <>
+struct Piece<int8_t> {
+  typedef int Sum;
+  static constexpr int N = 16;
+  u32x4 u;
+  __device__ __forceinline__ explicit Piece(u32x4 v) : u(v) {}
+  __device__ __forceinline__ void add(const Piece &o, int &sum) const {
+#pragma unroll
+    for (int i = 0; i < 4; ++i) sum = __builtin_amdgcn_sdot4(int(u[i]), int(o.u[i]), sum, false);
+  }
+};
+// Sums of V values over a wave, each step halving the values a lane still adds up: lane l returns that of
+// value l / (64 / V).
+template <int V, typename S>
+__device__ __forceinline__ S fold(S (&v)[V]) {
+  int o = 32;
+#pragma unroll
+  for (int n = V / 2; n > 0; n /= 2, o /= 2) {
+    const bool up = __lane_id() & o;
+#pragma unroll
+    for (int i = 0; i < n; ++i) {
+      const S lower = v[i], upper = v[i + n];              // (selected as values: v stays in registers)
+      v[i] = (up ? upper : lower) + __shfl_xor(up ? lower : upper, o);
+    }
+  }
+#pragma unroll
+  for (; o > 0; o /= 2) v[0] += __shfl_xor(v[0], o);
+  return v[0];
+}
+
+struct FewArgs {
+  const void *x, *w;
+  int64_t K, ldx, ldw;
+};
+constexpr int FEW_MOST = 4, FEW_WIDE = 2560, FEW_THREADS = 256;
+// M: rows of x, or more (those past the last read it again and store nothing).
+template <typename T, int M, int R>
+__global__ void __launch_bounds__(FEW_THREADS) k_few_rows(FewArgs a, Epilogue e) {
+  typedef typename Piece<T>::Sum Sum;
+  typedef std::conditional_t<sizeof(T) == 2, uint16_t, uint8_t> Bits;
+  constexpr int WAVES = FEW_THREADS / 64, V = M * R, AHEAD = R == 1 ? 4 : 2;
+  __shared__ Sum slots[WAVES][V];
+  const int64_t n0 = int64_t(blockIdx.x) * R;
+  const T *x[M], *w[R];
+#pragma unroll
+  for (int m = 0; m < M; ++m) x[m] = static_cast<const T *>(a.x) + min(int64_t(m), e.M - 1) * a.ldx;
+#pragma unroll
+  for (int r = 0; r < R; ++r) w[r] = static_cast<const T *>(a.w) + min(n0 + r, e.N - 1) * a.ldw;
+  Sum acc[V] = {};
+  auto add = [&](const u32x4 (&ux)[M], const u32x4 (&uw)[R]) {
+#pragma unroll
+    for (int m = 0; m < M; ++m) {
+      const Piece<T> px(ux[m]);
+#pragma unroll
+      for (int r = 0; r < R; ++r) Piece<T>(uw[r]).add(px, acc[m * R + r]);
+    }
+  };
+  const int pieces = int(a.K / Piece<T>::N);
+  for (int p0 = threadIdx.x; p0 < pieces; p0 += AHEAD * FEW_THREADS) {
+    u32x4 ux[AHEAD][M] = {}, uw[AHEAD][R] = {};
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) {
+      const int p = p0 + i * FEW_THREADS;
+      if (p >= pieces) break;
+#pragma unroll
+      for (int r = 0; r < R; ++r) uw[i][r] = load_bytes16(w[r] + int64_t(p) * Piece<T>::N);
+#pragma unroll
+      for (int m = 0; m < M; ++m) ux[i][m] = load_bytes16(x[m] + int64_t(p) * Piece<T>::N);
+    }
+#pragma unroll
+    for (int i = 0; i < AHEAD; ++i) add(ux[i], uw[i]);
+  }
+  // the elements past the last whole piece, one a thread
+  if (const int64_t k = int64_t(pieces) * Piece<T>::N + threadIdx.x; k < a.K) {
+    u32x4 ux[M] = {}, uw[R] = {};
+#pragma unroll
+    for (int r = 0; r < R; ++r) uw[r][0] = reinterpret_cast<const Bits *>(w[r])[k];
+#pragma unroll
+    for (int m = 0; m < M; ++m) ux[m][0] = reinterpret_cast<const Bits *>(x[m])[k];
+    add(ux, uw);
+  }
+  const Sum mine = fold<V>(acc);
+  const int lane = threadIdx.x % 64;
+  if (lane % (64 / V) == 0) slots[threadIdx.x / 64][lane / (64 / V)] = mine;
+  __syncthreads();
+  const int64_t m = threadIdx.x / R, n = n0 + threadIdx.x % R;
+  if (threadIdx.x >= V || m >= e.M || n >= e.N) return;
+  Sum sum = slots[0][threadIdx.x];
+#pragma unroll
+  for (int i = 1; i < WAVES; ++i) sum += slots[i][threadIdx.x];
+  with_act(e.act, [&]<int ACT>() {
+    float v[8] = {float(sum)};
+    Finish<ACT> f(e);
+    f.column(n);
+    f.finish(m, n, v, f.fetch(m, n));
   });
 }
 
@@ -361,7 +510,7 @@ __global__ void __launch_bounds__(256) k_dbias(DbiasArgs a) {
 }
 
 // Two products of small tiles side by side, and dbias: the backward's dx and dw where each alone leaves
-// CUs idle (777 x 1000 x 513: 13 instead of 22 + 4 us).
+// CUs idle (777 x 1000 x 513: 10 instead of 22 + 4 us).
 __global__ void __launch_bounds__(tile::Small::THREADS, 2) k_product_pair(Product px, Epilogue ex, Product pw, Epilogue ew, DbiasArgs b) {
   typedef tile::Small S;
   static_assert(S::THREADS == 256, "dbias takes 256 threads");
@@ -446,6 +595,21 @@ int launch_product(const tile::Plan &plan, Operand x, Operand w, int64_t M, int6
   return FQT_OK;
 }
 
+// Four rows of w a workgroup where they fill the chip all the same, since x is then read a quarter as often;
+// one where they do not (us with four and one, bf16, K = 25088: 1 x 512 11.1 and 7.9, 1 x 2048 20.4 and 20.4, 4 x 512
+// 15.1 and 12.2, 4 x 1000 16.5 and 20.6, 4 x 2048 23.3 and 36.4).
+template <typename T>
+int launch_few(const FewArgs &a, const Epilogue &e, hipStream_t st) {
+  auto rows = [&]<int M>() {
+    if (M * e.N >= FEW_WIDE) k_few_rows<T, M, 4><<<dim3(uint32_t((e.N + 3) / 4)), dim3(FEW_THREADS), 0, st>>>(a, e);
+    else k_few_rows<T, M, 1><<<dim3(uint32_t(e.N)), dim3(FEW_THREADS), 0, st>>>(a, e);
+  };
+  if (e.M == 1) rows.template operator()<1>();
+  else if (e.M == 2) rows.template operator()<2>();
+  else rows.template operator()<4>();
+  return last_launch_status();
+}
+
 // The copy of an operand into rows of `pitch` elements of e bytes.
 Copy copy_of(const void *src, int64_t rows, int64_t cols, int64_t ld, void *dst, int64_t pitch, int64_t e) {
   const int64_t all = rows * (pitch * e / 16);
@@ -457,6 +621,7 @@ Copy copy_of(const void *src, int64_t rows, int64_t cols, int64_t ld, void *dst,
 struct FwdWs { size_t x, w, part, total; int64_t pitch, e; tile::Plan plan; bool widen, copy_x, copy_w; };
 FwdWs fwd_ws(const fqt_linear_desc &d, const Sizes &s) {
   FwdWs f{};
+  if (s.M <= FEW_MOST) return f;
   // The e4m3 matrix instruction adds the products of a step in fewer bits than float32 has (sums off by
   // 1e-5 to 6e-5 of their norm): below the rounding of a bf16 output, not of a float32 one, for which the
   // codes go through bf16 copies (exact) and that type's instruction.
@@ -538,6 +703,12 @@ extern "C" int fqt_linear_forward(const fqt_linear_desc *d, const void *x, const
   const FwdWs f = fwd_ws(*d, s);
   if (ws_bytes < f.total) return FQT_E_WORKSPACE;
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  Epilogue e{x_scale, w_scale, bias, residual, z, y, s.M, s.N, s.ldr, s.ldz, s.ldy, d->y_dtype, d->act};
+  if (s.M <= FEW_MOST) {
+    const FewArgs a{x, w, s.K, s.ldx, s.ldw};
+    if (d->x_dtype == FQT_BF16) return launch_few<bf16>(a, e, st);
+    return d->x_dtype == FQT_I8 ? launch_few<int8_t>(a, e, st) : launch_few<e4m3>(a, e, st);
+  }
   char *base = static_cast<char *>(ws);
   auto operand = [&](const void *p, bool copy, size_t at, int64_t rows, int64_t ld, Copy *c) -> Operand {
     if (!copy) return {static_cast<const char *>(p), ld * f.e, rows};
@@ -553,7 +724,6 @@ extern "C" int fqt_linear_forward(const fqt_linear_desc *d, const void *x, const
     FQT_TRY_(last_launch_status());
   }
   const int64_t K = f.copy_x || f.copy_w ? f.pitch : s.K;
-  Epilogue e{x_scale, w_scale, bias, residual, z, y, 0, 0, s.ldr, s.ldz, s.ldy, d->y_dtype, d->act};
   float *part = reinterpret_cast<float *>(base + f.part);
   if (d->x_dtype == FQT_BF16 || f.widen)
     return launch_product<tile::BF16K, ROWS, ROWS>(f.plan, xo, wo, s.M, s.N, K, e, part, st);

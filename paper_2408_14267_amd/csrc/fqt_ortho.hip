@@ -345,8 +345,8 @@ __global__ void __launch_bounds__(512) k_ns_join_symmetric(NsArgs a) {
 // Up to 64 rows: a launch or two per step instead of three or four.  Workgroup b keeps columns
 // [b slice, (b + 1) slice) of X.  It adds up everyone's partial sums of P (in order), takes Q from it in
 // LDS, and goes over its columns 64 at a time: X' = a X + Q X, and its part of the next P = X' X'^T.
-// Past DIRECT workgroups the sums are joined by a launch of their own (64 x 25088: 13 instead of 32 us a
-// step on 32 workgroups).  All operands are 64 rows of 128 bytes per 32 columns, swizzled as
+// Past DIRECT workgroups the sums are joined by a launch of their own (64 x 25088: 10 + 5 instead of 32 us
+// a step on 32 workgroups).  All operands are 64 rows of 128 bytes per 32 columns, swizzled as
 // fqt_tile.hpp says.
 struct SmallArgs {
   NsArgs n;

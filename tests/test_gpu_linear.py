@@ -347,3 +347,90 @@ def test_own_stream_and_captured_replays(M, N, K):
         torch.cuda.synchronize()
         assert all(torch.equal(a, c) for a, c in zip(outputs(), want)), i
         step()
+
+
+@pytest.mark.parametrize("M", [1, 2, 3, 4])
+@pytest.mark.parametrize("N,K", [(1, 1), (5, 16), (1, 31), (9, 17), (700, 1003), (641, 4096), (2561, 2065), (7, 25095)])
+@pytest.mark.parametrize("xt", ["bf16", "int8", "e4m3"])
+def test_forward_few_rows(M, N, K, xt):
+    check_forward(M, N, K, xt, "bf16", "silu", True, True, True, inplace=True)
+    check_forward(M, N, K, xt, "f32", "gelu", True, True, True)
+    check_forward(M, N, K, xt, "f32", "none", False, False, False)
+
+
+@pytest.mark.parametrize("M", [1, 3])
+@pytest.mark.parametrize("N", [30, 2600])
+@pytest.mark.parametrize("xt", ["bf16", "int8", "e4m3"])
+def test_few_rows_strides(M, N, xt):
+    """Rows of any alignment give the bits that dense rows give."""
+    d = dense()
+    K, lx, lw, lo = 1037, 1041, 1039, 2 * N + 1
+    x, w, xs, wsc, *_ = operands(M, N, K, xt)
+    xv, xk = guarded(M, K, x.dtype, lx)
+    wv, wk = guarded(N, K, w.dtype, lw)
+    xv.copy_(x), wv.copy_(w)
+    bf = dict(dtype=torch.bfloat16, device="cuda")
+    r, y0, z0 = gen(M, N, seed=6).bfloat16(), torch.empty(M, N, **bf), torch.empty(M, N, **bf)
+    y, y_ok = guarded(M, N, torch.bfloat16, lo, 5)
+    z, z_ok = guarded(M, N, torch.bfloat16, lo, 1)
+    desc = d.linear_desc(M, N, K, x_dtype=xt, act="hardtanh", ldx=lx, ldw=lw, ldy=lo, ldz=lo)
+    d.fqt_linear_forward(desc, xv, wv, y, d.linear_workspace(desc), residual=r, x_scale=xs, w_scale=wsc, z=z)
+    D = d.linear_desc(M, N, K, x_dtype=xt, act="hardtanh")
+    d.fqt_linear_forward(D, x, w, y0, d.linear_workspace(D), residual=r, x_scale=xs, w_scale=wsc, z=z0)
+    y_ok(), z_ok(), xk(), wk()
+    assert torch.equal(y, y0) and torch.equal(z, z0)
+
+
+def test_few_rows_all_codes():
+    """Every product of two e4m3 codes, the smallest and NaN among them: a product of two 4-bit significands
+    is exact.  int8: the largest sums, 133144 times 127^2 in magnitude, are exact too (below 2^31, rounded once)."""
+    d = dense()
+    c = torch.arange(256, device="cuda", dtype=torch.uint8).view(torch.float8_e4m3fn)[:, None].contiguous()
+    one = torch.ones(256, device="cuda")
+    desc = d.linear_desc(4, 256, 1, x_dtype="e4m3", y_dtype="f32")
+    y, ws = torch.empty(4, 256, device="cuda"), d.linear_workspace(desc)
+    for m in range(0, 256, 4):
+        x = c[m:m + 4].clone()
+        d.fqt_linear_forward(desc, x, c, y, ws, x_scale=one[:4], w_scale=one)
+        want = x.float() * c.float().t()
+        assert torch.equal(y.isnan(), want.isnan()) and torch.equal(y.nan_to_num(), want.nan_to_num())
+    K = 133144
+    desc = d.linear_desc(1, 2, K, x_dtype="int8", y_dtype="f32")
+    x = torch.full((1, K), -127, dtype=torch.int8, device="cuda")
+    w = torch.stack([x[0], -x[0]])
+    y = torch.empty(1, 2, device="cuda")
+    d.fqt_linear_forward(desc, x, w, y, d.linear_workspace(desc), x_scale=one[:1], w_scale=one[:2])
+    assert y.tolist() == [[float(torch.tensor(float(127 * 127 * K), dtype=torch.float32)),
+                           -float(torch.tensor(float(127 * 127 * K), dtype=torch.float32))]]
+
+
+@pytest.mark.parametrize("xt", ["bf16", "e4m3"])
+def test_few_rows_non_finite_values_stay_in_their_rows(xt):
+    d = dense()
+    M, N, K = 3, 70, 1003
+    x, w, xs, wsc, *_ = operands(M, N, K, xt)
+    desc = d.linear_desc(M, N, K, x_dtype=xt)
+    ws, y0, y = d.linear_workspace(desc), torch.empty(M, N, dtype=torch.bfloat16, device="cuda"), \
+        torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+    d.fqt_linear_forward(desc, x, w, y0, ws, x_scale=xs, w_scale=wsc)
+    x.view(torch.uint8 if xt == "e4m3" else torch.int16)[2, 1002] = 0x7F if xt == "e4m3" else 0x7FC0
+    w.view(torch.uint8 if xt == "e4m3" else torch.int16)[9, 3] = 0x7F if xt == "e4m3" else 0x7F80
+    d.fqt_linear_forward(desc, x, w, y, ws, x_scale=xs, w_scale=wsc)
+    cols = [j for j in range(N) if j != 9]
+    assert torch.isnan(y[2]).all() and not torch.isfinite(y[:, 9]).any()
+    assert torch.equal(y[:2][:, cols], y0[:2][:, cols])
+
+
+def test_few_rows_offsets_beyond_31_bits():
+    """Rows of w whose element offsets pass 2^31: 600 rows 2^22 elements apart."""
+    d = dense()
+    M, N, K, ld = 2, 600, 64, 1 << 22
+    buf = torch.empty(N * ld, dtype=torch.bfloat16, device="cuda")
+    x, w, *_ = operands(M, N, K, "bf16")
+    wv = buf.view(N, ld)[:, :K]
+    wv.copy_(w)
+    y, y0 = torch.empty(M, N, dtype=torch.bfloat16, device="cuda"), torch.empty(M, N, dtype=torch.bfloat16, device="cuda")
+    desc, D = d.linear_desc(M, N, K, ldw=ld), d.linear_desc(M, N, K)
+    d.fqt_linear_forward(desc, x, wv, y, d.linear_workspace(desc))
+    d.fqt_linear_forward(D, x, w, y0, d.linear_workspace(D))
+    assert torch.equal(y, y0)
