@@ -565,7 +565,7 @@ int64_t round_up(int64_t v, int64_t q) { return (v + q - 1) / q * q; }
 bool whole_pieces(int64_t n, int64_t ld, size_t e) { return n * e % 16 == 0 && ld * e % 16 == 0; }
 
 tile::Plan plan_of(int64_t M, int64_t N, int64_t K, size_t e) {
-  return tile::make_plan(M, N, (K * int64_t(e) + tile::KB - 1) / tile::KB, false);
+  return tile::make_plan(M, N, (K * int64_t(e) + tile::KB - 1) / tile::KB, false, tile::DENSE_COSTS);
 }
 size_t part_bytes(const tile::Plan &p, int64_t M, int64_t N) {
   return p.splits > 1 ? align256(size_t(p.splits) * M * round_up(N, 8) * 4) : 0;

@@ -560,9 +560,9 @@ int check_ortho(const fqt_ortho_desc *d, NsSizes *s) {
 }
 NsWs ns_ws(const NsSizes &s) {
   NsWs w{};
-  w.gram = tile::make_plan(s.mp, s.mp, s.np / 32, true);
-  w.poly = tile::make_plan(s.mp, s.mp, s.mp / 32, true);
-  w.apply = tile::make_plan(s.mp, s.np, s.mp / 32, false);
+  w.gram = tile::make_plan(s.mp, s.mp, s.np / 32, true, tile::SYMMETRIC_COSTS);
+  w.poly = tile::make_plan(s.mp, s.mp, s.mp / 32, true, tile::SYMMETRIC_COSTS);
+  w.apply = tile::make_plan(s.mp, s.np, s.mp / 32, false, tile::PAIR_COSTS);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += align256(bytes); return o; };
   w.norm = take(NORM_BLOCKS * sizeof(double) + sizeof(Units));

@@ -543,7 +543,15 @@ struct Plan {
   uint32_t splits;
 };
 
-inline Plan make_plan(int64_t M, int64_t N, int64_t steps, bool symmetric) {
+// us a step of a workgroup with one, two or three of them on a CU, and us before the first and after the last
+// step with Large, Middle and Small tiles: measured on bf16 operands, on pairs as PANEL_ROWS x PANEL_COLS
+// (512 and 1024 rows) and on symmetric products of pairs (512 to 4096 rows).
+struct Costs { double large[1], middle[2], small[3], start[3]; };
+constexpr Costs DENSE_COSTS{{1.58}, {0.60, 0.90}, {0.25, 0.40, 0.58}, {6, 5, 4}},
+    PAIR_COSTS{{2.0}, {0.81, 1.26}, {0.28, 0.39, 0.62}, {18, 8, 5}},
+    SYMMETRIC_COSTS{{2.0}, {0.81, 1.15}, {0.28, 0.40, 0.75}, {10, 8, 4}};
+
+inline Plan make_plan(int64_t M, int64_t N, int64_t steps, bool symmetric, const Costs &costs) {
   auto grid = [&](int64_t b) {
     Tiles t{};
     t.nm = uint32_t((M + b - 1) / b);
@@ -561,15 +569,13 @@ inline Plan make_plan(int64_t M, int64_t N, int64_t steps, bool symmetric) {
   };
   const double s = double(steps);
   const double entries = double(M) * double(N) * (symmetric ? 0.5 : 1.0);
-  // us of `blocks` workgroups of `n` steps, `cu` of which fit a CU, at step[k] us a step with k + 1 of them
-  // there (measured on bf16) and `start` us before the first and after the last
+  // us of `blocks` workgroups of `n` steps, `cu` of which fit a CU
   auto run = [](uint32_t blocks, double n, int cu, const double *step, double start) {
     const uint32_t full = 256 * cu, rest = blocks % full;
     double c = blocks / full * (step[cu - 1] * n + start);
     if (rest) c += step[(rest - 1) / 256] * n + start;
     return c;
   };
-  static const double large[] = {1.58}, middle[] = {0.60, 0.90}, small[] = {0.25, 0.40, 0.58};
   const double launch = 3;
   {
     const Tiles t = grid(256);
@@ -580,7 +586,7 @@ inline Plan make_plan(int64_t M, int64_t N, int64_t steps, bool symmetric) {
       p.t[1].first = t.count - tail;
       p.t[1].count = tail;
       p.t[1].parts = 1;
-      take(run(p.t[0].count, s, 1, large, 6) + run(16 * tail, s, 3, small, 4) + 2 * launch, p);
+      take(run(p.t[0].count, s, 1, costs.large, costs.start[0]) + run(16 * tail, s, 3, costs.small, costs.start[2]) + 2 * launch, p);
     }
   }
   auto split = [&](int shape, int64_t b, int cu, const double *step, double start) {
@@ -595,9 +601,9 @@ inline Plan make_plan(int64_t M, int64_t N, int64_t steps, bool symmetric) {
       take(c, Plan{{shape, shape}, {t, t}, 1, t.splits});
     }
   };
-  split(LARGE, 256, 1, large, 6);
-  split(MIDDLE, 128, 2, middle, 5);
-  split(SMALL, 64, 3, small, 4);
+  split(LARGE, 256, 1, costs.large, costs.start[0]);
+  split(MIDDLE, 128, 2, costs.middle, costs.start[1]);
+  split(SMALL, 64, 3, costs.small, costs.start[2]);
   return best;
 }
 
@@ -608,16 +614,17 @@ struct Place {
   bool diagonal;           // of a symmetric product: the tile is its own mirror image
 };
 // Each XCD (b % 8) walks a contiguous run of the order below, which goes down GROUP tiles of m before
-// the next n, so that the tiles an XCD has in flight share operand rows in its L2.
+// the next n, one split after the other, so that the tiles an XCD has in flight share operand rows and
+// their piece of the contraction in its L2 (512 x 512 x 25088 bf16: 26 us; each split over all XCDs 40).
 template <int SHAPE>
 __device__ __forceinline__ Place place(const Tiles &t, uint32_t b) {
   typedef typename ShapeOf<SHAPE>::type S;
   const uint32_t parts = SHAPE == SMALL && t.parts ? 16 : 1;
-  const uint32_t total = t.count * parts;
-  const uint32_t split = b / total;
-  b %= total;
-  const uint32_t q = total / XCDS, r = total % XCDS, x = b % XCDS;
+  const uint32_t total = t.count * parts, all = total * t.splits;
+  const uint32_t q = all / XCDS, r = all % XCDS, x = b % XCDS;
   uint32_t s = x * q + min(x, r) + b / XCDS;
+  const uint32_t split = s / total;
+  s %= total;
   const uint32_t part = s % parts;
   s = s / parts + t.first;
   uint32_t m, n;
