@@ -46,6 +46,9 @@ extern "C" {
  *   y = h * rstd * g                       (from the unrounded sum; stored rounded to y_dtype)
  *   scale = max over cols of |y| / T       (T = 127 for FQT_I8, 448 for FQT_E4M3)
  *   q = y / scale rounded to nearest even  (0 where scale is 0)
+ * The quotient is taken as h g (T / max over cols of |h g|), a few float32 roundings off y / scale, so a tie
+ * may go to either neighbour.  h^2 is summed in float32: a row whose sum passes 3.4e38 has rstd, y,
+ * scale and q 0.
  * x, residual, h: x_dtype; g [cols]: float32; y: y_dtype; q: q_dtype; scale, rstd: float32 [rows]. */
 typedef struct {
   int64_t rows, cols;

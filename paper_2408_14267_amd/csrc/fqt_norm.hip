@@ -72,13 +72,14 @@ __device__ __forceinline__ void reduce_row(float &ss, uint32_t &mx, float2 (*slo
 template <int TPR> constexpr int block_of = TPR == 64 ? 256 : TPR;
 
 // What a row's codes are multiplied by: T / max, in two factors so that a maximum near the smallest
-// float32 values does not overflow it.
+// float32 values does not overflow it, and 0 where the row's scale is 0 (also of a row that is not: its
+// maximum may be so small, or its norm so large, that the scale has no float32).
 struct CodeScale { float pre, inv; };
-__device__ __forceinline__ CodeScale code_scale(uint32_t mx, float top) {
+__device__ __forceinline__ CodeScale code_scale(uint32_t mx, float scale, float top) {
   const float m = __uint_as_float(mx);
   CodeScale c;
   c.pre = m < 1e-30f ? 0x1p100f : 1.0f;
-  c.inv = mx ? top / (m * c.pre) : 0.0f;
+  c.inv = scale != 0.0f ? top / (m * c.pre) : 0.0f;
   return c;
 }
 
@@ -178,11 +179,12 @@ __global__ void __launch_bounds__(block_of<TPR>) k_norm_fwd(NormArgs a) {
     fetch(row + stride);
     reduce_row<TPR>(ss, mx, slots, half);
     const float rstd = a.norm ? 1.0f / sqrtf(ss / float(a.cols) + a.eps) : 1.0f;
+    const float scale = rstd * __uint_as_float(mx) / code_top(a.q_dtype);
     if (t == 0) {
       if (a.rstd) a.rstd[row] = rstd;
-      if (a.scale) a.scale[row] = rstd * __uint_as_float(mx) / code_top(a.q_dtype);
+      if (a.scale) a.scale[row] = scale;
     }
-    const CodeScale cs = code_scale(mx, code_top(a.q_dtype));
+    const CodeScale cs = code_scale(mx, scale, code_top(a.q_dtype));
 #pragma unroll
     for (int v = 0; v < VPT; ++v) {
       if (left(v) <= 0) continue;
@@ -241,11 +243,12 @@ __global__ void __launch_bounds__(LONG_TPR) k_norm_fwd_long(NormArgs a) {
     }
     reduce_row<LONG_TPR>(ss, mx, slots, half);
     const float rstd = a.norm ? 1.0f / sqrtf(ss / float(a.cols) + a.eps) : 1.0f;
+    const float scale = rstd * __uint_as_float(mx) / code_top(a.q_dtype);
     if (threadIdx.x == 0) {
       if (a.rstd) a.rstd[row] = rstd;
-      if (a.scale) a.scale[row] = rstd * __uint_as_float(mx) / code_top(a.q_dtype);
+      if (a.scale) a.scale[row] = scale;
     }
-    const CodeScale cs = code_scale(mx, code_top(a.q_dtype));
+    const CodeScale cs = code_scale(mx, scale, code_top(a.q_dtype));
     for (int c = threadIdx.x * 8; c < a.cols; c += LONG_TPR * 8) {
       const int n = a.cols - c;
       float h[8], g[8], u[8];
