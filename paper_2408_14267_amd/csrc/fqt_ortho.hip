@@ -26,13 +26,16 @@ using tile::PANEL_ROWS;
 using tile::PANEL_COLS;
 
 constexpr float NS_A = 3.4445f, NS_B = -4.7750f, NS_C = 2.0315f;
-// Where |u| is small beside eps every X_i is: |X_i| <= a^i |X_0|.  All of X, P and Q are then stored
-// with k more bits of scale (2^15+k, 2^14+2k, 2^13+2k; k = 0 for |X_0| a^steps >= 1/4), so that float16
-// holds the smallest gradients as well as any.  The factors depend on |u|, so they stay on the device:
+// Where |u| is small beside eps the first X_i are: |X_i| <= a^i |X_0|.  Step i then stores its X, P and Q with
+// k_i more bits of scale (2^15+k, 2^14+2k, 2^13+2k; 2^-k_i the power of two above a^i |X_0|, k_i = 0 where that
+// reaches 1/2), so that float16 holds the smallest gradients as well as any, whatever the number of
+// steps.  The factors depend on |u|, so they stay on the device, one set a step:
 struct Units {
   float down;            // 2^-2k, in the terms of Q and X' that have P once more
-  float out;             // 2^-(15+k), from the stored X to X
+  float up;              // 2^(k' - k) to the next step's k' (1 after the last step)
+  float out;             // 2^-k, from the stored X 2^-15 to X
 };
+constexpr int MAX_STEPS = 32;
 
 struct Split { uint16_t hi, lo; };
 __device__ __forceinline__ Split split(float v) {
@@ -137,7 +140,7 @@ __global__ void __launch_bounds__(256) k_ns_norm(Source s, FastDiv groups, uint3
   sum = block_sum(sum, slots);
   if (threadIdx.x == 0) part[blockIdx.x] = sum;
 }
-// 2^(15+k) / (|u| + eps) from the partial sums; one workgroup writes the units of the stored matrices.
+// 2^(15+k_0) / (|u| + eps) from the partial sums; one workgroup writes the units of the steps.
 struct Start {
   const double *part;
   int32_t parts, steps;
@@ -148,12 +151,16 @@ __device__ __forceinline__ double unit_scale(const Start &s, double *slots, bool
   double sum = 0.0;
   for (int i = threadIdx.x; i < s.parts; i += 256) sum += s.part[i];
   const double norm = sqrt(block_sum(sum, slots));
-  double most = norm / (norm + double(s.eps));             // bound of |X_i| over the steps
-  for (int i = 0; i < s.steps; ++i) most = fmin(1.0, most * double(NS_A));
+  double most = norm / (norm + double(s.eps));             // bound of |X_i|, i = 0 here
   // |X_i| < 2^-k: X below 2^15, P below 2^14, Q (|b| P at most) below 4.8 2^13.  (NaN: 0)
-  const int k = most > 0.0 ? max(0, -ilogb(most) - 1) : 0;
-  if (write && threadIdx.x == 0) *s.units = {float(ldexp(1.0, -2 * k)), float(ldexp(1.0, -15 - k))};
-  return ldexp(1.0, 15 + k) / (norm + double(s.eps));
+  auto bits = [](double v) { return v > 0.0 ? max(0, -ilogb(v) - 1) : 0; };
+  const double inv = ldexp(1.0, 15 + bits(most)) / (norm + double(s.eps));
+  if (const int i = threadIdx.x; write && i < s.steps) {   // a thread a step
+    for (int j = 0; j < i; ++j) most = fmin(1.0, most * double(NS_A));
+    const int k = bits(most), next = i + 1 < s.steps ? bits(fmin(1.0, most * double(NS_A))) : k;
+    s.units[i] = {ldexpf(1.0f, -2 * k), ldexpf(1.0f, next - k), ldexpf(1.0f, -k)};
+  }
+  return inv;
 }
 // The 64 x 64 tile of X_0 2^15 at (x0, y0): put(row, column, 8 values) in the tile.  Tall matrices are
 // transposed on the way, through t.
@@ -200,7 +207,7 @@ struct NsArgs {
   int64_t m, n;          // without padding
   tile::Tiles tiles;
   float *part;
-  const Units *units;
+  const Units *units;    // this step's
   // the last step's result
   void *out;             // o, or null
   float *w;              // weights, or null
@@ -209,26 +216,26 @@ struct NsArgs {
   float keep, rate;      // w = keep w - rate X
 };
 
-// X' or its last form, 8 columns from n of row m: v is X' 2^15.
+// The last step's X', 8 columns from n of row m: v is X' 2^(15+k).
 __device__ __forceinline__ void store_result8(const NsArgs &a, int64_t m, int64_t n, const float (&v)[8]) {
   if (m >= a.m) return;
 #pragma unroll
   for (int i = 0; i < 8; ++i) {
     if (n + i >= a.n) break;
     const int64_t at = a.tall ? (n + i) * a.ldo + m : m * a.ldo + n + i;
-    const float o = v[i] * a.units->out;
+    const float o = v[i] * 0x1p-15f * a.units->out;
     if (a.w) a.w[at] = fmaf(a.keep, a.w[at], -a.rate * o);
     else if (a.o_dtype == FQT_BF16) static_cast<bf16 *>(a.out)[at] = from_f32<bf16>(o);
     else static_cast<float *>(a.out)[at] = o;
   }
 }
 // P 2^14 from sums 2^30; Q 2^13 from sums 2^28 and P 2^14; X' 2^15 from sums 2^28 and X 2^15 (and the k
-// bits of each; down = 2^-2k).
+// bits of each; down = 2^-2k, up = 2^(k'-k)).
 __device__ __forceinline__ float gram_of(float sum) { return sum * 0x1p-16f; }
 __device__ __forceinline__ float poly_of(float sum, float p, float down) {
   return fmaf(NS_B * 0.5f, p, sum * (NS_C * 0x1p-15f) * down);
 }
-__device__ __forceinline__ float apply_of(float sum, float x, float down) { return fmaf(NS_A, x, sum * 0x1p-13f * down); }
+__device__ __forceinline__ float apply_of(float sum, float x, const Units &u) { return fmaf(NS_A, x, sum * 0x1p-13f * u.down) * u.up; }
 
 // The epilogue of 8 consecutive n (tile::run_epilogue).  diagonal: the tile holds its own mirror image.
 template <int MODE>
@@ -241,9 +248,9 @@ struct Finish {
   __device__ __forceinline__ bool in(int64_t m, int64_t n) const {
     return m < a.mp && n < (MODE == APPLY ? a.np : a.mp);
   }
-  float down;
+  Units units;
   __device__ __forceinline__ void columns(int64_t) {
-    if constexpr (MODE != GRAM) down = a.units->down;
+    if constexpr (MODE != GRAM) units = *a.units;
   }
   __device__ __forceinline__ Fetch fetch(int64_t m, int64_t n) {
     Fetch f;
@@ -256,8 +263,8 @@ struct Finish {
 #pragma unroll
     for (int i = 0; i < 8; ++i) {
       if constexpr (MODE == GRAM) v[i] = gram_of(v[i]);
-      else if constexpr (MODE == POLY) v[i] = poly_of(v[i], f.x[i], down);
-      else v[i] = apply_of(v[i], f.x[i], down);
+      else if constexpr (MODE == POLY) v[i] = poly_of(v[i], f.x[i], units.down);
+      else v[i] = apply_of(v[i], f.x[i], units);
     }
     if (MODE == APPLY && a.last) store_result8(a, m, n, v);
     else store_split8(MODE == GRAM ? a.p : MODE == POLY ? a.q : a.next, m, n, v);
@@ -455,7 +462,7 @@ __global__ void __launch_bounds__(256, 1) k_ns_small(SmallArgs a, int32_t blocks
   __shared__ __attribute__((aligned(16))) char p[2 * PANEL], q[2 * PANEL], x[2 * PANEL], y[2 * PANEL];
   const uint32_t wave = wave_id(), l = __lane_id(), wm = wave / 2 * 32, wn = wave % 2 * 32;
   const int64_t n_first = blockIdx.x * a.slice, end = min(a.n.np, n_first + a.slice);
-  const float down = a.n.units->down;
+  const Units units = *a.n.units;
   // X is read along its rows' order (m is the contraction)
   const Operand xo{reinterpret_cast<const char *>(a.n.x.p), 64 * tile::KB, a.n.np};
   auto load_x = [&](int64_t n0) {
@@ -495,7 +502,7 @@ __global__ void __launch_bounds__(256, 1) k_ns_small(SmallArgs a, int32_t blocks
         float o[4], v[4];
         join4(p + panel_at(m, n, 0), p + panel_at(m, n, 1), o);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = poly_of(acc[i][j][k], o[k], down);
+        for (int k = 0; k < 4; ++k) v[k] = poly_of(acc[i][j][k], o[k], units.down);
         put4(q, m, n, v);
       }
   }
@@ -515,7 +522,7 @@ __global__ void __launch_bounds__(256, 1) k_ns_small(SmallArgs a, int32_t blocks
         float o[4], v[4];
         join4(at, at + 32 * tile::KB, o);
 #pragma unroll
-        for (int k = 0; k < 4; ++k) v[k] = apply_of(acc[i][j][k], o[k], down);
+        for (int k = 0; k < 4; ++k) v[k] = apply_of(acc[i][j][k], o[k], units);
         if (a.n.last) {
           float r[8] = {v[0], v[1], v[2], v[3]};
           NsArgs cut = a.n;
@@ -544,7 +551,7 @@ int check_ortho(const fqt_ortho_desc *d, NsSizes *s) {
   if (!d) return FQT_E_NULL;
   if (!float_type(d->g_dtype) || !float_type(d->o_dtype)) return FQT_E_DTYPE;
   if (d->rows < 0 || d->cols < 0 || d->rows > FQT_MAX_LD || d->cols > FQT_MAX_LD) return FQT_E_SHAPE;
-  if (d->steps < 1 || d->steps > 32 || !(d->eps > 0.0f) || !std::isfinite(d->eps)) return FQT_E_INVAL;
+  if (d->steps < 1 || d->steps > MAX_STEPS || !(d->eps > 0.0f) || !std::isfinite(d->eps)) return FQT_E_INVAL;
   s->tall = d->rows > d->cols;
   s->m = std::min(d->rows, d->cols);
   s->n = std::max(d->rows, d->cols);
@@ -565,7 +572,7 @@ NsWs ns_ws(const NsSizes &s) {
   w.apply = tile::make_plan(s.mp, s.np, s.mp / 32, false, tile::PAIR_COSTS);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += align256(bytes); return o; };
-  w.norm = take(NORM_BLOCKS * sizeof(double) + sizeof(Units));
+  w.norm = take(NORM_BLOCKS * sizeof(double) + MAX_STEPS * sizeof(Units));
   const size_t x = size_t(s.mp) * s.np * 4, p = size_t(s.mp) * s.mp * 4;       // two planes of 2 bytes
   w.x[0] = take(x);
   w.x[1] = take(x);
@@ -614,7 +621,6 @@ int run_ortho(const fqt_ortho_desc *d, const NsSizes &s, Source src, NsArgs a, v
   a.q = pairs(w.q);
   a.part = reinterpret_cast<float *>(base + w.part);
   const Start start{norm, parts, d->steps, d->eps, reinterpret_cast<Units *>(norm + NORM_BLOCKS)};
-  a.units = start.units;
   a.ldo = s.ldo;
   a.o_dtype = d->o_dtype;
   a.tall = s.tall;
@@ -628,6 +634,7 @@ int run_ortho(const fqt_ortho_desc *d, const NsSizes &s, Source src, NsArgs a, v
     else k_ns_small_start<false><<<dim3(blocks), dim3(256), 0, st>>>(src, start, q);
     FQT_TRY_(last_launch_status());
     for (int i = 0; i < d->steps; ++i) {
+      q.n.units = start.units + i;
       q.n.x = x;
       q.n.next = next;
       q.n.last = i + 1 == d->steps;
@@ -649,6 +656,7 @@ int run_ortho(const fqt_ortho_desc *d, const NsSizes &s, Source src, NsArgs a, v
   else k_ns_start<false><<<grid, dim3(256), 0, st>>>(src, start, x);
   FQT_TRY_(last_launch_status());
   for (int i = 0; i < d->steps; ++i) {
+    a.units = start.units + i;
     a.x = x;
     a.next = next;
     a.last = i + 1 == d->steps;
