@@ -3,7 +3,7 @@
 // The forward is one launch of matrix tiles (fqt_tile.hpp) whose epilogue scales, adds the bias,
 // applies the activation and adds the residual to the float32 sums: no intermediate touches memory
 // but the pre-activation, if asked for.  Contractions that are long for the number of output tiles
-// are split over workgroups; their float32 partial sums meet, in a fixed order, in a second launch
+// are split over workgroups; their partial sums (float32, int32 of int8 operands) meet, in a fixed order, in a second launch
 // with the same epilogue.
 //
 // The backward is one pass over dy (and z) that writes dz = dy act'(z) in bf16 and sums dbias, then
@@ -104,7 +104,7 @@ __device__ __forceinline__ void store8(void *p, int64_t at, int dt, int n, const
 template <int ACT>
 struct Finish {
   static constexpr int DEPTH = 4;
-  static constexpr bool MIRROR = false;
+  static constexpr bool MIRROR = false, SUMS = false;
   struct Fetch {
     uint32_t res[8];       // the residual: 8 float32, or 8 bf16 in the first four
     float sx;
@@ -183,7 +183,7 @@ struct Product {
   Operand x, w;
   int64_t M, N, K;
   tile::Tiles tiles;
-  float *part;           // [splits][M][ldp] partial sums (splits > 1)
+  float *part;           // [splits][M][ldp] partial sums (splits > 1), int32 words for int8 operands
   int64_t ldp;
 };
 
@@ -202,7 +202,8 @@ __global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_prod
 }
 
 // The partial sums of a split contraction, added in order, through the epilogue.  part: rows of ldp
-// (a multiple of 8) floats.
+// (a multiple of 8) words.
+template <bool INTS>
 __global__ void __launch_bounds__(256) k_product_finish(Product p, Epilogue e) {
   const int64_t groups = p.ldp / 8, all = p.M * groups;
   with_act(e.act, [&]<int ACT>() {
@@ -211,14 +212,20 @@ __global__ void __launch_bounds__(256) k_product_finish(Product p, Epilogue e) {
       Finish<ACT> f(e);
       f.columns(n);
       const auto q = f.fetch(m, n);
-      float v[8] = {};
+      std::conditional_t<INTS, int, float> sum[8] = {};
 #pragma unroll 4
       for (uint32_t s = 0; s < p.tiles.splits; ++s) {
         float t[8];
         load8f(p.part + (s * p.M + m) * p.ldp + n, 8, t);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] += t[j];
+        for (int j = 0; j < 8; ++j) {
+          if constexpr (INTS) sum[j] += __float_as_int(t[j]);
+          else sum[j] += t[j];
+        }
       }
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = float(sum[j]);
       f.finish(m, n, v, q);
     }
   });
@@ -589,7 +596,7 @@ int launch_product(const tile::Plan &plan, Operand x, Operand w, int64_t M, int6
   FQT_TRY_(last_launch_status());
   if (plan.splits > 1) {
     const int64_t all = M * (p.ldp / 8);
-    k_product_finish<<<dim3(std::min<int64_t>((all + 255) / 256, 4096)), dim3(256), 0, st>>>(p, e);
+    k_product_finish<KIND == tile::I8K><<<dim3(std::min<int64_t>((all + 255) / 256, 4096)), dim3(256), 0, st>>>(p, e);
     return last_launch_status();
   }
   return FQT_OK;

@@ -241,7 +241,7 @@ __device__ __forceinline__ float apply_of(float sum, float x, const Units &u) { 
 template <int MODE>
 struct Finish {
   static constexpr int DEPTH = MODE == GRAM ? 1 : 4;
-  static constexpr bool MIRROR = MODE != APPLY;
+  static constexpr bool MIRROR = MODE != APPLY, SUMS = false;
   struct Fetch { float x[MODE == GRAM ? 1 : 8]; };         // X, or P
   const NsArgs &a;
   bool diagonal;

@@ -444,6 +444,8 @@ __device__ __forceinline__ void wave_fence() {
 //                             product over 64 steps
 //   e.finish(m, n, v, f)      the group's sums v and its fetch f
 //   e.mirror(n, m, v)         E::MIRROR only: 8 finished values of column n from row m on
+// E::SUMS takes the accumulators' words as they are (int32 sums of 8-bit products stay exact); the others
+// get them as float32.
 template <int KIND, typename S, typename E>
 __device__ __forceinline__ void run_epilogue(const typename Acc<KIND>::type (&acc)[S::FM][S::FN], char *lds,
                                              int64_t m0, int64_t n0, E &&e) {
@@ -465,9 +467,10 @@ __device__ __forceinline__ void run_epilogue(const typename Acc<KIND>::type (&ac
   for (int k = 0; k < S::FM; ++k) {
 #pragma unroll
     for (int j = 0; j < S::FN; ++j) {
-      const typename Acc<KIND>::type a = acc[k][j];
-      *reinterpret_cast<float4 *>(patch + (l % 16) * PITCH + j * 16 + 4 * (l / 16)) =
-          make_float4(float(a[0]), float(a[1]), float(a[2]), float(a[3]));
+      f32x4 a;
+      if constexpr (std::remove_reference_t<E>::SUMS) a = __builtin_bit_cast(f32x4, acc[k][j]);
+      else a = __builtin_convertvector(acc[k][j], f32x4);
+      *reinterpret_cast<f32x4 *>(patch + (l % 16) * PITCH + j * 16 + 4 * (l / 16)) = a;
     }
     wave_fence();
 #pragma unroll
@@ -501,10 +504,10 @@ __device__ __forceinline__ void run_epilogue(const typename Acc<KIND>::type (&ac
     }
   }
 }
-// Partial sums of a split contraction: rows of ld (a multiple of 8) floats.
+// Partial sums of a split contraction: rows of ld (a multiple of 8) words, int32 or float32.
 struct StorePart {
   static constexpr int DEPTH = 1;
-  static constexpr bool MIRROR = false;
+  static constexpr bool MIRROR = false, SUMS = true;
   struct Fetch {};
   float *part;
   int64_t M, ld;
