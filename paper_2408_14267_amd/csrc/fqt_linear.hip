@@ -154,9 +154,9 @@ struct Finish {
   }
   __device__ __forceinline__ void finish(int64_t m, int64_t n, float (&v)[8], const Fetch &f) {
     if (m >= e.M || cnt == 0) return;
-    if (e.sx) {
+    if (e.sx) {            // (the sum times one and then the other: the scales' product may leave float32)
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] *= f.sx * sw[i];
+      for (int i = 0; i < 8; ++i) v[i] = v[i] * f.sx * sw[i];
     }
     if (e.bias) {
 #pragma unroll
