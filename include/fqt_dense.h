@@ -92,7 +92,8 @@ int fqt_quantize_rows(const fqt_norm_desc *desc, const void *x, void *q, float *
  * rows, the form for single tokens, are summed on the vector units, in float32 for every type. */
 #define FQT_ACT_NONE 0
 #define FQT_ACT_RELU 1
-#define FQT_ACT_GELU 2                    /* z * Phi(z), Phi by the error function */
+#define FQT_ACT_GELU 2                    /* z * Phi(z), Phi the normal distribution
+                                           * function, to 2.5e-7               */
 #define FQT_ACT_SILU 3                    /* z / (1 + exp(-z))                     */
 #define FQT_ACT_HARDTANH 4                /* z clamped to [-1, 1]                  */
 typedef struct {

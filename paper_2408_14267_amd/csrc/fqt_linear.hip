@@ -23,25 +23,35 @@ using tile::COLS;
 
 // ----------------------------------------------------------------------------- activations
 
-__device__ __forceinline__ float exp_neg(float v) {        // exp(-v)
-  return __builtin_amdgcn_exp2f(v * -1.44269504088896341f);
+// exp(-v).  WIDE: the rounding of the exponent, up to |v| 2^-24 of the result, is taken back (v is held
+// where the result is neither 0 nor infinite already); for float32 outputs, since bf16's do not show it.
+template <bool WIDE>
+__device__ __forceinline__ float exp_neg(float v) {
+  constexpr float LOG2E = 1.44269504088896341f, LOG2E_LOW = 1.92596299e-8f, LN2 = 0.69314718055994531f;
+  if constexpr (WIDE) v = fminf(fmaxf(v, -150.0f), 150.0f);
+  const float b = v * -LOG2E, e = __builtin_amdgcn_exp2f(b);
+  if constexpr (!WIDE) return e;
+  else return e * fmaf(fmaf(v, -LOG2E_LOW, fmaf(v, -LOG2E, -b)), LN2, 1.0f);
 }
-// Phi(-a) and exp(-a^2 / 2) for a >= 0, Phi the normal distribution function: Phi(-a) = exp(-a^2 / 2)
-// times a quintic in t = 1 / (1 + p a / sqrt 2) (Abramowitz and Stegun 7.1.26 halved; absolute error
-// below 8e-8).  About 20 issue slots; the library's erf costs four times that, and a 256 x 256 tile pays
-// 0.4 us for each slot.
+// Phi(-a) and exp(-a^2 / 2) for a >= 0, Phi the normal distribution function: exp(a^2 / 2) Phi(-a) (a + 3) is
+// smooth in s = (a - 3) / (a + 3), and a sextic in it, fitted to the least largest error of a Phi(-a), is
+// within 9e-9 of that; float32 roundings bring Phi to 2.5e-7 and a Phi(-a) to 9e-8.  The coefficients fall off, so
+// nothing cancels.  About 23 issue slots; the library's erf costs four times that, and a 256 x 256 tile
+// pays 0.4 us for each slot.
 __device__ __forceinline__ float normal_tail(float a, float *e) {
-  const float t = __builtin_amdgcn_rcpf(fmaf(a, 0.3275911f * 0.70710678118654752f, 1.0f));
-  float q = fmaf(t, 0.5f * 1.061405429f, 0.5f * -1.453152027f);
-  q = fmaf(t, q, 0.5f * 1.421413741f);
-  q = fmaf(t, q, 0.5f * -0.284496736f);
-  q = fmaf(t, q, 0.5f * 0.254829592f);
+  const float t = __builtin_amdgcn_rcpf(a + 3.0f), s = fmaf(t, -6.0f, 1.0f);
+  float q = fmaf(s, 0.00200464337f, 0.00693698652f);
+  q = fmaf(s, q, -0.0110280172f);
+  q = fmaf(s, q, -0.0475851104f);
+  q = fmaf(s, q, 0.229960269f);
+  q = fmaf(s, q, -0.509330356f);
+  q = fmaf(s, q, 0.729084549f);
   *e = __builtin_amdgcn_exp2f(a * (a * -0.72134752044448170f));
   return q * t * *e;
 }
 // (Phi(-30) is 0 in float32: a need not be larger, and an infinite one would meet it.)
 __device__ __forceinline__ float tail_arg(float z) { return fminf(fabsf(z), 30.0f); }
-template <int ACT>
+template <int ACT, bool WIDE>
 __device__ __forceinline__ float activate(float z) {
   if constexpr (ACT == FQT_ACT_RELU) return z > 0.0f ? z : (z != z ? z : 0.0f);
   else if constexpr (ACT == FQT_ACT_GELU) {
@@ -50,7 +60,7 @@ __device__ __forceinline__ float activate(float z) {
     float e;
     const float q = normal_tail(a, &e);
     return z != z ? z : fmaf(-a, q, fmaxf(z, 0.0f));
-  } else if constexpr (ACT == FQT_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + exp_neg(z));
+  } else if constexpr (ACT == FQT_ACT_SILU) return z * __builtin_amdgcn_rcpf(1.0f + exp_neg<WIDE>(z));
   else if constexpr (ACT == FQT_ACT_HARDTANH) return z != z ? z : fminf(fmaxf(z, -1.0f), 1.0f);
   else return z;
 }
@@ -63,7 +73,7 @@ __device__ __forceinline__ float slope(float z) {
     const float q = normal_tail(a, &e), d = z > 0.0f ? 1.0f - q : q;
     return z != z ? z : fmaf(copysignf(a, z) * 0.39894228040143268f, e, d);
   } else if constexpr (ACT == FQT_ACT_SILU) {
-    const float t = __builtin_amdgcn_rcpf(1.0f + exp_neg(z));
+    const float t = __builtin_amdgcn_rcpf(1.0f + exp_neg<false>(z));
     return t * fmaf(z, 1.0f - t, 1.0f);
   } else if constexpr (ACT == FQT_ACT_HARDTANH) return z > -1.0f && z < 1.0f ? 1.0f : 0.0f;
   else return 1.0f;
@@ -163,10 +173,15 @@ struct Finish {
       for (int i = 0; i < 8; ++i) v[i] += bias[i];
     }
     if (e.z) store8(e.z, m * e.ldz + n, e.y_dtype, cnt, v);
+    const bool half = e.y_dtype == FQT_BF16;
+    if (ACT != FQT_ACT_SILU || half) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = activate<ACT>(v[i]);
+      for (int i = 0; i < 8; ++i) v[i] = activate<ACT, false>(v[i]);
+    } else {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = activate<ACT, true>(v[i]);
+    }
     if (e.res) {
-      const bool half = e.y_dtype == FQT_BF16;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const uint32_t two = f.res[i / 2];
