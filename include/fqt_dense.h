@@ -86,8 +86,8 @@ int fqt_quantize_rows(const fqt_norm_desc *desc, const void *x, void *q, float *
  * x [M][K] and w [N][K] of x_dtype; the scales (float32 [M], [N]) belong to the 8-bit types and are
  * NULL for FQT_BF16.  bias float32 [N], residual, z, y [M][N] of y_dtype; bias, residual and z are
  * optional.  z is stored rounded; y comes from the unrounded z.  y may be residual (same ld).
- * FQT_I8 sums are exact in int32, so K <= 133144 there; M N, M K and N K are at most 2^40
- * (FQT_E_SHAPE).  FQT_E4M3 sums have the precision of their matrix instruction, 1e-5 to 6e-5 of their
+ * FQT_I8 sums are exact in int32, so K <= 133144 there; fewer than 2^23 tiles of 256 x 256 cover
+ * M x N, M x K and N x K each (FQT_E_SHAPE).  FQT_E4M3 sums have the precision of their matrix instruction, 1e-5 to 6e-5 of their
  * norm, where y is FQT_BF16, and float32's (through bf16 copies of the codes) where it is FQT_F32.  Up to four
  * rows, the form for single tokens, are summed on the vector units, in float32 for every type. */
 #define FQT_ACT_NONE 0
@@ -105,6 +105,20 @@ typedef struct {
   int32_t dx_dtype, dw_dtype;         /* FQT_F32 or FQT_BF16                                      */
   int32_t act;
 } fqt_linear_desc;
+
+/* How a call lays out a matrix product, from its sizes alone (nothing is launched): the edge of the
+ * output tiles and the workgroups of each launch (a second one takes the last tiles in smaller ones),
+ * and the pieces that the contraction is split into.  No launches: the sizes take a form without
+ * tiles (forwards of up to four rows, orthogonalisations of up to 64). */
+typedef struct {
+  int32_t launches, splits;
+  int32_t tile[2], threads[2];
+  int64_t workgroups[2];
+} fqt_product_plan;
+#define FQT_PRODUCT_FORWARD 0
+#define FQT_PRODUCT_DX 1
+#define FQT_PRODUCT_DW 2
+int fqt_linear_plan(const fqt_linear_desc *desc, int32_t product, fqt_product_plan *plan);
 
 int fqt_linear_workspace_size(const fqt_linear_desc *desc, int32_t backward, size_t *bytes);
 int fqt_linear_forward(const fqt_linear_desc *desc, const void *x, const void *w,
@@ -131,7 +145,7 @@ int fqt_linear_backward(const fqt_linear_desc *desc, const void *x, const void *
  * taken on the short side of u; steps of them bring the singular values of u near 1.  The products
  * run on the 16-bit matrix cores from operands split in two (22 bits and their rounding), with
  * float32 sums: results as from float32 products.  The shorter side is at most 65536, rows times cols
- * below 2^34 (FQT_E_SHAPE otherwise). */
+ * (in eights) below 2^34 (FQT_E_SHAPE otherwise). */
 typedef struct {
   int64_t rows, cols;
   int64_t ldg, ldo, ldm;              /* g; o and w; m                                           */
@@ -148,6 +162,11 @@ typedef struct {
   int32_t nesterov;
 } fqt_muon_cfg;
 
+/* The plans of P = X X^T, of b P + c P^2 (both symmetric) and of its product with X. */
+#define FQT_PRODUCT_GRAM 0
+#define FQT_PRODUCT_POLY 1
+#define FQT_PRODUCT_APPLY 2
+int fqt_ortho_plan(const fqt_ortho_desc *desc, int32_t product, fqt_product_plan *plan);
 int fqt_ortho_workspace_size(const fqt_ortho_desc *desc, size_t *bytes);
 /* o = X_steps(g).  o may be g where both have one type and stride. */
 int fqt_orthogonalize(const fqt_ortho_desc *desc, const void *g, void *o, void *ws,

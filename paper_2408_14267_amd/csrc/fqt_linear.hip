@@ -571,9 +571,9 @@ int check_linear(const fqt_linear_desc *d, Sizes *s) {
   if (d->act < FQT_ACT_NONE || d->act > FQT_ACT_HARDTANH) return FQT_E_INVAL;
   if (d->M < 0 || d->N < 0 || d->K < 0 || d->M >= FQT_MAX_ROWS || d->N > FQT_MAX_LD || d->K > FQT_MAX_LD)
     return FQT_E_SHAPE;
-  // (tiles and workgroups are counted in 32 bits)
-  constexpr double MOST = 1ull << 40;
-  if (double(d->M) * d->N > MOST || double(d->M) * d->K > MOST || double(d->N) * d->K > MOST) return FQT_E_SHAPE;
+  // (a launch counts its threads in 32 bits)
+  for (const uint64_t tiles : {tile::large_tiles(d->M, d->N), tile::large_tiles(d->M, d->K), tile::large_tiles(d->N, d->K)})
+    if (tiles >= tile::MOST_LARGE) return FQT_E_SHAPE;
   if (d->x_dtype == FQT_I8 && d->K > 133144) return FQT_E_SHAPE;   // 127^2 K < 2^31
   *s = {d->M, d->N, d->K, row_stride(d->ldx, d->K), row_stride(d->ldw, d->K), row_stride(d->ldr, d->N),
         row_stride(d->ldy, d->N), row_stride(d->ldz, d->N), row_stride(d->lddx, d->K),
@@ -606,7 +606,7 @@ int launch_product(const tile::Plan &plan, Operand x, Operand w, int64_t M, int6
   e = sized(e, M, N);
   tile::for_launches(plan, [&]<int SHAPE>(const tile::Tiles &t) {
     p.tiles = t;
-    k_product<KIND, LX, LW, SHAPE><<<dim3(tile::blocks_of(t)), dim3(tile::ShapeOf<SHAPE>::type::THREADS), 0, st>>>(p, e);
+    k_product<KIND, LX, LW, SHAPE><<<dim3(uint32_t(tile::blocks_of(t))), dim3(tile::ShapeOf<SHAPE>::type::THREADS), 0, st>>>(p, e);
   });
   FQT_TRY_(last_launch_status());
   if (plan.splits > 1) {
@@ -705,6 +705,18 @@ extern "C" int fqt_linear_workspace_size(const fqt_linear_desc *d, int32_t backw
   FQT_TRY_(check_linear(d, &s));
   if (!bytes) return FQT_E_NULL;
   *bytes = std::max<size_t>(256, backward ? bwd_ws(s).total : fwd_ws(*d, s).total);
+  return FQT_OK;
+}
+
+extern "C" int fqt_linear_plan(const fqt_linear_desc *d, int32_t product, fqt_product_plan *plan) {
+  Sizes s;
+  FQT_TRY_(check_linear(d, &s));
+  if (!plan) return FQT_E_NULL;
+  if (product < FQT_PRODUCT_FORWARD || product > FQT_PRODUCT_DW) return FQT_E_INVAL;
+  tile::Plan p{};
+  if (product == FQT_PRODUCT_FORWARD) p = fwd_ws(*d, s).plan;
+  else p = product == FQT_PRODUCT_DX ? bwd_ws(s).dx : bwd_ws(s).dw;
+  tile::describe(p, plan);
   return FQT_OK;
 }
 

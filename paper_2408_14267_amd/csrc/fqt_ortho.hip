@@ -593,7 +593,7 @@ template <int MODE>
 int launch_ns(const tile::Plan &plan, NsArgs a, hipStream_t st) {
   tile::for_launches(plan, [&]<int SHAPE>(const tile::Tiles &t) {
     a.tiles = t;
-    k_ns<MODE, SHAPE><<<dim3(tile::blocks_of(t)), dim3(tile::ShapeOf<SHAPE>::type::THREADS), 0, st>>>(a);
+    k_ns<MODE, SHAPE><<<dim3(uint32_t(tile::blocks_of(t))), dim3(tile::ShapeOf<SHAPE>::type::THREADS), 0, st>>>(a);
     if (t.splits > 1) {
       if constexpr (MODE == APPLY)
         k_ns_join<<<dim3(std::min<int64_t>((a.mp * a.np / 8 + 255) / 256, 4096)), dim3(256), 0, st>>>(a);
@@ -680,6 +680,20 @@ extern "C" int fqt_ortho_workspace_size(const fqt_ortho_desc *d, size_t *bytes) 
   FQT_TRY_(check_ortho(d, &s));
   if (!bytes) return FQT_E_NULL;
   *bytes = s.m ? ns_ws(s).total : 256;
+  return FQT_OK;
+}
+
+extern "C" int fqt_ortho_plan(const fqt_ortho_desc *d, int32_t product, fqt_product_plan *plan) {
+  NsSizes s;
+  FQT_TRY_(check_ortho(d, &s));
+  if (!plan) return FQT_E_NULL;
+  if (product < FQT_PRODUCT_GRAM || product > FQT_PRODUCT_APPLY) return FQT_E_INVAL;
+  tile::Plan p{};
+  if (s.mp > 64) {
+    const NsWs w = ns_ws(s);
+    p = product == FQT_PRODUCT_GRAM ? w.gram : product == FQT_PRODUCT_POLY ? w.poly : w.apply;
+  }
+  tile::describe(p, plan);
   return FQT_OK;
 }
 

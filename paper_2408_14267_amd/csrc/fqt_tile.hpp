@@ -528,6 +528,7 @@ template <int SHAPE> struct ShapeOf;
 template <> struct ShapeOf<LARGE> { typedef Large type; };
 template <> struct ShapeOf<MIDDLE> { typedef Middle type; };
 template <> struct ShapeOf<SMALL> { typedef Small type; };
+constexpr int EDGES[] = {Large::BM, Middle::BM, Small::BM}, SHAPE_THREADS[] = {Large::THREADS, Middle::THREADS, Small::THREADS};
 
 // One launch of a product: `count` tiles from tile `first` on, of an order over nm x nn tiles or,
 // symmetric, over the tiles on and above the diagonal.  parts: workgroups take sixteenths (Small) of
@@ -554,6 +555,32 @@ constexpr Costs DENSE_COSTS{{1.58}, {0.60, 0.90}, {0.25, 0.40, 0.58}, {6, 5, 4}}
     PAIR_COSTS{{2.0}, {0.81, 1.26}, {0.28, 0.39, 0.62}, {18, 8, 5}},
     SYMMETRIC_COSTS{{2.0}, {0.81, 1.15}, {0.28, 0.40, 0.75}, {10, 8, 4}};
 
+// Workgroups of a launch.
+inline uint64_t blocks_of(const Tiles &t) { return uint64_t(t.count) * t.splits * (t.parts ? 16 : 1); }
+// Whether a launch counts its threads in 32 bits.
+inline bool launchable(const Plan &p) {
+  for (int i = 0; i < p.launches; ++i)
+    if (blocks_of(p.t[i]) * SHAPE_THREADS[p.shape[i]] >> 32) return false;
+  return true;
+}
+// Large tiles that cover M x N.
+inline uint64_t large_tiles(int64_t M, int64_t N) {
+  return uint64_t((M + Large::BM - 1) / Large::BM) * uint64_t((N + Large::BN - 1) / Large::BN);
+}
+constexpr uint64_t MOST_LARGE = 1ull << 23;                // fewer than this are one launch
+
+inline void describe(const Plan &p, fqt_product_plan *o) {
+  *o = {};
+  o->launches = p.launches;
+  o->splits = int32_t(p.splits);
+  for (int i = 0; i < p.launches; ++i) {
+    o->tile[i] = p.t[i].parts ? Small::BM : EDGES[p.shape[i]];
+    o->threads[i] = SHAPE_THREADS[p.shape[i]];
+    o->workgroups[i] = int64_t(blocks_of(p.t[i]));
+  }
+}
+
+// The cheapest plan that can be launched; products of fewer than MOST_LARGE tiles have one.
 inline Plan make_plan(int64_t M, int64_t N, int64_t steps, bool symmetric, const Costs &costs) {
   auto grid = [&](int64_t b) {
     Tiles t{};
@@ -568,14 +595,14 @@ inline Plan make_plan(int64_t M, int64_t N, int64_t steps, bool symmetric, const
   Plan best{};
   double cost = 1e30;
   auto take = [&](double c, const Plan &p) {
-    if (c < cost) cost = c, best = p;
+    if (c < cost && launchable(p)) cost = c, best = p;
   };
   const double s = double(steps);
   const double entries = double(M) * double(N) * (symmetric ? 0.5 : 1.0);
   // us of `blocks` workgroups of `n` steps, `cu` of which fit a CU
-  auto run = [](uint32_t blocks, double n, int cu, const double *step, double start) {
-    const uint32_t full = 256 * cu, rest = blocks % full;
-    double c = blocks / full * (step[cu - 1] * n + start);
+  auto run = [](uint64_t blocks, double n, int cu, const double *step, double start) {
+    const uint64_t full = 256 * cu, rest = blocks % full;
+    double c = double(blocks / full) * (step[cu - 1] * n + start);
     if (rest) c += step[(rest - 1) / 256] * n + start;
     return c;
   };
@@ -598,7 +625,7 @@ inline Plan make_plan(int64_t M, int64_t N, int64_t steps, bool symmetric, const
       Tiles t = g;
       t.steps = uint32_t(std::max<int64_t>(1, (steps + n - 1) / n));
       t.splits = uint32_t(std::max<int64_t>(1, (steps + t.steps - 1) / t.steps));
-      double c = run(t.count * t.splits, t.steps, cu, step, start) + launch;
+      double c = run(blocks_of(t), t.steps, cu, step, start) + launch;
       // the partial sums, written and read at 4 TB/s one split after the other, and their launch
       if (t.splits > 1) c += 4 + 0.2 * t.splits + t.splits * entries * 8 / 4e6;
       take(c, Plan{{shape, shape}, {t, t}, 1, t.splits});
@@ -646,8 +673,6 @@ __device__ __forceinline__ Place place(const Tiles &t, uint32_t b) {
   if (parts > 1) return {int64_t(m) * 256 + part / 4 * 64, int64_t(n) * 256 + part % 4 * 64, split, m == n};
   return {int64_t(m) * S::BM, int64_t(n) * S::BN, split, m == n};
 }
-// Workgroups of a launch.
-inline uint32_t blocks_of(const Tiles &t) { return t.count * t.splits * (t.parts ? 16 : 1); }
 
 // The accumulators of a placed tile, by the loop that suits the shape.
 template <int KIND, int LX, int LW, int SHAPE, typename S>

@@ -22,9 +22,10 @@ FQT_MAX_LD = 1 << 22
 ACTIVATIONS = {"none": FQT_ACT_NONE, "relu": FQT_ACT_RELU, "gelu": FQT_ACT_GELU,
                "silu": FQT_ACT_SILU, "hardtanh": FQT_ACT_HARDTANH}
 EXPORTED = ("fqt_rmsnorm_forward", "fqt_norm_workspace_size", "fqt_rmsnorm_backward",
-            "fqt_quantize_rows", "fqt_linear_workspace_size", "fqt_linear_forward",
-            "fqt_linear_backward", "fqt_ortho_workspace_size", "fqt_orthogonalize",
-            "fqt_muon_step")
+            "fqt_quantize_rows", "fqt_linear_plan", "fqt_linear_workspace_size",
+            "fqt_linear_forward", "fqt_linear_backward", "fqt_ortho_plan",
+            "fqt_ortho_workspace_size", "fqt_orthogonalize", "fqt_muon_step")
+LINEAR_PRODUCTS, ORTHO_PRODUCTS = ("forward", "dx", "dw"), ("gram", "poly", "apply")
 
 _CODES = {torch.float32: FQT_F32, "f32": FQT_F32, torch.bfloat16: FQT_BF16, "bf16": FQT_BF16,
           torch.int8: FQT_I8, "int8": FQT_I8, torch.float8_e4m3fn: FQT_E4M3, "e4m3": FQT_E4M3,
@@ -65,18 +66,25 @@ class fqt_muon_cfg(Structure):
                 ("scale", c_float), ("nesterov", c_int32)]
 
 
+class fqt_product_plan(Structure):
+    _fields_ = [("launches", c_int32), ("splits", c_int32), ("tile", c_int32 * 2),
+                ("threads", c_int32 * 2), ("workgroups", c_int64 * 2)]
+
+
 def _bind(lib):
-    N, L, O, U = (POINTER(t) for t in (fqt_norm_desc, fqt_linear_desc, fqt_ortho_desc,
-                                       fqt_muon_cfg))
+    N, L, O, U, P = (POINTER(t) for t in (fqt_norm_desc, fqt_linear_desc, fqt_ortho_desc,
+                                          fqt_muon_cfg, fqt_product_plan))
     p, size = c_void_p, POINTER(c_size_t)
     for name, args in {
             "fqt_rmsnorm_forward": [N] + [p] * 9,
             "fqt_norm_workspace_size": [N, size],
             "fqt_rmsnorm_backward": [N] + [p] * 8 + [c_size_t, p],
             "fqt_quantize_rows": [N] + [p] * 4,
+            "fqt_linear_plan": [L, c_int32, P],
             "fqt_linear_workspace_size": [L, c_int32, size],
             "fqt_linear_forward": [L] + [p] * 9 + [c_size_t, p],
             "fqt_linear_backward": [L] + [p] * 10 + [c_size_t, p],
+            "fqt_ortho_plan": [O, c_int32, P],
             "fqt_ortho_workspace_size": [O, size],
             "fqt_orthogonalize": [O] + [p] * 3 + [c_size_t, p],
             "fqt_muon_step": [O, U] + [p] * 4 + [c_size_t, p]}.items():
@@ -261,6 +269,19 @@ def fqt_quantize_rows(desc, x, q, scale, stream=None):
 
 # ----------------------------------------------------------------------------- linear
 
+def _plan(fn, desc, product, products):
+    if product not in products:
+        raise ValueError(f"unknown product {product!r}: {', '.join(products)}")
+    plan = fqt_product_plan()
+    _check(fn(desc, products.index(product), ctypes.byref(plan)), fn.__name__)
+    return plan
+
+
+def fqt_linear_plan(desc, product="forward"):
+    """The fqt_product_plan of "forward", "dx" or "dw" (host only)."""
+    return _plan(_lib.fqt_linear_plan, desc, product, LINEAR_PRODUCTS)
+
+
 def fqt_linear_workspace_size(desc, backward=False):
     n = c_size_t()
     _check(_lib.fqt_linear_workspace_size(desc, int(backward), ctypes.byref(n)),
@@ -330,6 +351,11 @@ def fqt_linear_backward(desc, x, w, dy, ws, z=None, x_scale=None, w_scale=None, 
 
 
 # ----------------------------------------------------------------------------- orthogonalisation
+
+def fqt_ortho_plan(desc, product):
+    """The fqt_product_plan of "gram", "poly" or "apply" (host only)."""
+    return _plan(_lib.fqt_ortho_plan, desc, product, ORTHO_PRODUCTS)
+
 
 def fqt_ortho_workspace_size(desc):
     n = c_size_t()
