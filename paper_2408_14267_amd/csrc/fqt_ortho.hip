@@ -292,35 +292,17 @@ __global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_ns(N
     tile::contract<tile::SPLITK, PANEL_ROWS, PANEL_ROWS, SHAPE, S>(op(a.p, a.mp), op(a.p, a.mp), K, at, a.tiles, lds, acc);
   else
     tile::contract<tile::SPLITK, PANEL_ROWS, PANEL_COLS, SHAPE, S>(op(a.q, a.mp), op(a.x, a.np), K, at, a.tiles, lds, acc);
-  if (a.tiles.splits > 1) {
-    const int64_t N = MODE == APPLY ? a.np : a.mp;
-    tile::run_epilogue<tile::SPLITK, S>(acc, lds, at.m0, at.n0, tile::StorePart{a.part + at.split * a.mp * N, a.mp, N});
-  } else {
-    tile::run_epilogue<tile::SPLITK, S>(acc, lds, at.m0, at.n0, Finish<MODE>{a, at.diagonal});
-  }
+  if constexpr (MODE != APPLY)
+    if (a.tiles.splits > 1) {
+      tile::run_epilogue<tile::SPLITK, S>(acc, lds, at.m0, at.n0,
+                                          tile::StorePart{a.part + at.split * a.mp * a.mp, a.mp, a.mp});
+      return;
+    }
+  tile::run_epilogue<tile::SPLITK, S>(acc, lds, at.m0, at.n0, Finish<MODE>{a, at.diagonal});
 }
 
-// The partial sums of a split contraction, added in order.  APPLY: a thread per 8 columns.
-__global__ void __launch_bounds__(256) k_ns_join(NsArgs a) {
-  const int64_t groups = a.np / 8, all = a.mp * groups;
-  for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < all; i += int64_t(gridDim.x) * 256) {
-    const int64_t m = i / groups, n = i % groups * 8;
-    Finish<APPLY> f{a, false};
-    f.columns(n);
-    const auto q = f.fetch(m, n);
-    float v[8] = {};
-#pragma unroll 4
-    for (uint32_t s = 0; s < a.tiles.splits; ++s) {
-      float t[8];
-      load8f(a.part + (s * a.mp + m) * a.np + n, 8, t);
-#pragma unroll
-      for (int j = 0; j < 8; ++j) v[j] += t[j];
-    }
-    f.finish(m, n, v, q);
-  }
-}
-// The symmetric products: a workgroup per 64 x 64 tile on or above the diagonal of tiles of edge B, whose
-// mirror image goes out through LDS.
+// The partial sums of a split symmetric product, added in order: a workgroup per 64 x 64 tile on or above
+// the diagonal of tiles of edge B, whose mirror image goes out through LDS.
 template <int MODE, int B>
 __global__ void __launch_bounds__(512) k_ns_join_symmetric(NsArgs a) {
   __shared__ float t[64][65];
@@ -569,7 +551,8 @@ NsWs ns_ws(const NsSizes &s) {
   NsWs w{};
   w.gram = tile::make_plan(s.mp, s.mp, s.np / 32, true, tile::SYMMETRIC_COSTS);
   w.poly = tile::make_plan(s.mp, s.mp, s.mp / 32, true, tile::SYMMETRIC_COSTS);
-  w.apply = tile::make_plan(s.mp, s.np, s.mp / 32, false, tile::PAIR_COSTS);
+  // (X' has at least as many entries as its contraction is long: splitting it never pays)
+  w.apply = tile::make_plan(s.mp, s.np, s.mp / 32, false, tile::PAIR_COSTS, 1);
   size_t at = 0;
   auto take = [&](size_t bytes) { const size_t o = at; at += align256(bytes); return o; };
   w.norm = take(NORM_BLOCKS * sizeof(double) + MAX_STEPS * sizeof(Units));
@@ -584,7 +567,7 @@ NsWs ns_ws(const NsSizes &s) {
     return w;
   }
   auto part = [&](const tile::Plan &pl, size_t entries) { return pl.splits > 1 ? size_t(pl.splits) * entries * 4 : 0; };
-  w.part = take(std::max({part(w.gram, s.mp * s.mp), part(w.poly, s.mp * s.mp), part(w.apply, s.mp * s.np)}));
+  w.part = take(std::max(part(w.gram, s.mp * s.mp), part(w.poly, s.mp * s.mp)));
   w.total = at;
   return w;
 }
@@ -594,12 +577,9 @@ int launch_ns(const tile::Plan &plan, NsArgs a, hipStream_t st) {
   tile::for_launches(plan, [&]<int SHAPE>(const tile::Tiles &t) {
     a.tiles = t;
     k_ns<MODE, SHAPE><<<dim3(uint32_t(tile::blocks_of(t))), dim3(tile::ShapeOf<SHAPE>::type::THREADS), 0, st>>>(a);
-    if (t.splits > 1) {
-      if constexpr (MODE == APPLY)
-        k_ns_join<<<dim3(std::min<int64_t>((a.mp * a.np / 8 + 255) / 256, 4096)), dim3(256), 0, st>>>(a);
-      else
+    if constexpr (MODE != APPLY)
+      if (t.splits > 1)
         k_ns_join_symmetric<MODE, tile::ShapeOf<SHAPE>::type::BM><<<dim3(a.mp / 64, a.mp / 64), dim3(512), 0, st>>>(a);
-    }
   });
   return last_launch_status();
 }

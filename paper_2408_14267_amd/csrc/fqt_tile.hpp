@@ -580,8 +580,9 @@ inline void describe(const Plan &p, fqt_product_plan *o) {
   }
 }
 
-// The cheapest plan that can be launched; products of fewer than MOST_LARGE tiles have one.
-inline Plan make_plan(int64_t M, int64_t N, int64_t steps, bool symmetric, const Costs &costs) {
+// The cheapest plan that can be launched; products of fewer than MOST_LARGE tiles have one.  most: the most pieces
+// of the contraction.
+inline Plan make_plan(int64_t M, int64_t N, int64_t steps, bool symmetric, const Costs &costs, int64_t most = 64) {
   auto grid = [&](int64_t b) {
     Tiles t{};
     t.nm = uint32_t((M + b - 1) / b);
@@ -621,7 +622,7 @@ inline Plan make_plan(int64_t M, int64_t N, int64_t steps, bool symmetric, const
   }
   auto split = [&](int shape, int64_t b, int cu, const double *step, double start) {
     const Tiles g = grid(b);
-    for (int64_t n = 1; n <= 64 && (n == 1 || steps / n >= 4); n += n < 16 ? 1 : 8) {
+    for (int64_t n = 1; n <= most && (n == 1 || steps / n >= 4); n += n < 16 ? 1 : 8) {
       Tiles t = g;
       t.steps = uint32_t(std::max<int64_t>(1, (steps + n - 1) / n));
       t.splits = uint32_t(std::max<int64_t>(1, (steps + t.steps - 1) / t.steps));
