@@ -15,29 +15,16 @@ import torch
 import torch.nn as nn
 from torch.autograd.function import once_differentiable
 
-from . import dense, fqt, train
+from . import dense, train
 
 _BF16, _F32 = torch.bfloat16, torch.float32
 
 
-class _Slots:
-    """Workspaces per call shape, device and stream (one serves one call at a time).  A capture takes one
-    that is there: a new one would belong to the graph's pool."""
-
-    def __init__(self):
-        self.slots = {}
-
-    def get(self, key, size, device):
-        slots = self.slots.setdefault(key, {})
-        at = device.index, fqt.current_stream()
-        ws = slots.get(at)
-        if ws is None:
-            if torch.cuda.is_current_stream_capturing():
-                for (index, _), ws in slots.items():
-                    if index == device.index:
-                        return ws
-            ws = slots[at] = torch.empty(max(size, 1), dtype=torch.uint8, device=device)
-        return ws
+def _workspace(size, device):
+    """A call's workspace, from torch's allocator for that call alone: the calls of a stream take the same
+    memory one after the other, those of other streams, threads and graphs (a capture's comes from the
+    graph's pool) never, and nothing is held between calls."""
+    return torch.empty(max(size, 1), dtype=torch.uint8, device=device)
 
 
 def _rows(t, cols, name):
@@ -60,7 +47,7 @@ class _NormFn(torch.autograd.Function):
         dense.fqt_rmsnorm_forward(desc, x, g, residual=residual, h=h if residual is not None else None,
                                   y=y, rstd=rstd)
         ctx.save_for_backward(h, g, rstd)
-        ctx.desc, ctx.mod, ctx.residual = desc, mod, residual is not None
+        ctx.desc, ctx.residual = desc, residual is not None
         return (y, h) if ctx.residual else y
 
     @staticmethod
@@ -69,7 +56,7 @@ class _NormFn(torch.autograd.Function):
         h, g, rstd = ctx.saved_tensors
         desc = ctx.desc
         dx, dg = torch.empty_like(h), torch.empty_like(g)
-        ws = ctx.mod.slots.get(("norm", desc.rows), dense.fqt_norm_workspace_size(desc), h.device)
+        ws = _workspace(dense.fqt_norm_workspace_size(desc), h.device)
         dense.fqt_rmsnorm_backward(desc, h, g, rstd, dy.contiguous(), dx, dg, ws,
                                    dres=dh.contiguous() if ctx.residual else None)
         return dx, dx if ctx.residual else None, dg, None
@@ -83,7 +70,6 @@ class RMSNorm(nn.Module):
         super().__init__()
         self.weight = nn.Parameter(torch.ones(features))
         self.features, self.eps, self.out_dtype = features, eps, out_dtype
-        self.slots = _Slots()
 
     def forward(self, x, residual=None):
         m = _rows(x, self.features, "x")
@@ -112,18 +98,18 @@ def _linear_forward(mod, x, x_scale, w, bias, residual, out_dtype):
                              dw_dtype=_F32)
     y = torch.empty(M, N, dtype=out_dtype, device=x.device)
     z = torch.empty_like(y) if mod.act != "none" else None
-    ws = mod.slots.get(("fwd", M, out_dtype), dense.fqt_linear_workspace_size(desc), x.device)
+    ws = _workspace(dense.fqt_linear_workspace_size(desc), x.device)
     dense.fqt_linear_forward(desc, x, wq, y, ws, bias=bias, residual=residual, x_scale=x_scale,
                              w_scale=w_scale, z=z)
     return y, z, wq, w_scale, desc
 
 
-def _linear_backward(ctx, mod, desc, x, x_scale, wq, w_scale, z, dy, need_x, need_bias):
+def _linear_backward(desc, x, x_scale, wq, w_scale, z, dy, need_x, need_bias):
     dy = dy.contiguous()
     dx = torch.empty(desc.M, desc.K, dtype=_BF16, device=dy.device) if need_x else None
     dw = torch.empty(desc.N, desc.K, device=dy.device)
     db = torch.empty(desc.N, device=dy.device) if need_bias else None
-    ws = mod.slots.get(("bwd", desc.M, dy.dtype), dense.fqt_linear_workspace_size(desc, True), dy.device)
+    ws = _workspace(dense.fqt_linear_workspace_size(desc, True), dy.device)
     dense.fqt_linear_backward(desc, x, wq, dy, ws, z=z, x_scale=x_scale, w_scale=w_scale, dx=dx, dw=dw,
                               dbias=db)
     return dx, dw, db
@@ -136,7 +122,7 @@ class _LinearFn(torch.autograd.Function):
         y, z, wq, w_scale, desc = _linear_forward(mod, xq, x_scale, w, bias, residual,
                                                   residual.dtype if residual is not None else x.dtype)
         ctx.save_for_backward(xq, x_scale, wq, w_scale, z)
-        ctx.desc, ctx.mod, ctx.x_dtype = desc, mod, x.dtype
+        ctx.desc, ctx.x_dtype = desc, x.dtype
         ctx.residual, ctx.bias = residual is not None, bias is not None
         return y
 
@@ -144,7 +130,7 @@ class _LinearFn(torch.autograd.Function):
     @once_differentiable
     def backward(ctx, dy):
         xq, x_scale, wq, w_scale, z = ctx.saved_tensors
-        dx, dw, db = _linear_backward(ctx, ctx.mod, ctx.desc, xq, x_scale, wq, w_scale, z, dy,
+        dx, dw, db = _linear_backward(ctx.desc, xq, x_scale, wq, w_scale, z, dy,
                                       ctx.needs_input_grad[0], ctx.bias)
         return (None if dx is None else dx.to(ctx.x_dtype)), (dy if ctx.residual else None), dw, db, None
 
@@ -160,7 +146,6 @@ class Linear(nn.Module):
         nn.init.kaiming_uniform_(self.weight, a=5 ** 0.5)
         self.bias = nn.Parameter(torch.zeros(fout)) if bias else None
         self.fin, self.fout, self.act, self.operands = fin, fout, act, operands
-        self.slots = _Slots()
 
     def forward(self, x, residual=None):
         r = None if residual is None else _rows(residual, self.fout, "residual")
@@ -188,7 +173,7 @@ class _NormLinearFn(torch.autograd.Function):
             dense.fqt_rmsnorm_forward(desc, x, g, q=n, scale=scale, **out)
         y, z, wq, w_scale, ldesc = _linear_forward(mod, n, scale, w, bias, None, mod.out_dtype)
         ctx.save_for_backward(h, g, rstd, n, scale, wq, w_scale, z)
-        ctx.descs, ctx.mod = (desc, ldesc), mod
+        ctx.descs = desc, ldesc
         ctx.residual, ctx.bias = residual is not None, bias is not None
         return (y, h) if ctx.residual else y
 
@@ -197,9 +182,9 @@ class _NormLinearFn(torch.autograd.Function):
     def backward(ctx, dy, dh=None):
         h, g, rstd, n, scale, wq, w_scale, z = ctx.saved_tensors
         desc, ldesc = ctx.descs
-        dn, dw, db = _linear_backward(ctx, ctx.mod, ldesc, n, scale, wq, w_scale, z, dy, True, ctx.bias)
+        dn, dw, db = _linear_backward(ldesc, n, scale, wq, w_scale, z, dy, True, ctx.bias)
         dx, dg = torch.empty_like(h), torch.empty_like(g)
-        ws = ctx.mod.slots.get(("norm", desc.rows), dense.fqt_norm_workspace_size(desc), h.device)
+        ws = _workspace(dense.fqt_norm_workspace_size(desc), h.device)
         dense.fqt_rmsnorm_backward(desc, h, g, rstd, dn, dx, dg, ws,
                                    dres=dh.contiguous() if ctx.residual else None)
         return dx, dx if ctx.residual else None, dg, dw, db, None
@@ -218,7 +203,6 @@ class NormLinear(nn.Module):
         self.bias = nn.Parameter(torch.zeros(fout)) if bias else None
         self.fin, self.fout, self.act, self.operands = fin, fout, act, operands
         self.eps, self.out_dtype = eps, out_dtype
-        self.slots = _Slots()
 
     def forward(self, x, residual=None):
         m = _rows(x, self.fin, "x")
@@ -244,7 +228,6 @@ class Muon(torch.optim.Optimizer):
             for p in group["params"]:
                 if p.dim() < 2 or p.dtype != _F32:
                     raise ValueError(f"Muon updates float32 matrices, got {p.dtype} {tuple(p.shape)}")
-        self._slots = _Slots()
 
     @torch.no_grad()
     def step(self, closure=None):
@@ -264,7 +247,7 @@ class Muon(torch.optim.Optimizer):
                 if "momentum" not in state:
                     state["momentum"] = torch.zeros_like(p)
                 desc = dense.ortho_desc(*w.shape, g_dtype=g.dtype, steps=group["steps"], eps=group["eps"])
-                ws = self._slots.get(tuple(w.shape), dense.fqt_ortho_workspace_size(desc), p.device)
+                ws = _workspace(dense.fqt_ortho_workspace_size(desc), p.device)
                 dense.fqt_muon_step(desc, w, g, state["momentum"].view_as(w), ws, lr=group["lr"],
                                     momentum=group["momentum"], weight_decay=group["weight_decay"],
                                     scale=math.sqrt(max(1.0, w.shape[0] / w.shape[1])),
