@@ -104,10 +104,11 @@ def _linear_forward(mod, x, x_scale, w, bias, residual, out_dtype):
     return y, z, wq, w_scale, desc
 
 
-def _linear_backward(desc, x, x_scale, wq, w_scale, z, dy, need_x, need_bias):
+def _linear_backward(desc, x, x_scale, wq, w_scale, z, dy, need_x, need_w, need_bias):
+    """The gradients that are needed, None for the others."""
     dy = dy.contiguous()
     dx = torch.empty(desc.M, desc.K, dtype=_BF16, device=dy.device) if need_x else None
-    dw = torch.empty(desc.N, desc.K, device=dy.device)
+    dw = torch.empty(desc.N, desc.K, device=dy.device) if need_w else None
     db = torch.empty(desc.N, device=dy.device) if need_bias else None
     ws = _workspace(dense.fqt_linear_workspace_size(desc, True), dy.device)
     dense.fqt_linear_backward(desc, x, wq, dy, ws, z=z, x_scale=x_scale, w_scale=w_scale, dx=dx, dw=dw,
@@ -123,15 +124,15 @@ class _LinearFn(torch.autograd.Function):
                                                   residual.dtype if residual is not None else x.dtype)
         ctx.save_for_backward(xq, x_scale, wq, w_scale, z)
         ctx.desc, ctx.x_dtype = desc, x.dtype
-        ctx.residual, ctx.bias = residual is not None, bias is not None
+        ctx.residual = residual is not None
         return y
 
     @staticmethod
     @once_differentiable
     def backward(ctx, dy):
         xq, x_scale, wq, w_scale, z = ctx.saved_tensors
-        dx, dw, db = _linear_backward(ctx.desc, xq, x_scale, wq, w_scale, z, dy,
-                                      ctx.needs_input_grad[0], ctx.bias)
+        need_x, _, need_w, need_bias, _ = ctx.needs_input_grad
+        dx, dw, db = _linear_backward(ctx.desc, xq, x_scale, wq, w_scale, z, dy, need_x, need_w, need_bias)
         return (None if dx is None else dx.to(ctx.x_dtype)), (dy if ctx.residual else None), dw, db, None
 
 
@@ -174,7 +175,7 @@ class _NormLinearFn(torch.autograd.Function):
         y, z, wq, w_scale, ldesc = _linear_forward(mod, n, scale, w, bias, None, mod.out_dtype)
         ctx.save_for_backward(h, g, rstd, n, scale, wq, w_scale, z)
         ctx.descs = desc, ldesc
-        ctx.residual, ctx.bias = residual is not None, bias is not None
+        ctx.residual = residual is not None
         return (y, h) if ctx.residual else y
 
     @staticmethod
@@ -182,7 +183,11 @@ class _NormLinearFn(torch.autograd.Function):
     def backward(ctx, dy, dh=None):
         h, g, rstd, n, scale, wq, w_scale, z = ctx.saved_tensors
         desc, ldesc = ctx.descs
-        dn, dw, db = _linear_backward(ldesc, n, scale, wq, w_scale, z, dy, True, ctx.bias)
+        need_w, need_bias = ctx.needs_input_grad[3:5]
+        need_norm = any(ctx.needs_input_grad[:3])
+        dn, dw, db = _linear_backward(ldesc, n, scale, wq, w_scale, z, dy, need_norm, need_w, need_bias)
+        if not need_norm:
+            return None, None, None, dw, db, None
         dx, dg = torch.empty_like(h), torch.empty_like(g)
         ws = _workspace(dense.fqt_norm_workspace_size(desc), h.device)
         dense.fqt_rmsnorm_backward(desc, h, g, rstd, dn, dx, dg, ws,
