@@ -7,7 +7,8 @@ them together with BinaryLinear: a float32 residual stream, blocks of a normed 8
 GELU and a binary projection, the first and last layers at full width as in the networks of `train`.
 
 Modules take [..., features] inputs of float32 or bfloat16, keep float32 parameters, and cast or
-quantize the weight in every forward pass.  Their backward cannot be differentiated again.
+quantize the weight in every forward pass.  Gradients come in the type of what they belong to (the products
+of the backward take dz in bf16, as fqt_linear_backward says) and cannot be differentiated again.
 """
 import math
 
@@ -90,12 +91,13 @@ def _quantized(w, kind):
     return q, scale
 
 
-def _linear_forward(mod, x, x_scale, w, bias, residual, out_dtype):
-    """y, the pre-activation (None without an activation), the operand form of w, and the descriptor."""
+def _linear_forward(mod, x, x_scale, w, bias, residual, out_dtype, stream_dtype):
+    """y, the pre-activation (None without an activation), the operand form of w, and the descriptor.
+    stream_dtype: the type of the module's input, which its gradient has."""
     (M, K), N = x.shape, w.shape[0]
     wq, w_scale = _quantized(w, mod.operands)
-    desc = dense.linear_desc(M, N, K, x_dtype=mod.operands, y_dtype=out_dtype, act=mod.act, dx_dtype=_BF16,
-                             dw_dtype=_F32)
+    desc = dense.linear_desc(M, N, K, x_dtype=mod.operands, y_dtype=out_dtype, act=mod.act,
+                             dx_dtype=stream_dtype, dw_dtype=_F32)
     y = torch.empty(M, N, dtype=out_dtype, device=x.device)
     z = torch.empty_like(y) if mod.act != "none" else None
     ws = _workspace(dense.fqt_linear_workspace_size(desc), x.device)
@@ -107,7 +109,7 @@ def _linear_forward(mod, x, x_scale, w, bias, residual, out_dtype):
 def _linear_backward(desc, x, x_scale, wq, w_scale, z, dy, need_x, need_w, need_bias):
     """The gradients that are needed, None for the others."""
     dy = dy.contiguous()
-    dx = torch.empty(desc.M, desc.K, dtype=_BF16, device=dy.device) if need_x else None
+    dx = torch.empty(desc.M, desc.K, dtype=dense._TORCH_OF[desc.dx_dtype], device=dy.device) if need_x else None
     dw = torch.empty(desc.N, desc.K, device=dy.device) if need_w else None
     db = torch.empty(desc.N, device=dy.device) if need_bias else None
     ws = _workspace(dense.fqt_linear_workspace_size(desc, True), dy.device)
@@ -121,10 +123,9 @@ class _LinearFn(torch.autograd.Function):
     def forward(ctx, x, residual, w, bias, mod):
         xq, x_scale = _quantized(x, mod.operands)
         y, z, wq, w_scale, desc = _linear_forward(mod, xq, x_scale, w, bias, residual,
-                                                  residual.dtype if residual is not None else x.dtype)
+                                                  residual.dtype if residual is not None else x.dtype, x.dtype)
         ctx.save_for_backward(xq, x_scale, wq, w_scale, z)
-        ctx.desc, ctx.x_dtype = desc, x.dtype
-        ctx.residual = residual is not None
+        ctx.desc, ctx.residual = desc, residual is not None
         return y
 
     @staticmethod
@@ -133,7 +134,7 @@ class _LinearFn(torch.autograd.Function):
         xq, x_scale, wq, w_scale, z = ctx.saved_tensors
         need_x, _, need_w, need_bias, _ = ctx.needs_input_grad
         dx, dw, db = _linear_backward(ctx.desc, xq, x_scale, wq, w_scale, z, dy, need_x, need_w, need_bias)
-        return (None if dx is None else dx.to(ctx.x_dtype)), (dy if ctx.residual else None), dw, db, None
+        return dx, (dy if ctx.residual else None), dw, db, None
 
 
 class Linear(nn.Module):
@@ -172,9 +173,10 @@ class _NormLinearFn(torch.autograd.Function):
             n = torch.empty(rows, cols, dtype=dense._TORCH_OF[dense.dtype_code(kind)], device=x.device)
             scale = torch.empty(rows, device=x.device)
             dense.fqt_rmsnorm_forward(desc, x, g, q=n, scale=scale, **out)
-        y, z, wq, w_scale, ldesc = _linear_forward(mod, n, scale, w, bias, None, mod.out_dtype)
+        y, z, wq, w_scale, ldesc = _linear_forward(mod, n, scale, w, bias, None, mod.out_dtype, x.dtype)
         ctx.save_for_backward(h, g, rstd, n, scale, wq, w_scale, z)
-        ctx.descs = desc, ldesc
+        # (the norm's own y is the product's operand; its gradient has the stream's type)
+        ctx.descs = dense.norm_desc(rows, cols, x_dtype=x.dtype, eps=mod.eps), ldesc
         ctx.residual = residual is not None
         return (y, h) if ctx.residual else y
 
