@@ -224,17 +224,31 @@ class NormLinear(nn.Module):
 class Muon(torch.optim.Optimizer):
     """Orthogonalised momentum for float32 weights of two or more dimensions (a convolution's is unfolded to
     [out][in kh kw]): m = momentum m + g, u = g + momentum m (nesterov) or m, w = (1 - lr weight_decay) w
-    - lr sqrt(max(1, rows / cols)) NS(u), one fqt_muon_step per weight."""
+    - lr sqrt(max(1, rows / cols)) NS(u), one fqt_muon_step per weight.  Weights of another memory order
+    (channels_last) are updated through a copy.  What cannot be updated is refused when its group is added."""
 
     def __init__(self, params, lr=0.02, momentum=0.95, weight_decay=0.0, nesterov=True, steps=5, eps=1e-7):
-        if lr < 0 or not 0 <= momentum < 1 or weight_decay < 0:
-            raise ValueError(f"lr {lr}, momentum {momentum}, weight_decay {weight_decay}: out of range")
         super().__init__(params, dict(lr=lr, momentum=momentum, weight_decay=weight_decay,
                                       nesterov=nesterov, steps=steps, eps=eps))
-        for group in self.param_groups:
+
+    def add_param_group(self, param_group):
+        super().add_param_group(param_group)
+        group = self.param_groups[-1]
+        try:
+            lr, momentum, weight_decay = group["lr"], group["momentum"], group["weight_decay"]
+            if lr < 0 or not 0 <= momentum < 1 or weight_decay < 0:
+                raise ValueError(f"lr {lr}, momentum {momentum}, weight_decay {weight_decay}: out of range")
             for p in group["params"]:
                 if p.dim() < 2 or p.dtype != _F32:
                     raise ValueError(f"Muon updates float32 matrices, got {p.dtype} {tuple(p.shape)}")
+                dense.fqt_ortho_workspace_size(self._desc(p, group))     # refuses sizes, steps and eps
+        except Exception:
+            self.param_groups.pop()
+            raise
+
+    @staticmethod
+    def _desc(p, group):
+        return dense.ortho_desc(p.shape[0], math.prod(p.shape[1:]), steps=group["steps"], eps=group["eps"])
 
     @torch.no_grad()
     def step(self, closure=None):
@@ -244,21 +258,23 @@ class Muon(torch.optim.Optimizer):
                 loss = closure()
         for group in self.param_groups:
             for p in group["params"]:
-                if p.grad is None:
+                if p.grad is None or p.numel() == 0:
                     continue
-                if not p.is_contiguous():
-                    raise ValueError("Muon updates contiguous weights in place")
-                w = p.view(p.shape[0], -1)
-                g = p.grad.reshape(p.shape[0], -1).contiguous()
                 state = self.state[p]
                 if "momentum" not in state:
                     state["momentum"] = torch.zeros_like(p)
-                desc = dense.ortho_desc(*w.shape, g_dtype=g.dtype, steps=group["steps"], eps=group["eps"])
-                ws = _workspace(dense.fqt_ortho_workspace_size(desc), p.device)
-                dense.fqt_muon_step(desc, w, g, state["momentum"].view_as(w), ws, lr=group["lr"],
-                                    momentum=group["momentum"], weight_decay=group["weight_decay"],
-                                    scale=math.sqrt(max(1.0, w.shape[0] / w.shape[1])),
+                desc, held = self._desc(p, group), (p, state["momentum"])
+                w, m = (t.contiguous() for t in held)
+                shape = desc.rows, desc.cols
+                dense.fqt_muon_step(desc, w.view(shape), p.grad.contiguous().view(shape), m.view(shape),
+                                    _workspace(dense.fqt_ortho_workspace_size(desc), p.device),
+                                    lr=group["lr"], momentum=group["momentum"],
+                                    weight_decay=group["weight_decay"],
+                                    scale=math.sqrt(max(1.0, desc.rows / desc.cols)),
                                     nesterov=group["nesterov"])
+                for t, dense_t in zip(held, (w, m)):
+                    if dense_t is not t:
+                        t.copy_(dense_t)
         return loss
 
 
