@@ -279,7 +279,8 @@ class Muon(torch.optim.Optimizer):
 
 
 class Optimizers:
-    """Several optimizers behind the interface that train.train_step uses."""
+    """Several optimizers behind the interface that train.train_step uses, with one checkpoint.  A scheduler
+    takes one of `optimizers`; param_groups has the groups of all."""
 
     def __init__(self, *optimizers):
         self.optimizers = optimizers
@@ -292,6 +293,20 @@ class Optimizers:
         for o in self.optimizers:
             o.step()
 
+    @property
+    def param_groups(self):
+        return [group for o in self.optimizers for group in o.param_groups]
+
+    def state_dict(self):
+        return {"optimizers": [o.state_dict() for o in self.optimizers]}
+
+    def load_state_dict(self, state):
+        states = state["optimizers"]
+        if len(states) != len(self.optimizers):
+            raise ValueError(f"a state of {len(states)} optimizers, there are {len(self.optimizers)}")
+        for o, s in zip(self.optimizers, states):
+            o.load_state_dict(s)
+
 
 def muon_and_adam(model, lr=0.02, adam_lr=1e-3, first_last=()):
     """Muon for the weight matrices of a model, Adam for its vectors and for the modules in first_last
@@ -300,7 +315,8 @@ def muon_and_adam(model, lr=0.02, adam_lr=1e-3, first_last=()):
     matrices = [p for p in model.parameters() if p.dim() >= 2 and id(p) not in apart]
     chosen = {id(p) for p in matrices}
     rest = [p for p in model.parameters() if id(p) not in chosen]
-    return Optimizers(Muon(matrices, lr=lr), torch.optim.Adam(rest, lr=adam_lr))
+    return Optimizers(*([Muon(matrices, lr=lr)] if matrices else []),
+                      *([torch.optim.Adam(rest, lr=adam_lr)] if rest else []))
 
 
 class ResidualMLP(nn.Module):

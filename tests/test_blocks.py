@@ -1,4 +1,6 @@
 """What the modules and the optimizer refuse before anything runs (no GPU needed)."""
+import copy
+
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -40,3 +42,40 @@ def test_muon_refuses_weights_when_added():
     with pytest.raises(ValueError, match="float32 matrices"):
         opt.add_param_group(dict(params=[weight(7)]))
     assert len(opt.param_groups) == 1
+
+
+def test_optimizers_checkpoint_and_schedule():
+    def make():
+        torch.manual_seed(0)
+        m = torch.nn.Sequential(torch.nn.Linear(4, 8), torch.nn.LayerNorm(8), torch.nn.Linear(8, 2))
+        o = blocks.Optimizers(torch.optim.SGD([m[0].weight, m[2].weight], lr=0.1, momentum=0.9),
+                              torch.optim.Adam([*m[0].parameters()][1:] + [*m[1].parameters()] + [m[2].bias]))
+        return m, o
+
+    def train(m, o, seeds):
+        for s in seeds:
+            o.zero_grad()
+            m(torch.randn(6, 4, generator=torch.Generator().manual_seed(s))).square().sum().backward()
+            o.step()
+
+    m, o = make()
+    assert [g["lr"] for g in o.param_groups] == [0.1, 1e-3]
+    o.param_groups[0]["lr"] = 0.05
+    torch.optim.lr_scheduler.StepLR(o.optimizers[1], 1)
+    train(m, o, range(3))
+    again, p = make()
+    again.load_state_dict(m.state_dict())
+    p.load_state_dict(copy.deepcopy(o.state_dict()))       # (torch keeps the tensors it is given)
+    assert p.param_groups[0]["lr"] == 0.05
+    train(m, o, range(3, 6))
+    train(again, p, range(3, 6))
+    assert all(torch.equal(a, b) for a, b in zip(m.parameters(), again.parameters()))
+    with pytest.raises(ValueError, match="a state of 1"):
+        p.load_state_dict({"optimizers": o.state_dict()["optimizers"][:1]})
+
+
+def test_models_without_matrices_or_without_vectors():
+    only = blocks.muon_and_adam(torch.nn.Linear(4, 8, bias=False))
+    assert [type(o) for o in only.optimizers] == [blocks.Muon]
+    vectors = blocks.muon_and_adam(torch.nn.LayerNorm(8))
+    assert [type(o) for o in vectors.optimizers] == [torch.optim.Adam]
