@@ -82,7 +82,8 @@ class RMSNorm(nn.Module):
 
 
 def _quantized(w, kind):
-    """Codes and scales of a weight's rows, or its bf16 copy."""
+    """Codes and scales of a matrix's rows, or its bf16 copy."""
+    w = w.contiguous()
     if kind == "bf16":
         return w.to(_BF16), None
     q = torch.empty(w.shape, dtype=dense._TORCH_OF[dense.dtype_code(kind)], device=w.device)
