@@ -341,5 +341,5 @@ class ResidualMLP(nn.Module):
             else:
                 z, h = up(add, h)
             add = down(nn.functional.hardtanh(z))
-        y, _ = self.norm(add, h)
+        y = self.norm(h) if add is None else self.norm(add, h)[0]
         return self.head(y)

@@ -1,4 +1,4 @@
-"""Modules at the ends of their ranges: no rows, one row, single vectors, more dimensions, weights that are
+"""Modules at the ends of their ranges: no rows, one row, single vectors, more dimensions, no blocks, weights that are
 views."""
 import pytest
 
@@ -48,7 +48,7 @@ def test_weight_that_is_a_view(operands):
     assert torch.equal(mod(x), twin(x)) and torch.equal(mod.weight.grad, twin.weight.grad)
 
 
-@pytest.mark.parametrize("depth", [1, 2])
+@pytest.mark.parametrize("depth", [0, 1, 2])
 def test_residual_network_of_any_depth(depth):
     from paper_2408_14267_amd import blocks as b
     net = b.ResidualMLP(20, 5, width=32, hidden=64, depth=depth).cuda()
@@ -56,3 +56,5 @@ def test_residual_network_of_any_depth(depth):
     y = net(x)
     y.square().mean().backward()
     assert y.shape == (16, 5) and all(torch.isfinite(p.grad).all() for p in net.parameters())
+    if depth == 0:
+        assert torch.equal(y, net.head(net.norm(net.stem(x))))
