@@ -101,7 +101,7 @@ __device__ __forceinline__ void store8f(T *p, int n, const float (&v)[8]) {
 // Largest code of an 8-bit type.
 __host__ __device__ constexpr float code_top(int q_dtype) { return q_dtype == FQT_I8 ? 127.0f : 448.0f; }
 // The code of v (already divided by its scale), rounded to nearest even, as its byte.  The clamp
-// takes the last rounding of v past the top; a NaN becomes the top (its row's scale is NaN).
+// takes the last rounding of v past the top; a NaN becomes the lowest code (its row's scale is NaN).
 __device__ __forceinline__ uint32_t code_i8(float v) {
   return uint32_t(int(rintf(fminf(fmaxf(v, -127.0f), 127.0f)))) & 0xFFu;
 }

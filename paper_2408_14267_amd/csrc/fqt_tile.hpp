@@ -549,7 +549,9 @@ struct Plan {
 
 // us a step of a workgroup with one, two or three of them on a CU, and us before the first and after the last
 // step with Large, Middle and Small tiles: measured on bf16 operands, on pairs as PANEL_ROWS x PANEL_COLS
-// (512 and 1024 rows) and on symmetric products of pairs (512 to 4096 rows).
+// (512 and 1024 rows) and on symmetric products of pairs (512 to 4096 rows).  8-bit operands and the backward's
+// layouts are planned with the bf16 costs, not measured apart: a step is the same bytes, but 8-bit matrix
+// instructions run faster and reads across the contraction slower (6 to 11 %).
 struct Costs { double large[1], middle[2], small[3], start[3]; };
 constexpr Costs DENSE_COSTS{{1.58}, {0.60, 0.90}, {0.25, 0.40, 0.58}, {6, 5, 4}},
     PAIR_COSTS{{2.0}, {0.81, 1.26}, {0.28, 0.39, 0.62}, {18, 8, 5}},
