@@ -226,7 +226,8 @@ class Muon(torch.optim.Optimizer):
     """Orthogonalised momentum for float32 weights of two or more dimensions (a convolution's is unfolded to
     [out][in kh kw]): m = momentum m + g, u = g + momentum m (nesterov) or m, w = (1 - lr weight_decay) w
     - lr sqrt(max(1, rows / cols)) NS(u), one fqt_muon_step per weight.  Weights of another memory order
-    (channels_last) are updated through a copy.  What cannot be updated is refused when its group is added."""
+    (channels_last) are updated through a copy.  What cannot be updated is refused when its group is added or,
+    where it has changed since, before a step updates anything."""
 
     def __init__(self, params, lr=0.02, momentum=0.95, weight_decay=0.0, nesterov=True, steps=5, eps=1e-7):
         super().__init__(params, dict(lr=lr, momentum=momentum, weight_decay=weight_decay,
@@ -236,9 +237,7 @@ class Muon(torch.optim.Optimizer):
         super().add_param_group(param_group)
         group = self.param_groups[-1]
         try:
-            lr, momentum, weight_decay = group["lr"], group["momentum"], group["weight_decay"]
-            if lr < 0 or not 0 <= momentum < 1 or weight_decay < 0:
-                raise ValueError(f"lr {lr}, momentum {momentum}, weight_decay {weight_decay}: out of range")
+            self._check_rates(group)
             for p in group["params"]:
                 if p.dim() < 2 or p.dtype != _F32:
                     raise ValueError(f"Muon updates float32 matrices, got {p.dtype} {tuple(p.shape)}")
@@ -246,6 +245,12 @@ class Muon(torch.optim.Optimizer):
         except Exception:
             self.param_groups.pop()
             raise
+
+    @staticmethod
+    def _check_rates(group):
+        lr, momentum, weight_decay = group["lr"], group["momentum"], group["weight_decay"]
+        if not (0 <= lr < math.inf and 0 <= momentum < 1 and 0 <= weight_decay < math.inf):
+            raise ValueError(f"lr {lr}, momentum {momentum}, weight_decay {weight_decay}: out of range")
 
     @staticmethod
     def _desc(p, group):
@@ -257,25 +262,32 @@ class Muon(torch.optim.Optimizer):
         if closure is not None:
             with torch.enable_grad():
                 loss = closure()
+        todo = []
         for group in self.param_groups:
+            self._check_rates(group)
             for p in group["params"]:
                 if p.grad is None or p.numel() == 0:
                     continue
-                state = self.state[p]
-                if "momentum" not in state:
-                    state["momentum"] = torch.zeros_like(p)
-                desc, held = self._desc(p, group), (p, state["momentum"])
-                w, m = (t.contiguous() for t in held)
-                shape = desc.rows, desc.cols
-                dense.fqt_muon_step(desc, w.view(shape), p.grad.contiguous().view(shape), m.view(shape),
-                                    _workspace(dense.fqt_ortho_workspace_size(desc), p.device),
-                                    lr=group["lr"], momentum=group["momentum"],
-                                    weight_decay=group["weight_decay"],
-                                    scale=math.sqrt(max(1.0, desc.rows / desc.cols)),
-                                    nesterov=group["nesterov"])
-                for t, dense_t in zip(held, (w, m)):
-                    if dense_t is not t:
-                        t.copy_(dense_t)
+                if p.grad.layout != torch.strided or p.device.type != "cuda" or \
+                        p.device.index != torch.cuda.current_device():
+                    raise ValueError(f"Muon updates weights with dense gradients on the current device, got "
+                                     f"{p.grad.layout} on {p.device}")
+                desc = self._desc(p, group)
+                todo.append((group, p, desc, dense.fqt_ortho_workspace_size(desc)))
+        for group, p, desc, size in todo:
+            state = self.state[p]
+            if "momentum" not in state:
+                state["momentum"] = torch.zeros_like(p)
+            held = p, state["momentum"]
+            w, m = (t.contiguous() for t in held)
+            shape = desc.rows, desc.cols
+            dense.fqt_muon_step(desc, w.view(shape), p.grad.contiguous().view(shape), m.view(shape),
+                                _workspace(size, p.device), lr=group["lr"], momentum=group["momentum"],
+                                weight_decay=group["weight_decay"],
+                                scale=math.sqrt(max(1.0, desc.rows / desc.cols)), nesterov=group["nesterov"])
+            for t, dense_t in zip(held, (w, m)):
+                if dense_t is not t:
+                    t.copy_(dense_t)
         return loss
 
 
