@@ -10,7 +10,8 @@ CSRC = os.path.join(PKG, "csrc")
 BUILD = os.path.join(PKG, "_build")
 LIB = os.path.join(PKG, "libfqt.so")
 SOURCES = ["fqt_api.hip", "fqt_quantize.hip", "fqt_pack.hip", "fqt_gemm.hip", "fqt_taps.hip",
-           "fqt_forward.hip", "fqt_engines.hip", "fqt_norm.hip", "fqt_linear.hip", "fqt_ortho.hip"]
+           "fqt_forward.hip", "fqt_engines.hip", "fqt_norm.hip", "fqt_linear.hip", "fqt_ortho.hip",
+           "fqt_loss.hip", "fqt_params.hip"]
 
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 FLAGS = [

@@ -9,7 +9,7 @@
 // The backward is one pass over dy (and z) that writes dz = dy act'(z) in bf16 and sums dbias, then
 // the two products, which read dz and the operands as they are stored: dx = dz w reads w along n
 // (COLS), dw = dz^T x reads both operands along m.
-#include "fqt_tile.hpp"
+#include "fqt_product.hpp"
 
 namespace fqt {
 namespace dense {
@@ -98,6 +98,7 @@ struct Epilogue {
   void *z, *y;
   int64_t M, N, ldr, ldz, ldy;
   int32_t y_dtype, act;
+  int32_t r_dtype;         // of the residual
 };
 
 // Loads or stores of 8 elements whose type is known at run time (uniform).
@@ -139,7 +140,7 @@ struct Finish {
     if (e.sx) f.sx = e.sx[m];
     if (e.res) {
       const int64_t at = m * e.ldr + n;
-      if (e.y_dtype == FQT_BF16) {
+      if (e.r_dtype == FQT_BF16) {
         const bf16 *p = static_cast<const bf16 *>(e.res) + at;
         if (cnt == 8) {
           const u32x4 u = load_bytes16(p);
@@ -182,10 +183,11 @@ struct Finish {
       for (int i = 0; i < 8; ++i) v[i] = activate<ACT, true>(v[i]);
     }
     if (e.res) {
+      const bool pairs = e.r_dtype == FQT_BF16;
 #pragma unroll
       for (int i = 0; i < 8; ++i) {
         const uint32_t two = f.res[i / 2];
-        v[i] += __uint_as_float(half ? (i & 1 ? two & 0xFFFF0000u : two << 16) : f.res[i]);
+        v[i] += __uint_as_float(pairs ? (i & 1 ? two & 0xFFFF0000u : two << 16) : f.res[i]);
       }
     }
     store8(e.y, m * e.ldy + n, e.y_dtype, cnt, v);
@@ -402,12 +404,6 @@ template <> __device__ __forceinline__ bf16 widen<int8_t, bf16>(int8_t v) { retu
 template <> __device__ __forceinline__ bf16 widen<e4m3, bf16>(e4m3 v) {
   return from_f32<bf16>(__builtin_amdgcn_cvt_f32_fp8(int(v.v), 0));
 }
-struct Copy {
-  const void *src;
-  void *dst;
-  int64_t rows, cols, ld, pitch;
-  uint32_t blocks;         // workgroups of 256 threads (0: no copy)
-};
 template <typename ST, typename DT>
 __device__ __forceinline__ void repack_rows(const Copy &a, uint32_t block) {
   constexpr int V = 16 / sizeof(DT);
@@ -505,12 +501,6 @@ __global__ void __launch_bounds__(256) k_prepare(DzArgs a, Copy x, Copy w) {
 }
 
 // dbias[n] = sum of the partial rows: 32 columns per workgroup, 8 threads per column, fixed order.
-struct DbiasArgs {
-  const float *part;
-  float *dbias;            // or null
-  int64_t N;
-  int32_t parts;
-};
 __device__ __forceinline__ void sum_dbias(const DbiasArgs &a, uint32_t block, float (*s)[32]) {
   const int64_t c = int64_t(block) * 32 + threadIdx.x % 32;
   const int k = threadIdx.x / 32;
@@ -582,9 +572,7 @@ int check_linear(const fqt_linear_desc *d, Sizes *s) {
   return FQT_OK;
 }
 
-int64_t round_up(int64_t v, int64_t q) { return (v + q - 1) / q * q; }
-// Whether rows of n elements, ld apart, are whole 16-byte pieces.
-bool whole_pieces(int64_t n, int64_t ld, size_t e) { return n * e % 16 == 0 && ld * e % 16 == 0; }
+}  // namespace
 
 tile::Plan plan_of(int64_t M, int64_t N, int64_t K, size_t e) {
   return tile::make_plan(M, N, (K * int64_t(e) + tile::KB - 1) / tile::KB, false, tile::DENSE_COSTS);
@@ -592,6 +580,8 @@ tile::Plan plan_of(int64_t M, int64_t N, int64_t K, size_t e) {
 size_t part_bytes(const tile::Plan &p, int64_t M, int64_t N) {
   return p.splits > 1 ? align256(size_t(p.splits) * M * round_up(N, 8) * 4) : 0;
 }
+
+namespace {
 
 Epilogue sized(Epilogue e, int64_t M, int64_t N) {
   e.M = M;
@@ -632,11 +622,24 @@ int launch_few(const FewArgs &a, const Epilogue &e, hipStream_t st) {
   return last_launch_status();
 }
 
-// The copy of an operand into rows of `pitch` elements of e bytes.
+}  // namespace
+
 Copy copy_of(const void *src, int64_t rows, int64_t cols, int64_t ld, void *dst, int64_t pitch, int64_t e) {
   const int64_t all = rows * (pitch * e / 16);
   return {src, dst, rows, cols, ld, pitch, uint32_t(std::min<int64_t>((all + 255) / 256, 4096))};
 }
+
+int launch_copies(const Copy &x, const Copy &w, int32_t dtype, bool widen, hipStream_t st) {
+  const dim3 grid(x.blocks + w.blocks), block(256);
+  if (grid.x == 0) return FQT_OK;
+  if (dtype == FQT_BF16) k_repack<bf16, bf16><<<grid, block, 0, st>>>(x, w);
+  else if (!widen) k_repack<int8_t, int8_t><<<grid, block, 0, st>>>(x, w);
+  else if (dtype == FQT_I8) k_repack<int8_t, bf16><<<grid, block, 0, st>>>(x, w);
+  else k_repack<e4m3, bf16><<<grid, block, 0, st>>>(x, w);
+  return last_launch_status();
+}
+
+namespace {
 
 // Workspace of the forward: padded copies of operands whose rows are not whole 16-byte pieces, and
 // the partial sums of a split contraction.
@@ -686,6 +689,8 @@ BwdWs bwd_ws(const Sizes &s) {
   return f;
 }
 
+}  // namespace
+
 int zero_matrix(void *p, int64_t rows, int64_t cols, int64_t ld, size_t e, hipStream_t st) {
   if (rows == 0 || cols == 0) return FQT_OK;
   k_zero<<<dim3(std::min<int64_t>((rows * cols * int64_t(e) + 255) / 256, 4096)), dim3(256), 0, st>>>(
@@ -693,7 +698,27 @@ int zero_matrix(void *p, int64_t rows, int64_t cols, int64_t ld, size_t e, hipSt
   return last_launch_status();
 }
 
-}  // namespace
+int launch_gradients(const Gradients &g, hipStream_t st) {
+  const uint32_t bias_blocks = g.bias.dbias ? uint32_t((g.N + 31) / 32) : 0;
+  const Epilogue ex{nullptr, nullptr, nullptr, g.add, nullptr, g.dx, 0, 0, g.ldadd, 0, g.lddx, g.dx_dtype, FQT_ACT_NONE, FQT_F32};
+  const Epilogue ew{nullptr, nullptr, nullptr, nullptr, nullptr, g.dw, 0, 0, 0, 0, g.lddw, g.dw_dtype, FQT_ACT_NONE, FQT_F32};
+  auto small = [](const tile::Plan &p) { return p.shape[0] == tile::SMALL && p.launches == 1 && p.splits == 1; };
+  if (g.dx && g.dw && g.K && small(g.plan_dx) && small(g.plan_dw)) {
+    const Product px{g.dzx, g.w, g.M, g.K, g.N, g.plan_dx.t[0], nullptr, 0}, pw{g.dzw, g.x, g.N, g.K, g.M, g.plan_dw.t[0], nullptr, 0};
+    k_product_pair<<<dim3(px.tiles.count + pw.tiles.count + bias_blocks), dim3(tile::Small::THREADS), 0, st>>>(
+        px, sized(ex, g.M, g.K), pw, sized(ew, g.N, g.K), g.bias);
+    return last_launch_status();
+  }
+  if (g.bias.dbias) {
+    k_dbias<<<dim3(bias_blocks), dim3(256), 0, st>>>(g.bias);
+    FQT_TRY_(last_launch_status());
+  }
+  if (g.K == 0) return FQT_OK;
+  if (g.dx) FQT_TRY_((launch_product<tile::BF16K, ROWS, COLS>(g.plan_dx, g.dzx, g.w, g.M, g.K, g.N, ex, g.part, st)));
+  if (g.dw) FQT_TRY_((launch_product<tile::BF16K, COLS, COLS>(g.plan_dw, g.dzw, g.x, g.N, g.K, g.M, ew, g.part, st)));
+  return FQT_OK;
+}
+
 }  // namespace dense
 }  // namespace fqt
 
@@ -737,7 +762,7 @@ extern "C" int fqt_linear_forward(const fqt_linear_desc *d, const void *x, const
   const FwdWs f = fwd_ws(*d, s);
   if (ws_bytes < f.total) return FQT_E_WORKSPACE;
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  Epilogue e{x_scale, w_scale, bias, residual, z, y, s.M, s.N, s.ldr, s.ldz, s.ldy, d->y_dtype, d->act};
+  Epilogue e{x_scale, w_scale, bias, residual, z, y, s.M, s.N, s.ldr, s.ldz, s.ldy, d->y_dtype, d->act, d->y_dtype};
   if (s.M <= FEW_MOST) {
     const FewArgs a{x, w, s.K, s.ldx, s.ldw};
     if (d->x_dtype == FQT_BF16) return launch_few<bf16>(a, e, st);
@@ -751,12 +776,7 @@ extern "C" int fqt_linear_forward(const fqt_linear_desc *d, const void *x, const
   };
   Copy cx{}, cw{};
   const Operand xo = operand(x, f.copy_x, f.x, s.M, s.ldx, &cx), wo = operand(w, f.copy_w, f.w, s.N, s.ldw, &cw);
-  if (const dim3 grid(cx.blocks + cw.blocks); grid.x) {
-    if (f.widen) k_repack<e4m3, bf16><<<grid, dim3(256), 0, st>>>(cx, cw);
-    else if (codes) k_repack<int8_t, int8_t><<<grid, dim3(256), 0, st>>>(cx, cw);
-    else k_repack<bf16, bf16><<<grid, dim3(256), 0, st>>>(cx, cw);
-    FQT_TRY_(last_launch_status());
-  }
+  FQT_TRY_(launch_copies(cx, cw, d->x_dtype, f.widen, st));
   const int64_t K = f.copy_x || f.copy_w ? f.pitch : s.K;
   float *part = reinterpret_cast<float *>(base + f.part);
   if (d->x_dtype == FQT_BF16 || f.widen)
@@ -825,27 +845,17 @@ extern "C" int fqt_linear_backward(const fqt_linear_desc *d, const void *x, cons
     else k_prepare<bf16><<<grid, dim3(256), 0, st>>>(a, cx, cw);
     FQT_TRY_(last_launch_status());
   }
-  const DbiasArgs bias{a.part, dbias, s.N, int32_t(f.rows)};
-  const uint32_t bias_blocks = dbias ? uint32_t((s.N + 31) / 32) : 0;
-  float *part = reinterpret_cast<float *>(base + f.part);
   // dz rows are dz_pitch long in the workspace, zeros past N, so a contraction over n may end on a whole
   // piece; as a COLS operand dz has whole pieces of 8 columns.
   dzw.rows = same ? s.N : f.dz_pitch;
-  const Epilogue ex{nullptr, nullptr, nullptr, nullptr, nullptr, dx, 0, 0, 0, 0, s.lddx, d->dx_dtype, FQT_ACT_NONE};
-  const Epilogue ew{nullptr, nullptr, nullptr, nullptr, nullptr, dw, 0, 0, 0, 0, s.lddw, d->dw_dtype, FQT_ACT_NONE};
-  auto small = [](const tile::Plan &p) { return p.shape[0] == tile::SMALL && p.launches == 1 && p.splits == 1; };
-  if (dx && dw && s.K && small(f.dx) && small(f.dw)) {
-    const Product px{dzx, wo, s.M, s.K, s.N, f.dx.t[0], nullptr, 0}, pw{dzw, xo, s.N, s.K, s.M, f.dw.t[0], nullptr, 0};
-    k_product_pair<<<dim3(px.tiles.count + pw.tiles.count + bias_blocks), dim3(tile::Small::THREADS), 0, st>>>(
-        px, sized(ex, s.M, s.K), pw, sized(ew, s.N, s.K), bias);
-    return last_launch_status();
-  }
-  if (dbias) {
-    k_dbias<<<dim3(bias_blocks), dim3(256), 0, st>>>(bias);
-    FQT_TRY_(last_launch_status());
-  }
-  if (s.K == 0) return FQT_OK;
-  if (dx) FQT_TRY_((launch_product<tile::BF16K, ROWS, COLS>(f.dx, dzx, wo, s.M, s.K, s.N, ex, part, st)));
-  if (dw) FQT_TRY_((launch_product<tile::BF16K, COLS, COLS>(f.dw, dzw, xo, s.N, s.K, s.M, ew, part, st)));
-  return FQT_OK;
+  Gradients g{};
+  g.M = s.M; g.N = s.N; g.K = s.K;
+  g.dzx = dzx; g.dzw = dzw; g.w = wo; g.x = xo;
+  g.plan_dx = f.dx; g.plan_dw = f.dw;
+  g.dx = dx; g.dw = dw;
+  g.lddx = s.lddx; g.lddw = s.lddw;
+  g.dx_dtype = d->dx_dtype; g.dw_dtype = d->dw_dtype;
+  g.part = reinterpret_cast<float *>(base + f.part);
+  g.bias = {a.part, dbias, s.N, int32_t(f.rows)};
+  return launch_gradients(g, st);
 }

@@ -1,0 +1,704 @@
+// Softmax cross entropy of a linear layer's outputs without keeping them, and its gradients.
+//
+// The forward is the product's tiles (fqt_tile.hpp) with an epilogue that takes each row of a wave's 64
+// columns down to a pair (largest z, sum of the exponentials of the others over it); a second launch joins
+// the pairs of a row.  8 bytes for 64 columns touch memory instead of 256.  The backward computes z again
+// piece by piece of the classes, writes dz of a piece in bf16, and multiplies it into dx and dw
+// (fqt_linear.hip's products) while it is still in the last-level cache.  All of it is bound by the matrix cores on
+// large batches, by reading w on small ones.
+#include "fqt_product.hpp"
+#include "fqt_step.h"
+
+namespace fqt {
+namespace dense {
+namespace {
+
+#pragma clang fp contract(fast)
+
+using tile::Operand;
+using tile::ROWS;
+
+constexpr float LOG2E = 1.44269504088896341f;
+__device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * LOG2E); }
+// (NaN if either is one)
+__device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
+__device__ __forceinline__ float smaller(float a, float b) { return __builtin_elementwise_minimum(a, b); }
+
+// A set of z: its largest, and the sum of exp(z - top) over all others.  The largest's own 1 is left out, so
+// that a loss near 0, the sum of the others, keeps its precision.
+struct Soft {
+  float top, rest;
+};
+constexpr float NOTHING = -__builtin_inff();
+// What is subtracted: classes may all be out (minus infinity).
+__device__ __forceinline__ float base_of(float top) { return top == NOTHING ? 0.0f : top; }
+__device__ __forceinline__ Soft join(Soft a, Soft b) {
+  const float hi = larger(a.top, b.top), e = exp_of(smaller(a.top, b.top) - base_of(hi));
+  const bool first = a.top >= b.top;
+  return {hi, fmaf((first ? b.rest : a.rest) + 1.0f, e, first ? a.rest : b.rest)};
+}
+template <int X>
+__device__ __forceinline__ Soft join_lanes(Soft a) {
+  return join(a, Soft{lane_xor_f<X>(a.top), lane_xor_f<X>(a.rest)});
+}
+// N values: a pass of min and max leaves the largest and the others.
+template <int N>
+__device__ __forceinline__ Soft soft_of(const float (&v)[N]) {
+  float top = v[0], low[N];
+#pragma unroll
+  for (int i = 1; i < N; ++i) {
+    low[i] = smaller(top, v[i]);
+    top = larger(top, v[i]);
+  }
+  const float base = base_of(top);
+  float s[2] = {0.0f, 0.0f};
+#pragma unroll
+  for (int i = 1; i < N; ++i) s[i % 2] += exp_of(low[i] - base);
+  return {top, s[0] + s[1]};
+}
+
+struct Out {
+  const int64_t *target;
+  float *loss, *lse;
+  int64_t M, N, ignore;
+  float smoothing;
+};
+// Row m from its pair, the sum of its z and the target's z.
+__device__ __forceinline__ void finish_row(const Out &o, int64_t m, Soft s, float sum, float at) {
+  const float rest = log1pf(s.rest);
+  o.lse[m] = s.top + rest;
+  const int64_t t = o.target[m];
+  float loss = s.top - at;
+  if (o.smoothing > 0.0f) loss = (1.0f - o.smoothing) * loss + o.smoothing * (s.top - sum / float(o.N));
+  loss += rest;
+  o.loss[m] = t == o.ignore ? 0.0f : t < 0 || t >= o.N ? __builtin_nanf("") : loss;
+}
+
+// ----------------------------------------------------------------------------- forward by tiles
+
+struct Logits {
+  Operand x, w;
+  int64_t M, N, K;
+  tile::Tiles tiles;
+  const float *sx, *sw, *bias;
+  float *part;             // [splits][M][ldp] partial sums (splits > 1)
+  int64_t ldp;
+};
+constexpr int SLOT = 64;   // columns of a pair
+struct Pairs {
+  Soft *pairs;             // [ceil(N / SLOT)][M]
+  float *sums;             // the same of z, or null
+  float *at;               // [M] the target's z
+  const int64_t *target;
+};
+
+// The pairs of a tile, straight from the accumulators: lane l has row l % 16 of each 16 x 16 result and four
+// columns from 4 (l / 16), so a row's 64 columns are in four lanes, 16 each.
+template <int KIND, typename S>
+__device__ __forceinline__ void store_pairs(const Logits &p, const Pairs &o, const tile::Place &at,
+                                            const typename tile::Acc<KIND>::type (&acc)[S::FM][S::FN], char *lds) {
+  constexpr int PER = S::FN * 4;
+  const uint32_t wave = wave_id(), l = __lane_id(), q = l / 16;
+  const int64_t m0 = at.m0 + (wave / S::WN) * S::TM, n0 = at.n0 + (wave % S::WN) * S::TN;
+  const int64_t col = n0 + 4 * q;
+  // columns past the last are out
+  float bias[PER], sw[PER];
+#pragma unroll
+  for (int j = 0; j < S::FN; ++j)
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const int64_t n = col + 16 * j + i;
+      bias[4 * j + i] = n >= p.N ? NOTHING : p.bias ? p.bias[n] : 0.0f;
+      sw[4 * j + i] = p.sw && n < p.N ? p.sw[n] : 1.0f;
+    }
+  int where[S::FM];        // the target's place among the wave's columns
+#pragma unroll
+  for (int k = 0; k < S::FM; ++k) {
+    const int64_t m = m0 + k * 16 + l % 16;
+    const int64_t t = m < p.M ? o.target[m] - n0 : -1;
+    where[k] = t >= 0 && t < S::TN && t < p.N - n0 ? int(t) : -1;
+  }
+  Soft held{};
+  float held_sum = 0.0f;
+#pragma unroll
+  for (int k = 0; k < S::FM; ++k) {
+    const int64_t m = m0 + k * 16 + l % 16;
+    const float sx = p.sx ? p.sx[min(m, p.M - 1)] : 1.0f;
+    float v[PER];
+#pragma unroll
+    for (int j = 0; j < S::FN; ++j)
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        float z = float(acc[k][j][i]);
+        if (p.sx) z = z * sx * sw[4 * j + i];
+        v[4 * j + i] = z + bias[4 * j + i];
+      }
+    if (const bool mine = where[k] >= 0 && uint32_t(where[k] / 4 % 4) == q; __any(mine)) {
+      const int i = where[k] / 16 * 4 + where[k] % 4;
+      float z = v[0];
+#pragma unroll
+      for (int j = 1; j < PER; ++j) z = i == j ? v[j] : z;
+      if (mine) o.at[m] = z;
+    }
+    Soft s = join_lanes<32>(join_lanes<16>(soft_of<PER>(v)));
+    float sum = 0.0f;
+    if (o.sums) {
+#pragma unroll
+      for (int j = 0; j < PER; ++j) sum += col + 16 * (j / 4) + j % 4 < p.N ? v[j] : 0.0f;
+      sum += lane_xor_f<16>(sum);
+      sum += lane_xor_f<32>(sum);
+    }
+    if constexpr (S::TN == SLOT) {
+      // each quarter of the lanes keeps one of four results, so that a store takes 64 rows
+      if (k % 4 == int(q)) held = s, held_sum = sum;
+      if (k % 4 == 3) {
+        const int64_t r = m0 + (k / 4) * 64 + l;
+        if (r < p.M && n0 < p.N) {
+          o.pairs[n0 / SLOT * p.M + r] = held;
+          if (o.sums) o.sums[n0 / SLOT * p.M + r] = held_sum;
+        }
+      }
+    } else {
+      static_assert(S::TN * 2 == SLOT && S::WN == 2 && S::BN == SLOT, "two waves make a slot");
+      float4 *both = reinterpret_cast<float4 *>(lds);      // [2][BM]
+      if (q == 0) both[wave % 2 * S::BM + (wave / 2) * S::TM + k * 16 + l] = make_float4(s.top, s.rest, sum, 0.0f);
+    }
+  }
+  if constexpr (S::TN != SLOT) {
+    const float4 *both = reinterpret_cast<const float4 *>(lds);
+    __syncthreads();
+    const int64_t r = at.m0 + threadIdx.x;
+    if (threadIdx.x < S::BM && r < p.M) {
+      const float4 a = both[threadIdx.x], b = both[S::BM + threadIdx.x];
+      o.pairs[at.n0 / SLOT * p.M + r] = join(Soft{a.x, a.y}, Soft{b.x, b.y});
+      if (o.sums) o.sums[at.n0 / SLOT * p.M + r] = a.z + b.z;
+    }
+  }
+}
+
+template <int KIND, int SHAPE>
+__global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_loss_tiles(Logits p, Pairs o) {
+  typedef typename tile::ShapeOf<SHAPE>::type S;
+  __shared__ __attribute__((aligned(16))) char lds[S::LDS];
+  const tile::Place at = tile::place<SHAPE>(p.tiles, blockIdx.x);
+  if (at.m0 >= p.M || at.n0 >= p.N) return;              // (parts of an edge tile)
+  typename tile::Acc<KIND>::type acc[S::FM][S::FN];
+  tile::contract<KIND, ROWS, ROWS, SHAPE, S>(p.x, p.w, p.K, at, p.tiles, lds, acc);
+  if (p.tiles.splits > 1)
+    tile::run_epilogue<KIND, S>(acc, lds, at.m0, at.n0, tile::StorePart{p.part + at.split * p.M * p.ldp, p.M, p.ldp});
+  else
+    store_pairs<KIND, S>(p, o, at, acc, lds);
+}
+
+// Joins the pairs of 16 rows by 16 threads each, which take every 16th slot.
+__global__ void __launch_bounds__(256) k_loss_rows(Pairs p, Out o) {
+  constexpr int AHEAD = 8;
+  __shared__ float4 all[16][17];
+  const int r = threadIdx.x % 16, g = threadIdx.x / 16;
+  const int64_t m = int64_t(blockIdx.x) * 16 + r, slots = (o.N + SLOT - 1) / SLOT;
+  Soft s{NOTHING, 0.0f};
+  float sum = 0.0f;
+  if (m < o.M)
+    for (int64_t i0 = g; i0 < slots; i0 += 16 * AHEAD) {
+      Soft t[AHEAD];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i)
+        t[i] = i0 + 16 * i < slots ? p.pairs[(i0 + 16 * i) * o.M + m] : Soft{NOTHING, 0.0f};
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) s = join(s, t[i]);
+      if (p.sums)
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) sum += i0 + 16 * i < slots ? p.sums[(i0 + 16 * i) * o.M + m] : 0.0f;
+    }
+  all[g][r] = make_float4(s.top, s.rest, sum, 0.0f);
+  __syncthreads();
+  if (g || m >= o.M) return;
+#pragma unroll
+  for (int i = 1; i < 16; ++i) {
+    const float4 b = all[i][r];
+    s = join(s, Soft{b.x, b.y});
+    sum += b.z;
+  }
+  const int64_t t = p.target[m];
+  finish_row(o, m, s, sum, t >= 0 && t < o.N ? p.at[m] : 0.0f);
+}
+
+// ----------------------------------------------------------------------------- forward by rows
+// Where z passes through the workspace (few rows, or a split contraction): a workgroup takes a row, whose z
+// are sums of `splits` words.
+struct RowArgs {
+  const float *part;
+  const float *sx, *sw, *bias;
+  int64_t ldp;
+  uint32_t splits;
+};
+constexpr int ROW_THREADS = 1024;
+template <bool INTS>
+__global__ void __launch_bounds__(ROW_THREADS) k_loss_dense(RowArgs a, Out o) {
+  __shared__ float4 waves[ROW_THREADS / 64];
+  __shared__ float found;
+  const int64_t m = blockIdx.x, t = o.target[m];
+  const float sx = a.sx ? a.sx[m] : 1.0f;
+  if (threadIdx.x == 0) found = 0.0f;
+  __syncthreads();
+  Soft s{NOTHING, 0.0f};
+  float sum = 0.0f;
+#pragma unroll 4
+  for (int64_t n = int64_t(threadIdx.x) * 4; n < o.N; n += int64_t(blockDim.x) * 4) {
+    const int cnt = int(min(o.N - n, int64_t(4)));
+    std::conditional_t<INTS, int, float> w[4] = {};
+    for (uint32_t p = 0; p < a.splits; ++p) {
+      const float *at = a.part + (p * o.M + m) * a.ldp + n;
+      uint32_t u[4] = {};
+      if (cnt == 4) {
+        const u32x4 q = load_bytes16(at);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) u[i] = q[i];
+      } else {
+#pragma unroll
+        for (int i = 0; i < 3; ++i)
+          if (i < cnt) u[i] = __float_as_uint(at[i]);
+      }
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        if constexpr (INTS) w[i] += int(u[i]);
+        else w[i] += __uint_as_float(u[i]);
+      }
+    }
+    float v[4];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      v[i] = float(w[i]);
+      if (i >= cnt) {
+        v[i] = NOTHING;
+        continue;
+      }
+      if (a.sx) v[i] = v[i] * sx * a.sw[n + i];
+      if (a.bias) v[i] += a.bias[n + i];
+      sum += v[i];
+      if (n + i == t) found = v[i];
+    }
+    s = join(s, soft_of<4>(v));
+  }
+  s = join_lanes<32>(join_lanes<16>(join_lanes<8>(join_lanes<4>(join_lanes<2>(join_lanes<1>(s))))));
+  sum += lane_xor_f<1>(sum);
+  sum += lane_xor_f<2>(sum);
+  sum += lane_xor_f<4>(sum);
+  sum += lane_xor_f<8>(sum);
+  sum += lane_xor_f<16>(sum);
+  sum += lane_xor_f<32>(sum);
+  if (threadIdx.x % 64 == 0) waves[threadIdx.x / 64] = make_float4(s.top, s.rest, sum, 0.0f);
+  __syncthreads();
+  if (threadIdx.x) return;
+  for (uint32_t i = 1; i < blockDim.x / 64; ++i) {
+    s = join(s, Soft{waves[i].x, waves[i].y});
+    sum += waves[i].z;
+  }
+  finish_row(o, m, s, sum, found);
+}
+
+// mean[0]: of the losses of the rows that count, mean[1]: 1 / their number.
+__global__ void __launch_bounds__(1024) k_loss_mean(const float *loss, const int64_t *target, int64_t ignore, int64_t M, float *mean) {
+  __shared__ double sums[16];
+  __shared__ int64_t counts[16];
+  double sum = 0.0;
+  int64_t count = 0;
+#pragma unroll 4
+  for (int64_t m = threadIdx.x; m < M; m += 1024)
+    if (target[m] != ignore) {
+      sum += loss[m];
+      ++count;
+    }
+#pragma unroll
+  for (int o = 32; o > 0; o /= 2) {
+    sum += __shfl_xor(sum, o);
+    count += __shfl_xor(count, o);
+  }
+  if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = sum, counts[threadIdx.x / 64] = count;
+  __syncthreads();
+  if (threadIdx.x) return;
+  for (int i = 1; i < 16; ++i) sum += sums[i], count += counts[i];
+  mean[0] = count ? float(sum / double(count)) : 0.0f;
+  mean[1] = count ? float(1.0 / double(count)) : 0.0f;
+}
+
+// ----------------------------------------------------------------------------- dz
+
+struct DzOut {
+  const float *lse, *dloss, *dmean, *mean;
+  const int64_t *target;
+  int64_t ignore, classes, first;  // all classes; the piece's first
+  float keep, even;                // 1 - smoothing, smoothing / classes
+  bf16 *dzx, *dzw;                 // dz sw and dz sx, rows of `pitch` (one array for bf16 operands); or null
+  int64_t pitch;
+  float *part;                     // [ceil(M / unit)][N] partial column sums, or null
+  int32_t unit;
+};
+// The epilogue of 8 consecutive classes (tile::run_epilogue).
+struct StoreDz {
+  static constexpr int DEPTH = 4;
+  static constexpr bool MIRROR = false, SUMS = false;
+  struct Fetch {
+    float lse, c, sx;
+    int32_t t;             // the target's place from n on; -1: not there, -2: the row is left out
+  };
+  const Logits &p;
+  const DzOut &o;
+  float sw[8], bias[8], sum[8], each;
+  int cnt;
+  __device__ __forceinline__ StoreDz(const Logits &p_, const DzOut &o_) : p(p_), o(o_) {
+    each = o.dmean ? o.dmean[0] * o.mean[1] : 0.0f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sum[i] = 0.0f;
+  }
+  __device__ __forceinline__ void columns(int64_t n) {
+    cnt = int(max(int64_t(0), min(p.N - n, int64_t(8))));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sw[i] = 1.0f, bias[i] = 0.0f;
+    if (p.sw) load8f(p.sw + n, cnt, sw);
+    if (p.bias) load8f(p.bias + n, cnt, bias);
+  }
+  __device__ __forceinline__ Fetch fetch(int64_t m, int64_t n) {
+    Fetch f{};
+    if (m >= p.M || cnt == 0) return f;
+    const int64_t t = o.target[m];
+    f.lse = o.lse[m];
+    f.c = o.dloss ? o.dloss[m] : each;
+    f.sx = p.sx ? p.sx[m] : 1.0f;
+    const int64_t d = t - o.first - n;
+    if (t == o.ignore) f.t = -2;
+    else if (t < 0 || t >= o.classes) f.t = -1, f.c = __builtin_nanf("");
+    else f.t = d >= 0 && d < 8 ? int(d) : -1;
+    return f;
+  }
+  __device__ __forceinline__ void finish(int64_t m, int64_t n, float (&v)[8], const Fetch &f) {
+    if (m >= p.M || cnt == 0) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      float z = v[i];
+      if (p.sx) z = z * f.sx * sw[i];
+      const float d = exp_of(z + bias[i] - f.lse) - o.even - (f.t == i ? o.keep : 0.0f);
+      v[i] = f.t == -2 || i >= cnt ? 0.0f : d * f.c;
+      sum[i] += v[i];
+    }
+    if (!p.sx) {
+      if (o.dzx) store8f(o.dzx + m * o.pitch + n, 8, v);
+      return;
+    }
+    float u[8];
+    if (o.dzx) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) u[i] = v[i] * sw[i];
+      store8f(o.dzx + m * o.pitch + n, 8, u);
+    }
+    if (o.dzw) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) u[i] = v[i] * f.sx;
+      store8f(o.dzw + m * o.pitch + n, 8, u);
+    }
+  }
+};
+// dz of a piece of the classes; its row pitch is a multiple of 8, zeros past the piece.
+template <int SHAPE>
+__global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_loss_dz(Logits p, DzOut o) {
+  typedef typename tile::ShapeOf<SHAPE>::type S;
+  __shared__ __attribute__((aligned(16))) char lds[S::LDS];
+  const tile::Place at = tile::place<SHAPE>(p.tiles, blockIdx.x);
+  if (at.m0 >= p.M || at.n0 >= p.N) return;              // (parts of an edge tile)
+  tile::f32x4 acc[S::FM][S::FN];
+  tile::contract<tile::BF16K, ROWS, ROWS, SHAPE, S>(p.x, p.w, p.K, at, p.tiles, lds, acc);
+  StoreDz e(p, o);
+  tile::run_epilogue<tile::BF16K, S>(acc, lds, at.m0, at.n0, e);
+  if (!o.part) return;
+  // A lane has the sums of its 8 columns over every (512 / TN)th row of the wave.
+  constexpr int PER_ROW = S::TN / 8;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    if constexpr (PER_ROW == 4) e.sum[i] += lane_xor_f<4>(e.sum[i]);
+    e.sum[i] += lane_xor_f<8>(e.sum[i]);
+    e.sum[i] += lane_xor_f<16>(e.sum[i]);
+    e.sum[i] += lane_xor_f<32>(e.sum[i]);
+  }
+  const uint32_t wave = wave_id(), l = __lane_id();
+  const int64_t m = at.m0 + (wave / S::WN) * S::TM, n = at.n0 + (wave % S::WN) * S::TN + l * 8;
+  if (l >= PER_ROW || m >= p.M) return;
+  // (the launch's other tiles may be smaller: a part for each `unit` rows, the first of them has the sum)
+  for (int64_t u = m / o.unit; u * o.unit < min(m + S::TM, p.M); ++u) {
+    store8f(o.part + u * p.N + n, e.cnt, e.sum);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) e.sum[i] = 0.0f;
+  }
+}
+
+// ----------------------------------------------------------------------------- host side
+
+struct Sizes {
+  int64_t M, N, K;
+  int64_t ldx, ldw, lddx, lddw;
+  size_t xe;
+  bool codes;
+};
+int check_loss(const fqt_loss_desc *d, Sizes *s) {
+  if (!d) return FQT_E_NULL;
+  if (!(d->x_dtype == FQT_BF16 || code_type(d->x_dtype)) || !float_type(d->dx_dtype) || !float_type(d->dw_dtype))
+    return FQT_E_DTYPE;
+  if (!(d->smoothing >= 0.0f && d->smoothing <= 1.0f)) return FQT_E_INVAL;
+  if (d->M < 0 || d->N < 1 || d->K < 0 || d->M >= FQT_MAX_ROWS || d->N > FQT_MAX_LD || d->K > FQT_MAX_LD)
+    return FQT_E_SHAPE;
+  // (a launch counts its threads in 32 bits)
+  for (const uint64_t tiles : {tile::large_tiles(d->M, d->N), tile::large_tiles(d->M, d->K), tile::large_tiles(d->N, d->K)})
+    if (tiles >= tile::MOST_LARGE) return FQT_E_SHAPE;
+  if (d->x_dtype == FQT_I8 && d->K > 133144) return FQT_E_SHAPE;   // 127^2 K < 2^31
+  *s = {d->M, d->N, d->K, row_stride(d->ldx, d->K), row_stride(d->ldw, d->K), row_stride(d->lddx, d->K),
+        row_stride(d->lddw, d->K), elem_size(d->x_dtype), code_type(d->x_dtype)};
+  if (!s->ldx || !s->ldw || !s->lddx || !s->lddw) return FQT_E_SHAPE;
+  return FQT_OK;
+}
+int check_pointers(const fqt_loss_desc &d, const Sizes &s, const void *x, const void *w, const float *sx,
+                   const float *sw, const float *bias, const int64_t *target) {
+  if (!s.codes && (sx || sw)) return FQT_E_DTYPE;
+  if (s.M && (!target || (s.K && (!x || !w)) || (s.codes && (!sx || !sw)))) return FQT_E_NULL;
+  if (!aligned(x, 16) || !aligned(w, 16) || !aligned(sx, 4) || !aligned(sw, 4) || !aligned(bias, 4) ||
+      !aligned(target, 8))
+    return FQT_E_ALIGN;
+  return FQT_OK;
+}
+
+// Up to this many rows z is a product on the vector units, written to the workspace: its bytes are few beside
+// those of w.
+constexpr int64_t FEW_ROWS = 4;
+
+// Workspace of the forward: copies of operands whose rows are not whole 16-byte pieces (e4m3: bf16 copies),
+// and z of few rows, or partial sums, or pairs, sums and the targets' z.
+struct FwdWs { size_t x, w, part, pairs, sums, at, total; int64_t pitch, e; tile::Plan plan; bool few, widen, copy_x, copy_w; };
+FwdWs fwd_ws(const fqt_loss_desc &d, const Sizes &s) {
+  FwdWs f{};
+  f.few = s.M <= FEW_ROWS;
+  if (f.few) {
+    f.total = align256(size_t(s.M) * s.N * 4);
+    return f;
+  }
+  f.widen = d.x_dtype == FQT_E4M3;
+  f.e = f.widen ? 2 : int64_t(s.xe);
+  f.pitch = round_up(s.K, 16 / f.e);
+  f.copy_x = f.widen || !whole_pieces(s.K, s.ldx, s.xe);
+  f.copy_w = f.widen || !whole_pieces(s.K, s.ldw, s.xe);
+  f.plan = plan_of(s.M, s.N, s.K, f.e);
+  f.w = f.x + (f.copy_x ? align256(size_t(s.M) * f.pitch * f.e) : 0);
+  f.part = f.w + (f.copy_w ? align256(size_t(s.N) * f.pitch * f.e) : 0);
+  if (f.plan.splits > 1) {
+    f.total = f.part + part_bytes(f.plan, s.M, s.N);
+    return f;
+  }
+  const size_t slots = size_t((s.N + SLOT - 1) / SLOT) * s.M;
+  f.pairs = f.part;
+  f.sums = f.pairs + align256(slots * sizeof(Soft));
+  f.at = f.sums + (d.smoothing > 0.0f ? align256(slots * 4) : 0);
+  f.total = f.at + align256(size_t(s.M) * 4);
+  return f;
+}
+
+// The classes of a piece of the backward: dz in bf16 of a piece takes about PIECE_BYTES.
+constexpr int64_t PIECE_BYTES = int64_t(256) << 20, PIECE_LEAST = 4096;
+int64_t piece_of(const Sizes &s) {
+  const int64_t most = std::max(PIECE_LEAST, PIECE_BYTES / std::max<int64_t>(1, s.M * (s.codes ? 4 : 2)));
+  if (s.N <= most + most / 4) return s.N;
+  const int64_t pieces = (s.N + most - 1) / most;
+  return std::min(s.N, round_up((s.N + pieces - 1) / pieces, 256));
+}
+
+// Workspace of the backward: dz of a piece (twice for scaled operands), bf16 copies of operands that are codes
+// or whose rows are not whole pieces (w: of a piece), dx in float32 where several pieces add up to it,
+// the partial sums of dbias and those of the products.
+struct BwdWs { size_t dzx, dzw, x, w, dx, bias, part, total; int64_t piece, dz_pitch, pitch, least; bool copy_x, copy_w, sum_dx; };
+struct PiecePlan { tile::Plan z, dx, dw; int64_t unit; };
+PiecePlan plan_piece(const Sizes &s, int64_t n, int64_t K) {
+  PiecePlan p{};
+  p.z = tile::make_plan(s.M, n, (K * 2 + tile::KB - 1) / tile::KB, false, tile::DENSE_COSTS, 1);
+  p.dx = plan_of(s.M, s.K, n, 2);
+  p.dw = plan_of(n, s.K, s.M, 2);
+  p.unit = 128;            // rows of a wave's results: the fewest of the launches
+  for (int i = 0; i < p.z.launches; ++i)
+    p.unit = std::min<int64_t>(p.unit, p.z.shape[i] == tile::LARGE ? 128 : p.z.shape[i] == tile::MIDDLE ? 64 : 32);
+  return p;
+}
+BwdWs bwd_ws(const fqt_loss_desc &d, const Sizes &s) {
+  BwdWs f{};
+  f.piece = piece_of(s);
+  f.dz_pitch = round_up(f.piece, 8);
+  f.pitch = round_up(s.K, 8);
+  f.copy_x = s.codes || !whole_pieces(s.K, s.ldx, 2);
+  f.copy_w = s.codes || !whole_pieces(s.K, s.ldw, 2);
+  f.sum_dx = f.piece < s.N && d.dx_dtype != FQT_F32;
+  const size_t dz = align256(size_t(s.M) * f.dz_pitch * 2);
+  f.dzw = f.dzx + (s.codes ? dz : 0);
+  f.x = f.dzw + dz;
+  f.w = f.x + (f.copy_x ? align256(size_t(s.M) * f.pitch * 2) : 0);
+  f.dx = f.w + (f.copy_w ? align256(size_t(f.piece) * f.pitch * 2) : 0);
+  f.bias = f.dx + (f.sum_dx ? align256(size_t(s.M) * s.K * 4) : 0);
+  f.part = f.bias + align256(size_t((s.M + 31) / 32) * f.piece * 4);
+  size_t part = 0;
+  for (const int64_t n : {f.piece, s.N % f.piece ? s.N % f.piece : f.piece}) {
+    const PiecePlan p = plan_piece(s, n, f.copy_x || f.copy_w ? f.pitch : s.K);
+    part = std::max({part, part_bytes(p.dx, s.M, s.K), part_bytes(p.dw, n, s.K)});
+  }
+  f.total = f.part + part;
+  return f;
+}
+
+template <int KIND>
+int launch_logits(const tile::Plan &plan, Logits p, const Pairs &o, hipStream_t st) {
+  tile::for_launches(plan, [&]<int SHAPE>(const tile::Tiles &t) {
+    p.tiles = t;
+    k_loss_tiles<KIND, SHAPE><<<dim3(uint32_t(tile::blocks_of(t))), dim3(tile::ShapeOf<SHAPE>::type::THREADS), 0, st>>>(p, o);
+  });
+  return last_launch_status();
+}
+int launch_dense(const RowArgs &a, const Out &o, bool ints, hipStream_t st) {
+  const dim3 grid{uint32_t(o.M)}, block(o.N <= 2048 ? 256 : ROW_THREADS);
+  if (ints) k_loss_dense<true><<<grid, block, 0, st>>>(a, o);
+  else k_loss_dense<false><<<grid, block, 0, st>>>(a, o);
+  return last_launch_status();
+}
+
+}  // namespace
+}  // namespace dense
+}  // namespace fqt
+
+using namespace fqt;
+using namespace fqt::dense;
+
+extern "C" int fqt_loss_workspace_size(const fqt_loss_desc *d, int32_t backward, size_t *bytes) {
+  Sizes s;
+  FQT_TRY_(check_loss(d, &s));
+  if (!bytes) return FQT_E_NULL;
+  *bytes = std::max<size_t>(256, backward ? bwd_ws(*d, s).total : fwd_ws(*d, s).total);
+  return FQT_OK;
+}
+
+extern "C" int fqt_loss_forward(const fqt_loss_desc *d, const void *x, const void *w, const float *x_scale,
+                                const float *w_scale, const float *bias, const int64_t *target, float *loss,
+                                float *lse, float *mean, void *ws, size_t ws_bytes, void *hip_stream) {
+  Sizes s;
+  FQT_TRY_(check_loss(d, &s));
+  FQT_TRY_(check_pointers(*d, s, x, w, x_scale, w_scale, bias, target));
+  if (!ws || (s.M && (!loss || !lse))) return FQT_E_NULL;
+  if (!aligned(loss, 4) || !aligned(lse, 4) || !aligned(mean, 4) || !aligned(ws, 256)) return FQT_E_ALIGN;
+  const FwdWs f = fwd_ws(*d, s);
+  if (ws_bytes < f.total) return FQT_E_WORKSPACE;
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  char *base = static_cast<char *>(ws);
+  const Out o{target, loss, lse, s.M, s.N, d->ignore, d->smoothing};
+  if (s.M && f.few) {
+    fqt_linear_desc l{};
+    l.M = s.M; l.N = s.N; l.K = s.K;
+    l.ldx = s.ldx; l.ldw = s.ldw;
+    l.x_dtype = d->x_dtype;
+    l.y_dtype = l.dx_dtype = l.dw_dtype = FQT_F32;
+    float *z = reinterpret_cast<float *>(base);
+    FQT_TRY_(fqt_linear_forward(&l, x, w, x_scale, w_scale, bias, nullptr, nullptr, z, ws, ws_bytes, hip_stream));
+    FQT_TRY_(launch_dense({z, nullptr, nullptr, nullptr, s.N, 1}, o, false, st));
+  } else if (s.M) {
+    Copy cx{}, cw{};
+    auto operand = [&](const void *p, bool copy, size_t at, int64_t rows, int64_t ld, Copy *c) -> Operand {
+      if (!copy) return {static_cast<const char *>(p), ld * f.e, rows};
+      *c = copy_of(p, rows, s.K, ld, base + at, f.pitch, f.e);
+      return {base + at, f.pitch * f.e, rows};
+    };
+    const Operand xo = operand(x, f.copy_x, f.x, s.M, s.ldx, &cx), wo = operand(w, f.copy_w, f.w, s.N, s.ldw, &cw);
+    FQT_TRY_(launch_copies(cx, cw, d->x_dtype, f.widen, st));
+    const Logits p{xo, wo, s.M, s.N, f.copy_x || f.copy_w ? f.pitch : s.K, f.plan.t[0], x_scale, w_scale, bias,
+                   reinterpret_cast<float *>(base + f.part), round_up(s.N, 8)};
+    const Pairs pairs{reinterpret_cast<Soft *>(base + f.pairs),
+                      d->smoothing > 0.0f ? reinterpret_cast<float *>(base + f.sums) : nullptr,
+                      reinterpret_cast<float *>(base + f.at), target};
+    const bool ints = d->x_dtype == FQT_I8;
+    FQT_TRY_(ints ? launch_logits<tile::I8K>(f.plan, p, pairs, st) : launch_logits<tile::BF16K>(f.plan, p, pairs, st));
+    if (f.plan.splits > 1) {
+      FQT_TRY_(launch_dense({p.part, x_scale, w_scale, bias, p.ldp, f.plan.splits}, o, ints, st));
+    } else {
+      k_loss_rows<<<dim3(uint32_t((s.M + 15) / 16)), dim3(256), 0, st>>>(pairs, o);
+      FQT_TRY_(last_launch_status());
+    }
+  }
+  if (!mean) return FQT_OK;
+  k_loss_mean<<<dim3(1), dim3(1024), 0, st>>>(loss, target, d->ignore, s.M, mean);
+  return last_launch_status();
+}
+
+extern "C" int fqt_loss_backward(const fqt_loss_desc *d, const void *x, const void *w, const float *x_scale,
+                                 const float *w_scale, const float *bias, const int64_t *target, const float *lse,
+                                 const float *dloss, const float *dmean, const float *mean, void *dx, void *dw,
+                                 float *dbias, void *ws, size_t ws_bytes, void *hip_stream) {
+  Sizes s;
+  FQT_TRY_(check_loss(d, &s));
+  FQT_TRY_(check_pointers(*d, s, x, w, x_scale, w_scale, bias, target));
+  if ((dloss && dmean) || (!dmean) != (!mean)) return FQT_E_INVAL;
+  if (!dx && !dw && !dbias) return FQT_OK;
+  if (!ws || (s.M && (!lse || (!dloss && !dmean)))) return FQT_E_NULL;
+  if (!aligned(lse, 4) || !aligned(dloss, 4) || !aligned(dmean, 4) || !aligned(mean, 4) ||
+      !elem_aligned(dx, d->dx_dtype) || !elem_aligned(dw, d->dw_dtype) || !aligned(dbias, 4) || !aligned(ws, 256))
+    return FQT_E_ALIGN;
+  const BwdWs f = bwd_ws(*d, s);
+  if (ws_bytes < f.total) return FQT_E_WORKSPACE;
+  const hipStream_t st = static_cast<hipStream_t>(hip_stream);
+  if (s.M == 0) {          // sums over nothing
+    if (dw) FQT_TRY_(zero_matrix(dw, s.N, s.K, s.lddw, elem_size(d->dw_dtype), st));
+    if (dbias) FQT_TRY_(zero_matrix(dbias, 1, s.N, s.N, 4, st));
+    return FQT_OK;
+  }
+  char *base = static_cast<char *>(ws);
+  const int64_t K = f.copy_x || f.copy_w ? f.pitch : s.K;
+  for (int64_t first = 0; first < s.N; first += f.piece) {
+    const int64_t n = std::min(f.piece, s.N - first), dz_pitch = round_up(n, 8);
+    const PiecePlan plan = plan_piece(s, n, K);
+    // The operands along k (for z) and along the features (for the gradients).
+    Copy cx{}, cw{};
+    Operand xr{static_cast<const char *>(x), s.ldx * 2, s.M};
+    Operand wr{static_cast<const char *>(w) + first * s.ldw * int64_t(s.xe), s.ldw * 2, n};
+    if (f.copy_x) {
+      if (first == 0) cx = copy_of(x, s.M, s.K, s.ldx, base + f.x, f.pitch, 2);
+      xr = {base + f.x, f.pitch * 2, s.M};
+    }
+    if (f.copy_w) {
+      cw = copy_of(wr.p, n, s.K, s.ldw, base + f.w, f.pitch, 2);
+      wr = {base + f.w, f.pitch * 2, n};
+    }
+    FQT_TRY_(launch_copies(cx, cw, d->x_dtype, s.codes, st));
+    Logits p{xr, wr, s.M, n, K, {}, x_scale, w_scale ? w_scale + first : nullptr, bias ? bias + first : nullptr, nullptr, 0};
+    DzOut o{lse, dloss, dmean, mean, target, d->ignore, s.N, first, 1.0f - d->smoothing, d->smoothing / float(s.N),
+            reinterpret_cast<bf16 *>(base + f.dzx), reinterpret_cast<bf16 *>(base + f.dzw), dz_pitch,
+            dbias ? reinterpret_cast<float *>(base + f.bias) : nullptr, int32_t(plan.unit)};
+    if (!dx && (s.codes || !dw)) o.dzx = nullptr;
+    if (!dw) o.dzw = nullptr;
+    tile::for_launches(plan.z, [&]<int SHAPE>(const tile::Tiles &t) {
+      p.tiles = t;
+      k_loss_dz<SHAPE><<<dim3(uint32_t(tile::blocks_of(t))), dim3(tile::ShapeOf<SHAPE>::type::THREADS), 0, st>>>(p, o);
+    });
+    FQT_TRY_(last_launch_status());
+    Gradients g{};
+    g.M = s.M; g.N = n; g.K = s.K;
+    g.dzx = {base + f.dzx, dz_pitch * 2, s.M};
+    g.dzw = {base + f.dzw, dz_pitch * 2, dz_pitch};
+    g.w = {wr.p, wr.ld, f.copy_w ? f.pitch : s.K};
+    g.x = {xr.p, xr.ld, f.copy_x ? f.pitch : s.K};
+    g.plan_dx = plan.dx; g.plan_dw = plan.dw;
+    if (dx) {
+      // dx adds up in float32: in place, or in the workspace until the last piece
+      const bool last = first + n == s.N || !f.sum_dx;
+      float *acc = f.sum_dx ? reinterpret_cast<float *>(base + f.dx) : static_cast<float *>(dx);
+      const int64_t ldacc = f.sum_dx ? std::max<int64_t>(1, s.K) : s.lddx;
+      g.dx = last ? dx : acc;
+      g.lddx = last ? s.lddx : ldacc;
+      g.dx_dtype = last ? d->dx_dtype : FQT_F32;
+      if (first) g.add = acc, g.ldadd = ldacc;
+    }
+    if (dw) g.dw = static_cast<char *>(dw) + first * s.lddw * int64_t(elem_size(d->dw_dtype));
+    g.lddw = s.lddw;
+    g.dw_dtype = d->dw_dtype;
+    g.part = reinterpret_cast<float *>(base + f.part);
+    if (dbias) g.bias = {o.part, dbias + first, n, int32_t((s.M + plan.unit - 1) / plan.unit)};
+    FQT_TRY_(launch_gradients(g, st));
+  }
+  return FQT_OK;
+}
