@@ -541,6 +541,24 @@ __global__ void __launch_bounds__(tile::Small::THREADS, 2) k_product_pair(Produc
     sum_dbias(b, blockIdx.x - second, reinterpret_cast<float (*)[32]>(lds));
   }
 }
+
+// Both products of large tiles in one launch.  dw_first: its tiles are the first workgroups.
+__global__ void __launch_bounds__(tile::Large::THREADS, 2) k_product_both(Product px, Epilogue ex, Product pw, Epilogue ew, int dw_first) {
+  typedef tile::Large S;
+  __shared__ __attribute__((aligned(16))) char lds[S::LDS];
+  tile::f32x4 acc[S::FM][S::FN];
+  const uint32_t before = dw_first ? pw.tiles.count : px.tiles.count;
+  const uint32_t b = blockIdx.x < before ? blockIdx.x : blockIdx.x - before;
+  if ((blockIdx.x < before) == (dw_first != 0)) {
+    const tile::Place at = tile::place<tile::LARGE>(pw.tiles, b);
+    tile::contract<tile::BF16K, COLS, COLS, tile::LARGE, S>(pw.x, pw.w, pw.K, at, pw.tiles, lds, acc);
+    tile::run_epilogue<tile::BF16K, S>(acc, lds, at.m0, at.n0, Finish<FQT_ACT_NONE>(ew));
+  } else {
+    const tile::Place at = tile::place<tile::LARGE>(px.tiles, b);
+    tile::contract<tile::BF16K, ROWS, COLS, tile::LARGE, S>(px.x, px.w, px.K, at, px.tiles, lds, acc);
+    tile::run_epilogue<tile::BF16K, S>(acc, lds, at.m0, at.n0, Finish<FQT_ACT_NONE>(ex));
+  }
+}
 __global__ void __launch_bounds__(256) k_zero(char *p, int64_t rows, int64_t bytes, int64_t ld) {
   for (int64_t i = blockIdx.x * 256 + threadIdx.x; i < rows * bytes; i += int64_t(gridDim.x) * 256)
     p[i / bytes * ld + i % bytes] = 0;
@@ -698,13 +716,49 @@ int zero_matrix(void *p, int64_t rows, int64_t cols, int64_t ld, size_t e, hipSt
   return last_launch_status();
 }
 
+namespace {
+// All tiles of `edge` a side of a product of bf16 operands.
+tile::Tiles whole_grid(int64_t M, int64_t N, int64_t K, int64_t edge) {
+  tile::Tiles t{};
+  t.nm = uint32_t((M + edge - 1) / edge);
+  t.nn = uint32_t((N + edge - 1) / edge);
+  t.count = t.nm * t.nn;
+  t.splits = 1;
+  t.steps = uint32_t((K * 2 + tile::KB - 1) / tile::KB);
+  return t;
+}
+}  // namespace
+
+Together plan_together(int64_t M, int64_t N, int64_t K, const tile::Plan &dx, const tile::Plan &dw) {
+  const tile::Costs &c = tile::DENSE_COSTS;
+  double best = dx.us + dw.us;
+  Together how = APART;
+  // us of both products' tiles, `cu` of them on a CU at a time: evenly over the CUs, and half of one of the last
+  // tiles; no less than the longer tiles' rounds
+  auto take = [&](Together t, int64_t edge, int cu, double step, double start) {
+    const tile::Tiles x = whole_grid(M, K, N, edge), w = whole_grid(N, K, M, edge);
+    if (uint64_t(x.count) + w.count >= tile::MOST_LARGE) return;
+    const double ex = step * x.steps + start, ew = step * w.steps + start, slots = 256.0 * cu;
+    const double rounds = std::ceil((ex > ew ? x : w).count / slots);
+    const double us = std::max((x.count * ex + w.count * ew) / slots + std::min(ex, ew) / 2, rounds * std::max(ex, ew)) + 3;
+    if (us < best) best = us, how = t;
+  };
+  if (tile::large_tiles(M, K) < tile::MOST_LARGE / 32 && tile::large_tiles(N, K) < tile::MOST_LARGE / 32)
+    take(SMALL_BOTH, tile::Small::BM, 3, c.small[2], c.start[2]);
+  take(LARGE_BOTH, tile::Large::BM, 1, c.large[0], c.start[0]);
+  return how;
+}
+
 int launch_gradients(const Gradients &g, hipStream_t st) {
   const uint32_t bias_blocks = g.bias.dbias ? uint32_t((g.N + 31) / 32) : 0;
   const Epilogue ex{nullptr, nullptr, nullptr, g.add, nullptr, g.dx, 0, 0, g.ldadd, 0, g.lddx, g.dx_dtype, FQT_ACT_NONE, FQT_F32};
   const Epilogue ew{nullptr, nullptr, nullptr, nullptr, nullptr, g.dw, 0, 0, 0, 0, g.lddw, g.dw_dtype, FQT_ACT_NONE, FQT_F32};
   auto small = [](const tile::Plan &p) { return p.shape[0] == tile::SMALL && p.launches == 1 && p.splits == 1; };
-  if (g.dx && g.dw && g.K && small(g.plan_dx) && small(g.plan_dw)) {
-    const Product px{g.dzx, g.w, g.M, g.K, g.N, g.plan_dx.t[0], nullptr, 0}, pw{g.dzw, g.x, g.N, g.K, g.M, g.plan_dw.t[0], nullptr, 0};
+  const bool together = g.dx && g.dw && g.K;
+  if (together && (g.together == SMALL_BOTH || (small(g.plan_dx) && small(g.plan_dw)))) {
+    const int64_t edge = tile::Small::BM;
+    const Product px{g.dzx, g.w, g.M, g.K, g.N, whole_grid(g.M, g.K, g.N, edge), nullptr, 0},
+        pw{g.dzw, g.x, g.N, g.K, g.M, whole_grid(g.N, g.K, g.M, edge), nullptr, 0};
     k_product_pair<<<dim3(px.tiles.count + pw.tiles.count + bias_blocks), dim3(tile::Small::THREADS), 0, st>>>(
         px, sized(ex, g.M, g.K), pw, sized(ew, g.N, g.K), g.bias);
     return last_launch_status();
@@ -714,6 +768,14 @@ int launch_gradients(const Gradients &g, hipStream_t st) {
     FQT_TRY_(last_launch_status());
   }
   if (g.K == 0) return FQT_OK;
+  if (together && g.together == LARGE_BOTH) {
+    const int64_t edge = tile::Large::BM;
+    const Product px{g.dzx, g.w, g.M, g.K, g.N, whole_grid(g.M, g.K, g.N, edge), nullptr, 0},
+        pw{g.dzw, g.x, g.N, g.K, g.M, whole_grid(g.N, g.K, g.M, edge), nullptr, 0};
+    k_product_both<<<dim3(px.tiles.count + pw.tiles.count), dim3(tile::Large::THREADS), 0, st>>>(
+        px, sized(ex, g.M, g.K), pw, sized(ew, g.N, g.K), pw.tiles.steps > px.tiles.steps);
+    return last_launch_status();
+  }
   if (g.dx) FQT_TRY_((launch_product<tile::BF16K, ROWS, COLS>(g.plan_dx, g.dzx, g.w, g.M, g.K, g.N, ex, g.part, st)));
   if (g.dw) FQT_TRY_((launch_product<tile::BF16K, COLS, COLS>(g.plan_dw, g.dzw, g.x, g.N, g.K, g.M, ew, g.part, st)));
   return FQT_OK;

@@ -86,10 +86,11 @@ struct Logits {
 };
 constexpr int SLOT = 64;   // columns of a pair
 struct Pairs {
-  Soft *pairs;             // [ceil(N / SLOT)][M]
+  Soft *pairs;             // [slots][M]
   float *sums;             // the same of z, or null
   float *at;               // [M] the target's z
   const int64_t *target;
+  int64_t slots;
 };
 
 // The pairs of a tile, straight from the accumulators: lane l has row l % 16 of each 16 x 16 result and four
@@ -195,7 +196,7 @@ __global__ void __launch_bounds__(256) k_loss_rows(Pairs p, Out o) {
   constexpr int AHEAD = 8;
   __shared__ float4 all[16][17];
   const int r = threadIdx.x % 16, g = threadIdx.x / 16;
-  const int64_t m = int64_t(blockIdx.x) * 16 + r, slots = (o.N + SLOT - 1) / SLOT;
+  const int64_t m = int64_t(blockIdx.x) * 16 + r, slots = p.slots;
   Soft s{NOTHING, 0.0f};
   float sum = 0.0f;
   if (m < o.M)
@@ -224,45 +225,47 @@ __global__ void __launch_bounds__(256) k_loss_rows(Pairs p, Out o) {
 }
 
 // ----------------------------------------------------------------------------- forward by rows
-// Where z passes through the workspace (few rows, or a split contraction): a workgroup takes a row, whose z
-// are sums of `splits` words.
+// Where z passes through the workspace (few rows, or a split contraction): a workgroup takes CHUNK columns of a
+// row down to a pair, or the whole row to its loss if that is all; z are sums of `splits` words.  One row of 65536 by
+// one workgroup took 18 us.
 struct RowArgs {
   const float *part;
   const float *sx, *sw, *bias;
   int64_t ldp;
   uint32_t splits;
 };
-constexpr int ROW_THREADS = 1024;
+constexpr int CHUNK = 4096;
 template <bool INTS>
-__global__ void __launch_bounds__(ROW_THREADS) k_loss_dense(RowArgs a, Out o) {
-  __shared__ float4 waves[ROW_THREADS / 64];
+__global__ void __launch_bounds__(256) k_loss_dense(RowArgs a, Pairs p, Out o) {
+  __shared__ float4 waves[4];
   __shared__ float found;
-  const int64_t m = blockIdx.x, t = o.target[m];
+  const int64_t m = blockIdx.x / p.slots, slot = blockIdx.x % p.slots, t = o.target[m];
+  const int64_t n0 = slot * CHUNK, end = min(o.N, n0 + CHUNK);
   const float sx = a.sx ? a.sx[m] : 1.0f;
   if (threadIdx.x == 0) found = 0.0f;
   __syncthreads();
   Soft s{NOTHING, 0.0f};
   float sum = 0.0f;
 #pragma unroll 4
-  for (int64_t n = int64_t(threadIdx.x) * 4; n < o.N; n += int64_t(blockDim.x) * 4) {
-    const int cnt = int(min(o.N - n, int64_t(4)));
+  for (int64_t n = n0 + threadIdx.x * 4; n < end; n += 1024) {
+    const int cnt = int(min(end - n, int64_t(4)));
     std::conditional_t<INTS, int, float> w[4] = {};
-    for (uint32_t p = 0; p < a.splits; ++p) {
-      const float *at = a.part + (p * o.M + m) * a.ldp + n;
+    for (uint32_t i = 0; i < a.splits; ++i) {
+      const float *at = a.part + (i * o.M + m) * a.ldp + n;
       uint32_t u[4] = {};
       if (cnt == 4) {
         const u32x4 q = load_bytes16(at);
 #pragma unroll
-        for (int i = 0; i < 4; ++i) u[i] = q[i];
+        for (int j = 0; j < 4; ++j) u[j] = q[j];
       } else {
 #pragma unroll
-        for (int i = 0; i < 3; ++i)
-          if (i < cnt) u[i] = __float_as_uint(at[i]);
+        for (int j = 0; j < 3; ++j)
+          if (j < cnt) u[j] = __float_as_uint(at[j]);
       }
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        if constexpr (INTS) w[i] += int(u[i]);
-        else w[i] += __uint_as_float(u[i]);
+      for (int j = 0; j < 4; ++j) {
+        if constexpr (INTS) w[j] += int(u[j]);
+        else w[j] += __uint_as_float(u[j]);
       }
     }
     float v[4];
@@ -290,11 +293,18 @@ __global__ void __launch_bounds__(ROW_THREADS) k_loss_dense(RowArgs a, Out o) {
   if (threadIdx.x % 64 == 0) waves[threadIdx.x / 64] = make_float4(s.top, s.rest, sum, 0.0f);
   __syncthreads();
   if (threadIdx.x) return;
-  for (uint32_t i = 1; i < blockDim.x / 64; ++i) {
+#pragma unroll
+  for (int i = 1; i < 4; ++i) {
     s = join(s, Soft{waves[i].x, waves[i].y});
     sum += waves[i].z;
   }
-  finish_row(o, m, s, sum, found);
+  if (p.slots == 1) {
+    finish_row(o, m, s, sum, found);
+    return;
+  }
+  p.pairs[slot * o.M + m] = s;
+  if (p.sums) p.sums[slot * o.M + m] = sum;
+  if (t >= n0 && t < end) p.at[m] = found;
 }
 
 // mean[0]: of the losses of the rows that count, mean[1]: 1 / their number.
@@ -304,11 +314,11 @@ __global__ void __launch_bounds__(1024) k_loss_mean(const float *loss, const int
   double sum = 0.0;
   int64_t count = 0;
 #pragma unroll 4
-  for (int64_t m = threadIdx.x; m < M; m += 1024)
-    if (target[m] != ignore) {
-      sum += loss[m];
-      ++count;
-    }
+  for (int64_t m = threadIdx.x; m < M; m += 1024) {
+    // (a row that is left out has loss 0)
+    sum += loss[m];
+    count += target[m] != ignore;
+  }
 #pragma unroll
   for (int o = 32; o > 0; o /= 2) {
     sum += __shfl_xor(sum, o);
@@ -373,13 +383,39 @@ struct StoreDz {
   }
   __device__ __forceinline__ void finish(int64_t m, int64_t n, float (&v)[8], const Fetch &f) {
     if (m >= p.M || cnt == 0) return;
+    // (what few rows or launches need stands behind branches: a group of 8 takes 100 issue slots of the 160 that
+    // it took with selects for all of it)
+    if (p.sx) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      float z = v[i];
-      if (p.sx) z = z * f.sx * sw[i];
-      const float d = exp_of(z + bias[i] - f.lse) - o.even - (f.t == i ? o.keep : 0.0f);
-      v[i] = f.t == -2 || i >= cnt ? 0.0f : d * f.c;
-      sum[i] += v[i];
+      for (int i = 0; i < 8; ++i) v[i] = v[i] * f.sx * sw[i];
+    }
+    if (p.bias) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] += bias[i];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = exp_of(v[i] - f.lse);
+    if (o.even != 0.0f) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] -= o.even;
+    }
+    if (f.t >= 0) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] -= f.t == i ? o.keep : 0.0f;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] *= f.c;
+    if (f.t == -2) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = 0.0f;
+    }
+    if (cnt < 8) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) v[i] = i < cnt ? v[i] : 0.0f;
+    }
+    if (o.part) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i) sum[i] += v[i];
     }
     if (!p.sx) {
       if (o.dzx) store8f(o.dzx + m * o.pitch + n, 8, v);
@@ -407,6 +443,10 @@ __global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_loss
   if (at.m0 >= p.M || at.n0 >= p.N) return;              // (parts of an edge tile)
   tile::f32x4 acc[S::FM][S::FN];
   tile::contract<tile::BF16K, ROWS, ROWS, SHAPE, S>(p.x, p.w, p.K, at, p.tiles, lds, acc);
+  if (p.tiles.splits > 1) {
+    tile::run_epilogue<tile::BF16K, S>(acc, lds, at.m0, at.n0, tile::StorePart{p.part + at.split * p.M * p.ldp, p.M, p.ldp});
+    return;
+  }
   StoreDz e(p, o);
   tile::run_epilogue<tile::BF16K, S>(acc, lds, at.m0, at.n0, e);
   if (!o.part) return;
@@ -428,6 +468,38 @@ __global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_loss
 #pragma unroll
     for (int i = 0; i < 8; ++i) e.sum[i] = 0.0f;
   }
+}
+
+// dz from the partial sums of a split contraction: a thread takes 8 columns, a wave every fourth row of the
+// workgroup's `unit`.
+__global__ void __launch_bounds__(256) k_loss_dz_join(Logits p, DzOut o, uint32_t groups) {
+  __shared__ float sums[3][8][64];
+  const int lane = threadIdx.x % 64, wave = threadIdx.x / 64;
+  const int64_t u = blockIdx.x % groups, n = (int64_t(blockIdx.x / groups) * 64 + lane) * 8;
+  StoreDz e(p, o);
+  e.columns(n);
+  if (e.cnt)
+    for (int64_t m = u * o.unit + wave; m < min(p.M, (u + 1) * o.unit); m += 4) {
+      const auto f = e.fetch(m, n);
+      float v[8] = {};
+#pragma unroll 4
+      for (uint32_t s = 0; s < p.tiles.splits; ++s) {
+        float t[8];
+        load8f(p.part + (s * p.M + m) * p.ldp + n, 8, t);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] += t[i];
+      }
+      e.finish(m, n, v, f);
+    }
+  if (!o.part) return;
+  if (wave)
+#pragma unroll
+    for (int i = 0; i < 8; ++i) sums[wave - 1][i][lane] = e.sum[i];
+  __syncthreads();
+  if (wave || !e.cnt) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) e.sum[i] = ((e.sum[i] + sums[0][i][lane]) + sums[1][i][lane]) + sums[2][i][lane];
+  store8f(o.part + u * p.N + n, e.cnt, e.sum);
 }
 
 // ----------------------------------------------------------------------------- host side
@@ -469,13 +541,21 @@ int check_pointers(const fqt_loss_desc &d, const Sizes &s, const void *x, const 
 constexpr int64_t FEW_ROWS = 4;
 
 // Workspace of the forward: copies of operands whose rows are not whole 16-byte pieces (e4m3: bf16 copies),
-// and z of few rows, or partial sums, or pairs, sums and the targets' z.
-struct FwdWs { size_t x, w, part, pairs, sums, at, total; int64_t pitch, e; tile::Plan plan; bool few, widen, copy_x, copy_w; };
+// z of few rows or partial sums, and pairs, sums and the targets' z.
+struct FwdWs { size_t x, w, part, pairs, sums, at, total; int64_t pitch, e, slots; tile::Plan plan; bool few, widen, copy_x, copy_w; };
 FwdWs fwd_ws(const fqt_loss_desc &d, const Sizes &s) {
   FwdWs f{};
   f.few = s.M <= FEW_ROWS;
+  auto pairs = [&](size_t from, int64_t slots) {
+    f.slots = slots;
+    f.pairs = from;
+    f.sums = f.pairs + align256(size_t(slots) * s.M * sizeof(Soft));
+    f.at = f.sums + (d.smoothing > 0.0f ? align256(size_t(slots) * s.M * 4) : 0);
+    f.total = f.at + align256(size_t(s.M) * 4);
+  };
+  const int64_t chunks = (s.N + CHUNK - 1) / CHUNK;
   if (f.few) {
-    f.total = align256(size_t(s.M) * s.N * 4);
+    pairs(align256(size_t(s.M) * s.N * 4), chunks);
     return f;
   }
   f.widen = d.x_dtype == FQT_E4M3;
@@ -486,15 +566,8 @@ FwdWs fwd_ws(const fqt_loss_desc &d, const Sizes &s) {
   f.plan = plan_of(s.M, s.N, s.K, f.e);
   f.w = f.x + (f.copy_x ? align256(size_t(s.M) * f.pitch * f.e) : 0);
   f.part = f.w + (f.copy_w ? align256(size_t(s.N) * f.pitch * f.e) : 0);
-  if (f.plan.splits > 1) {
-    f.total = f.part + part_bytes(f.plan, s.M, s.N);
-    return f;
-  }
-  const size_t slots = size_t((s.N + SLOT - 1) / SLOT) * s.M;
-  f.pairs = f.part;
-  f.sums = f.pairs + align256(slots * sizeof(Soft));
-  f.at = f.sums + (d.smoothing > 0.0f ? align256(slots * 4) : 0);
-  f.total = f.at + align256(size_t(s.M) * 4);
+  if (f.plan.splits > 1) pairs(f.part + part_bytes(f.plan, s.M, s.N), chunks);
+  else pairs(f.part, (s.N + SLOT - 1) / SLOT);
   return f;
 }
 
@@ -511,15 +584,18 @@ int64_t piece_of(const Sizes &s) {
 // or whose rows are not whole pieces (w: of a piece), dx in float32 where several pieces add up to it,
 // the partial sums of dbias and those of the products.
 struct BwdWs { size_t dzx, dzw, x, w, dx, bias, part, total; int64_t piece, dz_pitch, pitch, least; bool copy_x, copy_w, sum_dx; };
-struct PiecePlan { tile::Plan z, dx, dw; int64_t unit; };
+struct PiecePlan { tile::Plan z, dx, dw; int64_t unit; Together together; };
 PiecePlan plan_piece(const Sizes &s, int64_t n, int64_t K) {
   PiecePlan p{};
-  p.z = tile::make_plan(s.M, n, (K * 2 + tile::KB - 1) / tile::KB, false, tile::DENSE_COSTS, 1);
+  p.z = plan_of(s.M, n, K, 2);
   p.dx = plan_of(s.M, s.K, n, 2);
   p.dw = plan_of(n, s.K, s.M, 2);
+  p.together = plan_together(s.M, n, s.K, p.dx, p.dw);
   p.unit = 128;            // rows of a wave's results: the fewest of the launches
   for (int i = 0; i < p.z.launches; ++i)
     p.unit = std::min<int64_t>(p.unit, p.z.shape[i] == tile::LARGE ? 128 : p.z.shape[i] == tile::MIDDLE ? 64 : 32);
+  // (of a joining workgroup: enough of them, few partial sums)
+  if (p.z.splits > 1) p.unit = std::max<int64_t>(4, (s.M + 127) / 128);
   return p;
 }
 BwdWs bwd_ws(const fqt_loss_desc &d, const Sizes &s) {
@@ -536,12 +612,13 @@ BwdWs bwd_ws(const fqt_loss_desc &d, const Sizes &s) {
   f.w = f.x + (f.copy_x ? align256(size_t(s.M) * f.pitch * 2) : 0);
   f.dx = f.w + (f.copy_w ? align256(size_t(f.piece) * f.pitch * 2) : 0);
   f.bias = f.dx + (f.sum_dx ? align256(size_t(s.M) * s.K * 4) : 0);
-  f.part = f.bias + align256(size_t((s.M + 31) / 32) * f.piece * 4);
-  size_t part = 0;
+  size_t part = 0, groups = 1;
   for (const int64_t n : {f.piece, s.N % f.piece ? s.N % f.piece : f.piece}) {
     const PiecePlan p = plan_piece(s, n, f.copy_x || f.copy_w ? f.pitch : s.K);
-    part = std::max({part, part_bytes(p.dx, s.M, s.K), part_bytes(p.dw, n, s.K)});
+    part = std::max({part, part_bytes(p.z, s.M, n), part_bytes(p.dx, s.M, s.K), part_bytes(p.dw, n, s.K)});
+    groups = std::max(groups, size_t((s.M + p.unit - 1) / p.unit));
   }
+  f.part = f.bias + align256(groups * f.piece * 4);
   f.total = f.part + part;
   return f;
 }
@@ -554,10 +631,16 @@ int launch_logits(const tile::Plan &plan, Logits p, const Pairs &o, hipStream_t 
   });
   return last_launch_status();
 }
-int launch_dense(const RowArgs &a, const Out &o, bool ints, hipStream_t st) {
-  const dim3 grid{uint32_t(o.M)}, block(o.N <= 2048 ? 256 : ROW_THREADS);
-  if (ints) k_loss_dense<true><<<grid, block, 0, st>>>(a, o);
-  else k_loss_dense<false><<<grid, block, 0, st>>>(a, o);
+// z in the workspace to pairs.
+int launch_dense(const RowArgs &a, const Pairs &p, const Out &o, bool ints, hipStream_t st) {
+  const dim3 grid(uint32_t(o.M * p.slots)), block(256);
+  if (ints) k_loss_dense<true><<<grid, block, 0, st>>>(a, p, o);
+  else k_loss_dense<false><<<grid, block, 0, st>>>(a, p, o);
+  return last_launch_status();
+}
+// Pairs to the losses (nothing where the pass before had whole rows).
+int launch_rows(const Pairs &p, const Out &o, hipStream_t st) {
+  k_loss_rows<<<dim3(uint32_t((o.M + 15) / 16)), dim3(256), 0, st>>>(p, o);
   return last_launch_status();
 }
 
@@ -589,6 +672,9 @@ extern "C" int fqt_loss_forward(const fqt_loss_desc *d, const void *x, const voi
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   char *base = static_cast<char *>(ws);
   const Out o{target, loss, lse, s.M, s.N, d->ignore, d->smoothing};
+  const Pairs pairs{reinterpret_cast<Soft *>(base + f.pairs),
+                    d->smoothing > 0.0f ? reinterpret_cast<float *>(base + f.sums) : nullptr,
+                    reinterpret_cast<float *>(base + f.at), target, f.slots};
   if (s.M && f.few) {
     fqt_linear_desc l{};
     l.M = s.M; l.N = s.N; l.K = s.K;
@@ -597,7 +683,8 @@ extern "C" int fqt_loss_forward(const fqt_loss_desc *d, const void *x, const voi
     l.y_dtype = l.dx_dtype = l.dw_dtype = FQT_F32;
     float *z = reinterpret_cast<float *>(base);
     FQT_TRY_(fqt_linear_forward(&l, x, w, x_scale, w_scale, bias, nullptr, nullptr, z, ws, ws_bytes, hip_stream));
-    FQT_TRY_(launch_dense({z, nullptr, nullptr, nullptr, s.N, 1}, o, false, st));
+    FQT_TRY_(launch_dense({z, nullptr, nullptr, nullptr, s.N, 1}, pairs, o, false, st));
+    if (f.slots > 1) FQT_TRY_(launch_rows(pairs, o, st));
   } else if (s.M) {
     Copy cx{}, cw{};
     auto operand = [&](const void *p, bool copy, size_t at, int64_t rows, int64_t ld, Copy *c) -> Operand {
@@ -609,17 +696,10 @@ extern "C" int fqt_loss_forward(const fqt_loss_desc *d, const void *x, const voi
     FQT_TRY_(launch_copies(cx, cw, d->x_dtype, f.widen, st));
     const Logits p{xo, wo, s.M, s.N, f.copy_x || f.copy_w ? f.pitch : s.K, f.plan.t[0], x_scale, w_scale, bias,
                    reinterpret_cast<float *>(base + f.part), round_up(s.N, 8)};
-    const Pairs pairs{reinterpret_cast<Soft *>(base + f.pairs),
-                      d->smoothing > 0.0f ? reinterpret_cast<float *>(base + f.sums) : nullptr,
-                      reinterpret_cast<float *>(base + f.at), target};
     const bool ints = d->x_dtype == FQT_I8;
     FQT_TRY_(ints ? launch_logits<tile::I8K>(f.plan, p, pairs, st) : launch_logits<tile::BF16K>(f.plan, p, pairs, st));
-    if (f.plan.splits > 1) {
-      FQT_TRY_(launch_dense({p.part, x_scale, w_scale, bias, p.ldp, f.plan.splits}, o, ints, st));
-    } else {
-      k_loss_rows<<<dim3(uint32_t((s.M + 15) / 16)), dim3(256), 0, st>>>(pairs, o);
-      FQT_TRY_(last_launch_status());
-    }
+    if (f.plan.splits > 1) FQT_TRY_(launch_dense({p.part, x_scale, w_scale, bias, p.ldp, f.plan.splits}, pairs, o, ints, st));
+    if (f.plan.splits == 1 || f.slots > 1) FQT_TRY_(launch_rows(pairs, o, st));
   }
   if (!mean) return FQT_OK;
   k_loss_mean<<<dim3(1), dim3(1024), 0, st>>>(loss, target, d->ignore, s.M, mean);
@@ -665,7 +745,8 @@ extern "C" int fqt_loss_backward(const fqt_loss_desc *d, const void *x, const vo
       wr = {base + f.w, f.pitch * 2, n};
     }
     FQT_TRY_(launch_copies(cx, cw, d->x_dtype, s.codes, st));
-    Logits p{xr, wr, s.M, n, K, {}, x_scale, w_scale ? w_scale + first : nullptr, bias ? bias + first : nullptr, nullptr, 0};
+    Logits p{xr, wr, s.M, n, K, {}, x_scale, w_scale ? w_scale + first : nullptr, bias ? bias + first : nullptr,
+             reinterpret_cast<float *>(base + f.part), round_up(n, 8)};
     DzOut o{lse, dloss, dmean, mean, target, d->ignore, s.N, first, 1.0f - d->smoothing, d->smoothing / float(s.N),
             reinterpret_cast<bf16 *>(base + f.dzx), reinterpret_cast<bf16 *>(base + f.dzw), dz_pitch,
             dbias ? reinterpret_cast<float *>(base + f.bias) : nullptr, int32_t(plan.unit)};
@@ -675,6 +756,10 @@ extern "C" int fqt_loss_backward(const fqt_loss_desc *d, const void *x, const vo
       p.tiles = t;
       k_loss_dz<SHAPE><<<dim3(uint32_t(tile::blocks_of(t))), dim3(tile::ShapeOf<SHAPE>::type::THREADS), 0, st>>>(p, o);
     });
+    if (plan.z.splits > 1) {
+      const uint32_t groups = uint32_t((s.M + plan.unit - 1) / plan.unit);
+      k_loss_dz_join<<<dim3(groups * uint32_t((n + 511) / 512)), dim3(256), 0, st>>>(p, o, groups);
+    }
     FQT_TRY_(last_launch_status());
     Gradients g{};
     g.M = s.M; g.N = n; g.K = s.K;
@@ -697,6 +782,7 @@ extern "C" int fqt_loss_backward(const fqt_loss_desc *d, const void *x, const vo
     g.lddw = s.lddw;
     g.dw_dtype = d->dw_dtype;
     g.part = reinterpret_cast<float *>(base + f.part);
+    g.together = plan.together;
     if (dbias) g.bias = {o.part, dbias + first, n, int32_t((s.M + plan.unit - 1) / plan.unit)};
     FQT_TRY_(launch_gradients(g, st));
   }

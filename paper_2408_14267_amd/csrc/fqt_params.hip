@@ -17,25 +17,40 @@ namespace {
 
 constexpr int BLOCK = FQT_STATE_BLOCK;
 
-// The tensors of a launch; chunk c of `size` elements belongs to the last tensor whose `begin` is <= c.
-struct Entry {
+// The tensors of a launch; chunk c of the launch belongs to the last entry whose `begin` is <= c.  Launches have
+// 4 KB of arguments, so entries hold what their kernel needs: 62 tensors with 8-bit states are one launch of 51
+// us, as two launches of 48 and 14 they took 57.
+struct NormEntry {
+  const void *g;
+  uint32_t n;                         // elements (a longer tensor has several entries)
+};
+struct AdamEntry {
+  const void *g;
+  float *p, *m, *v;
+  uint32_t n;
+};
+struct CodesEntry {
   const void *g;
   float *p;
   char *m, *v;
   float *m_scale, *v_scale;
-  int64_t n, first;
+  uint32_t n;
+  uint32_t quad;                      // (place in the random sequence) / 4 from the list's `quad` on
 };
-constexpr int LIST = 48;              // 48 entries are 3.3 KB of the 4 KB of arguments
+template <typename E>
 struct List {
-  Entry e[LIST];
-  uint32_t begin[LIST];
+  static constexpr int MOST = (4096 - 192) / (sizeof(E) + 4);
+  E e[MOST];
+  uint32_t begin[MOST];               // first chunks
+  uint32_t half[(MOST + 31) / 32];    // bit i: the gradient of entry i is bf16
   int32_t count;
-  uint32_t half;                      // bit i: entries 32 i ... hold ... (see half_of)
-  uint32_t half_hi;
+  uint64_t quad;
 };
-static_assert(sizeof(List) <= 3600, "kernel arguments");
-__device__ __forceinline__ bool is_half(const List &l, int i) { return (i < 32 ? l.half >> i : l.half_hi >> (i - 32)) & 1; }
-__device__ __forceinline__ int entry_of(const List &l, uint32_t chunk) {
+static_assert(sizeof(List<NormEntry>) <= 3968 && sizeof(List<AdamEntry>) <= 3968 && sizeof(List<CodesEntry>) <= 3968, "kernel arguments");
+template <typename E>
+__device__ __forceinline__ bool is_half(const List<E> &l, int i) { return l.half[i / 32] >> (i % 32) & 1; }
+template <typename E>
+__device__ __forceinline__ int entry_of(const List<E> &l, uint32_t chunk) {
   int lo = 0, hi = l.count;
   while (hi - lo > 1) {
     const int mid = (lo + hi) / 2;
@@ -167,10 +182,11 @@ __device__ __forceinline__ void decode(uint32_t u, float scale, float (&o)[4]) {
 
 // A wave takes BLOCKS blocks of 256 elements, four consecutive elements a lane, all loads first.
 constexpr int ADAM_BLOCKS = 4, ADAM_CHUNK = 4 * ADAM_BLOCKS * BLOCK;
-template <bool CODES>
-__global__ void __launch_bounds__(256) k_adamw(List list, Adam a) {
+template <typename E>
+__global__ void __launch_bounds__(256) k_adamw(List<E> list, Adam a) {
+  constexpr bool CODES = std::is_same_v<E, CodesEntry>;
   const int at = entry_of(list, blockIdx.x);
-  const Entry &e = list.e[at];
+  const E &e = list.e[at];
   const bool half = is_half(list, at);
   if (a.step) at_step(a, max(*a.step, int64_t(1)));
   const float s = a.scale ? *a.scale : 1.0f;
@@ -181,7 +197,7 @@ __global__ void __launch_bounds__(256) k_adamw(List list, Adam a) {
   float sm[ADAM_BLOCKS], sv[ADAM_BLOCKS];
 #pragma unroll
   for (int b = 0; b < ADAM_BLOCKS; ++b) {
-    const int64_t i = (b0 + b) * BLOCK + lane * 4, left = e.n - i;
+    const int64_t i = (b0 + b) * BLOCK + lane * 4, left = int64_t(e.n) - i;
     load4(e.g, i, half, left, g[b]);
     load4(e.p + i, left, p[b]);
     if constexpr (CODES) {
@@ -191,13 +207,13 @@ __global__ void __launch_bounds__(256) k_adamw(List list, Adam a) {
       sm[b] = any ? e.m_scale[b0 + b] : 0.0f;
       sv[b] = any ? e.v_scale[b0 + b] : 0.0f;
     } else {
-      load4(reinterpret_cast<float *>(e.m) + i, left, m[b]);
-      load4(reinterpret_cast<float *>(e.v) + i, left, v[b]);
+      load4(e.m + i, left, m[b]);
+      load4(e.v + i, left, v[b]);
     }
   }
 #pragma unroll
   for (int b = 0; b < ADAM_BLOCKS; ++b) {
-    const int64_t i = (b0 + b) * BLOCK + lane * 4, left = e.n - i;
+    const int64_t i = (b0 + b) * BLOCK + lane * 4, left = int64_t(e.n) - i;
     if ((b0 + b) * BLOCK >= e.n) break;
     float root[4];
     if constexpr (CODES) {
@@ -215,12 +231,12 @@ __global__ void __launch_bounds__(256) k_adamw(List list, Adam a) {
     }
     store4(e.p + i, left, p[b]);
     if constexpr (CODES) {
-      const Ctr4 r = philox_block(uint64_t(e.first + i) >> 2, 3, a.seed, a.t, 0);
+      const Ctr4 r = philox_block(list.quad + e.quad + (uint64_t(i) >> 2), 3, a.seed, a.t, 0);
       store_codes(e.m + i, left, encode<false>(m[b], r.v, e.m_scale + b0 + b, lane == 0));
       store_codes(e.v + i, left, encode<true>(root, r.v, e.v_scale + b0 + b, lane == 0));
     } else {
-      store4(reinterpret_cast<float *>(e.m) + i, left, m[b]);
-      store4(reinterpret_cast<float *>(e.v) + i, left, v[b]);
+      store4(e.m + i, left, m[b]);
+      store4(e.v + i, left, v[b]);
     }
   }
 }
@@ -235,15 +251,15 @@ __device__ __forceinline__ double wave_sum(double v) {
   for (int o = 32; o > 0; o /= 2) v += __shfl_xor(v, o);
   return v;
 }
-__global__ void __launch_bounds__(256) k_sum_squares(List list, double *part) {
+__global__ void __launch_bounds__(256) k_sum_squares(List<NormEntry> list, double *part) {
   __shared__ double waves[4];
   const int at = entry_of(list, blockIdx.x);
-  const Entry &e = list.e[at];
+  const NormEntry &e = list.e[at];
   const bool half = is_half(list, at);
   const int64_t i0 = int64_t(blockIdx.x - list.begin[at]) * NORM_CHUNK + threadIdx.x * 4;
   float g[NORM_QUADS][4];
 #pragma unroll
-  for (int q = 0; q < NORM_QUADS; ++q) load4(e.g, i0 + q * 1024, half, e.n - i0 - q * 1024, g[q]);
+  for (int q = 0; q < NORM_QUADS; ++q) load4(e.g, i0 + q * 1024, half, int64_t(e.n) - i0 - q * 1024, g[q]);
   double sum = 0.0;
 #pragma unroll
   for (int q = 0; q < NORM_QUADS; ++q)
@@ -272,37 +288,49 @@ __global__ void __launch_bounds__(1024) k_norm(const double *part, int64_t parts
 
 // ----------------------------------------------------------------------------- host side
 
-// Calls f(list, chunks) for each launch: lists of up to LIST tensors and MOST_CHUNKS chunks; longer
-// tensors go over several.
-constexpr int64_t MOST_CHUNKS = 1 << 23;                   // (a launch counts its threads in 32 bits)
-template <typename F>
-int for_lists(const fqt_param *t, int32_t count, int64_t chunk, int state_bytes, F &&f) {
-  List l{};
+// Calls f(list, chunks) for each launch of up to List::MOST entries and MOST_CHUNKS chunks; longer tensors have
+// several entries of SPAN elements.
+constexpr int64_t MOST_CHUNKS = 1 << 23, SPAN = 1 << 30;   // (a launch counts its threads in 32 bits)
+template <typename E, typename F>
+int for_lists(const fqt_param *t, int32_t count, int64_t chunk, F &&f) {
+  List<E> l{};
   int64_t chunks = 0;
   auto flush = [&]() -> int {
     if (!l.count) return FQT_OK;
     const int st = f(l, uint32_t(chunks));
-    l = List{};
+    l.count = 0;
+    std::fill(std::begin(l.half), std::end(l.half), 0u);
     chunks = 0;
     return st;
   };
   for (int32_t i = 0; i < count; ++i) {
-    for (int64_t at = 0; at < t[i].n;) {
-      if (l.count == LIST || chunks == MOST_CHUNKS) FQT_TRY_(flush());
-      const int64_t n = std::min(t[i].n - at, (MOST_CHUNKS - chunks) * chunk);
-      Entry &e = l.e[l.count];
+    for (int64_t at = 0; at < t[i].n; at += SPAN) {
+      const int64_t n = std::min(t[i].n - at, SPAN), c = (n + chunk - 1) / chunk;
+      if (l.count == List<E>::MOST || chunks + c > MOST_CHUNKS) FQT_TRY_(flush());
+      if constexpr (std::is_same_v<E, CodesEntry>) {
+        const uint64_t quad = uint64_t(t[i].first + at) / 4;
+        if (l.count && (quad < l.quad || quad - l.quad > UINT32_MAX)) FQT_TRY_(flush());
+        if (!l.count) l.quad = quad;
+      }
+      E &e = l.e[l.count];
       e.g = static_cast<const char *>(t[i].g) + at * elem_size(t[i].g_dtype);
-      if (t[i].p) e.p = t[i].p + at;
-      if (t[i].m) e.m = static_cast<char *>(t[i].m) + at * state_bytes;
-      if (t[i].v) e.v = static_cast<char *>(t[i].v) + at * state_bytes;
-      if (t[i].m_scale) e.m_scale = t[i].m_scale + at / BLOCK;
-      if (t[i].v_scale) e.v_scale = t[i].v_scale + at / BLOCK;
-      e.n = n;
-      e.first = t[i].first + at;
-      if (t[i].g_dtype == FQT_BF16) (l.count < 32 ? l.half : l.half_hi) |= 1u << l.count % 32;
-      l.begin[l.count++] = uint32_t(chunks);
-      chunks += (n + chunk - 1) / chunk;
-      at += n;
+      if constexpr (std::is_same_v<E, AdamEntry>) {
+        e.p = t[i].p + at;
+        e.m = static_cast<float *>(t[i].m) + at;
+        e.v = static_cast<float *>(t[i].v) + at;
+      } else if constexpr (std::is_same_v<E, CodesEntry>) {
+        e.p = t[i].p + at;
+        e.m = static_cast<char *>(t[i].m) + at;
+        e.v = static_cast<char *>(t[i].v) + at;
+        e.m_scale = t[i].m_scale + at / BLOCK;
+        e.v_scale = t[i].v_scale + at / BLOCK;
+        e.quad = uint32_t(uint64_t(t[i].first + at) / 4 - l.quad);
+      }
+      e.n = uint32_t(n);
+      l.begin[l.count] = uint32_t(chunks);
+      if (t[i].g_dtype == FQT_BF16) l.half[l.count / 32] |= 1u << l.count % 32;
+      ++l.count;
+      chunks += c;
     }
   }
   return flush();
@@ -352,7 +380,7 @@ extern "C" int fqt_grad_norm(const fqt_param *params, int32_t count, float max_n
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   double *part = static_cast<double *>(ws);
   int64_t done = 0;
-  FQT_TRY_(for_lists(params, count, NORM_CHUNK, 0, [&](const List &l, uint32_t chunks) {
+  FQT_TRY_(for_lists<NormEntry>(params, count, NORM_CHUNK, [&](const List<NormEntry> &l, uint32_t chunks) {
     k_sum_squares<<<dim3(chunks), dim3(256), 0, st>>>(l, part + done);
     done += chunks;
     return last_launch_status();
@@ -397,9 +425,11 @@ extern "C" int fqt_adamw_step(const fqt_adamw_cfg *cfg, const fqt_param *params,
   a.scale = grad_scale;
   if (!step_dev) at_step(a, step);
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
-  return for_lists(params, count, ADAM_CHUNK, codes ? 1 : 4, [&](const List &l, uint32_t chunks) {
-    if (codes) k_adamw<true><<<dim3(chunks), dim3(256), 0, st>>>(l, a);
-    else k_adamw<false><<<dim3(chunks), dim3(256), 0, st>>>(l, a);
-    return last_launch_status();
-  });
+  auto run = [&]<typename E>() {
+    return for_lists<E>(params, count, ADAM_CHUNK, [&](const List<E> &l, uint32_t chunks) {
+      k_adamw<E><<<dim3(chunks), dim3(256), 0, st>>>(l, a);
+      return last_launch_status();
+    });
+  };
+  return codes ? run.template operator()<CodesEntry>() : run.template operator()<AdamEntry>();
 }

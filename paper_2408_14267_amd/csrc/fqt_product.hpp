@@ -34,8 +34,14 @@ struct Gradients {
   int32_t dx_dtype, dw_dtype;
   float *part;             // part_bytes of either plan
   DbiasArgs bias;
+  int together;            // plan_together
 };
 int launch_gradients(const Gradients &g, hipStream_t st);
+// How dx and dw are launched: APART, one after the other by their plans, or in one launch of Small or of Large
+// tiles (those of the longer contraction first), where the tiles that a last round of one leaves CUs idle
+// with run beside those of the other.
+enum Together { APART, SMALL_BOTH, LARGE_BOTH };
+Together plan_together(int64_t M, int64_t N, int64_t K, const tile::Plan &dx, const tile::Plan &dw);
 
 // Rows of src (cols elements, stride ld) to rows of `pitch` elements, zero past cols.
 struct Copy {

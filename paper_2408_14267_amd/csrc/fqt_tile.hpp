@@ -545,6 +545,7 @@ struct Plan {
   Tiles t[2];
   int launches;
   uint32_t splits;
+  double us;               // what the costs below make of it
 };
 
 // us a step of a workgroup with one, two or three of them on a CU, and us before the first and after the last
@@ -598,7 +599,7 @@ inline Plan make_plan(int64_t M, int64_t N, int64_t steps, bool symmetric, const
   Plan best{};
   double cost = 1e30;
   auto take = [&](double c, const Plan &p) {
-    if (c < cost && launchable(p)) cost = c, best = p;
+    if (c < cost && launchable(p)) cost = c, best = p, best.us = c;
   };
   const double s = double(steps);
   const double entries = double(M) * double(N) * (symmetric ? 0.5 : 1.0);
