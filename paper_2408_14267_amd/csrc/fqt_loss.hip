@@ -580,6 +580,8 @@ int64_t piece_of(const Sizes &s) {
   return std::min(s.N, round_up((s.N + pieces - 1) / pieces, 256));
 }
 
+int64_t dz_pitch_of(int64_t n) { return n <= 512 ? round_up(n, 8) : (round_up(n, 64) / 64 | 1) * 64; }
+
 // Workspace of the backward: dz of a piece (twice for scaled operands), bf16 copies of operands that are codes
 // or whose rows are not whole pieces (w: of a piece), dx in float32 where several pieces add up to it,
 // the partial sums of dbias and those of the products.
@@ -601,7 +603,7 @@ PiecePlan plan_piece(const Sizes &s, int64_t n, int64_t K) {
 BwdWs bwd_ws(const fqt_loss_desc &d, const Sizes &s) {
   BwdWs f{};
   f.piece = piece_of(s);
-  f.dz_pitch = round_up(f.piece, 8);
+  f.dz_pitch = dz_pitch_of(f.piece);
   f.pitch = round_up(s.K, 8);
   f.copy_x = s.codes || !whole_pieces(s.K, s.ldx, 2);
   f.copy_w = s.codes || !whole_pieces(s.K, s.ldw, 2);
@@ -730,7 +732,7 @@ extern "C" int fqt_loss_backward(const fqt_loss_desc *d, const void *x, const vo
   char *base = static_cast<char *>(ws);
   const int64_t K = f.copy_x || f.copy_w ? f.pitch : s.K;
   for (int64_t first = 0; first < s.N; first += f.piece) {
-    const int64_t n = std::min(f.piece, s.N - first), dz_pitch = round_up(n, 8);
+    const int64_t n = std::min(f.piece, s.N - first), dz_pitch = dz_pitch_of(n);
     const PiecePlan plan = plan_piece(s, n, K);
     // The operands along k (for z) and along the features (for the gradients).
     Copy cx{}, cw{};
@@ -764,7 +766,7 @@ extern "C" int fqt_loss_backward(const fqt_loss_desc *d, const void *x, const vo
     Gradients g{};
     g.M = s.M; g.N = n; g.K = s.K;
     g.dzx = {base + f.dzx, dz_pitch * 2, s.M};
-    g.dzw = {base + f.dzw, dz_pitch * 2, dz_pitch};
+    g.dzw = {base + f.dzw, dz_pitch * 2, round_up(n, 8)};
     g.w = {wr.p, wr.ld, f.copy_w ? f.pitch : s.K};
     g.x = {xr.p, xr.ld, f.copy_x ? f.pitch : s.K};
     g.plan_dx = plan.dx; g.plan_dw = plan.dw;
