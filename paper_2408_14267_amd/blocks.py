@@ -1,9 +1,10 @@
-"""Residual blocks and an optimizer around binary layers: torch modules over the dense operators.
+"""Residual blocks, a loss and optimizers around binary layers: torch modules over the dense operators.
 
 RMSNorm, Linear and NormLinear call fqt_rmsnorm_*, fqt_quantize_rows and fqt_linear_* (forward and
 backward); NormLinear keeps the activations between the norm and the product as 8-bit codes.  Muon
-updates latent weight matrices (and convolution weights, unfolded) by fqt_muon_step.  ResidualMLP puts
-them together with BinaryLinear: a float32 residual stream, blocks of a normed 8-bit expansion with
+updates latent weight matrices (and convolution weights, unfolded) by fqt_muon_step.  Linear.loss is the softmax
+cross entropy of a layer's outputs without computing them as a matrix (fqt_loss_*); AdamW updates all tensors of a model
+by fqt_adamw_step, with states in float32 or 8 bits, clipped by fqt_grad_norm.  ResidualMLP puts them together with BinaryLinear: a float32 residual stream, blocks of a normed 8-bit expansion with
 GELU and a binary projection, the first and last layers at full width as in the networks of `train`.
 
 Modules take [..., features] inputs of float32 or bfloat16, keep float32 parameters, and cast or
@@ -16,7 +17,7 @@ import torch
 import torch.nn as nn
 from torch.autograd.function import once_differentiable
 
-from . import dense, train
+from . import dense, step, train
 
 _BF16, _F32 = torch.bfloat16, torch.float32
 
@@ -138,6 +139,37 @@ class _LinearFn(torch.autograd.Function):
         return dx, (dy if ctx.residual else None), dw, db, None
 
 
+class _LossFn(torch.autograd.Function):
+    @staticmethod
+    def forward(ctx, x, w, bias, target, mod, smoothing, ignore, mean):
+        (M, K), N = x.shape, w.shape[0]
+        xq, x_scale = _quantized(x, mod.operands)
+        wq, w_scale = _quantized(w, mod.operands)
+        desc = step.loss_desc(M, N, K, x_dtype=mod.operands, dx_dtype=x.dtype, dw_dtype=_F32, smoothing=smoothing,
+                              ignore=ignore)
+        loss, lse = torch.empty(M, device=x.device), torch.empty(M, device=x.device)
+        average = torch.empty(2, device=x.device) if mean else None
+        step.fqt_loss_forward(desc, xq, wq, target, loss, lse, _workspace(step.fqt_loss_workspace_size(desc), x.device),
+                              bias=bias, x_scale=x_scale, w_scale=w_scale, mean=average)
+        ctx.save_for_backward(xq, x_scale, wq, w_scale, bias, target, lse, average)
+        ctx.desc = desc
+        return average[0].clone() if mean else loss
+
+    @staticmethod
+    @once_differentiable
+    def backward(ctx, d):
+        xq, x_scale, wq, w_scale, bias, target, lse, average = ctx.saved_tensors
+        desc, (need_x, need_w, need_bias) = ctx.desc, ctx.needs_input_grad[:3]
+        dx = torch.empty(desc.M, desc.K, dtype=dense._TORCH_OF[desc.dx_dtype], device=d.device) if need_x else None
+        dw = torch.empty(desc.N, desc.K, device=d.device) if need_w else None
+        db = torch.empty(desc.N, device=d.device) if need_bias else None
+        given = dict(dloss=d.contiguous()) if average is None else dict(dmean=d.reshape(1), mean=average)
+        ws = _workspace(step.fqt_loss_workspace_size(desc, True), d.device)
+        step.fqt_loss_backward(desc, xq, wq, target, lse, ws, bias=bias, x_scale=x_scale, w_scale=w_scale, dx=dx, dw=dw,
+                               dbias=db, **given)
+        return dx, dw, db, None, None, None, None, None
+
+
 class Linear(nn.Module):
     """act(x W^T + bias) + residual with bf16, int8 or e4m3 operands (quantized per row, gradients passed
     through the rounding)."""
@@ -154,6 +186,22 @@ class Linear(nn.Module):
         r = None if residual is None else _rows(residual, self.fout, "residual")
         y = _LinearFn.apply(_rows(x, self.fin, "x"), r, self.weight, self.bias, self)
         return y.view(*x.shape[:-1], self.fout)
+
+    def loss(self, x, target, smoothing=0.0, ignore=-100, reduction="mean"):
+        """The softmax cross entropy of this layer's outputs for x against class numbers (int64, of x's shape
+        without its last dimension), without computing the outputs as a matrix.  Rows whose target is `ignore` are left
+        out; any other target that is no class gives NaN.  reduction: "mean" over the rows that count (0 if none
+        does) or "none"."""
+        if self.act != "none":
+            raise ValueError(f"loss: the outputs of a layer with activation {self.act} are no logits")
+        if reduction not in ("mean", "none"):
+            raise ValueError(f"loss: unknown reduction {reduction!r}: mean, none")
+        if target.dtype != torch.int64 or target.shape != x.shape[:-1] or target.device != x.device:
+            raise ValueError(f"loss: target: int64 {tuple(x.shape[:-1])} on {x.device} is needed, got {target.dtype} "
+                             f"{tuple(target.shape)} on {target.device}")
+        y = _LossFn.apply(_rows(x, self.fin, "x"), self.weight, self.bias, target.reshape(-1).contiguous(), self,
+                          smoothing, ignore, reduction == "mean")
+        return y if reduction == "mean" else y.view(target.shape)
 
 
 class _NormLinearFn(torch.autograd.Function):
@@ -291,6 +339,171 @@ class Muon(torch.optim.Optimizer):
         return loss
 
 
+def _flat(t):
+    """The elements of t in memory order, or None where they have gaps or overlap."""
+    expected = 1
+    for stride, size in sorted((s, n) for s, n in zip(t.stride(), t.shape) if n != 1):
+        if stride != expected:
+            return None
+        expected *= size
+    return t.detach().as_strided((t.numel(),), (1,))
+
+
+class AdamW(torch.optim.Optimizer):
+    """AdamW for float32 weights of any shape, all tensors of a group in one fqt_adamw_step.  states: "f32", or "e4m3"
+    for 8-bit states, stochastically rounded with the random sequence of `seed` (2 bytes a weight instead of 8).
+    max_norm: the gradients are clipped to this norm over all groups; `grad_norm` holds the last step's norm
+    and factor (on the device).  capturable: the step number is counted on the device (one for each group, weights without a
+    gradient included), so that step() may be captured into a graph; the learning rate is then the captured one.
+    What cannot be updated is refused when its group is added or before a step updates anything."""
+
+    def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, states="f32", seed=0,
+                 max_norm=None, capturable=False):
+        if states not in ("f32", "e4m3"):
+            raise ValueError(f"states {states!r}: f32, e4m3")
+        if max_norm is not None and not max_norm > 0:
+            raise ValueError(f"max_norm {max_norm}: out of range")
+        self.states, self.seed, self.max_norm, self.capturable = states, seed, max_norm, capturable
+        self.grad_norm = None
+        self._lists = {}
+        super().__init__(params, dict(lr=lr, betas=betas, eps=eps, weight_decay=weight_decay))
+
+    def add_param_group(self, param_group):
+        super().add_param_group(param_group)
+        group = self.param_groups[-1]
+        try:
+            self._config(group)
+            for p in group["params"]:
+                if p.dtype != _F32 or _flat(p) is None:
+                    raise ValueError(f"AdamW updates float32 weights without gaps, got {p.dtype} {tuple(p.shape)}, "
+                                     f"strides {p.stride()}")
+        except Exception:
+            self.param_groups.pop()
+            raise
+
+    def _config(self, group):
+        lr, (beta1, beta2), eps, decay = group["lr"], group["betas"], group["eps"], group["weight_decay"]
+        if not (0 <= lr < math.inf and 0 <= beta1 < 1 and 0 <= beta2 < 1 and 0 <= eps < math.inf and
+                0 <= decay < math.inf):
+            raise ValueError(f"lr {lr}, betas {group['betas']}, eps {eps}, weight_decay {decay}: out of range")
+        return step.adamw_cfg(lr=lr, beta1=beta1, beta2=beta2, eps=eps, weight_decay=decay, seed=self.seed,
+                              states=self.states)
+
+    def _state(self, p):
+        state = self.state[p]
+        if "m" not in state:
+            self._not_captured("states are made")
+            state["step"] = 0
+            if self.states == "f32":
+                state["m"], state["v"] = torch.zeros_like(p), torch.zeros_like(p)
+            else:
+                blocks = -(-p.numel() // step.FQT_STATE_BLOCK)
+                for name in ("m", "v"):
+                    state[name] = torch.zeros(p.numel(), dtype=torch.float8_e4m3fn, device=p.device)
+                    state[name + "_scale"] = torch.zeros(blocks, device=p.device)
+        return state
+
+    @staticmethod
+    def _not_captured(what):
+        if torch.cuda.is_current_stream_capturing():
+            raise RuntimeError(f"AdamW: {what} in the first step: take one before a capture")
+
+    def _gradient(self, p):
+        """p's gradient, its elements in p's memory order."""
+        g = p.grad
+        if g.layout != torch.strided or g.dtype not in (_F32, _BF16) or p.device.type != "cuda" or                 p.device.index != torch.cuda.current_device():
+            raise ValueError(f"AdamW updates weights with dense float32 or bfloat16 gradients on the current device, got "
+                             f"{g.layout} {g.dtype} on {p.device}")
+        if g.stride() != p.stride():
+            g = torch.empty_like(p, dtype=g.dtype).copy_(g)
+        return g if g.is_contiguous() else _flat(g)
+
+    def _list(self, key, params, starts):
+        """The ParamList of some weights and their states, made again when any of them has moved."""
+        states = [self._state(p) for p in params]
+        held = [(p.data_ptr(), s["m"].data_ptr(), s["v"].data_ptr()) for p, s in zip(params, states)]
+        at = self._lists.get(key)
+        if at is None or at[0] != held:
+            flat = {k: [_flat(s[k]) for s in states] for k in ("m", "v")}
+            for k in ("m_scale", "v_scale"):
+                flat[k] = [s[k] for s in states] if self.states == "e4m3" else None
+            weights = [_flat(p) for p in params]
+            at = self._lists[key] = held, step.param_list(weights, weights, flat["m"], flat["v"], flat["m_scale"],
+                                                          flat["v_scale"], first=starts)
+        return at[1]
+
+    @torch.no_grad()
+    def step(self, closure=None):
+        loss = None
+        if closure is not None:
+            with torch.enable_grad():
+                loss = closure()
+        if not self.capturable and torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
+            raise RuntimeError("AdamW: a captured step would keep its number: make the optimizer capturable")
+        # weights with a gradient, by group and by how many steps they have taken
+        todo, gradients, at = {}, [], 0
+        for i, group in enumerate(self.param_groups):
+            cfg = self._config(group)
+            for p in group["params"]:
+                if p.grad is not None and p.numel():
+                    g = self._gradient(p)
+                    t = 0 if self.capturable else self.state[p].get("step", 0)
+                    todo.setdefault((i, t), (cfg, [], [], []))
+                    for held, value in zip(todo[i, t][1:], (p, g, at)):
+                        held.append(value)
+                    gradients.append(g)
+                at += -(-p.numel() // step.FQT_STATE_BLOCK) * step.FQT_STATE_BLOCK
+        if not todo:
+            return loss
+        lists = []
+        for (i, t), (cfg, params, g, starts) in todo.items():
+            params_list = self._list((i, tuple(starts)), params, starts)
+            params_list.set_gradients(g)
+            lists.append((i, t, cfg, params, params_list))
+        scale = None
+        if self.max_norm is not None:
+            whole = lists[0][4] if len(lists) == 1 else step.param_list(gradients)
+            if self.grad_norm is None:
+                self.grad_norm = torch.empty(2, device=gradients[0].device)
+            step.fqt_grad_norm(whole, self.grad_norm, _workspace(step.fqt_grad_norm_workspace_size(whole),
+                                                                 self.grad_norm.device), max_norm=self.max_norm)
+            scale = self.grad_norm[1:]
+        for i, t, cfg, params, params_list in lists:
+            if self.capturable:
+                group = self.param_groups[i]
+                if group.get("clock") is None:
+                    self._not_captured("the step counter is made")
+                    group["clock"] = torch.zeros(1, dtype=torch.int64, device=params[0].device)
+                number = group["clock"].add_(1)
+            else:
+                number = t + 1
+                for p in params:
+                    self.state[p]["step"] = number
+            step.fqt_adamw_step(cfg, params_list, number, grad_scale=scale)
+        return loss
+
+    def load_state_dict(self, state_dict):
+        if any(("m_scale" in s) != (self.states == "e4m3") for s in state_dict["state"].values()):
+            raise ValueError(f"a state of another kind than {self.states}")
+        super().load_state_dict(state_dict)
+        self._lists = {}
+        for state in self.state.values():
+            if self.states == "e4m3":          # (loading casts to the weights' type, which holds the codes exactly)
+                for name in ("m", "v"):
+                    state[name] = state[name].to(torch.float8_e4m3fn)
+
+
+def grad_norm(params, max_norm=math.inf):
+    """The norm of the gradients of params, and the factor that clips them to max_norm: two scalars on the device."""
+    g = [p.grad if p.grad.is_contiguous() else p.grad.contiguous() for p in params if p.grad is not None]
+    if not g:
+        raise ValueError("grad_norm: no gradients")
+    listed = step.param_list(g)
+    out = torch.empty(2, device=g[0].device)
+    step.fqt_grad_norm(listed, out, _workspace(step.fqt_grad_norm_workspace_size(listed), out.device), max_norm=max_norm)
+    return out[0], out[1]
+
+
 class Optimizers:
     """Several optimizers behind the interface that train.train_step uses, with one checkpoint.  A scheduler
     takes one of `optimizers`; param_groups has the groups of all."""
@@ -321,15 +534,19 @@ class Optimizers:
             o.load_state_dict(s)
 
 
-def muon_and_adam(model, lr=0.02, adam_lr=1e-3, first_last=()):
+def muon_and_adam(model, lr=0.02, adam_lr=1e-3, first_last=(), states=None, max_norm=None):
     """Muon for the weight matrices of a model, Adam for its vectors and for the modules in first_last
-    (input and output layers, whose singular values carry meaning)."""
+    (input and output layers, whose singular values carry meaning).  states: None for torch's Adam, "f32" or "e4m3" for
+    AdamW here, with max_norm."""
+    if states is None and max_norm is not None:
+        raise ValueError("max_norm comes with states")
     apart = {id(p) for m in first_last for p in m.parameters()}
     matrices = [p for p in model.parameters() if p.dim() >= 2 and id(p) not in apart]
     chosen = {id(p) for p in matrices}
     rest = [p for p in model.parameters() if id(p) not in chosen]
     return Optimizers(*([Muon(matrices, lr=lr)] if matrices else []),
-                      *([torch.optim.Adam(rest, lr=adam_lr)] if rest else []))
+                      *([torch.optim.Adam(rest, lr=adam_lr) if states is None else
+                         AdamW(rest, lr=adam_lr, states=states, max_norm=max_norm)] if rest else []))
 
 
 class ResidualMLP(nn.Module):
@@ -345,7 +562,8 @@ class ResidualMLP(nn.Module):
         self.norm = RMSNorm(width)
         self.head = Linear(width, classes)
 
-    def forward(self, x):
+    def features(self, x):
+        """What the head reads."""
         h, add = self.stem(x), None
         for up, down in zip(self.up, self.down):
             if add is None:
@@ -353,5 +571,11 @@ class ResidualMLP(nn.Module):
             else:
                 z, h = up(add, h)
             add = down(nn.functional.hardtanh(z))
-        y = self.norm(h) if add is None else self.norm(add, h)[0]
-        return self.head(y)
+        return self.norm(h) if add is None else self.norm(add, h)[0]
+
+    def forward(self, x):
+        return self.head(self.features(x))
+
+    def loss(self, x, target, **kw):
+        """The loss of forward(x), without its logits (Linear.loss)."""
+        return self.head.loss(self.features(x), target, **kw)

@@ -224,10 +224,13 @@ class ResNet18(nn.Module):
         return self.fc(torch.flatten(F.adaptive_avg_pool2d(x, 1), 1))
 
 
-def train_step(model, opt, x, y, autocast_dtype=None):
-    """One step: forward, cross-entropy loss, backward, Adam update.  Returns the loss."""
+def train_step(model, opt, x, y, autocast_dtype=None, fused_loss=False):
+    """One step: forward, cross-entropy loss, backward, optimizer update.  Returns the loss.  fused_loss: by
+    model.loss(x, y), which computes no logits (blocks.ResidualMLP)."""
     opt.zero_grad(set_to_none=True)
-    if autocast_dtype is not None:
+    if fused_loss:
+        loss = model.loss(x, y)
+    elif autocast_dtype is not None:
         with torch.autocast("cuda", dtype=autocast_dtype):
             loss = F.cross_entropy(model(x), y)
     else:
