@@ -47,28 +47,30 @@ template <> struct Acc<I8K> { typedef i32x4 type; };
 template <int KIND> constexpr int elem_bytes = KIND == I8K || KIND == E4M3K ? 1 : KIND == SPLITK ? 4 : 2;
 
 // acc += w-fragment (rows of the result tile) x x-fragment (columns) over one 128-byte step, from
-// the two 16-byte pieces of each.  Lane l of the result holds n = 4 (l / 16) + i, m = l % 16.
-template <int KIND>
-__device__ __forceinline__ void mma(typename Acc<KIND>::type &acc, const i32x4 (&w)[2], const i32x4 (&x)[2]) {
+// the two 16-byte pieces of each, in mma_parts instructions.  Lane l of the result holds n = 4 (l / 16) + i, m = l % 16.
+template <int KIND> constexpr int mma_parts = KIND == E4M3K ? 1 : KIND == SPLITK ? 3 : 2;
+template <int KIND, int PART>
+__device__ __forceinline__ void mma_part(typename Acc<KIND>::type &acc, const i32x4 (&w)[2], const i32x4 (&x)[2]) {
   if constexpr (KIND == BF16K) {
-#pragma unroll
-    for (int s = 0; s < 2; ++s)
-      acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[s]),
-                                                    __builtin_bit_cast(bf16x8, x[s]), acc, 0, 0, 0);
-  } else if constexpr (KIND == SPLITK) {
-    auto h = [](const i32x4 &v) { return __builtin_bit_cast(f16x8, v); };
-    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(h(w[0]), h(x[1]), acc, 0, 0, 0);
-    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(h(w[1]), h(x[0]), acc, 0, 0, 0);
-    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(h(w[0]), h(x[0]), acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, w[PART]),
+                                                  __builtin_bit_cast(bf16x8, x[PART]), acc, 0, 0, 0);
+  } else if constexpr (KIND == SPLITK) {               // hi lo, lo hi, hi hi
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, w[PART == 1]),
+                                                 __builtin_bit_cast(f16x8, x[PART == 0]), acc, 0, 0, 0);
   } else if constexpr (KIND == I8K) {
-#pragma unroll
-    for (int s = 0; s < 2; ++s) acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[s], x[s], acc, 0, 0, 0);
+    acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[PART], x[PART], acc, 0, 0, 0);
   } else {
     // unit scales (exponent 127) and e4m3 on both sides
     const i32x8 a = __builtin_shufflevector(w[0], w[1], 0, 1, 2, 3, 4, 5, 6, 7);
     const i32x8 b = __builtin_shufflevector(x[0], x[1], 0, 1, 2, 3, 4, 5, 6, 7);
     acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, acc, 0, 0, 0, 0x7F7F7F7F, 0, 0x7F7F7F7F);
   }
+}
+template <int KIND>
+__device__ __forceinline__ void mma(typename Acc<KIND>::type &acc, const i32x4 (&w)[2], const i32x4 (&x)[2]) {
+  mma_part<KIND, 0>(acc, w, x);
+  if constexpr (mma_parts<KIND> > 1) mma_part<KIND, 1>(acc, w, x);
+  if constexpr (mma_parts<KIND> > 2) mma_part<KIND, 2>(acc, w, x);
 }
 
 // One operand as a kernel argument: `rows` x K elements, row stride ld bytes (of a k row in COLS, of a
@@ -195,6 +197,42 @@ __device__ __forceinline__ void read_cols(const char *a, const char *b, i32x4 (&
   y[1] = __builtin_shufflevector(r[6], r[7], 0, 1, 2, 3);
 }
 
+// The same for four fragments, from the lane's addresses a[0 ... 3].
+template <int LINES>
+__device__ __forceinline__ void read_cols4(const char *lds, const uint32_t *a, i32x4 (&o)[4][2]) {
+  typedef int i32x2 __attribute__((ext_vector_type(2)));
+  i32x2 r[16];
+  const uint32_t at = (uint32_t)(uintptr_t)lds;
+  asm volatile(
+      "ds_read_b64_tr_b16 %0, %16\n"
+      "ds_read_b64_tr_b16 %1, %16 offset:%20\n"
+      "ds_read_b64_tr_b16 %2, %16 offset:%21\n"
+      "ds_read_b64_tr_b16 %3, %16 offset:%22\n"
+      "ds_read_b64_tr_b16 %4, %17\n"
+      "ds_read_b64_tr_b16 %5, %17 offset:%20\n"
+      "ds_read_b64_tr_b16 %6, %17 offset:%21\n"
+      "ds_read_b64_tr_b16 %7, %17 offset:%22\n"
+      "ds_read_b64_tr_b16 %8, %18\n"
+      "ds_read_b64_tr_b16 %9, %18 offset:%20\n"
+      "ds_read_b64_tr_b16 %10, %18 offset:%21\n"
+      "ds_read_b64_tr_b16 %11, %18 offset:%22\n"
+      "ds_read_b64_tr_b16 %12, %19\n"
+      "ds_read_b64_tr_b16 %13, %19 offset:%20\n"
+      "ds_read_b64_tr_b16 %14, %19 offset:%21\n"
+      "ds_read_b64_tr_b16 %15, %19 offset:%22\n"
+      "s_waitcnt lgkmcnt(0)"
+      : "=&v"(r[0]), "=&v"(r[1]), "=&v"(r[2]), "=&v"(r[3]), "=&v"(r[4]), "=&v"(r[5]), "=&v"(r[6]), "=&v"(r[7]),
+        "=&v"(r[8]), "=&v"(r[9]), "=&v"(r[10]), "=&v"(r[11]), "=&v"(r[12]), "=&v"(r[13]), "=&v"(r[14]), "=&v"(r[15])
+      : "v"(at + a[0]), "v"(at + a[1]), "v"(at + a[2]), "v"(at + a[3]), "i"(4 * LINES * 2), "i"(32 * LINES * 2),
+        "i"(36 * LINES * 2)
+      : "memory");
+#pragma unroll
+  for (int f = 0; f < 4; ++f) {
+    o[f][0] = __builtin_shufflevector(r[4 * f], r[4 * f + 1], 0, 1, 2, 3);
+    o[f][1] = __builtin_shufflevector(r[4 * f + 2], r[4 * f + 3], 0, 1, 2, 3);
+  }
+}
+
 // Fragment reads of one operand's step by a wave: FRAGS tiles of 16 lines from line0.
 template <int LAYOUT, int LINES, int FRAGS>
 struct Reader {
@@ -214,6 +252,11 @@ struct Reader {
         at[i] = k * (LINES * 2) + piece * 16 + (l & 1) * 8;
       }
     }
+  }
+  // Fragments i ... i + 3, COLS ones with their own wait.
+  __device__ __forceinline__ void read4(const char *lds, int i, i32x4 (&o)[4][2]) const {
+    if constexpr (by_rows(LAYOUT)) read<false>(lds, i, o);
+    else read_cols4<LINES>(lds, at + i, o);
   }
   // Fragments i ... i + N - 1.  WHOLE: COLS fragments come with their own wait (read_cols).
   template <bool WHOLE, int N>
@@ -266,15 +309,15 @@ struct Feed {
   }
 };
 
-// BM x BN outputs by WM x WN waves, through BUFS step buffers.
-template <int BM_, int BN_, int WM_, int WN_, int BUFS_ = 2>
+// BM x BN outputs by WM x WN waves, through BUFS step buffers (XBUFS of x).
+template <int BM_, int BN_, int WM_, int WN_, int BUFS_ = 2, int XBUFS_ = BUFS_>
 struct Shape {
   static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, BUFS = BUFS_;
   static constexpr int THREADS = 64 * WM * WN;
   static constexpr int TM = BM / WM, TN = BN / WN;        // outputs of a wave
   static constexpr int FM = TM / 16, FN = TN / 16;
   static constexpr int BUF = (BM + BN) * KB;              // bytes of one step
-  static constexpr int LDS = BUFS * BUF;
+  static constexpr int LDS = (XBUFS_ * BM + BUFS * BN) * KB;
 };
 
 // A barrier of the workgroup that waits for nothing else: what has to be complete is waited for by
@@ -356,21 +399,18 @@ __device__ __forceinline__ void run_tile(const Operand &x, const Operand &w, int
 
 // The same for workgroups of eight waves, two per SIMD, with 256 or so outputs a side: while one wave
 // of a SIMD issues matrix instructions, the other one reads fragments and starts loads.  Waves 4-7
-// run one barrier behind waves 0-3 for that.  A step is four quarters of a wave's tile, each a
-// reading phase and a matrix phase with a barrier after it:
-//   quarter   fragments read            step loaded (half of its pieces per quarter)
-//   0         x, first half             x of step t + 1, into the other buffer
-//   1         w, second half            x of step t + 1
-//   2         x, second half            w of step t + 2, into this buffer (w is read by now)
-//   3         w, first half, step t+1   w of step t + 2
-// so that w has four, x two to four quarters to arrive.  A wave waits for its own loads at the end of
-// the reading phase before the one that needs them, and the barrier between makes them everyone's.
+// run one barrier behind waves 0-3 for that.  A step is two halves of a wave's tile, each a
+// reading phase and a matrix phase of 512 cycles with a barrier after it:
+//   half   fragments read          step loaded
+//   0      x, first half; w        x of step t + 2, into the third buffer
+//   1      x, second half          w of step t + 2, into this buffer (w is read by now)
+// so that x has eight, w six phases to arrive.  A wave waits for its own loads at the end of the reading
+// phase before the one that needs them, and the barrier between makes them everyone's.
 template <int KIND, int LX, int LW, typename S>
 __device__ __forceinline__ void run_tile8(const Operand &x, const Operand &w, int64_t K,
                                           int64_t m0, int64_t n0, int64_t t0, int64_t t1, char *lds,
                                           typename Acc<KIND>::type (&acc)[S::FM][S::FN]) {
-  static_assert(S::THREADS == 512 && S::FM % 2 == 0 && S::FN % 2 == 0 && S::BUFS == 2, "tiles in quarters");
-  constexpr int HM = S::FM / 2, HN = S::FN / 2;
+  static_assert(S::THREADS == 512 && S::FM == 8 && S::FN == 4 && S::LDS == (3 * S::BM + 2 * S::BN) * KB, "tiles in halves");
   const uint32_t wave = wave_id();
   Reader<LX, S::BM, S::FM> rx;
   Reader<LW, S::BN, S::FN> rw;
@@ -382,47 +422,46 @@ __device__ __forceinline__ void run_tile8(const Operand &x, const Operand &w, in
   Feed<KIND, LW, S::BN, S::THREADS> gw;
   gx.init(x, K, m0, t0, t1);
   gw.init(w, K, n0, t0, t1);
-  constexpr int NX = gx.g.PER, NW = gw.g.PER, NX0 = (NX + 1) / 2, NW0 = (NW + 1) / 2;
-  auto xbuf = [&](int b) { return lds + b * S::BUF; };
-  auto wbuf = [&](int b) { return lds + b * S::BUF + S::BM * KB; };
-  gw.load(wbuf(0));
-  gx.load(xbuf(0));
-  gw.load(wbuf(1));
-  wait_loads<NW>();
+  constexpr int NX = gx.g.PER, NW = gw.g.PER;
+  constexpr uint32_t XBUF = S::BM * KB, WBUF = S::BN * KB;
+  char *const xs = lds, *const ws = lds + 3 * XBUF;
+  gw.load(ws);
+  gx.load(xs);
+  gw.load(ws + WBUF);
+  gx.load(xs + XBUF);
+  wait_loads<NX + NW>();
   barrier_only();
-  i32x4 fx[HM][2], fa[HN][2], fb[HN][2], fn[HN][2];
-  rw.template read<false>(wbuf(0), 0, fn);
   if (wave >= 4) barrier_only();
-  auto quarter = [&](int m, int n, i32x4 (&f)[HN][2]) {
+  i32x4 fx[4][2], fw[4][2];
+  auto half = [&](int m) {
     wait_lds();
     barrier_only();
     __builtin_amdgcn_s_setprio(1);
+    auto part = [&]<int P>() {
 #pragma unroll
-    for (int i = 0; i < HM; ++i)
+      for (int i = 0; i < 4; ++i)
 #pragma unroll
-      for (int j = 0; j < HN; ++j) mma<KIND>(acc[m + i][n + j], f[j], fx[i]);
+        for (int j = 0; j < 4; ++j) mma_part<KIND, P>(acc[m + i][j], fw[j], fx[i]);
+    };
+    part.template operator()<0>();
+    if constexpr (mma_parts<KIND> > 1) part.template operator()<1>();
+    if constexpr (mma_parts<KIND> > 2) part.template operator()<2>();
     __builtin_amdgcn_s_setprio(0);
     barrier_only();
   };
-  int buf = 0;
+  char *xat = xs, *xto = xs + 2 * XBUF, *wat = ws;
   for (int64_t t = t0; t < t1; ++t) {
-#pragma unroll
-    for (int j = 0; j < HN; ++j) fa[j][0] = fn[j][0], fa[j][1] = fn[j][1];
-    rx.template read<false>(xbuf(buf), 0, fx);
-    gx.template load<0, NX0>(xbuf(buf ^ 1));
-    quarter(0, 0, fa);
-    rw.template read<false>(wbuf(buf), HN, fb);
-    gx.template load<NX0, NX>(xbuf(buf ^ 1));
-    quarter(0, HN, fb);
-    rx.template read<false>(xbuf(buf), HM, fx);
-    gw.template load<0, NW0>(wbuf(buf));
-    wait_loads<NX + NW0>();                                // w of step t + 1
-    quarter(HM, HN, fb);
-    rw.template read<false>(wbuf(buf ^ 1), 0, fn);
-    gw.template load<NW0, NW>(wbuf(buf));
-    wait_loads<NW>();                                      // x of step t + 1
-    quarter(HM, 0, fa);
-    buf ^= 1;
+    rx.read4(xat, 0, fx);
+    rw.read4(wat, 0, fw);
+    gx.load(xto);
+    half(0);
+    rx.read4(xat, 4, fx);
+    gw.load(wat);
+    wait_loads<NX + NW>();                                 // both of step t + 1
+    half(4);
+    xto = xat;
+    xat = xat == xs + 2 * XBUF ? xs : xat + XBUF;
+    wat = wat == ws ? ws + WBUF : ws;
   }
   if (wave < 4) barrier_only();
   wait_loads<0>();
@@ -520,7 +559,7 @@ struct StorePart {
 
 // ----------------------------------------------------------------------------- plans
 // The shapes of a workgroup's tile.
-using Large = Shape<256, 256, 2, 4>;
+using Large = Shape<256, 256, 2, 4, 2, 3>;
 using Middle = Shape<128, 128, 2, 2>;
 using Small = Shape<64, 64, 2, 2, 3>;
 enum ShapeId { LARGE, MIDDLE, SMALL };
