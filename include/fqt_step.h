@@ -30,8 +30,8 @@ extern "C" {
  * small (the largest z is left out of the sum that is added to it).
  * mean, float32 [2], optional: the mean loss over the rows that count, and 1 / their number; both 0 if none
  * does.
- * Sums are exact in int32 for FQT_I8 (K <= 133144), float32 otherwise (FQT_E4M3 through bf16 copies of the
- * codes).  N >= 1; sizes as in fqt_linear_forward. */
+ * Sums are exact in int32 for FQT_I8 (K <= 133144), float32 otherwise (of FQT_E4M3 too: the matrix cores take
+ * its codes widened to bf16).  N >= 1; sizes as in fqt_linear_forward. */
 typedef struct {
   int64_t M, N, K;                    /* rows, classes, features                                 */
   int64_t ldx, ldw, lddx, lddw;

@@ -540,9 +540,12 @@ int check_pointers(const fqt_loss_desc &d, const Sizes &s, const void *x, const 
 // those of w.
 constexpr int64_t FEW_ROWS = 4;
 
-// Workspace of the forward: copies of operands whose rows are not whole 16-byte pieces (e4m3: bf16 copies),
+// us a step and before and after the steps of widened codes (as tile::DENSE_COSTS).
+constexpr tile::Costs WIDE_COSTS{{2.9}, {1.1, 1.6}, {0.35, 0.55, 0.85}, {6, 5, 4}};
+
+// Workspace of the forward: copies of operands whose rows are not whole 16-byte pieces,
 // z of few rows or partial sums, and pairs, sums and the targets' z.
-struct FwdWs { size_t x, w, part, pairs, sums, at, total; int64_t pitch, e, slots; tile::Plan plan; bool few, widen, copy_x, copy_w; };
+struct FwdWs { size_t x, w, part, pairs, sums, at, total; int64_t pitch, e, slots; tile::Plan plan; bool few, copy_x, copy_w; };
 FwdWs fwd_ws(const fqt_loss_desc &d, const Sizes &s) {
   FwdWs f{};
   f.few = s.M <= FEW_ROWS;
@@ -558,12 +561,12 @@ FwdWs fwd_ws(const fqt_loss_desc &d, const Sizes &s) {
     pairs(align256(size_t(s.M) * s.N * 4), chunks);
     return f;
   }
-  f.widen = d.x_dtype == FQT_E4M3;
-  f.e = f.widen ? 2 : int64_t(s.xe);
+  f.e = int64_t(s.xe);
   f.pitch = round_up(s.K, 16 / f.e);
-  f.copy_x = f.widen || !whole_pieces(s.K, s.ldx, s.xe);
-  f.copy_w = f.widen || !whole_pieces(s.K, s.ldw, s.xe);
-  f.plan = plan_of(s.M, s.N, s.K, f.e);
+  f.copy_x = !whole_pieces(s.K, s.ldx, s.xe);
+  f.copy_w = !whole_pieces(s.K, s.ldw, s.xe);
+  f.plan = d.x_dtype == FQT_E4M3 ? tile::make_plan(s.M, s.N, (s.K + tile::KB - 1) / tile::KB, false, WIDE_COSTS)
+                                 : plan_of(s.M, s.N, s.K, f.e);
   f.w = f.x + (f.copy_x ? align256(size_t(s.M) * f.pitch * f.e) : 0);
   f.part = f.w + (f.copy_w ? align256(size_t(s.N) * f.pitch * f.e) : 0);
   if (f.plan.splits > 1) pairs(f.part + part_bytes(f.plan, s.M, s.N), chunks);
@@ -695,11 +698,13 @@ extern "C" int fqt_loss_forward(const fqt_loss_desc *d, const void *x, const voi
       return {base + at, f.pitch * f.e, rows};
     };
     const Operand xo = operand(x, f.copy_x, f.x, s.M, s.ldx, &cx), wo = operand(w, f.copy_w, f.w, s.N, s.ldw, &cw);
-    FQT_TRY_(launch_copies(cx, cw, d->x_dtype, f.widen, st));
+    FQT_TRY_(launch_copies(cx, cw, d->x_dtype, false, st));
     const Logits p{xo, wo, s.M, s.N, f.copy_x || f.copy_w ? f.pitch : s.K, f.plan.t[0], x_scale, w_scale, bias,
                    reinterpret_cast<float *>(base + f.part), round_up(s.N, 8)};
     const bool ints = d->x_dtype == FQT_I8;
-    FQT_TRY_(ints ? launch_logits<tile::I8K>(f.plan, p, pairs, st) : launch_logits<tile::BF16K>(f.plan, p, pairs, st));
+    if (ints) FQT_TRY_(launch_logits<tile::I8K>(f.plan, p, pairs, st));
+    else if (s.codes) FQT_TRY_(launch_logits<tile::WIDEK>(f.plan, p, pairs, st));
+    else FQT_TRY_(launch_logits<tile::BF16K>(f.plan, p, pairs, st));
     if (f.plan.splits > 1) FQT_TRY_(launch_dense({p.part, x_scale, w_scale, bias, p.ldp, f.plan.splits}, pairs, o, ints, st));
     if (f.plan.splits == 1 || f.slots > 1) FQT_TRY_(launch_rows(pairs, o, st));
   }

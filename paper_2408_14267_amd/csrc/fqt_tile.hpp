@@ -10,6 +10,9 @@
 // The order of the k's inside a fragment does not matter as long as both operands use the same, so
 // 8-bit fragments are simply the 16-byte pieces l / 16 and 4 + l / 16 of a 128-byte row.
 //
+// WIDE operands are e4m3 codes, widened to bf16 (exact) between LDS and the matrix cores, for sums in float32: half the
+// bytes of bf16 copies, which are not written.
+//
 // SPLIT operands hold float16 pairs hi + lo in panels: panel c has the columns 32 c ... 32 c + 31 of
 // all rows, 128 bytes a row, the 32 hi before the 32 lo.  A step is 32 columns; the two pieces of a
 // fragment are its hi and its lo, and three matrix instructions (hi hi, hi lo, lo hi) feed on them: half
@@ -28,7 +31,7 @@
 namespace fqt {
 namespace tile {
 
-enum Kind { BF16K, SPLITK, I8K, E4M3K };
+enum Kind { BF16K, SPLITK, I8K, E4M3K, WIDEK };
 enum Layout { ROWS, COLS, PANEL_ROWS, PANEL_COLS };
 
 typedef float f32x4 __attribute__((ext_vector_type(4)));
@@ -44,11 +47,18 @@ constexpr bool by_rows(int layout) { return layout == ROWS || layout == PANEL_RO
 
 template <int KIND> struct Acc { typedef f32x4 type; };
 template <> struct Acc<I8K> { typedef i32x4 type; };
-template <int KIND> constexpr int elem_bytes = KIND == I8K || KIND == E4M3K ? 1 : KIND == SPLITK ? 4 : 2;
+template <int KIND> constexpr int elem_bytes = KIND == I8K || KIND == E4M3K || KIND == WIDEK ? 1 : KIND == SPLITK ? 4 : 2;
 
 // acc += w-fragment (rows of the result tile) x x-fragment (columns) over one 128-byte step, from
 // the two 16-byte pieces of each, in mma_parts instructions.  Lane l of the result holds n = 4 (l / 16) + i, m = l % 16.
-template <int KIND> constexpr int mma_parts = KIND == E4M3K ? 1 : KIND == SPLITK ? 3 : 2;
+template <int KIND> constexpr int mma_parts = KIND == E4M3K ? 1 : KIND == SPLITK ? 3 : KIND == WIDEK ? 4 : 2;
+// Eight codes as bf16.
+__device__ __forceinline__ bf16x8 widen8(int lo, int hi) {
+  typedef __bf16 bf16x2 __attribute__((ext_vector_type(2)));
+  const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(uint32_t(lo), 1.0f, false), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(uint32_t(lo), 1.0f, true),
+               c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(uint32_t(hi), 1.0f, false), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8(uint32_t(hi), 1.0f, true);
+  return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
+}
 template <int KIND, int PART>
 __device__ __forceinline__ void mma_part(typename Acc<KIND>::type &acc, const i32x4 (&w)[2], const i32x4 (&x)[2]) {
   if constexpr (KIND == BF16K) {
@@ -57,6 +67,10 @@ __device__ __forceinline__ void mma_part(typename Acc<KIND>::type &acc, const i3
   } else if constexpr (KIND == SPLITK) {               // hi lo, lo hi, hi hi
     acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, w[PART == 1]),
                                                  __builtin_bit_cast(f16x8, x[PART == 0]), acc, 0, 0, 0);
+  } else if constexpr (KIND == WIDEK) {
+    constexpr int H = PART % 2 * 2;
+    acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(widen8(w[PART / 2][H], w[PART / 2][H + 1]),
+                                                  widen8(x[PART / 2][H], x[PART / 2][H + 1]), acc, 0, 0, 0);
   } else if constexpr (KIND == I8K) {
     acc = __builtin_amdgcn_mfma_i32_16x16x64_i8(w[PART], x[PART], acc, 0, 0, 0);
   } else {
@@ -71,6 +85,7 @@ __device__ __forceinline__ void mma(typename Acc<KIND>::type &acc, const i32x4 (
   mma_part<KIND, 0>(acc, w, x);
   if constexpr (mma_parts<KIND> > 1) mma_part<KIND, 1>(acc, w, x);
   if constexpr (mma_parts<KIND> > 2) mma_part<KIND, 2>(acc, w, x);
+  if constexpr (mma_parts<KIND> > 3) mma_part<KIND, 3>(acc, w, x);
 }
 
 // One operand as a kernel argument: `rows` x K elements, row stride ld bytes (of a k row in COLS, of a
@@ -446,6 +461,7 @@ __device__ __forceinline__ void run_tile8(const Operand &x, const Operand &w, in
     part.template operator()<0>();
     if constexpr (mma_parts<KIND> > 1) part.template operator()<1>();
     if constexpr (mma_parts<KIND> > 2) part.template operator()<2>();
+    if constexpr (mma_parts<KIND> > 3) part.template operator()<3>();
     __builtin_amdgcn_s_setprio(0);
     barrier_only();
   };
