@@ -18,14 +18,15 @@ namespace {
 using tile::Operand;
 using tile::ROWS;
 
-constexpr float LOG2E = 1.44269504088896341f;
+constexpr float LOG2E = 1.44269504088896341f, LN2 = 0.69314718055994531f;
 __device__ __forceinline__ float exp_of(float v) { return __builtin_amdgcn_exp2f(v * LOG2E); }
 // (NaN if either is one)
 __device__ __forceinline__ float larger(float a, float b) { return __builtin_elementwise_maximum(a, b); }
 __device__ __forceinline__ float smaller(float a, float b) { return __builtin_elementwise_minimum(a, b); }
 
-// A set of z: its largest, and the sum of exp(z - top) over all others.  The largest's own 1 is left out, so
-// that a loss near 0, the sum of the others, keeps its precision.
+// A set of y = z log2(e): its largest, and the sum of 2^(y - top) over all others.  The largest's own 1 is left
+// out, so that a loss near 0, the sum of the others, keeps its precision.  (In these units a value goes into the exponential
+// without a product of its own; y and top are each off by half a unit in the last place, 2^-25 |y|.)
 struct Soft {
   float top, rest;
 };
@@ -33,7 +34,7 @@ constexpr float NOTHING = -__builtin_inff();
 // What is subtracted: classes may all be out (minus infinity).
 __device__ __forceinline__ float base_of(float top) { return top == NOTHING ? 0.0f : top; }
 __device__ __forceinline__ Soft join(Soft a, Soft b) {
-  const float hi = larger(a.top, b.top), e = exp_of(smaller(a.top, b.top) - base_of(hi));
+  const float hi = larger(a.top, b.top), e = __builtin_amdgcn_exp2f(smaller(a.top, b.top) - base_of(hi));
   const bool first = a.top >= b.top;
   return {hi, fmaf((first ? b.rest : a.rest) + 1.0f, e, first ? a.rest : b.rest)};
 }
@@ -53,7 +54,7 @@ __device__ __forceinline__ Soft soft_of(const float (&v)[N]) {
   const float base = base_of(top);
   float s[2] = {0.0f, 0.0f};
 #pragma unroll
-  for (int i = 1; i < N; ++i) s[i % 2] += exp_of(low[i] - base);
+  for (int i = 1; i < N; ++i) s[i % 2] += __builtin_amdgcn_exp2f(low[i] - base);
   return {top, s[0] + s[1]};
 }
 
@@ -63,14 +64,14 @@ struct Out {
   int64_t M, N, ignore;
   float smoothing;
 };
-// Row m from its pair, the sum of its z and the target's z.
+// Row m from its pair, the sum of its y and the target's y.
 __device__ __forceinline__ void finish_row(const Out &o, int64_t m, Soft s, float sum, float at) {
   const float rest = log1pf(s.rest);
-  o.lse[m] = s.top + rest;
+  o.lse[m] = fmaf(s.top, LN2, rest);
   const int64_t t = o.target[m];
   float loss = s.top - at;
   if (o.smoothing > 0.0f) loss = (1.0f - o.smoothing) * loss + o.smoothing * (s.top - sum / float(o.N));
-  loss += rest;
+  loss = fmaf(loss, LN2, rest);
   o.loss[m] = t == o.ignore ? 0.0f : t < 0 || t >= o.N ? __builtin_nanf("") : loss;
 }
 
@@ -87,63 +88,117 @@ struct Logits {
 constexpr int SLOT = 64;   // columns of a pair
 struct Pairs {
   Soft *pairs;             // [slots][M]
-  float *sums;             // the same of z, or null
-  float *at;               // [M] the target's z
+  float *sums;             // [slots][M] sums of y, or null
+  float *at;               // [M] the target's y
   const int64_t *target;
   int64_t slots;
 };
 
+// Keeps what depends on v behind the branch it is in (the compiler moves cheap work before branches).
+__device__ __forceinline__ void stay_here(float &v) { asm volatile("" : "+v"(v)); }
+
+// A value of the lanes with bit X (16 or 32) clear and of those with it set, each to both.
+template <int X>
+__device__ __forceinline__ void halves(float v, float &clear, float &set) {
+  const int i = __float_as_int(v);
+  if constexpr (X == 16) {
+    const auto r = __builtin_amdgcn_permlane16_swap(i, i, false, false);
+    clear = __int_as_float(r[0]), set = __int_as_float(r[1]);
+  } else {
+    const auto r = __builtin_amdgcn_permlane32_swap(i, i, false, false);
+    clear = __int_as_float(r[0]), set = __int_as_float(r[1]);
+  }
+}
+// The pair of N values in each of four lanes (l, l ^ 16, l ^ 32, l ^ 48): the largest of all first, then one exponential
+// of every other value; the losers among the four lanes' largest are two of the first exchange and one of the second.
+template <int N>
+__device__ __forceinline__ Soft soft_of_four(const float (&v)[N]) {
+  float top = v[0], low[N + 1];
+#pragma unroll
+  for (int i = 1; i < N; ++i) {
+    low[i - 1] = smaller(top, v[i]);
+    top = larger(top, v[i]);
+  }
+  const uint32_t l = __lane_id();
+  float a, b;
+  halves<16>(top, a, b);
+  low[N - 1] = l & 16 ? NOTHING : smaller(a, b);
+  top = larger(a, b);
+  halves<32>(top, a, b);
+  low[N] = l & 48 ? NOTHING : smaller(a, b);
+  top = larger(a, b);
+  const float base = base_of(top);
+  float s[2] = {0.0f, 0.0f};
+#pragma unroll
+  for (int i = 0; i <= N; ++i) s[i % 2] += __builtin_amdgcn_exp2f(low[i] - base);
+  halves<16>(s[0] + s[1], a, b);
+  halves<32>(a + b, a, b);
+  return {top, a + b};
+}
+
 // The pairs of a tile, straight from the accumulators: lane l has row l % 16 of each 16 x 16 result and four
-// columns from 4 (l / 16), so a row's 64 columns are in four lanes, 16 each.
-template <int KIND, typename S>
+// columns from 4 (l / 16), so a row's 64 columns are in four lanes, 16 each.  SMOOTH: their sums too.  8192 x 100003 x 2304
+// int8 (18 steps of 1.37 us a tile): of 19 us that a tile took beside its steps, 5 were this arithmetic, 3 the loads that
+// are issued together here.
+template <int KIND, bool SMOOTH, typename S>
 __device__ __forceinline__ void store_pairs(const Logits &p, const Pairs &o, const tile::Place &at,
                                             const typename tile::Acc<KIND>::type (&acc)[S::FM][S::FN], char *lds) {
   constexpr int PER = S::FN * 4;
   const uint32_t wave = wave_id(), l = __lane_id(), q = l / 16;
   const int64_t m0 = at.m0 + (wave / S::WN) * S::TM, n0 = at.n0 + (wave % S::WN) * S::TN;
   const int64_t col = n0 + 4 * q;
+  // (no branch between the loads: past the ends they read the last element again)
+  float bias[PER], sw[PER], sx[S::FM];
+  int64_t target[S::FM];
+#pragma unroll
+  for (int k = 0; k < S::FM; ++k) target[k] = o.target[min(m0 + k * 16 + l % 16, p.M - 1)];
+  if constexpr (KIND != tile::BF16K) {
+#pragma unroll
+    for (int k = 0; k < S::FM; ++k) sx[k] = p.sx[min(m0 + k * 16 + l % 16, p.M - 1)];
+#pragma unroll
+    for (int j = 0; j < PER; ++j) sw[j] = p.sw[min(col + 16 * (j / 4) + j % 4, p.N - 1)];
+  }
+  if (p.bias) {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) bias[j] = p.bias[min(col + 16 * (j / 4) + j % 4, p.N - 1)] * LOG2E;
+  } else {
+#pragma unroll
+    for (int j = 0; j < PER; ++j) bias[j] = 0.0f;
+  }
   // columns past the last are out
-  float bias[PER], sw[PER];
+  if (n0 + S::TN > p.N) {
 #pragma unroll
-  for (int j = 0; j < S::FN; ++j)
-#pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      const int64_t n = col + 16 * j + i;
-      bias[4 * j + i] = n >= p.N ? NOTHING : p.bias ? p.bias[n] : 0.0f;
-      sw[4 * j + i] = p.sw && n < p.N ? p.sw[n] : 1.0f;
-    }
+    for (int j = 0; j < PER; ++j) bias[j] = col + 16 * (j / 4) + j % 4 < p.N ? bias[j] : NOTHING;
+  }
   int where[S::FM];        // the target's place among the wave's columns
 #pragma unroll
   for (int k = 0; k < S::FM; ++k) {
-    const int64_t m = m0 + k * 16 + l % 16;
-    const int64_t t = m < p.M ? o.target[m] - n0 : -1;
-    where[k] = t >= 0 && t < S::TN && t < p.N - n0 ? int(t) : -1;
+    const int64_t t = target[k] - n0;
+    where[k] = m0 + k * 16 + l % 16 < p.M && t >= 0 && t < S::TN && t < p.N - n0 ? int(t) : -1;
   }
   Soft held{};
   float held_sum = 0.0f;
 #pragma unroll
   for (int k = 0; k < S::FM; ++k) {
-    const int64_t m = m0 + k * 16 + l % 16;
-    const float sx = p.sx ? p.sx[min(m, p.M - 1)] : 1.0f;
     float v[PER];
 #pragma unroll
     for (int j = 0; j < S::FN; ++j)
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        float z = float(acc[k][j][i]);
-        if (p.sx) z = z * sx * sw[4 * j + i];
-        v[4 * j + i] = z + bias[4 * j + i];
+        if constexpr (KIND == tile::BF16K) v[4 * j + i] = fmaf(acc[k][j][i], LOG2E, bias[4 * j + i]);
+        else v[4 * j + i] = fmaf(float(acc[k][j][i]) * (sx[k] * LOG2E), sw[4 * j + i], bias[4 * j + i]);
       }
     if (const bool mine = where[k] >= 0 && uint32_t(where[k] / 4 % 4) == q; __any(mine)) {
       const int i = where[k] / 16 * 4 + where[k] % 4;
       float z = v[0];
+      stay_here(z);
 #pragma unroll
       for (int j = 1; j < PER; ++j) z = i == j ? v[j] : z;
-      if (mine) o.at[m] = z;
+      if (mine) o.at[m0 + k * 16 + l % 16] = z;
     }
-    Soft s = join_lanes<32>(join_lanes<16>(soft_of<PER>(v)));
+    const Soft s = soft_of_four<PER>(v);
     float sum = 0.0f;
-    if (o.sums) {
+    if constexpr (SMOOTH) {
 #pragma unroll
       for (int j = 0; j < PER; ++j) sum += col + 16 * (j / 4) + j % 4 < p.N ? v[j] : 0.0f;
       sum += lane_xor_f<16>(sum);
@@ -156,7 +211,7 @@ __device__ __forceinline__ void store_pairs(const Logits &p, const Pairs &o, con
         const int64_t r = m0 + (k / 4) * 64 + l;
         if (r < p.M && n0 < p.N) {
           o.pairs[n0 / SLOT * p.M + r] = held;
-          if (o.sums) o.sums[n0 / SLOT * p.M + r] = held_sum;
+          if constexpr (SMOOTH) o.sums[n0 / SLOT * p.M + r] = held_sum;
         }
       }
     } else {
@@ -172,12 +227,12 @@ __device__ __forceinline__ void store_pairs(const Logits &p, const Pairs &o, con
     if (threadIdx.x < S::BM && r < p.M) {
       const float4 a = both[threadIdx.x], b = both[S::BM + threadIdx.x];
       o.pairs[at.n0 / SLOT * p.M + r] = join(Soft{a.x, a.y}, Soft{b.x, b.y});
-      if (o.sums) o.sums[at.n0 / SLOT * p.M + r] = a.z + b.z;
+      if constexpr (SMOOTH) o.sums[at.n0 / SLOT * p.M + r] = a.z + b.z;
     }
   }
 }
 
-template <int KIND, int SHAPE>
+template <int KIND, bool SMOOTH, int SHAPE>
 __global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_loss_tiles(Logits p, Pairs o) {
   typedef typename tile::ShapeOf<SHAPE>::type S;
   __shared__ __attribute__((aligned(16))) char lds[S::LDS];
@@ -188,7 +243,7 @@ __global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_loss
   if (p.tiles.splits > 1)
     tile::run_epilogue<KIND, S>(acc, lds, at.m0, at.n0, tile::StorePart{p.part + at.split * p.M * p.ldp, p.M, p.ldp});
   else
-    store_pairs<KIND, S>(p, o, at, acc, lds);
+    store_pairs<KIND, SMOOTH, S>(p, o, at, acc, lds);
 }
 
 // Joins the pairs of 16 rows by 16 threads each, which take every 16th slot.
@@ -278,6 +333,7 @@ __global__ void __launch_bounds__(256) k_loss_dense(RowArgs a, Pairs p, Out o) {
       }
       if (a.sx) v[i] = v[i] * sx * a.sw[n + i];
       if (a.bias) v[i] += a.bias[n + i];
+      v[i] *= LOG2E;
       sum += v[i];
       if (n + i == t) found = v[i];
     }
@@ -648,7 +704,9 @@ template <int KIND>
 int launch_logits(const tile::Plan &plan, Logits p, const Pairs &o, hipStream_t st) {
   tile::for_launches(plan, [&]<int SHAPE>(const tile::Tiles &t) {
     p.tiles = t;
-    k_loss_tiles<KIND, SHAPE><<<dim3(uint32_t(tile::blocks_of(t))), dim3(tile::ShapeOf<SHAPE>::type::THREADS), 0, st>>>(p, o);
+    const dim3 grid(uint32_t(tile::blocks_of(t))), block(tile::ShapeOf<SHAPE>::type::THREADS);
+    if (o.sums) k_loss_tiles<KIND, true, SHAPE><<<grid, block, 0, st>>>(p, o);
+    else k_loss_tiles<KIND, false, SHAPE><<<grid, block, 0, st>>>(p, o);
   });
   return last_launch_status();
 }
