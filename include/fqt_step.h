@@ -26,7 +26,7 @@ extern "C" {
  * 8-bit types and are NULL for FQT_BF16; bias float32 [N], optional; target int64 [M]; loss and lse float32
  * [M].  Row m is left out where target[m] is `ignore`: its loss is 0, its lse as ever.  Any other target that
  * is no class makes the row's loss NaN, and its gradients (nothing outside the arrays is read for it).  A
- * bias of minus infinity takes a class out.  The loss holds its relative precision also where it is
+ * bias of minus infinity takes a class out (not with smoothing, whose mean is over all).  The loss holds its relative precision also where it is
  * small (the largest z is left out of the sum that is added to it).
  * mean, float32 [2], optional: the mean loss over the rows that count, and 1 / their number; both 0 if none
  * does.
@@ -89,7 +89,8 @@ int fqt_grad_norm(const fqt_param *params, int32_t count, float max_norm, float 
  *   m = beta1 m + (1 - beta1) s g;  v = beta2 v + (1 - beta2) (s g)^2
  *   p = p - lr weight_decay p - lr / (1 - beta1^t) * m / (sqrt(v / (1 - beta2^t)) + eps)
  * in float32, the factors in float64.  t is `step`, or *step_dev (device memory, read as the kernel runs: for
- * captured graphs) where that is given; t >= 1 (a smaller *step_dev counts as 1).
+ * captured graphs) where that is given; t >= 1 (a smaller *step_dev counts as 1).  With eps = 0 an element whose m and v
+ * are 0 becomes NaN; so does one whose gradient is infinite, also where s is 0.
  *
  * States of 8 bits (state_dtype FQT_E4M3): m and sqrt(v) are held as e4m3 codes, with one float32 scale for
  * each block of FQT_STATE_BLOCK elements of a tensor: scale = max of the block / 448, and a code stands for
@@ -99,7 +100,7 @@ int fqt_grad_norm(const fqt_param *params, int32_t count, float max_norm, float 
  * its m may not.  A block whose maximum is below 2^-100 is stored as zeros.  A value that is not finite
  * makes its block's scale so, and with the next step the block.
  * The random bits are those of Philox4x32-10 with the key `seed` and the counter
- * ((first + i) / 4, 3 << 30 in the second word, 0, t): word (first + i) % 4 belongs to element i, its lower
+ * ((first + i) / 4 (64 bits, 3 << 30 in the upper word), 0, t modulo 2^32): word (first + i) % 4 belongs to element i, its lower
  * 16 bits to m, the upper to v. */
 typedef struct {
   double lr, beta1, beta2, eps, weight_decay;   /* finite; lr, eps, weight_decay >= 0, 0 <= beta < 1 */

@@ -428,9 +428,9 @@ class AdamW(torch.optim.Optimizer):
             for k in ("m_scale", "v_scale"):
                 flat[k] = [s[k] for s in states] if self.states == "e4m3" else None
             weights = [_flat(p) for p in params]
-            at = self._lists[key] = held, step.param_list(weights, weights, flat["m"], flat["v"], flat["m_scale"],
-                                                          flat["v_scale"], first=starts)
-        return at[1]
+            at = held, step.param_list(weights, weights, flat["m"], flat["v"], flat["m_scale"], flat["v_scale"],
+                                       first=starts)
+        return at
 
     @torch.no_grad()
     def step(self, closure=None):
@@ -455,11 +455,14 @@ class AdamW(torch.optim.Optimizer):
                 at += -(-p.numel() // step.FQT_STATE_BLOCK) * step.FQT_STATE_BLOCK
         if not todo:
             return loss
-        lists = []
+        lists, kept = [], {}
         for (i, t), (cfg, params, g, starts) in todo.items():
-            params_list = self._list((i, tuple(starts)), params, starts)
+            key = i, tuple(starts)
+            kept[key] = self._list(key, params, starts)
+            params_list = kept[key][1]
             params_list.set_gradients(g)
             lists.append((i, t, cfg, params, params_list))
+        self._lists = kept                   # (those of this step: other sets of weights with gradients go)
         scale = None
         if self.max_norm is not None:
             whole = lists[0][4] if len(lists) == 1 else step.param_list(gradients)
@@ -480,7 +483,12 @@ class AdamW(torch.optim.Optimizer):
                 for p in params:
                     self.state[p]["step"] = number
             step.fqt_adamw_step(cfg, params_list, number, grad_scale=scale)
+            params_list.drop_gradients()     # (their memory is free for the next backward pass)
         return loss
+
+    def __getstate__(self):
+        return {**super().__getstate__(), "states": self.states, "seed": self.seed, "max_norm": self.max_norm,
+                "capturable": self.capturable, "grad_norm": None, "_lists": {}}
 
     def load_state_dict(self, state_dict):
         if any(("m_scale" in s) != (self.states == "e4m3") for s in state_dict["state"].values()):

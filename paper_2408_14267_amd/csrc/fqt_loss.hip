@@ -246,37 +246,42 @@ __global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_loss
     store_pairs<KIND, SMOOTH, S>(p, o, at, acc, lds);
 }
 
-// Joins the pairs of 16 rows by 16 threads each, which take every 16th slot.
+// Joins the pairs of 16 rows by 16 threads each, which take every 16th slot; workgroups walk the rows.
 __global__ void __launch_bounds__(256) k_loss_rows(Pairs p, Out o) {
   constexpr int AHEAD = 8;
   __shared__ float4 all[16][17];
   const int r = threadIdx.x % 16, g = threadIdx.x / 16;
-  const int64_t m = int64_t(blockIdx.x) * 16 + r, slots = p.slots;
-  Soft s{NOTHING, 0.0f};
-  float sum = 0.0f;
-  if (m < o.M)
-    for (int64_t i0 = g; i0 < slots; i0 += 16 * AHEAD) {
-      Soft t[AHEAD];
+  const int64_t slots = p.slots;
+  for (int64_t m0 = int64_t(blockIdx.x) * 16; m0 < o.M; m0 += int64_t(gridDim.x) * 16) {
+    const int64_t m = m0 + r;
+    Soft s{NOTHING, 0.0f};
+    float sum = 0.0f;
+    if (m < o.M)
+      for (int64_t i0 = g; i0 < slots; i0 += 16 * AHEAD) {
+        Soft t[AHEAD];
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i)
-        t[i] = i0 + 16 * i < slots ? p.pairs[(i0 + 16 * i) * o.M + m] : Soft{NOTHING, 0.0f};
+        for (int i = 0; i < AHEAD; ++i)
+          t[i] = i0 + 16 * i < slots ? p.pairs[(i0 + 16 * i) * o.M + m] : Soft{NOTHING, 0.0f};
 #pragma unroll
-      for (int i = 0; i < AHEAD; ++i) s = join(s, t[i]);
-      if (p.sums)
+        for (int i = 0; i < AHEAD; ++i) s = join(s, t[i]);
+        if (p.sums)
 #pragma unroll
-        for (int i = 0; i < AHEAD; ++i) sum += i0 + 16 * i < slots ? p.sums[(i0 + 16 * i) * o.M + m] : 0.0f;
+          for (int i = 0; i < AHEAD; ++i) sum += i0 + 16 * i < slots ? p.sums[(i0 + 16 * i) * o.M + m] : 0.0f;
+      }
+    all[g][r] = make_float4(s.top, s.rest, sum, 0.0f);
+    __syncthreads();
+    if (g == 0 && m < o.M) {
+#pragma unroll
+      for (int i = 1; i < 16; ++i) {
+        const float4 b = all[i][r];
+        s = join(s, Soft{b.x, b.y});
+        sum += b.z;
+      }
+      const int64_t t = p.target[m];
+      finish_row(o, m, s, sum, t >= 0 && t < o.N ? p.at[m] : 0.0f);
     }
-  all[g][r] = make_float4(s.top, s.rest, sum, 0.0f);
-  __syncthreads();
-  if (g || m >= o.M) return;
-#pragma unroll
-  for (int i = 1; i < 16; ++i) {
-    const float4 b = all[i][r];
-    s = join(s, Soft{b.x, b.y});
-    sum += b.z;
+    __syncthreads();
   }
-  const int64_t t = p.target[m];
-  finish_row(o, m, s, sum, t >= 0 && t < o.N ? p.at[m] : 0.0f);
 }
 
 // ----------------------------------------------------------------------------- forward by rows
@@ -731,7 +736,8 @@ int launch_dense(const RowArgs &a, const Pairs &p, const Out &o, bool ints, hipS
 }
 // Pairs to the losses (nothing where the pass before had whole rows).
 int launch_rows(const Pairs &p, const Out &o, hipStream_t st) {
-  k_loss_rows<<<dim3(uint32_t((o.M + 15) / 16)), dim3(256), 0, st>>>(p, o);
+  // (a launch counts its threads in 32 bits)
+  k_loss_rows<<<dim3(uint32_t(std::min<int64_t>((o.M + 15) / 16, 1 << 16))), dim3(256), 0, st>>>(p, o);
   return last_launch_status();
 }
 

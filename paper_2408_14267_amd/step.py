@@ -163,6 +163,12 @@ class ParamList:
             d.g, d.g_dtype = t.data_ptr(), FQT_F32 if t.dtype is torch.float32 else FQT_BF16
         self.tensors["g"] = list(g)
 
+    def drop_gradients(self):
+        """Forgets the gradients, whose memory may then be used again; others have to be set before the next call."""
+        for d in self.array:
+            d.g = None
+        self.tensors["g"] = []
+
 
 def _flat(where, name, t, dtypes, n, dev):
     if t.dtype not in dtypes:

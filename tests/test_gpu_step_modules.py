@@ -192,6 +192,32 @@ def test_adamw_checkpoint(states):
         b.AdamW(weights(), states="f32" if states == "e4m3" else "e4m3").load_state_dict(oa.state_dict())
 
 
+def test_adamw_copies_and_gradients_of_some():
+    """A deep copy goes on like its original; weights with and without gradients change from step to step; gradients
+    are not held after a step."""
+    import gc
+    import weakref
+    b = blocks()
+    params = weights()
+    opt = b.AdamW(params, lr=0.01, states="e4m3", max_norm=1.0)
+    for s in range(4):
+        for i, p in enumerate(params):
+            p.grad = gen(*p.shape, seed=10 * s + i) if (i + s) % 2 else None
+        held = [weakref.ref(p.grad) for p in params if p.grad is not None]
+        opt.step()
+        for p in params:
+            p.grad = None
+        gc.collect()
+        assert all(r() is None for r in held)
+        assert len(opt._lists) <= 2
+    both = copy.deepcopy((params, opt))
+    for q, o in ((params, opt), both):
+        for i, p in enumerate(q):
+            p.grad = gen(*p.shape, seed=50 + i)
+        o.step()
+    assert all(torch.equal(p, q) for p, q in zip(params, both[0]))
+
+
 def test_adamw_refusals():
     b = blocks()
     for bad in (torch.zeros(3, device="cuda").double(), torch.zeros(3, 4, device="cuda")[:, :2]):
