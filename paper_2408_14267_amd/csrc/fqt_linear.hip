@@ -542,21 +542,34 @@ __global__ void __launch_bounds__(tile::Small::THREADS, 2) k_product_pair(Produc
   }
 }
 
-// Both products of large tiles in one launch.  dw_first: its tiles are the first workgroups.
-__global__ void __launch_bounds__(tile::Large::THREADS, 2) k_product_both(Product px, Epilogue ex, Product pw, Epilogue ew, int dw_first) {
-  typedef tile::Large S;
+// Both products in one launch, and dbias (by the first 256 threads of the last workgroups).  dw_first: its tiles
+// are the first workgroups.
+template <int SHAPE>
+__global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_product_both(Product px, Epilogue ex, Product pw, Epilogue ew, DbiasArgs bias, int dw_first) {
+  typedef typename tile::ShapeOf<SHAPE>::type S;
   __shared__ __attribute__((aligned(16))) char lds[S::LDS];
   tile::f32x4 acc[S::FM][S::FN];
-  const uint32_t before = dw_first ? pw.tiles.count : px.tiles.count;
+  const uint32_t nx = px.tiles.count * px.tiles.splits, nw = pw.tiles.count * pw.tiles.splits;
+  const uint32_t before = dw_first ? nw : nx;
+  if (blockIdx.x >= nx + nw) {
+    if (threadIdx.x < 256) sum_dbias(bias, blockIdx.x - nx - nw, reinterpret_cast<float (*)[32]>(lds));
+    return;
+  }
   const uint32_t b = blockIdx.x < before ? blockIdx.x : blockIdx.x - before;
+  auto finish = [&](const Product &p, const Epilogue &e, const tile::Place &at) {
+    if (p.tiles.splits > 1)
+      tile::run_epilogue<tile::BF16K, S>(acc, lds, at.m0, at.n0, tile::StorePart{p.part + at.split * p.M * p.ldp, p.M, p.ldp});
+    else
+      tile::run_epilogue<tile::BF16K, S>(acc, lds, at.m0, at.n0, Finish<FQT_ACT_NONE>(e));
+  };
   if ((blockIdx.x < before) == (dw_first != 0)) {
-    const tile::Place at = tile::place<tile::LARGE>(pw.tiles, b);
-    tile::contract<tile::BF16K, COLS, COLS, tile::LARGE, S>(pw.x, pw.w, pw.K, at, pw.tiles, lds, acc);
-    tile::run_epilogue<tile::BF16K, S>(acc, lds, at.m0, at.n0, Finish<FQT_ACT_NONE>(ew));
+    const tile::Place at = tile::place<SHAPE>(pw.tiles, b);
+    tile::contract<tile::BF16K, COLS, COLS, SHAPE, S>(pw.x, pw.w, pw.K, at, pw.tiles, lds, acc);
+    finish(pw, ew, at);
   } else {
-    const tile::Place at = tile::place<tile::LARGE>(px.tiles, b);
-    tile::contract<tile::BF16K, ROWS, COLS, tile::LARGE, S>(px.x, px.w, px.K, at, px.tiles, lds, acc);
-    tile::run_epilogue<tile::BF16K, S>(acc, lds, at.m0, at.n0, Finish<FQT_ACT_NONE>(ex));
+    const tile::Place at = tile::place<SHAPE>(px.tiles, b);
+    tile::contract<tile::BF16K, ROWS, COLS, SHAPE, S>(px.x, px.w, px.K, at, px.tiles, lds, acc);
+    finish(px, ex, at);
   }
 }
 __global__ void __launch_bounds__(256) k_zero(char *p, int64_t rows, int64_t bytes, int64_t ld) {
@@ -732,21 +745,37 @@ tile::Tiles whole_grid(int64_t M, int64_t N, int64_t K, int64_t edge) {
 Together plan_together(int64_t M, int64_t N, int64_t K, const tile::Plan &dx, const tile::Plan &dw) {
   const tile::Costs &c = tile::DENSE_COSTS;
   double best = dx.us + dw.us;
-  Together how = APART;
+  Together how{};
   // us of both products' tiles, `cu` of them on a CU at a time: evenly over the CUs, and half of one of the last
   // tiles; no less than the longer tiles' rounds
-  auto take = [&](Together t, int64_t edge, int cu, double step, double start) {
-    const tile::Tiles x = whole_grid(M, K, N, edge), w = whole_grid(N, K, M, edge);
+  auto take = [&](int shape, int cu, double step, double start) {
+    tile::Tiles x = whole_grid(M, K, N, tile::EDGES[shape]), w = whole_grid(N, K, M, tile::EDGES[shape]);
     if (uint64_t(x.count) + w.count >= tile::MOST_LARGE) return;
-    const double ex = step * x.steps + start, ew = step * w.steps + start, slots = 256.0 * cu;
-    const double rounds = std::ceil((ex > ew ? x : w).count / slots);
-    const double us = std::max((x.count * ex + w.count * ew) / slots + std::min(ex, ew) / 2, rounds * std::max(ex, ew)) + 3;
-    if (us < best) best = us, how = t;
+    tile::Tiles &longer = x.steps > w.steps ? x : w, &shorter = x.steps > w.steps ? w : x;
+    const double entries = double(x.steps > w.steps ? M : N) * K;
+    const uint32_t steps = longer.steps;
+    for (uint32_t n = 1; n <= 32 && (n == 1 || steps / n >= 4); n *= 2) {
+      longer.steps = std::max(1u, (steps + n - 1) / n);
+      longer.splits = std::max(1u, (steps + longer.steps - 1) / longer.steps);
+      if ((uint64_t(longer.count) * longer.splits + shorter.count) * tile::SHAPE_THREADS[shape] >> 31) continue;
+      const double el = step * longer.steps + start, es = step * shorter.steps + start, slots = 256.0 * cu;
+      const double many = double(longer.count) * longer.splits, rounds = std::ceil(many / slots);
+      double us = std::max((many * el + shorter.count * es) / slots + std::min(el, es) / 2, rounds * el) + 3;
+      if (longer.splits > 1) us += 4 + 0.2 * longer.splits + longer.splits * entries * 8 / 4e6;
+      if (us < best) best = us, how = {true, shape, x, w};
+    }
   };
-  if (tile::large_tiles(M, K) < tile::MOST_LARGE / 32 && tile::large_tiles(N, K) < tile::MOST_LARGE / 32)
-    take(SMALL_BOTH, tile::Small::BM, 3, c.small[2], c.start[2]);
-  take(LARGE_BOTH, tile::Large::BM, 1, c.large[0], c.start[0]);
+  if (tile::large_tiles(M, K) < tile::MOST_LARGE / 32 && tile::large_tiles(N, K) < tile::MOST_LARGE / 32) {
+    take(tile::SMALL, 3, c.small[2], c.start[2]);
+    take(tile::MIDDLE, 2, c.middle[1], c.start[1]);
+  }
+  take(tile::LARGE, 1, c.large[0], c.start[0]);
   return how;
+}
+size_t part_bytes(const Together &t, int64_t M, int64_t N, int64_t K) {
+  if (!t.on) return 0;
+  auto bytes = [&](const tile::Tiles &s, int64_t m) { return s.splits > 1 ? align256(size_t(s.splits) * m * round_up(K, 8) * 4) : 0; };
+  return std::max(bytes(t.dx, M), bytes(t.dw, N));
 }
 
 int launch_gradients(const Gradients &g, hipStream_t st) {
@@ -754,11 +783,31 @@ int launch_gradients(const Gradients &g, hipStream_t st) {
   const Epilogue ex{nullptr, nullptr, nullptr, g.add, nullptr, g.dx, 0, 0, g.ldadd, 0, g.lddx, g.dx_dtype, FQT_ACT_NONE, FQT_F32};
   const Epilogue ew{nullptr, nullptr, nullptr, nullptr, nullptr, g.dw, 0, 0, 0, 0, g.lddw, g.dw_dtype, FQT_ACT_NONE, FQT_F32};
   auto small = [](const tile::Plan &p) { return p.shape[0] == tile::SMALL && p.launches == 1 && p.splits == 1; };
-  const bool together = g.dx && g.dw && g.K;
-  if (together && (g.together == SMALL_BOTH || (small(g.plan_dx) && small(g.plan_dw)))) {
-    const int64_t edge = tile::Small::BM;
-    const Product px{g.dzx, g.w, g.M, g.K, g.N, whole_grid(g.M, g.K, g.N, edge), nullptr, 0},
-        pw{g.dzw, g.x, g.N, g.K, g.M, whole_grid(g.N, g.K, g.M, edge), nullptr, 0};
+  const bool both = g.dx && g.dw && g.K;
+  if (both && g.together.on) {
+    const Product px{g.dzx, g.w, g.M, g.K, g.N, g.together.dx, g.part, round_up(g.K, 8)},
+        pw{g.dzw, g.x, g.N, g.K, g.M, g.together.dw, g.part, round_up(g.K, 8)};
+    const Epilogue fx = sized(ex, g.M, g.K), fw = sized(ew, g.N, g.K);
+    // the longer contraction's tiles first (its pieces are no shorter than four steps)
+    const int dw_first = g.M > g.N;
+    auto run = [&]<int SHAPE>() {
+      const dim3 grid(px.tiles.count * px.tiles.splits + pw.tiles.count * pw.tiles.splits + bias_blocks);
+      k_product_both<SHAPE><<<grid, dim3(tile::ShapeOf<SHAPE>::type::THREADS), 0, st>>>(px, fx, pw, fw, g.bias, dw_first);
+    };
+    switch (g.together.shape) {
+      case tile::LARGE: run.template operator()<tile::LARGE>(); break;
+      case tile::MIDDLE: run.template operator()<tile::MIDDLE>(); break;
+      default: run.template operator()<tile::SMALL>();
+    }
+    FQT_TRY_(last_launch_status());
+    if (px.tiles.splits == 1 && pw.tiles.splits == 1) return FQT_OK;
+    const bool of_x = px.tiles.splits > 1;               // (one of the two is split)
+    const int64_t all = (of_x ? px.M : pw.M) * (px.ldp / 8);
+    k_product_finish<false><<<dim3(std::min<int64_t>((all + 255) / 256, 4096)), dim3(256), 0, st>>>(of_x ? px : pw, of_x ? fx : fw);
+    return last_launch_status();
+  }
+  if (both && small(g.plan_dx) && small(g.plan_dw)) {
+    const Product px{g.dzx, g.w, g.M, g.K, g.N, g.plan_dx.t[0], nullptr, 0}, pw{g.dzw, g.x, g.N, g.K, g.M, g.plan_dw.t[0], nullptr, 0};
     k_product_pair<<<dim3(px.tiles.count + pw.tiles.count + bias_blocks), dim3(tile::Small::THREADS), 0, st>>>(
         px, sized(ex, g.M, g.K), pw, sized(ew, g.N, g.K), g.bias);
     return last_launch_status();
@@ -768,14 +817,6 @@ int launch_gradients(const Gradients &g, hipStream_t st) {
     FQT_TRY_(last_launch_status());
   }
   if (g.K == 0) return FQT_OK;
-  if (together && g.together == LARGE_BOTH) {
-    const int64_t edge = tile::Large::BM;
-    const Product px{g.dzx, g.w, g.M, g.K, g.N, whole_grid(g.M, g.K, g.N, edge), nullptr, 0},
-        pw{g.dzw, g.x, g.N, g.K, g.M, whole_grid(g.N, g.K, g.M, edge), nullptr, 0};
-    k_product_both<<<dim3(px.tiles.count + pw.tiles.count), dim3(tile::Large::THREADS), 0, st>>>(
-        px, sized(ex, g.M, g.K), pw, sized(ew, g.N, g.K), pw.tiles.steps > px.tiles.steps);
-    return last_launch_status();
-  }
   if (g.dx) FQT_TRY_((launch_product<tile::BF16K, ROWS, COLS>(g.plan_dx, g.dzx, g.w, g.M, g.K, g.N, ex, g.part, st)));
   if (g.dw) FQT_TRY_((launch_product<tile::BF16K, COLS, COLS>(g.plan_dw, g.dzw, g.x, g.N, g.K, g.M, ew, g.part, st)));
   return FQT_OK;

@@ -697,7 +697,8 @@ BwdWs bwd_ws(const fqt_loss_desc &d, const Sizes &s) {
   size_t part = 0, groups = 1;
   for (const int64_t n : {f.piece, s.N % f.piece ? s.N % f.piece : f.piece}) {
     const PiecePlan p = plan_piece(d, s, n, f);
-    part = std::max({part, part_bytes(p.z, s.M, n), part_bytes(p.dx, s.M, s.K), part_bytes(p.dw, n, s.K)});
+    part = std::max({part, part_bytes(p.z, s.M, n), part_bytes(p.dx, s.M, s.K), part_bytes(p.dw, n, s.K),
+                     part_bytes(p.together, s.M, n, s.K)});
     groups = std::max(groups, size_t((s.M + p.unit - 1) / p.unit));
   }
   f.part = f.bias + align256(groups * f.piece * 4);

@@ -21,6 +21,17 @@ struct DbiasArgs {
   int64_t N;
   int32_t parts;
 };
+// dx and dw in one launch of tiles of one shape, the longer contraction's first and perhaps split: the tiles that a last
+// round of one leaves CUs idle with run beside those of the other.
+struct Together {
+  bool on;                 // (off: one after the other by their plans)
+  int shape;
+  tile::Tiles dx, dw;
+};
+// The cheapest of these, on if it takes less time than the two plans.
+Together plan_together(int64_t M, int64_t N, int64_t K, const tile::Plan &dx, const tile::Plan &dw);
+size_t part_bytes(const Together &t, int64_t M, int64_t N, int64_t K);
+
 // dx = dz w + add and dw = dz^T x, each computed where its pointer is given.  dzx and dzw: dz as it goes into
 // either, rows of M; w and x: operands along the features, their `rows` features.  add: float32 with
 // dx's stride, may be dx itself; null for none.
@@ -32,17 +43,11 @@ struct Gradients {
   const float *add;
   int64_t lddx, ldadd, lddw;
   int32_t dx_dtype, dw_dtype;
-  float *part;             // part_bytes of either plan
+  float *part;             // part_bytes of either plan, or of both together
   DbiasArgs bias;
-  int together;            // plan_together
+  Together together;
 };
 int launch_gradients(const Gradients &g, hipStream_t st);
-// How dx and dw are launched: APART, one after the other by their plans, or in one launch of Small or of Large
-// tiles (those of the longer contraction first), where the tiles that a last round of one leaves CUs idle
-// with run beside those of the other.
-enum Together { APART, SMALL_BOTH, LARGE_BOTH };
-Together plan_together(int64_t M, int64_t N, int64_t K, const tile::Plan &dx, const tile::Plan &dw);
-
 // Rows of src (cols elements, stride ld) to rows of `pitch` elements, zero past cols.
 struct Copy {
   const void *src;
