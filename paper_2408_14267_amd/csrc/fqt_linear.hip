@@ -411,9 +411,17 @@ __device__ __forceinline__ void repack_rows(const Copy &a, uint32_t block) {
   for (int64_t i = int64_t(block) * 256 + threadIdx.x; i < all; i += int64_t(a.blocks) * 256) {
     const int64_t r = i / groups, c = i % groups * V;
     const ST *src = static_cast<const ST *>(a.src) + r * a.ld + c;
+    // (whole groups by one load at any alignment)
+    ST in[V];
+    if (c + V <= a.cols) {
+      __builtin_memcpy(in, src, sizeof(in));
+    } else {
+#pragma unroll
+      for (int j = 0; j < V; ++j) in[j] = c + j < a.cols ? src[j] : ST{};
+    }
     DT o[V];
 #pragma unroll
-    for (int j = 0; j < V; ++j) o[j] = c + j < a.cols ? widen<ST, DT>(src[j]) : DT{};
+    for (int j = 0; j < V; ++j) o[j] = widen<ST, DT>(in[j]);
     uint4 u;
     __builtin_memcpy(&u, o, 16);
     *reinterpret_cast<uint4 *>(static_cast<DT *>(a.dst) + r * a.pitch + c) = u;
