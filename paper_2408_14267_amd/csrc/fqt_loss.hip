@@ -661,8 +661,13 @@ int64_t dz_pitch_of(int64_t n) { return n <= 512 ? round_up(n, 8) : (round_up(n,
 // Workspace of the backward: dz of a piece (twice for scaled operands), bf16 copies of operands that are codes
 // or whose rows are not whole pieces (w: of a piece), dx in float32 where several pieces add up to it,
 // the partial sums of dbias and those of the products.
-struct BwdWs { size_t dzx, dzw, x, w, dx, bias, part, total; int64_t piece, dz_pitch, pitch, K; bool copy_x, copy_w, direct, sum_dx; };
 struct PiecePlan { tile::Plan z, dx, dw; int64_t unit; Together together; };
+struct BwdWs {
+  size_t dzx, dzw, x, w, dx, bias, part, total;
+  int64_t piece, dz_pitch, pitch, K;
+  bool copy_x, copy_w, direct, sum_dx;
+  PiecePlan plan[2];       // of the pieces, of the last one
+};
 PiecePlan plan_piece(const fqt_loss_desc &d, const Sizes &s, int64_t n, const BwdWs &f) {
   PiecePlan p{};
   p.z = plan_z(d.x_dtype, f.direct, s.M, n, f.K);
@@ -695,8 +700,10 @@ BwdWs bwd_ws(const fqt_loss_desc &d, const Sizes &s) {
   f.dx = f.w + (f.copy_w ? align256(size_t(f.piece) * f.pitch * 2) : 0);
   f.bias = f.dx + (f.sum_dx ? align256(size_t(s.M) * s.K * 4) : 0);
   size_t part = 0, groups = 1;
-  for (const int64_t n : {f.piece, s.N % f.piece ? s.N % f.piece : f.piece}) {
-    const PiecePlan p = plan_piece(d, s, n, f);
+  for (int i = 0; i < 2; ++i) {
+    const int64_t n = i && s.N % f.piece ? s.N % f.piece : f.piece;
+    // (a plan costs the host 2.5 us)
+    const PiecePlan &p = f.plan[i] = i && n == f.piece ? f.plan[0] : plan_piece(d, s, n, f);
     part = std::max({part, part_bytes(p.z, s.M, n), part_bytes(p.dx, s.M, s.K), part_bytes(p.dw, n, s.K),
                      part_bytes(p.together, s.M, n, s.K)});
     groups = std::max(groups, size_t((s.M + p.unit - 1) / p.unit));
@@ -830,7 +837,7 @@ extern "C" int fqt_loss_backward(const fqt_loss_desc *d, const void *x, const vo
   char *base = static_cast<char *>(ws);
   for (int64_t first = 0; first < s.N; first += f.piece) {
     const int64_t n = std::min(f.piece, s.N - first), dz_pitch = dz_pitch_of(n);
-    const PiecePlan plan = plan_piece(*d, s, n, f);
+    const PiecePlan &plan = f.plan[n != f.piece];
     // The operands along k (for z) and along the features (for the gradients).
     Copy cx{}, cw{};
     Operand xr{static_cast<const char *>(x), s.ldx * 2, s.M};

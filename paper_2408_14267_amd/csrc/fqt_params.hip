@@ -180,23 +180,27 @@ __device__ __forceinline__ void decode(uint32_t u, float scale, float (&o)[4]) {
   o[3] = __builtin_amdgcn_cvt_f32_fp8(int(u), 3) * scale;
 }
 
-// A wave takes BLOCKS blocks of 256 elements, four consecutive elements a lane, all loads first.
-constexpr int ADAM_BLOCKS = 4, ADAM_CHUNK = 4 * ADAM_BLOCKS * BLOCK;
+// A wave takes BLOCKS blocks of 256 elements, four consecutive elements a lane, all loads first: four of them with
+// 8-bit states, one with float32 (VGG-16, us with one, two and four blocks: 8-bit states, bf16 gradients 404, 390, 383: 5.1
+// TB/s; float32 686, 730, 725: 5.6 TB/s).
+template <typename E> constexpr int adam_blocks = std::is_same_v<E, CodesEntry> ? 4 : 1;
+template <typename E> constexpr int adam_chunk = 4 * adam_blocks<E> * BLOCK;
 template <typename E>
 __global__ void __launch_bounds__(256) k_adamw(List<E> list, Adam a) {
   constexpr bool CODES = std::is_same_v<E, CodesEntry>;
+  constexpr int BLOCKS = adam_blocks<E>;
   const int at = entry_of(list, blockIdx.x);
   const E &e = list.e[at];
   const bool half = is_half(list, at);
   if (a.step) at_step(a, max(*a.step, int64_t(1)));
   const float s = a.scale ? *a.scale : 1.0f;
   const int lane = threadIdx.x % 64;
-  const int64_t b0 = (int64_t(blockIdx.x - list.begin[at]) * 4 + wave_id()) * ADAM_BLOCKS;
-  float g[ADAM_BLOCKS][4], p[ADAM_BLOCKS][4], m[ADAM_BLOCKS][4], v[ADAM_BLOCKS][4];
-  uint32_t cm[ADAM_BLOCKS], cv[ADAM_BLOCKS];
-  float sm[ADAM_BLOCKS], sv[ADAM_BLOCKS];
+  const int64_t b0 = (int64_t(blockIdx.x - list.begin[at]) * 4 + wave_id()) * BLOCKS;
+  float g[BLOCKS][4], p[BLOCKS][4], m[BLOCKS][4], v[BLOCKS][4];
+  uint32_t cm[BLOCKS], cv[BLOCKS];
+  float sm[BLOCKS], sv[BLOCKS];
 #pragma unroll
-  for (int b = 0; b < ADAM_BLOCKS; ++b) {
+  for (int b = 0; b < BLOCKS; ++b) {
     const int64_t i = (b0 + b) * BLOCK + lane * 4, left = int64_t(e.n) - i;
     load4(e.g, i, half, left, g[b]);
     load4(e.p + i, left, p[b]);
@@ -212,7 +216,7 @@ __global__ void __launch_bounds__(256) k_adamw(List<E> list, Adam a) {
     }
   }
 #pragma unroll
-  for (int b = 0; b < ADAM_BLOCKS; ++b) {
+  for (int b = 0; b < BLOCKS; ++b) {
     const int64_t i = (b0 + b) * BLOCK + lane * 4, left = int64_t(e.n) - i;
     if ((b0 + b) * BLOCK >= e.n) break;
     float root[4];
@@ -426,7 +430,7 @@ extern "C" int fqt_adamw_step(const fqt_adamw_cfg *cfg, const fqt_param *params,
   if (!step_dev) at_step(a, step);
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   auto run = [&]<typename E>() {
-    return for_lists<E>(params, count, ADAM_CHUNK, [&](const List<E> &l, uint32_t chunks) {
+    return for_lists<E>(params, count, adam_chunk<E>, [&](const List<E> &l, uint32_t chunks) {
       k_adamw<E><<<dim3(chunks), dim3(256), 0, st>>>(l, a);
       return last_launch_status();
     });
