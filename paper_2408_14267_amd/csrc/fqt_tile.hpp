@@ -1,9 +1,9 @@
 // Matrix-product tile of the dense operators: D[m][n] = sum over k of x[m][k] w[n][k].
 //
 // A workgroup computes BM x BN outputs, each of its WM x WN waves (BM / WM) x (BN / WN) of them as
-// 16 x 16 MFMA tiles.  The contraction runs in steps of 128 bytes per row through two LDS buffers:
-// the loads of step t + 1 go from memory into LDS without passing registers (buffer_load ... lds)
-// while the matrix cores work on step t, with one barrier per step.
+// 16 x 16 MFMA tiles.  The contraction runs in steps of 128 bytes per row through two or three LDS buffers:
+// the loads of later steps go from memory into LDS without passing registers (buffer_load ... lds)
+// while the matrix cores work on step t.
 //
 // Operand layouts.  ROWS: the operand's rows run along k (x as [M][K], w as [N][K]).  COLS (16-bit
 // types only): it is stored [K][rows], and the transposing LDS read gathers the k's of a fragment.
@@ -420,7 +420,9 @@ __device__ __forceinline__ void run_tile(const Operand &x, const Operand &w, int
 //   0      x, first half; w        x of step t + 2, into the third buffer
 //   1      x, second half          w of step t + 2, into this buffer (w is read by now)
 // so that x has eight, w six phases to arrive.  A wave waits for its own loads at the end of the reading
-// phase before the one that needs them, and the barrier between makes them everyone's.
+// phase before the one that needs them, and the barrier between makes them everyone's.  A step takes 1.37 us (2048
+// cycles of matrix instructions, at the 1.8 to 1.9 GHz that the power limit leaves; 76 % busy in long products).  Quarters
+// (phases of 256 cycles, shorter than a reading phase) took 1.58, and 1.9 with operands across the contraction.
 template <int KIND, int LX, int LW, typename S>
 __device__ __forceinline__ void run_tile8(const Operand &x, const Operand &w, int64_t K,
                                           int64_t m0, int64_t n0, int64_t t0, int64_t t1, char *lds,
@@ -605,7 +607,8 @@ struct Plan {
 
 // us a step of a workgroup with one, two or three of them on a CU, and us before the first and after the last
 // step with Large, Middle and Small tiles: measured on bf16 operands, on pairs as PANEL_ROWS x PANEL_COLS
-// (512 and 1024 rows) and on symmetric products of pairs (512 to 4096 rows).  8-bit operands and the backward's
+// (512 and 1024 rows) and on symmetric products of pairs (512 to 4096 rows).  (Of Large tiles with the loop in quarters:
+// kept, so that plans, and with them the order of sums, stay as they were.)  8-bit operands and the backward's
 // layouts are planned with the bf16 costs, not measured apart: a step is the same bytes, but 8-bit matrix
 // instructions run faster and reads across the contraction slower (6 to 11 %).
 struct Costs { double large[1], middle[2], small[3], start[3]; };
