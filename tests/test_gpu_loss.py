@@ -1,10 +1,11 @@
 """Softmax cross entropy of a linear layer, and its gradients, against the formulas in float64.
 
 Tolerances, with u = 2^-24.  On operands whose sums float32 holds exactly (small integers times powers of two),
-z is exact, and so is z - top; an exponential is off by the rounding of its exponent (|z - top| 1.45 u 2, held to
-|z - top| <= 40 here: 116 u) and its instruction (2 u); at most 80 additions one after the other join them, each
-with an exponential of a difference: their sum is off by 200 u + 80 * 4 u = 520 u at most, and with it log1p of it,
-lse and loss, relative to log1p of the sum; lse, loss and smoothing add their own roundings of 8 u of the terms.
+z is exact; y = z log2(e) is off by u |y| / 2 and the constant's u / 3 of |y - top|, so an exponential, with |z| <= 40 and |z -
+top| <= 40 here, by 2 * 29 u + 20 u + 29 u, its difference's rounding, and its instruction's 2 u: 140 u; at most 80 additions one
+after the other join them, each with an exponential of a difference: their sum is off by 200 u + 80 * 4 u = 520 u at most, and
+with it log1p of it, lse and loss, relative to log1p of the sum; lse, loss and smoothing add their own roundings of 8 u of the
+terms.
 Other operands: z is off by (K + 8) u of the sum of |x w| and the bias, which enters lse once and loss twice.
 Gradients: dz in float32 by 600 u and z's error relative to its terms, then 2^-8 for bf16, carried to dx and dw with the
 magnitudes of the terms; sums of n terms n u of the sum of magnitudes; outputs in bf16 2^-8.
