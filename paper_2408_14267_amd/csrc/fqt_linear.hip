@@ -508,15 +508,18 @@ __global__ void __launch_bounds__(256) k_prepare(DzArgs a, Copy x, Copy w) {
   else repack_rows<ST, bf16>(w, b - a.blocks - x.blocks);
 }
 
-// dbias[n] = sum of the partial rows: 32 columns per workgroup, 8 threads per column, fixed order.
+// dbias[n] = sum of the partial rows: 32 columns per workgroup, 8 threads per column (the first 256 of the
+// workgroup), fixed order.
 __device__ __forceinline__ void sum_dbias(const DbiasArgs &a, uint32_t block, float (*s)[32]) {
   const int64_t c = int64_t(block) * 32 + threadIdx.x % 32;
   const int k = threadIdx.x / 32;
   float v = 0.0f;
-  if (c < a.N)
+  if (k < 8) {
+    if (c < a.N)
 #pragma unroll 8
-    for (int p = k; p < a.parts; p += 8) v += a.part[int64_t(p) * a.N + c];
-  s[k][threadIdx.x % 32] = v;
+      for (int p = k; p < a.parts; p += 8) v += a.part[int64_t(p) * a.N + c];
+    s[k][threadIdx.x % 32] = v;
+  }
   __syncthreads();
   if (k == 0 && c < a.N) {
 #pragma unroll
@@ -550,7 +553,7 @@ __global__ void __launch_bounds__(tile::Small::THREADS, 2) k_product_pair(Produc
   }
 }
 
-// Both products in one launch, and dbias (by the first 256 threads of the last workgroups).  dw_first: its tiles
+// Both products in one launch, and dbias (by the last workgroups).  dw_first: its tiles
 // are the first workgroups.
 template <int SHAPE>
 __global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_product_both(Product px, Epilogue ex, Product pw, Epilogue ew, DbiasArgs bias, int dw_first) {
@@ -560,7 +563,7 @@ __global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_prod
   const uint32_t nx = px.tiles.count * px.tiles.splits, nw = pw.tiles.count * pw.tiles.splits;
   const uint32_t before = dw_first ? nw : nx;
   if (blockIdx.x >= nx + nw) {
-    if (threadIdx.x < 256) sum_dbias(bias, blockIdx.x - nx - nw, reinterpret_cast<float (*)[32]>(lds));
+    sum_dbias(bias, blockIdx.x - nx - nw, reinterpret_cast<float (*)[32]>(lds));
     return;
   }
   const uint32_t b = blockIdx.x < before ? blockIdx.x : blockIdx.x - before;
