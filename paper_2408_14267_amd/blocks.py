@@ -408,22 +408,24 @@ class AdamW(torch.optim.Optimizer):
         if torch.cuda.is_current_stream_capturing():
             raise RuntimeError(f"AdamW: {what} in the first step: take one before a capture")
 
-    def _gradient(self, p):
-        """p's gradient, its elements in p's memory order."""
-        g = p.grad
-        if g.layout != torch.strided or g.dtype not in (_F32, _BF16) or p.device.type != "cuda" or                 p.device.index != torch.cuda.current_device():
+    def _gradient(self, p, g, device):
+        """g, the gradient of p, its elements in p's memory order.  device: the current one."""
+        if g.layout is not torch.strided or g.dtype not in (_F32, _BF16) or p.get_device() != device:
             raise ValueError(f"AdamW updates weights with dense float32 or bfloat16 gradients on the current device, got "
                              f"{g.layout} {g.dtype} on {p.device}")
+        if g.is_contiguous() and p.is_contiguous():
+            return g
         if g.stride() != p.stride():
             g = torch.empty_like(p, dtype=g.dtype).copy_(g)
         return g if g.is_contiguous() else _flat(g)
 
     def _list(self, key, params, starts):
         """The ParamList of some weights and their states, made again when any of them has moved."""
-        states = [self._state(p) for p in params]
-        held = [(p.data_ptr(), s["m"].data_ptr(), s["v"].data_ptr()) for p, s in zip(params, states)]
         at = self._lists.get(key)
-        if at is None or at[0] != held:
+        if at is None or any(p.data_ptr() != where or self.state[p] is not s or s["m"] is not m or s["v"] is not v
+                             for p, (where, s, m, v) in zip(params, at[0])):
+            states = [self._state(p) for p in params]
+            held = [(p.data_ptr(), s, s["m"], s["v"]) for p, s in zip(params, states)]
             flat = {k: [_flat(s[k]) for s in states] for k in ("m", "v")}
             for k in ("m_scale", "v_scale"):
                 flat[k] = [s[k] for s in states] if self.states == "e4m3" else None
@@ -441,18 +443,22 @@ class AdamW(torch.optim.Optimizer):
         if not self.capturable and torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
             raise RuntimeError("AdamW: a captured step would keep its number: make the optimizer capturable")
         # weights with a gradient, by group and by how many steps they have taken
-        todo, gradients, at = {}, [], 0
+        todo, gradients, at, device = {}, [], 0, dense._device() if torch.cuda.is_available() else None
         for i, group in enumerate(self.param_groups):
             cfg = self._config(group)
             for p in group["params"]:
-                if p.grad is not None and p.numel():
-                    g = self._gradient(p)
-                    t = 0 if self.capturable else self.state[p].get("step", 0)
-                    todo.setdefault((i, t), (cfg, [], [], []))
-                    for held, value in zip(todo[i, t][1:], (p, g, at)):
-                        held.append(value)
+                n, g = p.numel(), p.grad
+                if g is not None and n:
+                    g = self._gradient(p, g, device)
+                    key = i, 0 if self.capturable else self.state[p].get("step", 0)
+                    if key not in todo:
+                        todo[key] = cfg, [], [], []
+                    _, params, grads, starts = todo[key]
+                    params.append(p)
+                    grads.append(g)
+                    starts.append(at)
                     gradients.append(g)
-                at += -(-p.numel() // step.FQT_STATE_BLOCK) * step.FQT_STATE_BLOCK
+                at += -(-n // step.FQT_STATE_BLOCK) * step.FQT_STATE_BLOCK
         if not todo:
             return loss
         lists, kept = [], {}

@@ -152,15 +152,19 @@ class ParamList:
     def __init__(self, array, tensors, device, states):
         self.array, self.tensors, self.device, self.states = array, tensors, device, states
         self.count = len(array)
+        self.sizes = [d.n for d in array]
 
     def set_gradients(self, g):
         """Other gradients for the same tensors: of their sizes, float32 or bfloat16, contiguous."""
         if len(g) != self.count:
             raise ValueError(f"set_gradients: {len(g)} gradients for {self.count} tensors")
-        for i, t in enumerate(g):
-            _flat("set_gradients", f"g[{i}]", t, (torch.float32, torch.bfloat16), self.array[i].n, self.device)
+        f32, bf16, device = torch.float32, torch.bfloat16, self.device
+        for i, (t, n) in enumerate(zip(g, self.sizes)):
+            if not ((t.dtype is f32 or t.dtype is bf16) and t.numel() == n and t.is_contiguous() and
+                    t.get_device() == device):
+                _flat("set_gradients", f"g[{i}]", t, (f32, bf16), n, device)
         for d, t in zip(self.array, g):
-            d.g, d.g_dtype = t.data_ptr(), FQT_F32 if t.dtype is torch.float32 else FQT_BF16
+            d.g, d.g_dtype = t.data_ptr(), FQT_F32 if t.dtype is f32 else FQT_BF16
         self.tensors["g"] = list(g)
 
     def drop_gradients(self):

@@ -315,6 +315,58 @@ def test_a_captured_training_step(states):
         assert torch.equal(oa.grad_norm, ob.grad_norm)
 
 
+def test_two_graphs_of_a_loss():
+    """Each graph has workspaces of its own: replayed one after the other, on streams side by side, and between eager calls."""
+    b = blocks()
+    mods = [b.Linear(64, n, operands=o).cuda() for n, o in ((300, "bf16"), (5000, "int8"))]
+    xs, ts = [gen(m, 64, seed=m) for m in (200, 40)], [targets((m,), n) for m, n in ((200, 300), (40, 5000))]
+
+    def call(i):
+        return torch.autograd.grad(mods[i].loss(xs[i], ts[i]), list(mods[i].parameters()))
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        for i in range(2):
+            call(i)
+    torch.cuda.current_stream().wait_stream(side)
+    graphs, outs = [], []
+    for i in range(2):
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph):
+            outs.append(call(i))
+        graphs.append(graph)
+    for s in range(3):
+        for i in range(2):
+            xs[i].copy_(gen(*xs[i].shape, seed=10 * s + i))
+        want = [[g.clone() for g in call(i)] for i in range(2)]
+        torch.cuda.synchronize()
+        with torch.cuda.stream(side):
+            graphs[0].replay()
+        graphs[1].replay()
+        torch.cuda.synchronize()
+        for i in range(2):
+            assert all(torch.equal(p, q) for p, q in zip(want[i], outs[i])), (s, i)
+
+
+def test_adamw_on_another_stream_and_with_other_states():
+    b = blocks()
+    (pa, pb) = (weights(), weights())
+    oa, ob = (b.AdamW(p, lr=0.01, max_norm=0.5) for p in (pa, pb))
+    side = torch.cuda.Stream()
+    for s in range(3):
+        for i, (p, q) in enumerate(zip(pa, pb)):
+            p.grad, q.grad = gen(*p.shape, seed=10 * s + i), gen(*p.shape, seed=10 * s + i)
+        oa.step()
+        side.wait_stream(torch.cuda.current_stream())
+        with torch.cuda.stream(side):
+            ob.step()
+        torch.cuda.current_stream().wait_stream(side)
+        if s == 0:                                           # the same states in other tensors
+            ob.state[pb[0]] = {k: v.clone() if torch.is_tensor(v) else v for k, v in ob.state[pb[0]].items()}
+    assert all(torch.equal(p, q) for p, q in zip(pa, pb))
+
+
 def test_a_first_step_is_not_captured():
     b = blocks()
     p = torch.nn.Parameter(gen(100))
