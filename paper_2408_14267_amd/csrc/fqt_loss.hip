@@ -63,16 +63,41 @@ struct Out {
   float *loss, *lse;
   int64_t M, N, ignore;
   float smoothing;
+  float *mean;             // for a launch of one workgroup that has all rows, or null
 };
 // Row m from its pair, the sum of its y and the target's y.
-__device__ __forceinline__ void finish_row(const Out &o, int64_t m, Soft s, float sum, float at) {
+// Returns its loss, and in `counts` whether it counts.
+__device__ __forceinline__ float finish_row(const Out &o, int64_t m, Soft s, float sum, float at, bool &counts) {
   const float rest = log1pf(s.rest);
   o.lse[m] = fmaf(s.top, LN2, rest);
   const int64_t t = o.target[m];
   float loss = s.top - at;
   if (o.smoothing > 0.0f) loss = (1.0f - o.smoothing) * loss + o.smoothing * (s.top - sum / float(o.N));
   loss = fmaf(loss, LN2, rest);
-  o.loss[m] = t == o.ignore ? 0.0f : t < 0 || t >= o.N ? __builtin_nanf("") : loss;
+  counts = t != o.ignore;
+  loss = !counts ? 0.0f : t < 0 || t >= o.N ? __builtin_nanf("") : loss;
+  o.loss[m] = loss;
+  return loss;
+}
+// mean[0]: of the losses of the rows that count, mean[1]: 1 / their number.
+__device__ __forceinline__ void store_mean(float *mean, double sum, int64_t count) {
+  mean[0] = count ? float(sum / double(count)) : 0.0f;
+  mean[1] = count ? float(1.0 / double(count)) : 0.0f;
+}
+// The sum and the count of a workgroup's threads to its mean.
+__device__ __forceinline__ void mean_of(float *mean, double sum, int64_t count) {
+  __shared__ double sums[16];
+  __shared__ int64_t counts[16];
+#pragma unroll
+  for (int o = 32; o > 0; o /= 2) {
+    sum += __shfl_xor(sum, o);
+    count += __shfl_xor(count, o);
+  }
+  if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = sum, counts[threadIdx.x / 64] = count;
+  __syncthreads();
+  if (threadIdx.x) return;
+  for (uint32_t i = 1; i < blockDim.x / 64; ++i) sum += sums[i], count += counts[i];
+  store_mean(mean, sum, count);
 }
 
 // ----------------------------------------------------------------------------- forward by tiles
@@ -278,16 +303,53 @@ __global__ void __launch_bounds__(256) k_loss_rows(Pairs p, Out o) {
         sum += b.z;
       }
       const int64_t t = p.target[m];
-      finish_row(o, m, s, sum, t >= 0 && t < o.N ? p.at[m] : 0.0f);
+      bool counts;
+      finish_row(o, m, s, sum, t >= 0 && t < o.N ? p.at[m] : 0.0f, counts);
     }
     __syncthreads();
   }
 }
+// The same for up to 1024 rows by one workgroup, `rows` (a power of two) threads side by side, and their mean: a launch less
+// (4 us of the 15 of a small call).
+__global__ void __launch_bounds__(1024) k_loss_rows_mean(Pairs p, Out o, uint32_t rows) {
+  constexpr int AHEAD = 8;
+  __shared__ float4 all[1024];
+  const uint32_t groups = 1024 / rows, g = threadIdx.x / rows;
+  const int64_t m = threadIdx.x % rows;
+  Soft s{NOTHING, 0.0f};
+  float sum = 0.0f;
+  if (m < o.M)
+    for (int64_t i0 = g; i0 < p.slots; i0 += groups * AHEAD) {
+      Soft t[AHEAD];
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i)
+        t[i] = i0 + groups * i < p.slots ? p.pairs[(i0 + groups * i) * o.M + m] : Soft{NOTHING, 0.0f};
+#pragma unroll
+      for (int i = 0; i < AHEAD; ++i) s = join(s, t[i]);
+      if (p.sums)
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) sum += i0 + groups * i < p.slots ? p.sums[(i0 + groups * i) * o.M + m] : 0.0f;
+    }
+  all[threadIdx.x] = make_float4(s.top, s.rest, sum, 0.0f);
+  __syncthreads();
+  float loss = 0.0f;
+  bool counts = false;
+  if (g == 0 && m < o.M) {
+    for (uint32_t i = 1; i < groups; ++i) {
+      const float4 b = all[i * rows + m];
+      s = join(s, Soft{b.x, b.y});
+      sum += b.z;
+    }
+    const int64_t t = p.target[m];
+    loss = finish_row(o, m, s, sum, t >= 0 && t < o.N ? p.at[m] : 0.0f, counts);
+  }
+  mean_of(o.mean, double(loss), counts);
+}
 
 // ----------------------------------------------------------------------------- forward by rows
 // Where z passes through the workspace (few rows, or a split contraction): a workgroup takes CHUNK columns of a
-// row down to a pair, or the whole row to its loss if that is all; z are sums of `splits` words.  One row of 65536 by
-// one workgroup took 18 us.
+// row down to a pair, or the whole row to its loss if that is all (then every 256 threads of a workgroup take a row, and one
+// with all rows their mean); z are sums of `splits` words.  One row of 65536 by one workgroup took 18 us.
 struct RowArgs {
   const float *part;
   const float *sx, *sw, *bias;
@@ -296,18 +358,20 @@ struct RowArgs {
 };
 constexpr int CHUNK = 4096;
 template <bool INTS>
-__global__ void __launch_bounds__(256) k_loss_dense(RowArgs a, Pairs p, Out o) {
-  __shared__ float4 waves[4];
-  __shared__ float found;
-  const int64_t m = blockIdx.x / p.slots, slot = blockIdx.x % p.slots, t = o.target[m];
+__global__ void __launch_bounds__(1024) k_loss_dense(RowArgs a, Pairs p, Out o) {
+  __shared__ float4 waves[16];
+  __shared__ float found_of[4];
+  const uint32_t thread = threadIdx.x % 256, row = threadIdx.x / 256;
+  const int64_t m = blockIdx.x / p.slots * (blockDim.x / 256) + row, slot = blockIdx.x % p.slots, t = o.target[m];
   const int64_t n0 = slot * CHUNK, end = min(o.N, n0 + CHUNK);
   const float sx = a.sx ? a.sx[m] : 1.0f;
-  if (threadIdx.x == 0) found = 0.0f;
+  float &found = found_of[row];
+  if (thread == 0) found = 0.0f;
   __syncthreads();
   Soft s{NOTHING, 0.0f};
   float sum = 0.0f;
 #pragma unroll 4
-  for (int64_t n = n0 + threadIdx.x * 4; n < end; n += 1024) {
+  for (int64_t n = n0 + thread * 4; n < end; n += 1024) {
     const int cnt = int(min(end - n, int64_t(4)));
     std::conditional_t<INTS, int, float> w[4] = {};
     for (uint32_t i = 0; i < a.splits; ++i) {
@@ -353,25 +417,28 @@ __global__ void __launch_bounds__(256) k_loss_dense(RowArgs a, Pairs p, Out o) {
   sum += lane_xor_f<32>(sum);
   if (threadIdx.x % 64 == 0) waves[threadIdx.x / 64] = make_float4(s.top, s.rest, sum, 0.0f);
   __syncthreads();
-  if (threadIdx.x) return;
+  if (thread == 0) {
 #pragma unroll
-  for (int i = 1; i < 4; ++i) {
-    s = join(s, Soft{waves[i].x, waves[i].y});
-    sum += waves[i].z;
+    for (int i = 1; i < 4; ++i) {
+      const float4 b = waves[row * 4 + i];
+      s = join(s, Soft{b.x, b.y});
+      sum += b.z;
+    }
   }
   if (p.slots == 1) {
-    finish_row(o, m, s, sum, found);
+    float loss = 0.0f;
+    bool counts = false;
+    if (thread == 0) loss = finish_row(o, m, s, sum, found, counts);
+    if (o.mean) mean_of(o.mean, double(loss), counts);
     return;
   }
+  if (thread) return;
   p.pairs[slot * o.M + m] = s;
   if (p.sums) p.sums[slot * o.M + m] = sum;
   if (t >= n0 && t < end) p.at[m] = found;
 }
 
-// mean[0]: of the losses of the rows that count, mean[1]: 1 / their number.
 __global__ void __launch_bounds__(1024) k_loss_mean(const float *loss, const int64_t *target, int64_t ignore, int64_t M, float *mean) {
-  __shared__ double sums[16];
-  __shared__ int64_t counts[16];
   double sum = 0.0;
   int64_t count = 0;
 #pragma unroll 4
@@ -380,17 +447,7 @@ __global__ void __launch_bounds__(1024) k_loss_mean(const float *loss, const int
     sum += loss[m];
     count += target[m] != ignore;
   }
-#pragma unroll
-  for (int o = 32; o > 0; o /= 2) {
-    sum += __shfl_xor(sum, o);
-    count += __shfl_xor(count, o);
-  }
-  if (threadIdx.x % 64 == 0) sums[threadIdx.x / 64] = sum, counts[threadIdx.x / 64] = count;
-  __syncthreads();
-  if (threadIdx.x) return;
-  for (int i = 1; i < 16; ++i) sum += sums[i], count += counts[i];
-  mean[0] = count ? float(sum / double(count)) : 0.0f;
-  mean[1] = count ? float(1.0 / double(count)) : 0.0f;
+  mean_of(mean, sum, count);
 }
 
 // ----------------------------------------------------------------------------- dz
@@ -735,17 +792,29 @@ int launch_dz(const PiecePlan &plan, Logits p, const DzOut &o, hipStream_t st) {
   }
   return last_launch_status();
 }
-// z in the workspace to pairs.
-int launch_dense(const RowArgs &a, const Pairs &p, const Out &o, bool ints, hipStream_t st) {
-  const dim3 grid(uint32_t(o.M * p.slots)), block(256);
+// z in the workspace to pairs, or to the losses where a chunk is a row; few: all rows by one workgroup then, and the
+// mean, if it is asked for.
+int launch_dense(const RowArgs &a, const Pairs &p, Out o, bool ints, bool few, float *mean, hipStream_t st) {
+  few = few && p.slots == 1;
+  if (few) o.mean = mean;
+  const dim3 grid(few ? 1u : uint32_t(o.M * p.slots)), block(few ? uint32_t(256 * o.M) : 256);
   if (ints) k_loss_dense<true><<<grid, block, 0, st>>>(a, p, o);
   else k_loss_dense<false><<<grid, block, 0, st>>>(a, p, o);
   return last_launch_status();
 }
-// Pairs to the losses (nothing where the pass before had whole rows).
-int launch_rows(const Pairs &p, const Out &o, hipStream_t st) {
-  // (a launch counts its threads in 32 bits)
-  k_loss_rows<<<dim3(uint32_t(std::min<int64_t>((o.M + 15) / 16, 1 << 16))), dim3(256), 0, st>>>(p, o);
+// Whether one workgroup takes all rows' pairs, 32 each at most.
+bool one_group(const Pairs &p, int64_t M) { return M <= 1024 && M * p.slots <= 32768; }
+// Pairs to the losses, and the mean where one workgroup has all rows.
+int launch_rows(const Pairs &p, Out o, float *mean, hipStream_t st) {
+  if (mean && one_group(p, o.M)) {
+    uint32_t rows = 16;
+    while (rows < o.M) rows *= 2;
+    o.mean = mean;
+    k_loss_rows_mean<<<dim3(1), dim3(1024), 0, st>>>(p, o, rows);
+  } else {
+    // (a launch counts its threads in 32 bits)
+    k_loss_rows<<<dim3(uint32_t(std::min<int64_t>((o.M + 15) / 16, 1 << 16))), dim3(256), 0, st>>>(p, o);
+  }
   return last_launch_status();
 }
 
@@ -776,7 +845,8 @@ extern "C" int fqt_loss_forward(const fqt_loss_desc *d, const void *x, const voi
   if (ws_bytes < f.total) return FQT_E_WORKSPACE;
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   char *base = static_cast<char *>(ws);
-  const Out o{target, loss, lse, s.M, s.N, d->ignore, d->smoothing};
+  const Out o{target, loss, lse, s.M, s.N, d->ignore, d->smoothing, nullptr};
+  bool averaged = false;
   const Pairs pairs{reinterpret_cast<Soft *>(base + f.pairs),
                     d->smoothing > 0.0f ? reinterpret_cast<float *>(base + f.sums) : nullptr,
                     reinterpret_cast<float *>(base + f.at), target, f.slots};
@@ -788,8 +858,9 @@ extern "C" int fqt_loss_forward(const fqt_loss_desc *d, const void *x, const voi
     l.y_dtype = l.dx_dtype = l.dw_dtype = FQT_F32;
     float *z = reinterpret_cast<float *>(base);
     FQT_TRY_(fqt_linear_forward(&l, x, w, x_scale, w_scale, bias, nullptr, nullptr, z, ws, ws_bytes, hip_stream));
-    FQT_TRY_(launch_dense({z, nullptr, nullptr, nullptr, s.N, 1}, pairs, o, false, st));
-    if (f.slots > 1) FQT_TRY_(launch_rows(pairs, o, st));
+    FQT_TRY_(launch_dense({z, nullptr, nullptr, nullptr, s.N, 1}, pairs, o, false, true, mean, st));
+    averaged = f.slots == 1 || one_group(pairs, s.M);
+    if (f.slots > 1) FQT_TRY_(launch_rows(pairs, o, mean, st));
   } else if (s.M) {
     Copy cx{}, cw{};
     auto operand = [&](const void *p, bool copy, size_t at, int64_t rows, int64_t ld, Copy *c) -> Operand {
@@ -805,10 +876,13 @@ extern "C" int fqt_loss_forward(const fqt_loss_desc *d, const void *x, const voi
     if (ints) FQT_TRY_(launch_logits<tile::I8K>(f.plan, p, pairs, st));
     else if (s.codes) FQT_TRY_(launch_logits<tile::WIDEK>(f.plan, p, pairs, st));
     else FQT_TRY_(launch_logits<tile::BF16K>(f.plan, p, pairs, st));
-    if (f.plan.splits > 1) FQT_TRY_(launch_dense({p.part, x_scale, w_scale, bias, p.ldp, f.plan.splits}, pairs, o, ints, st));
-    if (f.plan.splits == 1 || f.slots > 1) FQT_TRY_(launch_rows(pairs, o, st));
+    if (f.plan.splits > 1) FQT_TRY_(launch_dense({p.part, x_scale, w_scale, bias, p.ldp, f.plan.splits}, pairs, o, ints, false, nullptr, st));
+    if (f.plan.splits == 1 || f.slots > 1) {
+      averaged = one_group(pairs, s.M);
+      FQT_TRY_(launch_rows(pairs, o, mean, st));
+    }
   }
-  if (!mean) return FQT_OK;
+  if (!mean || averaged) return FQT_OK;
   k_loss_mean<<<dim3(1), dim3(1024), 0, st>>>(loss, target, d->ignore, s.M, mean);
   return last_launch_status();
 }
