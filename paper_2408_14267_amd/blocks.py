@@ -4,8 +4,9 @@ RMSNorm, Linear and NormLinear call fqt_rmsnorm_*, fqt_quantize_rows and fqt_lin
 backward); NormLinear keeps the activations between the norm and the product as 8-bit codes.  Muon
 updates latent weight matrices (and convolution weights, unfolded) by fqt_muon_step.  Linear.loss is the softmax
 cross entropy of a layer's outputs without computing them as a matrix (fqt_loss_*); AdamW updates all tensors of a model
-by fqt_adamw_step, with states in float32 or 8 bits, clipped by fqt_grad_norm.  ResidualMLP puts them together with BinaryLinear: a float32 residual stream, blocks of a normed 8-bit expansion with
-GELU and a binary projection, the first and last layers at full width as in the networks of `train`.
+by fqt_adamw_step, with states in float32 or 8 bits, clipped by fqt_grad_norm.  ResidualMLP puts them together with
+BinaryLinear: a float32 residual stream, blocks of a normed 8-bit expansion with GELU and a binary projection, the
+first and last layers at full width as in the networks of `train`.
 
 Modules take [..., features] inputs of float32 or bfloat16, keep float32 parameters, and cast or
 quantize the weight in every forward pass.  Gradients come in the type of what they belong to (the products
@@ -354,7 +355,8 @@ class AdamW(torch.optim.Optimizer):
     for 8-bit states, stochastically rounded with the random sequence of `seed` (2 bytes a weight instead of 8).
     max_norm: the gradients are clipped to this norm over all groups; `grad_norm` holds the last step's norm
     and factor (on the device).  capturable: the step number is counted on the device (one for each group, weights without a
-    gradient included), so that step() may be captured into a graph; the learning rate is then the captured one.
+    gradient included), so that step() may be captured into a graph; the learning rate is then the captured one, and a
+    checkpoint is loaded before the capture.
     What cannot be updated is refused when its group is added or before a step updates anything."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, states="f32", seed=0,
@@ -443,21 +445,21 @@ class AdamW(torch.optim.Optimizer):
         if not self.capturable and torch.cuda.is_available() and torch.cuda.is_current_stream_capturing():
             raise RuntimeError("AdamW: a captured step would keep its number: make the optimizer capturable")
         # weights with a gradient, by group and by how many steps they have taken
-        todo, gradients, at, device = {}, [], 0, dense._device() if torch.cuda.is_available() else None
+        todo, at, device = {}, 0, dense._device() if torch.cuda.is_available() else None
         for i, group in enumerate(self.param_groups):
             cfg = self._config(group)
             for p in group["params"]:
                 n, g = p.numel(), p.grad
                 if g is not None and n:
                     g = self._gradient(p, g, device)
-                    key = i, 0 if self.capturable else self.state[p].get("step", 0)
+                    state = None if self.capturable else self.state.get(p)   # (none is made before all are checked)
+                    key = i, state["step"] if state else 0
                     if key not in todo:
                         todo[key] = cfg, [], [], []
                     _, params, grads, starts = todo[key]
                     params.append(p)
                     grads.append(g)
                     starts.append(at)
-                    gradients.append(g)
                 at += -(-n // step.FQT_STATE_BLOCK) * step.FQT_STATE_BLOCK
         if not todo:
             return loss
@@ -471,9 +473,9 @@ class AdamW(torch.optim.Optimizer):
         self._lists = kept                   # (those of this step: other sets of weights with gradients go)
         scale = None
         if self.max_norm is not None:
-            whole = lists[0][4] if len(lists) == 1 else step.param_list(gradients)
+            whole = step.joined([at[4] for at in lists])
             if self.grad_norm is None:
-                self.grad_norm = torch.empty(2, device=gradients[0].device)
+                self.grad_norm = torch.empty(2, device=lists[0][3][0].device)
             step.fqt_grad_norm(whole, self.grad_norm, _workspace(step.fqt_grad_norm_workspace_size(whole),
                                                                  self.grad_norm.device), max_norm=self.max_norm)
             scale = self.grad_norm[1:]
@@ -497,12 +499,12 @@ class AdamW(torch.optim.Optimizer):
                 "capturable": self.capturable, "grad_norm": None, "_lists": {}}
 
     def load_state_dict(self, state_dict):
-        if any(("m_scale" in s) != (self.states == "e4m3") for s in state_dict["state"].values()):
+        if any(s and ("m_scale" in s) != (self.states == "e4m3") for s in state_dict["state"].values()):
             raise ValueError(f"a state of another kind than {self.states}")
         super().load_state_dict(state_dict)
         self._lists = {}
         for state in self.state.values():
-            if self.states == "e4m3":          # (loading casts to the weights' type, which holds the codes exactly)
+            if "m_scale" in state:             # (loading casts to the weights' type, which holds the codes exactly)
                 for name in ("m", "v"):
                     state[name] = state[name].to(torch.float8_e4m3fn)
 

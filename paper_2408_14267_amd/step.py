@@ -229,6 +229,19 @@ def param_list(g, p=None, m=None, v=None, m_scale=None, v_scale=None, first=None
     return ParamList(array, tensors, dev, states)
 
 
+def joined(lists):
+    """The gradients of several lists on one device as a ParamList for fqt_grad_norm, until theirs change."""
+    if len(lists) == 1:
+        return lists[0]
+    array, at = (fqt_param * sum(p.count for p in lists))(), 0
+    for p in lists:
+        if p.device != lists[0].device:
+            raise ValueError(f"joined: lists on devices {lists[0].device} and {p.device}")
+        ctypes.memmove(ctypes.byref(array, at * ctypes.sizeof(fqt_param)), p.array, ctypes.sizeof(p.array))
+        at += p.count
+    return ParamList(array, {"g": [t for p in lists for t in p.tensors["g"]]}, lists[0].device, None)
+
+
 def fqt_grad_norm_workspace_size(params):
     n = c_size_t()
     _check(_lib.fqt_grad_norm_workspace_size(params.array, params.count, ctypes.byref(n)),

@@ -228,6 +228,8 @@ def train_step(model, opt, x, y, autocast_dtype=None, fused_loss=False):
     """One step: forward, cross-entropy loss, backward, optimizer update.  Returns the loss.  fused_loss: by
     model.loss(x, y), which computes no logits (blocks.ResidualMLP)."""
     opt.zero_grad(set_to_none=True)
+    if fused_loss and autocast_dtype is not None:
+        raise ValueError("fused_loss takes the types of the model's layers, not autocast's")
     if fused_loss:
         loss = model.loss(x, y)
     elif autocast_dtype is not None:

@@ -235,6 +235,16 @@ def test_adamw_refusals():
     with pytest.raises(ValueError, match="current device"):
         opt.step()
     assert torch.equal(p, before)                        # nothing was updated
+    for kind in ("f32", "e4m3"):                         # and nothing is left that a checkpoint would carry
+        opt = b.AdamW([p, torch.nn.Parameter(torch.zeros(4))], states=kind)
+        opt.param_groups[0]["params"][1].grad = torch.zeros(4)
+        with pytest.raises(ValueError):
+            opt.step()
+        b.AdamW([p, torch.nn.Parameter(torch.zeros(4))], states=kind).load_state_dict(opt.state_dict())
+    from paper_2408_14267_amd import train
+    with pytest.raises(ValueError, match="autocast"):
+        train.train_step(b.ResidualMLP(8, 3, width=16, hidden=16, depth=0).cuda(), b.Optimizers(), None, None,
+                         autocast_dtype=torch.bfloat16, fused_loss=True)
     with pytest.raises(ValueError, match="max_norm"):
         b.muon_and_adam(torch.nn.Linear(3, 3), max_norm=1.0)
 
