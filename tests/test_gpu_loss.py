@@ -135,7 +135,8 @@ def check_forward(o, M, N, K, kind, smoothing=0.0, exact_sums=False, **kw):
 SHAPES = [(1, 1, 8), (1, 10, 64), (1, 4099, 513), (2, 1000, 4096), (4, 65, 1), (3, 32768, 96), (5, 1, 16),
           (5, 7, 3), (16, 1000, 2048), (63, 64, 64), (64, 65, 65), (64, 1000, 4096), (65, 129, 300), (128, 128, 512),
           (129, 255, 72), (130, 10007, 40), (257, 300, 1153), (300, 4096, 256), (513, 2049, 128), (777, 1000, 513),
-          (1000, 513, 64), (2049, 130, 64), (2304, 4864, 64), (40, 131072, 16), (5000, 10, 32)]
+          (1000, 513, 64), (2049, 130, 64), (2304, 4864, 64), (40, 131072, 16), (5000, 10, 32), (4608, 4097, 72),
+          (1100, 9000, 520)]
 
 
 @pytest.mark.parametrize("M,N,K", SHAPES)
@@ -163,6 +164,7 @@ def test_forward_of_strided_rows(M, N, K, ldx, ldw, kind):
 @pytest.mark.parametrize("M,N,K", [(1, 10, 64), (5, 1000, 256), (64, 1000, 4096), (300, 700, 128), (1500, 4100, 64)])
 @pytest.mark.parametrize("smoothing", [0.1, 1.0])
 def test_smoothing(M, N, K, smoothing):
+    check_forward(make(M, N, K, "e4m3", seed=4), M, N, K, "e4m3", smoothing)
     check_forward(make(M, N, K, "bf16", seed=4), M, N, K, "bf16", smoothing)
     check_forward(make(M, N, K, "int8", seed=4, bias=False), M, N, K, "int8", smoothing)
 
@@ -301,7 +303,7 @@ def check_backward(o, M, N, K, kind, smoothing=0.0, reduction="none", dx_dtype="
 
 BACK = [(1, 10, 64), (1, 4099, 513), (4, 65, 1), (5, 1, 16), (5, 7, 3), (16, 1000, 2048), (64, 1000, 4096), (65, 129, 300),
         (129, 255, 72), (130, 10007, 40), (257, 300, 1153), (777, 1000, 513), (1000, 513, 64), (2304, 4864, 64),
-        (5000, 10, 32)]
+        (5000, 10, 32), (4608, 4097, 72), (1100, 9000, 520), (512, 8192, 1024), (3000, 257, 2048), (9000, 100, 512)]
 
 
 @pytest.mark.parametrize("M,N,K", BACK)
@@ -348,6 +350,15 @@ def test_backward_in_pieces(M, N, K, kind, dx_dtype):
     check_backward(make(M, N, K, kind, seed=13), M, N, K, kind, dx_dtype=dx_dtype)
 
 
+@pytest.mark.parametrize("kind", ["bf16", "int8", "e4m3"])
+def test_large(kind):
+    """Sizes that take 256 x 256 tiles in every product, smoothed labels."""
+    M, N, K = 4608, 12288, 1024
+    o = make(M, N, K, kind, seed=24)
+    check_forward(o, M, N, K, kind, 0.1)
+    check_backward(o, M, N, K, kind, 0.1)
+
+
 def test_backward_of_rows_that_do_not_count():
     M, N, K = 300, 700, 128
     o = make(M, N, K, "bf16", seed=14, ignored=2.0)
@@ -373,6 +384,36 @@ def test_backward_of_no_rows():
     s.fqt_loss_backward(desc, x, w, torch.empty(0, dtype=torch.int64, device="cuda"), e, s.loss_workspace(desc, True),
                         dloss=e, dw=dw, dbias=dbias)
     assert (dw == 0).all() and (dbias == 0).all()
+
+
+@pytest.mark.parametrize("M,N", [(1, 1), (3, 10), (300, 700)])
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+def test_no_features(M, N, kind):
+    """A contraction over nothing: z is the bias."""
+    o = make(M, N, 0, kind, seed=22, ignored=0.0)
+    check_forward(o, M, N, 0, kind)
+    got = check_backward(o, M, N, 0, kind)
+    assert got["dx"].shape == (M, 0) and got["dw"].shape == (N, 0)
+
+
+@pytest.mark.parametrize("M,N,K", [(3, 100, 64), (200, 300, 96)])
+def test_ignored_class_numbers(M, N, K):
+    """`ignore` may be a class (a padding token): its rows are left out, the class stays in the sums."""
+    s = step()
+    o = make(M, N, K, "bf16", seed=23, ignored=0.0)
+    o["target"][::2] = 7
+    desc = s.loss_desc(M, N, K, ignore=7)
+    loss, lse, mean = (torch.empty(n, device="cuda") for n in (M, M, 2))
+    s.fqt_loss_forward(desc, o["x"], o["w"], o["target"], loss, lse, s.loss_workspace(desc), bias=o["bias"], mean=mean)
+    z, lse64, _, _, zerr, _ = reference(o)
+    assert (loss[::2] == 0).all() and ((lse.double() - lse64).abs() <= 600 * U * lse64.abs() + zerr).all()
+    dx, db = torch.empty_like(o["x"]), torch.empty(N, device="cuda")
+    s.fqt_loss_backward(desc, o["x"], o["w"], o["target"], lse, s.loss_workspace(desc, True), dmean=torch.ones(1, device="cuda"),
+                        mean=mean, bias=o["bias"], dx=dx, dbias=db)
+    assert (dx[::2] == 0).all() and (o["target"] == 7).sum() + round(1 / mean[1].item()) == M
+    counted = o["target"] != 7
+    want = (torch.exp(z - lse.double()[:, None])[counted].sum(dim=0) - torch.bincount(o["target"][counted], minlength=N)) * mean[1].double()
+    assert ((db.double() - want).abs() <= (700 * U + 4 * zerr.max()) * 2 * mean[1].double() * M + 1e-12).all()
 
 
 def test_gradient_against_differences():
