@@ -616,8 +616,8 @@ int check_linear(const fqt_linear_desc *d, Sizes *s) {
 
 }  // namespace
 
-tile::Plan plan_of(int64_t M, int64_t N, int64_t K, size_t e) {
-  return tile::make_plan(M, N, (K * int64_t(e) + tile::KB - 1) / tile::KB, false, tile::DENSE_COSTS);
+tile::Plan plan_of(int64_t M, int64_t N, int64_t K, size_t e, const tile::Costs &costs) {
+  return tile::make_plan(M, N, (K * int64_t(e) + tile::KB - 1) / tile::KB, false, costs);
 }
 size_t part_bytes(const tile::Plan &p, int64_t M, int64_t N) {
   return p.splits > 1 ? align256(size_t(p.splits) * M * round_up(N, 8) * 4) : 0;
@@ -754,7 +754,7 @@ tile::Tiles whole_grid(int64_t M, int64_t N, int64_t K, int64_t edge) {
 }  // namespace
 
 Together plan_together(int64_t M, int64_t N, int64_t K, const tile::Plan &dx, const tile::Plan &dw) {
-  const tile::Costs &c = tile::DENSE_COSTS;
+  const tile::Costs &c = tile::STEP_COSTS;
   double best = dx.us + dw.us;
   Together how{};
   // us of both products' tiles, `cu` of them on a CU at a time: evenly over the CUs, and half of one of the last

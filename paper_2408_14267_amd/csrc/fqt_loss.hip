@@ -665,13 +665,13 @@ int check_pointers(const fqt_loss_desc &d, const Sizes &s, const void *x, const 
 // those of w.
 constexpr int64_t FEW_ROWS = 4;
 
-// us a step and before and after the steps of widened codes (as tile::DENSE_COSTS).
-constexpr tile::Costs WIDE_COSTS{{2.9}, {1.1, 1.6}, {0.35, 0.55, 0.85}, {6, 5, 4}};
+// us a step and before and after the steps of widened codes (as tile::STEP_COSTS).
+constexpr tile::Costs WIDE_COSTS{{2.5}, {1.1, 1.6}, {0.35, 0.55, 0.85}, {6, 5, 4}};
 
 // z's plan, from codes themselves (direct) or operands of 16 bits.
 tile::Plan plan_z(int32_t dtype, bool direct, int64_t M, int64_t n, int64_t K) {
   if (direct && dtype == FQT_E4M3) return tile::make_plan(M, n, (K + tile::KB - 1) / tile::KB, false, WIDE_COSTS);
-  return plan_of(M, n, K, direct ? 1 : 2);
+  return plan_of(M, n, K, direct ? 1 : 2, tile::STEP_COSTS);
 }
 
 // Workspace of the forward: copies of operands whose rows are not whole 16-byte pieces,
@@ -728,8 +728,8 @@ struct BwdWs {
 PiecePlan plan_piece(const fqt_loss_desc &d, const Sizes &s, int64_t n, const BwdWs &f) {
   PiecePlan p{};
   p.z = plan_z(d.x_dtype, f.direct, s.M, n, f.K);
-  p.dx = plan_of(s.M, s.K, n, 2);
-  p.dw = plan_of(n, s.K, s.M, 2);
+  p.dx = plan_of(s.M, s.K, n, 2, tile::STEP_COSTS);
+  p.dw = plan_of(n, s.K, s.M, 2, tile::STEP_COSTS);
   p.together = plan_together(s.M, n, s.K, p.dx, p.dw);
   p.unit = 128;            // rows of a wave's results: the fewest of the launches
   for (int i = 0; i < p.z.launches; ++i)

@@ -8,7 +8,7 @@ namespace fqt {
 namespace dense {
 
 // Plan of a product of operands of e bytes, and the bytes of its partial sums.
-tile::Plan plan_of(int64_t M, int64_t N, int64_t K, size_t e);
+tile::Plan plan_of(int64_t M, int64_t N, int64_t K, size_t e, const tile::Costs &costs = tile::DENSE_COSTS);
 size_t part_bytes(const tile::Plan &p, int64_t M, int64_t N);
 inline int64_t round_up(int64_t v, int64_t q) { return (v + q - 1) / q * q; }
 // Whether rows of n elements of e bytes, ld apart, are whole 16-byte pieces.
@@ -28,7 +28,7 @@ struct Together {
   int shape;
   tile::Tiles dx, dw;
 };
-// The cheapest of these, on if it takes less time than the two plans.
+// The cheapest of these by tile::STEP_COSTS, on if it takes less time than the two plans.
 Together plan_together(int64_t M, int64_t N, int64_t K, const tile::Plan &dx, const tile::Plan &dw);
 size_t part_bytes(const Together &t, int64_t M, int64_t N, int64_t K);
 
