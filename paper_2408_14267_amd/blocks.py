@@ -350,13 +350,21 @@ def _flat(t):
     return t.detach().as_strided((t.numel(),), (1,))
 
 
+def _same_order(p, strides):
+    """Whether p's elements lie in memory as those of a tensor of its shape with these strides."""
+    have = p.stride()
+    return have == strides or (len(have) == len(strides) and
+                               all(a == b or n == 1 for a, b, n in zip(have, strides, p.shape)))
+
+
 class AdamW(torch.optim.Optimizer):
     """AdamW for float32 weights of any shape, all tensors of a group in one fqt_adamw_step.  states: "f32", or "e4m3"
     for 8-bit states, stochastically rounded with the random sequence of `seed` (2 bytes a weight instead of 8).
     max_norm: the gradients are clipped to this norm over all groups; `grad_norm` holds the last step's norm
     and factor (on the device).  capturable: the step number is counted on the device (one for each group, weights without a
     gradient included), so that step() may be captured into a graph; the learning rate is then the captured one, and a
-    checkpoint is loaded before the capture.
+    checkpoint is loaded before the capture.  States lie in memory as their weights do: those in float32 follow weights whose
+    memory order has changed, 8-bit ones, whose blocks are of memory order, are refused then.
     What cannot be updated is refused when its group is added or before a step updates anything."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.0, states="f32", seed=0,
@@ -403,7 +411,21 @@ class AdamW(torch.optim.Optimizer):
                 for name in ("m", "v"):
                     state[name] = torch.zeros(p.numel(), dtype=torch.float8_e4m3fn, device=p.device)
                     state[name + "_scale"] = torch.zeros(blocks, device=p.device)
+                state["strides"] = p.stride()
+        elif self.states == "f32":
+            for name in ("m", "v"):
+                if not _same_order(p, state[name].stride()):
+                    self._not_captured("states are laid out again")
+                    state[name] = torch.empty_like(p).copy_(state[name])
         return state
+
+    def _check_state(self, p, state):
+        if self.states == "f32":
+            if state["m"].shape != p.shape or state["v"].shape != p.shape:
+                raise ValueError(f"AdamW: states of shapes {tuple(state['m'].shape)}, {tuple(state['v'].shape)} for "
+                                 f"weights of {tuple(p.shape)}")
+        elif not _same_order(p, state["strides"]):
+            raise ValueError(f"AdamW: 8-bit states of weights with strides {state['strides']}, got {p.stride()}")
 
     @staticmethod
     def _not_captured(what):
@@ -424,10 +446,11 @@ class AdamW(torch.optim.Optimizer):
     def _list(self, key, params, starts):
         """The ParamList of some weights and their states, made again when any of them has moved."""
         at = self._lists.get(key)
-        if at is None or any(p.data_ptr() != where or self.state[p] is not s or s["m"] is not m or s["v"] is not v
-                             for p, (where, s, m, v) in zip(params, at[0])):
+        if at is None or any(p.data_ptr() != where or p.stride() != strides or self.state[p] is not s or
+                             s["m"] is not m or s["v"] is not v
+                             for p, (where, strides, s, m, v) in zip(params, at[0])):
             states = [self._state(p) for p in params]
-            held = [(p.data_ptr(), s, s["m"], s["v"]) for p, s in zip(params, states)]
+            held = [(p.data_ptr(), p.stride(), s, s["m"], s["v"]) for p, s in zip(params, states)]
             flat = {k: [_flat(s[k]) for s in states] for k in ("m", "v")}
             for k in ("m_scale", "v_scale"):
                 flat[k] = [s[k] for s in states] if self.states == "e4m3" else None
@@ -452,8 +475,10 @@ class AdamW(torch.optim.Optimizer):
                 n, g = p.numel(), p.grad
                 if g is not None and n:
                     g = self._gradient(p, g, device)
-                    state = None if self.capturable else self.state.get(p)   # (none is made before all are checked)
-                    key = i, state["step"] if state else 0
+                    state = self.state.get(p)                # (none is made before all are checked)
+                    if state:
+                        self._check_state(p, state)
+                    key = i, state["step"] if state and not self.capturable else 0
                     if key not in todo:
                         todo[key] = cfg, [], [], []
                     _, params, grads, starts = todo[key]

@@ -192,6 +192,79 @@ def test_adamw_checkpoint(states):
         b.AdamW(weights(), states="f32" if states == "e4m3" else "e4m3").load_state_dict(oa.state_dict())
 
 
+def test_adamw_states_follow_their_weights():
+    """Weights whose memory order changes between steps, by a conversion, a view or a checkpoint of another model."""
+    b = blocks()
+    values = [gen(16, 8, 3, 3, seed=1), gen(20, 20, seed=2), gen(6, 5, 1, 1, seed=3)]
+    mine = [torch.nn.Parameter(v.clone()) for v in values]
+    theirs = [torch.nn.Parameter(v.double()) for v in values]
+    kw = dict(lr=0.01, betas=(0.8, 0.95), weight_decay=0.1)
+    opt, ref = b.AdamW(mine, **kw), torch.optim.AdamW(theirs, **kw)
+
+    def steps(opt, weights, seed):
+        for s in range(2):
+            for i, (p, q) in enumerate(zip(weights, theirs)):
+                g = gen(*p.shape, seed=seed + 10 * s + i)
+                p.grad, q.grad = g, g.double()
+            opt.step()
+            ref.step()
+        for p, q in zip(weights, theirs):                  # (the formula's float32 roundings, a few of 2^-24 a step)
+            assert (p.double() - q).abs().max() <= 4e-6 * max(1, q.abs().max().item())
+    steps(opt, mine, 100)
+    mine[0].data = mine[0].data.to(memory_format=torch.channels_last)
+    mine[2].data = mine[2].data.to(memory_format=torch.channels_last)
+    steps(opt, mine, 200)
+    assert opt.state[mine[0]]["m"].stride() == mine[0].stride()
+    for p in (mine[1], theirs[1]):
+        p.data = p.data.t()                                # at the same address
+    steps(opt, mine, 300)
+    other = [torch.nn.Parameter(p.detach().clone(memory_format=torch.contiguous_format)) for p in mine]
+    again = b.AdamW(other, **kw)
+    again.load_state_dict(copy.deepcopy(opt.state_dict()))
+    steps(again, other, 400)
+    # states of other shapes
+    wrong = [torch.nn.Parameter(p.detach().flatten()) for p in mine]
+    refused = b.AdamW(wrong, **kw)
+    refused.load_state_dict(copy.deepcopy(opt.state_dict()))
+    for p in wrong:
+        p.grad = torch.ones_like(p)
+    before = [p.detach().clone() for p in wrong]
+    with pytest.raises(ValueError, match="states of shapes"):
+        refused.step()
+    assert all(torch.equal(p, q) for p, q in zip(wrong, before))
+
+
+def test_adamw_8_bit_states_of_another_memory_order():
+    b = blocks()
+    conv, point, rest = (torch.nn.Parameter(gen(*n, seed=i)) for i, n in enumerate([(16, 8, 3, 3), (6, 5, 1, 1), (9,)]))
+    opt = b.AdamW([rest, point, conv], states="e4m3")
+
+    def step():
+        for p in (conv, point, rest):
+            p.grad = torch.ones_like(p)
+        opt.step()
+    step()
+    point.data = point.data.to(memory_format=torch.channels_last)      # the same memory order
+    step()
+    contiguous = conv.data
+    conv.data = conv.data.to(memory_format=torch.channels_last)
+    before = [p.detach().clone() for p in (conv, point, rest)]
+    with pytest.raises(ValueError, match="8-bit states of weights with strides"):
+        step()
+    assert all(torch.equal(p, q) for p, q in zip((conv, point, rest), before))
+    assert {s["step"] for s in opt.state.values()} == {2}
+    conv.data = contiguous
+    step()
+    other = [torch.nn.Parameter(p.detach().clone()) for p in (rest, point, conv)]
+    again = b.AdamW(other, states="e4m3")
+    again.load_state_dict(copy.deepcopy(opt.state_dict()))
+    for p, q in zip(other, (rest, point, conv)):
+        p.grad = q.grad = torch.ones_like(p)
+    again.step()
+    opt.step()
+    assert all(torch.equal(p, q) for p, q in zip(other, (rest, point, conv)))
+
+
 def test_adamw_copies_and_gradients_of_some():
     """A deep copy goes on like its original; weights with and without gradients change from step to step; gradients
     are not held after a step."""
