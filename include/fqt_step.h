@@ -55,7 +55,9 @@ int fqt_loss_forward(const fqt_loss_desc *desc, const void *x, const void *w, co
  * the gradient of the forward's mean; mean as the forward left it): one of the two is given, the other
  * is NULL.  dz is 0 in rows that are left out, whatever z is there; but x has to be finite there too for dw
  * (0 times infinity).  dx, dw, dbias are optional, each given one is computed.  The matrix cores take dz
- * (times w_scale or x_scale) rounded once to bf16, and sum in float32; dbias sums it unrounded. */
+ * (times w_scale or x_scale) rounded once to bf16, and sum in float32; dbias sums it unrounded.
+ * At a target whose probability is over 1/2 dz is c (expm1(log p) + smoothing - smoothing / N), with log p = z - lse from a z
+ * summed in float64: p - 1 keeps its precision relative to itself for the lse that is given. */
 int fqt_loss_backward(const fqt_loss_desc *desc, const void *x, const void *w, const float *x_scale,
                       const float *w_scale, const float *bias, const int64_t *target,
                       const float *lse, const float *dloss, const float *dmean, const float *mean,

@@ -450,13 +450,86 @@ __global__ void __launch_bounds__(1024) k_loss_mean(const float *loss, const int
   mean_of(mean, sum, count);
 }
 
+// ----------------------------------------------------------------------------- log p of the targets
+// dz at a target that is nearly certain is p - 1: a float32 z is off by 2^-24 |z| a rounding, which is then left alone
+// (10 classes, losses of 1e-5: wrong in the second digit).  So z of the targets, M of the M x N, is summed in float64, a wave a
+// row, and its difference from lse rounded once.  Bound by reading x again and M rows of w: 4608 x 65536 x 4096 bf16 in 17 us
+// of 5850, 777 x 10007 x 513 e4m3 in 4.6 (its launch) of 78; beside the tiles of a split contraction it costs nothing.
+
+struct Targets {
+  const void *x, *w;
+  const float *sx, *sw, *bias, *lse;
+  const int64_t *target;
+  int64_t M, N, K, ldx, ldw, ignore;
+  float *logp;             // [M]
+  int32_t dtype;
+};
+// The sum of the products that a lane has of two rows: of pieces of 16 bytes, and the elements behind them.  Exact for int8 (K
+// <= 133144), float64 for the others, whose products float32 holds exactly.
+template <int DTYPE>
+__device__ __forceinline__ double dot_rows(const void *xp, const void *wp, int64_t K) {
+  typedef std::conditional_t<DTYPE == FQT_BF16, uint16_t, uint8_t> Bits;
+  constexpr int V = 16 / sizeof(Bits);
+  const Bits *x = static_cast<const Bits *>(xp), *w = static_cast<const Bits *>(wp);
+  std::conditional_t<DTYPE == FQT_I8, int, double> sum = 0;
+  auto add = [&](uint32_t a, uint32_t b) {               // the elements of a word of each
+    if constexpr (DTYPE == FQT_BF16) {
+      sum += double(__uint_as_float(a << 16) * __uint_as_float(b << 16));
+      sum += double(__uint_as_float(a & 0xFFFF0000u) * __uint_as_float(b & 0xFFFF0000u));
+    } else if constexpr (DTYPE == FQT_I8) {
+#pragma unroll
+      for (int i = 0; i < 4; ++i) sum += int(int8_t(a >> (8 * i))) * int(int8_t(b >> (8 * i)));
+    } else {
+      sum += double(__builtin_amdgcn_cvt_f32_fp8(int(a), 0) * __builtin_amdgcn_cvt_f32_fp8(int(b), 0));
+      sum += double(__builtin_amdgcn_cvt_f32_fp8(int(a), 1) * __builtin_amdgcn_cvt_f32_fp8(int(b), 1));
+      sum += double(__builtin_amdgcn_cvt_f32_fp8(int(a), 2) * __builtin_amdgcn_cvt_f32_fp8(int(b), 2));
+      sum += double(__builtin_amdgcn_cvt_f32_fp8(int(a), 3) * __builtin_amdgcn_cvt_f32_fp8(int(b), 3));
+    }
+  };
+  const int64_t pieces = K / V;
+#pragma unroll 4
+  for (int64_t i = __lane_id(); i < pieces; i += 64) {
+    const u32x4 a = load_bytes16(x + i * V), b = load_bytes16(w + i * V);
+#pragma unroll
+    for (int j = 0; j < 4; ++j) add(a[j], b[j]);
+  }
+  if (const int64_t k = pieces * V + __lane_id(); k < K) add(x[k], w[k]);      // (zeros above)
+  return double(sum);
+}
+// The rows of wave `wave` of `waves`.
+__device__ __forceinline__ void target_rows(const Targets &a, int64_t wave, int64_t waves) {
+  const int64_t e = a.dtype == FQT_BF16 ? 2 : 1;
+  for (int64_t m = wave; m < a.M; m += waves) {
+    const int64_t t = a.target[m];
+    double z = 0.0;
+    const bool counts = t != a.ignore && t >= 0 && t < a.N;
+    if (counts) {
+      const void *x = static_cast<const char *>(a.x) + m * a.ldx * e, *w = static_cast<const char *>(a.w) + t * a.ldw * e;
+      if (a.dtype == FQT_BF16) z = dot_rows<FQT_BF16>(x, w, a.K);
+      else if (a.dtype == FQT_I8) z = dot_rows<FQT_I8>(x, w, a.K);
+      else z = dot_rows<FQT_E4M3>(x, w, a.K);
+#pragma unroll
+      for (int o = 32; o > 0; o /= 2) z += __shfl_xor(z, o);
+      if (a.sx) z *= double(a.sx[m]) * double(a.sw[t]);
+      if (a.bias) z += double(a.bias[t]);
+      z -= double(a.lse[m]);
+    }
+    if (__lane_id() == 0) a.logp[m] = float(z);
+  }
+}
+__global__ void __launch_bounds__(256) k_loss_targets(Targets a) {
+  target_rows(a, int64_t(blockIdx.x) * 4 + wave_id(), int64_t(gridDim.x) * 4);
+}
+
 // ----------------------------------------------------------------------------- dz
 
+constexpr float LIKELY = -LN2;     // log p of a target from which on dz comes from expm1
 struct DzOut {
-  const float *lse, *dloss, *dmean, *mean;
+  const float *lse, *logp, *dloss, *dmean, *mean;
   const int64_t *target;
   int64_t ignore, classes, first;  // all classes; the piece's first
   float keep, even;                // 1 - smoothing, smoothing / classes
+  float rise;                      // smoothing - smoothing / classes
   bf16 *dzx, *dzw;                 // dz sw and dz sx, rows of `pitch` (one array for bf16 operands); or null
   int64_t pitch;
   float *part;                     // [ceil(M / unit)][N] partial column sums, or null
@@ -467,7 +540,7 @@ struct StoreDz {
   static constexpr int DEPTH = 4;
   static constexpr bool MIRROR = false, SUMS = false;
   struct Fetch {
-    float lse, c, sx;
+    float lse, logp, c, sx;
     int32_t t;             // the target's place from n on; -1: not there, -2: the row is left out
   };
   const Logits &p;
@@ -491,6 +564,7 @@ struct StoreDz {
     if (m >= p.M || cnt == 0) return f;
     const int64_t t = o.target[m];
     f.lse = o.lse[m];
+    f.logp = o.logp[m];
     f.c = o.dloss ? o.dloss[m] : each;
     f.sx = p.sx ? p.sx[m] : 1.0f;
     const int64_t d = t - o.first - n;
@@ -518,8 +592,11 @@ struct StoreDz {
       for (int i = 0; i < 8; ++i) v[i] -= o.even;
     }
     if (f.t >= 0) {
+      // p - 1 of a likely target without cancellation (an unlikely one's p counts where labels are smoothed)
+      const bool likely = f.logp > LIKELY;
+      const float own = expm1f(f.logp) + o.rise;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) v[i] -= f.t == i ? o.keep : 0.0f;
+      for (int i = 0; i < 8; ++i) v[i] = f.t != i ? v[i] : likely ? own : v[i] - o.keep;
     }
 #pragma unroll
     for (int i = 0; i < 8; ++i) v[i] *= f.c;
@@ -553,10 +630,16 @@ struct StoreDz {
   }
 };
 // dz of a piece of the classes; its row pitch is a multiple of 8, zeros past the piece.
+// With a split contraction, whose join makes dz, the workgroups behind the `tiles` that compute z take the targets.
 template <int KIND, int SHAPE>
-__global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_loss_dz(Logits p, DzOut o) {
+__global__ void __launch_bounds__(tile::ShapeOf<SHAPE>::type::THREADS, 2) k_loss_dz(Logits p, DzOut o, Targets a, uint32_t tiles) {
   typedef typename tile::ShapeOf<SHAPE>::type S;
   __shared__ __attribute__((aligned(16))) char lds[S::LDS];
+  if (blockIdx.x >= tiles) {
+    constexpr int WAVES = S::THREADS / 64;
+    target_rows(a, int64_t(blockIdx.x - tiles) * WAVES + wave_id(), int64_t(gridDim.x - tiles) * WAVES);
+    return;
+  }
   const tile::Place at = tile::place<SHAPE>(p.tiles, blockIdx.x);
   if (at.m0 >= p.M || at.n0 >= p.N) return;              // (parts of an edge tile)
   typename tile::Acc<KIND>::type acc[S::FM][S::FN];
@@ -720,7 +803,7 @@ int64_t dz_pitch_of(int64_t n) { return n <= 512 ? round_up(n, 8) : (round_up(n,
 // the partial sums of dbias and those of the products.
 struct PiecePlan { tile::Plan z, dx, dw; int64_t unit; Together together; };
 struct BwdWs {
-  size_t dzx, dzw, x, w, dx, bias, part, total;
+  size_t dzx, dzw, x, w, dx, logp, bias, part, total;
   int64_t piece, dz_pitch, pitch, K;
   bool copy_x, copy_w, direct, sum_dx;
   PiecePlan plan[2];       // of the pieces, of the last one
@@ -755,7 +838,8 @@ BwdWs bwd_ws(const fqt_loss_desc &d, const Sizes &s) {
   f.x = f.dzw + dz;
   f.w = f.x + (f.copy_x ? align256(size_t(s.M) * f.pitch * 2) : 0);
   f.dx = f.w + (f.copy_w ? align256(size_t(f.piece) * f.pitch * 2) : 0);
-  f.bias = f.dx + (f.sum_dx ? align256(size_t(s.M) * s.K * 4) : 0);
+  f.logp = f.dx + (f.sum_dx ? align256(size_t(s.M) * s.K * 4) : 0);
+  f.bias = f.logp + align256(size_t(s.M) * 4);
   size_t part = 0, groups = 1;
   for (int i = 0; i < 2; ++i) {
     const int64_t n = i && s.N % f.piece ? s.N % f.piece : f.piece;
@@ -780,11 +864,18 @@ int launch_logits(const tile::Plan &plan, Logits p, const Pairs &o, hipStream_t 
   });
   return last_launch_status();
 }
+// Workgroups of `waves` waves for the targets of M rows; they walk where the rows are more.
+uint32_t target_blocks(int64_t M, int64_t waves) { return uint32_t(std::min<int64_t>((M + waves - 1) / waves, 1 << 14)); }
+// a: null where o.logp is there already.
 template <int KIND>
-int launch_dz(const PiecePlan &plan, Logits p, const DzOut &o, hipStream_t st) {
+int launch_dz(const PiecePlan &plan, Logits p, const DzOut &o, const Targets *a, hipStream_t st) {
+  const bool beside = a && plan.z.splits > 1;
+  if (a && !beside) k_loss_targets<<<dim3(target_blocks(a->M, 4)), dim3(256), 0, st>>>(*a);
   tile::for_launches(plan.z, [&]<int SHAPE>(const tile::Tiles &t) {
     p.tiles = t;
-    k_loss_dz<KIND, SHAPE><<<dim3(uint32_t(tile::blocks_of(t))), dim3(tile::ShapeOf<SHAPE>::type::THREADS), 0, st>>>(p, o);
+    constexpr int THREADS = tile::ShapeOf<SHAPE>::type::THREADS;
+    const uint32_t tiles = uint32_t(tile::blocks_of(t)), more = beside ? target_blocks(a->M, THREADS / 64) : 0;
+    k_loss_dz<KIND, SHAPE><<<dim3(tiles + more), dim3(THREADS), 0, st>>>(p, o, a ? *a : Targets{}, tiles);
   });
   if (plan.z.splits > 1) {
     const uint32_t groups = uint32_t((p.M + plan.unit - 1) / plan.unit);
@@ -928,14 +1019,18 @@ extern "C" int fqt_loss_backward(const fqt_loss_desc *d, const void *x, const vo
     const Operand xz{static_cast<const char *>(x), s.ldx, s.M}, wz{static_cast<const char *>(w) + first * s.ldw, s.ldw, n};
     Logits p{f.direct ? xz : xr, f.direct ? wz : wr, s.M, n, f.K, {}, x_scale, w_scale ? w_scale + first : nullptr, bias ? bias + first : nullptr,
              reinterpret_cast<float *>(base + f.part), round_up(n, 8)};
-    DzOut o{lse, dloss, dmean, mean, target, d->ignore, s.N, first, 1.0f - d->smoothing, d->smoothing / float(s.N),
+    const Targets targets{x, w, x_scale, w_scale, bias, lse, target, s.M, s.N, s.K, s.ldx, s.ldw, d->ignore,
+                          reinterpret_cast<float *>(base + f.logp), d->x_dtype};
+    const Targets *const a = first ? nullptr : &targets;
+    DzOut o{lse, targets.logp, dloss, dmean, mean, target, d->ignore, s.N, first, 1.0f - d->smoothing,
+            d->smoothing / float(s.N), d->smoothing - d->smoothing / float(s.N),
             reinterpret_cast<bf16 *>(base + f.dzx), reinterpret_cast<bf16 *>(base + f.dzw), dz_pitch,
             dbias ? reinterpret_cast<float *>(base + f.bias) : nullptr, int32_t(plan.unit)};
     if (!dx && (s.codes || !dw)) o.dzx = nullptr;
     if (!dw) o.dzw = nullptr;
-    if (f.direct && d->x_dtype == FQT_I8) FQT_TRY_(launch_dz<tile::I8K>(plan, p, o, st));
-    else if (f.direct) FQT_TRY_(launch_dz<tile::WIDEK>(plan, p, o, st));
-    else FQT_TRY_(launch_dz<tile::BF16K>(plan, p, o, st));
+    if (f.direct && d->x_dtype == FQT_I8) FQT_TRY_(launch_dz<tile::I8K>(plan, p, o, a, st));
+    else if (f.direct) FQT_TRY_(launch_dz<tile::WIDEK>(plan, p, o, a, st));
+    else FQT_TRY_(launch_dz<tile::BF16K>(plan, p, o, a, st));
     Gradients g{};
     g.M = s.M; g.N = n; g.K = s.K;
     g.dzx = {base + f.dzx, dz_pitch * 2, s.M};

@@ -1,0 +1,119 @@
+"""Gradients of rows whose target is nearly certain: dz at the target, p - 1, relative to itself.
+
+Tolerances, with u = 2^-24 and the formulas of the other tests of the loss.  At the target p - 1 = expm1(log p), and log p
+is z - lse with z in float64: its rounding to float32 u, expm1 2 u relative to its result, which for log p > -log 2 is at most 1.4 times as
+sensitive, its factor and the product u each: 8 u of dz.  A target below 1/2 and the other classes as anywhere: p by 600 u and z's
+error, then 4 u of |lse| p and 4 u of the terms.  Sums over M rows M u of the sum of magnitudes.
+"""
+import math
+
+import pytest
+
+torch = pytest.importorskip("torch")
+pytestmark = pytest.mark.gpu
+
+U = 2.0 ** -24
+HALF = 2.0 ** -8
+IGNORE = -100
+
+
+def step():
+    from paper_2408_14267_amd import step as s
+    return s
+
+
+def quantized(x, w, kind):
+    """The operands, their scales and their float64 values."""
+    if kind == "bf16":
+        x, w = x.bfloat16(), w.bfloat16()
+        return x, w, None, None, x.double(), w.double()
+    top, dt = (127.0, torch.int8) if kind == "int8" else (448.0, torch.float8_e4m3fn)
+    sx, sw = (t.abs().amax(dim=1).clamp_min(1e-20) / top for t in (x, w))
+    x, w = x / sx[:, None], w / sw[:, None]
+    x, w = (t.round() if kind == "int8" else t for t in (x, w))
+    x, w = x.to(dt), w.to(dt)
+    return x, w, sx, sw, x.float().double() * sx.double()[:, None], w.float().double() * sw.double()[:, None]
+
+
+def make(M, N, K, kind, seed, low=6.0, high=30.0):
+    """Rows that point at their target's weights by different lengths."""
+    g = torch.Generator(device="cuda").manual_seed(seed * 104729 + 31 * M + 7 * N + K)
+
+    def normal(*shape):
+        return torch.randn(shape, generator=g, device="cuda")
+
+    w = normal(N, K)
+    w /= w.norm(dim=1, keepdim=True)
+    t = torch.randint(0, N, (M,), generator=g, device="cuda")
+    size = low + (high - low) * torch.rand(M, generator=g, device="cuda")
+    x = 0.3 * normal(M, K) + size[:, None] * w[t]
+    o = dict(zip(("x", "w", "x_scale", "w_scale", "x64", "w64"), quantized(x, w, kind)))
+    o["bias"] = 0.3 * normal(N)
+    o["target"] = torch.where(torch.rand(M, generator=g, device="cuda") < 0.3, IGNORE, t) if M > 1 else t
+    return o
+
+
+def logits(o):
+    z = o["x64"] @ o["w64"].t().contiguous() + o["bias"].double()
+    mag = o["x64"].abs() @ o["w64"].abs().t().contiguous() + o["bias"].double().abs()
+    return z, ((o["x"].shape[1] + 8) * U * mag).amax(dim=1)
+
+
+def check(got, o, z, zerr, lse, c, smoothing, own=0.0):
+    """dbias, dx and dw (float32) against the formulas with this lse (float64).  own: what dz at a likely target may be
+    off by beside 8 u, relative to itself."""
+    M, N = z.shape
+    t = o["target"].clamp(min=0)[:, None]
+    c = torch.where(o["target"] == IGNORE, 0.0, c.double())
+    logp = z - lse[:, None]
+    p = torch.exp(logp)
+    q = torch.full_like(z, smoothing / N).scatter_add_(1, t, torch.full_like(z[:, :1], 1 - smoothing))
+    dz = p - q
+    at = logp.gather(1, t)
+    likely = at > -math.log(2.0)
+    dz.scatter_(1, t, torch.where(likely, torch.expm1(at) + (smoothing - smoothing / N), dz.gather(1, t)))
+    lim = p * (600 * U + 2 * zerr[:, None] + 4 * U * lse.abs()[:, None]) + 4 * U * (p + q)
+    off = (8 * U + own) * torch.expm1(at).abs() + 8 * U * smoothing
+    lim.scatter_(1, t, torch.where(likely, off, lim.gather(1, t)))
+    dz, lim = dz * c[:, None], lim * c.abs()[:, None] + M * U * (dz * c[:, None]).abs()
+    d16 = lim + HALF * (dz.abs() + lim)
+    x, w = o["x64"], o["w64"]
+    sums = {"dbias": (dz.sum(dim=0), lim.sum(dim=0)),
+            "dx": (dz @ w, d16 @ w.abs() + N * U * (dz.abs() @ w.abs())),
+            "dw": (dz.t().contiguous() @ x, d16.t().contiguous() @ x.abs() + M * U * (dz.abs().t().contiguous() @ x.abs()))}
+    for k, v in got.items():
+        want, bound = sums[k]
+        bound = bound + 2 * U * want.abs() + 1e-37
+        err = (v.double() - want).abs()
+        assert torch.isfinite(v).all() and (err <= bound).all(), f"{k}: off by {(err / bound).max().item():.3g} of the bound"
+
+
+def gradients(o, kind, lse, c, smoothing, **kw):
+    s = step()
+    (M, K), N = o["x"].shape, o["w"].shape[0]
+    desc = s.loss_desc(M, N, K, x_dtype=kind, dx_dtype="f32", dw_dtype="f32", smoothing=smoothing, ignore=IGNORE)
+    out = {"dx": torch.empty(M, K, device="cuda"), "dw": torch.empty(N, K, device="cuda"),
+           "dbias": torch.empty(N, device="cuda")}
+    s.fqt_loss_backward(desc, o["x"], o["w"], o["target"], lse, s.loss_workspace(desc, True), dloss=c, bias=o["bias"],
+                        x_scale=o["x_scale"], w_scale=o["w_scale"], **out, **kw)
+    return out
+
+
+# (1 to 64 rows of 2048 and 4096 features: a split contraction; odd features: copied operands; 9000 x 20011: pieces)
+SIZES = [(1, 2, 8), (1, 10, 64), (1, 10, 594), (3, 10, 4096), (10, 10, 512), (5, 7, 3), (1, 1000, 4096), (16, 1000, 2048),
+         (64, 1000, 4096), (65, 129, 300), (130, 10007, 140), (300, 700, 128), (777, 1000, 513), (2304, 4864, 64),
+         (5000, 10, 32), (4608, 12288, 1024), (9000, 20011, 72)]
+
+
+@pytest.mark.parametrize("M,N,K", SIZES)
+@pytest.mark.parametrize("kind", ["bf16", "int8", "e4m3"])
+@pytest.mark.parametrize("smoothing", [0.0, 0.1])
+def test_gradients_for_an_lse(M, N, K, kind, smoothing):
+    """The definition, exp(z - lse), with the float32 lse that is given."""
+    if smoothing and M * N > 10 ** 7:
+        pytest.skip("sizes of the unsmoothed case")
+    o = make(M, N, K, kind, seed=1)
+    z, zerr = logits(o)
+    lse = torch.logsumexp(z, dim=1).float()
+    c = torch.randn(M, generator=torch.Generator(device="cuda").manual_seed(M), device="cuda")
+    check(gradients(o, kind, lse, c, smoothing), o, z, zerr, lse.double(), c, smoothing)
