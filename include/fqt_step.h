@@ -57,12 +57,25 @@ int fqt_loss_forward(const fqt_loss_desc *desc, const void *x, const void *w, co
  * (0 times infinity).  dx, dw, dbias are optional, each given one is computed.  The matrix cores take dz
  * (times w_scale or x_scale) rounded once to bf16, and sum in float32; dbias sums it unrounded.
  * At a target whose probability is over 1/2 dz is c (expm1(log p) + smoothing - smoothing / N), with log p = z - lse from a z
- * summed in float64: p - 1 keeps its precision relative to itself for the lse that is given. */
+ * summed in float64: p - 1 keeps its precision relative to itself for the lse that is given.  But an lse in float32 is
+ * itself off by 2^-25 of its size, which is more than p - 1 of a well fitted row: the functions below pass log p on. */
 int fqt_loss_backward(const fqt_loss_desc *desc, const void *x, const void *w, const float *x_scale,
                       const float *w_scale, const float *bias, const int64_t *target,
                       const float *lse, const float *dloss, const float *dmean, const float *mean,
                       void *dx, void *dw, float *dbias, void *ws, size_t ws_bytes,
                       void *hip_stream);
+
+/* The same with log p of the targets, float32 [M], which the forward leaves (0 in rows that are left out, NaN where the
+ * target is no class) and the backward takes instead of computing it: gradients of rows whose loss is small then
+ * keep the relative precision that the loss has.  logp NULL: as the functions above. */
+int fqt_loss_forward_logp(const fqt_loss_desc *desc, const void *x, const void *w, const float *x_scale,
+                          const float *w_scale, const float *bias, const int64_t *target, float *loss,
+                          float *lse, float *logp, float *mean, void *ws, size_t ws_bytes, void *hip_stream);
+int fqt_loss_backward_logp(const fqt_loss_desc *desc, const void *x, const void *w, const float *x_scale,
+                           const float *w_scale, const float *bias, const int64_t *target,
+                           const float *lse, const float *logp, const float *dloss, const float *dmean,
+                           const float *mean, void *dx, void *dw, float *dbias, void *ws, size_t ws_bytes,
+                           void *hip_stream);
 
 /* ------------------------------------------------------------------ lists of tensors
  * One tensor of a list, n contiguous elements.  Lists are read by the host during the call: they may

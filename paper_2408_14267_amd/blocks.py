@@ -148,18 +148,18 @@ class _LossFn(torch.autograd.Function):
         wq, w_scale = _quantized(w, mod.operands)
         desc = step.loss_desc(M, N, K, x_dtype=mod.operands, dx_dtype=x.dtype, dw_dtype=_F32, smoothing=smoothing,
                               ignore=ignore)
-        loss, lse = torch.empty(M, device=x.device), torch.empty(M, device=x.device)
+        loss, lse, logp = (torch.empty(M, device=x.device) for _ in range(3))
         average = torch.empty(2, device=x.device) if mean else None
         step.fqt_loss_forward(desc, xq, wq, target, loss, lse, _workspace(step.fqt_loss_workspace_size(desc), x.device),
-                              bias=bias, x_scale=x_scale, w_scale=w_scale, mean=average)
-        ctx.save_for_backward(xq, x_scale, wq, w_scale, bias, target, lse, average)
+                              bias=bias, x_scale=x_scale, w_scale=w_scale, mean=average, logp=logp)
+        ctx.save_for_backward(xq, x_scale, wq, w_scale, bias, target, lse, logp, average)
         ctx.desc = desc
         return average[0].clone() if mean else loss
 
     @staticmethod
     @once_differentiable
     def backward(ctx, d):
-        xq, x_scale, wq, w_scale, bias, target, lse, average = ctx.saved_tensors
+        xq, x_scale, wq, w_scale, bias, target, lse, logp, average = ctx.saved_tensors
         desc, (need_x, need_w, need_bias) = ctx.desc, ctx.needs_input_grad[:3]
         dx = torch.empty(desc.M, desc.K, dtype=dense._TORCH_OF[desc.dx_dtype], device=d.device) if need_x else None
         dw = torch.empty(desc.N, desc.K, device=d.device) if need_w else None
@@ -167,7 +167,7 @@ class _LossFn(torch.autograd.Function):
         given = dict(dloss=d.contiguous()) if average is None else dict(dmean=d.reshape(1), mean=average)
         ws = _workspace(step.fqt_loss_workspace_size(desc, True), d.device)
         step.fqt_loss_backward(desc, xq, wq, target, lse, ws, bias=bias, x_scale=x_scale, w_scale=w_scale, dx=dx, dw=dw,
-                               dbias=db, **given)
+                               dbias=db, logp=logp, **given)
         return dx, dw, db, None, None, None, None, None
 
 

@@ -64,6 +64,7 @@ struct Out {
   int64_t M, N, ignore;
   float smoothing;
   float *mean;             // for a launch of one workgroup that has all rows, or null
+  float *logp;             // log p of the targets, or null
 };
 // Row m from its pair, the sum of its y and the target's y.
 // Returns its loss, and in `counts` whether it counts.
@@ -71,12 +72,15 @@ __device__ __forceinline__ float finish_row(const Out &o, int64_t m, Soft s, flo
   const float rest = log1pf(s.rest);
   o.lse[m] = fmaf(s.top, LN2, rest);
   const int64_t t = o.target[m];
-  float loss = s.top - at;
+  const float gap = s.top - at;
+  float loss = gap;
   if (o.smoothing > 0.0f) loss = (1.0f - o.smoothing) * loss + o.smoothing * (s.top - sum / float(o.N));
   loss = fmaf(loss, LN2, rest);
   counts = t != o.ignore;
-  loss = !counts ? 0.0f : t < 0 || t >= o.N ? __builtin_nanf("") : loss;
+  auto valid = [&](float v) { return !counts ? 0.0f : t < 0 || t >= o.N ? __builtin_nanf("") : v; };
+  loss = valid(loss);
   o.loss[m] = loss;
+  if (o.logp) o.logp[m] = valid(-fmaf(gap, LN2, rest));
   return loss;
 }
 // mean[0]: of the losses of the rows that count, mean[1]: 1 / their number.
@@ -452,7 +456,7 @@ __global__ void __launch_bounds__(1024) k_loss_mean(const float *loss, const int
 
 // ----------------------------------------------------------------------------- log p of the targets
 // dz at a target that is nearly certain is p - 1: a float32 z is off by 2^-24 |z| a rounding, which is then left alone
-// (10 classes, losses of 1e-5: wrong in the second digit).  So z of the targets, M of the M x N, is summed in float64, a wave a
+// (10 classes, losses of 1e-5: wrong in the second digit).  The forward leaves log p; where it is not given, z of the targets, M of the M x N, is summed in float64, a wave a
 // row, and its difference from lse rounded once.  Bound by reading x again and M rows of w: 4608 x 65536 x 4096 bf16 in 17 us
 // of 5850, 777 x 10007 x 513 e4m3 in 4.6 (its launch) of 78; beside the tiles of a split contraction it costs nothing.
 
@@ -927,16 +931,24 @@ extern "C" int fqt_loss_workspace_size(const fqt_loss_desc *d, int32_t backward,
 extern "C" int fqt_loss_forward(const fqt_loss_desc *d, const void *x, const void *w, const float *x_scale,
                                 const float *w_scale, const float *bias, const int64_t *target, float *loss,
                                 float *lse, float *mean, void *ws, size_t ws_bytes, void *hip_stream) {
+  return fqt_loss_forward_logp(d, x, w, x_scale, w_scale, bias, target, loss, lse, nullptr, mean, ws, ws_bytes, hip_stream);
+}
+
+extern "C" int fqt_loss_forward_logp(const fqt_loss_desc *d, const void *x, const void *w, const float *x_scale,
+                                     const float *w_scale, const float *bias, const int64_t *target, float *loss,
+                                     float *lse, float *logp, float *mean, void *ws, size_t ws_bytes,
+                                     void *hip_stream) {
   Sizes s;
   FQT_TRY_(check_loss(d, &s));
   FQT_TRY_(check_pointers(*d, s, x, w, x_scale, w_scale, bias, target));
   if (!ws || (s.M && (!loss || !lse))) return FQT_E_NULL;
-  if (!aligned(loss, 4) || !aligned(lse, 4) || !aligned(mean, 4) || !aligned(ws, 256)) return FQT_E_ALIGN;
+  if (!aligned(loss, 4) || !aligned(lse, 4) || !aligned(logp, 4) || !aligned(mean, 4) || !aligned(ws, 256))
+    return FQT_E_ALIGN;
   const FwdWs f = fwd_ws(*d, s);
   if (ws_bytes < f.total) return FQT_E_WORKSPACE;
   const hipStream_t st = static_cast<hipStream_t>(hip_stream);
   char *base = static_cast<char *>(ws);
-  const Out o{target, loss, lse, s.M, s.N, d->ignore, d->smoothing, nullptr};
+  const Out o{target, loss, lse, s.M, s.N, d->ignore, d->smoothing, nullptr, logp};
   bool averaged = false;
   const Pairs pairs{reinterpret_cast<Soft *>(base + f.pairs),
                     d->smoothing > 0.0f ? reinterpret_cast<float *>(base + f.sums) : nullptr,
@@ -982,13 +994,22 @@ extern "C" int fqt_loss_backward(const fqt_loss_desc *d, const void *x, const vo
                                  const float *w_scale, const float *bias, const int64_t *target, const float *lse,
                                  const float *dloss, const float *dmean, const float *mean, void *dx, void *dw,
                                  float *dbias, void *ws, size_t ws_bytes, void *hip_stream) {
+  return fqt_loss_backward_logp(d, x, w, x_scale, w_scale, bias, target, lse, nullptr, dloss, dmean, mean, dx, dw,
+                                dbias, ws, ws_bytes, hip_stream);
+}
+
+extern "C" int fqt_loss_backward_logp(const fqt_loss_desc *d, const void *x, const void *w, const float *x_scale,
+                                      const float *w_scale, const float *bias, const int64_t *target,
+                                      const float *lse, const float *logp, const float *dloss, const float *dmean,
+                                      const float *mean, void *dx, void *dw, float *dbias, void *ws, size_t ws_bytes,
+                                      void *hip_stream) {
   Sizes s;
   FQT_TRY_(check_loss(d, &s));
   FQT_TRY_(check_pointers(*d, s, x, w, x_scale, w_scale, bias, target));
   if ((dloss && dmean) || (!dmean) != (!mean)) return FQT_E_INVAL;
   if (!dx && !dw && !dbias) return FQT_OK;
   if (!ws || (s.M && (!lse || (!dloss && !dmean)))) return FQT_E_NULL;
-  if (!aligned(lse, 4) || !aligned(dloss, 4) || !aligned(dmean, 4) || !aligned(mean, 4) ||
+  if (!aligned(lse, 4) || !aligned(logp, 4) || !aligned(dloss, 4) || !aligned(dmean, 4) || !aligned(mean, 4) ||
       !elem_aligned(dx, d->dx_dtype) || !elem_aligned(dw, d->dw_dtype) || !aligned(dbias, 4) || !aligned(ws, 256))
     return FQT_E_ALIGN;
   const BwdWs f = bwd_ws(*d, s);
@@ -1021,8 +1042,8 @@ extern "C" int fqt_loss_backward(const fqt_loss_desc *d, const void *x, const vo
              reinterpret_cast<float *>(base + f.part), round_up(n, 8)};
     const Targets targets{x, w, x_scale, w_scale, bias, lse, target, s.M, s.N, s.K, s.ldx, s.ldw, d->ignore,
                           reinterpret_cast<float *>(base + f.logp), d->x_dtype};
-    const Targets *const a = first ? nullptr : &targets;
-    DzOut o{lse, targets.logp, dloss, dmean, mean, target, d->ignore, s.N, first, 1.0f - d->smoothing,
+    const Targets *const a = first || logp ? nullptr : &targets;
+    DzOut o{lse, logp ? logp : targets.logp, dloss, dmean, mean, target, d->ignore, s.N, first, 1.0f - d->smoothing,
             d->smoothing / float(s.N), d->smoothing - d->smoothing / float(s.N),
             reinterpret_cast<bf16 *>(base + f.dzx), reinterpret_cast<bf16 *>(base + f.dzw), dz_pitch,
             dbias ? reinterpret_cast<float *>(base + f.bias) : nullptr, int32_t(plan.unit)};

@@ -19,8 +19,8 @@ from .dense import (_bytes, _check, _current, _device, _matrix, _required, _stre
 from .fqt import FQT_BF16, FQT_F32, FqtError  # noqa: F401
 
 FQT_STATE_BLOCK, FQT_MAX_PARAMS = 256, 65536
-EXPORTED = ("fqt_loss_workspace_size", "fqt_loss_forward", "fqt_loss_backward", "fqt_grad_norm_workspace_size",
-            "fqt_grad_norm", "fqt_adamw_step")
+EXPORTED = ("fqt_loss_workspace_size", "fqt_loss_forward", "fqt_loss_backward", "fqt_loss_forward_logp",
+            "fqt_loss_backward_logp", "fqt_grad_norm_workspace_size", "fqt_grad_norm", "fqt_adamw_step")
 
 
 class fqt_loss_desc(Structure):
@@ -46,6 +46,8 @@ def _bind(lib):
             "fqt_loss_workspace_size": [L, c_int32, size],
             "fqt_loss_forward": [L] + [p] * 10 + [c_size_t, p],
             "fqt_loss_backward": [L] + [p] * 14 + [c_size_t, p],
+            "fqt_loss_forward_logp": [L] + [p] * 11 + [c_size_t, p],
+            "fqt_loss_backward_logp": [L] + [p] * 15 + [c_size_t, p],
             "fqt_grad_norm_workspace_size": [T, c_int32, size],
             "fqt_grad_norm": [T, c_int32, c_float, p, p, c_size_t, p],
             "fqt_adamw_step": [A, T, c_int32, c_int64, p, p, p]}.items():
@@ -97,7 +99,9 @@ def _loss_inputs(where, desc, x, w, target, bias, x_scale, w_scale, dev):
         _vector(where, "w_scale", w_scale, N, dev)
 
 
-def fqt_loss_forward(desc, x, w, target, loss, lse, ws, bias=None, x_scale=None, w_scale=None, mean=None, stream=None):
+def fqt_loss_forward(desc, x, w, target, loss, lse, ws, bias=None, x_scale=None, w_scale=None, mean=None, stream=None,
+                     logp=None):
+    """logp: log p of the targets, for the backward (fqt_loss_forward_logp)."""
     where = "fqt_loss_forward"
     if x is None or w is None or target is None or loss is None or lse is None:
         _required(where, x=x, w=w, target=target, loss=loss, lse=lse)
@@ -107,15 +111,19 @@ def fqt_loss_forward(desc, x, w, target, loss, lse, ws, bias=None, x_scale=None,
     _vector(where, "lse", lse, desc.M, dev)
     if mean is not None:
         _vector(where, "mean", mean, 2, dev)
+    if logp is not None:
+        _vector(where, "logp", logp, desc.M, dev)
     if dev < 0 or dev != _device():
         _current(where, dev)
-    _check(_lib.fqt_loss_forward(
+    _check(_lib.fqt_loss_forward_logp(
         desc, x.data_ptr(), w.data_ptr(), _ptr(x_scale), _ptr(w_scale), _ptr(bias), target.data_ptr(),
-        loss.data_ptr(), lse.data_ptr(), _ptr(mean), *_workspace(where, ws, dev), _stream(stream, dev)), where)
+        loss.data_ptr(), lse.data_ptr(), _ptr(logp), _ptr(mean), *_workspace(where, ws, dev),
+        _stream(stream, dev)), where)
 
 
 def fqt_loss_backward(desc, x, w, target, lse, ws, dloss=None, dmean=None, mean=None, bias=None, x_scale=None,
-                      w_scale=None, dx=None, dw=None, dbias=None, stream=None):
+                      w_scale=None, dx=None, dw=None, dbias=None, stream=None, logp=None):
+    """logp: as the forward left it (fqt_loss_backward_logp)."""
     where = "fqt_loss_backward"
     if x is None or w is None or target is None or lse is None:
         _required(where, x=x, w=w, target=target, lse=lse)
@@ -125,6 +133,8 @@ def fqt_loss_backward(desc, x, w, target, lse, ws, dloss=None, dmean=None, mean=
     M, N, K = desc.M, desc.N, desc.K
     _loss_inputs(where, desc, x, w, target, bias, x_scale, w_scale, dev)
     _vector(where, "lse", lse, M, dev)
+    if logp is not None:
+        _vector(where, "logp", logp, M, dev)
     if dloss is not None:
         _vector(where, "dloss", dloss, M, dev)
     else:
@@ -138,9 +148,9 @@ def fqt_loss_backward(desc, x, w, target, lse, ws, dloss=None, dmean=None, mean=
         _vector(where, "dbias", dbias, N, dev)
     if dev < 0 or dev != _device():
         _current(where, dev)
-    _check(_lib.fqt_loss_backward(
+    _check(_lib.fqt_loss_backward_logp(
         desc, x.data_ptr(), w.data_ptr(), _ptr(x_scale), _ptr(w_scale), _ptr(bias), target.data_ptr(),
-        lse.data_ptr(), _ptr(dloss), _ptr(dmean), _ptr(mean), _ptr(dx), _ptr(dw), _ptr(dbias),
+        lse.data_ptr(), _ptr(logp), _ptr(dloss), _ptr(dmean), _ptr(mean), _ptr(dx), _ptr(dw), _ptr(dbias),
         *_workspace(where, ws, dev), _stream(stream, dev)), where)
 
 

@@ -117,3 +117,96 @@ def test_gradients_for_an_lse(M, N, K, kind, smoothing):
     lse = torch.logsumexp(z, dim=1).float()
     c = torch.randn(M, generator=torch.Generator(device="cuda").manual_seed(M), device="cuda")
     check(gradients(o, kind, lse, c, smoothing), o, z, zerr, lse.double(), c, smoothing)
+
+
+# ----------------------------------------------------------------------------- from the forward's own outputs
+
+def peaked(M, N, K, kind, seed):
+    """Rows of losses from 1e-1 to 1e-7 under top logits of 10 to 80, a few with another target than the largest; class n
+    reads feature n alone, so that z is known to the last bit but for the scales' roundings."""
+    assert K >= N
+    g = torch.Generator(device="cuda").manual_seed(seed + M + N)
+
+    def uniform(*shape):
+        return torch.rand(shape, generator=g, device="cuda")
+
+    top = torch.tensor([10.0, 20.0, 40.0, 80.0], device="cuda")[torch.randint(0, 4, (M,), generator=g, device="cuda")]
+    loss = 10.0 ** -(1 + 6 * uniform(M))
+    t = torch.randint(0, N, (M,), generator=g, device="cuda")
+    x = torch.zeros(M, K, device="cuda")
+    x[:, :N] = (top + torch.log(loss / max(N - 1, 1)))[:, None] + uniform(M, N) - 0.5
+    x.scatter_(1, t[:, None], top[:, None])
+    w = torch.zeros(N, K, device="cuda")
+    w[torch.arange(N), torch.arange(N)] = 1.0
+    o = dict(zip(("x", "w", "x_scale", "w_scale", "x64", "w64"), quantized(x, w, kind)))
+    o["bias"] = torch.randint(-2, 3, (N,), generator=g, device="cuda").float() / 8
+    if M > 4:
+        t = torch.where(uniform(M) < 0.1, (t + 1) % N, t)
+        t = torch.where(uniform(M) < 0.1, IGNORE, t)
+    o["target"] = t
+    return o
+
+
+PEAKED = [(1, 2, 8), (1, 10, 64), (3, 10, 4096), (4, 5000, 5000), (10, 10, 16), (20, 300, 333), (64, 1000, 4096), (300, 700, 768),
+          (513, 300, 320), (1500, 1000, 1024), (2304, 5000, 5120)]
+
+
+@pytest.mark.parametrize("M,N,K", PEAKED)
+@pytest.mark.parametrize("kind", ["bf16", "int8", "e4m3"])
+@pytest.mark.parametrize("smoothing", [0.0, 0.01])
+def test_gradients_from_the_forward(M, N, K, kind, smoothing):
+    """Forward, then backward: the gradients of the loss itself, relative to themselves where it is small.
+
+    log p = -((top - y) log 2 + log1p(rest)) is off by the exponents of rest: y and top by 2^-25 |y| each (|z| <= 81 here: 80 u of an
+    exponential), the scales' products another 3 u of |z| each, 2 u the instruction, 4 u each of at most 80 additions: 420 u and 6 u |z|, within
+    600 u and 8 u |z|."""
+    s = step()
+    o = peaked(M, N, K, kind, seed=1)
+    z, _ = logits(o)
+    desc = s.loss_desc(M, N, K, x_dtype=kind, smoothing=smoothing, ignore=IGNORE)
+    loss, lse, logp = (torch.full((M,), 7.0, device="cuda") for _ in range(3))
+    args = dict(bias=o["bias"], x_scale=o["x_scale"], w_scale=o["w_scale"])
+    s.fqt_loss_forward(desc, o["x"], o["w"], o["target"], loss, lse, s.loss_workspace(desc), logp=logp, **args)
+    again = [torch.empty(M, device="cuda") for _ in range(2)]
+    s.fqt_loss_forward(desc, o["x"], o["w"], o["target"], *again, s.loss_workspace(desc), **args)
+    assert torch.equal(again[0], loss) and torch.equal(again[1], lse)
+    big = z.abs().amax(dim=1)
+    zerr = 8 * U * big
+    own = 600 * U + 8 * U * big[:, None]
+    # log p itself, without the largest's own 1 in the sum
+    counted = o["target"] != IGNORE
+    t = o["target"].clamp(min=0)[:, None]
+    rest = torch.exp(z - z.amax(dim=1, keepdim=True)).scatter_(1, z.argmax(dim=1, keepdim=True), 0.0).sum(dim=1)
+    exact = (z.gather(1, t)[:, 0] - z.amax(dim=1)) - torch.log1p(rest)
+    assert (logp[~counted] == 0).all()
+    assert ((logp.double() - exact).abs() <= (own[:, 0] * torch.log1p(rest) + 12 * U * big * (exact < -0.5)))[counted].all()
+    if not smoothing:
+        assert torch.equal(logp[counted], -loss[counted])
+    c = torch.randn(M, generator=torch.Generator(device="cuda").manual_seed(M), device="cuda")
+    top = z.amax(dim=1, keepdim=True)
+    check(gradients(o, kind, lse, c, smoothing, logp=logp), o, z, zerr, (top[:, 0] + torch.log1p(rest)), c, smoothing, own)
+
+
+@pytest.mark.parametrize("kind", ["bf16", "int8", "e4m3"])
+@pytest.mark.parametrize("reduction", ["mean", "none"])
+def test_gradients_of_a_layer(kind, reduction):
+    """Linear.loss: the gradient of the bias over rows that are all nearly certain."""
+    from paper_2408_14267_amd import blocks
+    M, N, K = 40, 30, 64
+    o = peaked(M, N, K, "bf16", seed=2)
+    mod = blocks.Linear(K, N, operands=kind).cuda()
+    mod.weight.data.copy_(o["w"].float())
+    mod.bias.data.copy_(o["bias"])
+    x = o["x"].float()
+    q = dict(zip(("x", "w", "x_scale", "w_scale", "x64", "w64"), quantized(x, o["w"].float(), kind)), bias=o["bias"])
+    z, _ = logits(q)
+    target = z.argmax(dim=1)
+    mod.loss(x, target, reduction=reduction).sum().backward()
+    rest = torch.exp(z - z.amax(dim=1, keepdim=True)).scatter_(1, target[:, None], 0.0)
+    dz = torch.exp(z - z.amax(dim=1, keepdim=True) - torch.log1p(rest.sum(dim=1, keepdim=True)))
+    dz.scatter_(1, target[:, None], torch.expm1(-torch.log1p(rest.sum(dim=1, keepdim=True))))
+    if reduction == "mean":
+        dz = dz / M
+    # (every term by 1300 u and 16 u of |z| <= 81, and the sums)
+    bound = (2600 + M) * U * dz.abs().sum(dim=0)
+    assert ((mod.bias.grad.double() - dz.sum(dim=0)).abs() <= bound).all()

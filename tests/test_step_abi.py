@@ -135,6 +135,25 @@ def test_loss_binding_checks():
             step.fqt_loss_backward(d, x, w, t, f, ws, **bad)
 
 
+def test_loss_logp_checks():
+    d = _loss()
+    for off, status in ((2, fqt.FQT_E_ALIGN), (0, fqt.FQT_E_WORKSPACE)):
+        at = FAKE + off
+        assert step._lib.fqt_loss_forward_logp(d, FAKE, FAKE, None, None, None, FAKE, FAKE, FAKE, at, None, FAKE, 0,
+                                               None) == status
+        assert step._lib.fqt_loss_backward_logp(d, FAKE, FAKE, None, None, None, FAKE, FAKE, at, FAKE, None, None, FAKE,
+                                                FAKE, FAKE, FAKE, 0, None) == status
+    bf = torch.bfloat16
+    d = step.loss_desc(4, 8, 16)
+    x, w, t = torch.empty(4, 16, dtype=bf), torch.empty(8, 16, dtype=bf), torch.zeros(4, dtype=torch.int64)
+    f, ws = torch.empty(4), torch.empty(256, dtype=torch.uint8)
+    for bad in (f[:3], f.double(), torch.empty(8)[::2]):
+        with pytest.raises(ValueError, match="logp"):
+            step.fqt_loss_forward(d, x, w, t, f, f.clone(), ws, logp=bad)
+        with pytest.raises(ValueError, match="logp"):
+            step.fqt_loss_backward(d, x, w, t, f, ws, dloss=f, logp=bad)
+
+
 # ----------------------------------------------------------------------------- lists
 
 def _params(count=1, **kw):
