@@ -363,7 +363,8 @@ class AdamW(torch.optim.Optimizer):
     max_norm: the gradients are clipped to this norm over all groups; `grad_norm` holds the last step's norm
     and factor (on the device).  capturable: the step number is counted on the device (one for each group, weights without a
     gradient included), so that step() may be captured into a graph; the learning rate is then the captured one, and a
-    checkpoint is loaded before the capture.  States lie in memory as their weights do: those in float32 follow weights whose
+    checkpoint is loaded before the capture.  A checkpoint of either kind goes on in the other: the states' step number becomes
+    the group's counter (it has to be one number for the group's weights) or the other way.  States lie in memory as their weights do: those in float32 follow weights whose
     memory order has changed, 8-bit ones, whose blocks are of memory order, are refused then.
     What cannot be updated is refused when its group is added or before a step updates anything."""
 
@@ -432,6 +433,14 @@ class AdamW(torch.optim.Optimizer):
         if torch.cuda.is_current_stream_capturing():
             raise RuntimeError(f"AdamW: {what} in the first step: take one before a capture")
 
+    def _clock(self, group, device):
+        """The group's counter of steps on the device, made before the first one."""
+        if group.get("clock") is None:
+            self._not_captured("the step counter is made")
+            group["clock"] = torch.zeros(1, dtype=torch.int64, device=device)
+        if group["clock"].device != device:
+            raise ValueError(f"AdamW: a step counter on {group['clock'].device}, weights on {device}")
+
     def _gradient(self, p, g, device):
         """g, the gradient of p, its elements in p's memory order.  device: the current one."""
         if g.layout is not torch.strided or g.dtype not in (_F32, _BF16) or p.get_device() != device:
@@ -495,6 +504,8 @@ class AdamW(torch.optim.Optimizer):
             params_list = kept[key][1]
             params_list.set_gradients(g)
             lists.append((i, t, cfg, params, params_list))
+            if self.capturable:
+                self._clock(self.param_groups[i], params[0].device)
         self._lists = kept                   # (those of this step: other sets of weights with gradients go)
         scale = None
         if self.max_norm is not None:
@@ -506,11 +517,7 @@ class AdamW(torch.optim.Optimizer):
             scale = self.grad_norm[1:]
         for i, t, cfg, params, params_list in lists:
             if self.capturable:
-                group = self.param_groups[i]
-                if group.get("clock") is None:
-                    self._not_captured("the step counter is made")
-                    group["clock"] = torch.zeros(1, dtype=torch.int64, device=params[0].device)
-                number = group["clock"].add_(1)
+                number = self.param_groups[i]["clock"].add_(1)
             else:
                 number = t + 1
                 for p in params:
@@ -523,11 +530,32 @@ class AdamW(torch.optim.Optimizer):
         return {**super().__getstate__(), "states": self.states, "seed": self.seed, "max_norm": self.max_norm,
                 "capturable": self.capturable, "grad_norm": None, "_lists": {}}
 
+    def _steps_taken(self, group, states):
+        """The number of steps that a saved group's weights have taken, from its counter or their states; None where it
+        has no states, or where each state keeps its own."""
+        if group.get("clock") is not None:
+            return int(group["clock"])
+        numbers = {states[i]["step"] for i in group["params"] if states.get(i)}
+        if not self.capturable or not numbers:
+            return None
+        if len(numbers) > 1:
+            raise ValueError(f"AdamW: weights of a group that have taken different numbers of steps, {sorted(numbers)}: a "
+                             f"capturable optimizer counts one number for a group")
+        return numbers.pop()
+
     def load_state_dict(self, state_dict):
         if any(s and ("m_scale" in s) != (self.states == "e4m3") for s in state_dict["state"].values()):
             raise ValueError(f"a state of another kind than {self.states}")
+        taken = [self._steps_taken(group, state_dict["state"]) for group in state_dict["param_groups"]]
         super().load_state_dict(state_dict)
         self._lists = {}
+        for group, number in zip(self.param_groups, taken):
+            group.pop("clock", None)
+            if self.capturable and number is not None:
+                group["clock"] = torch.full((1,), number, dtype=torch.int64, device=group["params"][0].device)
+            for p in group["params"]:
+                if number is not None and self.state.get(p):
+                    self.state[p]["step"] = 0 if self.capturable else number
         for state in self.state.values():
             if "m_scale" in state:             # (loading casts to the weights' type, which holds the codes exactly)
                 for name in ("m", "v"):
