@@ -546,6 +546,11 @@ class AdamW(torch.optim.Optimizer):
     def load_state_dict(self, state_dict):
         if any(s and ("m_scale" in s) != (self.states == "e4m3") for s in state_dict["state"].values()):
             raise ValueError(f"a state of another kind than {self.states}")
+        needed = ("step", "m", "v") if self.states == "f32" else ("step", "m", "v", "m_scale", "v_scale", "strides")
+        for state in state_dict["state"].values():
+            missing = [name for name in needed if state and name not in state]
+            if missing:
+                raise ValueError(f"AdamW: a state without {', '.join(missing)}: it has {', '.join(map(str, state))}")
         taken = [self._steps_taken(group, state_dict["state"]) for group in state_dict["param_groups"]]
         super().load_state_dict(state_dict)
         self._lists = {}

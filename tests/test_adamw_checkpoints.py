@@ -132,3 +132,27 @@ def test_a_counter_elsewhere_is_refused():
         step()
     assert clocks(opt) == [1, 1]
     assert all(torch.equal(p, q) for p, q in zip(before, [p for g in opt.param_groups for p in g["params"]]))
+
+
+# ----------------------------------------------------------------------------- what is refused
+
+@pytest.mark.parametrize("states", ["f32", "e4m3"])
+def test_states_of_another_optimizer(states):
+    p = torch.nn.Parameter(gen(30, 7))
+    p.grad = torch.ones_like(p)
+    other = torch.optim.AdamW([p])
+    other.step()
+    opt = blocks.AdamW([p], states=states)
+    with pytest.raises(ValueError, match="state"):
+        opt.load_state_dict(other.state_dict())
+    assert not opt.state.get(p)
+    # and a part of one of its own
+    whole = with_states(blocks.AdamW([p]), [[3]]).state_dict()
+    for missing in ("step", "m", "v"):
+        part = copy.deepcopy(whole)
+        del part["state"][0][missing]
+        opt = blocks.AdamW([p])
+        with pytest.raises(ValueError, match=missing):
+            opt.load_state_dict(part)
+        assert not opt.state.get(p)
+    blocks.AdamW([p]).load_state_dict(whole)
