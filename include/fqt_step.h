@@ -118,7 +118,7 @@ int fqt_grad_norm(const fqt_param *params, int32_t count, float max_norm, float 
  * ((first + i) / 4 (64 bits, 3 << 30 in the upper word), 0, t modulo 2^32): word (first + i) % 4 belongs to element i, its lower
  * 16 bits to m, the upper to v. */
 typedef struct {
-  double lr, beta1, beta2, eps, weight_decay;   /* finite; lr, eps, weight_decay >= 0, 0 <= beta < 1 */
+  double lr, beta1, beta2, eps, weight_decay;   /* lr, eps, weight_decay and lr weight_decay 0 ... 1e30, 0 <= beta < 1 */
   uint64_t seed;
   int32_t state_dtype;                          /* FQT_F32 or FQT_E4M3                              */
 } fqt_adamw_cfg;

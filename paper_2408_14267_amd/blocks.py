@@ -357,6 +357,9 @@ def _same_order(p, strides):
                                all(a == b or n == 1 for a, b, n in zip(have, strides, p.shape)))
 
 
+_MOST = 1e30                   # of the settings of fqt_adamw_step, and of lr * weight_decay
+
+
 class AdamW(torch.optim.Optimizer):
     """AdamW for float32 weights of any shape, all tensors of a group in one fqt_adamw_step.  states: "f32", or "e4m3"
     for 8-bit states, stochastically rounded with the random sequence of `seed` (2 bytes a weight instead of 8).
@@ -394,8 +397,8 @@ class AdamW(torch.optim.Optimizer):
 
     def _config(self, group):
         lr, (beta1, beta2), eps, decay = group["lr"], group["betas"], group["eps"], group["weight_decay"]
-        if not (0 <= lr < math.inf and 0 <= beta1 < 1 and 0 <= beta2 < 1 and 0 <= eps < math.inf and
-                0 <= decay < math.inf):
+        if not (0 <= lr <= _MOST and 0 <= beta1 < 1 and 0 <= beta2 < 1 and 0 <= eps <= _MOST and 0 <= decay <= _MOST and
+                lr * decay <= _MOST):
             raise ValueError(f"lr {lr}, betas {group['betas']}, eps {eps}, weight_decay {decay}: out of range")
         return step.adamw_cfg(lr=lr, beta1=beta1, beta2=beta2, eps=eps, weight_decay=decay, seed=self.seed,
                               states=self.states)

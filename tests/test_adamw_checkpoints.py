@@ -156,3 +156,32 @@ def test_states_of_another_optimizer(states):
             opt.load_state_dict(part)
         assert not opt.state.get(p)
     blocks.AdamW([p]).load_state_dict(whole)
+
+
+@pytest.mark.parametrize("kw", [dict(lr=2e30), dict(eps=2e30), dict(weight_decay=2e30), dict(lr=1e20, weight_decay=1e20)])
+def test_settings_that_a_step_refuses(kw):
+    """What fqt_adamw_step takes no value of is refused with its group, not in a step whose other groups are updated."""
+    a, b = (torch.nn.Parameter(gen(5)) for _ in range(2))
+    opt = blocks.AdamW([a])
+    with pytest.raises(ValueError, match="out of range"):
+        opt.add_param_group(dict(params=[b], **kw))
+    assert len(opt.param_groups) == 1
+    opt.add_param_group(dict(params=[b], lr=1e30))
+
+
+@pytest.mark.gpu
+def test_settings_changed_between_steps():
+    opt = blocks.AdamW(groups("cuda"))
+
+    def step():
+        for group in opt.param_groups:
+            for p in group["params"]:
+                p.grad = torch.ones_like(p)
+        opt.step()
+    step()
+    opt.param_groups[1]["lr"] = 1e31
+    before = [p.detach().clone() for g in opt.param_groups for p in g["params"]]
+    with pytest.raises(ValueError, match="out of range"):
+        step()
+    assert numbers(opt) == [[1, 1], [1]]
+    assert all(torch.equal(p, q) for p, q in zip(before, [p for g in opt.param_groups for p in g["params"]]))
