@@ -342,6 +342,8 @@ class Muon(torch.optim.Optimizer):
 
 def _flat(t):
     """The elements of t in memory order, or None where they have gaps or overlap."""
+    if t.numel() == 0:
+        return t.detach().reshape(-1)
     expected = 1
     for stride, size in sorted((s, n) for s, n in zip(t.stride(), t.shape) if n != 1):
         if stride != expected:

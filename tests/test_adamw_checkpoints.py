@@ -185,3 +185,10 @@ def test_settings_changed_between_steps():
         step()
     assert numbers(opt) == [[1, 1], [1]]
     assert all(torch.equal(p, q) for p, q in zip(before, [p for g in opt.param_groups for p in g["params"]]))
+
+
+@pytest.mark.parametrize("shape", [(0,), (5, 0), (0, 5), (3, 0, 2)])
+def test_empty_weights(shape):
+    """A weight of no elements has no gaps, whatever its strides."""
+    opt = blocks.AdamW([torch.nn.Parameter(torch.zeros(shape))])
+    assert len(opt.param_groups[0]["params"]) == 1
