@@ -448,11 +448,14 @@ class AdamW(torch.optim.Optimizer):
 
     def _gradient(self, p, g, device):
         """g, the gradient of p, its elements in p's memory order.  device: the current one."""
-        if g.layout is not torch.strided or g.dtype not in (_F32, _BF16) or p.get_device() != device:
-            raise ValueError(f"AdamW updates weights with dense float32 or bfloat16 gradients on the current device, got "
-                             f"{g.layout} {g.dtype} on {p.device}")
+        if (g.layout is not torch.strided or g.dtype not in (_F32, _BF16) or p.dtype is not _F32 or
+                p.get_device() != device):
+            raise ValueError(f"AdamW updates float32 weights with dense float32 or bfloat16 gradients on the current device, "
+                             f"got {p.dtype} with {g.layout} {g.dtype} on {p.device}")
         if g.is_contiguous() and p.is_contiguous():
             return g
+        if _flat(p) is None:
+            raise ValueError(f"AdamW updates weights without gaps, got {tuple(p.shape)}, strides {p.stride()}")
         if g.stride() != p.stride():
             g = torch.empty_like(p, dtype=g.dtype).copy_(g)
         return g if g.is_contiguous() else _flat(g)

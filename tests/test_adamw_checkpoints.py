@@ -192,3 +192,30 @@ def test_empty_weights(shape):
     """A weight of no elements has no gaps, whatever its strides."""
     opt = blocks.AdamW([torch.nn.Parameter(torch.zeros(shape))])
     assert len(opt.param_groups[0]["params"]) == 1
+
+
+@pytest.mark.gpu
+@pytest.mark.parametrize("states", ["f32", "e4m3"])
+@pytest.mark.parametrize("change", ["gaps", "bf16"])
+@pytest.mark.parametrize("first", [True, False])
+def test_weights_that_changed(states, change, first):
+    """A weight that can no longer be updated is refused before a state is made or another weight is updated."""
+    q, p = (torch.nn.Parameter(gen(*s, device="cuda")) for s in ((7,), (40, 6)))
+    opt = blocks.AdamW([dict(params=[q]), dict(params=[p])], states=states)
+
+    def step():
+        for t in (p, q):
+            t.grad = torch.ones_like(t)
+        opt.step()
+    if not first:
+        step()
+    good = p.data
+    p.data = torch.zeros(40, 12, device="cuda")[:, :6] if change == "gaps" else good.bfloat16()
+    before = q.detach().clone()
+    with pytest.raises(ValueError, match="AdamW"):
+        step()
+    assert torch.equal(q, before)
+    assert [opt.state[t]["step"] for t in (p, q) if opt.state.get(t)] == ([] if first else [1, 1])
+    p.grad, p.data = None, good
+    step()
+    assert torch.isfinite(p).all() and not torch.equal(q, before)
