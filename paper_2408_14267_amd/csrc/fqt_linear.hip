@@ -328,7 +328,7 @@ struct FewArgs {
   const void *x, *w;
   int64_t K, ldx, ldw;
 };
-constexpr int FEW_MOST = 4, FEW_WIDE = 2560, FEW_THREADS = 256;
+constexpr int FEW_WIDE = 2560, FEW_THREADS = 256;
 // M: rows of x, or more (those past the last read it again and store nothing).
 template <typename T, int M, int R>
 __global__ void __launch_bounds__(FEW_THREADS) k_few_rows(FewArgs a, Epilogue e) {

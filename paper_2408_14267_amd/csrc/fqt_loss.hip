@@ -748,10 +748,6 @@ int check_pointers(const fqt_loss_desc &d, const Sizes &s, const void *x, const 
   return FQT_OK;
 }
 
-// Up to this many rows z is a product on the vector units, written to the workspace: its bytes are few beside
-// those of w.
-constexpr int64_t FEW_ROWS = 4;
-
 // us a step and before and after the steps of widened codes (as tile::STEP_COSTS).
 constexpr tile::Costs WIDE_COSTS{{2.5}, {1.1, 1.6}, {0.35, 0.55, 0.85}, {6, 5, 4}};
 
@@ -766,7 +762,8 @@ tile::Plan plan_z(int32_t dtype, bool direct, int64_t M, int64_t n, int64_t K) {
 struct FwdWs { size_t x, w, part, pairs, sums, at, total; int64_t pitch, e, slots; tile::Plan plan; bool few, copy_x, copy_w; };
 FwdWs fwd_ws(const fqt_loss_desc &d, const Sizes &s) {
   FwdWs f{};
-  f.few = s.M <= FEW_ROWS;
+  // z of few rows is written to the workspace by fqt_linear_forward: its bytes are few beside those of w
+  f.few = s.M <= FEW_MOST;
   auto pairs = [&](size_t from, int64_t slots) {
     f.slots = slots;
     f.pairs = from;

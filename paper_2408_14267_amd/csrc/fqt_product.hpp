@@ -10,6 +10,9 @@ namespace dense {
 // Plan of a product of operands of e bytes, and the bytes of its partial sums.
 tile::Plan plan_of(int64_t M, int64_t N, int64_t K, size_t e, const tile::Costs &costs = tile::DENSE_COSTS);
 size_t part_bytes(const tile::Plan &p, int64_t M, int64_t N);
+// Up to this many rows fqt_linear_forward is a product on the vector units, one launch that takes no workspace (callers keep other
+// things there).
+constexpr int FEW_MOST = 4;
 inline int64_t round_up(int64_t v, int64_t q) { return (v + q - 1) / q * q; }
 // Whether rows of n elements of e bytes, ld apart, are whole 16-byte pieces.
 inline bool whole_pieces(int64_t n, int64_t ld, size_t e) { return n * e % 16 == 0 && ld * e % 16 == 0; }
