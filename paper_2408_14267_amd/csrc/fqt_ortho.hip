@@ -375,8 +375,8 @@ __device__ __forceinline__ void small_product(const char *x, const char *w, uint
 #pragma unroll
   for (int s = 0; s < 2; ++s) {
     tile::i32x4 fx[2][2], fw[2][2];
-    rx.template read<true>(x + s * PANEL, 0, fx);
-    rw.template read<true>(w + s * PANEL, 0, fw);
+    rx.read(x + s * PANEL, 0, fx);
+    rw.read(w + s * PANEL, 0, fw);
 #pragma unroll
     for (int i = 0; i < 2; ++i)
 #pragma unroll

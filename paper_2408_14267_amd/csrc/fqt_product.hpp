@@ -36,8 +36,8 @@ Together plan_together(int64_t M, int64_t N, int64_t K, const tile::Plan &dx, co
 size_t part_bytes(const Together &t, int64_t M, int64_t N, int64_t K);
 
 // dx = dz w + add and dw = dz^T x, each computed where its pointer is given.  dzx and dzw: dz as it goes into
-// either, rows of M; w and x: operands along the features, their `rows` features.  add: float32 with
-// dx's stride, may be dx itself; null for none.
+// either, rows of M; w and x: operands along the features, their `rows` features.  add: float32 of row stride
+// ldadd, may be dx itself; null for none.
 struct Gradients {
   int64_t M, N, K;
   tile::Operand dzx, dzw, w, x;

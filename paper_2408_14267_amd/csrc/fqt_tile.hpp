@@ -37,8 +37,6 @@ enum Layout { ROWS, COLS, PANEL_ROWS, PANEL_COLS };
 typedef float f32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x4 __attribute__((ext_vector_type(4)));
 typedef int i32x8 __attribute__((ext_vector_type(8)));
-typedef short i16x4 __attribute__((ext_vector_type(4)));
-typedef short i16x8 __attribute__((ext_vector_type(8)));
 typedef __bf16 bf16x8 __attribute__((ext_vector_type(8)));
 typedef _Float16 f16x8 __attribute__((ext_vector_type(8)));
 
@@ -179,12 +177,8 @@ struct Loader {
   }
 };
 
-__device__ __forceinline__ i16x4 read_tr(const char *p) {
-  typedef __attribute__((address_space(3))) i16x4 lds_v4;
-  return __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_v4 *)(uint32_t)(uintptr_t)p);
-}
 // Two fragments of a COLS operand by transposing reads, from the lane's addresses a and b, as one block
-// of assembly with its own wait.  For the builtin the compiler waits until every load to LDS in flight
+// of assembly with its own wait.  For its own reads of this kind the compiler waits until every load to LDS in flight
 // has arrived, though those fill other buffers; where one tile's step has to hide the next one's loads
 // (run_tile) that costs more than the closer wait: 128 x 128 tiles of 8192 x 8192 x 4096 in 501 instead
 // of 566 us.
@@ -270,11 +264,11 @@ struct Reader {
   }
   // Fragments i ... i + 3, COLS ones with their own wait.
   __device__ __forceinline__ void read4(const char *lds, int i, i32x4 (&o)[4][2]) const {
-    if constexpr (by_rows(LAYOUT)) read<false>(lds, i, o);
+    if constexpr (by_rows(LAYOUT)) read(lds, i, o);
     else read_cols4<LINES>(lds, at + i, o);
   }
-  // Fragments i ... i + N - 1.  WHOLE: COLS fragments come with their own wait (read_cols).
-  template <bool WHOLE, int N>
+  // Fragments i ... i + N - 1, COLS ones in pairs with their own wait.
+  template <int N>
   __device__ __forceinline__ void read(const char *lds, int i, i32x4 (&o)[N][2]) const {
     if constexpr (by_rows(LAYOUT)) {
 #pragma unroll
@@ -282,15 +276,6 @@ struct Reader {
 #pragma unroll
         for (int s = 0; s < 2; ++s)
           o[j][s] = *reinterpret_cast<const i32x4 *>(lds + at[s] + (i + j) * 16 * KB);
-    } else if constexpr (!WHOLE) {
-#pragma unroll
-      for (int j = 0; j < N; ++j)
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const char *p = lds + at[i + j] + s * 32 * LINES * 2;
-          const i16x8 c = __builtin_shufflevector(read_tr(p), read_tr(p + 4 * LINES * 2), 0, 1, 2, 3, 4, 5, 6, 7);
-          o[j][s] = __builtin_bit_cast(i32x4, c);
-        }
     } else {
       static_assert(N % 2 == 0, "fragments in pairs");
 #pragma unroll
@@ -314,13 +299,10 @@ struct Feed {
     left = K - t0 * STEP;
     todo = t1 - t0;
   }
-  template <int FROM = 0, int TO = L::PER>
   __device__ __forceinline__ void load(char *lds) {
-    g.template load<FROM, TO>(lds, todo > 0 ? left * UNIT : 0);
-    if constexpr (TO == L::PER) {
-      --todo;
-      left -= STEP;
-    }
+    g.template load<0, L::PER>(lds, todo > 0 ? left * UNIT : 0);
+    --todo;
+    left -= STEP;
   }
 };
 
@@ -394,12 +376,12 @@ __device__ __forceinline__ void run_tile(const Operand &x, const Operand &w, int
     gx.load(to);
     gw.load(to + S::BM * KB);
     i32x4 fw[S::FN][2];
-    rw.template read<true>(at + S::BM * KB, 0, fw);
+    rw.read(at + S::BM * KB, 0, fw);
     constexpr int XS = by_rows(LX) ? 1 : 2;                // x fragments read at a time
 #pragma unroll
     for (int k = 0; k < S::FM; k += XS) {
       i32x4 fx[XS][2];
-      rx.template read<true>(at, k, fx);
+      rx.read(at, k, fx);
 #pragma unroll
       for (int i = 0; i < XS; ++i)
 #pragma unroll
