@@ -46,7 +46,8 @@ int fqt_loss_forward(const fqt_loss_desc *desc, const void *x, const void *w, co
                      const float *w_scale, const float *bias, const int64_t *target, float *loss,
                      float *lse, float *mean, void *ws, size_t ws_bytes, void *hip_stream);
 
-/* Gradients, with z computed again in pieces of the classes:
+/* Gradients, with z computed again in pieces of the classes (dz of a piece lies in the workspace in bf16, twice for the 8-bit
+ * types: about 256 MB, or 4096 classes of all rows where that is more; up to 5120 classes are one piece):
  *   dz[m][n] = c[m] (exp(z[m][n] - lse[m]) - (1 - smoothing) [n = target[m]] - smoothing / N)
  *   dx[m][k] = sum over n of dz[m][n] w_scale[n] w[n][k]
  *   dw[n][k] = sum over m of dz[m][n] x_scale[m] x[m][k]   (the gradient of w_scale[n] w[n][k])

@@ -788,7 +788,10 @@ FwdWs fwd_ws(const fqt_loss_desc &d, const Sizes &s) {
   return f;
 }
 
-// The classes of a piece of the backward: dz in bf16 of a piece takes about PIECE_BYTES.
+// The classes of a piece of the backward: dz in bf16 of a piece takes about PIECE_BYTES, but a piece has PIECE_LEAST
+// classes at least, up to a quarter more where these are all: past 32768 rows (16384 of codes, which have dz twice) dz grows with the
+// rows, 131072 x 65536 takes 1.1 GB (2.2 GB of codes).  (Each
+// piece reads and writes a float32 dx, 8 M K bytes, beside the 4 M n of its dz.)
 constexpr int64_t PIECE_BYTES = int64_t(256) << 20, PIECE_LEAST = 4096;
 int64_t piece_of(const Sizes &s) {
   const int64_t most = std::max(PIECE_LEAST, PIECE_BYTES / std::max<int64_t>(1, s.M * (s.codes ? 4 : 2)));

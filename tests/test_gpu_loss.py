@@ -496,3 +496,49 @@ def test_on_another_stream():
         got = forward(o, M, N, K, "bf16")
     side.synchronize()
     assert all(torch.equal(a, b) for a, b in zip(want, got))
+
+
+@pytest.mark.parametrize("smoothing", [0.0, 0.1])
+def test_slopes_along_the_gradients(smoothing):
+    """The slope of the float64 loss along the sign of each gradient by itself, where it is the sum of the gradient's magnitudes:
+    dx and dw are off by 2^-8 of the magnitudes of their terms, dbias by its own float32."""
+    M, N, K = 60, 90, 40
+    o = make(M, N, K, "bf16", seed=25)
+    z, lse64, _, counted, zerr, _ = reference(o, smoothing)
+    got = backward(o, M, N, K, "bf16", lse64.float(), dloss=torch.ones(M, device="cuda"), smoothing=smoothing, dx_dtype="f32",
+                   dw_dtype="f32")
+    got = {k: v.double() for k, v in got.items()}
+    p = torch.exp(z - lse64[:, None])
+    q = torch.full_like(z, smoothing / N).scatter_add_(1, o["target"].clamp(min=0)[:, None],
+                                                       torch.full_like(z[:, :1], 1 - smoothing))
+    dz = (p + q) * counted[:, None]                         # at least the magnitudes
+    off = {"dx": HALF * (dz @ o["w64"].abs()).sum(), "dw": HALF * (dz.t().contiguous() @ o["x64"].abs()).sum(), "dbias": 0.0}
+    small = (600 * U + 4 * zerr.max() + (M + N) * U) * dz.sum() * (1 + o["x64"].abs().max() * K + o["w64"].abs().max() * K)
+    h = 1e-4
+    for name, key in (("dx", "x64"), ("dw", "w64"), ("dbias", "bias")):
+        way = got[name].sign()
+
+        def total(step):
+            return reference(dict(o, **{key: o[key].double() + step * way}), smoothing)[2].sum()
+
+        slope = (total(h) - total(-h)).item() / (2 * h)
+        # (the difference itself: squares of h times the change of z, at most 1e-2, relative to the slope)
+        bound = 2 * off[name] + (small if name != "dbias" else (600 * U + 4 * zerr.max() + M * U) * dz.sum()) + 1e-4 * slope
+        assert slope > 0 and abs(got[name].abs().sum().item() - slope) <= bound, name
+        assert bound < 0.1 * slope, name                    # that the bound says something
+
+
+@pytest.mark.parametrize("M,N", [(2, 131072), (40, 131072), (600, 3000), (1500, 30011), (300, 700)])
+@pytest.mark.parametrize("kind", ["bf16", "int8"])
+def test_smoothed_sums_over_many_classes(M, N, kind):
+    """The mean of z, all of it on one side of 0: at most N / 1024 + 160 additions one after the other, each off by u of the
+    sum, and the roundings of z in units of log 2."""
+    K = 16
+    o = make(M, N, K, kind, seed=26, integers=True, ignored=0.0)
+    o["bias"] = o["bias"] + 9.0
+    loss, _, _ = forward(o, M, N, K, kind, 0.5)
+    z, _, loss64, _, _, tail = reference(o, 0.5)
+    big = z.abs().amax(dim=1)
+    lim = 520 * U * tail + 8 * U * loss64.abs() + 0.5 * (N / 1024 + 160 + 16) * U * big
+    err = (loss.double() - loss64).abs()
+    assert (err <= lim).all(), f"loss off by {(err / lim).max().item():.3g} of the bound"

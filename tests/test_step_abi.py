@@ -113,6 +113,18 @@ def test_loss_workspace_stays_below_the_outputs():
     assert step.fqt_loss_workspace_size(d, True) < 16384 * (1 << 20) // 16
 
 
+@pytest.mark.parametrize("M", [131072, 1 << 20])
+@pytest.mark.parametrize("kind,codes", [("bf16", 1), ("int8", 2)])
+def test_loss_workspace_of_many_rows(M, kind, codes):
+    """dz of a piece has 4096 classes at least (up to 5120 where that is all of them), so of many rows it takes more than 256 MB;
+    what else there is: copies and a float32 dx, sums of dbias, a float32 a row."""
+    for N, K in ((32768, 512), (65536, 512), (1 << 18, 64), (5120, 512), (4096, 64), (1000, 512)):
+        most = 5120 if N <= 5120 else 4096 + 256
+        rest = M * K * 8 + most * K * 2 + M * 4 + (M // 32 + 1) * most * 4 + (1 << 28)
+        size = step.fqt_loss_workspace_size(step.loss_desc(M, N, K, x_dtype=kind), True)
+        assert size <= M * (min(N, most) + 128) * 2 * codes + rest
+
+
 def test_loss_binding_checks():
     bf = torch.bfloat16
     d = step.loss_desc(4, 8, 16)
