@@ -619,7 +619,7 @@ class Optimizers:
 def muon_and_adam(model, lr=0.02, adam_lr=1e-3, first_last=(), states=None, max_norm=None):
     """Muon for the weight matrices of a model, Adam for its vectors and for the modules in first_last
     (input and output layers, whose singular values carry meaning).  states: None for torch's Adam, "f32" or "e4m3" for
-    AdamW here, with max_norm."""
+    AdamW here, with max_norm (over the gradients that it takes: Muon's update does not go by the size of its own)."""
     if states is None and max_norm is not None:
         raise ValueError("max_norm comes with states")
     apart = {id(p) for m in first_last for p in m.parameters()}
