@@ -210,3 +210,74 @@ def test_gradients_of_a_layer(kind, reduction):
     # (every term by 1300 u and 16 u of |z| <= 81, and the sums)
     bound = (2600 + M) * U * dz.abs().sum(dim=0)
     assert ((mod.bias.grad.double() - dz.sum(dim=0)).abs() <= bound).all()
+
+
+# ----------------------------------------------------------------------------- rows and calls
+
+@pytest.mark.parametrize("kind", ["bf16", "int8", "e4m3"])
+def test_more_rows_than_a_launch_has_waves(kind):
+    M, N, K = 70001, 10, 40
+    o = make(M, N, K, kind, seed=3)
+    z, zerr = logits(o)
+    lse = torch.logsumexp(z, dim=1).float()
+    c = torch.randn(M, generator=torch.Generator(device="cuda").manual_seed(M), device="cuda") / 100
+    check(gradients(o, kind, lse, c, 0.0), o, z, zerr, lse.double(), c, 0.0)
+
+
+@pytest.mark.parametrize("M,N,K", [(6, 30, 100), (64, 1000, 2048), (300, 700, 96)])
+@pytest.mark.parametrize("kind", ["bf16", "int8", "e4m3"])
+def test_strided_rows(M, N, K, kind):
+    s = step()
+    o = make(M, N, K, kind, seed=4)
+    z, zerr = logits(o)
+    lse = torch.logsumexp(z, dim=1).float()
+    c = torch.randn(M, generator=torch.Generator(device="cuda").manual_seed(M), device="cuda")
+    want = gradients(o, kind, lse, c, 0.0)
+    for more in (3, 32):
+        wide = [torch.full((t.shape[0], K + more), 3.0, device="cuda").to(t.dtype) for t in (o["x"], o["w"])]
+        for t, v in zip(wide, (o["x"], o["w"])):
+            t[:, :K] = v
+        desc = s.loss_desc(M, N, K, x_dtype=kind, dx_dtype="f32", dw_dtype="f32", ignore=IGNORE, ldx=K + more, ldw=K + more)
+        out = {k: torch.empty_like(v) for k, v in want.items()}
+        s.fqt_loss_backward(desc, wide[0][:, :K], wide[1][:, :K], o["target"], lse, s.loss_workspace(desc, True), dloss=c,
+                            bias=o["bias"], x_scale=o["x_scale"], w_scale=o["w_scale"], **out)
+        check(out, o, z, zerr, lse.double(), c, 0.0)
+
+
+@pytest.mark.parametrize("M,N,K", [(2, 10, 64), (64, 1000, 2048), (700, 1500, 128)])
+def test_captured(M, N, K):
+    """Both ways to log p in one graph, replayed on other inputs between eager calls."""
+    s = step()
+    desc = s.loss_desc(M, N, K, dx_dtype="f32", dw_dtype="f32", ignore=IGNORE)
+    held = make(M, N, K, "bf16", seed=5)
+    loss, lse, logp, c = (torch.ones(M, device="cuda") for _ in range(4))
+    outs = [{"dx": torch.empty(M, K, device="cuda"), "dw": torch.empty(N, K, device="cuda"),
+             "dbias": torch.empty(N, device="cuda")} for _ in range(2)]
+    wf, wb = s.loss_workspace(desc), s.loss_workspace(desc, True)
+
+    def call():
+        s.fqt_loss_forward(desc, held["x"], held["w"], held["target"], loss, lse, wf, bias=held["bias"], logp=logp)
+        for out, given in zip(outs, (logp, None)):
+            s.fqt_loss_backward(desc, held["x"], held["w"], held["target"], lse, wb, dloss=c, bias=held["bias"], logp=given,
+                                **out)
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        call()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        call()
+    every = [logp] + [t for out in outs for t in out.values()]
+    for seed in (6, 7, 8):
+        o = make(M, N, K, "bf16", seed=seed)
+        for k in ("x", "w", "target", "bias"):
+            held[k].copy_(o[k])
+        call()
+        want = [t.clone() for t in every]
+        for t in every:
+            t.fill_(7)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip(want, every))
